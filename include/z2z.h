@@ -197,6 +197,30 @@ int z2z_codebook_prune(z2z_ctx* ctx, const int32_t* d_keep, int32_t* d_new_id, i
 int z2z_hyper_embed(z2z_ctx* ctx, const void* d_E, void* d_W_hyper, const int32_t* d_first,
                     int32_t max_new, void* stream);
 
+/* embed_codes.  The input rows of a compressed sequence (section 2.2: base embeddings and hyper-embeddings):
+ *   X[b, i, :] = scale * T[codes[b, i], :],  T = [E ; W_hyper[b]] over the columns that exist (V + C_b),  i < n_codes[b];
+ * the product in fp32, rounded once to the storage type (scale = 1: the row as it is).  A code that names no row gives a row of zeros
+ * and sets BAD_CODE for its sequence; the others are unaffected.  Rows at and behind n_codes[b] are left as they were.
+ *   d_codes [B, stride] int32, d_n_codes [B] or NULL (every row has `stride`);  scale finite (else Z2Z_EINVAL)
+ *   d_E [V, d], d_W_hyper [B, cap, d], d_X [B, stride, d] out: dtype of the context;  d_status [B] int32 out
+ * One code per sequence (stride 1) is the input of a generation step. */
+int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, const void* d_E,
+                    const void* d_W_hyper, float scale, void* d_X, int32_t* d_status, void* stream);
+
+/* Backward of z2z_embed_codes: every row of the joint table receives scale * the sum of dX over the positions that named it,
+ *   dE[v, :] = scale * sum_{b, i: codes[b, i] = v} dX[b, i, :],   dW_hyper[b, e, :] = scale * sum_{i: codes[b, i] = V + e} dX[b, i, :].
+ * Positions at and behind n_codes[b] and codes that name no row contribute nothing.  Sums are fp32 over the positions in a fixed order
+ * (sorted by row, no atomics): the same inputs give the same bits.
+ *   d_dX [B, stride, d] dtype of the context;  d_dE [V, d] float;  d_dW_hyper [B, cap, d] dtype of the context
+ *   flags  0: both gradients are overwritten, rows that no position names (and rows at and beyond C_b) with zeros;
+ *          Z2Z_GRAD_ADD: added to what is there (rows that no position names are not touched), one rounding per element
+ * With z2z_hyper_embed_backward behind it the gradient reaches E through the entries, too: that call adds to the same d_dE.
+ * B * stride and V + B * cap below 2^31, else Z2Z_EUNSUPPORTED.  Work space: 16 bytes per position and a quarter of dX's
+ * size (an eighth in fp32), library scratch. */
+#define Z2Z_GRAD_ADD 1
+int z2z_embed_codes_backward(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, float scale,
+                             const void* d_dX, int32_t flags, float* d_dE, void* d_dW_hyper, void* stream);
+
 /* hyper_encode: the learned hyper-encoder f_phi of section 2.2 (the attention and transformer rows of the
  * hyper-encoder ablation table; the training setup uses two transformer layers, M = 3).  The paper names the
  * architectures only; computed here is the standard pre-norm encoder over an entry's M padded slots:
@@ -330,6 +354,40 @@ int z2z_extended_sample(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t row
                         const void* d_W_base, const void* d_W_hyper, float temperature, int32_t top_k,
                         float top_p, uint64_t seed, uint64_t step, int32_t* d_token, float* d_logprob,
                         void* stream);
+
+/* extended_beam.  The generation step's pick for a beam search (section 2.3, steps 8-9, over several continuations of a prompt):
+ * sequences p * beams .. p * beams + beams - 1 of the context are the beams of prompt p, one hidden row each.  Of all
+ * continuations (beam r of the prompt, column v) the n_pick with the largest
+ *   d_score[row r] + logit[row r, v] - lse[row r]        (the beam's log-probability so far plus the column's; fp32)
+ * are picked, over the same columns as z2z_extended_logits, largest first, equal ones by lower beam, then lower column.  A
+ * continuation whose value is -inf, +inf or NaN is not picked: a beam with d_score = -inf is dead (at a prompt's first step all but
+ * one are), one whose hidden row holds a NaN is passed over.
+ *   d_score  [rows] float;  rows must be B, B a multiple of beams
+ *   d_parent [B / beams, n_pick] int32 out: the beam, 0 .. beams - 1, that is continued
+ *   d_code   [B / beams, n_pick] int32 out: by this base token or hypertoken (of the parent's codebook)
+ *   d_picked [B / beams, n_pick] float out: the value above, the new beam's score
+ *            (-1, -1 and -inf where fewer continuations are there)
+ * n_pick may be larger than beams: the caller takes out finished sequences first.  A step goes on with z2z_codebook_reorder,
+ * then z2z_step_update with the picked codes.
+ * beams <= Z2Z_MAX_BEAMS and n_pick <= Z2Z_MAX_PICK, else Z2Z_EUNSUPPORTED; any storage type and width.  The logits go
+ * through rows * (V + cap) floats of library scratch. */
+#define Z2Z_MAX_BEAMS 32
+#define Z2Z_MAX_PICK 64
+int z2z_extended_beam(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t beams, const void* d_W_base, const void* d_W_hyper,
+                      const float* d_score, int32_t n_pick, int32_t* d_parent, int32_t* d_code, float* d_picked,
+                      void* stream);
+
+/* codebook_reorder.  The beams' states follow the pick: afterwards sequence p * beams + k has the codebook, the pending phrase and the
+ * hyper-embedding cache rows that sequence p * beams + d_source[p * beams + k] had before, for all beams at once (a beam may be
+ * taken over by several and give up its own).  A source outside 0 .. beams - 1 leaves the sequence as it is, so d_parent of
+ * z2z_extended_beam serves with n_pick = beams.
+ *   d_source  [B] int32, beams within the prompt;  B a multiple of beams, beams <= Z2Z_MAX_BEAMS
+ *   d_W_hyper [B, cap, d] in place, or NULL: the codebooks alone.  The cache is taken to be current in all of a prompt's
+ *             sequences and to come from the same embeddings (z2z_hyper_embed or z2z_hyper_encode): an entry that spells the
+ *             same phrase at the same place in both has its vector already and is not copied.  Rows at and beyond C_b keep
+ *             what they hold.
+ * (Handing a prompt's codebook to all of its beams is a call with every source 0.) */
+int z2z_codebook_reorder(z2z_ctx* ctx, int32_t beams, const int32_t* d_source, void* d_W_hyper, void* stream);
 
 /* extended_nll.  The per-position term of the training objective over compressed sequences (section 2.4,
  * the next-token loss on z = LZW(y)): for hidden row r with target code t = d_targets[r],

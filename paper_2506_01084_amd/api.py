@@ -27,8 +27,10 @@ E_INVAL, E_NOMEM, E_HIP, E_UNSUPPORTED, E_LIMIT, E_CAPTURE = -1, -2, -3, -4, -5,
 STATIC_PARTS = 1 << 22
 
 ENC_KEPT = 1
+GRAD_ADD = 1
+MAX_BEAMS, MAX_PICK = 32, 64
 EXPORTS = ["z2z_create", "z2z_destroy", "z2z_reset", "z2z_lzw_encode", "z2z_lzw_decode", "z2z_step_update", "z2z_lzw_rounds", "z2z_codebook", "z2z_codebook_prefill", "z2z_codebook_usage", "z2z_codebook_prune",
-           "z2z_hyper_embed", "z2z_hyper_encode", "z2z_hyper_encode_backward", "z2z_hyper_encode_keep", "z2z_extended_logits", "z2z_extended_logits_static", "z2z_extended_sample", "z2z_extended_nll", "z2z_extended_nll_backward", "z2z_hyper_embed_backward", "z2z_set_option",
+           "z2z_hyper_embed", "z2z_embed_codes", "z2z_embed_codes_backward", "z2z_extended_beam", "z2z_codebook_reorder", "z2z_hyper_encode", "z2z_hyper_encode_backward", "z2z_hyper_encode_keep", "z2z_extended_logits", "z2z_extended_logits_static", "z2z_extended_sample", "z2z_extended_nll", "z2z_extended_nll_backward", "z2z_hyper_embed_backward", "z2z_set_option",
            "z2z_read_timing", "z2z_read_launches", "z2z_strerror"]
 
 
@@ -116,6 +118,12 @@ def load_library() -> ctypes.CDLL:
     lib.z2z_extended_nll_backward.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
                                               c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.z2z_hyper_embed_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.z2z_embed_codes.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p]
+    lib.z2z_embed_codes_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p,
+                                             c_void_p]
+    lib.z2z_extended_beam.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                                      c_void_p, c_void_p]
+    lib.z2z_codebook_reorder.argtypes = [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]
     lib.z2z_set_option.argtypes = [c_void_p, c_int32, c_int32]
     lib.z2z_read_timing.argtypes = [c_void_p, POINTER(c_float), P32]
     lib.z2z_read_launches.argtypes = [c_void_p, POINTER(ctypes.c_int64)]
@@ -276,6 +284,33 @@ class Context:
         _check(self._lib.z2z_hyper_embed(self._h, _ptr(E, self.torch_dtype), _ptr(W_hyper, self.torch_dtype),
                                          _ptr(first, torch.int32), max_new, _stream()), "z2z_hyper_embed")
 
+    def embed_codes(self, codes: torch.Tensor, n_codes: Optional[torch.Tensor], E: torch.Tensor, W_hyper: torch.Tensor,
+                    X: torch.Tensor, status: torch.Tensor, scale: float = 1.0) -> None:
+        """X[b, i] = scale * (row of E or W_hyper[b] that codes[b, i] names); rows behind n_codes[b] are left as they were."""
+        assert codes.dim() == 2 and codes.shape[0] == self.B and tuple(X.shape) == (*codes.shape, self.d)
+        assert tuple(E.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
+        assert (n_codes is None or n_codes.numel() == self.B) and status.numel() == self.B
+        _check(self._lib.z2z_embed_codes(self._h, _ptr(codes, torch.int32), _ptr(n_codes, torch.int32), codes.shape[1],
+                                         _ptr(E, self.torch_dtype), _ptr(W_hyper, self.torch_dtype), float(scale),
+                                         _ptr(X, self.torch_dtype), _ptr(status, torch.int32), _stream()), "z2z_embed_codes")
+
+    def embed_codes_backward(self, codes: torch.Tensor, n_codes: Optional[torch.Tensor], dX: torch.Tensor, dE: torch.Tensor,
+                             dW_hyper: torch.Tensor, scale: float = 1.0, add: bool = False) -> None:
+        """The gradients of embed_codes, overwritten or (add=True) added to what is there."""
+        assert codes.dim() == 2 and codes.shape[0] == self.B and tuple(dX.shape) == (*codes.shape, self.d)
+        assert tuple(dE.shape) == (self.V, self.d) and tuple(dW_hyper.shape) == (self.B, self.cap, self.d)
+        assert n_codes is None or n_codes.numel() == self.B
+        _check(self._lib.z2z_embed_codes_backward(self._h, _ptr(codes, torch.int32), _ptr(n_codes, torch.int32), codes.shape[1],
+                                                  float(scale), _ptr(dX, self.torch_dtype), GRAD_ADD if add else 0,
+                                                  _ptr(dE, torch.float32), _ptr(dW_hyper, self.torch_dtype), _stream()),
+               "z2z_embed_codes_backward")
+
+    def codebook_reorder(self, beams: int, source: torch.Tensor, W_hyper: Optional[torch.Tensor] = None) -> None:
+        """Sequence p * beams + k takes over the state of sequence p * beams + source[p * beams + k] (in place, cache rows too)."""
+        assert source.numel() == self.B and (W_hyper is None or tuple(W_hyper.shape) == (self.B, self.cap, self.d))
+        _check(self._lib.z2z_codebook_reorder(self._h, int(beams), _ptr(source, torch.int32), _ptr(W_hyper, self.torch_dtype),
+                                              _stream()), "z2z_codebook_reorder")
+
     def hyper_encode(self, E: torch.Tensor, encoder: "Encoder", W_hyper: torch.Tensor,
                      first: Optional[torch.Tensor] = None, max_new: int = 0) -> None:
         assert tuple(E.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
@@ -333,6 +368,19 @@ class Context:
                                              float(temperature), int(top_k), float(top_p), int(seed), int(step),
                                              _ptr(token, torch.int32),
                                              _ptr(logprob, torch.float32), _stream()), "z2z_extended_sample")
+
+    def extended_beam(self, H: torch.Tensor, beams: int, W_base: torch.Tensor, W_hyper: torch.Tensor, score: torch.Tensor,
+                      parent: torch.Tensor, code: torch.Tensor, picked: torch.Tensor) -> None:
+        """The best continuations of every prompt's beams; parent, code and picked are [B / beams, n_pick]."""
+        rows = H.shape[0]
+        assert H.shape[1] == self.d and tuple(W_base.shape) == (self.V, self.d)
+        assert tuple(W_hyper.shape) == (self.B, self.cap, self.d) and score.numel() == rows
+        assert beams >= 1 and parent.dim() == 2 and parent.shape[0] * beams == rows
+        assert tuple(code.shape) == tuple(parent.shape) and tuple(picked.shape) == tuple(parent.shape)
+        _check(self._lib.z2z_extended_beam(self._h, _ptr(H, self.torch_dtype), rows, int(beams), _ptr(W_base, self.torch_dtype),
+                                           _ptr(W_hyper, self.torch_dtype), _ptr(score, torch.float32), parent.shape[1],
+                                           _ptr(parent, torch.int32), _ptr(code, torch.int32), _ptr(picked, torch.float32),
+                                           _stream()), "z2z_extended_beam")
 
     def extended_nll(self, H: torch.Tensor, rows_per_seq: int, W_base: torch.Tensor, W_hyper: torch.Tensor,
                      targets: torch.Tensor, nll: torch.Tensor, lse: torch.Tensor) -> None:

@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(const float* partial, i
 int ensure_partial(z2z_ctx* c, size_t need, hipStream_t s) {
   if (need <= c->skinny_partial_bytes) return Z2Z_OK;
   Z2Z_TRY_GROW(s);
-  if (c->skinny_partial) (void)hipFree(c->skinny_partial);
+  z2z_release(c, c->skinny_partial);
   c->skinny_partial = nullptr;
   c->skinny_partial_bytes = 0;
   const size_t want = need > ((size_t)64 << 20) ? need : ((size_t)64 << 20);

@@ -1,0 +1,571 @@
+// The input side of a model over the extended vocabulary (gfx950): the lookup of a batch of code streams in the joint
+// table [E ; W_hyper[b]], and its gradient.
+//
+// Section 2.2 of the zip2zip paper embeds a compressed sequence through the base embeddings and the hyper-embeddings of
+// the sequence's own codebook.  X[b, i, :] = scale * (c < V ? E[c, :] : W_hyper[b, c - V, :]), c = codes[b, i], is a gather;
+// its transpose adds dX[b, i, :] to the row that position named.
+#include "hyper_embed_common.h"
+
+#include <string.h>
+
+#include <algorithm>
+
+namespace {
+
+using z2z_embed::u32x4;
+
+constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+
+struct LookupArgs {
+  const int32_t* codes;     // [B, stride]
+  const int32_t* n_codes;   // [B] or nullptr: stride
+  const int32_t* size;      // [B] C_b
+  int32_t B, V, cap, stride, chunks;   // chunks: 16-byte pieces of a row
+  uint32_t sentinel;        // V + B * cap: what a position that names no row sorts by
+};
+
+__device__ __forceinline__ int codes_of(const LookupArgs& a, int b) {
+  return a.n_codes ? min(max(a.n_codes[b], 0), a.stride) : a.stride;
+}
+
+__device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+__device__ __forceinline__ uint32_t pack_two(float a, float b) {
+  typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, z2z_embed::bf16x2));
+}
+
+// One 16-byte piece times scale: the product in fp32, rounded once to the storage type.
+template <bool BF16>
+__device__ __forceinline__ u32x4 scaled(u32x4 x, float scale) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    x[e] = BF16 ? pack_two(lo_bf16(x[e]) * scale, hi_bf16(x[e]) * scale) : __float_as_uint(__uint_as_float(x[e]) * scale);
+  return x;
+}
+
+// Blocks [0, B): the status of sequence b, all of its codes looked over.  The others: a wave per position and `split`-th of its
+// row.  Bound by HBM: the rows written and each named row read once (popular ones come out of the caches).
+template <bool BF16>
+__global__ void __launch_bounds__(256) embed_codes_kernel(LookupArgs a, const u32x4* E, const u32x4* W, u32x4* X, int32_t* status,
+                                                          float scale, int split) {
+  const int lane = threadIdx.x & 63;
+  if ((int)blockIdx.x < a.B) {
+    const int b = blockIdx.x, n = codes_of(a, b), columns = a.V + min(max(a.size[b], 0), a.cap);
+    const int32_t* c = a.codes + (size_t)b * a.stride;
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += 256) bad |= c[i] < 0 || c[i] >= columns;
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) status[b] = any ? Z2Z_ST_BAD_CODE : Z2Z_ST_OK;
+    return;
+  }
+  const long long wid = (long long)(blockIdx.x - a.B) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long pos = wid / split;
+  const int part = (int)(wid % split);
+  if (pos >= (long long)a.B * a.stride) return;
+  const int b = (int)(pos / a.stride), i = (int)(pos % a.stride);
+  if (i >= codes_of(a, b)) return;                   // rows behind a sequence's end stay as they were
+  const int c = a.codes[pos];
+  const bool base = c < a.V, named = c >= 0 && (base || c - a.V < min(max(a.size[b], 0), a.cap));
+  const u32x4* row = base ? E + (size_t)(named ? c : 0) * a.chunks : W + ((size_t)b * a.cap + (named ? c - a.V : 0)) * a.chunks;
+  u32x4* out = X + (size_t)pos * a.chunks;
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+  constexpr int U = 4;
+  for (int k0 = part * 64 + lane; k0 < a.chunks; k0 += U * 64 * split) {
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = named ? row[min(k0 + u * 64 * split, a.chunks - 1)] : zero;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u * 64 * split < a.chunks) out[k0 + u * 64 * split] = named ? scaled<BF16>(x[u], scale) : zero;
+  }
+}
+
+// ---- gradient: positions sorted by the row they name -------------------------------------------------------------------------
+// A row of the table collects the gradients of all its positions, in the order of the positions whatever the launch
+// does: no float atomics.  The positions are sorted by their key -- the token, or V + b * cap + entry -- with a stable
+// radix sort by digits of up to 10 bits, least significant first; equal keys then stand together in order of position.
+
+constexpr int S_TILE = 4096;              // items of a workgroup: 16 waves, each up to 4 rounds of 64 in a row
+constexpr int S_ROUNDS = S_TILE / 1024;
+constexpr int S_DIGITS = 1024;
+
+__device__ __forceinline__ uint32_t key_of(const LookupArgs& a, uint32_t i) {
+  const uint32_t b = i / (uint32_t)a.stride, j = i - b * (uint32_t)a.stride;
+  if ((int)j >= codes_of(a, (int)b)) return a.sentinel;
+  const int c = a.codes[i];
+  if (c < 0) return a.sentinel;
+  if (c < a.V) return (uint32_t)c;
+  return c - a.V < min(max(a.size[b], 0), a.cap) ? (uint32_t)a.V + b * (uint32_t)a.cap + (uint32_t)(c - a.V) : a.sentinel;
+}
+
+struct SortLds {
+  uint16_t cnt[16][S_DIGITS];             // per wave: how often a digit came so far, then where its next one goes
+  uint32_t wave_sum[16];
+};
+
+// Where every item of the tile goes among the tile's items: item (wave, round r, lane) is number wave * 64 * rounds + 64 r + lane.
+// Equal digits within a wave's 64 are found by ballots, one per bit; the lanes below count.  Behind the last item of a
+// tile stand dummies with all bits set: they stay behind every item, which are put in order before them.
+// Returns per item its place, and leaves in l.cnt[0][d] the place of the tile's first item with digit d.
+__device__ __forceinline__ void tile_places(SortLds& l, const uint32_t (&key)[S_ROUNDS], int rounds, int shift, int bits, uint32_t (&place)[S_ROUNDS]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t mask = (1u << bits) - 1u;
+  const int digits = 1 << bits;
+  for (int i = tid; i < 16 * S_DIGITS / 2; i += 1024) reinterpret_cast<uint32_t*>(l.cnt)[i] = 0u;
+  __syncthreads();
+  volatile uint16_t* mine = l.cnt[wave];
+  uint32_t rank[S_ROUNDS];
+#pragma unroll
+  for (int r = 0; r < S_ROUNDS; ++r) {
+    rank[r] = 0u;
+    if (r < rounds) {                     // (uniform)
+      const uint32_t digit = (key[r] >> shift) & mask;
+      uint64_t peers = ~0ull;
+      for (int k = 0; k < bits; ++k) {
+        const bool bit = (digit >> k) & 1u;
+        const uint64_t m = __ballot(bit);
+        peers &= bit ? m : ~m;
+      }
+      const uint32_t before = mine[digit];
+      const uint32_t below = (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
+      __builtin_amdgcn_wave_barrier();    // (a wave's LDS operations are carried out in order: all read before one writes)
+      if (below == 0u) mine[digit] = (uint16_t)(before + (uint32_t)__popcll(peers));
+      __builtin_amdgcn_wave_barrier();
+      rank[r] = before + below;
+    }
+  }
+  __syncthreads();
+  uint32_t total = 0u;
+  uint16_t of_wave[16];
+  if (tid < digits) {
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      of_wave[w] = (uint16_t)total;
+      total += l.cnt[w][tid];
+    }
+  }
+  uint32_t incl = total;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(incl, off);
+    if (lane >= off) incl += o;
+  }
+  if (lane == 63) l.wave_sum[wave] = incl;
+  __syncthreads();
+  uint32_t first = incl - total;
+  for (int w = 0; w < wave; ++w) first += l.wave_sum[w];
+  if (tid < digits) {
+#pragma unroll
+    for (int w = 0; w < 16; ++w) l.cnt[w][tid] = (uint16_t)(first + of_wave[w]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < S_ROUNDS; ++r)
+    if (r < rounds) place[r] = (uint32_t)l.cnt[wave][(key[r] >> shift) & mask] + rank[r];
+}
+
+// Up to S_TILE positions: the whole sort in one workgroup, from pass to pass through LDS.
+__global__ void __launch_bounds__(1024) sort_small_kernel(LookupArgs a, uint32_t n, int bits, int passes, uint32_t* skey, uint32_t* spos) {
+  __shared__ SortLds l;
+  __shared__ uint32_t xkey[S_TILE];
+  __shared__ uint16_t xpos[S_TILE];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rounds = (int)((n + 1023u) / 1024u);
+  uint32_t key[S_ROUNDS], pos[S_ROUNDS], place[S_ROUNDS];
+#pragma unroll
+  for (int r = 0; r < S_ROUNDS; ++r) {
+    const uint32_t i = (uint32_t)(wave * 64 * rounds + 64 * r + lane);
+    pos[r] = i;
+    key[r] = r < rounds && i < n ? key_of(a, i) : kNoKey;
+    place[r] = 0u;
+  }
+  for (int p = 0; p < passes; ++p) {
+    tile_places(l, key, rounds, p * bits, bits, place);
+#pragma unroll
+    for (int r = 0; r < S_ROUNDS; ++r)
+      if (r < rounds) {
+        xkey[place[r]] = key[r];
+        xpos[place[r]] = (uint16_t)pos[r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < S_ROUNDS; ++r)
+      if (r < rounds) {
+        const int i = wave * 64 * rounds + 64 * r + lane;
+        key[r] = xkey[i];
+        pos[r] = xpos[i];
+      }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < S_ROUNDS; ++r) {
+    const uint32_t i = (uint32_t)(wave * 64 * rounds + 64 * r + lane);
+    if (r < rounds && i < n) {
+      skey[i] = key[r];
+      spos[i] = pos[r];
+    }
+  }
+}
+
+// More: per pass, every tile counts its digits ...
+__global__ void __launch_bounds__(1024) sort_count_kernel(LookupArgs a, uint32_t n, const uint32_t* key_in, int shift, int bits, uint32_t* count) {
+  __shared__ uint32_t cnt[S_DIGITS];
+  const int digits = 1 << bits;
+  for (int i = threadIdx.x; i < digits; i += 1024) cnt[i] = 0u;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < S_ROUNDS; ++r) {
+    const uint32_t i = blockIdx.x * (uint32_t)S_TILE + 1024u * r + threadIdx.x;
+    if (i < n) atomicAdd(&cnt[((key_in ? key_in[i] : key_of(a, i)) >> shift) & (uint32_t)(digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < digits; i += 1024) count[(size_t)blockIdx.x * digits + i] = cnt[i];
+}
+
+// ... and puts its items behind those of smaller digits and of the same digit in the tiles before.
+__global__ void __launch_bounds__(1024) sort_place_kernel(LookupArgs a, uint32_t n, const uint32_t* key_in, const uint32_t* pos_in, int shift,
+                                                          int bits, const uint32_t* count, uint32_t* key_out, uint32_t* pos_out) {
+  __shared__ SortLds l;
+  __shared__ uint32_t go[S_DIGITS];       // where the tile's first item with the digit goes
+  __shared__ uint32_t sums[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int digits = 1 << bits, tiles = (int)gridDim.x;
+  const uint32_t t0 = blockIdx.x * (uint32_t)S_TILE;
+  uint32_t key[S_ROUNDS], pos[S_ROUNDS], place[S_ROUNDS];
+#pragma unroll
+  for (int r = 0; r < S_ROUNDS; ++r) {
+    const uint32_t i = t0 + (uint32_t)(wave * 64 * S_ROUNDS + 64 * r + lane);
+    const bool there = i < n;
+    key[r] = there ? (key_in ? key_in[i] : key_of(a, i)) : kNoKey;
+    pos[r] = there && pos_in ? pos_in[i] : i;
+    place[r] = 0u;
+  }
+  uint32_t total = 0u, before = 0u;
+  if (tid < digits)
+    for (int t = 0; t < tiles; ++t) {
+      const uint32_t x = count[(size_t)t * digits + tid];
+      total += x;
+      before += t < (int)blockIdx.x ? x : 0u;
+    }
+  uint32_t incl = total;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(incl, off);
+    if (lane >= off) incl += o;
+  }
+  if (lane == 63) sums[wave] = incl;
+  __syncthreads();
+  uint32_t first = incl - total;
+  for (int w = 0; w < wave; ++w) first += sums[w];
+  if (tid < digits) go[tid] = first + before;
+  tile_places(l, key, S_ROUNDS, shift, bits, place);       // (its barriers make `go` visible)
+#pragma unroll
+  for (int r = 0; r < S_ROUNDS; ++r) {
+    const uint32_t i = t0 + (uint32_t)(wave * 64 * S_ROUNDS + 64 * r + lane);
+    if (i < n) {
+      const uint32_t digit = (key[r] >> shift) & (uint32_t)(digits - 1);
+      const uint32_t to = go[digit] + (place[r] - (uint32_t)l.cnt[0][digit]);
+      key_out[to] = key[r];
+      pos_out[to] = pos[r];
+    }
+  }
+}
+
+// ---- gradient: sums over runs of equal keys -----------------------------------------------------------------------------------
+constexpr int R_PIECE = 32;               // sorted positions of a wave
+
+struct GradArgs {
+  const u32x4* dX;
+  const uint32_t* skey;
+  const uint32_t* spos;
+  float* dE;
+  void* dW;
+  float* head;                            // [pieces, d]: the sum of a run that began in an earlier piece
+  float* tail;                            // [pieces, d]: the sum of a run that begins here and goes on
+  uint32_t n, pieces, V, sentinel;
+  int32_t chunks, slices, d, add, fill_blocks;
+  float scale;
+};
+
+// N consecutive features of a table row := (+=) scale * sum.
+template <bool BF16, int N>
+__device__ __forceinline__ void store_row(const GradArgs& a, uint32_t key, size_t at, const float (&sum)[N]) {
+  float x[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = sum[e] * a.scale;
+  if (key < a.V || !BF16) {
+    float4* to = reinterpret_cast<float4*>((key < a.V ? a.dE + (size_t)key * a.d : reinterpret_cast<float*>(a.dW) + (size_t)(key - a.V) * a.d) + at);
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+      float4 o = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+      if (a.add) {
+        const float4 was = to[q];
+        o = float4{was.x + o.x, was.y + o.y, was.z + o.z, was.w + o.w};
+      }
+      to[q] = o;
+    }
+    return;
+  }
+  uint2* to = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.dW) + (size_t)(key - a.V) * a.d + at);
+#pragma unroll
+  for (int q = 0; q < N / 4; ++q) {
+    if (a.add) {
+      const uint2 was = to[q];
+      x[4 * q] += lo_bf16(was.x);
+      x[4 * q + 1] += hi_bf16(was.x);
+      x[4 * q + 2] += lo_bf16(was.y);
+      x[4 * q + 3] += hi_bf16(was.y);
+    }
+    to[q] = uint2{pack_two(x[4 * q], x[4 * q + 1]), pack_two(x[4 * q + 2], x[4 * q + 3])};
+  }
+}
+
+// The first sorted position whose key is at least `key`.
+__device__ __forceinline__ uint32_t lower_bound(const uint32_t* skey, uint32_t lo, uint32_t hi, uint32_t key) {
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (skey[mid] < key) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Blocks [0, fill_blocks) write zeros to the table rows that no position names: a wave per 16 rows, each looked up by a
+// lane.  The others: a wave per R_PIECE sorted positions and 64 pieces of 16 bytes of their rows, eight rows requested at a
+// time, added in fp32 in order.  Runs inside the piece are stored, what crosses its ends is left for join_kernel.
+template <bool BF16>
+__global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
+  const int lane = threadIdx.x & 63;
+  constexpr int EPC = BF16 ? 8 : 4;
+  if ((int)blockIdx.x < a.fill_blocks) {
+    const uint32_t first = ((uint32_t)blockIdx.x * 4u + (threadIdx.x >> 6)) * 16u;
+    const uint32_t key = first + (uint32_t)(lane & 15);
+    bool empty = false;
+    if (key < a.sentinel && lane < 16) {
+      const uint32_t at = lower_bound(a.skey, 0u, a.n, key);
+      empty = at >= a.n || a.skey[at] != key;
+    }
+    const uint64_t rows = __ballot(empty);
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    for (int r = 0; r < 16; ++r) {
+      if (!((rows >> r) & 1ull)) continue;
+      const uint32_t k = first + (uint32_t)r;
+      const int per_row = k < a.V ? a.d / 4 : a.chunks;
+      u32x4* to = k < a.V ? reinterpret_cast<u32x4*>(a.dE) + (size_t)k * per_row : reinterpret_cast<u32x4*>(a.dW) + (size_t)(k - a.V) * per_row;
+      for (int q = lane; q < per_row; q += 64) to[q] = zero;
+    }
+    return;
+  }
+  const uint32_t wid = (blockIdx.x - (uint32_t)a.fill_blocks) * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t piece = wid / (uint32_t)a.slices;
+  if (piece >= a.pieces) return;
+  const int chunk = (int)(wid % (uint32_t)a.slices) * 64 + lane;
+  const bool on = chunk < a.chunks;
+  const uint32_t p0 = piece * R_PIECE;
+  const int cnt = (int)min((uint32_t)R_PIECE, a.n - p0);
+  const uint32_t my_key = lane < cnt ? a.skey[p0 + lane] : kNoKey;
+  const uint32_t my_pos = lane < cnt ? a.spos[p0 + lane] : 0u;
+  uint32_t key = __builtin_amdgcn_readfirstlane(my_key);
+  if (key >= a.sentinel) return;
+  const uint32_t prev = p0 > 0u ? a.skey[p0 - 1] : kNoKey, next = p0 + cnt < a.n ? a.skey[p0 + cnt] : kNoKey;
+  bool began_before = prev == key;
+  float acc[EPC];
+#pragma unroll
+  for (int e = 0; e < EPC; ++e) acc[e] = 0.f;
+  const u32x4* column = a.dX + min(chunk, a.chunks - 1);
+  for (int i0 = 0; i0 < R_PIECE; i0 += 8) {
+    if (i0 >= cnt) break;
+    u32x4 x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = column[(size_t)(uint32_t)__builtin_amdgcn_readlane(my_pos, min(i0 + u, cnt - 1)) * a.chunks];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + u;
+      if (i >= cnt) break;
+      if (key >= a.sentinel) return;                 // (positions that name nothing stand at the end)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (BF16) {
+          acc[2 * e] += lo_bf16(x[u][e]);
+          acc[2 * e + 1] += hi_bf16(x[u][e]);
+        } else {
+          acc[e] += __uint_as_float(x[u][e]);
+        }
+      }
+      const bool last = i + 1 == cnt;
+      const uint32_t after = last ? next : (uint32_t)__builtin_amdgcn_readlane(my_key, min(i + 1, R_PIECE - 1));
+      if (last || after != key) {
+        const bool goes_on = last && after == key;
+        if (on) {
+          if (began_before || goes_on) {
+            float4* to = reinterpret_cast<float4*>((began_before ? a.head : a.tail) + (size_t)piece * a.d + (size_t)chunk * EPC);
+#pragma unroll
+            for (int q = 0; q < EPC / 4; ++q) to[q] = float4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+          } else {
+            store_row<BF16, EPC>(a, key, (size_t)chunk * EPC, acc);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) acc[e] = 0.f;
+        began_before = false;
+        key = after;
+      }
+    }
+  }
+}
+
+// A run over several pieces: block (p, y) joins the run that begins in piece p and goes on, 256 features of it.  Its four waves add a quarter of
+// the pieces each, in order, and the quarters in order.
+template <bool BF16>
+__global__ void __launch_bounds__(256) join_kernel(GradArgs a) {
+  __shared__ float4 part[4][64];
+  const uint32_t p = blockIdx.x, p0 = p * R_PIECE, p1 = p0 + R_PIECE;
+  if (p1 >= a.n) return;
+  const uint32_t key = a.skey[p1 - 1];
+  if (key >= a.sentinel || a.skey[p1] != key || (p0 > 0u && a.skey[p0] == key && a.skey[p0 - 1] == key)) return;
+  const uint32_t end = lower_bound(a.skey, p1, a.n, key + 1u), q1 = (end - 1u) / R_PIECE;      // the run's last piece
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int f = (int)blockIdx.y * 256 + lane * 4;
+  const bool on = f < a.d;
+  const uint32_t heads = q1 - p, each = (heads + 3u) / 4u;
+  const uint32_t from = p + 1u + min((uint32_t)wave * each, heads), to = p + 1u + min(((uint32_t)wave + 1u) * each, heads);
+  float4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (on) {
+    if (wave == 0) sum = *reinterpret_cast<const float4*>(a.tail + (size_t)p * a.d + f);
+#pragma unroll 8
+    for (uint32_t q = from; q < to; ++q) {
+      const float4 x = *reinterpret_cast<const float4*>(a.head + (size_t)q * a.d + f);
+      sum.x += x.x;
+      sum.y += x.y;
+      sum.z += x.z;
+      sum.w += x.w;
+    }
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && on) {
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const float4 x = part[w][lane];
+      sum.x += x.x;
+      sum.y += x.y;
+      sum.z += x.z;
+      sum.w += x.w;
+    }
+    const float s[4] = {sum.x, sum.y, sum.z, sum.w};
+    store_row<BF16, 4>(a, key, (size_t)f, s);
+  }
+}
+
+LookupArgs lookup_args(const z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride) {
+  LookupArgs a;
+  a.codes = codes;
+  a.n_codes = n_codes;
+  a.size = c->st.size;
+  a.B = c->cfg.B;
+  a.V = c->cfg.V;
+  a.cap = c->cfg.cap;
+  a.stride = stride;
+  a.chunks = c->cfg.d / (c->cfg.dtype == Z2Z_BF16 ? 8 : 4);
+  a.sentinel = (uint32_t)((long long)c->cfg.V + (long long)c->cfg.B * c->cfg.cap);
+  return a;
+}
+
+}  // namespace
+
+int z2z_launch_embed_codes(z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride, const void* E, const void* W_hyper,
+                           float scale, void* X, int32_t* status, hipStream_t s) {
+  const LookupArgs a = lookup_args(c, codes, n_codes, stride);
+  const long long positions = (long long)a.B * stride;
+  int split = 1;
+  while (split < 16 && positions * split < 2048 && a.chunks > 64 * split) split *= 2;
+  const long long blocks = a.B + (positions * split + 3) / 4;
+  if (blocks > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
+  const dim3 grid((unsigned)blocks), block(256);
+  const u32x4 *e = reinterpret_cast<const u32x4*>(E), *w = reinterpret_cast<const u32x4*>(W_hyper);
+  if (c->cfg.dtype == Z2Z_BF16)
+    hipLaunchKernelGGL(embed_codes_kernel<true>, grid, block, 0, s, a, e, w, reinterpret_cast<u32x4*>(X), status, scale, split);
+  else
+    hipLaunchKernelGGL(embed_codes_kernel<false>, grid, block, 0, s, a, e, w, reinterpret_cast<u32x4*>(X), status, scale, split);
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}
+
+int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride, float scale, const void* dX,
+                                    int32_t flags, float* dE, void* dW_hyper, hipStream_t s) {
+  const LookupArgs a = lookup_args(c, codes, n_codes, stride);
+  const long long positions = (long long)a.B * stride, keys = (long long)a.V + (long long)a.B * a.cap;
+  // (positions and rows of the joint table are 32-bit numbers here)
+  if (positions > 0x7FFFFFFFLL || keys > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
+  const uint32_t n = (uint32_t)positions;
+  const bool bf16 = c->cfg.dtype == Z2Z_BF16, add = flags == Z2Z_GRAD_ADD;
+  if (n == 0u && add) return Z2Z_OK;
+  int key_bits = 1;
+  while ((keys >> key_bits) != 0) ++key_bits;        // (the sentinel is a key, too)
+  const int passes = (key_bits + 9) / 10, bits = (key_bits + passes - 1) / passes;
+  const uint32_t tiles = (n + S_TILE - 1) / S_TILE, pieces = (n + R_PIECE - 1) / R_PIECE;
+  // work space: sorted keys and positions (twice where the passes go through memory), the tiles' counts, sums that cross pieces
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t at = off; off += (bytes + 255) / 256 * 256; return at; };
+  const bool small = n <= (uint32_t)S_TILE;
+  const size_t o_key[2] = {take((size_t)n * 4), small ? 0 : take((size_t)n * 4)};
+  const size_t o_pos[2] = {take((size_t)n * 4), small ? 0 : take((size_t)n * 4)};
+  const size_t o_count = small ? 0 : take((size_t)tiles * (1u << bits) * 4);
+  const size_t o_head = pieces > 1 ? take((size_t)pieces * c->cfg.d * 4) : 0;
+  const size_t o_tail = pieces > 1 ? take((size_t)pieces * c->cfg.d * 4) : 0;
+  const int rc = z2z_work_reserve(c, &c->lookup_ws, off, s);
+  if (rc != Z2Z_OK) return rc;
+  unsigned char* ws = reinterpret_cast<unsigned char*>(c->lookup_ws.p);
+  auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
+  int from = 0;
+  if (n == 0u) {
+    // (nothing to sort: zeros alone)
+  } else if (small) {
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(1024), 0, s, a, n, bits, passes, words(o_key[0]), words(o_pos[0]));
+  } else {
+    for (int p = 0; p < passes; ++p) {
+      const uint32_t *key_in = p > 0 ? words(o_key[from]) : nullptr, *pos_in = p > 0 ? words(o_pos[from]) : nullptr;
+      const int to = p > 0 ? from ^ 1 : 0;
+      hipLaunchKernelGGL(sort_count_kernel, dim3(tiles), dim3(1024), 0, s, a, n, key_in, p * bits, bits, words(o_count));
+      hipLaunchKernelGGL(sort_place_kernel, dim3(tiles), dim3(1024), 0, s, a, n, key_in, pos_in, p * bits, bits, words(o_count),
+                         words(o_key[to]), words(o_pos[to]));
+      from = to;
+    }
+  }
+  GradArgs g;
+  memset(&g, 0, sizeof(g));
+  g.dX = reinterpret_cast<const u32x4*>(dX);
+  g.skey = n ? words(o_key[from]) : nullptr;
+  g.spos = n ? words(o_pos[from]) : nullptr;
+  g.dE = dE;
+  g.dW = dW_hyper;
+  g.head = pieces > 1 ? reinterpret_cast<float*>(ws + o_head) : nullptr;
+  g.tail = pieces > 1 ? reinterpret_cast<float*>(ws + o_tail) : nullptr;
+  g.n = n;
+  g.pieces = pieces;
+  g.V = (uint32_t)a.V;
+  g.sentinel = a.sentinel;
+  g.chunks = a.chunks;
+  g.slices = (a.chunks + 63) / 64;
+  g.d = c->cfg.d;
+  g.add = add ? 1 : 0;
+  g.fill_blocks = add ? 0 : (int)((keys + 63) / 64);
+  g.scale = scale;
+  const long long blocks = g.fill_blocks + ((long long)pieces * g.slices + 3) / 4;
+  if (blocks > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
+  if (bf16)
+    hipLaunchKernelGGL(reduce_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, s, g);
+  else
+    hipLaunchKernelGGL(reduce_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, s, g);
+  if (pieces > 1) {
+    const dim3 grid(pieces, (unsigned)((c->cfg.d + 255) / 256));
+    if (bf16)
+      hipLaunchKernelGGL(join_kernel<true>, grid, dim3(256), 0, s, g);
+    else
+      hipLaunchKernelGGL(join_kernel<false>, grid, dim3(256), 0, s, g);
+  }
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}

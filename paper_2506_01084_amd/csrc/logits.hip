@@ -198,8 +198,8 @@ __global__ void __launch_bounds__(256) target_nll_kernel(const uint4* H, const u
 int ensure_sample_scratch(z2z_ctx* c, size_t need, hipStream_t s) {
   if (need <= c->part_vl_capacity) return Z2Z_OK;
   Z2Z_TRY_GROW(s);
-  if (c->part_v) (void)hipFree(c->part_v);
-  if (c->part_l) (void)hipFree(c->part_l);
+  z2z_release(c, c->part_v);
+  z2z_release(c, c->part_l);
   c->part_v = nullptr;
   c->part_l = nullptr;
   c->part_vl_capacity = 0;
@@ -212,9 +212,9 @@ int ensure_sample_scratch(z2z_ctx* c, size_t need, hipStream_t s) {
 int ensure_scratch(z2z_ctx* c, size_t need, hipStream_t s) {
   if (need <= c->part_capacity) return Z2Z_OK;
   Z2Z_TRY_GROW(s);
-  if (c->part_m) (void)hipFree(c->part_m);
-  if (c->part_s) (void)hipFree(c->part_s);
-  if (c->part_i) (void)hipFree(c->part_i);
+  z2z_release(c, c->part_m);
+  z2z_release(c, c->part_s);
+  z2z_release(c, c->part_i);
   c->part_m = nullptr;
   c->part_s = nullptr;
   c->part_i = nullptr;
@@ -569,6 +569,94 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
   return launch_combine(parts, n_parts, rows, argmax, mx, lse, s);
 }
 
+// Room for one row of logits per sequence, the row maxima and log-sum-exps.
+static int ensure_sample_logits(z2z_ctx* c, int32_t rows, hipStream_t s) {
+  const size_t need = (size_t)rows * (size_t)(c->cfg.V + c->cfg.cap);
+  if (need > c->sample_logits_capacity) {
+    Z2Z_TRY_GROW(s);
+    z2z_release(c, c->sample_logits);
+    z2z_release(c, c->row_max);
+    c->sample_logits = nullptr;
+    c->row_max = nullptr;
+    c->sample_logits_capacity = 0;
+    if (!z2z_device_malloc(&c->sample_logits, need * sizeof(float))) return Z2Z_ENOMEM;
+    // the row maxima and log-sum-exps, followed by the selection kernels' scratch
+    if (!z2z_device_malloc(&c->row_max, (2 * (size_t)rows + z2z_sample_truncated_work_floats(rows)) * sizeof(float)))
+      return Z2Z_ENOMEM;
+    c->sample_logits_capacity = need;
+  }
+  return Z2Z_OK;
+}
+
+// One hidden row per sequence, every logit / T stored in the context's sample_logits (rows x (V + cap) floats) and folded into parts of
+// *base_columns and *hyper_columns columns (0: the decode kernel's units).  mid_base: the base vocabulary goes to the weight-streaming kernel.
+static int launch_stored_logits(z2z_ctx* c, const void* H, int32_t rows, const void* W_base, const void* W_hyper,
+                                const z2z_sample_params& sp, bool mid_base, int* parts_out, int* base_out, int* hyper_out,
+                                hipStream_t s) {
+  const bool timed = c->opt_timing && c->n_timed < Z2Z_MAX_TIMED && c->ev_created;
+  const bool timed_pair = timed && mid_base && rows <= 64;       // a split step's two launches are timed together
+  int n_parts = z2z_logits_decode_parts(c);
+  int rc = ensure_sample_logits(c, rows, s);
+  if (rc != Z2Z_OK) return rc;
+  int base_columns = 0, hyper_columns = 0;           // of a part: the decode kernel's units unless set
+  if ((rows > 64 || mid_base) && c->cfg.d % 64 == 0 && c->fast_ready && c->opt_logits_kernel != 1) {
+    // more than one pass of the decode kernel's base units, or a split step: the tile or the streaming kernel stores and folds the base
+    // vocabulary's scaled logits, the hyper units run alone (strips of at most 2 tiles: the selection kernels'
+    // short-list pass takes parts of up to 512 columns)
+    const int base_vt = (c->cfg.V + 255) / 256;
+    int strip_b = mid_base ? 1 : pick_strip_for(c, (rows + 255) / 256, base_vt);
+    if (strip_b > 2) strip_b = 2;
+    const int mid_columns = z2z_logits_mid_columns(c, c->cfg.V);
+    const int base_strips = mid_base ? (c->cfg.V + mid_columns - 1) / mid_columns : (base_vt + strip_b - 1) / strip_b;
+    // (hyper units of 512 rows are too few for a small batch: smaller ones, while the short-list pass takes as many parts.  21 sequences of up to
+    // 4096 entries, V = 32064 121 -> 84 us, 20 x 1024, V = 128256 271 -> 213, 6 x 4096, V = 151936 291 -> 250.  From 200 of 512 rows on those
+    // are the better ones here: a unit's logits leave it row by row, 108 x 1024 356 us, 361 in 432 of 256; 56 x 2048 341 and 348, 32 x 4096 338
+    // and 349.  Below that at least 512 where those of 256 would be more than a round (129 to 199 of 512; units of 512 / 256 / 128 rows, codebooks full:
+    // 33 x 2048, V = 128256 283 / 304 / 286 us, V = 32064 133 / 145 / 130, V = 151936 318 / 333 / 312; 96 x 1024 314 / 323 / 317, 150 / 156 / 150, 346 /
+    // 352 / 344; a third full 40 x 2048 271 / 237 / 227, 120 / 94 / 84, 301 / 271 / 260) and where room for more than 2048 entries is seldom full and the units
+    // that exist are few of them (21 x 730 of 4096 96 us in 336 units, 84 in 672; full 8 x 4096, V = 128256 260 -> 221))
+    const long long wide = (long long)rows * ((c->cfg.cap + 511) / 512);
+    hyper_columns = z2z_logits_decode_hyper_unit(c, wide < 200 && (c->cfg.cap > 2048 || wide > 128) ? 512 : 200);
+    while (hyper_columns < 512 && base_strips + (c->cfg.cap + hyper_columns - 1) / hyper_columns > z2z_sample_list_parts()) hyper_columns *= 2;
+    n_parts = base_strips + (c->cfg.cap + hyper_columns - 1) / hyper_columns;
+    base_columns = mid_base ? mid_columns : strip_b * 256;
+    LogitsArgs a;
+    memset(&a, 0, sizeof(a));
+    a.H = H;
+    a.rows = rows;
+    a.rows_per_seq = 1;
+    a.d = c->cfg.d;
+    a.part_m = c->part_m;
+    a.part_s = c->part_s;
+    a.part_i = c->part_i;
+    a.n_parts = n_parts;
+    a.sample = 2;
+    a.inv_temperature = 1.0f / sp.temperature;
+    a.logits = c->sample_logits;
+    a.ld = c->cfg.V + c->cfg.cap;
+    if (timed_pair) Z2Z_HIP_TRY(hipEventRecord(c->ev_start[c->n_timed], s));
+    a.once = mid_base && split_few_once(c, rows);
+    if (mid_base)
+      rc = z2z_launch_logits_mid(c, a, W_base, c->cfg.V, 0, s);
+    else
+      rc = z2z_launch_logits_part(c, false, a, W_base, c->cfg.V, 0, 0, strip_b, rows, 1, timed, s);
+    if (rc != Z2Z_OK) return rc;
+    if (c->cfg.cap > 0) {
+      int np = 0;
+      rc = z2z_launch_logits_decode(c, H, W_base, W_hyper, &np, false, &sp, c->sample_logits, s, base_strips, nullptr, 1, hyper_columns);
+      if (rc != Z2Z_OK) return rc;
+    }
+    if (timed_pair) Z2Z_HIP_TRY(hipEventRecord(c->ev_stop[c->n_timed++], s));
+  } else {
+    rc = z2z_launch_logits_decode(c, H, W_base, W_hyper, &n_parts, timed, &sp, c->sample_logits, s);
+    if (rc != Z2Z_OK) return rc;
+  }
+  *parts_out = n_parts;
+  *base_out = base_columns;
+  *hyper_out = hyper_columns;
+  return Z2Z_OK;
+}
+
 int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                const void* W_hyper, float temperature, int32_t top_k, float top_p, uint64_t seed,
                                uint64_t step, int32_t* token, float* logprob, hipStream_t s) {
@@ -652,79 +740,49 @@ int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t 
   // filters: the kernel stores the rows' logits / T (rows x (V + cap) floats of library scratch), the merge
   // gives the row maxima and log-sum-exps, and one workgroup per row selects the kept prefix and draws
   if (!c->trunc_ready) return Z2Z_EUNSUPPORTED;
-  const size_t need = (size_t)rows * (size_t)(c->cfg.V + c->cfg.cap);
-  if (need > c->sample_logits_capacity) {
-    Z2Z_TRY_GROW(s);
-    if (c->sample_logits) (void)hipFree(c->sample_logits);
-    if (c->row_max) (void)hipFree(c->row_max);
-    c->sample_logits = nullptr;
-    c->row_max = nullptr;
-    c->sample_logits_capacity = 0;
-    if (!z2z_device_malloc(&c->sample_logits, need * sizeof(float))) return Z2Z_ENOMEM;
-    // the row maxima and log-sum-exps, followed by the selection kernels' scratch
-    if (!z2z_device_malloc(&c->row_max, (2 * (size_t)rows + z2z_sample_truncated_work_floats(rows)) * sizeof(float)))
-      return Z2Z_ENOMEM;
-    c->sample_logits_capacity = need;
-  }
-  int base_columns = 0, hyper_columns = 0;           // of a part: the decode kernel's units unless set
-  if ((rows > 64 || mid_base) && c->cfg.d % 64 == 0 && c->fast_ready && c->opt_logits_kernel != 1) {
-    // more than one pass of the decode kernel's base units, or a split step: the tile or the streaming kernel stores and folds the base
-    // vocabulary's scaled logits, the hyper units run alone (strips of at most 2 tiles: the selection kernels'
-    // short-list pass takes parts of up to 512 columns)
-    const int base_vt = (c->cfg.V + 255) / 256;
-    int strip_b = mid_base ? 1 : pick_strip_for(c, (rows + 255) / 256, base_vt);
-    if (strip_b > 2) strip_b = 2;
-    const int mid_columns = z2z_logits_mid_columns(c, c->cfg.V);
-    const int base_strips = mid_base ? (c->cfg.V + mid_columns - 1) / mid_columns : (base_vt + strip_b - 1) / strip_b;
-    // (hyper units of 512 rows are too few for a small batch: smaller ones, while the short-list pass takes as many parts.  21 sequences of up to
-    // 4096 entries, V = 32064 121 -> 84 us, 20 x 1024, V = 128256 271 -> 213, 6 x 4096, V = 151936 291 -> 250.  From 200 of 512 rows on those
-    // are the better ones here: a unit's logits leave it row by row, 108 x 1024 356 us, 361 in 432 of 256; 56 x 2048 341 and 348, 32 x 4096 338
-    // and 349.  Below that at least 512 where those of 256 would be more than a round (129 to 199 of 512; units of 512 / 256 / 128 rows, codebooks full:
-    // 33 x 2048, V = 128256 283 / 304 / 286 us, V = 32064 133 / 145 / 130, V = 151936 318 / 333 / 312; 96 x 1024 314 / 323 / 317, 150 / 156 / 150, 346 /
-    // 352 / 344; a third full 40 x 2048 271 / 237 / 227, 120 / 94 / 84, 301 / 271 / 260) and where room for more than 2048 entries is seldom full and the units
-    // that exist are few of them (21 x 730 of 4096 96 us in 336 units, 84 in 672; full 8 x 4096, V = 128256 260 -> 221))
-    const long long wide = (long long)rows * ((c->cfg.cap + 511) / 512);
-    hyper_columns = z2z_logits_decode_hyper_unit(c, wide < 200 && (c->cfg.cap > 2048 || wide > 128) ? 512 : 200);
-    while (hyper_columns < 512 && base_strips + (c->cfg.cap + hyper_columns - 1) / hyper_columns > z2z_sample_list_parts()) hyper_columns *= 2;
-    n_parts = base_strips + (c->cfg.cap + hyper_columns - 1) / hyper_columns;
-    base_columns = mid_base ? mid_columns : strip_b * 256;
-    LogitsArgs a;
-    memset(&a, 0, sizeof(a));
-    a.H = H;
-    a.rows = rows;
-    a.rows_per_seq = 1;
-    a.d = c->cfg.d;
-    a.part_m = c->part_m;
-    a.part_s = c->part_s;
-    a.part_i = c->part_i;
-    a.n_parts = n_parts;
-    a.sample = 2;
-    a.inv_temperature = 1.0f / temperature;
-    a.logits = c->sample_logits;
-    a.ld = c->cfg.V + c->cfg.cap;
-    if (timed_pair) Z2Z_HIP_TRY(hipEventRecord(c->ev_start[c->n_timed], s));
-    a.once = mid_base && split_few_once(c, rows);
-    if (mid_base)
-      rc = z2z_launch_logits_mid(c, a, W_base, c->cfg.V, 0, s);
-    else
-      rc = z2z_launch_logits_part(c, false, a, W_base, c->cfg.V, 0, 0, strip_b, rows, 1, timed, s);
-    if (rc != Z2Z_OK) return rc;
-    if (c->cfg.cap > 0) {
-      int np = 0;
-      rc = z2z_launch_logits_decode(c, H, W_base, W_hyper, &np, false, &sp, c->sample_logits, s, base_strips, nullptr, 1, hyper_columns);
-      if (rc != Z2Z_OK) return rc;
-    }
-    if (timed_pair) Z2Z_HIP_TRY(hipEventRecord(c->ev_stop[c->n_timed++], s));
-  } else {
-    rc = z2z_launch_logits_decode(c, H, W_base, W_hyper, &n_parts, timed, &sp, c->sample_logits, s);
-    if (rc != Z2Z_OK) return rc;
-  }
+  int base_columns = 0, hyper_columns = 0;
+  rc = launch_stored_logits(c, H, rows, W_base, W_hyper, sp, mid_base, &n_parts, &base_columns, &hyper_columns, s);
+  if (rc != Z2Z_OK) return rc;
   if (!z2z_sample_truncated_merges_parts(c, n_parts, top_k, base_columns, hyper_columns)) {
     rc = launch_combine(ctx_parts(c), n_parts, rows, nullptr, c->row_max, c->row_max + rows, s);
     if (rc != Z2Z_OK) return rc;
   }
   return z2z_launch_sample_truncated(c, c->sample_logits, c->row_max, rows, n_parts, c->row_max + 2 * (size_t)rows, &sp,
                                      top_k, top_p, token, logprob, s, base_columns, hyper_columns);
+}
+
+int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
+                             int32_t picks, int32_t* parent, int32_t* code, float* picked, hipStream_t s) {
+  const int rows = c->cfg.B;
+  int n_parts = 0, base_columns = 256, hyper_columns = 256;
+  int rc = ensure_scratch(c, step_parts(c) * rows, s);
+  if (rc != Z2Z_OK) return rc;
+  rc = ensure_sample_logits(c, rows, s);
+  if (rc != Z2Z_OK) return rc;
+  float* row_lse = c->row_max + rows;
+  if (c->decode_ready) {
+    // the kernels of a filtered step, at temperature 1: every logit stored, a maximum per part
+    z2z_sample_params sp;
+    sp.temperature = 1.0f;
+    sp.seed = sp.step = 0;
+    const bool mid_base = (rows > 64 || split_few(c, rows, true)) && c->opt_logits_kernel == 0 && z2z_logits_mid_ok(c, rows);
+    int base = 0, hyper = 0;
+    rc = launch_stored_logits(c, H, rows, W_base, W_hyper, sp, mid_base, &n_parts, &base, &hyper, s);
+    if (rc != Z2Z_OK) return rc;
+    z2z_logits_decode_units(&base_columns, &hyper_columns);
+    if (base > 0) base_columns = base;
+    if (hyper > 0) hyper_columns = hyper;
+    rc = launch_combine(ctx_parts(c), n_parts, rows, nullptr, nullptr, row_lse, s);
+  } else {
+    // (fp32, or widths that the step's kernels do not take: the general kernel stores the logits, and a maximum per 256 columns comes
+    // from those)
+    rc = z2z_launch_extended_logits(c, H, rows, 1, W_base, W_hyper, nullptr, nullptr, row_lse, c->sample_logits, s);
+    if (rc != Z2Z_OK) return rc;
+    rc = z2z_launch_part_max(c, c->sample_logits, c->part_m, &n_parts, s);
+  }
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_beam_pick(c, c->sample_logits, c->part_m, n_parts, base_columns, hyper_columns, row_lse, beams, score, picks, parent, code,
+                              picked, s);
 }
 
 int z2z_launch_extended_nll(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,

@@ -920,7 +920,7 @@ int z2z_launch_linear_skinny(z2z_ctx* c, const void* A, const void* W, const flo
     const size_t need = slots * ksplit * D_LINEAR_UNIT * 64 * sizeof(float);
     if (need > c->skinny_partial_bytes) {
       Z2Z_TRY_GROW(s);
-      if (c->skinny_partial) (void)hipFree(c->skinny_partial);
+      z2z_release(c, c->skinny_partial);
       c->skinny_partial = nullptr;
       c->skinny_partial_bytes = 0;
       const size_t want_bytes = need > ((size_t)16 << 20) ? need : ((size_t)16 << 20);

@@ -108,7 +108,7 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   if (layout(n_seq) > limit) return Z2Z_ENOMEM;      // one sequence alone does not fit
   if (off > c->bwd_ws_bytes) {
     Z2Z_TRY_GROW(s);
-    if (c->bwd_ws) (void)hipFree(c->bwd_ws);
+    z2z_release(c, c->bwd_ws);
     c->bwd_ws = nullptr;
     c->bwd_ws_bytes = 0;
     if (!z2z_device_malloc(&c->bwd_ws, off)) return Z2Z_ENOMEM;

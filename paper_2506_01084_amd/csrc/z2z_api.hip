@@ -36,6 +36,13 @@ void free_ctx(z2z_ctx* c) {
   (void)hipFree(c->coef_dev);
   (void)hipFree(c->prune_prefix);
   (void)hipFree(c->skinny_partial);
+  (void)hipFree(c->lookup_ws.p);
+  while (c->kept) {
+    z2z_kept* k = c->kept;
+    c->kept = k->next;
+    (void)hipFree(k->p);
+    delete k;
+  }
   if (c->ev_created) {
     for (int i = 0; i < Z2Z_MAX_TIMED; ++i) {
       (void)hipEventDestroy(c->ev_start[i]);
@@ -45,7 +52,42 @@ void free_ctx(z2z_ctx* c) {
   delete c;
 }
 
+// A call that uses work buffers: on the context's device, and noted where it is captured into a graph.
+int enter(z2z_ctx* c, hipStream_t s) {
+  int device = -1;
+  if (hipGetDevice(&device) != hipSuccess) return Z2Z_EHIP;
+  if (device != c->device) return Z2Z_EINVAL;
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) != hipSuccess) return Z2Z_EHIP;
+  if (st != hipStreamCaptureStatusNone) c->captured = true;
+  return Z2Z_OK;
+}
+
 }  // namespace
+
+void z2z_release(z2z_ctx* c, void* p) {
+  if (!p) return;
+  if (!c->captured) {
+    (void)hipFree(p);
+    return;
+  }
+  z2z_kept* k = new (std::nothrow) z2z_kept;
+  if (!k) return;                                    // (lost rather than pulled away under a graph)
+  k->p = p;
+  k->next = c->kept;
+  c->kept = k;
+}
+
+int z2z_work_reserve(z2z_ctx* c, z2z_work* w, size_t bytes, hipStream_t s) {
+  if (bytes <= w->bytes) return Z2Z_OK;
+  Z2Z_TRY_GROW(s);
+  z2z_release(c, w->p);
+  w->p = nullptr;
+  w->bytes = 0;
+  if (!z2z_device_malloc(&w->p, bytes)) return Z2Z_ENOMEM;
+  w->bytes = bytes;
+  return Z2Z_OK;
+}
 
 extern "C" {
 
@@ -315,6 +357,55 @@ Z2Z_API int z2z_extended_sample(z2z_ctx* ctx, const void* d_H, int32_t rows, int
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   return z2z_launch_extended_sample(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, temperature, top_k, top_p,
                                     seed, step, d_token, d_logprob, static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, const void* d_E,
+                            const void* d_W_hyper, float scale, void* d_X, int32_t* d_status, void* stream) {
+  if (!ctx || !d_E || !d_status || stride < 0) return Z2Z_EINVAL;
+  if (stride > 0 && (!d_codes || !d_X)) return Z2Z_EINVAL;
+  if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
+  if (!isfinite(scale)) return Z2Z_EINVAL;
+  if (!aligned16(d_E) || !aligned16(d_W_hyper) || !aligned16(d_X)) return Z2Z_EINVAL;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_embed_codes(ctx, d_codes, d_n_codes, stride, d_E, d_W_hyper, scale, d_X, d_status,
+                                static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_embed_codes_backward(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, float scale,
+                                     const void* d_dX, int32_t flags, float* d_dE, void* d_dW_hyper, void* stream) {
+  if (!ctx || !d_dE || stride < 0) return Z2Z_EINVAL;
+  if (stride > 0 && (!d_codes || !d_dX)) return Z2Z_EINVAL;
+  if (ctx->cfg.cap > 0 && !d_dW_hyper) return Z2Z_EINVAL;
+  if (flags != 0 && flags != Z2Z_GRAD_ADD) return Z2Z_EINVAL;
+  if (!isfinite(scale)) return Z2Z_EINVAL;
+  if (!aligned16(d_dX) || !aligned16(d_dE) || !aligned16(d_dW_hyper)) return Z2Z_EINVAL;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_embed_codes_backward(ctx, d_codes, d_n_codes, stride, scale, d_dX, flags, d_dE, d_dW_hyper,
+                                         static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_extended_beam(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t beams, const void* d_W_base, const void* d_W_hyper,
+                              const float* d_score, int32_t n_pick, int32_t* d_parent, int32_t* d_code, float* d_picked, void* stream) {
+  if (!ctx || !d_H || !d_W_base || !d_score || !d_parent || !d_code || !d_picked) return Z2Z_EINVAL;
+  if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
+  if (rows != ctx->cfg.B || beams < 1 || rows % beams != 0 || n_pick < 1) return Z2Z_EINVAL;
+  if (beams > Z2Z_MAX_BEAMS || n_pick > Z2Z_MAX_PICK) return Z2Z_EUNSUPPORTED;
+  if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_extended_beam(ctx, d_H, beams, d_W_base, d_W_hyper, d_score, n_pick, d_parent, d_code, d_picked,
+                                  static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_codebook_reorder(z2z_ctx* ctx, int32_t beams, const int32_t* d_source, void* d_W_hyper, void* stream) {
+  if (!ctx || !d_source || beams < 1 || ctx->cfg.B % beams != 0) return Z2Z_EINVAL;
+  if (beams > Z2Z_MAX_BEAMS) return Z2Z_EUNSUPPORTED;
+  if (!aligned16(d_W_hyper)) return Z2Z_EINVAL;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_codebook_reorder(ctx, beams, d_source, d_W_hyper, static_cast<hipStream_t>(stream));
 }
 
 Z2Z_API int z2z_extended_nll(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,

@@ -40,6 +40,18 @@ struct z2z_parts {
   size_t capacity;
 };
 
+// A work buffer of the context that grows with the calls.
+struct z2z_work {
+  void* p;
+  size_t bytes;
+};
+
+// Work buffers that had to grow after a call was captured into a graph: the graph still names the old one.
+struct z2z_kept {
+  void* p;
+  z2z_kept* next;
+};
+
 struct z2z_ctx {
   z2z_config cfg;
   int device;
@@ -77,6 +89,9 @@ struct z2z_ctx {
   // dense layers on few rows with K split over workgroups: the partial tiles
   void* skinny_partial;
   size_t skinny_partial_bytes;
+  z2z_work lookup_ws;      // gradient of the code lookup: sorted positions, sums that cross pieces
+  bool captured;           // a call that uses work buffers has been captured into a graph: none is freed from then on
+  z2z_kept* kept;
   // options
   int opt_backward_chunk;
   int opt_logits_kernel, opt_logits_strip, opt_lzw_kernel, opt_decode_kernel, opt_timing, opt_logits_map,
@@ -130,6 +145,24 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
                                   const void* dW_hyper, const z2z_encoder* grad, float* dE, hipStream_t s);
 int z2z_launch_extended_nll(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                             const void* W_hyper, const int32_t* targets, float* nll, float* lse, hipStream_t s);
+
+int z2z_launch_embed_codes(z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride, const void* E, const void* W_hyper,
+                           float scale, void* X, int32_t* status, hipStream_t s);
+int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride, float scale, const void* dX,
+                                    int32_t flags, float* dE, void* dW_hyper, hipStream_t s);
+int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
+                             int32_t picks, int32_t* parent, int32_t* code, float* picked, hipStream_t s);
+// The pick from stored logits [B, V + cap] and the largest of each part of base_columns / hyper_columns columns (powers of two).
+int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, int n_parts, int base_columns, int hyper_columns,
+                         const float* row_lse, int beams, const float* score, int picks, int32_t* parent, int32_t* code, float* picked,
+                         hipStream_t s);
+int z2z_launch_part_max(z2z_ctx* c, const float* logits, float* part_m, int* n_parts, hipStream_t s);   // parts of 256 columns
+int z2z_launch_codebook_reorder(z2z_ctx* c, int32_t beams, const int32_t* source, void* W_hyper, hipStream_t s);
+
+// A work buffer's memory is given back, or kept until z2z_destroy where a captured graph may still use it.
+void z2z_release(z2z_ctx* c, void* p);
+// At least `bytes` in the work buffer (Z2Z_ECAPTURE where it would have to grow under capture).
+int z2z_work_reserve(z2z_ctx* c, z2z_work* w, size_t bytes, hipStream_t s);
 
 // A work buffer that has to grow is freed and allocated again (hipFree / hipMalloc: the device synchronises that
 // once).  A stream capture does not survive that, so under capture the call is refused instead, before anything
