@@ -420,6 +420,36 @@ int z2z_extended_nll_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32
                               const float* d_lse, const float* d_grad_nll, void* d_dH, void* d_dW_base,
                               void* d_dW_hyper, void* stream);
 
+/* extended_distill.  The loss of section 2.4's training over compressed sequences when a position's target is a teacher's distribution
+ * over its K = n_teacher best columns instead of one code.  With ids = d_ids[r, :], t = d_teacher[r, :] and T = temperature,
+ *   q = softmax(t / T) over the listed columns,   ln p_v = logit[r, v] / T - d_lse[r],   d_lse[r] = ln sum_v exp(logit[r, v] / T)
+ *   d_kl[r] = sum_k q_k (ln q_k - ln p_{ids_k})
+ * over the same columns as z2z_extended_logits; the Kullback-Leibler divergence from the student to the teacher, whose mass outside its
+ * list is left out.  ids < V are base tokens, V <= ids < V + C_b entries of the row's sequence; a negative id lists nothing
+ * (its teacher logit is not read), nor does a teacher logit of -inf or one more than 87 T below the row's largest (q < e^-87); a column listed twice counts twice.  A row that lists nothing has
+ * d_kl = 0; one that lists a column that does not exist has +inf; a teacher logit of NaN or +inf makes the row NaN.  K = 1 at
+ * T = 1 is z2z_extended_nll.
+ *   d_ids [rows, K] int32; d_teacher [rows, K] float
+ *   d_kl, d_lse [rows] float out; d_student [rows, K] float out: logit[r, ids_k] (not divided by T; 0 where no existing column is listed)
+ *   temperature between 1/16 and 1024 (else Z2Z_EINVAL); K <= Z2Z_MAX_TEACHER, else Z2Z_EUNSUPPORTED
+ * Any shape and storage type z2z_extended_logits takes, and its work buffers. */
+#define Z2Z_MAX_TEACHER 256
+int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,
+                         const void* d_W_hyper, int32_t n_teacher, const int32_t* d_ids, const float* d_teacher,
+                         float temperature, float* d_kl, float* d_lse, float* d_student, void* stream);
+
+/* Backward of z2z_extended_distill: the gradient of  L = sum_r grad_kl[r] * kl[r]  with respect to the hidden rows and both unembedding
+ * matrices,  dZ[r, v] = grad_kl[r] / T * (p_v - sum_{k: ids_k = v} q_k)  in place of the loss's dZ above, everything else as for
+ * z2z_extended_nll_backward.  (The usual factor T^2 is the caller's, in grad_kl.)  Rows that list nothing and rows with kl = +inf
+ * contribute nothing.
+ *   d_lse, d_student   what z2z_extended_distill returned for the same inputs
+ *   d_grad_kl          [rows] float or NULL (= 1 for every row)
+ * Types, restrictions, errors and work space as for z2z_extended_nll_backward. */
+int z2z_extended_distill_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,
+                                  const void* d_W_hyper, int32_t n_teacher, const int32_t* d_ids, const float* d_teacher,
+                                  float temperature, const float* d_lse, const float* d_student, const float* d_grad_kl,
+                                  void* d_dH, void* d_dW_base, void* d_dW_hyper, void* stream);
+
 /* Backward of z2z_hyper_embed (the pooling is linear in E):  dE[t_j, :] += a_j * dW_hyper[b, e, :]  for every
  * token t_j of every existing entry, with the coefficients a_j of the forward pass.
  *   d_dW_hyper [B, cap, d] bf16;  d_dE [V, d] float, ACCUMULATED into (zero it first for the plain gradient).

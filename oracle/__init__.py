@@ -31,7 +31,8 @@ from .embed import hyper_embed, pool_coefficients  # noqa: F401
 from .logits import extended_logits  # noqa: F401
 from .sampling import (extended_sample, kept_prefix, philox4x32_10, sample_row,  # noqa: F401
                        sample_row_truncated)
-from .loss import extended_nll, extended_nll_backward, hyper_embed_backward  # noqa: F401
+from .loss import (extended_distill, extended_distill_backward, extended_nll, extended_nll_backward,  # noqa: F401
+                   hyper_embed_backward)
 from .lookup import embed_codes, embed_codes_backward  # noqa: F401
 from .beam import beam_pick, beam_reorder, continuations  # noqa: F401
 from .encoder import hyper_encode, hyper_encode_backward  # noqa: F401

@@ -28,9 +28,9 @@ STATIC_PARTS = 1 << 22
 
 ENC_KEPT = 1
 GRAD_ADD = 1
-MAX_BEAMS, MAX_PICK = 32, 64
+MAX_BEAMS, MAX_PICK, MAX_TEACHER = 32, 64, 256
 EXPORTS = ["z2z_create", "z2z_destroy", "z2z_reset", "z2z_lzw_encode", "z2z_lzw_decode", "z2z_step_update", "z2z_lzw_rounds", "z2z_codebook", "z2z_codebook_prefill", "z2z_codebook_usage", "z2z_codebook_prune",
-           "z2z_hyper_embed", "z2z_embed_codes", "z2z_embed_codes_backward", "z2z_extended_beam", "z2z_codebook_reorder", "z2z_hyper_encode", "z2z_hyper_encode_backward", "z2z_hyper_encode_keep", "z2z_extended_logits", "z2z_extended_logits_static", "z2z_extended_sample", "z2z_extended_nll", "z2z_extended_nll_backward", "z2z_hyper_embed_backward", "z2z_set_option",
+           "z2z_hyper_embed", "z2z_embed_codes", "z2z_embed_codes_backward", "z2z_extended_beam", "z2z_codebook_reorder", "z2z_hyper_encode", "z2z_hyper_encode_backward", "z2z_hyper_encode_keep", "z2z_extended_logits", "z2z_extended_logits_static", "z2z_extended_sample", "z2z_extended_nll", "z2z_extended_nll_backward", "z2z_extended_distill", "z2z_extended_distill_backward", "z2z_hyper_embed_backward", "z2z_set_option",
            "z2z_read_timing", "z2z_read_launches", "z2z_strerror"]
 
 
@@ -118,6 +118,10 @@ def load_library() -> ctypes.CDLL:
     lib.z2z_extended_nll_backward.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
                                               c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.z2z_hyper_embed_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.z2z_extended_distill.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_float,
+                                         c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.z2z_extended_distill_backward.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                                                  c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.z2z_embed_codes.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p]
     lib.z2z_embed_codes_backward.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_float, c_void_p, c_int32, c_void_p, c_void_p,
                                              c_void_p]
@@ -406,6 +410,38 @@ class Context:
                                                    _ptr(grad_nll, torch.float32), _ptr(dH, self.torch_dtype),
                                                    _ptr(dW_base, self.torch_dtype), _ptr(dW_hyper, self.torch_dtype),
                                                    _stream()), "z2z_extended_nll_backward")
+
+    def extended_distill(self, H: torch.Tensor, rows_per_seq: int, W_base: torch.Tensor, W_hyper: torch.Tensor, ids: torch.Tensor,
+                         teacher: torch.Tensor, kl: torch.Tensor, lse: torch.Tensor, student: torch.Tensor,
+                         temperature: float = 1.0) -> None:
+        """The loss against a teacher's listed logits; ids, teacher and student are [rows, K]."""
+        rows = H.shape[0]
+        assert H.shape[1] == self.d and tuple(W_base.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
+        assert ids.dim() == 2 and ids.shape[0] == rows and tuple(teacher.shape) == tuple(ids.shape) == tuple(student.shape)
+        assert kl.numel() == rows and lse.numel() == rows
+        _check(self._lib.z2z_extended_distill(self._h, _ptr(H, self.torch_dtype), rows, rows_per_seq, _ptr(W_base, self.torch_dtype),
+                                              _ptr(W_hyper, self.torch_dtype), ids.shape[1], _ptr(ids, torch.int32),
+                                              _ptr(teacher, torch.float32), float(temperature), _ptr(kl, torch.float32),
+                                              _ptr(lse, torch.float32), _ptr(student, torch.float32), _stream()),
+               "z2z_extended_distill")
+
+    def extended_distill_backward(self, H: torch.Tensor, rows_per_seq: int, W_base: torch.Tensor, W_hyper: torch.Tensor,
+                                  ids: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor, student: torch.Tensor,
+                                  grad_kl: Optional[torch.Tensor], dH: torch.Tensor, dW_base: torch.Tensor,
+                                  dW_hyper: torch.Tensor, temperature: float = 1.0) -> None:
+        rows = H.shape[0]
+        assert H.shape[1] == self.d and tuple(W_base.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
+        assert ids.dim() == 2 and ids.shape[0] == rows and tuple(teacher.shape) == tuple(ids.shape) == tuple(student.shape)
+        assert lse.numel() == rows and (grad_kl is None or grad_kl.numel() == rows)
+        assert tuple(dH.shape) == tuple(H.shape) and tuple(dW_base.shape) == tuple(W_base.shape)
+        assert tuple(dW_hyper.shape) == (self.B, self.cap, self.d)
+        _check(self._lib.z2z_extended_distill_backward(self._h, _ptr(H, self.torch_dtype), rows, rows_per_seq,
+                                                       _ptr(W_base, self.torch_dtype), _ptr(W_hyper, self.torch_dtype), ids.shape[1],
+                                                       _ptr(ids, torch.int32), _ptr(teacher, torch.float32), float(temperature),
+                                                       _ptr(lse, torch.float32), _ptr(student, torch.float32),
+                                                       _ptr(grad_kl, torch.float32), _ptr(dH, self.torch_dtype),
+                                                       _ptr(dW_base, self.torch_dtype), _ptr(dW_hyper, self.torch_dtype), _stream()),
+               "z2z_extended_distill_backward")
 
     def hyper_embed_backward(self, dW_hyper: torch.Tensor, dE: torch.Tensor) -> None:
         assert tuple(dW_hyper.shape) == (self.B, self.cap, self.d) and tuple(dE.shape) == (self.V, self.d)

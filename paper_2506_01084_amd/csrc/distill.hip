@@ -1,0 +1,245 @@
+// Distillation over the extended vocabulary (gfx950): the loss of the joint softmax against a teacher's top logits, and its part of
+// the gradient with respect to the logits.
+//
+// Section 2.4 of the zip2zip paper trains on the compressed sequence with one target code per position; here the target is a
+// teacher's distribution q over K listed columns.  With p the joint softmax of section 2.3 at temperature T,
+//   kl[r] = sum_k q_k (ln q_k - ln p_{id_k}),   ln p_v = logit[r, v] / T - lse[r],   q = softmax over the listed teacher logits / T.
+// The log-sum-exp comes from the logits' kernels; only the K listed logits are needed besides.
+#include "logits_common.h"
+
+namespace {
+
+using namespace z2z_logits;
+
+struct TeacherArgs {
+  const int32_t* ids;       // [rows, K]
+  const float* teacher;     // [rows, K]
+  const int32_t* size;      // [sequences]
+  int32_t rows, rows_per_seq, V, cap, K;
+  float inv_t;
+};
+
+// A listed column this far below the best one (in logit / T) counts as nothing: e^-87 is next to the smallest normal number.
+constexpr float kLeast = -87.f;
+constexpr int T_PER_LANE = Z2Z_MAX_TEACHER / 64;
+
+// A row's teacher in a wave: lane l has columns l + 64 u.  q = 0 where nothing is listed.
+struct Teacher {
+  float q[T_PER_LANE], ln_q[T_PER_LANE];
+  int32_t id[T_PER_LANE];   // -1: nothing listed
+  bool some;                // the row has a distribution
+  bool outside;             // some of it lies on a column that does not exist
+};
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
+  return x;
+}
+
+__device__ __forceinline__ Teacher load_teacher(const TeacherArgs& a, int r, int columns) {
+  const int lane = threadIdx.x & 63;
+  Teacher t;
+  float x[T_PER_LANE], m = kNegInf;
+  bool nan = false;
+#pragma unroll
+  for (int u = 0; u < T_PER_LANE; ++u) {
+    const int k = lane + 64 * u;
+    t.id[u] = k < a.K ? a.ids[(size_t)r * a.K + k] : -1;
+    x[u] = t.id[u] >= 0 ? a.teacher[(size_t)r * a.K + k] : kNegInf;
+    if (t.id[u] < 0) t.id[u] = -1;
+    nan |= x[u] != x[u];
+    m = fmaxf(m, x[u]);
+  }
+  m = wave_max(m);
+  const bool any_nan = __ballot(nan) != 0ull;
+  t.some = m > kNegInf || any_nan;
+  float s = 0.f;
+#pragma unroll
+  for (int u = 0; u < T_PER_LANE; ++u) {
+    // (differences of the logits first: exact where they matter; an infinite maximum makes NaN)
+    t.ln_q[u] = t.some ? (x[u] - m) * a.inv_t : 0.f;
+    t.q[u] = t.some && t.id[u] >= 0 && !(t.ln_q[u] < kLeast) ? expf(t.ln_q[u]) : 0.f;
+    s += t.q[u];
+  }
+  s = wave_sum(s);
+  const float ln_s = logf(s);
+  bool outside = false;
+#pragma unroll
+  for (int u = 0; u < T_PER_LANE; ++u) {
+    t.ln_q[u] -= ln_s;
+    t.q[u] = t.id[u] >= 0 && t.some ? t.q[u] / s : 0.f;
+    outside |= t.id[u] >= columns && t.q[u] > 0.f;
+  }
+  t.outside = __ballot(outside) != 0ull;
+  return t;
+}
+
+template <bool BF16>
+__device__ __forceinline__ float dot16(const uint4& x, const uint4& y, float acc) {
+  const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (BF16) {
+      acc = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), acc);
+      acc = fmaf(__uint_as_float(xs[e] & 0xFFFF0000u), __uint_as_float(ys[e] & 0xFFFF0000u), acc);
+    } else {
+      acc = fmaf(__uint_as_float(xs[e]), __uint_as_float(ys[e]), acc);
+    }
+  }
+  return acc;
+}
+
+// One workgroup per hidden row: its four waves take the listed columns in turn, four at a time against one read of the hidden row; then
+// wave 0 has the loss.  Bound by the gather of K rows of W per hidden row (popular ones come out of the caches).
+template <bool BF16>
+__global__ void __launch_bounds__(256) teacher_loss_kernel(TeacherArgs a, const uint4* H, const uint4* W_base, const uint4* W_hyper, int d,
+                                                           const float* lse, float* kl, float* student) {
+  __shared__ float z_row[Z2Z_MAX_TEACHER];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = blockIdx.x, b = r / a.rows_per_seq;
+  const int columns = a.V + min(max(a.size[b], 0), a.cap);
+  const int n_chunks = d / (BF16 ? 8 : 4);
+  const uint4* h = H + (size_t)r * n_chunks;
+  constexpr int G = 4;
+  for (int k0 = wave * G; k0 < a.K; k0 += 4 * G) {
+    const uint4* w[G];
+    bool there[G];
+    float acc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int id = k0 + g < a.K ? a.ids[(size_t)r * a.K + k0 + g] : -1;
+      there[g] = id >= 0 && id < columns;
+      w[g] = !there[g] ? W_base : (id < a.V ? W_base + (size_t)id * n_chunks : W_hyper + ((size_t)b * a.cap + (id - a.V)) * n_chunks);
+      acc[g] = 0.f;
+    }
+    for (int c = lane; c < n_chunks; c += 64) {
+      const uint4 x = h[c];
+      uint4 y[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) y[g] = w[g][c];
+#pragma unroll
+      for (int g = 0; g < G; ++g) acc[g] = dot16<BF16>(x, y[g], acc[g]);
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      acc[g] = wave_sum(acc[g]);
+      if (lane == 0 && k0 + g < a.K) z_row[k0 + g] = there[g] ? acc[g] : 0.f;
+    }
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < a.K; k += 256) student[(size_t)r * a.K + k] = z_row[k];
+  if (wave != 0) return;
+  const Teacher t = load_teacher(a, r, columns);
+  const float l = lse[r];
+  float sum = 0.f;
+#pragma unroll
+  for (int u = 0; u < T_PER_LANE; ++u)
+    if (t.q[u] != 0.f) sum += t.q[u] * (t.ln_q[u] - fmaf(z_row[min(lane + 64 * u, a.K - 1)], a.inv_t, -l));
+  sum = wave_sum(sum);
+  if (lane == 0) kl[r] = !t.some ? 0.f : (t.outside ? INFINITY : sum);
+}
+
+// g[r] = the row's upstream gradient (1 without one) / T, 0 for rows without a distribution or with some of it on a column that
+// does not exist; targets[r] = -1: the probability epilogue takes no column out.
+__global__ void __launch_bounds__(256) teacher_grad_kernel(TeacherArgs a, const float* grad, float* g, int32_t* targets) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= a.rows) return;
+  const int columns = a.V + min(max(a.size[r / a.rows_per_seq], 0), a.cap);
+  const Teacher t = load_teacher(a, r, columns);
+  if ((threadIdx.x & 63) == 0) {
+    g[r] = t.some && !t.outside ? (grad ? grad[r] : 1.0f) * a.inv_t : 0.f;
+    targets[r] = -1;
+  }
+}
+
+// The listed columns of dZ = g (p - q), behind the kernel that has stored g p everywhere: p again from the row's own logits, so that the
+// difference is rounded once; a column listed several times has the sum of its q.  A wave per row.
+__global__ void __launch_bounds__(256) teacher_dz_kernel(TeacherArgs a, const float* lse, const float* student, const float* g, uint16_t* base,
+                                                         size_t ld_base, uint16_t* hyper, size_t ld_hyper) {
+  const int lane = threadIdx.x & 63;
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= a.rows) return;
+  const float gr = g[r];
+  if (gr == 0.f) return;
+  const int columns = a.V + min(max(a.size[r / a.rows_per_seq], 0), a.cap);
+  const Teacher t = load_teacher(a, r, columns);
+  float total[T_PER_LANE];
+#pragma unroll
+  for (int u = 0; u < T_PER_LANE; ++u) total[u] = 0.f;
+#pragma unroll
+  for (int v = 0; v < T_PER_LANE; ++v) {
+    if (64 * v >= a.K) break;
+    const int n = min(64, a.K - 64 * v);
+    for (int l = 0; l < n; ++l) {
+      const int id = __builtin_amdgcn_readlane(t.id[v], l);
+      const float q = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(t.q[v]), l));
+#pragma unroll
+      for (int u = 0; u < T_PER_LANE; ++u) total[u] += id == t.id[u] ? q : 0.f;
+    }
+  }
+  const float l = lse[r];
+#pragma unroll
+  for (int u = 0; u < T_PER_LANE; ++u) {
+    const int id = t.id[u];
+    if (id < 0 || id >= columns) continue;
+    const float p = expf(fmaf(student[(size_t)r * a.K + lane + 64 * u], a.inv_t, -l));
+    const uint16_t x = (uint16_t)pack_bf16(gr * (p - total[u]), 0.f);
+    if (id < a.V)
+      base[(size_t)r * ld_base + id] = x;
+    else
+      hyper[(size_t)r * ld_hyper + (id - a.V)] = x;
+  }
+}
+
+TeacherArgs teacher_args(const z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq) {
+  TeacherArgs a;
+  a.ids = t.ids + (size_t)r0 * t.K;
+  a.teacher = t.logits + (size_t)r0 * t.K;
+  a.size = c->st.size + r0 / rows_per_seq;
+  a.rows = rows;
+  a.rows_per_seq = rows_per_seq;
+  a.V = c->cfg.V;
+  a.cap = c->cfg.cap;
+  a.K = t.K;
+  a.inv_t = 1.0f / t.temperature;
+  return a;
+}
+
+}  // namespace
+
+int z2z_launch_extended_distill(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base, const void* W_hyper,
+                                const z2z_teacher& t, float* kl, float* lse, float* student, hipStream_t s) {
+  const int rc = z2z_launch_extended_logits(c, H, rows, rows_per_seq, W_base, W_hyper, nullptr, nullptr, lse, nullptr, s, false, t.temperature);
+  if (rc != Z2Z_OK) return rc;
+  const TeacherArgs a = teacher_args(c, t, 0, rows, rows_per_seq);
+  const uint4 *h = reinterpret_cast<const uint4*>(H), *wb = reinterpret_cast<const uint4*>(W_base), *wh = reinterpret_cast<const uint4*>(W_hyper);
+  if (c->cfg.dtype == Z2Z_BF16)
+    hipLaunchKernelGGL(teacher_loss_kernel<true>, dim3((unsigned)rows), dim3(256), 0, s, a, h, wb, wh, c->cfg.d, lse, kl, student);
+  else
+    hipLaunchKernelGGL(teacher_loss_kernel<false>, dim3((unsigned)rows), dim3(256), 0, s, a, h, wb, wh, c->cfg.d, lse, kl, student);
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}
+
+int z2z_launch_teacher_grad(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* grad, float* g, int32_t* targets,
+                            hipStream_t s) {
+  const TeacherArgs a = teacher_args(c, t, r0, rows, rows_per_seq);
+  hipLaunchKernelGGL(teacher_grad_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, grad ? grad + r0 : nullptr, g, targets);
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}
+
+int z2z_launch_teacher_dz(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* lse, const float* g, void* base,
+                          size_t ld_base, void* hyper, size_t ld_hyper, hipStream_t s) {
+  const TeacherArgs a = teacher_args(c, t, r0, rows, rows_per_seq);
+  hipLaunchKernelGGL(teacher_dz_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, lse + r0, t.student + (size_t)r0 * t.K, g,
+                     reinterpret_cast<uint16_t*>(base), ld_base, reinterpret_cast<uint16_t*>(hyper), ld_hyper);
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}

@@ -23,7 +23,7 @@ using namespace z2z_logits;
 template <int ROW_THREADS>
 __global__ void __launch_bounds__(256) logits_combine_kernel(const float* part_m, const float* part_s,
                                                              const int32_t* part_i, int n_parts, int rows,
-                                                             int32_t* argmax, float* mx, float* lse) {
+                                                             int32_t* argmax, float* mx, float* lse, float inv_t) {
   constexpr int ROWS_PER_BLOCK = 256 / ROW_THREADS;
   const int lane = threadIdx.x & 63;
   const int t = threadIdx.x % ROW_THREADS;
@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(256) logits_combine_kernel(const float* part_m
       o.m = part_m[base + p];
       o.s = part_s[base + p];
       o.i = part_i[base + p];
-      merge_triple(tr, o);
+      merge_triple(tr, o, inv_t);
     }
   }
 #pragma unroll
@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(256) logits_combine_kernel(const float* part_m
     o.m = __shfl_xor(tr.m, off);
     o.s = __shfl_xor(tr.s, off);
     o.i = __shfl_xor(tr.i, off);
-    merge_triple(tr, o);
+    merge_triple(tr, o, inv_t);
   }
   if (ROW_THREADS > 64) {
     __shared__ Triple xch[4];
@@ -53,23 +53,24 @@ __global__ void __launch_bounds__(256) logits_combine_kernel(const float* part_m
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
-      for (int w = 1; w < 4; ++w) merge_triple(tr, xch[w]);
+      for (int w = 1; w < 4; ++w) merge_triple(tr, xch[w], inv_t);
     }
   }
   if (t == 0 && r < rows) {
     if (argmax) argmax[r] = tr.i;
     if (mx) mx[r] = tr.m;
-    if (lse) lse[r] = tr.m + logf(tr.s);
+    if (lse) lse[r] = fmaf(tr.m, inv_t, logf(tr.s));
   }
 }
 
-int launch_combine(const z2z_parts& p, int n_parts, int rows, int32_t* argmax, float* mx, float* lse, hipStream_t s) {
+// (inv_t: of a softmax at a temperature, see LogitsArgs; the log-sum-exp is then that of logit / T)
+int launch_combine(const z2z_parts& p, int n_parts, int rows, int32_t* argmax, float* mx, float* lse, hipStream_t s, float inv_t = 1.f) {
   if (n_parts > 256)
     hipLaunchKernelGGL(logits_combine_kernel<256>, dim3(rows), dim3(256), 0, s, p.m, p.s, p.i, n_parts, rows, argmax,
-                       mx, lse);
+                       mx, lse, inv_t);
   else
     hipLaunchKernelGGL(logits_combine_kernel<64>, dim3((rows + 3) / 4), dim3(256), 0, s, p.m, p.s, p.i, n_parts, rows,
-                       argmax, mx, lse);
+                       argmax, mx, lse, inv_t);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
@@ -404,7 +405,7 @@ static size_t step_parts(const z2z_ctx* c) {
 
 int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                const void* W_hyper, int32_t* argmax, float* mx, float* lse, float* logits,
-                               hipStream_t s, bool use_static) {
+                               hipStream_t s, bool use_static, float temperature) {
   const int V = c->cfg.V, cap = c->cfg.cap;
   const bool timed = c->opt_timing && c->n_timed < Z2Z_MAX_TIMED && c->ev_created;
   z2z_parts parts;
@@ -423,13 +424,15 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
   // decode step: one hidden row per sequence -> the bandwidth-bound kernel (it can store the logits too).
   // Its base units serve 64 rows per pass over W_base, each pass at about the cost of the first; from the second
   // pass on the tile kernel takes the base vocabulary (all rows at once) and only the hyper units run here
-  const bool decode_step = rows_per_seq == 1 && c->decode_ready && c->opt_decode_kernel != 1;
+  // (at a temperature every part goes to the kernels whose folds take one)
+  const bool plain = temperature == 1.0f;
+  const bool decode_step = rows_per_seq == 1 && c->decode_ready && c->opt_decode_kernel != 1 && plain;
   const bool decode_split = decode_step && fast_ok && (rows > 64 || split_few(c, rows, false)) && c->opt_logits_kernel != 1;
   // a few rows per sequence (2..64: a verification step over drafted codes, a short chunk): every sequence's
   // W_hyper meets only its own rows, so the hyper part is bandwidth-bound like the decode step's; it goes to
   // that kernel's matrix-core units (one pass over each W_hyper), the base vocabulary to the tile kernel
   const bool seq_split = !decode_step && fast_ok && rows_per_seq >= 2 && rows_per_seq <= 64 && cap > 0 &&
-                         c->decode_ready && c->opt_decode_kernel != 1 && c->opt_logits_kernel != 1;
+                         c->decode_ready && plain && c->opt_decode_kernel != 1 && c->opt_logits_kernel != 1;
   if (decode_step && !decode_split) {
     int n_parts = z2z_logits_decode_parts(c);
     int rc = reserve((use_static ? (size_t)n_parts : step_parts(c)) * rows);
@@ -507,6 +510,7 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
   a.logits = logits;
   a.ld = V + cap;
   a.n_parts = n_parts;
+  set_softmax_temperature(a, temperature);
 
   if (!fast) {
     // both parts in one launch of the general kernel
@@ -526,7 +530,7 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
                          c->st.size);
       Z2Z_HIP_TRY(hipGetLastError());
     }
-    return launch_combine(parts, n_parts, rows, argmax, mx, lse, s);
+    return launch_combine(parts, n_parts, rows, argmax, mx, lse, s, a.inv_t);
   }
 
   // Both parts in one launch of the tile kernel (the measurement probes run the base part alone), up to 32768 tiles, where the hyper part is a hundredth
@@ -566,7 +570,7 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
     Z2Z_HIP_TRY(hipEventRecord(c->ev_stop[c->n_timed], s));
     c->n_timed++;
   }
-  return launch_combine(parts, n_parts, rows, argmax, mx, lse, s);
+  return launch_combine(parts, n_parts, rows, argmax, mx, lse, s, a.inv_t);
 }
 
 // Room for one row of logits per sequence, the row maxima and log-sum-exps.
@@ -632,6 +636,7 @@ static int launch_stored_logits(z2z_ctx* c, const void* H, int32_t rows, const v
     a.n_parts = n_parts;
     a.sample = 2;
     a.inv_temperature = 1.0f / sp.temperature;
+    set_softmax_temperature(a, 1.0f);
     a.logits = c->sample_logits;
     a.ld = c->cfg.V + c->cfg.cap;
     if (timed_pair) Z2Z_HIP_TRY(hipEventRecord(c->ev_start[c->n_timed], s));
@@ -704,6 +709,7 @@ int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t 
     a.n_parts = n_parts;
     a.sample = 1;
     a.inv_temperature = 1.0f / temperature;
+    set_softmax_temperature(a, 1.0f);
     a.key0 = (uint32_t)seed;
     a.key1 = (uint32_t)(seed >> 32);
     a.ctr2 = (uint32_t)step;

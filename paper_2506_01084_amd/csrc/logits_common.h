@@ -32,14 +32,14 @@ __device__ __forceinline__ Triple empty_triple() {
   return t;
 }
 
-// Merge b into a; equal maxima keep the lower column.
-__device__ __forceinline__ void merge_triple(Triple& a, const Triple& b) {
+// Merge b into a; equal maxima keep the lower column.  inv_t: of sums of exp((x - max) * inv_t), 1 unless the softmax has a temperature.
+__device__ __forceinline__ void merge_triple(Triple& a, const Triple& b, float inv_t = 1.f) {
   const bool b_wins = (b.m > a.m) || (b.m == a.m && b.i < a.i);
   const float hi = b_wins ? b.m : a.m;
   const float lo = b_wins ? a.m : b.m;
   const float s_hi = b_wins ? b.s : a.s;
   const float s_lo = b_wins ? a.s : b.s;
-  const float scale = (lo == kNegInf) ? 0.f : __expf(lo - hi);
+  const float scale = (lo == kNegInf) ? 0.f : __expf((lo - hi) * inv_t);
   a.s = s_hi + s_lo * scale;
   a.m = hi;
   a.i = b_wins ? b.i : a.i;
@@ -92,8 +92,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // multiply-add and one hardware exponential per logit.
 template <int NI, int NJ, bool TAIL>
 __device__ __forceinline__ void fold_tile_impl(const f32x16 (&acc)[NI][NJ], Triple (&run)[NJ], int col_base, int col0,
-                                               int n_valid) {
-  constexpr float kLog2e = 1.4426950408889634f;
+                                               int n_valid, float inv_t, float log2e_t) {
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
 #pragma unroll
@@ -112,19 +111,19 @@ __device__ __forceinline__ void fold_tile_impl(const f32x16 (&acc)[NI][NJ], Trip
         int targ = 15;
 #pragma unroll
         for (int v = 14; v >= 0; --v) targ = (x[v] == gmax) ? v : targ;
-        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf(run[j].m - gmax);
+        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf((run[j].m - gmax) * inv_t);
         run[j].m = gmax;
         run[j].i = col0 + col_base + i * 32 + (targ >> 2) * 8 + (targ & 3);
       }
       if (!TAIL || col_base + i * 32 < n_valid) {
         // (where nothing has been above -inf yet, columns that do not exist add 0 and a hidden row's NaN stay NaN; without a tail
         // every logit is finite or NaN, and so is the sum)
-        const float m2 = TAIL && run[j].m == kNegInf ? 0.f : -run[j].m * kLog2e;
+        const float m2 = TAIL && run[j].m == kNegInf ? 0.f : -run[j].m * log2e_t;
         float add0 = 0.f, add1 = 0.f;
 #pragma unroll
         for (int v = 0; v < 16; v += 2) {
-          add0 += __builtin_amdgcn_exp2f(fmaf(x[v], kLog2e, m2));
-          add1 += __builtin_amdgcn_exp2f(fmaf(x[v + 1], kLog2e, m2));
+          add0 += __builtin_amdgcn_exp2f(fmaf(x[v], log2e_t, m2));
+          add1 += __builtin_amdgcn_exp2f(fmaf(x[v + 1], log2e_t, m2));
         }
         run[j].s += add0 + add1;
       }
@@ -134,11 +133,11 @@ __device__ __forceinline__ void fold_tile_impl(const f32x16 (&acc)[NI][NJ], Trip
 
 template <int NI, int NJ>
 __device__ __forceinline__ void fold_tile(const f32x16 (&acc)[NI][NJ], Triple (&run)[NJ], int col_base, int col0,
-                                          int n_valid, bool tail) {
+                                          int n_valid, bool tail, float inv_t, float log2e_t) {
   if (tail)
-    fold_tile_impl<NI, NJ, true>(acc, run, col_base, col0, n_valid);
+    fold_tile_impl<NI, NJ, true>(acc, run, col_base, col0, n_valid, inv_t, log2e_t);
   else
-    fold_tile_impl<NI, NJ, false>(acc, run, col_base, col0, n_valid);
+    fold_tile_impl<NI, NJ, false>(acc, run, col_base, col0, n_valid, inv_t, log2e_t);
 }
 
 __device__ __forceinline__ uint32_t bf16_bits_rne(float f) {
@@ -258,7 +257,10 @@ struct LogitsArgs {
   int32_t act;            // 0 none, 1 GELU (erf)
   int32_t ldo;
   int32_t stream_f32;     // 1: residual and out are fp32 (a residual stream kept unrounded between layers)
-  // probability mode (the backward pass of the loss): out[r, c] = g[r] * (exp(logit - lse[r]) - [col0 + c == target[r]])
+  // softmax at a temperature (folds that draw nothing, probability mode): 1 / T, and log2(e) / T; 1 and log2(e) without one.  The triples'
+  // maxima are of the logits, their sums of exp((logit - max) / T)
+  float inv_t, log2e_t;
+  // probability mode (the backward pass of the loss): out[r, c] = g[r] * (exp(logit / T - lse[r]) - [col0 + c == target[r]])
   // for the existing columns c < n_valid, 0 for the other columns below ldo; bf16, row stride ldo
   const float* lse;       // [rows]
   const float* row_grad;  // [rows] g: the upstream gradient, 0 for rows without a usable target
@@ -295,6 +297,11 @@ struct LogitsArgs {
     int32_t ldo, cap, col0, strip, n_strips, part0, row_tiles, n_work, n_seq;
   } hyper;
 };
+
+inline void set_softmax_temperature(LogitsArgs& a, float temperature) {
+  a.inv_t = 1.0f / temperature;
+  a.log2e_t = (float)(1.4426950408889634 / temperature);
+}
 
 // Weights of up to this many bytes are read through the memory-side cache (256 MB), where the next step finds them; more
 // go past the caches (logits_decode.hip has the figures).

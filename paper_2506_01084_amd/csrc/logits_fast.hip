@@ -336,8 +336,7 @@ __device__ __forceinline__ void mask_tail16(Acc& acc, int col_base, int n_valid)
 // Fold one finished tile into the running triples, 16 values of a row at a time, in increasing column order per lane, so
 // strict comparisons keep the lowest column among equal maxima.  The running sum is kept against the running maximum in
 // base-2 units: exp(x - m) is one multiply-add and one hardware exponential.
-__device__ __forceinline__ void fold_tile16(const Acc& acc, Triple (&run)[F_N], int col_base, int col0, int n_valid) {
-  constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ void fold_tile16(const Acc& acc, Triple (&run)[F_N], int col_base, int col0, int n_valid, float inv_t, float log2e_t) {
 #pragma unroll
   for (int j = 0; j < F_N; ++j) {
 #pragma unroll
@@ -353,19 +352,19 @@ __device__ __forceinline__ void fold_tile16(const Acc& acc, Triple (&run)[F_N], 
         int targ = 15;
 #pragma unroll
         for (int v = 14; v >= 0; --v) targ = (x[v] == gmax) ? v : targ;
-        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf(run[j].m - gmax);
+        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf((run[j].m - gmax) * inv_t);
         run[j].m = gmax;
         run[j].i = col0 + col_base + h * 64 + (targ >> 2) * 16 + (targ & 3);
       }
       if (col_base + h * 64 < n_valid) {
         // (where nothing has been above -inf yet, columns that do not exist add 0 and a hidden row's NaN stay NaN.  The branch keeps
         // the groups apart: without it they are scheduled together and spill 48 bytes a lane.)
-        const float m2 = run[j].m == kNegInf ? 0.f : -run[j].m * kLog2e;
+        const float m2 = run[j].m == kNegInf ? 0.f : -run[j].m * log2e_t;
         float add0 = 0.f, add1 = 0.f;
 #pragma unroll
         for (int v = 0; v < 16; v += 2) {
-          add0 += __builtin_amdgcn_exp2f(fmaf(x[v], kLog2e, m2));
-          add1 += __builtin_amdgcn_exp2f(fmaf(x[v + 1], kLog2e, m2));
+          add0 += __builtin_amdgcn_exp2f(fmaf(x[v], log2e_t, m2));
+          add1 += __builtin_amdgcn_exp2f(fmaf(x[v + 1], log2e_t, m2));
         }
         run[j].s += add0 + add1;
       }
@@ -662,7 +661,7 @@ __device__ __forceinline__ void store_prob16(const Acc& acc, const LogitsArgs& a
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float z = read_acc(acc[i][j][e]);
-        const float p = __expf(z - lse[j]) - (col + e == tgt[j] ? 1.f : 0.f);
+        const float p = __expf(fmaf(z, a.inv_t, -lse[j])) - (col + e == tgt[j] ? 1.f : 0.f);
         x[e] = col + e < n_valid ? g[j] * p : 0.f;
       }
       o[i] = uint2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -688,11 +687,11 @@ struct Swap32 {
     y = r[1];
   }
 };
-__device__ __forceinline__ void merge(Triple& a, const Triple& b) { merge_triple(a, b); }
-__device__ __forceinline__ void merge(Draw& a, const Draw& b) { merge_draw(a, b); }
+__device__ __forceinline__ void merge(Triple& a, const Triple& b, float inv_t) { merge_triple(a, b, inv_t); }
+__device__ __forceinline__ void merge(Draw& a, const Draw& b, float) { merge_draw(a, b); }
 
 template <int N, typename R, typename S>
-__device__ __forceinline__ void merge_rows(R (&a)[F_N], S swap) {
+__device__ __forceinline__ void merge_rows(R (&a)[F_N], S swap, float inv_t = 1.f) {
   static_assert(sizeof(R) == 12, "three words");
 #pragma unroll
   for (int k = 0; k < N; ++k) {
@@ -704,7 +703,7 @@ __device__ __forceinline__ void merge_rows(R (&a)[F_N], S swap) {
     R other;
     __builtin_memcpy(&a[k], x, 12);
     __builtin_memcpy(&other, y, 12);
-    merge(a[k], other);
+    merge(a[k], other, inv_t);
   }
 }
 
@@ -1184,7 +1183,7 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
         fold_store16(acc, run, a, row_base, r_end, col_base, n_valid);
       } else {
         if ((vt + 1) * FT > n_valid) mask_tail16(acc, col_base, n_valid);
-        fold_tile16(acc, run, col_base, hyper ? a.hyper.col0 : a.col0, n_valid);
+        fold_tile16(acc, run, col_base, hyper ? a.hyper.col0 : a.col0, n_valid, a.inv_t, a.log2e_t);
       }
     }
     if (MODE >= 2 && MODE <= 5) continue;
@@ -1192,8 +1191,9 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
     // (each exchange halves a lane's rows: 6 merges and no shuffles, where every row merged in all lanes took 16 and 48 and three
     // lanes in four idled behind them.  32000 columns, 300 / 3500 rows, d = 64 33.1 -> 28.2, 92.4 -> 80.1 us, d = 1024 66.0 -> 61.4,
     // 246.9 -> 232.4)
-    merge_rows<4>(run, Swap16{});
-    merge_rows<2>(run, Swap32{});
+    const float inv_t = MODE < 2 ? a.inv_t : 1.f;    // (the draws' values are logit / T)
+    merge_rows<4>(run, Swap16{}, inv_t);
+    merge_rows<2>(run, Swap32{}, inv_t);
     if (MODE == 6) {
       merge_rows<4>(draw, Swap16{});
       merge_rows<2>(draw, Swap32{});
@@ -1214,7 +1214,7 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
     if (wv == 0) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        merge_triple(run[e], xch[hrow0 + e * 16]);
+        merge_triple(run[e], xch[hrow0 + e * 16], inv_t);
         const int hrow = r0 + hrow0 + e * 16;
         if (hrow < r_end) {
           const size_t q = (size_t)hrow * a.n_parts + (hyper ? a.hyper.part0 : a.part0) + st;

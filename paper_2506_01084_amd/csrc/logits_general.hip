@@ -102,7 +102,7 @@ __device__ __forceinline__ void fold_general(const f32x16 (&acc)[NI][2], Triple 
         if (STORE && col < n_valid && hrow < r_end) out[col] = x[v];
       }
       if (gmax > run[j].m) {
-        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf(run[j].m - gmax);
+        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf((run[j].m - gmax) * a.inv_t);
         run[j].m = gmax;
         run[j].i = a.col0 + col_base + i * 32 + (targ >> 2) * 8 + (targ & 3);
       }
@@ -111,7 +111,7 @@ __device__ __forceinline__ void fold_general(const f32x16 (&acc)[NI][2], Triple 
         const float m = run[j].m == kNegInf ? 0.f : run[j].m;
         float add = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) add += __expf(x[v] - m);
+        for (int v = 0; v < 16; ++v) add += __expf((x[v] - m) * a.inv_t);
         run[j].s += add;
       }
     }
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(256, per_cu(TV)) logits_general_kernel(General
     o.m = __shfl_xor(run[j].m, 32);
     o.s = __shfl_xor(run[j].s, 32);
     o.i = __shfl_xor(run[j].i, 32);
-    merge_triple(run[j], o);
+    merge_triple(run[j], o, a.inv_t);
   }
   __syncthreads();            // all waves are done reading the operand tiles
   Triple* xch = reinterpret_cast<Triple*>(lds);   // [2 row halves][64 rows]
@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(256, per_cu(TV)) logits_general_kernel(General
   if (wv == 0 && lane < 32) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      merge_triple(run[j], xch[wr * 64 + j * 32 + lane]);
+      merge_triple(run[j], xch[wr * 64 + j * 32 + lane], a.inv_t);
       const int hrow = r0 + wr * 64 + j * 32 + lane;
       if (hrow < r_end) {
         const size_t p = (size_t)hrow * a.n_parts + a.part0 + st;

@@ -115,7 +115,7 @@ __device__ __forceinline__ void store_prob_tile(const f32x16 (&acc)[1][NJV], con
       float x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p = __expf(read_acc(acc[0][j][q * 4 + e]) - lse) - (col + e == tgt ? 1.f : 0.f);
+        const float p = __expf(fmaf(read_acc(acc[0][j][q * 4 + e]), a.inv_t, -lse)) - (col + e == tgt ? 1.f : 0.f);
         x[e] = col + e < t.n_valid ? g * p : 0.f;
       }
       if (col < t.ldo)                     // (a multiple of 64)
@@ -329,14 +329,15 @@ __device__ __forceinline__ void mid_tile(const LogitsArgs& a, const MidTile& t, 
   else if (SMODE == 2 || SMODE == 6)
     fold_tile_store<1, NJV>(acc, run, a, 0, r_end, col_base, n_valid);
   else
-    fold_tile<1, NJV>(acc, run, col_base, t.col0, n_valid, v0 + TILE > n_valid);
+    fold_tile<1, NJV>(acc, run, col_base, t.col0, n_valid, v0 + TILE > n_valid, a.inv_t, a.log2e_t);
+  const float inv_t = SMODE == 0 || SMODE == 4 ? a.inv_t : 1.f;         // (the draws' values are logit / T)
 #pragma unroll
   for (int j = 0; j < NJV; ++j) {                          // lanes l and l + 32 hold the same hidden row
     Triple o;
     o.m = __shfl_xor(run[j].m, 32);
     o.s = __shfl_xor(run[j].s, 32);
     o.i = __shfl_xor(run[j].i, 32);
-    merge_triple(run[j], o);
+    merge_triple(run[j], o, inv_t);
     if (SMODE == 1 || SMODE == 5) {
       Draw od;
       od.v = __shfl_xor(draw[j].v, 32);
@@ -358,7 +359,7 @@ __device__ __forceinline__ void mid_tile(const LogitsArgs& a, const MidTile& t, 
   if (tid < nr) {
     Triple tr = xch[tid];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) merge_triple(tr, xch[w * M_HT + tid]);
+    for (int w = 1; w < WAVES; ++w) merge_triple(tr, xch[w * M_HT + tid], inv_t);
     const size_t p = (size_t)(t.row0 + tid) * a.n_parts + t.part;
     a.part_m[p] = tr.m;
     a.part_s[p] = tr.s;

@@ -79,10 +79,12 @@ int z2z_launch_hyper_embed_backward(z2z_ctx* c, const void* dW_hyper, float* dE,
 // forward kernel with another epilogue, using the forward pass's lse), then
 //   dH = dZ_base W_base + dZ_hyper[b] W_hyper[b],   dW_base = dZ_base^T H,   dW_hyper[b] = dZ_hyper[b]^T H[b]
 // are four dense products on the same MFMA kernel (the last and the second term, one per sequence, in a launch each), which reads
-// every operand as it is.
+// every operand as it is.  With a teacher the rows' targets are its listed columns (distill.hip): the epilogue stores g p everywhere, and a
+// small kernel behind it g (p - q) in those.
 int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                      const void* W_hyper, const int32_t* targets, const float* lse,
-                                     const float* grad_nll, void* dH, void* dW_base, void* dW_hyper, hipStream_t s) {
+                                     const float* grad_nll, void* dH, void* dW_base, void* dW_hyper, hipStream_t s,
+                                     const z2z_teacher* teacher) {
   const int B = c->cfg.B, V = c->cfg.V, cap = c->cfg.cap, d = c->cfg.d;
   if (c->cfg.dtype != Z2Z_BF16 || d % 64 != 0 || !c->fast_ready) return Z2Z_EUNSUPPORTED;
   const size_t Vp = round_up(V, 64), capp = round_up(cap, 64);
@@ -91,12 +93,13 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   // bf16 result of the earlier ones (one more rounding per chunk).
   // work space (bf16 unless noted), 256-byte aligned pieces
   size_t off = 0;
-  size_t o_g, o_Pb, o_Ph;
+  size_t o_g, o_t, o_Pb, o_Ph;
   auto take = [&](size_t bytes) { const size_t at = off; off += round_up(bytes, 256); return at; };
   auto layout = [&](int n_seq) {
     const size_t rc = (size_t)n_seq * rows_per_seq;
     off = 0;
     o_g = take(rc * 4);                              // float g[rows of the chunk]
+    o_t = teacher ? take(rc * 4) : 0;                // their targets: none
     o_Pb = take(rc * Vp * 2);                        // dZ, base columns      [rows, Vp]
     o_Ph = take(rc * capp * 2);                      // dZ, hyper columns     [rows, capp]
     return off;
@@ -116,6 +119,7 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   }
   unsigned char* ws = reinterpret_cast<unsigned char*>(c->bwd_ws);
   float* g = reinterpret_cast<float*>(ws + o_g);
+  int32_t* no_targets = reinterpret_cast<int32_t*>(ws + o_t);
   void *Pb = ws + o_Pb, *Ph = ws + o_Ph;
   // (nothing is folded over a strip here, and a workgroup's operand stream runs on from tile to tile anyway.  Tiles one by one, against
   // strips of four: base part of 1448 rows, V = 151936 1332 -> 1238 us, 109, V = 32064 237 -> 66, 32768, V = 128256 24.55 -> 24.39 ms;
@@ -130,8 +134,13 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
     const int r0 = b0 * rows_per_seq, rows_c = nb * rows_per_seq;
     const uint16_t* Hc = H16 + (size_t)r0 * d;
     const uint16_t* Whc = Wh16 + (size_t)b0 * cap * d;
-    hipLaunchKernelGGL(row_grad_kernel, dim3((rows_c + 255) / 256), dim3(256), 0, s, targets + r0,
-                       grad_nll ? grad_nll + r0 : nullptr, c->st.size + b0, rows_c, rows_per_seq, V, cap, g);
+    if (teacher) {
+      rc = z2z_launch_teacher_grad(c, *teacher, r0, rows_c, rows_per_seq, grad_nll, g, no_targets, s);
+      if (rc != Z2Z_OK) return rc;
+    } else {
+      hipLaunchKernelGGL(row_grad_kernel, dim3((rows_c + 255) / 256), dim3(256), 0, s, targets + r0,
+                         grad_nll ? grad_nll + r0 : nullptr, c->st.size + b0, rows_c, rows_per_seq, V, cap, g);
+    }
     // ---- dZ: the forward kernel with the probability epilogue -------------------------------------------
     // (up to 192 rows are bound by the weights' bytes, as in the forward pass: the streaming kernel)
     const bool few = c->opt_logits_kernel == 0 && z2z_logits_mid_ok(c, rows_c);
@@ -152,9 +161,10 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
       a.rows = nq * rows_per_seq;
       a.rows_per_seq = rows_per_seq;
       a.d = d;
+      set_softmax_temperature(a, teacher ? teacher->temperature : 1.0f);
       a.lse = lse + r0 + row;
       a.row_grad = g + row;
-      a.targets = targets + r0 + row;
+      a.targets = teacher ? no_targets + row : targets + r0 + row;
       a.out = reinterpret_cast<uint16_t*>(Pb) + row * Vp;
       a.ldo = (int)Vp;
       if (cap > 0) {
@@ -169,6 +179,10 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
       } else {
         rc = z2z_launch_logits_part(c, false, a, W_base, V, 0, 0, strip, nq * rows_per_seq, rows_per_seq, false, s, true);
       }
+      if (rc != Z2Z_OK) return rc;
+    }
+    if (teacher) {
+      rc = z2z_launch_teacher_dz(c, *teacher, r0, rows_c, rows_per_seq, lse, g, Pb, Vp, Ph, capp, s);
       if (rc != Z2Z_OK) return rc;
     }
     // ---- the products ------------------------------------------------------------------------------------------

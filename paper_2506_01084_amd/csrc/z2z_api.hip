@@ -52,6 +52,9 @@ void free_ctx(z2z_ctx* c) {
   delete c;
 }
 
+// (beyond this range the fp32 exponents of the softmax lose what they are to tell apart)
+bool temperature_ok(float t) { return t >= 0.0625f && t <= 1024.0f; }
+
 // A call that uses work buffers: on the context's device, and noted where it is captured into a graph.
 int enter(z2z_ctx* c, hipStream_t s) {
   int device = -1;
@@ -433,6 +436,43 @@ Z2Z_API int z2z_extended_nll_backward(z2z_ctx* ctx, const void* d_H, int32_t row
     return Z2Z_EINVAL;
   return z2z_launch_extended_nll_backward(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, d_targets, d_lse,
                                           d_grad_nll, d_dH, d_dW_base, d_dW_hyper, static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,
+                                 const void* d_W_hyper, int32_t n_teacher, const int32_t* d_ids, const float* d_teacher,
+                                 float temperature, float* d_kl, float* d_lse, float* d_student, void* stream) {
+  if (!ctx || !d_H || !d_W_base || !d_ids || !d_teacher || !d_kl || !d_lse || !d_student) return Z2Z_EINVAL;
+  if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
+  if (rows_per_seq < 1 || rows < 1 || n_teacher < 1) return Z2Z_EINVAL;
+  if ((long long)rows_per_seq * ctx->cfg.B != (long long)rows) return Z2Z_EINVAL;
+  if (!temperature_ok(temperature)) return Z2Z_EINVAL;
+  if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
+  if (n_teacher > Z2Z_MAX_TEACHER) return Z2Z_EUNSUPPORTED;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  const z2z_teacher t = {n_teacher, d_ids, d_teacher, temperature, nullptr};
+  return z2z_launch_extended_distill(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, t, d_kl, d_lse, d_student,
+                                     static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_extended_distill_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,
+                                          const void* d_W_hyper, int32_t n_teacher, const int32_t* d_ids, const float* d_teacher,
+                                          float temperature, const float* d_lse, const float* d_student, const float* d_grad_kl,
+                                          void* d_dH, void* d_dW_base, void* d_dW_hyper, void* stream) {
+  if (!ctx || !d_H || !d_W_base || !d_ids || !d_teacher || !d_lse || !d_student || !d_dH || !d_dW_base) return Z2Z_EINVAL;
+  if (ctx->cfg.cap > 0 && (!d_W_hyper || !d_dW_hyper)) return Z2Z_EINVAL;
+  if (rows_per_seq < 1 || rows < 1 || n_teacher < 1) return Z2Z_EINVAL;
+  if ((long long)rows_per_seq * ctx->cfg.B != (long long)rows) return Z2Z_EINVAL;
+  if (!temperature_ok(temperature)) return Z2Z_EINVAL;
+  if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper) || !aligned16(d_dH) || !aligned16(d_dW_base) ||
+      !aligned16(d_dW_hyper))
+    return Z2Z_EINVAL;
+  if (n_teacher > Z2Z_MAX_TEACHER) return Z2Z_EUNSUPPORTED;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  const z2z_teacher t = {n_teacher, d_ids, d_teacher, temperature, d_student};
+  return z2z_launch_extended_nll_backward(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, nullptr, d_lse, d_grad_kl, d_dH, d_dW_base,
+                                          d_dW_hyper, static_cast<hipStream_t>(stream), &t);
 }
 
 Z2Z_API int z2z_hyper_embed_backward(z2z_ctx* ctx, const void* d_dW_hyper, float* d_dE, void* stream) {

@@ -108,6 +108,15 @@ struct z2z_ctx {
   long long n_launch[Z2Z_N_KERNEL_FAMILIES];   // launches enqueued per logits kernel family
 };
 
+// What a row is distilled from (z2z_extended_distill).
+struct z2z_teacher {
+  int32_t K;
+  const int32_t* ids;      // [rows, K]
+  const float* logits;     // [rows, K]
+  float temperature;
+  const float* student;    // [rows, K] the student's logits there (backward)
+};
+
 // launchers (each validates nothing: the C-ABI layer has done so)
 int z2z_lzw_prepare(z2z_ctx* c);   // raises the dynamic-LDS ceiling of the parse kernels
 int z2z_launch_lzw_reset(z2z_ctx* c, hipStream_t s);
@@ -128,7 +137,7 @@ int z2z_launch_hyper_embed(z2z_ctx* c, const void* E, void* W_hyper, const int32
 // do not fit) instead of the context's growable buffers
 int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                const void* W_hyper, int32_t* argmax, float* mx, float* lse, float* logits,
-                               hipStream_t s, bool use_static = false);
+                               hipStream_t s, bool use_static = false, float temperature = 1.0f);
 int z2z_static_scratch_prepare(z2z_ctx* c);   // z2z_create: look up the static array's address on c->device
 int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                const void* W_hyper, float temperature, int32_t top_k, float top_p, uint64_t seed,
@@ -136,7 +145,8 @@ int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t 
 int z2z_sample_truncated_prepare(z2z_ctx* c);
 int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                      const void* W_hyper, const int32_t* targets, const float* lse,
-                                     const float* grad_nll, void* dH, void* dW_base, void* dW_hyper, hipStream_t s);
+                                     const float* grad_nll, void* dH, void* dW_base, void* dW_hyper, hipStream_t s,
+                                     const z2z_teacher* teacher = nullptr);
 int z2z_launch_hyper_embed_backward(z2z_ctx* c, const void* dW_hyper, float* dE, hipStream_t s);
 bool z2z_hyper_encode_ok(const z2z_ctx* c, const z2z_encoder* enc);
 int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, void* W_hyper, const int32_t* first,
@@ -150,6 +160,13 @@ int z2z_launch_embed_codes(z2z_ctx* c, const int32_t* codes, const int32_t* n_co
                            float scale, void* X, int32_t* status, hipStream_t s);
 int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride, float scale, const void* dX,
                                     int32_t flags, float* dE, void* dW_hyper, hipStream_t s);
+int z2z_launch_extended_distill(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base, const void* W_hyper,
+                                const z2z_teacher& t, float* kl, float* lse, float* student, hipStream_t s);
+// For the backward pass, rows [r0, r0 + rows): the row gradients and targets of the probability epilogue; behind it the listed columns of dZ.
+int z2z_launch_teacher_grad(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* grad, float* g, int32_t* targets,
+                            hipStream_t s);
+int z2z_launch_teacher_dz(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* lse, const float* g, void* base,
+                          size_t ld_base, void* hyper, size_t ld_hyper, hipStream_t s);
 int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
                              int32_t picks, int32_t* parent, int32_t* code, float* picked, hipStream_t s);
 // The pick from stored logits [B, V + cap] and the largest of each part of base_columns / hyper_columns columns (powers of two).

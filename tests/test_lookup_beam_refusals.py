@@ -96,3 +96,49 @@ stub.stub_capacity(stub.stub_used())
 assert pick(c=fresh) == api.E_NOMEM
 clean()
 """)
+
+
+def test_distill_refusals(without_a_device):
+    without_a_device("""
+h = context(B=4, V=1000, M=3, cap=100, d=128)
+Q = P + 8
+fwd = lambda c=h, H=P, rows=40, rps=10, Wb=P, Wh=P, K=8, ids=P, t=P, T=2.0, kl=P, lse=P, st=P: lib.z2z_extended_distill(c, H, rows, rps, Wb, Wh, K, ids, t, T, kl, lse, st, None)
+bwd = lambda c=h, H=P, rows=40, rps=10, Wb=P, Wh=P, K=8, ids=P, t=P, T=2.0, lse=P, st=P, g=P, dH=P, dWb=P, dWh=P: lib.z2z_extended_distill_backward(c, H, rows, rps, Wb, Wh, K, ids, t, T, lse, st, g, dH, dWb, dWh, None)
+common = [dict(c=None), dict(H=None), dict(Wb=None), dict(Wh=None), dict(ids=None), dict(t=None), dict(lse=None), dict(st=None), dict(rows=0), dict(rows=41),
+          dict(rps=0), dict(K=0), dict(K=-3), dict(T=0.0), dict(T=-1.0), dict(T=0.06), dict(T=1025.0), dict(T=float("nan")), dict(T=float("inf")),
+          dict(H=Q), dict(Wb=Q), dict(Wh=Q)]
+for bad in common + [dict(kl=None)]:
+    assert fwd(**bad) == api.E_INVAL, bad
+for bad in common + [dict(dH=None), dict(dWb=None), dict(dWh=None), dict(dH=Q), dict(dWb=Q), dict(dWh=Q)]:
+    assert bwd(**bad) == api.E_INVAL, bad
+assert fwd(K=257) == api.E_UNSUPPORTED and bwd(K=257) == api.E_UNSUPPORTED
+f32 = context(B=4, V=1000, M=3, cap=100, d=128, dtype=api.F32)
+assert bwd(c=f32) == api.E_UNSUPPORTED and bwd(c=context(B=4, V=1000, M=3, cap=100, d=72)) == api.E_UNSUPPORTED
+assert launches() == []
+assert fwd() == 0 and fwd(K=256) == 0 and fwd(c=f32) == 0 and bwd() == 0 and bwd(g=None) == 0
+log = launches()
+assert len(named(log, "teacher_loss")) == 3 and len(named(log, "teacher_dz")) == 2 and not named(log, "row_grad"), log
+clean()
+fresh = context(B=4, V=1000, M=3, cap=100, d=128)
+stub.stub_capturing(1)
+assert fwd(c=fresh) == api.E_CAPTURE and bwd(c=fresh) == api.E_CAPTURE and launches() == []
+stub.stub_capturing(0)
+stub.stub_capacity(stub.stub_used())
+assert fwd(c=fresh) == api.E_NOMEM and bwd(c=fresh) == api.E_NOMEM
+clean()
+""")
+
+
+def test_a_temperature_leaves_the_decode_kernels(without_a_device):
+    """At T = 1 the log-sum-exp comes from the kernels that extended_nll takes, at another T from those whose folds take one."""
+    without_a_device("""
+for rps in (1, 5, 100):
+    h = context(B=8, V=40000, M=3, cap=1024, d=256)
+    fwd = lambda T: lib.z2z_extended_distill(h, P, 8 * rps, rps, P, P, 4, P, P, T, P, P, P, None)
+    assert lib.z2z_extended_nll(h, P, 8 * rps, rps, P, P, P, P, P, None) == 0
+    nll = [n for n, _ in launches() if "logits_" in n]
+    assert fwd(1.0) == 0
+    assert [n for n, _ in launches() if "logits_" in n] == nll
+    assert fwd(2.0) == 0
+    assert not named(launches(), "logits_decode")
+""")
