@@ -244,10 +244,15 @@ __global__ void __launch_bounds__(1024) sort_place_kernel(LookupArgs a, uint32_t
   }
   uint32_t total = 0u, before = 0u;
   if (tid < digits)
-    for (int t = 0; t < tiles; ++t) {
-      const uint32_t x = count[(size_t)t * digits + tid];
-      total += x;
-      before += t < (int)blockIdx.x ? x : 0u;
+    for (int t0 = 0; t0 < tiles; t0 += 8) {          // (eight loads on the way at a time)
+      uint32_t x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = count[(size_t)min(t0 + u, tiles - 1) * digits + tid];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        total += t0 + u < tiles ? x[u] : 0u;
+        before += t0 + u < (int)blockIdx.x ? x[u] : 0u;
+      }
     }
   uint32_t incl = total;
 #pragma unroll
@@ -274,29 +279,38 @@ __global__ void __launch_bounds__(1024) sort_place_kernel(LookupArgs a, uint32_t
 }
 
 // ---- gradient: sums over runs of equal keys -----------------------------------------------------------------------------------
-constexpr int R_PIECE = 32;               // sorted positions of a wave
+// What is summed up, and where to (KIND):
+//   LOOKUP_BF16, LOOKUP_F32   the rows of dX, a position's own each; base rows are fp32
+//   WEIGHTED                  weight[position] times row position / per_row of a bf16 matrix; base rows are bf16, everything is added
+enum { LOOKUP_BF16 = 0, LOOKUP_F32 = 1, WEIGHTED = 2 };
+
+// Sorted positions of a wave.  A piece's sums that cross its ends go through memory, so few positions are short of work for long
+// pieces, and many (a teacher's list has K a row) of memory for short ones.
+constexpr int piece_of(int kind) { return kind == WEIGHTED ? 64 : 32; }
 
 struct GradArgs {
   const u32x4* dX;
+  const float* weight;
   const uint32_t* skey;
   const uint32_t* spos;
-  float* dE;
+  void* dE;
   void* dW;
   float* head;                            // [pieces, d]: the sum of a run that began in an earlier piece
   float* tail;                            // [pieces, d]: the sum of a run that begins here and goes on
   uint32_t n, pieces, V, sentinel;
-  int32_t chunks, slices, d, add, fill_blocks;
+  int32_t chunks, slices, d, add, fill_blocks, per_row;
   float scale;
 };
 
 // N consecutive features of a table row := (+=) scale * sum.
-template <bool BF16, int N>
+template <int KIND, int N>
 __device__ __forceinline__ void store_row(const GradArgs& a, uint32_t key, size_t at, const float (&sum)[N]) {
   float x[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = sum[e] * a.scale;
-  if (key < a.V || !BF16) {
-    float4* to = reinterpret_cast<float4*>((key < a.V ? a.dE + (size_t)key * a.d : reinterpret_cast<float*>(a.dW) + (size_t)(key - a.V) * a.d) + at);
+  const size_t row = key < a.V ? (size_t)key * a.d : (size_t)(key - a.V) * a.d;
+  if (KIND == LOOKUP_F32 || (KIND == LOOKUP_BF16 && key < a.V)) {
+    float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(key < a.V ? a.dE : a.dW) + row + at);
 #pragma unroll
     for (int q = 0; q < N / 4; ++q) {
       float4 o = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
@@ -308,7 +322,7 @@ __device__ __forceinline__ void store_row(const GradArgs& a, uint32_t key, size_
     }
     return;
   }
-  uint2* to = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.dW) + (size_t)(key - a.V) * a.d + at);
+  uint2* to = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(key < a.V ? a.dE : a.dW) + row + at);
 #pragma unroll
   for (int q = 0; q < N / 4; ++q) {
     if (a.add) {
@@ -333,12 +347,13 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* skey, uint32_t l
 }
 
 // Blocks [0, fill_blocks) write zeros to the table rows that no position names: a wave per 16 rows, each looked up by a
-// lane.  The others: a wave per R_PIECE sorted positions and 64 pieces of 16 bytes of their rows, eight rows requested at a
+// lane.  The others: a wave per piece of sorted positions and 64 times 16 bytes of their rows, eight rows requested at a
 // time, added in fp32 in order.  Runs inside the piece are stored, what crosses its ends is left for join_kernel.
-template <bool BF16>
+template <int KIND>
 __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   const int lane = threadIdx.x & 63;
-  constexpr int EPC = BF16 ? 8 : 4;
+  constexpr bool BF16 = KIND != LOOKUP_F32;
+  constexpr int EPC = BF16 ? 8 : 4, PIECE = piece_of(KIND);
   if ((int)blockIdx.x < a.fill_blocks) {
     const uint32_t first = ((uint32_t)blockIdx.x * 4u + (threadIdx.x >> 6)) * 16u;
     const uint32_t key = first + (uint32_t)(lane & 15);
@@ -363,10 +378,15 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   if (piece >= a.pieces) return;
   const int chunk = (int)(wid % (uint32_t)a.slices) * 64 + lane;
   const bool on = chunk < a.chunks;
-  const uint32_t p0 = piece * R_PIECE;
-  const int cnt = (int)min((uint32_t)R_PIECE, a.n - p0);
+  const uint32_t p0 = piece * PIECE;
+  const int cnt = (int)min((uint32_t)PIECE, a.n - p0);
   const uint32_t my_key = lane < cnt ? a.skey[p0 + lane] : kNoKey;
-  const uint32_t my_pos = lane < cnt ? a.spos[p0 + lane] : 0u;
+  uint32_t my_pos = lane < cnt ? a.spos[p0 + lane] : 0u;
+  float my_weight = 1.f;
+  if (KIND == WEIGHTED) {
+    my_weight = a.weight[my_pos];
+    my_pos /= (uint32_t)a.per_row;
+  }
   uint32_t key = __builtin_amdgcn_readfirstlane(my_key);
   if (key >= a.sentinel) return;
   const uint32_t prev = p0 > 0u ? a.skey[p0 - 1] : kNoKey, next = p0 + cnt < a.n ? a.skey[p0 + cnt] : kNoKey;
@@ -375,7 +395,7 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
 #pragma unroll
   for (int e = 0; e < EPC; ++e) acc[e] = 0.f;
   const u32x4* column = a.dX + min(chunk, a.chunks - 1);
-  for (int i0 = 0; i0 < R_PIECE; i0 += 8) {
+  for (int i0 = 0; i0 < PIECE; i0 += 8) {
     if (i0 >= cnt) break;
     u32x4 x[8];
 #pragma unroll
@@ -385,9 +405,13 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
       const int i = i0 + u;
       if (i >= cnt) break;
       if (key >= a.sentinel) return;                 // (positions that name nothing stand at the end)
+      const float w = KIND == WEIGHTED ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(my_weight), i)) : 1.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (BF16) {
+        if (KIND == WEIGHTED) {
+          acc[2 * e] = fmaf(w, lo_bf16(x[u][e]), acc[2 * e]);
+          acc[2 * e + 1] = fmaf(w, hi_bf16(x[u][e]), acc[2 * e + 1]);
+        } else if (BF16) {
           acc[2 * e] += lo_bf16(x[u][e]);
           acc[2 * e + 1] += hi_bf16(x[u][e]);
         } else {
@@ -395,7 +419,7 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
         }
       }
       const bool last = i + 1 == cnt;
-      const uint32_t after = last ? next : (uint32_t)__builtin_amdgcn_readlane(my_key, min(i + 1, R_PIECE - 1));
+      const uint32_t after = last ? next : (uint32_t)__builtin_amdgcn_readlane(my_key, min(i + 1, PIECE - 1));
       if (last || after != key) {
         const bool goes_on = last && after == key;
         if (on) {
@@ -404,7 +428,7 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
 #pragma unroll
             for (int q = 0; q < EPC / 4; ++q) to[q] = float4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
           } else {
-            store_row<BF16, EPC>(a, key, (size_t)chunk * EPC, acc);
+            store_row<KIND, EPC>(a, key, (size_t)chunk * EPC, acc);
           }
         }
 #pragma unroll
@@ -418,14 +442,15 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
 
 // A run over several pieces: block (p, y) joins the run that begins in piece p and goes on, 256 features of it.  Its four waves add a quarter of
 // the pieces each, in order, and the quarters in order.
-template <bool BF16>
+template <int KIND>
 __global__ void __launch_bounds__(256) join_kernel(GradArgs a) {
   __shared__ float4 part[4][64];
-  const uint32_t p = blockIdx.x, p0 = p * R_PIECE, p1 = p0 + R_PIECE;
+  constexpr uint32_t PIECE = piece_of(KIND);
+  const uint32_t p = blockIdx.x, p0 = p * PIECE, p1 = p0 + PIECE;
   if (p1 >= a.n) return;
   const uint32_t key = a.skey[p1 - 1];
   if (key >= a.sentinel || a.skey[p1] != key || (p0 > 0u && a.skey[p0] == key && a.skey[p0 - 1] == key)) return;
-  const uint32_t end = lower_bound(a.skey, p1, a.n, key + 1u), q1 = (end - 1u) / R_PIECE;      // the run's last piece
+  const uint32_t end = lower_bound(a.skey, p1, a.n, key + 1u), q1 = (end - 1u) / PIECE;      // the run's last piece
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int f = (int)blockIdx.y * 256 + lane * 4;
   const bool on = f < a.d;
@@ -455,7 +480,7 @@ __global__ void __launch_bounds__(256) join_kernel(GradArgs a) {
       sum.w += x.w;
     }
     const float s[4] = {sum.x, sum.y, sum.z, sum.w};
-    store_row<BF16, 4>(a, key, (size_t)f, s);
+    store_row<KIND, 4>(a, key, (size_t)f, s);
   }
 }
 
@@ -493,79 +518,125 @@ int z2z_launch_embed_codes(z2z_ctx* c, const int32_t* codes, const int32_t* n_co
   return Z2Z_OK;
 }
 
-int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride, float scale, const void* dX,
-                                    int32_t flags, float* dE, void* dW_hyper, hipStream_t s) {
-  const LookupArgs a = lookup_args(c, codes, n_codes, stride);
-  const long long positions = (long long)a.B * stride, keys = (long long)a.V + (long long)a.B * a.cap;
+namespace {
+
+// How the work space of a sum by rows is laid out, and what its sort takes.
+struct SumPlan {
+  uint32_t n, tiles, pieces;
+  int bits, passes;
+  bool small;
+  size_t o_key[2], o_pos[2], o_count, o_head, o_tail, bytes;
+};
+
+bool plan_sum(const z2z_ctx* c, long long positions, int piece, SumPlan* p) {
+  const long long keys = (long long)c->cfg.V + (long long)c->cfg.B * c->cfg.cap;
   // (positions and rows of the joint table are 32-bit numbers here)
-  if (positions > 0x7FFFFFFFLL || keys > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
-  const uint32_t n = (uint32_t)positions;
-  const bool bf16 = c->cfg.dtype == Z2Z_BF16, add = flags == Z2Z_GRAD_ADD;
-  if (n == 0u && add) return Z2Z_OK;
+  if (positions > 0x7FFFFFFFLL || keys > 0x7FFFFFFFLL) return false;
+  p->n = (uint32_t)positions;
   int key_bits = 1;
   while ((keys >> key_bits) != 0) ++key_bits;        // (the sentinel is a key, too)
-  const int passes = (key_bits + 9) / 10, bits = (key_bits + passes - 1) / passes;
-  const uint32_t tiles = (n + S_TILE - 1) / S_TILE, pieces = (n + R_PIECE - 1) / R_PIECE;
-  // work space: sorted keys and positions (twice where the passes go through memory), the tiles' counts, sums that cross pieces
-  size_t off = 0;
-  auto take = [&](size_t bytes) { const size_t at = off; off += (bytes + 255) / 256 * 256; return at; };
-  const bool small = n <= (uint32_t)S_TILE;
-  const size_t o_key[2] = {take((size_t)n * 4), small ? 0 : take((size_t)n * 4)};
-  const size_t o_pos[2] = {take((size_t)n * 4), small ? 0 : take((size_t)n * 4)};
-  const size_t o_count = small ? 0 : take((size_t)tiles * (1u << bits) * 4);
-  const size_t o_head = pieces > 1 ? take((size_t)pieces * c->cfg.d * 4) : 0;
-  const size_t o_tail = pieces > 1 ? take((size_t)pieces * c->cfg.d * 4) : 0;
-  const int rc = z2z_work_reserve(c, &c->lookup_ws, off, s);
-  if (rc != Z2Z_OK) return rc;
-  unsigned char* ws = reinterpret_cast<unsigned char*>(c->lookup_ws.p);
+  p->passes = (key_bits + 9) / 10;
+  p->bits = (key_bits + p->passes - 1) / p->passes;
+  p->tiles = (p->n + S_TILE - 1) / S_TILE;
+  p->pieces = (p->n + piece - 1) / piece;
+  p->small = p->n <= (uint32_t)S_TILE;
+  // sorted keys and positions (twice where the passes go through memory), the tiles' counts, sums that cross pieces
+  p->bytes = 0;
+  auto take = [&](size_t bytes) { const size_t at = p->bytes; p->bytes += (bytes + 255) / 256 * 256; return at; };
+  for (int k = 0; k < 2; ++k) {
+    p->o_key[k] = k == 0 || !p->small ? take((size_t)p->n * 4) : 0;
+    p->o_pos[k] = k == 0 || !p->small ? take((size_t)p->n * 4) : 0;
+  }
+  p->o_count = p->small ? 0 : take((size_t)p->tiles * (1u << p->bits) * 4);
+  p->o_head = p->pieces > 1 ? take((size_t)p->pieces * c->cfg.d * 4) : 0;
+  p->o_tail = p->pieces > 1 ? take((size_t)p->pieces * c->cfg.d * 4) : 0;
+  return true;
+}
+
+// Sort the positions, sum up the runs, join those that cross pieces.  g: what is summed and where to.
+template <int KIND>
+int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned char* ws, GradArgs g, hipStream_t s) {
   auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
   int from = 0;
-  if (n == 0u) {
+  if (p.n == 0u) {
     // (nothing to sort: zeros alone)
-  } else if (small) {
-    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(1024), 0, s, a, n, bits, passes, words(o_key[0]), words(o_pos[0]));
+  } else if (p.small) {
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(1024), 0, s, a, p.n, p.bits, p.passes, words(p.o_key[0]), words(p.o_pos[0]));
   } else {
-    for (int p = 0; p < passes; ++p) {
-      const uint32_t *key_in = p > 0 ? words(o_key[from]) : nullptr, *pos_in = p > 0 ? words(o_pos[from]) : nullptr;
-      const int to = p > 0 ? from ^ 1 : 0;
-      hipLaunchKernelGGL(sort_count_kernel, dim3(tiles), dim3(1024), 0, s, a, n, key_in, p * bits, bits, words(o_count));
-      hipLaunchKernelGGL(sort_place_kernel, dim3(tiles), dim3(1024), 0, s, a, n, key_in, pos_in, p * bits, bits, words(o_count),
-                         words(o_key[to]), words(o_pos[to]));
+    for (int k = 0; k < p.passes; ++k) {
+      const uint32_t *key_in = k > 0 ? words(p.o_key[from]) : nullptr, *pos_in = k > 0 ? words(p.o_pos[from]) : nullptr;
+      const int to = k > 0 ? from ^ 1 : 0;
+      hipLaunchKernelGGL(sort_count_kernel, dim3(p.tiles), dim3(1024), 0, s, a, p.n, key_in, k * p.bits, p.bits, words(p.o_count));
+      hipLaunchKernelGGL(sort_place_kernel, dim3(p.tiles), dim3(1024), 0, s, a, p.n, key_in, pos_in, k * p.bits, p.bits, words(p.o_count),
+                         words(p.o_key[to]), words(p.o_pos[to]));
       from = to;
     }
   }
-  GradArgs g;
-  memset(&g, 0, sizeof(g));
-  g.dX = reinterpret_cast<const u32x4*>(dX);
-  g.skey = n ? words(o_key[from]) : nullptr;
-  g.spos = n ? words(o_pos[from]) : nullptr;
-  g.dE = dE;
-  g.dW = dW_hyper;
-  g.head = pieces > 1 ? reinterpret_cast<float*>(ws + o_head) : nullptr;
-  g.tail = pieces > 1 ? reinterpret_cast<float*>(ws + o_tail) : nullptr;
-  g.n = n;
-  g.pieces = pieces;
+  g.skey = p.n ? words(p.o_key[from]) : nullptr;
+  g.spos = p.n ? words(p.o_pos[from]) : nullptr;
+  g.head = p.pieces > 1 ? reinterpret_cast<float*>(ws + p.o_head) : nullptr;
+  g.tail = p.pieces > 1 ? reinterpret_cast<float*>(ws + p.o_tail) : nullptr;
+  g.n = p.n;
+  g.pieces = p.pieces;
   g.V = (uint32_t)a.V;
   g.sentinel = a.sentinel;
   g.chunks = a.chunks;
   g.slices = (a.chunks + 63) / 64;
   g.d = c->cfg.d;
-  g.add = add ? 1 : 0;
-  g.fill_blocks = add ? 0 : (int)((keys + 63) / 64);
-  g.scale = scale;
-  const long long blocks = g.fill_blocks + ((long long)pieces * g.slices + 3) / 4;
+  g.fill_blocks = g.add ? 0 : (int)(((long long)a.sentinel + 63) / 64);
+  const long long blocks = g.fill_blocks + ((long long)p.pieces * g.slices + 3) / 4;
   if (blocks > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
-  if (bf16)
-    hipLaunchKernelGGL(reduce_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, s, g);
-  else
-    hipLaunchKernelGGL(reduce_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, s, g);
-  if (pieces > 1) {
-    const dim3 grid(pieces, (unsigned)((c->cfg.d + 255) / 256));
-    if (bf16)
-      hipLaunchKernelGGL(join_kernel<true>, grid, dim3(256), 0, s, g);
-    else
-      hipLaunchKernelGGL(join_kernel<false>, grid, dim3(256), 0, s, g);
-  }
+  hipLaunchKernelGGL(reduce_kernel<KIND>, dim3((unsigned)blocks), dim3(256), 0, s, g);
+  if (p.pieces > 1)
+    hipLaunchKernelGGL(join_kernel<KIND>, dim3(p.pieces, (unsigned)((c->cfg.d + 255) / 256)), dim3(256), 0, s, g);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
+}
+
+}  // namespace
+
+int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int32_t* n_codes, int32_t stride, float scale, const void* dX,
+                                    int32_t flags, float* dE, void* dW_hyper, hipStream_t s) {
+  const bool add = flags == Z2Z_GRAD_ADD;
+  SumPlan p;
+  if (!plan_sum(c, (long long)c->cfg.B * stride, piece_of(LOOKUP_BF16), &p)) return Z2Z_EUNSUPPORTED;
+  if (p.n == 0u && add) return Z2Z_OK;
+  const int rc = z2z_work_reserve(c, &c->lookup_ws, p.bytes, s);
+  if (rc != Z2Z_OK) return rc;
+  GradArgs g;
+  memset(&g, 0, sizeof(g));
+  g.dX = reinterpret_cast<const u32x4*>(dX);
+  g.dE = dE;
+  g.dW = dW_hyper;
+  g.add = add ? 1 : 0;
+  g.scale = scale;
+  unsigned char* ws = reinterpret_cast<unsigned char*>(c->lookup_ws.p);
+  const LookupArgs a = lookup_args(c, codes, n_codes, stride);
+  return c->cfg.dtype == Z2Z_BF16 ? launch_sum<LOOKUP_BF16>(c, a, p, ws, g, s) : launch_sum<LOOKUP_F32>(c, a, p, ws, g, s);
+}
+
+int z2z_weighted_rows_reserve(z2z_ctx* c, long long rows, int per_row, float** weight, hipStream_t s) {
+  SumPlan p;
+  if (!plan_sum(c, rows * per_row, piece_of(WEIGHTED), &p)) return Z2Z_EUNSUPPORTED;
+  const int rc = z2z_work_reserve(c, &c->lookup_ws, p.bytes + (size_t)p.n * sizeof(float), s);
+  if (rc != Z2Z_OK) return rc;
+  *weight = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(c->lookup_ws.p) + p.bytes);
+  return Z2Z_OK;
+}
+
+int z2z_launch_weighted_rows(z2z_ctx* c, const int32_t* ids, long long rows, int per_row, const float* weight, const void* H, void* dW_base,
+                             void* dW_hyper, hipStream_t s) {
+  SumPlan p;
+  if (!plan_sum(c, rows * per_row, piece_of(WEIGHTED), &p)) return Z2Z_EUNSUPPORTED;
+  GradArgs g;
+  memset(&g, 0, sizeof(g));
+  g.dX = reinterpret_cast<const u32x4*>(H);
+  g.weight = weight;
+  g.dE = dW_base;
+  g.dW = dW_hyper;
+  g.add = 1;
+  g.per_row = per_row;
+  g.scale = 1.0f;
+  const LookupArgs a = lookup_args(c, ids, nullptr, (int32_t)(rows / c->cfg.B * per_row));     // (a sequence's lists behind each other)
+  return launch_sum<WEIGHTED>(c, a, p, reinterpret_cast<unsigned char*>(c->lookup_ws.p), g, s);
 }

@@ -79,8 +79,11 @@ int z2z_launch_hyper_embed_backward(z2z_ctx* c, const void* dW_hyper, float* dE,
 // forward kernel with another epilogue, using the forward pass's lse), then
 //   dH = dZ_base W_base + dZ_hyper[b] W_hyper[b],   dW_base = dZ_base^T H,   dW_hyper[b] = dZ_hyper[b]^T H[b]
 // are four dense products on the same MFMA kernel (the last and the second term, one per sequence, in a launch each), which reads
-// every operand as it is.  With a teacher the rows' targets are its listed columns (distill.hip): the epilogue stores g p everywhere, and a
-// small kernel behind it g (p - q) in those.
+// every operand as it is.
+// With a teacher dZ = g (p - q) is large in its listed columns, where q is, and small everywhere else; rounded to bf16, those few values would
+// carry nearly all of the products' error.  They stay fp32 (weight) and out of the matrix: the epilogue stores g p, a small kernel behind it
+// zeros in the listed columns, and the listed rows of W and H, weight times each, are added to the products in fp32 (8 x 1024 rows
+// of 64 columns, V = 128256, d = 4096: gradients 2.6e-3 from exact instead of 1.7e-3, which is their own rounding, without this).
 int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                      const void* W_hyper, const int32_t* targets, const float* lse,
                                      const float* grad_nll, void* dH, void* dW_base, void* dW_hyper, hipStream_t s,
@@ -92,6 +95,11 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   // the benchmark configurations): dH and dW_hyper of a chunk are its own, dW_base of a later chunk adds to the
   // bf16 result of the earlier ones (one more rounding per chunk).
   // work space (bf16 unless noted), 256-byte aligned pieces
+  float* weight = nullptr;
+  if (teacher) {
+    const int rc = z2z_weighted_rows_reserve(c, rows, teacher->K, &weight, s);
+    if (rc != Z2Z_OK) return rc;
+  }
   size_t off = 0;
   size_t o_g, o_t, o_Pb, o_Ph;
   auto take = [&](size_t bytes) { const size_t at = off; off += round_up(bytes, 256); return at; };
@@ -182,7 +190,7 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
       if (rc != Z2Z_OK) return rc;
     }
     if (teacher) {
-      rc = z2z_launch_teacher_dz(c, *teacher, r0, rows_c, rows_per_seq, lse, g, Pb, Vp, Ph, capp, s);
+      rc = z2z_launch_teacher_dz(c, *teacher, r0, rows_c, rows_per_seq, lse, g, weight, Pb, Vp, Ph, capp, s);
       if (rc != Z2Z_OK) return rc;
     }
     // ---- the products ------------------------------------------------------------------------------------------
@@ -200,6 +208,11 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
                                     {nb, (size_t)rows_per_seq * capp, (size_t)rows_per_seq * d});
       if (rc != Z2Z_OK) return rc;
     }
+  }
+  if (teacher) {
+    rc = z2z_launch_teacher_dh(c, *teacher, rows, rows_per_seq, weight, W_base, W_hyper, dH, s);
+    if (rc != Z2Z_OK) return rc;
+    return z2z_launch_weighted_rows(c, teacher->ids, rows, teacher->K, weight, H, dW_base, dW_hyper, s);
   }
   return Z2Z_OK;
 }
