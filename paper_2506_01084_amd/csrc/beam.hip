@@ -20,6 +20,7 @@ using namespace z2z_logits;
 struct PickArgs {
   const float* logits;      // [rows, ld]
   const float* part_m;      // [rows, n_parts] largest logit of each part
+  const float* part_s;      // [rows, n_parts] sums of exp(logit - part_m), or nullptr: row_lse is there
   const float* row_lse;     // [rows]
   const float* score;       // [rows]
   const int32_t* size;      // [rows]
@@ -46,7 +47,7 @@ __device__ __forceinline__ float key_value(Key k) {
 
 __device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
 
-constexpr int P_THREADS = 1024, P_GROUPS = 256, P_LIST = 4096;
+constexpr int P_THREADS = 1024, P_GROUPS = 256, P_LIST = 4096, P_KEPT = 8;
 
 struct PickLds {
   Key group[P_GROUPS];
@@ -58,37 +59,59 @@ struct PickLds {
 };
 
 // The n largest of key(0) .. key(count - 1), all different where they are not 0, in order into l.top; the rest of l.top is 0.
-// Every fourth thread of a kind has the maximum of a 256th of the keys; the n-th largest of those maxima is a bound that
+// The threads fall into 64 groups (n up to 16) or 256, each with the maximum of its keys; the n-th largest of those maxima is a bound that
 // at least n keys reach and at most n groups' worth: they are listed and ranked against each other.  A list that does
 // not fit (keys so arranged that many large ones fall to one group) is left for n passes, each taking the largest key below the last.
+// Up to 8 keys a thread stay in registers from the first look to the second; more are worked out again.
 template <typename F>
 __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F key) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  Key best = 0ull;
-  for (uint32_t i = tid; i < count; i += P_THREADS) best = max_key(best, key(i));
+  const bool kept = count <= (uint32_t)(P_KEPT * P_THREADS);
+  Key mine_all[P_KEPT], best = 0ull;
+#pragma unroll
+  for (int u = 0; u < P_KEPT; ++u) {
+    const uint32_t i = tid + (uint32_t)(u * P_THREADS);
+    mine_all[u] = kept && i < count ? key(i) : 0ull;
+  }
+#pragma unroll
+  for (int u = 0; u < P_KEPT; ++u) best = max_key(best, mine_all[u]);
+  if (!kept)
+    for (uint32_t i = tid; i < count; i += P_THREADS) best = max_key(best, key(i));
   best = max_key(best, __shfl_xor(best, 1));
   best = max_key(best, __shfl_xor(best, 2));
-  if ((tid & 3) == 0) l.group[tid >> 2] = best;
+  const int groups = n <= 16 ? 64 : P_GROUPS;
+  if (groups == 64) {
+    best = max_key(best, __shfl_xor(best, 4));
+    best = max_key(best, __shfl_xor(best, 8));
+    if ((tid & 15) == 0) l.group[tid >> 4] = best;
+  } else if ((tid & 3) == 0) {
+    l.group[tid >> 2] = best;
+  }
   if (tid < n) l.top[tid] = 0ull;
   if (tid == 0) {
     l.found = 0u;
     l.threshold = 1ull;                  // fewer than n groups have any: all of theirs
   }
   __syncthreads();
-  if (tid < P_GROUPS) {
+  if (tid < groups) {
     const Key mine = l.group[tid];
     int above = 0;
-    for (int i = 0; i < P_GROUPS; ++i) above += l.group[i] > mine;
+#pragma unroll 16
+    for (int i = 0; i < groups; ++i) above += l.group[i] > mine;
     if (above == n - 1 && mine != 0ull) l.threshold = mine;
   }
   __syncthreads();
   const Key threshold = l.threshold;
-  for (uint32_t i = tid; i < count; i += P_THREADS) {
-    const Key k = key(i);
-    if (k >= threshold) {
-      const uint32_t at = atomicAdd(&l.found, 1u);
-      if (at < (uint32_t)P_LIST) l.list[at] = k;
-    }
+  auto append = [&](Key k) {
+    if (k < threshold) return;
+    const uint32_t at = atomicAdd(&l.found, 1u);
+    if (at < (uint32_t)P_LIST) l.list[at] = k;
+  };
+  if (kept) {
+#pragma unroll
+    for (int u = 0; u < P_KEPT; ++u) append(mine_all[u]);
+  } else {
+    for (uint32_t i = tid; i < count; i += P_THREADS) append(key(i));
   }
   __syncthreads();
   const uint32_t found = l.found;
@@ -127,13 +150,49 @@ __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F ke
 __global__ void __launch_bounds__(P_THREADS) beam_pick_kernel(PickArgs a) {
   __shared__ PickLds l;
   __shared__ Key parts[Z2Z_MAX_PICK];
+  __shared__ float lse[Z2Z_MAX_BEAMS];
   const int tid = threadIdx.x;
   const int row0 = blockIdx.x * a.beams;
+  // the beams' log-sum-exps, given or merged from the parts here (a launch less): a wave per beam, 16 parts a lane on the way at a time
+  if (a.part_s) {
+    const int lane = tid & 63;
+    for (int beam = tid >> 6; beam < a.beams; beam += P_THREADS / 64) {
+      const float *pm = a.part_m + (size_t)(row0 + beam) * a.n_parts, *ps = a.part_s + (size_t)(row0 + beam) * a.n_parts;
+      float m = kNegInf, sum = 0.f;
+      for (int p0 = lane; p0 < a.n_parts; p0 += 16 * 64) {
+        float x[16], y[16], top = kNegInf;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          const int p = p0 + 64 * u;
+          x[u] = p < a.n_parts ? pm[p] : kNegInf;
+          y[u] = p < a.n_parts ? ps[p] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 16; ++u) top = fmaxf(top, x[u]);
+        const float up = fmaxf(m, top);
+        sum = m == kNegInf ? sum : sum * __expf(m - up);
+        // (an empty part adds nothing; a row's NaN stays NaN: a part that holds one has a NaN sum)
+#pragma unroll
+        for (int u = 0; u < 16; ++u) sum += x[u] == kNegInf ? y[u] : y[u] * __expf(x[u] - up);
+        m = up;
+      }
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) {
+        const float om = __shfl_xor(m, off), os = __shfl_xor(sum, off), up = fmaxf(m, om);
+        sum = (m == kNegInf ? sum : sum * __expf(m - up)) + (om == kNegInf ? os : os * __expf(om - up));
+        m = up;
+      }
+      if (lane == 0) lse[beam] = m + logf(sum);
+    }
+  } else if (tid < a.beams) {
+    lse[tid] = a.row_lse[row0 + tid];
+  }
+  __syncthreads();
   const uint32_t n_parts = (uint32_t)a.n_parts;
   const int n = a.picks;
   top_keys(l, n, (uint32_t)a.beams * n_parts, [&](uint32_t i) -> Key {
-    const int r = row0 + (int)(i / n_parts);
-    return make_key((a.part_m[(size_t)row0 * n_parts + i] - a.row_lse[r]) + a.score[r], i);
+    const int beam = (int)(i / n_parts);
+    return make_key((a.part_m[(size_t)row0 * n_parts + i] - lse[beam]) + a.score[row0 + beam], i);
   });
   if (tid < n) parts[tid] = l.top[tid];
   __syncthreads();
@@ -153,7 +212,7 @@ __global__ void __launch_bounds__(P_THREADS) beam_pick_kernel(PickArgs a) {
     }
     c += (int)(i & slot);
     if (c >= end) return 0ull;
-    return make_key((a.logits[(size_t)r * a.ld + c] - a.row_lse[r]) + a.score[r], beam * (uint32_t)a.ld + (uint32_t)c);
+    return make_key((a.logits[(size_t)r * a.ld + c] - lse[beam]) + a.score[r], beam * (uint32_t)a.ld + (uint32_t)c);
   });
   if (tid < n) {
     const Key k = l.top[tid];
@@ -292,13 +351,14 @@ __global__ void __launch_bounds__(256) reorder_kernel(ReorderArgs a) {
 
 }  // namespace
 
-int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, int n_parts, int base_columns, int hyper_columns,
-                         const float* row_lse, int beams, const float* score, int picks, int32_t* parent, int32_t* code, float* picked,
+int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, const float* part_s, int n_parts, int base_columns,
+                         int hyper_columns, const float* row_lse, int beams, const float* score, int picks, int32_t* parent, int32_t* code, float* picked,
                          hipStream_t s) {
   PickArgs a;
   memset(&a, 0, sizeof(a));
   a.logits = logits;
   a.part_m = part_m;
+  a.part_s = part_s;
   a.row_lse = row_lse;
   a.score = score;
   a.size = c->st.size;

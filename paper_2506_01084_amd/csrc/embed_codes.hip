@@ -284,9 +284,13 @@ __global__ void __launch_bounds__(1024) sort_place_kernel(LookupArgs a, uint32_t
 //   WEIGHTED                  weight[position] times row position / per_row of a bf16 matrix; base rows are bf16, everything is added
 enum { LOOKUP_BF16 = 0, LOOKUP_F32 = 1, WEIGHTED = 2 };
 
-// Sorted positions of a wave.  A piece's sums that cross its ends go through memory, so few positions are short of work for long
-// pieces, and many (a teacher's list has K a row) of memory for short ones.
-constexpr int piece_of(int kind) { return kind == WEIGHTED ? 64 : 32; }
+// Sorted positions of a wave: 8 where there are few, so that more waves share them, 32 or 64 else (sums that cross the ends of a piece go
+// through memory, [pieces, d] twice, and a teacher's lists have K positions a row).
+constexpr int kShortPiece = 8;
+int piece_of(int kind, long long positions, int slices) {
+  const int piece = kind == WEIGHTED ? 64 : 32;
+  return positions * slices < 4096LL * piece ? kShortPiece : piece;
+}
 
 struct GradArgs {
   const u32x4* dX;
@@ -297,7 +301,7 @@ struct GradArgs {
   void* dW;
   float* head;                            // [pieces, d]: the sum of a run that began in an earlier piece
   float* tail;                            // [pieces, d]: the sum of a run that begins here and goes on
-  uint32_t n, pieces, V, sentinel;
+  uint32_t n, pieces, piece, V, sentinel;
   int32_t chunks, slices, d, add, fill_blocks, per_row;
   float scale;
 };
@@ -349,11 +353,11 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* skey, uint32_t l
 // Blocks [0, fill_blocks) write zeros to the table rows that no position names: a wave per 16 rows, each looked up by a
 // lane.  The others: a wave per piece of sorted positions and 64 times 16 bytes of their rows, eight rows requested at a
 // time, added in fp32 in order.  Runs inside the piece are stored, what crosses its ends is left for join_kernel.
-template <int KIND>
+template <int KIND, int PIECE>
 __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   const int lane = threadIdx.x & 63;
   constexpr bool BF16 = KIND != LOOKUP_F32;
-  constexpr int EPC = BF16 ? 8 : 4, PIECE = piece_of(KIND);
+  constexpr int EPC = BF16 ? 8 : 4;
   if ((int)blockIdx.x < a.fill_blocks) {
     const uint32_t first = ((uint32_t)blockIdx.x * 4u + (threadIdx.x >> 6)) * 16u;
     const uint32_t key = first + (uint32_t)(lane & 15);
@@ -445,7 +449,7 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
 template <int KIND>
 __global__ void __launch_bounds__(256) join_kernel(GradArgs a) {
   __shared__ float4 part[4][64];
-  constexpr uint32_t PIECE = piece_of(KIND);
+  const uint32_t PIECE = a.piece;
   const uint32_t p = blockIdx.x, p0 = p * PIECE, p1 = p0 + PIECE;
   if (p1 >= a.n) return;
   const uint32_t key = a.skey[p1 - 1];
@@ -523,12 +527,12 @@ namespace {
 // How the work space of a sum by rows is laid out, and what its sort takes.
 struct SumPlan {
   uint32_t n, tiles, pieces;
-  int bits, passes;
+  int bits, passes, piece;
   bool small;
   size_t o_key[2], o_pos[2], o_count, o_head, o_tail, bytes;
 };
 
-bool plan_sum(const z2z_ctx* c, long long positions, int piece, SumPlan* p) {
+bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
   const long long keys = (long long)c->cfg.V + (long long)c->cfg.B * c->cfg.cap;
   // (positions and rows of the joint table are 32-bit numbers here)
   if (positions > 0x7FFFFFFFLL || keys > 0x7FFFFFFFLL) return false;
@@ -538,7 +542,8 @@ bool plan_sum(const z2z_ctx* c, long long positions, int piece, SumPlan* p) {
   p->passes = (key_bits + 9) / 10;
   p->bits = (key_bits + p->passes - 1) / p->passes;
   p->tiles = (p->n + S_TILE - 1) / S_TILE;
-  p->pieces = (p->n + piece - 1) / piece;
+  p->piece = piece_of(kind, positions, (c->cfg.d / (kind == LOOKUP_F32 ? 4 : 8) + 63) / 64);
+  p->pieces = (p->n + p->piece - 1) / p->piece;
   p->small = p->n <= (uint32_t)S_TILE;
   // sorted keys and positions (twice where the passes go through memory), the tiles' counts, sums that cross pieces
   p->bytes = 0;
@@ -578,6 +583,7 @@ int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned
   g.tail = p.pieces > 1 ? reinterpret_cast<float*>(ws + p.o_tail) : nullptr;
   g.n = p.n;
   g.pieces = p.pieces;
+  g.piece = (uint32_t)p.piece;
   g.V = (uint32_t)a.V;
   g.sentinel = a.sentinel;
   g.chunks = a.chunks;
@@ -586,7 +592,10 @@ int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned
   g.fill_blocks = g.add ? 0 : (int)(((long long)a.sentinel + 63) / 64);
   const long long blocks = g.fill_blocks + ((long long)p.pieces * g.slices + 3) / 4;
   if (blocks > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
-  hipLaunchKernelGGL(reduce_kernel<KIND>, dim3((unsigned)blocks), dim3(256), 0, s, g);
+  if (p.piece == kShortPiece)
+    hipLaunchKernelGGL((reduce_kernel<KIND, kShortPiece>), dim3((unsigned)blocks), dim3(256), 0, s, g);
+  else
+    hipLaunchKernelGGL((reduce_kernel<KIND, KIND == WEIGHTED ? 64 : 32>), dim3((unsigned)blocks), dim3(256), 0, s, g);
   if (p.pieces > 1)
     hipLaunchKernelGGL(join_kernel<KIND>, dim3(p.pieces, (unsigned)((c->cfg.d + 255) / 256)), dim3(256), 0, s, g);
   Z2Z_HIP_TRY(hipGetLastError());
@@ -599,7 +608,7 @@ int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int3
                                     int32_t flags, float* dE, void* dW_hyper, hipStream_t s) {
   const bool add = flags == Z2Z_GRAD_ADD;
   SumPlan p;
-  if (!plan_sum(c, (long long)c->cfg.B * stride, piece_of(LOOKUP_BF16), &p)) return Z2Z_EUNSUPPORTED;
+  if (!plan_sum(c, (long long)c->cfg.B * stride, c->cfg.dtype == Z2Z_BF16 ? LOOKUP_BF16 : LOOKUP_F32, &p)) return Z2Z_EUNSUPPORTED;
   if (p.n == 0u && add) return Z2Z_OK;
   const int rc = z2z_work_reserve(c, &c->lookup_ws, p.bytes, s);
   if (rc != Z2Z_OK) return rc;
@@ -617,7 +626,7 @@ int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int3
 
 int z2z_weighted_rows_reserve(z2z_ctx* c, long long rows, int per_row, float** weight, hipStream_t s) {
   SumPlan p;
-  if (!plan_sum(c, rows * per_row, piece_of(WEIGHTED), &p)) return Z2Z_EUNSUPPORTED;
+  if (!plan_sum(c, rows * per_row, WEIGHTED, &p)) return Z2Z_EUNSUPPORTED;
   const int rc = z2z_work_reserve(c, &c->lookup_ws, p.bytes + (size_t)p.n * sizeof(float), s);
   if (rc != Z2Z_OK) return rc;
   *weight = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(c->lookup_ws.p) + p.bytes);
@@ -627,7 +636,7 @@ int z2z_weighted_rows_reserve(z2z_ctx* c, long long rows, int per_row, float** w
 int z2z_launch_weighted_rows(z2z_ctx* c, const int32_t* ids, long long rows, int per_row, const float* weight, const void* H, void* dW_base,
                              void* dW_hyper, hipStream_t s) {
   SumPlan p;
-  if (!plan_sum(c, rows * per_row, piece_of(WEIGHTED), &p)) return Z2Z_EUNSUPPORTED;
+  if (!plan_sum(c, rows * per_row, WEIGHTED, &p)) return Z2Z_EUNSUPPORTED;
   GradArgs g;
   memset(&g, 0, sizeof(g));
   g.dX = reinterpret_cast<const u32x4*>(H);

@@ -479,7 +479,8 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
   }
   const int mid_columns = z2z_logits_mid_columns(c, V);
   // the streaming kernel takes the hyper part of longer runs of rows along (up to 64 rows a sequence it has units of its own)
-  const bool mid_both = mid_base && cap > 0 && rows_per_seq > 64 &&
+  // (at a temperature those are not there)
+  const bool mid_both = mid_base && cap > 0 && (rows_per_seq > 64 || !plain) &&
                         (size_t)((V + mid_columns - 1) / mid_columns + (cap + mid_columns - 1) / mid_columns) * rows <= Z2Z_STATIC_PARTS;
   const int base_strips = mid_base ? (V + mid_columns - 1) / mid_columns : (base_vt + strip_b - 1) / strip_b;
   int hyp_strips = mid_both ? (cap + mid_columns - 1) / mid_columns : cap > 0 ? (hyp_vt + strip_h - 1) / strip_h : 0;
@@ -778,7 +779,6 @@ int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const voi
     z2z_logits_decode_units(&base_columns, &hyper_columns);
     if (base > 0) base_columns = base;
     if (hyper > 0) hyper_columns = hyper;
-    rc = launch_combine(ctx_parts(c), n_parts, rows, nullptr, nullptr, row_lse, s);
   } else {
     // (fp32, or widths that the step's kernels do not take: the general kernel stores the logits, and a maximum per 256 columns comes
     // from those)
@@ -787,8 +787,8 @@ int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const voi
     rc = z2z_launch_part_max(c, c->sample_logits, c->part_m, &n_parts, s);
   }
   if (rc != Z2Z_OK) return rc;
-  return z2z_launch_beam_pick(c, c->sample_logits, c->part_m, n_parts, base_columns, hyper_columns, row_lse, beams, score, picks, parent, code,
-                              picked, s);
+  return z2z_launch_beam_pick(c, c->sample_logits, c->part_m, c->decode_ready ? c->part_s : nullptr, n_parts, base_columns, hyper_columns,
+                              row_lse, beams, score, picks, parent, code, picked, s);
 }
 
 int z2z_launch_extended_nll(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,

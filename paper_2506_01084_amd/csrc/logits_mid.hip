@@ -459,7 +459,7 @@ static void launch_mid(const LogitsArgs& a, hipStream_t s) {
     else
       hipLaunchKernelGGL((logits_mid_kernel<6, 2, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
   } else {
-    if (blocks == 2 && a.rows_per_seq == 1)
+    if (blocks == 2 && a.rows_per_seq == 1 && a.hyper.n_work == 0)   // (the hyper part rides along in SMODE 0)
       hipLaunchKernelGGL((logits_mid_kernel<2, 4, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
     else if (blocks == 2)
       hipLaunchKernelGGL((logits_mid_kernel<2, 0, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
@@ -482,7 +482,7 @@ int z2z_launch_logits_mid(z2z_ctx* c, LogitsArgs a, const void* W, int w_rows, i
   a.n_vtiles = (w_rows + columns - 1) / columns;
   a.once = a.once || (size_t)w_rows * a.d * sizeof(uint16_t) > kKeepBytes;
   c->n_launch[Z2Z_KERNEL_MID]++;
-  if (a.hyper.n_work > 0 && (a.sample != 0 || (a.rows_per_seq <= 64 && !a.row_grad))) return Z2Z_EUNSUPPORTED;
+  if (a.hyper.n_work > 0 && (a.sample != 0 || (a.rows_per_seq <= 64 && !a.row_grad && a.inv_t == 1.f))) return Z2Z_EUNSUPPORTED;
   // (two workgroups of the 64-row build per weight tile for 65..128 rows, sharing the tile's weights through an
   // XCD's L2, measured slower than one of the 128-row build: 383 against 293 us at config 2's shape)
   // builds: 2, 4 or 6 blocks of 32 hidden rows; the sampling calls come with one row per sequence.  (8 blocks, up to 256

@@ -177,9 +177,10 @@ int z2z_launch_weighted_rows(z2z_ctx* c, const int32_t* ids, long long rows, int
                              void* dW_hyper, hipStream_t s);
 int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
                              int32_t picks, int32_t* parent, int32_t* code, float* picked, hipStream_t s);
-// The pick from stored logits [B, V + cap] and the largest of each part of base_columns / hyper_columns columns (powers of two).
-int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, int n_parts, int base_columns, int hyper_columns,
-                         const float* row_lse, int beams, const float* score, int picks, int32_t* parent, int32_t* code, float* picked,
+// The pick from stored logits [B, V + cap] and the largest of each part of base_columns / hyper_columns columns (powers of two); the
+// rows' log-sum-exps come from the parts' sums, or are given (part_s: nullptr).
+int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, const float* part_s, int n_parts, int base_columns,
+                         int hyper_columns, const float* row_lse, int beams, const float* score, int picks, int32_t* parent, int32_t* code, float* picked,
                          hipStream_t s);
 int z2z_launch_part_max(z2z_ctx* c, const float* logits, float* part_m, int* n_parts, hipStream_t s);   // parts of 256 columns
 int z2z_launch_codebook_reorder(z2z_ctx* c, int32_t beams, const int32_t* source, void* W_hyper, hipStream_t s);
