@@ -47,7 +47,7 @@ __device__ __forceinline__ float key_value(Key k) {
 
 __device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
 
-constexpr int P_THREADS = 1024, P_GROUPS = 256, P_LIST = 4096, P_KEPT = 8;
+constexpr int P_THREADS = 1024, P_GROUPS = 256, P_LIST = 2048, P_KEPT = 8, P_PARTS = 8192;
 
 struct PickLds {
   Key group[P_GROUPS];
@@ -71,7 +71,8 @@ __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F ke
 #pragma unroll
   for (int u = 0; u < P_KEPT; ++u) {
     const uint32_t i = tid + (uint32_t)(u * P_THREADS);
-    mine_all[u] = kept && i < count ? key(i) : 0ull;
+    mine_all[u] = 0ull;
+    if (kept && (uint32_t)(u * P_THREADS) < count) mine_all[u] = i < count ? key(i) : 0ull;     // (a uniform branch: no work for what is not there)
   }
 #pragma unroll
   for (int u = 0; u < P_KEPT; ++u) best = max_key(best, mine_all[u]);
@@ -109,7 +110,8 @@ __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F ke
   };
   if (kept) {
 #pragma unroll
-    for (int u = 0; u < P_KEPT; ++u) append(mine_all[u]);
+    for (int u = 0; u < P_KEPT; ++u)
+      if ((uint32_t)(u * P_THREADS) < count) append(mine_all[u]);
   } else {
     for (uint32_t i = tid; i < count; i += P_THREADS) append(key(i));
   }
@@ -149,10 +151,18 @@ __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F ke
 // those has a better one, or an equal one of a lower index, than any other part), so only their logits are read.
 __global__ void __launch_bounds__(P_THREADS) beam_pick_kernel(PickArgs a) {
   __shared__ PickLds l;
-  __shared__ Key parts[Z2Z_MAX_PICK];
-  __shared__ float lse[Z2Z_MAX_BEAMS];
+  __shared__ int part_beam[Z2Z_MAX_PICK], part_from[Z2Z_MAX_PICK], part_end[Z2Z_MAX_PICK];
+  __shared__ float lse[Z2Z_MAX_BEAMS], score[Z2Z_MAX_BEAMS];
+  __shared__ int columns[Z2Z_MAX_BEAMS];
+  __shared__ float best[P_PARTS];
   const int tid = threadIdx.x;
   const int row0 = blockIdx.x * a.beams;
+  // (a prompt's parts stay at hand where they fit: their maxima serve the log-sum-exps and the choice of parts)
+  const bool at_hand = a.part_s && a.beams * a.n_parts <= P_PARTS;
+  if (tid < a.beams) {
+    score[tid] = a.score[row0 + tid];
+    columns[tid] = a.V + min(max(a.size[row0 + tid], 0), a.cap);
+  }
   // the beams' log-sum-exps, given or merged from the parts here (a launch less): a wave per beam, 16 parts a lane on the way at a time
   if (a.part_s) {
     const int lane = tid & 63;
@@ -166,6 +176,7 @@ __global__ void __launch_bounds__(P_THREADS) beam_pick_kernel(PickArgs a) {
           const int p = p0 + 64 * u;
           x[u] = p < a.n_parts ? pm[p] : kNegInf;
           y[u] = p < a.n_parts ? ps[p] : 0.f;
+          if (at_hand && p < a.n_parts) best[beam * a.n_parts + p] = x[u];
         }
 #pragma unroll
         for (int u = 0; u < 16; ++u) top = fmaxf(top, x[u]);
@@ -192,27 +203,30 @@ __global__ void __launch_bounds__(P_THREADS) beam_pick_kernel(PickArgs a) {
   const int n = a.picks;
   top_keys(l, n, (uint32_t)a.beams * n_parts, [&](uint32_t i) -> Key {
     const int beam = (int)(i / n_parts);
-    return make_key((a.part_m[(size_t)row0 * n_parts + i] - lse[beam]) + a.score[row0 + beam], i);
+    return make_key(((at_hand ? best[i] : a.part_m[(size_t)row0 * n_parts + i]) - lse[beam]) + score[beam], i);
   });
-  if (tid < n) parts[tid] = l.top[tid];
+  if (tid < n) {
+    const Key part = l.top[tid];
+    const uint32_t at = ~(uint32_t)part, beam = part ? at / n_parts : 0u, p = part ? at - beam * n_parts : 0u;
+    int c = 0, end = 0;                              // (no such part: no columns)
+    if (part && (int)p < a.n_base_parts) {
+      c = (int)p * a.base_columns;
+      end = min(c + a.base_columns, a.V);
+    } else if (part) {
+      c = a.V + ((int)p - a.n_base_parts) * a.hyper_columns;
+      end = min(c + a.hyper_columns, columns[beam]);
+    }
+    part_beam[tid] = (int)beam;
+    part_from[tid] = c;
+    part_end[tid] = end;
+  }
   __syncthreads();
   const uint32_t slot = (1u << a.slot_shift) - 1u;
   top_keys(l, n, (uint32_t)n << a.slot_shift, [&](uint32_t i) -> Key {
-    const Key part = parts[i >> a.slot_shift];
-    if (part == 0ull) return 0ull;
-    const uint32_t at = ~(uint32_t)part, beam = at / n_parts, p = at - beam * n_parts;
-    const int r = row0 + (int)beam;
-    int c, end;
-    if ((int)p < a.n_base_parts) {
-      c = (int)p * a.base_columns;
-      end = min(c + a.base_columns, a.V);
-    } else {
-      c = a.V + ((int)p - a.n_base_parts) * a.hyper_columns;
-      end = min(c + a.hyper_columns, a.V + min(max(a.size[r], 0), a.cap));
-    }
-    c += (int)(i & slot);
-    if (c >= end) return 0ull;
-    return make_key((a.logits[(size_t)r * a.ld + c] - lse[beam]) + a.score[r], beam * (uint32_t)a.ld + (uint32_t)c);
+    const uint32_t j = i >> a.slot_shift;
+    const int beam = part_beam[j], c = part_from[j] + (int)(i & slot);
+    if (c >= part_end[j]) return 0ull;
+    return make_key((a.logits[(size_t)(row0 + beam) * a.ld + c] - lse[beam]) + score[beam], (uint32_t)beam * (uint32_t)a.ld + (uint32_t)c);
   });
   if (tid < n) {
     const Key k = l.top[tid];

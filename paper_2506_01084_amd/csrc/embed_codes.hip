@@ -166,11 +166,37 @@ __device__ __forceinline__ void tile_places(SortLds& l, const uint32_t (&key)[S_
     if (r < rounds) place[r] = (uint32_t)l.cnt[wave][(key[r] >> shift) & mask] + rank[r];
 }
 
-// Up to S_TILE positions: the whole sort in one workgroup, from pass to pass through LDS.
-__global__ void __launch_bounds__(1024) sort_small_kernel(LookupArgs a, uint32_t n, int bits, int passes, uint32_t* skey, uint32_t* spos) {
+// A sort's launches are a few workgroups bound by latency; the others write zeros meanwhile: 16-byte pieces [begin, end) of the base gradient.
+struct Zeros {
+  u32x4* p;
+  size_t begin, end;
+  bool past;                // past the caches
+};
+
+// 16-byte pieces from, from + step .. below end.  (Two loops: of a choice within one the compiler makes a single plain store.)
+__device__ __forceinline__ void store_zeros(u32x4* p, size_t from, size_t end, size_t step, bool past) {
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+  if (past)
+    for (size_t i = from; i < end; i += step) __builtin_nontemporal_store(zero, p + i);
+  else
+    for (size_t i = from; i < end; i += step) p[i] = zero;
+}
+
+__device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t block, uint32_t blocks) {
+  store_zeros(z.p, z.begin + (size_t)block * 1024 + threadIdx.x, z.end, (size_t)blocks * 1024, z.past);
+}
+
+// Up to S_TILE positions: the whole sort in one workgroup, from pass to pass through LDS.  (joins: join_kernel's counter, cleared here.)
+__global__ void __launch_bounds__(1024) sort_small_kernel(LookupArgs a, uint32_t n, int bits, int passes, uint32_t* skey, uint32_t* spos,
+                                                          uint32_t* joins, Zeros z) {
   __shared__ SortLds l;
   __shared__ uint32_t xkey[S_TILE];
   __shared__ uint16_t xpos[S_TILE];
+  if (blockIdx.x > 0) {
+    write_zeros(z, blockIdx.x - 1u, gridDim.x - 1u);
+    return;
+  }
+  if (joins && threadIdx.x == 0) *joins = 0u;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rounds = (int)((n + 1023u) / 1024u);
   uint32_t key[S_ROUNDS], pos[S_ROUNDS], place[S_ROUNDS];
@@ -210,9 +236,15 @@ __global__ void __launch_bounds__(1024) sort_small_kernel(LookupArgs a, uint32_t
 }
 
 // More: per pass, every tile counts its digits ...
-__global__ void __launch_bounds__(1024) sort_count_kernel(LookupArgs a, uint32_t n, const uint32_t* key_in, int shift, int bits, uint32_t* count) {
+__global__ void __launch_bounds__(1024) sort_count_kernel(LookupArgs a, uint32_t n, uint32_t tiles, const uint32_t* key_in, int shift, int bits,
+                                                          uint32_t* count, uint32_t* joins, Zeros z) {
   __shared__ uint32_t cnt[S_DIGITS];
   const int digits = 1 << bits;
+  if (blockIdx.x >= tiles) {
+    write_zeros(z, blockIdx.x - tiles, gridDim.x - tiles);
+    return;
+  }
+  if (joins && blockIdx.x == 0 && threadIdx.x == 0) *joins = 0u;
   for (int i = threadIdx.x; i < digits; i += 1024) cnt[i] = 0u;
   __syncthreads();
 #pragma unroll
@@ -225,13 +257,18 @@ __global__ void __launch_bounds__(1024) sort_count_kernel(LookupArgs a, uint32_t
 }
 
 // ... and puts its items behind those of smaller digits and of the same digit in the tiles before.
-__global__ void __launch_bounds__(1024) sort_place_kernel(LookupArgs a, uint32_t n, const uint32_t* key_in, const uint32_t* pos_in, int shift,
-                                                          int bits, const uint32_t* count, uint32_t* key_out, uint32_t* pos_out) {
+__global__ void __launch_bounds__(1024) sort_place_kernel(LookupArgs a, uint32_t n, uint32_t n_tiles, const uint32_t* key_in, const uint32_t* pos_in,
+                                                          int shift, int bits, const uint32_t* count, uint32_t* key_out, uint32_t* pos_out,
+                                                          Zeros z) {
   __shared__ SortLds l;
   __shared__ uint32_t go[S_DIGITS];       // where the tile's first item with the digit goes
   __shared__ uint32_t sums[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int digits = 1 << bits, tiles = (int)gridDim.x;
+  if (blockIdx.x >= n_tiles) {
+    write_zeros(z, blockIdx.x - n_tiles, gridDim.x - n_tiles);
+    return;
+  }
+  const int digits = 1 << bits, tiles = (int)n_tiles;
   const uint32_t t0 = blockIdx.x * (uint32_t)S_TILE;
   uint32_t key[S_ROUNDS], pos[S_ROUNDS], place[S_ROUNDS];
 #pragma unroll
@@ -301,8 +338,11 @@ struct GradArgs {
   void* dW;
   float* head;                            // [pieces, d]: the sum of a run that began in an earlier piece
   float* tail;                            // [pieces, d]: the sum of a run that begins here and goes on
+  uint32_t* joins;                        // how many runs cross pieces, then the pieces that they begin in, in any order
   uint32_t n, pieces, piece, V, sentinel;
+  uint32_t fill_from;                     // first row of the joint table that reduce_kernel looks after (those below are zeros already)
   int32_t chunks, slices, d, add, fill_blocks, per_row;
+  bool past;                              // zeros past the caches
   float scale;
 };
 
@@ -340,44 +380,54 @@ __device__ __forceinline__ void store_row(const GradArgs& a, uint32_t key, size_
   }
 }
 
-// The first sorted position whose key is at least `key`.
+// The first sorted position in [lo, hi) whose key is at least `key` (hi: none), for a whole wave: 64 samples a step, so that a few loads
+// follow each other where halving takes twenty.
 __device__ __forceinline__ uint32_t lower_bound(const uint32_t* skey, uint32_t lo, uint32_t hi, uint32_t key) {
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (skey[mid] < key) lo = mid + 1;
-    else hi = mid;
+  const uint32_t lane = threadIdx.x & 63;
+  while (hi - lo > 64u) {
+    const uint32_t step = (hi - lo + 63u) / 64u, at = lo + lane * step;
+    const uint32_t smaller = (uint32_t)__popcll(__ballot(at < hi && skey[min(at, hi - 1u)] < key));
+    if (smaller == 0u) return lo;
+    hi = min(hi, lo + smaller * step);
+    lo += (smaller - 1u) * step + 1u;
   }
-  return lo;
+  return lo + (uint32_t)__popcll(__ballot(lo + lane < hi && skey[min(lo + lane, hi - 1u)] < key));
 }
 
-// Blocks [0, fill_blocks) write zeros to the table rows that no position names: a wave per 16 rows, each looked up by a
-// lane.  The others: a wave per piece of sorted positions and 64 times 16 bytes of their rows, eight rows requested at a
-// time, added in fp32 in order.  Runs inside the piece are stored, what crosses its ends is left for join_kernel.
+// The first blocks: a wave per piece of sorted positions and 64 times 16 bytes of their rows, eight rows requested at a
+// time, added in fp32 in order.  Runs inside the piece are stored, what crosses its ends is left for join_kernel.  The last fill_blocks
+// write zeros to the table rows that no position names: a wave per 16 rows.
+// Bound by HBM: dX read once, the gradients written once.  8 x 4096 positions of 24.6 k in use, V = 128256, d = 2048 (1.25 GB): zeros past the caches
+// where the gradients are larger than half of the memory-side one 280 -> 240 us (128 MB of them, V = 32000, d = 1000 fp32: 31 -> 38), these blocks
+// last 240 -> 237.
 template <int KIND, int PIECE>
 __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   const int lane = threadIdx.x & 63;
   constexpr bool BF16 = KIND != LOOKUP_F32;
   constexpr int EPC = BF16 ? 8 : 4;
-  if ((int)blockIdx.x < a.fill_blocks) {
-    const uint32_t first = ((uint32_t)blockIdx.x * 4u + (threadIdx.x >> 6)) * 16u;
-    const uint32_t key = first + (uint32_t)(lane & 15);
-    bool empty = false;
-    if (key < a.sentinel && lane < 16) {
-      const uint32_t at = lower_bound(a.skey, 0u, a.n, key);
-      empty = at >= a.n || a.skey[at] != key;
+  const uint32_t sum_blocks = gridDim.x - (uint32_t)a.fill_blocks;
+  if (blockIdx.x >= sum_blocks) {
+    const uint32_t first = a.fill_from + ((blockIdx.x - sum_blocks) * 4u + (threadIdx.x >> 6)) * 16u;
+    uint32_t named = 0u;                             // a bit per row
+    for (uint32_t at = lower_bound(a.skey, 0u, a.n, first); at < a.n; at += 64u) {
+      const uint32_t k = at + lane < a.n ? a.skey[at + lane] : kNoKey;
+      const uint32_t row = k - first;
+      uint32_t bits = k >= first && row < 16u ? 1u << row : 0u;
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) bits |= __shfl_xor(bits, off);
+      named |= bits;
+      if ((uint32_t)__builtin_amdgcn_readlane((int)k, 63) - first >= 16u) break;
     }
-    const uint64_t rows = __ballot(empty);
-    const u32x4 zero = {0u, 0u, 0u, 0u};
     for (int r = 0; r < 16; ++r) {
-      if (!((rows >> r) & 1ull)) continue;
+      if (((named >> r) & 1u) || first + (uint32_t)r >= a.sentinel) continue;
       const uint32_t k = first + (uint32_t)r;
       const int per_row = k < a.V ? a.d / 4 : a.chunks;
       u32x4* to = k < a.V ? reinterpret_cast<u32x4*>(a.dE) + (size_t)k * per_row : reinterpret_cast<u32x4*>(a.dW) + (size_t)(k - a.V) * per_row;
-      for (int q = lane; q < per_row; q += 64) to[q] = zero;
+      store_zeros(to, (size_t)lane, (size_t)per_row, 64, a.past);
     }
     return;
   }
-  const uint32_t wid = (blockIdx.x - (uint32_t)a.fill_blocks) * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t wid = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t piece = wid / (uint32_t)a.slices;
   if (piece >= a.pieces) return;
   const int chunk = (int)(wid % (uint32_t)a.slices) * 64 + lane;
@@ -426,6 +476,7 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
       const uint32_t after = last ? next : (uint32_t)__builtin_amdgcn_readlane(my_key, min(i + 1, PIECE - 1));
       if (last || after != key) {
         const bool goes_on = last && after == key;
+        if (goes_on && !began_before && chunk == 0) a.joins[1u + atomicAdd(a.joins, 1u)] = piece;
         if (on) {
           if (began_before || goes_on) {
             float4* to = reinterpret_cast<float4*>((began_before ? a.head : a.tail) + (size_t)piece * a.d + (size_t)chunk * EPC);
@@ -444,47 +495,56 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   }
 }
 
-// A run over several pieces: block (p, y) joins the run that begins in piece p and goes on, 256 features of it.  Its four waves add a quarter of
-// the pieces each, in order, and the quarters in order.
+// Runs over several pieces, each 256 features at a time: the four waves of a block add a quarter of the run's pieces each, in order, and the quarters
+// in order.
 template <int KIND>
 __global__ void __launch_bounds__(256) join_kernel(GradArgs a) {
   __shared__ float4 part[4][64];
-  const uint32_t PIECE = a.piece;
-  const uint32_t p = blockIdx.x, p0 = p * PIECE, p1 = p0 + PIECE;
-  if (p1 >= a.n) return;
-  const uint32_t key = a.skey[p1 - 1];
-  if (key >= a.sentinel || a.skey[p1] != key || (p0 > 0u && a.skey[p0] == key && a.skey[p0 - 1] == key)) return;
-  const uint32_t end = lower_bound(a.skey, p1, a.n, key + 1u), q1 = (end - 1u) / PIECE;      // the run's last piece
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int f = (int)blockIdx.y * 256 + lane * 4;
-  const bool on = f < a.d;
-  const uint32_t heads = q1 - p, each = (heads + 3u) / 4u;
-  const uint32_t from = p + 1u + min((uint32_t)wave * each, heads), to = p + 1u + min(((uint32_t)wave + 1u) * each, heads);
-  float4 sum = {0.f, 0.f, 0.f, 0.f};
-  if (on) {
-    if (wave == 0) sum = *reinterpret_cast<const float4*>(a.tail + (size_t)p * a.d + f);
+  const uint32_t groups = ((uint32_t)a.d + 255u) / 256u, jobs = a.joins[0] * groups;
+  for (uint32_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+    const uint32_t p = a.joins[1u + job / groups], p1 = (p + 1u) * a.piece;
+    const uint32_t key = a.skey[p1];
+    // the run's last piece: the last that begins with the key
+    uint32_t q1 = p;
+    for (;;) {
+      const uint32_t q = q1 + 1u + (uint32_t)lane;
+      const bool more = q < a.pieces && a.skey[min(q, a.pieces - 1u) * a.piece] == key;
+      const uint32_t pieces = (uint32_t)__popcll(__ballot(more));
+      q1 += pieces;
+      if (pieces < 64u) break;
+    }
+    const int f = (int)(job % groups) * 256 + lane * 4;
+    const bool on = f < a.d;
+    const uint32_t heads = q1 - p, each = (heads + 3u) / 4u;
+    const uint32_t from = p + 1u + min((uint32_t)wave * each, heads), to = p + 1u + min(((uint32_t)wave + 1u) * each, heads);
+    float4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (on) {
+      if (wave == 0) sum = *reinterpret_cast<const float4*>(a.tail + (size_t)p * a.d + f);
 #pragma unroll 8
-    for (uint32_t q = from; q < to; ++q) {
-      const float4 x = *reinterpret_cast<const float4*>(a.head + (size_t)q * a.d + f);
-      sum.x += x.x;
-      sum.y += x.y;
-      sum.z += x.z;
-      sum.w += x.w;
+      for (uint32_t q = from; q < to; ++q) {
+        const float4 x = *reinterpret_cast<const float4*>(a.head + (size_t)q * a.d + f);
+        sum.x += x.x;
+        sum.y += x.y;
+        sum.z += x.z;
+        sum.w += x.w;
+      }
     }
-  }
-  part[wave][lane] = sum;
-  __syncthreads();
-  if (wave == 0 && on) {
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && on) {
 #pragma unroll
-    for (int w = 1; w < 4; ++w) {
-      const float4 x = part[w][lane];
-      sum.x += x.x;
-      sum.y += x.y;
-      sum.z += x.z;
-      sum.w += x.w;
+      for (int w = 1; w < 4; ++w) {
+        const float4 x = part[w][lane];
+        sum.x += x.x;
+        sum.y += x.y;
+        sum.z += x.z;
+        sum.w += x.w;
+      }
+      const float s[4] = {sum.x, sum.y, sum.z, sum.w};
+      store_row<KIND, 4>(a, key, (size_t)f, s);
     }
-    const float s[4] = {sum.x, sum.y, sum.z, sum.w};
-    store_row<KIND, 4>(a, key, (size_t)f, s);
+    __syncthreads();
   }
 }
 
@@ -524,12 +584,16 @@ int z2z_launch_embed_codes(z2z_ctx* c, const int32_t* codes, const int32_t* n_co
 
 namespace {
 
+// Bytes of zeros that a sort's launch takes along at about its own length.
+constexpr size_t kZerosSmall = (size_t)128 << 20, kZerosCount = (size_t)32 << 20, kZerosPlace = (size_t)64 << 20;
+constexpr size_t kPastBytes = (size_t)128 << 20;     // half of the memory-side cache
+
 // How the work space of a sum by rows is laid out, and what its sort takes.
 struct SumPlan {
   uint32_t n, tiles, pieces;
   int bits, passes, piece;
   bool small;
-  size_t o_key[2], o_pos[2], o_count, o_head, o_tail, bytes;
+  size_t o_key[2], o_pos[2], o_count, o_joins, o_head, o_tail, bytes;
 };
 
 bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
@@ -553,6 +617,7 @@ bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
     p->o_pos[k] = k == 0 || !p->small ? take((size_t)p->n * 4) : 0;
   }
   p->o_count = p->small ? 0 : take((size_t)p->tiles * (1u << p->bits) * 4);
+  p->o_joins = take(((size_t)p->pieces + 1) * 4);
   p->o_head = p->pieces > 1 ? take((size_t)p->pieces * c->cfg.d * 4) : 0;
   p->o_tail = p->pieces > 1 ? take((size_t)p->pieces * c->cfg.d * 4) : 0;
   return true;
@@ -562,18 +627,34 @@ bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
 template <int KIND>
 int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned char* ws, GradArgs g, hipStream_t s) {
   auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
+  // zeros that go out with the sort: rows [0, fill_from) of the base gradient, `share` bytes a launch
+  const size_t row16 = (size_t)c->cfg.d / 4;         // 16-byte pieces of a base row (fp32)
+  g.past = (size_t)a.V * c->cfg.d * 4 + (size_t)a.B * a.cap * a.chunks * 16 > kPastBytes;
+  Zeros z = {reinterpret_cast<u32x4*>(g.dE), 0, 0, g.past};
+  unsigned fillers = 0;
+  auto next_zeros = [&](size_t bytes) {
+    z.begin = z.end;
+    if (g.add) return;
+    z.end = std::min(z.begin + bytes / 16 / row16 * row16, (size_t)a.V * row16);
+    fillers = z.end > z.begin ? 512u : 0u;
+  };
+  uint32_t* joins = words(p.o_joins);
   int from = 0;
   if (p.n == 0u) {
     // (nothing to sort: zeros alone)
   } else if (p.small) {
-    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(1024), 0, s, a, p.n, p.bits, p.passes, words(p.o_key[0]), words(p.o_pos[0]));
+    next_zeros(kZerosSmall);
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1 + fillers), dim3(1024), 0, s, a, p.n, p.bits, p.passes, words(p.o_key[0]), words(p.o_pos[0]), joins, z);
   } else {
     for (int k = 0; k < p.passes; ++k) {
       const uint32_t *key_in = k > 0 ? words(p.o_key[from]) : nullptr, *pos_in = k > 0 ? words(p.o_pos[from]) : nullptr;
       const int to = k > 0 ? from ^ 1 : 0;
-      hipLaunchKernelGGL(sort_count_kernel, dim3(p.tiles), dim3(1024), 0, s, a, p.n, key_in, k * p.bits, p.bits, words(p.o_count));
-      hipLaunchKernelGGL(sort_place_kernel, dim3(p.tiles), dim3(1024), 0, s, a, p.n, key_in, pos_in, k * p.bits, p.bits, words(p.o_count),
-                         words(p.o_key[to]), words(p.o_pos[to]));
+      next_zeros(kZerosCount);
+      hipLaunchKernelGGL(sort_count_kernel, dim3(p.tiles + fillers), dim3(1024), 0, s, a, p.n, p.tiles, key_in, k * p.bits, p.bits, words(p.o_count),
+                         k == 0 ? joins : nullptr, z);
+      next_zeros(kZerosPlace);
+      hipLaunchKernelGGL(sort_place_kernel, dim3(p.tiles + fillers), dim3(1024), 0, s, a, p.n, p.tiles, key_in, pos_in, k * p.bits, p.bits,
+                         words(p.o_count), words(p.o_key[to]), words(p.o_pos[to]), z);
       from = to;
     }
   }
@@ -589,7 +670,9 @@ int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned
   g.chunks = a.chunks;
   g.slices = (a.chunks + 63) / 64;
   g.d = c->cfg.d;
-  g.fill_blocks = g.add ? 0 : (int)(((long long)a.sentinel + 63) / 64);
+  g.joins = joins;
+  g.fill_from = (uint32_t)(z.end / row16);
+  g.fill_blocks = g.add ? 0 : (int)(((long long)a.sentinel - g.fill_from + 63) / 64);
   const long long blocks = g.fill_blocks + ((long long)p.pieces * g.slices + 3) / 4;
   if (blocks > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
   if (p.piece == kShortPiece)
@@ -597,7 +680,7 @@ int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned
   else
     hipLaunchKernelGGL((reduce_kernel<KIND, KIND == WEIGHTED ? 64 : 32>), dim3((unsigned)blocks), dim3(256), 0, s, g);
   if (p.pieces > 1)
-    hipLaunchKernelGGL(join_kernel<KIND>, dim3(p.pieces, (unsigned)((c->cfg.d + 255) / 256)), dim3(256), 0, s, g);
+    hipLaunchKernelGGL(join_kernel<KIND>, dim3((unsigned)std::min<long long>((long long)p.pieces * ((c->cfg.d + 255) / 256), 2048)), dim3(256), 0, s, g);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
