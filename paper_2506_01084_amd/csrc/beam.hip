@@ -47,7 +47,7 @@ __device__ __forceinline__ float key_value(Key k) {
 
 __device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
 
-constexpr int P_THREADS = 1024, P_GROUPS = 256, P_LIST = 2048, P_KEPT = 8, P_PARTS = 8192;
+constexpr int P_THREADS = 1024, P_GROUPS = 256, P_LIST = 2048, P_KEPT = 4, P_PARTS = 8192;
 
 struct PickLds {
   Key group[P_GROUPS];
@@ -62,22 +62,27 @@ struct PickLds {
 // The threads fall into 64 groups (n up to 16) or 256, each with the maximum of its keys; the n-th largest of those maxima is a bound that
 // at least n keys reach and at most n groups' worth: they are listed and ranked against each other.  A list that does
 // not fit (keys so arranged that many large ones fall to one group) is left for n passes, each taking the largest key below the last.
-// Up to 8 keys a thread stay in registers from the first look to the second; more are worked out again.
-template <typename F>
-__device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F key) {
+// Up to 4 keys a thread stay in registers from the first look to the second; more are worked out again.
+// read(i) is the value behind key i, from memory and without a branch, so that several are on the way together; make(i, value) the key.
+template <typename R, typename F>
+__device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, R read, F make) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool kept = count <= (uint32_t)(P_KEPT * P_THREADS);
+  auto key = [&](uint32_t i) -> Key { return make(i, read(i)); };
   Key mine_all[P_KEPT], best = 0ull;
+  if (kept) {
+    float x[P_KEPT];
 #pragma unroll
-  for (int u = 0; u < P_KEPT; ++u) {
-    const uint32_t i = tid + (uint32_t)(u * P_THREADS);
-    mine_all[u] = 0ull;
-    if (kept && (uint32_t)(u * P_THREADS) < count) mine_all[u] = i < count ? key(i) : 0ull;     // (a uniform branch: no work for what is not there)
-  }
+    for (int u = 0; u < P_KEPT; ++u) x[u] = read(min((uint32_t)(tid + u * P_THREADS), count - 1u));
 #pragma unroll
-  for (int u = 0; u < P_KEPT; ++u) best = max_key(best, mine_all[u]);
-  if (!kept)
+    for (int u = 0; u < P_KEPT; ++u) {
+      const uint32_t i = (uint32_t)(tid + u * P_THREADS);
+      mine_all[u] = i < count ? make(i, x[u]) : 0ull;
+      best = max_key(best, mine_all[u]);
+    }
+  } else {
     for (uint32_t i = tid; i < count; i += P_THREADS) best = max_key(best, key(i));
+  }
   best = max_key(best, __shfl_xor(best, 1));
   best = max_key(best, __shfl_xor(best, 2));
   const int groups = n <= 16 ? 64 : P_GROUPS;
@@ -97,7 +102,7 @@ __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F ke
   if (tid < groups) {
     const Key mine = l.group[tid];
     int above = 0;
-#pragma unroll 16
+#pragma unroll 8
     for (int i = 0; i < groups; ++i) above += l.group[i] > mine;
     if (above == n - 1 && mine != 0ull) l.threshold = mine;
   }
@@ -110,8 +115,7 @@ __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F ke
   };
   if (kept) {
 #pragma unroll
-    for (int u = 0; u < P_KEPT; ++u)
-      if ((uint32_t)(u * P_THREADS) < count) append(mine_all[u]);
+    for (int u = 0; u < P_KEPT; ++u) append(mine_all[u]);
   } else {
     for (uint32_t i = tid; i < count; i += P_THREADS) append(key(i));
   }
@@ -121,7 +125,13 @@ __device__ __forceinline__ void top_keys(PickLds& l, int n, uint32_t count, F ke
     for (uint32_t i = tid; i < found; i += P_THREADS) {
       const Key mine = l.list[i];
       uint32_t above = 0u;
-      for (uint32_t j = 0; j < found; ++j) above += l.list[j] > mine;
+      for (uint32_t j0 = 0; j0 < found; j0 += 8u) {  // (8 reads on the way at a time)
+        Key other[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) other[u] = l.list[min(j0 + (uint32_t)u, found - 1u)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) above += j0 + (uint32_t)u < found && other[u] > mine;
+      }
       if (above < (uint32_t)n) l.top[above] = mine;
     }
   } else {
@@ -163,28 +173,28 @@ __global__ void __launch_bounds__(P_THREADS) beam_pick_kernel(PickArgs a) {
     score[tid] = a.score[row0 + tid];
     columns[tid] = a.V + min(max(a.size[row0 + tid], 0), a.cap);
   }
-  // the beams' log-sum-exps, given or merged from the parts here (a launch less): a wave per beam, 16 parts a lane on the way at a time
+  // the beams' log-sum-exps, given or merged from the parts here (a launch less): a wave per beam, 8 parts a lane on the way at a time
   if (a.part_s) {
     const int lane = tid & 63;
     for (int beam = tid >> 6; beam < a.beams; beam += P_THREADS / 64) {
       const float *pm = a.part_m + (size_t)(row0 + beam) * a.n_parts, *ps = a.part_s + (size_t)(row0 + beam) * a.n_parts;
       float m = kNegInf, sum = 0.f;
-      for (int p0 = lane; p0 < a.n_parts; p0 += 16 * 64) {
-        float x[16], y[16], top = kNegInf;
+      for (int p0 = lane; p0 < a.n_parts; p0 += 8 * 64) {
+        float x[8], y[8], top = kNegInf;
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
+        for (int u = 0; u < 8; ++u) {
           const int p = p0 + 64 * u;
           x[u] = p < a.n_parts ? pm[p] : kNegInf;
           y[u] = p < a.n_parts ? ps[p] : 0.f;
           if (at_hand && p < a.n_parts) best[beam * a.n_parts + p] = x[u];
         }
 #pragma unroll
-        for (int u = 0; u < 16; ++u) top = fmaxf(top, x[u]);
+        for (int u = 0; u < 8; ++u) top = fmaxf(top, x[u]);
         const float up = fmaxf(m, top);
         sum = m == kNegInf ? sum : sum * __expf(m - up);
         // (an empty part adds nothing; a row's NaN stays NaN: a part that holds one has a NaN sum)
 #pragma unroll
-        for (int u = 0; u < 16; ++u) sum += x[u] == kNegInf ? y[u] : y[u] * __expf(x[u] - up);
+        for (int u = 0; u < 8; ++u) sum += x[u] == kNegInf ? y[u] : y[u] * __expf(x[u] - up);
         m = up;
       }
 #pragma unroll
@@ -199,35 +209,44 @@ __global__ void __launch_bounds__(P_THREADS) beam_pick_kernel(PickArgs a) {
     lse[tid] = a.row_lse[row0 + tid];
   }
   __syncthreads();
-  const uint32_t n_parts = (uint32_t)a.n_parts;
+  const uint32_t n_parts = (uint32_t)a.n_parts, slot = (1u << a.slot_shift) - 1u;
   const int n = a.picks;
-  top_keys(l, n, (uint32_t)a.beams * n_parts, [&](uint32_t i) -> Key {
-    const int beam = (int)(i / n_parts);
-    return make_key(((at_hand ? best[i] : a.part_m[(size_t)row0 * n_parts + i]) - lse[beam]) + score[beam], i);
-  });
-  if (tid < n) {
-    const Key part = l.top[tid];
-    const uint32_t at = ~(uint32_t)part, beam = part ? at / n_parts : 0u, p = part ? at - beam * n_parts : 0u;
-    int c = 0, end = 0;                              // (no such part: no columns)
-    if (part && (int)p < a.n_base_parts) {
-      c = (int)p * a.base_columns;
-      end = min(c + a.base_columns, a.V);
-    } else if (part) {
-      c = a.V + ((int)p - a.n_base_parts) * a.hyper_columns;
-      end = min(c + a.hyper_columns, columns[beam]);
+  // first the parts, then their columns (one piece of code for both: a single workgroup waits for its instructions, too)
+#pragma unroll 1
+  for (int phase = 0; phase < 2; ++phase) {
+    auto read = [&](uint32_t i) -> float {
+      if (phase == 0) return at_hand ? best[i] : a.part_m[(size_t)row0 * n_parts + i];      // (uniform)
+      const uint32_t j = i >> a.slot_shift;
+      return a.logits[(size_t)(row0 + part_beam[j]) * a.ld + min(part_from[j] + (int)(i & slot), a.ld - 1)];
+    };
+    auto make = [&](uint32_t i, float x) -> Key {
+      if (phase == 0) {
+        const uint32_t beam = i / n_parts;
+        return make_key((x - lse[beam]) + score[beam], i);
+      }
+      const uint32_t j = i >> a.slot_shift, beam = (uint32_t)part_beam[j];
+      const int c = part_from[j] + (int)(i & slot);
+      const Key k = make_key((x - lse[beam]) + score[beam], beam * (uint32_t)a.ld + (uint32_t)c);
+      return c < part_end[j] ? k : 0ull;
+    };
+    top_keys(l, n, phase == 0 ? (uint32_t)a.beams * n_parts : (uint32_t)n << a.slot_shift, read, make);
+    if (phase == 0 && tid < n) {
+      const Key part = l.top[tid];
+      const uint32_t at = ~(uint32_t)part, beam = part ? at / n_parts : 0u, p = part ? at - beam * n_parts : 0u;
+      int c = 0, end = 0;                            // (no such part: no columns)
+      if (part && (int)p < a.n_base_parts) {
+        c = (int)p * a.base_columns;
+        end = min(c + a.base_columns, a.V);
+      } else if (part) {
+        c = a.V + ((int)p - a.n_base_parts) * a.hyper_columns;
+        end = min(c + a.hyper_columns, columns[beam]);
+      }
+      part_beam[tid] = (int)beam;
+      part_from[tid] = c;
+      part_end[tid] = end;
     }
-    part_beam[tid] = (int)beam;
-    part_from[tid] = c;
-    part_end[tid] = end;
+    __syncthreads();
   }
-  __syncthreads();
-  const uint32_t slot = (1u << a.slot_shift) - 1u;
-  top_keys(l, n, (uint32_t)n << a.slot_shift, [&](uint32_t i) -> Key {
-    const uint32_t j = i >> a.slot_shift;
-    const int beam = part_beam[j], c = part_from[j] + (int)(i & slot);
-    if (c >= part_end[j]) return 0ull;
-    return make_key((a.logits[(size_t)(row0 + beam) * a.ld + c] - lse[beam]) + score[beam], (uint32_t)beam * (uint32_t)a.ld + (uint32_t)c);
-  });
   if (tid < n) {
     const Key k = l.top[tid];
     const size_t out = (size_t)blockIdx.x * n + tid;
