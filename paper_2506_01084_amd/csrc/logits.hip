@@ -772,7 +772,14 @@ int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const voi
     z2z_sample_params sp;
     sp.temperature = 1.0f;
     sp.seed = sp.step = 0;
-    const bool mid_base = (rows > 64 || split_few(c, rows, true)) && c->opt_logits_kernel == 0 && z2z_logits_mid_ok(c, rows);
+    // The base vocabulary on the weight-streaming kernel, the hyper units in a launch of their own, from 4 rows on, and from 2 on up to 256 tiles
+    // of it; else the decode kernel's units, both in one launch.  One launch / two, us, whole calls: 1 x 4 rows V = 8000, d = 512 48 / 26, 32000 x 1024
+    // 52 / 35, 32000 x 4096 88 / 73, 50257 x 768 54 / 35, 128256 x 2048 108 / 108, 128256 x 4096 196 / 188, 151936 x 3584 216 / 214; 2 rows 32 / 25, 37 / 35,
+    // 83 / 71, 43 / 35, 90 / 106, 184 / 185, 189 / 212; 1 row 24 / 26, 32 / 35, 60 / 72, 41 / 34, 90 / 108, 184 / 184, 187 / 212; 8 x 4 rows, entries up to
+    // 512 / 4096, V = 32000, d = 1024 45 / 38, 74 / 77, d = 4096 97 / 81, 182 / 188, V = 80000, d = 4096 218 / 167, 274 / 273; 16 x 4 rows 51 / 48, 101 / 106,
+    // 108 / 104, 320 / 316, 235 / 188, 402 / 404.
+    const bool mid_base = (rows >= 4 || (rows >= 2 && z2z_logits_mid_tiles(c->cfg.V) <= 256)) && c->opt_logits_kernel == 0 &&
+                          c->opt_decode_kernel == 0 && z2z_logits_mid_ok(c, rows);
     int base = 0, hyper = 0;
     rc = launch_stored_logits(c, H, rows, W_base, W_hyper, sp, mid_base, &n_parts, &base, &hyper, s);
     if (rc != Z2Z_OK) return rc;
