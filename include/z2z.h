@@ -32,8 +32,12 @@
  *     `stream` is being captured into a graph a buffer cannot grow: the call returns Z2Z_ECAPTURE and
  *     enqueues nothing -- make one eager call at the same shape before capturing, or use
  *     z2z_extended_logits_static, which never allocates.
+ *     Once a call of z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward or z2z_extended_beam has been
+ *     captured, no work buffer of the context is freed before z2z_destroy: one that grows leaves the old one to the graph.
  *   - Calls on one context must be issued from one host thread at a time, and work of one context
- *     must be ordered (same stream, or synchronised by the caller).
+ *     must be ordered (same stream, or synchronised by the caller).  z2z_embed_codes and what follows it in this list below
+ *     (embed_codes_backward, extended_distill and its backward pass, extended_beam, codebook_reorder) return Z2Z_EINVAL where
+ *     the current device is not the one that the context was created on.
  */
 #ifndef Z2Z_H
 #define Z2Z_H
@@ -202,7 +206,8 @@ int z2z_hyper_embed(z2z_ctx* ctx, const void* d_E, void* d_W_hyper, const int32_
  * the product in fp32, rounded once to the storage type (scale = 1: the row as it is).  A code that names no row gives a row of zeros
  * and sets BAD_CODE for its sequence; the others are unaffected.  Rows at and behind n_codes[b] are left as they were.
  *   d_codes [B, stride] int32, d_n_codes [B] or NULL (every row has `stride`);  scale finite (else Z2Z_EINVAL)
- *   d_E [V, d], d_W_hyper [B, cap, d], d_X [B, stride, d] out: dtype of the context;  d_status [B] int32 out
+ *   d_E [V, d], d_W_hyper [B, cap, d], d_X [B, stride, d] out: dtype of the context;  d_status [B] int32 out (not the buffer of
+ *   d_n_codes: Z2Z_EINVAL)
  * One code per sequence (stride 1) is the input of a generation step. */
 int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, const void* d_E,
                     const void* d_W_hyper, float scale, void* d_X, int32_t* d_status, void* stream);
@@ -366,7 +371,7 @@ int z2z_extended_sample(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t row
  *   d_parent [B / beams, n_pick] int32 out: the beam, 0 .. beams - 1, that is continued
  *   d_code   [B / beams, n_pick] int32 out: by this base token or hypertoken (of the parent's codebook)
  *   d_picked [B / beams, n_pick] float out: the value above, the new beam's score
- *            (-1, -1 and -inf where fewer continuations are there)
+ *            (-1, -1 and -inf where fewer continuations are there); with n_pick = beams it may be the buffer of d_score
  * n_pick may be larger than beams: the caller takes out finished sequences first.  A step goes on with z2z_codebook_reorder,
  * then z2z_step_update with the picked codes.
  * beams <= Z2Z_MAX_BEAMS and n_pick <= Z2Z_MAX_PICK, else Z2Z_EUNSUPPORTED; any storage type and width.  The logits go

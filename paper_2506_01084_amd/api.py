@@ -185,6 +185,7 @@ class Context:
             cfg.w[j] = float(w[j]) if w is not None and j < len(w) else 0.0
         self.B, self.V, self.M, self.cap, self.d, self.dtype = B, V, M, cap, d, dtype
         self.torch_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
+        self._device = torch.cuda.current_device()
         self._h = c_void_p()
         _check(self._lib.z2z_create(byref(self._h), byref(cfg)), "z2z_create")
 
@@ -198,6 +199,12 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def _own(self, t: Optional[torch.Tensor], dtype) -> Optional[int]:
+        """_ptr of a tensor that has to be on the context's device."""
+        if t is not None and t.get_device() != self._device:
+            raise ValueError(f"expected a tensor on cuda:{self._device}, got one on {t.device}")
+        return _ptr(t, dtype)
 
     def reset(self) -> None:
         _check(self._lib.z2z_reset(self._h, _stream()), "z2z_reset")
@@ -297,28 +304,28 @@ class Context:
     def embed_codes(self, codes: torch.Tensor, n_codes: Optional[torch.Tensor], E: torch.Tensor, W_hyper: torch.Tensor,
                     X: torch.Tensor, status: torch.Tensor, scale: float = 1.0) -> None:
         """X[b, i] = scale * (row of E or W_hyper[b] that codes[b, i] names); rows behind n_codes[b] are left as they were."""
-        assert codes.dim() == 2 and codes.shape[0] == self.B and tuple(X.shape) == (*codes.shape, self.d)
-        assert tuple(E.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
+        assert codes.dim() == 2 and codes.shape[0] == self.B and X.shape == (*codes.shape, self.d)
+        assert E.shape == (self.V, self.d) and W_hyper.shape == (self.B, self.cap, self.d)
         assert (n_codes is None or n_codes.numel() == self.B) and status.numel() == self.B
-        _check(self._lib.z2z_embed_codes(self._h, _ptr(codes, torch.int32), _ptr(n_codes, torch.int32), codes.shape[1],
-                                         _ptr(E, self.torch_dtype), _ptr(W_hyper, self.torch_dtype), float(scale),
-                                         _ptr(X, self.torch_dtype), _ptr(status, torch.int32), _stream()), "z2z_embed_codes")
+        _check(self._lib.z2z_embed_codes(self._h, self._own(codes, torch.int32), self._own(n_codes, torch.int32), codes.shape[1],
+                                         self._own(E, self.torch_dtype), self._own(W_hyper, self.torch_dtype), float(scale),
+                                         self._own(X, self.torch_dtype), self._own(status, torch.int32), _stream()), "z2z_embed_codes")
 
     def embed_codes_backward(self, codes: torch.Tensor, n_codes: Optional[torch.Tensor], dX: torch.Tensor, dE: torch.Tensor,
                              dW_hyper: torch.Tensor, scale: float = 1.0, add: bool = False) -> None:
         """The gradients of embed_codes, overwritten or (add=True) added to what is there."""
-        assert codes.dim() == 2 and codes.shape[0] == self.B and tuple(dX.shape) == (*codes.shape, self.d)
-        assert tuple(dE.shape) == (self.V, self.d) and tuple(dW_hyper.shape) == (self.B, self.cap, self.d)
+        assert codes.dim() == 2 and codes.shape[0] == self.B and dX.shape == (*codes.shape, self.d)
+        assert dE.shape == (self.V, self.d) and dW_hyper.shape == (self.B, self.cap, self.d)
         assert n_codes is None or n_codes.numel() == self.B
-        _check(self._lib.z2z_embed_codes_backward(self._h, _ptr(codes, torch.int32), _ptr(n_codes, torch.int32), codes.shape[1],
-                                                  float(scale), _ptr(dX, self.torch_dtype), GRAD_ADD if add else 0,
-                                                  _ptr(dE, torch.float32), _ptr(dW_hyper, self.torch_dtype), _stream()),
+        _check(self._lib.z2z_embed_codes_backward(self._h, self._own(codes, torch.int32), self._own(n_codes, torch.int32), codes.shape[1],
+                                                  float(scale), self._own(dX, self.torch_dtype), GRAD_ADD if add else 0,
+                                                  self._own(dE, torch.float32), self._own(dW_hyper, self.torch_dtype), _stream()),
                "z2z_embed_codes_backward")
 
     def codebook_reorder(self, beams: int, source: torch.Tensor, W_hyper: Optional[torch.Tensor] = None) -> None:
         """Sequence p * beams + k takes over the state of sequence p * beams + source[p * beams + k] (in place, cache rows too)."""
-        assert source.numel() == self.B and (W_hyper is None or tuple(W_hyper.shape) == (self.B, self.cap, self.d))
-        _check(self._lib.z2z_codebook_reorder(self._h, int(beams), _ptr(source, torch.int32), _ptr(W_hyper, self.torch_dtype),
+        assert source.numel() == self.B and (W_hyper is None or W_hyper.shape == (self.B, self.cap, self.d))
+        _check(self._lib.z2z_codebook_reorder(self._h, int(beams), self._own(source, torch.int32), self._own(W_hyper, self.torch_dtype),
                                               _stream()), "z2z_codebook_reorder")
 
     def hyper_encode(self, E: torch.Tensor, encoder: "Encoder", W_hyper: torch.Tensor,
@@ -383,13 +390,13 @@ class Context:
                       parent: torch.Tensor, code: torch.Tensor, picked: torch.Tensor) -> None:
         """The best continuations of every prompt's beams; parent, code and picked are [B / beams, n_pick]."""
         rows = H.shape[0]
-        assert H.shape[1] == self.d and tuple(W_base.shape) == (self.V, self.d)
-        assert tuple(W_hyper.shape) == (self.B, self.cap, self.d) and score.numel() == rows
+        assert H.shape[1] == self.d and W_base.shape == (self.V, self.d)
+        assert W_hyper.shape == (self.B, self.cap, self.d) and score.numel() == rows
         assert beams >= 1 and parent.dim() == 2 and parent.shape[0] * beams == rows
-        assert tuple(code.shape) == tuple(parent.shape) and tuple(picked.shape) == tuple(parent.shape)
-        _check(self._lib.z2z_extended_beam(self._h, _ptr(H, self.torch_dtype), rows, int(beams), _ptr(W_base, self.torch_dtype),
-                                           _ptr(W_hyper, self.torch_dtype), _ptr(score, torch.float32), parent.shape[1],
-                                           _ptr(parent, torch.int32), _ptr(code, torch.int32), _ptr(picked, torch.float32),
+        assert code.shape == parent.shape and picked.shape == parent.shape
+        _check(self._lib.z2z_extended_beam(self._h, self._own(H, self.torch_dtype), rows, int(beams), self._own(W_base, self.torch_dtype),
+                                           self._own(W_hyper, self.torch_dtype), self._own(score, torch.float32), parent.shape[1],
+                                           self._own(parent, torch.int32), self._own(code, torch.int32), self._own(picked, torch.float32),
                                            _stream()), "z2z_extended_beam")
 
     def extended_nll(self, H: torch.Tensor, rows_per_seq: int, W_base: torch.Tensor, W_hyper: torch.Tensor,
@@ -422,13 +429,13 @@ class Context:
                          temperature: float = 1.0) -> None:
         """The loss against a teacher's listed logits; ids, teacher and student are [rows, K]."""
         rows = H.shape[0]
-        assert H.shape[1] == self.d and tuple(W_base.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
-        assert ids.dim() == 2 and ids.shape[0] == rows and tuple(teacher.shape) == tuple(ids.shape) == tuple(student.shape)
+        assert H.shape[1] == self.d and W_base.shape == (self.V, self.d) and W_hyper.shape == (self.B, self.cap, self.d)
+        assert ids.dim() == 2 and ids.shape[0] == rows and teacher.shape == ids.shape == student.shape
         assert kl.numel() == rows and lse.numel() == rows
-        _check(self._lib.z2z_extended_distill(self._h, _ptr(H, self.torch_dtype), rows, rows_per_seq, _ptr(W_base, self.torch_dtype),
-                                              _ptr(W_hyper, self.torch_dtype), ids.shape[1], _ptr(ids, torch.int32),
-                                              _ptr(teacher, torch.float32), float(temperature), _ptr(kl, torch.float32),
-                                              _ptr(lse, torch.float32), _ptr(student, torch.float32), _stream()),
+        _check(self._lib.z2z_extended_distill(self._h, self._own(H, self.torch_dtype), rows, rows_per_seq, self._own(W_base, self.torch_dtype),
+                                              self._own(W_hyper, self.torch_dtype), ids.shape[1], self._own(ids, torch.int32),
+                                              self._own(teacher, torch.float32), float(temperature), self._own(kl, torch.float32),
+                                              self._own(lse, torch.float32), self._own(student, torch.float32), _stream()),
                "z2z_extended_distill")
 
     def extended_distill_backward(self, H: torch.Tensor, rows_per_seq: int, W_base: torch.Tensor, W_hyper: torch.Tensor,
@@ -436,17 +443,17 @@ class Context:
                                   grad_kl: Optional[torch.Tensor], dH: torch.Tensor, dW_base: torch.Tensor,
                                   dW_hyper: torch.Tensor, temperature: float = 1.0) -> None:
         rows = H.shape[0]
-        assert H.shape[1] == self.d and tuple(W_base.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
-        assert ids.dim() == 2 and ids.shape[0] == rows and tuple(teacher.shape) == tuple(ids.shape) == tuple(student.shape)
+        assert H.shape[1] == self.d and W_base.shape == (self.V, self.d) and W_hyper.shape == (self.B, self.cap, self.d)
+        assert ids.dim() == 2 and ids.shape[0] == rows and teacher.shape == ids.shape == student.shape
         assert lse.numel() == rows and (grad_kl is None or grad_kl.numel() == rows)
-        assert tuple(dH.shape) == tuple(H.shape) and tuple(dW_base.shape) == tuple(W_base.shape)
-        assert tuple(dW_hyper.shape) == (self.B, self.cap, self.d)
-        _check(self._lib.z2z_extended_distill_backward(self._h, _ptr(H, self.torch_dtype), rows, rows_per_seq,
-                                                       _ptr(W_base, self.torch_dtype), _ptr(W_hyper, self.torch_dtype), ids.shape[1],
-                                                       _ptr(ids, torch.int32), _ptr(teacher, torch.float32), float(temperature),
-                                                       _ptr(lse, torch.float32), _ptr(student, torch.float32),
-                                                       _ptr(grad_kl, torch.float32), _ptr(dH, self.torch_dtype),
-                                                       _ptr(dW_base, self.torch_dtype), _ptr(dW_hyper, self.torch_dtype), _stream()),
+        assert dH.shape == H.shape and dW_base.shape == W_base.shape
+        assert dW_hyper.shape == (self.B, self.cap, self.d)
+        _check(self._lib.z2z_extended_distill_backward(self._h, self._own(H, self.torch_dtype), rows, rows_per_seq,
+                                                       self._own(W_base, self.torch_dtype), self._own(W_hyper, self.torch_dtype), ids.shape[1],
+                                                       self._own(ids, torch.int32), self._own(teacher, torch.float32), float(temperature),
+                                                       self._own(lse, torch.float32), self._own(student, torch.float32),
+                                                       self._own(grad_kl, torch.float32), self._own(dH, self.torch_dtype),
+                                                       self._own(dW_base, self.torch_dtype), self._own(dW_hyper, self.torch_dtype), _stream()),
                "z2z_extended_distill_backward")
 
     def hyper_embed_backward(self, dW_hyper: torch.Tensor, dE: torch.Tensor) -> None:

@@ -367,6 +367,7 @@ Z2Z_API int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t*
   if (!ctx || !d_E || !d_status || stride < 0) return Z2Z_EINVAL;
   if (stride > 0 && (!d_codes || !d_X)) return Z2Z_EINVAL;
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
+  if (d_status == d_n_codes) return Z2Z_EINVAL;      // (other workgroups read the lengths while the statuses are written)
   if (!isfinite(scale)) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper) || !aligned16(d_X)) return Z2Z_EINVAL;
   const int rc = enter(ctx, static_cast<hipStream_t>(stream));

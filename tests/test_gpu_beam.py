@@ -172,11 +172,72 @@ def test_all_columns_equal_and_rows_that_are_not_finite():
         ctx.close()
 
 
-def _context_state(ctx, W):
+def test_large_values_that_crowd_into_few_groups():
+    """More large columns than the pick's short list holds, in few of its groups, and one group that has none of them: the passes behind the list."""
     import torch
+    from paper_2506_01084_amd import api
 
+    print("[case] beam, crowded columns", flush=True)
+    B, V, d = 4, 40000, 128
+    ctx = api.Context(B=B, V=V, M=2, cap=16, d=d, dtype="bf16")
+    c = np.arange(V)
+    value = np.where(c % 256 < 64, 8.0, 1.0)
+    value[(c % 256 >= 60) & (c % 256 < 64) & (c // 256 % 4 == 3)] = 4.0
+    E = torch.zeros((V, d), dtype=torch.bfloat16, device="cuda")
+    E[:, 0] = torch.from_numpy(value).cuda().bfloat16()
+    H = torch.zeros((B, d), dtype=torch.bfloat16, device="cuda")
+    H[:, 0] = 1.0
+    W = torch.zeros((B, 16, d), dtype=torch.bfloat16, device="cuda")
+    score = torch.tensor([0.0, -math.inf, -math.inf, -math.inf], device="cuda")
+    parent, code, picked = _run(ctx, H, 4, E, W, score, 64)
+    assert (parent == 0).all() and (code[0] == np.arange(64)).all() and len(set(picked[0])) == 1
+    ctx.close()
+
+
+@pytest.mark.parametrize("V,beams,picks", [(3_000_000, 2, 64), (200_001, 32, 40)])
+def test_very_large_vocabularies(V, beams, picks):
+    """More parts than stay at hand: whole numbers, the order by value, beam and column exactly."""
+    import torch
+    from paper_2506_01084_amd import api
+
+    print(f"[case] beam, V={V} beams={beams}", flush=True)
+    d = 4
+    rng = np.random.default_rng(V)
+    ctx = api.Context(B=beams, V=V, M=2, cap=0, d=d, dtype="f32")
+    E = rng.integers(-9, 10, size=(V, d)).astype(np.float32)
+    H = np.repeat(rng.integers(-3, 4, size=(1, d)), beams, axis=0).astype(np.float32)
+    parent, code, picked = _run(ctx, torch.from_numpy(H).cuda(), beams, torch.from_numpy(E).cuda(), torch.zeros((beams, 0, d), device="cuda"),
+                                torch.zeros(beams, device="cuda"), picks)
+    z = E @ H[0]
+    order = np.lexsort((np.arange(V), -z))[:picks]           # within a beam
+    want = sorted(((-z[c], r, c) for r in range(beams) for c in order), key=lambda x: x)[:picks]
+    assert [(int(r), int(c)) for r, c in zip(parent[0], code[0])] == [(r, c) for _, r, c in want]
+    assert (np.diff(picked[0]) <= 0).all()
+    ctx.close()
+
+
+def test_scores_may_be_picked_in_place_and_tensors_are_checked():
+    import torch
+    from paper_2506_01084_amd import api
+
+    print("[case] beam, in place", flush=True)
+    ctx, tokens, lens, ref, E, H, d_E, d_W = _setup("bf16", 24, 900, 128, 3, 60, 100, 8)
+    score = -torch.rand(24, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    d_H = torch_storage(H, "bf16")
+    parent, code, picked = _run(ctx, d_H, 4, d_E, d_W, score, 4)
+    both = score.clone()
+    p, c = (torch.zeros((6, 4), dtype=torch.int32, device="cuda") for _ in range(2))
+    ctx.extended_beam(d_H, 4, d_E, d_W, both, p, c, both.view(6, 4))
     torch.cuda.synchronize()
-    return [t.cpu().numpy().copy() for t in ctx.codebook()] + [W.view(torch.int16 if W.dtype == torch.bfloat16 else torch.int32).cpu().numpy().copy()]
+    assert (p.cpu().numpy() == parent).all() and (c.cpu().numpy() == code).all() and (both.cpu().numpy().reshape(6, 4) == picked).all()
+    for bad in (both.double(), both.cpu(), torch.zeros((24, 2), device="cuda")[:, 0]):
+        with pytest.raises(ValueError):
+            ctx.extended_beam(d_H, 4, d_E, d_W, bad, p, c, both.view(6, 4))
+    with pytest.raises(ValueError):
+        ctx.codebook_reorder(4, p.reshape(24).long(), d_W)
+    with pytest.raises(api.Z2ZError):
+        ctx.codebook_reorder(5, p.reshape(24), d_W)
+    ctx.close()
 
 
 @pytest.mark.parametrize("dtype,B,beams,V,d,M,cap,N", [

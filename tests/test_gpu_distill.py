@@ -78,6 +78,7 @@ SHAPES = [
     ("bf16", 3, 1, 3000, 128, 3, 100, 8, 1.0),        # one row per sequence
     ("bf16", 3, 1, 3000, 128, 3, 100, 8, 2.0),
     ("bf16", 70, 1, 30000, 128, 3, 50, 5, 4.0),
+    ("bf16", 300, 1, 600, 64, 3, 20, 3, 2.0),         # more rows than the streaming kernel takes, one per sequence
     ("bf16", 4, 5, 2000, 256, 4, 300, 33, 1.0),       # a few rows
     ("bf16", 4, 5, 2000, 256, 4, 300, 33, 0.0625),
     ("bf16", 2, 61, 5003, 192, 3, 200, 64, 2.0),      # the streaming kernel

@@ -197,6 +197,47 @@ def test_nan_and_infinities_stay_where_they_are():
     ctx.close()
 
 
+def test_empty_calls_and_refused_tensors():
+    import torch
+    from paper_2506_01084_amd import api
+
+    print("[case] lookup, empty and refused", flush=True)
+    B, V, d, cap = 3, 700, 40, 5
+    ctx = api.Context(B=B, V=V, M=2, cap=cap, d=d, dtype="bf16")
+    _book(ctx, [5, 0, 2], 1)
+    E, W = torch.ones((V, d), dtype=torch.bfloat16, device="cuda"), torch.ones((B, cap, d), dtype=torch.bfloat16, device="cuda")
+    none = torch.zeros((B, 0), dtype=torch.int32, device="cuda")
+    X0, st = torch.zeros((B, 0, d), dtype=torch.bfloat16, device="cuda"), torch.full((B,), 9, dtype=torch.int32, device="cuda")
+    ctx.embed_codes(none, None, E, W, X0, st)
+    dE, dW = torch.ones((V, d), device="cuda"), torch.ones((B, cap, d), dtype=torch.bfloat16, device="cuda")
+    ctx.embed_codes_backward(none, None, X0, dE, dW, add=True)
+    torch.cuda.synchronize()
+    assert st.tolist() == [0, 0, 0] and (dE == 1).all() and (dW == 1).all()
+    ctx.embed_codes_backward(none, None, X0, dE, dW)
+    torch.cuda.synchronize()
+    assert (dE == 0).all() and (dW == 0).all()
+    # lengths of zero alone, and lengths beyond the row
+    codes, X = torch.zeros((B, 4), dtype=torch.int32, device="cuda"), torch.full((B, 4, d), 3.0, dtype=torch.bfloat16, device="cuda")
+    ctx.embed_codes(codes, torch.tensor([0, -5, 0], dtype=torch.int32, device="cuda"), E, W, X, st)
+    dE.fill_(1)
+    ctx.embed_codes_backward(codes, torch.tensor([0, -5, 0], dtype=torch.int32, device="cuda"), X, dE, dW)
+    torch.cuda.synchronize()
+    assert (X == 3).all() and (dE == 0).all()
+    ctx.embed_codes(codes, torch.tensor([9, 4, 2 ** 31 - 1], dtype=torch.int32, device="cuda"), E, W, X, st)
+    torch.cuda.synchronize()
+    assert (X == 1).all()
+    for bad in (X.transpose(1, 2).contiguous().transpose(1, 2), X.float(), X.cpu()):
+        with pytest.raises(ValueError):
+            ctx.embed_codes(codes, None, E, W, bad, st)
+        with pytest.raises(ValueError):
+            ctx.embed_codes_backward(codes, None, bad, dE, dW)
+    with pytest.raises(api.Z2ZError):
+        ctx.embed_codes(codes, st, E, W, X, st)              # lengths and statuses in one buffer
+    with pytest.raises(api.Z2ZError):
+        ctx.embed_codes(codes, None, E, W, X, st, scale=math.inf)
+    ctx.close()
+
+
 def test_offsets_beyond_32_bits():
     """More than 2^32 bytes of rows, and rows of the joint table behind 2^31 elements: the far ends are right."""
     import torch

@@ -10,10 +10,10 @@ def test_lookup_refusals(without_a_device):
 h = context(B=4, V=1000, M=3, cap=100, d=128)
 Q = P + 8                                                 # not 16-byte aligned
 inf, nan = float("inf"), float("nan")
-fwd = lambda c=h, codes=P, n=P, stride=7, E=P, W=P, scale=1.0, X=P, st=P: lib.z2z_embed_codes(c, codes, n, stride, E, W, scale, X, st, None)
+fwd = lambda c=h, codes=P, n=P, stride=7, E=P, W=P, scale=1.0, X=P, st=P + 64: lib.z2z_embed_codes(c, codes, n, stride, E, W, scale, X, st, None)
 bwd = lambda c=h, codes=P, n=P, stride=7, scale=1.0, dX=P, flags=0, dE=P, dW=P: lib.z2z_embed_codes_backward(c, codes, n, stride, scale, dX, flags, dE, dW, None)
 for bad in (dict(c=None), dict(codes=None), dict(E=None), dict(W=None), dict(X=None), dict(st=None), dict(stride=-1), dict(scale=inf), dict(scale=nan),
-            dict(E=Q), dict(W=Q), dict(X=Q)):
+            dict(E=Q), dict(W=Q), dict(X=Q), dict(st=P)):             # (the last: the lengths' buffer)
     assert fwd(**bad) == api.E_INVAL, bad
 for bad in (dict(c=None), dict(codes=None), dict(dX=None), dict(dE=None), dict(dW=None), dict(stride=-1), dict(scale=-inf), dict(flags=2), dict(flags=-1),
             dict(dX=Q), dict(dE=Q), dict(dW=Q)):
