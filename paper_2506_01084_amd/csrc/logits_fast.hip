@@ -637,7 +637,7 @@ __device__ __forceinline__ void store_partial16(const Acc& acc, float* part, int
 // Store one finished tile as the gradient of the loss with respect to the logits (see LogitsArgs, probability mode).
 // Columns come in fours; ldo is a multiple of 64.
 __device__ __forceinline__ void store_prob16(const Acc& acc, const LogitsArgs& a, void* out, int ldo, int col0, int row_base, int r_end,
-                                             int col_base, int n_valid) {
+                                             int col_base, int n_valid, float inv_t) {
   const int lane15 = threadIdx.x & 15;
   float lse[F_N], g[F_N];
   int tgt[F_N];
@@ -661,7 +661,7 @@ __device__ __forceinline__ void store_prob16(const Acc& acc, const LogitsArgs& a
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float z = read_acc(acc[i][j][e]);
-        const float p = __expf(fmaf(z, a.inv_t, -lse[j])) - (col + e == tgt[j] ? 1.f : 0.f);
+        const float p = __expf(fmaf(z, inv_t, -lse[j])) - (col + e == tgt[j] ? 1.f : 0.f);
         x[e] = col + e < n_valid ? g[j] * p : 0.f;
       }
       o[i] = uint2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -730,10 +730,14 @@ __device__ __forceinline__ void merge_rows(R (&a)[F_N], S swap, float inv_t = 1.
 // HYP (modes 0 and 3): the items of the per-sequence hyper part (a.hyper) that exist are dealt out with the base part's last tiles.  In a launch
 // of its own that part is one or two rounds of tiles on a few CUs (58 us at d = 3072): V = 32064, 8 x 86 rows 190 -> 146 us, 17 x 75 257 -> 204;
 // V = 128256, d = 4096, 3 x 176 654 -> 597, 2 x 577 1090 -> 1043; level about 10000 rows (3 x 3577 7818 and 7826).
-template <int MODE, bool ROT = false, bool TW = false, bool TH = false, bool HYP = false>
+// TEMP (modes 0, 1 and 3): the softmax has a temperature.  (Instances of their own: with 1 / T and log2(e) / T read from the arguments in every call,
+// which costs two more scalar registers, 32768 rows x 128256 at T = 1 took 23.82 ms instead of 23.66.)
+template <int MODE, bool ROT = false, bool TW = false, bool TH = false, bool HYP = false, bool TEMP = false>
 __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   static_assert((MODE == 2 || !TW) && (TW || !TH), "dense layers only, and H K-major only where W is");
   static_assert(!HYP || MODE == 0 || (MODE == 3 && !ROT), "");
+  static_assert(!TEMP || MODE == 0 || MODE == 1 || MODE == 3, "");
+  const float inv_t = TEMP ? a.inv_t : 1.f, log2e_t = TEMP ? a.log2e_t : 1.4426950408889634f;
   constexpr bool PROBE_NOREQ = MODE == 8 || MODE == 9;
   constexpr bool PROBE_MFMA = MODE == 9;
   constexpr bool LIST = MODE != 1 && MODE != 5;
@@ -1176,14 +1180,14 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
         store_partial16(acc, a.partial + (size_t)ks * a.rows * a.ldo, a.ldo, row_base, r_end, col_base, n_valid);
       } else if (MODE == 3) {
         store_prob16(acc, a, hyper ? a.hyper.out : a.out, hyper ? a.hyper.ldo : a.ldo, hyper ? a.hyper.col0 : a.col0, row_base, r_end, col_base,
-                     n_valid);
+                     n_valid, inv_t);
       } else if (MODE == 6) {
         fold_sample16(acc, run, draw, a, row_base, col_base, n_valid);
       } else if (MODE == 7) {
         fold_store16(acc, run, a, row_base, r_end, col_base, n_valid);
       } else {
         if ((vt + 1) * FT > n_valid) mask_tail16(acc, col_base, n_valid);
-        fold_tile16(acc, run, col_base, hyper ? a.hyper.col0 : a.col0, n_valid, a.inv_t, a.log2e_t);
+        fold_tile16(acc, run, col_base, hyper ? a.hyper.col0 : a.col0, n_valid, inv_t, log2e_t);
       }
     }
     if (MODE >= 2 && MODE <= 5) continue;
@@ -1191,7 +1195,7 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
     // (each exchange halves a lane's rows: 6 merges and no shuffles, where every row merged in all lanes took 16 and 48 and three
     // lanes in four idled behind them.  32000 columns, 300 / 3500 rows, d = 64 33.1 -> 28.2, 92.4 -> 80.1 us, d = 1024 66.0 -> 61.4,
     // 246.9 -> 232.4)
-    const float inv_t = MODE < 2 ? a.inv_t : 1.f;    // (the draws' values are logit / T)
+    // (inv_t is 1 for draws: their values are logit / T)
     merge_rows<4>(run, Swap16{}, inv_t);
     merge_rows<2>(run, Swap32{}, inv_t);
     if (MODE == 6) {
@@ -1323,8 +1327,22 @@ int z2z_launch_linear_kmajor(const LogitsArgs& a, bool rows_too, unsigned grid, 
 
 int z2z_launch_logits_fast(int mode, const LogitsArgs& a, unsigned grid, hipStream_t s) {
   const bool rot = a.row_tiles == 1;
+  if (a.hyper.n_work > 0 && a.hyper.n_seq > F_HYP_SEQS) return Z2Z_EUNSUPPORTED;
+  if ((mode == 0 || mode == 1 || mode == 3) && a.inv_t != 1.f) {
+    if (mode == 0 && a.hyper.n_work > 0)
+      hipLaunchKernelGGL((logits_fast_kernel<0, false, false, false, true, true>), dim3(grid), dim3(F_THREADS), F_HYP_LDS, s, a);
+    else if (mode == 0)
+      hipLaunchKernelGGL((logits_fast_kernel<0, false, false, false, false, true>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+    else if (mode == 1)
+      hipLaunchKernelGGL((logits_fast_kernel<1, false, false, false, false, true>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+    else if (a.hyper.n_work > 0)
+      hipLaunchKernelGGL((logits_fast_kernel<3, false, false, false, true, true>), dim3(grid), dim3(F_THREADS), F_HYP_LDS, s, a);
+    else
+      hipLaunchKernelGGL((logits_fast_kernel<3, false, false, false, false, true>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+    Z2Z_HIP_TRY(hipGetLastError());
+    return Z2Z_OK;
+  }
   if (a.hyper.n_work > 0) {
-    if (a.hyper.n_seq > F_HYP_SEQS) return Z2Z_EUNSUPPORTED;
     if (mode == 3)
       hipLaunchKernelGGL((logits_fast_kernel<3, false, false, false, true>), dim3(grid), dim3(F_THREADS), F_HYP_LDS, s, a);
     else if (mode != 0)
@@ -1408,5 +1426,12 @@ int z2z_logits_fast_prepare(z2z_ctx* c) {
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<7, true>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
+  const void* at_a_temperature[] = {reinterpret_cast<const void*>(logits_fast_kernel<0, false, false, false, false, true>),
+                                    reinterpret_cast<const void*>(logits_fast_kernel<0, false, false, false, true, true>),
+                                    reinterpret_cast<const void*>(logits_fast_kernel<1, false, false, false, false, true>),
+                                    reinterpret_cast<const void*>(logits_fast_kernel<3, false, false, false, false, true>),
+                                    reinterpret_cast<const void*>(logits_fast_kernel<3, false, false, false, true, true>)};
+  for (const void* k : at_a_temperature)
+    Z2Z_HIP_TRY(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, F_HYP_LDS));
   return Z2Z_OK;
 }
