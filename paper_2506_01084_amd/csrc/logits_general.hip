@@ -80,7 +80,7 @@ __device__ __forceinline__ void meet() {
 // Fold the wave's 32 NI x 64 logits into the running triples (and store them).  TAIL: the tile has columns that do not exist.
 template <bool STORE, bool TAIL, int NI>
 __device__ __forceinline__ void fold_general(const f32x16 (&acc)[NI][2], Triple (&run)[2], const LogitsArgs& a, int row0,
-                                             int r_end, int col_base, int n_valid) {
+                                             int r_end, int col_base, int n_valid, float inv_t) {
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int hrow = row0 + j * 32;
@@ -102,7 +102,7 @@ __device__ __forceinline__ void fold_general(const f32x16 (&acc)[NI][2], Triple 
         if (STORE && col < n_valid && hrow < r_end) out[col] = x[v];
       }
       if (gmax > run[j].m) {
-        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf((run[j].m - gmax) * a.inv_t);
+        run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf((run[j].m - gmax) * inv_t);
         run[j].m = gmax;
         run[j].i = a.col0 + col_base + i * 32 + (targ >> 2) * 8 + (targ & 3);
       }
@@ -111,18 +111,21 @@ __device__ __forceinline__ void fold_general(const f32x16 (&acc)[NI][2], Triple 
         const float m = run[j].m == kNegInf ? 0.f : run[j].m;
         float add = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) add += __expf((x[v] - m) * a.inv_t);
+        for (int v = 0; v < 16; ++v) add += __expf((x[v] - m) * inv_t);
         run[j].s += add;
       }
     }
   }
 }
 
-template <typename T, int TV, bool STORE>
+// TEMP: the softmax has a temperature.  (1 / T from the arguments in every call: 1024 rows x 32000, d = 256, fp32 at T = 1 0.8 % longer.)
+template <typename T, int TV, bool STORE, bool TEMP = false>
 __global__ void __launch_bounds__(256, per_cu(TV)) logits_general_kernel(GeneralArgs g) {
   constexpr int A_BYTES = weight_bytes(TV), NI = blocks_v(TV), NA = stage_rows(TV);
   __shared__ __align__(16) unsigned char lds[2 * (A_BYTES + B_BYTES)];   // [buf][A|B]
   const int tid = threadIdx.x;
+  // (the arguments' fields are the same in both parts)
+  const float inv_t = TEMP ? g.base.inv_t : 1.f;
   const int lane = tid & 63;
   const int wave = tid >> 6;
   const int wv = wave & 1;    // which half of the tile's vocabulary rows
@@ -258,9 +261,9 @@ __global__ void __launch_bounds__(256, per_cu(TV)) logits_general_kernel(General
     const int col_base = v0 + wv * (TV / 2) + (lane >> 5) * 4;
     const int row0 = r0 + wr * 64 + (lane & 31);
     if (v0 + TV <= n_valid)
-      fold_general<STORE, false>(acc, run, a, row0, r_end, col_base, n_valid);
+      fold_general<STORE, false>(acc, run, a, row0, r_end, col_base, n_valid, inv_t);
     else
-      fold_general<STORE, true>(acc, run, a, row0, r_end, col_base, n_valid);
+      fold_general<STORE, true>(acc, run, a, row0, r_end, col_base, n_valid, inv_t);
   }
 
   // ---- end of strip: lanes l and l+32 hold the same hidden row; then the two vocabulary halves ---
@@ -270,7 +273,7 @@ __global__ void __launch_bounds__(256, per_cu(TV)) logits_general_kernel(General
     o.m = __shfl_xor(run[j].m, 32);
     o.s = __shfl_xor(run[j].s, 32);
     o.i = __shfl_xor(run[j].i, 32);
-    merge_triple(run[j], o, a.inv_t);
+    merge_triple(run[j], o, inv_t);
   }
   __syncthreads();            // all waves are done reading the operand tiles
   Triple* xch = reinterpret_cast<Triple*>(lds);   // [2 row halves][64 rows]
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(256, per_cu(TV)) logits_general_kernel(General
   if (wv == 0 && lane < 32) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      merge_triple(run[j], xch[wr * 64 + j * 32 + lane], a.inv_t);
+      merge_triple(run[j], xch[wr * 64 + j * 32 + lane], inv_t);
       const int hrow = r0 + wr * 64 + j * 32 + lane;
       if (hrow < r_end) {
         const size_t p = (size_t)hrow * a.n_parts + a.part0 + st;
@@ -311,7 +314,15 @@ int z2z_launch_logits_general(bool bf16, int columns, const LogitsArgs& base, co
   g.hyper_grid = hyper ? (hyper->n_work + 7) / 8 * 8 : 0;
   const dim3 grid((unsigned)g.hyper_grid + (unsigned)((base.n_work + 7) / 8 * 8)), block(256);
   const bool store = base.logits != nullptr;
-  if (bf16 && columns == 128 && store)
+  if (base.inv_t != 1.f) {                           // (the logits themselves are stored at T = 1 alone)
+    if (store) return Z2Z_EUNSUPPORTED;
+    if (bf16 && columns == 128)
+      hipLaunchKernelGGL((logits_general_kernel<uint16_t, 128, false, true>), grid, block, 0, s, g);
+    else if (bf16)
+      hipLaunchKernelGGL((logits_general_kernel<uint16_t, 64, false, true>), grid, block, 0, s, g);
+    else
+      hipLaunchKernelGGL((logits_general_kernel<float, 64, false, true>), grid, block, 0, s, g);
+  } else if (bf16 && columns == 128 && store)
     hipLaunchKernelGGL((logits_general_kernel<uint16_t, 128, true>), grid, block, 0, s, g);
   else if (bf16 && columns == 128)
     hipLaunchKernelGGL((logits_general_kernel<uint16_t, 128, false>), grid, block, 0, s, g);
