@@ -218,61 +218,6 @@ __global__ void __launch_bounds__(256) teacher_dz_kernel(TeacherArgs a, const fl
   }
 }
 
-// dH[r] += sum_k weight[r, k] W[ids[r, k]]: a wave per row and 64 times 16 bytes of it, eight rows of W requested at a time; fp32, one rounding.
-__global__ void __launch_bounds__(256) teacher_dh_kernel(TeacherArgs a, const float* weight, const uint4* W_base, const uint4* W_hyper, uint4* dH,
-                                                         int n_chunks, int slices) {
-  const int lane = threadIdx.x & 63;
-  const long long wid = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = (int)(wid / slices);
-  if (r >= a.rows) return;
-  const int chunk = (int)(wid % slices) * 64 + lane;
-  const int b = r / a.rows_per_seq;
-  const int columns = a.V + min(max(a.size[b], 0), a.cap);
-  float acc[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  bool any = false;
-  for (int k0 = 0; k0 < a.K; k0 += 64) {
-    const int k = k0 + lane;
-    const int my_id = k < a.K ? a.ids[(size_t)r * a.K + k] : -1;
-    const float my_w = k < a.K && my_id >= 0 && my_id < columns ? weight[(size_t)r * a.K + k] : 0.f;
-    uint64_t left = __ballot(my_w != 0.f);
-    any |= left != 0ull;
-    while (left != 0ull) {
-      uint4 x[8];
-      float w[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int l = left != 0ull ? __ffsll((long long)left) - 1 : 0;
-        const int id = __builtin_amdgcn_readlane(my_id, l);
-        w[u] = left != 0ull ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(my_w), l)) : 0.f;
-        const bool there = left != 0ull;
-        const uint4* row = !there ? W_base : (id < a.V ? W_base + (size_t)id * n_chunks : W_hyper + ((size_t)b * a.cap + (id - a.V)) * n_chunks);
-        x[u] = there ? row[min(chunk, n_chunks - 1)] : uint4{0u, 0u, 0u, 0u};
-        left &= left - 1ull;
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          acc[2 * e] = fmaf(w[u], __uint_as_float(xs[e] << 16), acc[2 * e]);
-          acc[2 * e + 1] = fmaf(w[u], __uint_as_float(xs[e] & 0xFFFF0000u), acc[2 * e + 1]);
-        }
-      }
-    }
-  }
-  if (!any || chunk >= n_chunks) return;
-  uint4* to = dH + (size_t)r * n_chunks + chunk;
-  const uint4 was = *to;
-  const uint32_t ws[4] = {was.x, was.y, was.z, was.w};
-  uint32_t out[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    out[e] = pack_bf16(__uint_as_float(ws[e] << 16) + acc[2 * e], __uint_as_float(ws[e] & 0xFFFF0000u) + acc[2 * e + 1]);
-  *to = uint4{out[0], out[1], out[2], out[3]};
-}
-
 TeacherArgs teacher_args(const z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq) {
   TeacherArgs a;
   a.ids = t.ids + (size_t)r0 * t.K;
@@ -329,17 +274,6 @@ int z2z_launch_teacher_dz(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, in
   else
     hipLaunchKernelGGL(teacher_dz_kernel<4>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, lse + r0, t.student + at, g, weight + at,
                        reinterpret_cast<uint16_t*>(base), ld_base, reinterpret_cast<uint16_t*>(hyper), ld_hyper);
-  Z2Z_HIP_TRY(hipGetLastError());
-  return Z2Z_OK;
-}
-
-int z2z_launch_teacher_dh(z2z_ctx* c, const z2z_teacher& t, int rows, int rows_per_seq, const float* weight, const void* W_base,
-                          const void* W_hyper, void* dH, hipStream_t s) {
-  const TeacherArgs a = teacher_args(c, t, 0, rows, rows_per_seq);
-  const int n_chunks = c->cfg.d / 8, slices = (n_chunks + 63) / 64;
-  const long long blocks = ((long long)rows * slices + 3) / 4;
-  hipLaunchKernelGGL(teacher_dh_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a, weight, reinterpret_cast<const uint4*>(W_base),
-                     reinterpret_cast<const uint4*>(W_hyper), reinterpret_cast<uint4*>(dH), n_chunks, slices);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }

@@ -209,10 +209,6 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
       if (rc != Z2Z_OK) return rc;
     }
   }
-  if (teacher) {
-    rc = z2z_launch_teacher_dh(c, *teacher, rows, rows_per_seq, weight, W_base, W_hyper, dH, s);
-    if (rc != Z2Z_OK) return rc;
-    return z2z_launch_weighted_rows(c, teacher->ids, rows, teacher->K, weight, H, dW_base, dW_hyper, s);
-  }
+  if (teacher) return z2z_launch_weighted_rows(c, teacher->ids, rows, teacher->K, weight, H, W_base, W_hyper, dH, dW_base, dW_hyper, s);
   return Z2Z_OK;
 }
