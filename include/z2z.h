@@ -10,6 +10,9 @@
  *   extended_logits  section 2.3 steps 7-9 (hyper rows appended to the LM head, joint softmax, pick)
  *   extended_sample  the same with the pick drawn from the softmax at a temperature (step 9)
  *   extended_nll     section 2.4 (next-token objective over compressed sequences): -log p(target) per row
+ *   extended_distill the same against a teacher's top logits
+ *   extended_beam    section 2.3 step 9 as a beam search's pick; codebook_reorder moves the beams' states after it
+ *   embed_codes      section 2.2 (the input rows of a compressed sequence) and its gradient
  *
  * Conventions
  *   - Every pointer named d_* is DEVICE memory owned by the caller; it must stay valid until the
@@ -35,9 +38,9 @@
  *     Once a call of z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward or z2z_extended_beam has been
  *     captured, no work buffer of the context is freed before z2z_destroy: one that grows leaves the old one to the graph.
  *   - Calls on one context must be issued from one host thread at a time, and work of one context
- *     must be ordered (same stream, or synchronised by the caller).  z2z_embed_codes and what follows it in this list below
- *     (embed_codes_backward, extended_distill and its backward pass, extended_beam, codebook_reorder) return Z2Z_EINVAL where
- *     the current device is not the one that the context was created on.
+ *     must be ordered (same stream, or synchronised by the caller).
+ *   - z2z_embed_codes, z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward, z2z_extended_beam and
+ *     z2z_codebook_reorder return Z2Z_EINVAL where the current device is not the one that the context was created on.
  */
 #ifndef Z2Z_H
 #define Z2Z_H
