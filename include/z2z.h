@@ -35,8 +35,8 @@
  *     `stream` is being captured into a graph a buffer cannot grow: the call returns Z2Z_ECAPTURE and
  *     enqueues nothing -- make one eager call at the same shape before capturing, or use
  *     z2z_extended_logits_static, which never allocates.
- *     Once a call of z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward or z2z_extended_beam has been
- *     captured, no work buffer of the context is freed before z2z_destroy: one that grows leaves the old one to the graph.
+ *     Once a call that uses work space has been captured, no work buffer of the context is freed before z2z_destroy: one that
+ *     grows leaves the old one to the graph.
  *   - Calls on one context must be issued from one host thread at a time, and work of one context
  *     must be ordered (same stream, or synchronised by the caller).
  *   - z2z_embed_codes, z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward, z2z_extended_beam and
@@ -375,6 +375,7 @@ int z2z_extended_sample(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t row
  *   d_code   [B / beams, n_pick] int32 out: by this base token or hypertoken (of the parent's codebook)
  *   d_picked [B / beams, n_pick] float out: the value above, the new beam's score
  *            (-1, -1 and -inf where fewer continuations are there); with n_pick = beams it may be the buffer of d_score
+ *            (else Z2Z_EINVAL)
  * n_pick may be larger than beams: the caller takes out finished sequences first.  A step goes on with z2z_codebook_reorder,
  * then z2z_step_update with the picked codes.
  * beams <= Z2Z_MAX_BEAMS and n_pick <= Z2Z_MAX_PICK, else Z2Z_EUNSUPPORTED; any storage type and width.  The logits go
@@ -438,7 +439,8 @@ int z2z_extended_nll_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32
  * d_kl = 0; one that lists a column that does not exist has +inf; a teacher logit of NaN or +inf makes the row NaN.  K = 1 at
  * T = 1 is z2z_extended_nll.
  *   d_ids [rows, K] int32; d_teacher [rows, K] float
- *   d_kl, d_lse [rows] float out; d_student [rows, K] float out: logit[r, ids_k] (not divided by T; 0 where no existing column is listed)
+ *   d_kl, d_lse [rows] float out; d_student [rows, K] float out: logit[r, ids_k] (not divided by T; 0 where no existing column is listed);
+ *            not the teacher's buffer (Z2Z_EINVAL)
  *   temperature between 1/16 and 1024 (else Z2Z_EINVAL); K <= Z2Z_MAX_TEACHER, else Z2Z_EUNSUPPORTED
  * Any shape and storage type z2z_extended_logits takes, and its work buffers. */
 #define Z2Z_MAX_TEACHER 256

@@ -892,7 +892,7 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
   auto room = [&](size_t need) -> int {
     if (need <= c->enc_ws_bytes) return Z2Z_OK;
     Z2Z_TRY_GROW(s);
-    if (c->enc_ws) (void)hipFree(c->enc_ws);
+    z2z_release(c, c->enc_ws);
     c->enc_ws = nullptr;
     c->enc_ws_bytes = 0;
     if (!z2z_device_malloc(&c->enc_ws, need)) return Z2Z_ENOMEM;
@@ -1081,7 +1081,7 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
   c->enc_kept = false;
   if (need > c->enc_bwd_ws_bytes) {
     Z2Z_TRY_GROW(s);
-    if (c->enc_bwd_ws) (void)hipFree(c->enc_bwd_ws);
+    z2z_release(c, c->enc_bwd_ws);
     c->enc_bwd_ws = nullptr;
     c->enc_bwd_ws_bytes = 0;
     if (!z2z_device_malloc(&c->enc_bwd_ws, need)) return Z2Z_ENOMEM;

@@ -55,14 +55,24 @@ void free_ctx(z2z_ctx* c) {
 // (beyond this range the fp32 exponents of the softmax lose what they are to tell apart)
 bool temperature_ok(float t) { return t >= 0.0625f && t <= 1024.0f; }
 
-// A call that uses work buffers: on the context's device, and noted where it is captured into a graph.
+// A call that uses work buffers is noted where it is captured into a graph (or may be: the runtime does not say).
+void note_capture(z2z_ctx* c, hipStream_t s) {
+  if (c->captured) return;
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) == hipSuccess) {
+    c->captured = st != hipStreamCaptureStatusNone;
+  } else {
+    (void)hipGetLastError();
+    c->captured = true;
+  }
+}
+
+// The same, on the context's device alone.
 int enter(z2z_ctx* c, hipStream_t s) {
   int device = -1;
   if (hipGetDevice(&device) != hipSuccess) return Z2Z_EHIP;
   if (device != c->device) return Z2Z_EINVAL;
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s, &st) != hipSuccess) return Z2Z_EHIP;
-  if (st != hipStreamCaptureStatusNone) c->captured = true;
+  note_capture(c, s);
   return Z2Z_OK;
 }
 
@@ -299,6 +309,7 @@ Z2Z_API int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* e
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
+  note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_hyper_encode(ctx, d_E, enc, d_W_hyper, d_first, max_new, static_cast<hipStream_t>(stream));
 }
 
@@ -307,6 +318,7 @@ Z2Z_API int z2z_hyper_encode_keep(z2z_ctx* ctx, const void* d_E, const z2z_encod
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
+  note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_hyper_encode_train(ctx, 1, d_E, enc, d_W_hyper, nullptr, nullptr, nullptr,
                                        static_cast<hipStream_t>(stream));
 }
@@ -319,6 +331,7 @@ Z2Z_API int z2z_hyper_encode_backward(z2z_ctx* ctx, const void* d_E, const z2z_e
   if (flags & ~Z2Z_ENC_KEPT) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_dW_hyper) || !aligned16(d_dE)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
+  note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_hyper_encode_train(ctx, (flags & Z2Z_ENC_KEPT) ? 2 : 0, d_E, enc, nullptr, d_dW_hyper, grad, d_dE,
                                        static_cast<hipStream_t>(stream));
 }
@@ -331,6 +344,7 @@ Z2Z_API int z2z_extended_logits(z2z_ctx* ctx, const void* d_H, int32_t rows, int
   if (rows_per_seq < 1 || rows < 1) return Z2Z_EINVAL;
   if ((long long)rows_per_seq * ctx->cfg.B != (long long)rows) return Z2Z_EINVAL;
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
+  note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_extended_logits(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, d_argmax, d_max, d_lse,
                                     d_logits, static_cast<hipStream_t>(stream));
 }
@@ -358,6 +372,7 @@ Z2Z_API int z2z_extended_sample(z2z_ctx* ctx, const void* d_H, int32_t rows, int
   if (!(temperature > 0.f) || !(temperature < 3.0e38f)) return Z2Z_EINVAL;
   if (!(top_p > 0.f)) return Z2Z_EINVAL;          // also rejects NaN; >= 1 switches the filter off
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
+  note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_extended_sample(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, temperature, top_k, top_p,
                                     seed, step, d_token, d_logprob, static_cast<hipStream_t>(stream));
 }
@@ -395,6 +410,7 @@ Z2Z_API int z2z_extended_beam(z2z_ctx* ctx, const void* d_H, int32_t rows, int32
   if (!ctx || !d_H || !d_W_base || !d_score || !d_parent || !d_code || !d_picked) return Z2Z_EINVAL;
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (rows != ctx->cfg.B || beams < 1 || rows % beams != 0 || n_pick < 1) return Z2Z_EINVAL;
+  if (d_picked == d_score && n_pick != beams) return Z2Z_EINVAL;     // (other prompts' scores would be written over)
   if (beams > Z2Z_MAX_BEAMS || n_pick > Z2Z_MAX_PICK) return Z2Z_EUNSUPPORTED;
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   const int rc = enter(ctx, static_cast<hipStream_t>(stream));
@@ -420,6 +436,7 @@ Z2Z_API int z2z_extended_nll(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_
   if (rows_per_seq < 1 || rows < 1) return Z2Z_EINVAL;
   if ((long long)rows_per_seq * ctx->cfg.B != (long long)rows) return Z2Z_EINVAL;
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
+  note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_extended_nll(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, d_targets, d_nll, d_lse,
                                  static_cast<hipStream_t>(stream));
 }
@@ -435,6 +452,7 @@ Z2Z_API int z2z_extended_nll_backward(z2z_ctx* ctx, const void* d_H, int32_t row
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper) || !aligned16(d_dH) || !aligned16(d_dW_base) ||
       !aligned16(d_dW_hyper))
     return Z2Z_EINVAL;
+  note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_extended_nll_backward(ctx, d_H, rows, rows_per_seq, d_W_base, d_W_hyper, d_targets, d_lse,
                                           d_grad_nll, d_dH, d_dW_base, d_dW_hyper, static_cast<hipStream_t>(stream));
 }
@@ -446,6 +464,7 @@ Z2Z_API int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, in
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (rows_per_seq < 1 || rows < 1 || n_teacher < 1) return Z2Z_EINVAL;
   if ((long long)rows_per_seq * ctx->cfg.B != (long long)rows) return Z2Z_EINVAL;
+  if (d_student == d_teacher) return Z2Z_EINVAL;     // (written before the teacher is read)
   if (!temperature_ok(temperature)) return Z2Z_EINVAL;
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (n_teacher > Z2Z_MAX_TEACHER) return Z2Z_EUNSUPPORTED;

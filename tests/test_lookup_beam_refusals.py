@@ -71,16 +71,17 @@ def test_beam_refusals(without_a_device):
     without_a_device("""
 h = context(B=12, V=1000, M=3, cap=100, d=128)
 Q = P + 8
-pick = lambda c=h, H=P, rows=12, beams=4, Wb=P, Wh=P, score=P, n=8, parent=P, code=P, picked=P: lib.z2z_extended_beam(c, H, rows, beams, Wb, Wh, score, n, parent, code, picked, None)
+pick = lambda c=h, H=P, rows=12, beams=4, Wb=P, Wh=P, score=P, n=8, parent=P, code=P, picked=P + 64: lib.z2z_extended_beam(c, H, rows, beams, Wb, Wh, score, n, parent, code, picked, None)
 for bad in (dict(c=None), dict(H=None), dict(Wb=None), dict(Wh=None), dict(score=None), dict(parent=None), dict(code=None), dict(picked=None),
-            dict(rows=11), dict(rows=24), dict(beams=0), dict(beams=-4), dict(beams=5), dict(n=0), dict(n=-1), dict(H=Q), dict(Wb=Q), dict(Wh=Q)):
+            dict(rows=11), dict(rows=24), dict(beams=0), dict(beams=-4), dict(beams=5), dict(n=0), dict(n=-1), dict(H=Q), dict(Wb=Q), dict(Wh=Q),
+            dict(picked=P), dict(picked=P, n=3)):                         # (in place of the scores, but of another length)
     assert pick(**bad) == api.E_INVAL, bad
 assert pick(n=65) == api.E_UNSUPPORTED
 wide = context(B=66, V=1000, M=3, cap=100, d=128)
 assert pick(c=wide, rows=66, beams=33) == api.E_UNSUPPORTED
 assert launches() == []
-assert pick() == 0 and pick(beams=12, n=64) == 0 and pick(beams=1, n=1) == 0
-assert named(launches(), "beam_pick") == [3, 1, 12]
+assert pick() == 0 and pick(beams=12, n=64) == 0 and pick(beams=1, n=1) == 0 and pick(picked=P, n=4) == 0
+assert named(launches(), "beam_pick") == [3, 1, 12, 3]
 move = lambda c=h, beams=4, source=P, W=P: lib.z2z_codebook_reorder(c, beams, source, W, None)
 for bad in (dict(c=None), dict(source=None), dict(beams=0), dict(beams=7), dict(W=Q)):
     assert move(**bad) == api.E_INVAL, bad
@@ -102,12 +103,12 @@ def test_distill_refusals(without_a_device):
     without_a_device("""
 h = context(B=4, V=1000, M=3, cap=100, d=128)
 Q = P + 8
-fwd = lambda c=h, H=P, rows=40, rps=10, Wb=P, Wh=P, K=8, ids=P, t=P, T=2.0, kl=P, lse=P, st=P: lib.z2z_extended_distill(c, H, rows, rps, Wb, Wh, K, ids, t, T, kl, lse, st, None)
+fwd = lambda c=h, H=P, rows=40, rps=10, Wb=P, Wh=P, K=8, ids=P, t=P, T=2.0, kl=P, lse=P, st=P + 64: lib.z2z_extended_distill(c, H, rows, rps, Wb, Wh, K, ids, t, T, kl, lse, st, None)
 bwd = lambda c=h, H=P, rows=40, rps=10, Wb=P, Wh=P, K=8, ids=P, t=P, T=2.0, lse=P, st=P, g=P, dH=P, dWb=P, dWh=P: lib.z2z_extended_distill_backward(c, H, rows, rps, Wb, Wh, K, ids, t, T, lse, st, g, dH, dWb, dWh, None)
 common = [dict(c=None), dict(H=None), dict(Wb=None), dict(Wh=None), dict(ids=None), dict(t=None), dict(lse=None), dict(st=None), dict(rows=0), dict(rows=41),
           dict(rps=0), dict(K=0), dict(K=-3), dict(T=0.0), dict(T=-1.0), dict(T=0.06), dict(T=1025.0), dict(T=float("nan")), dict(T=float("inf")),
           dict(H=Q), dict(Wb=Q), dict(Wh=Q)]
-for bad in common + [dict(kl=None)]:
+for bad in common + [dict(kl=None), dict(st=P)]:          # (the last: the teacher's buffer)
     assert fwd(**bad) == api.E_INVAL, bad
 for bad in common + [dict(dH=None), dict(dWb=None), dict(dWh=None), dict(dH=Q), dict(dWb=Q), dict(dWh=Q)]:
     assert bwd(**bad) == api.E_INVAL, bad
@@ -134,11 +135,50 @@ def test_a_temperature_leaves_the_decode_kernels(without_a_device):
     without_a_device("""
 for rps in (1, 5, 100):
     h = context(B=8, V=40000, M=3, cap=1024, d=256)
-    fwd = lambda T: lib.z2z_extended_distill(h, P, 8 * rps, rps, P, P, 4, P, P, T, P, P, P, None)
+    fwd = lambda T: lib.z2z_extended_distill(h, P, 8 * rps, rps, P, P, 4, P, P, T, P, P, P + 64, None)
     assert lib.z2z_extended_nll(h, P, 8 * rps, rps, P, P, P, P, P, None) == 0
     nll = [n for n, _ in launches() if "logits_" in n]
     assert fwd(1.0) == 0
     assert [n for n, _ in launches() if "logits_" in n] == nll
     assert fwd(2.0) == 0
     assert not named(launches(), "logits_decode")
+""")
+
+
+def test_buffers_of_captured_calls_stay(without_a_device):
+    """Calls that were captured into a graph, each with the buffers that it names, and larger calls of others behind it: nothing is given back
+    before the context goes."""
+    without_a_device("""
+V, cap, d = 4096, 100, 128
+enc = encoder(d)
+calls = dict(
+    logits=lambda h, n: lib.z2z_extended_logits(h, P, 4 * n, n, P, P, P, P, P, None, None),
+    sample=lambda h, n: lib.z2z_extended_sample(h, P, 4, 1, P, P, 1.0, 50, 0.9, 1, 2, P, P, None),
+    nll=lambda h, n: lib.z2z_extended_nll(h, P, 4 * n, n, P, P, P, P, P, None),
+    nll_backward=lambda h, n: nll_backward(h, 4, n),
+    encode=lambda h, n: lib.z2z_hyper_encode(h, P, ctypes.byref(enc), P, None, n, None),
+    distill=lambda h, n: lib.z2z_extended_distill(h, P, 4 * n, n, P, P, 8, P, P, 2.0, P, P, P + 64, None),
+    distill_backward=lambda h, n: lib.z2z_extended_distill_backward(h, P, 4 * n, n, P, P, 8, P, P, 2.0, P, P, P, P, P, P, None),
+    lookup_backward=lambda h, n: lib.z2z_embed_codes_backward(h, P, P, n, 1.0, P, 0, P, P, None),
+    beam=lambda h, n: lib.z2z_extended_beam(h, P, 4, 2, P, P, P, 3, P, P, P + 64, None))
+none = stub.stub_used()
+for name, call in calls.items():
+    h = context(B=4, V=V, M=3, cap=cap, d=d)
+    fixed = stub.stub_used()
+    assert call(h, 50) == 0, name
+    held = stub.stub_used()
+    assert held > fixed, name
+    stub.stub_capturing(1)
+    assert call(h, 50) == 0, name
+    stub.stub_capturing(0)
+    launches()
+    for other, larger in calls.items():
+        before = stub.stub_used()
+        stub.stub_capacity(before)                        # (no room: what the call gives back first is gone)
+        larger(h, 90)
+        assert stub.stub_used() == before, (name, other)
+        stub.stub_capacity(1 << 40)
+        assert larger(h, 90) == 0, (name, other)
+    assert lib.z2z_destroy(h) == 0 and stub.stub_used() == none
+clean()
 """)
