@@ -8,7 +8,7 @@
 // both operands between its waves, which meet at every slab (3.4-3.5 TB/s of weights at these row counts).  Here:
 //
 //   workgroup = 8 waves = one tile of 256 weight rows x all hidden rows; wave w owns weight rows 32 w .. 32 w + 31:
-//   2, 4 or 6 blocks of v_mfma_f32_32x32x16_bf16 (the kernel is built for up to 64, 128 and 192 rows).
+//   2 to 6 blocks of v_mfma_f32_32x32x16_bf16 (the kernel is built for up to 64, 96, 128, 160 and 192 rows).
 //   K advances in slabs of 64.  A wave moves its own weights straight from global memory into a ring of its
 //   own in LDS, four requests of 8 whole lines per slab, two or three slabs ahead, and reads its operands from there; nobody else
 //   touches the ring, so it needs no barrier.  (Loaded in operand layout, 32 rows and half a line each way, a
@@ -37,21 +37,24 @@ using namespace z2z_logits;
 
 constexpr int M_WAVES = 8;                // of a workgroup; four where tiles of 256 weight rows are too few for the CUs
 constexpr int M_WT = 32 * M_WAVES;        // weight rows of a workgroup's tile
-constexpr int M_HT = 192;                 // hidden rows of a call at most (the builds below: 2, 4 or 6 blocks of 32)
+constexpr int M_HT = 192;                 // hidden rows of a call at most (the builds below: 2 to 6 blocks of 32)
 constexpr int M_MAX_ROWS = M_HT;
 static_assert(M_HT <= 64 * M_WAVES / 2, "a thread per row");
 constexpr int M_SLAB = 128;               // bytes per row per K slab (64 bf16)
 // LDS per build (blocks of 32 hidden rows, waves): stages of a slab's hidden rows, and slots of the waves' rings.  Four waves
 // have the CU to themselves and ask for both up to five slabs ahead.
-constexpr int mid_stages(int njv, int waves) { return waves == 4 ? (njv == 2 ? 6 : njv == 4 ? 5 : 4) : njv == 6 ? 2 : 3; }
+constexpr int mid_stages(int njv, int waves) { return waves == 4 ? (njv == 2 ? 6 : njv <= 4 ? 5 : 4) : njv == 6 ? 2 : 3; }
 constexpr int mid_ring(int njv, int waves) { return waves == 4 ? mid_stages(njv, 4) : njv == 2 ? 4 : 3; }
 constexpr int mid_lds(int njv, int waves) {
   return mid_stages(njv, waves) * 32 * njv * M_SLAB + waves * 32 * M_SLAB * mid_ring(njv, waves);
 }
 constexpr int M_LDS_MAX = 160 * 1024;
-static_assert(mid_lds(2, 8) <= M_LDS_MAX && mid_lds(4, 8) <= M_LDS_MAX && mid_lds(6, 8) <= M_LDS_MAX, "");
-static_assert(mid_lds(2, 4) <= M_LDS_MAX && mid_lds(4, 4) <= M_LDS_MAX && mid_lds(6, 4) <= M_LDS_MAX, "");
-static_assert(M_WAVES * M_HT * (int)(sizeof(Triple) + sizeof(Draw)) <= mid_lds(6, 8), "the waves' triples are merged in the idle stages and rings");
+constexpr bool mid_fits(int waves) {
+  for (int njv = 2; njv <= 6; ++njv)        // (the waves' triples are merged in the idle stages and rings)
+    if (mid_lds(njv, waves) > M_LDS_MAX || mid_lds(njv, waves) < waves * M_HT * (int)(sizeof(Triple) + sizeof(Draw))) return false;
+  return true;
+}
+static_assert(mid_fits(8) && mid_fits(4), "");
 
 // 16 bytes per lane, global -> LDS without passing through registers (as in the tile kernel): address = 64-bit
 // scalar base + 32-bit per-lane offset; the LDS address is the wave-uniform byte offset in M0 plus 16 * lane.
@@ -177,21 +180,22 @@ __device__ __forceinline__ void mid_tile(const LogitsArgs& a, const MidTile& t, 
   // hidden rows: the 4 NJV groups of 8 rows of a slab are dealt to the waves, group g = i * WAVES + wave for the
   // wave's i-th request; lane l moves, for row g * 8 + (l >> 3), the chunk that lands at position l & 7 of the row's
   // 128 LDS bytes: chunk (l & 7) ^ ((row >> 1) & 7).  Rows past the last valid one read the last valid one.
-  constexpr int HL = (4 * NJV) / WAVES;                    // requests per wave and slab
-  static_assert(HL * WAVES == 4 * NJV, "whole groups per wave");
+  // (with an odd number of blocks half of eight waves ask for their last group twice: every wave has as many requests to wait for)
+  constexpr int HL = (4 * NJV + WAVES - 1) / WAVES;        // requests per wave and slab
+  auto group_of = [&](int i) { return i * WAVES + wave < 4 * NJV ? i * WAVES + wave : (i - 1) * WAVES + wave; };
   const unsigned char* Ht = reinterpret_cast<const unsigned char*>(t.H);
   const uint32_t lds_base = lds_offset_of(lds);
   uint32_t hsrc[HL];
 #pragma unroll
   for (int i = 0; i < HL; ++i) {
-    const int row = (i * WAVES + wave) * 8 + (lane >> 3);
+    const int row = group_of(i) * 8 + (lane >> 3);
     hsrc[i] = (uint32_t)(min(row, nr - 1) * (int)row_bytes + (((lane & 7) ^ ((row >> 1) & 7)) << 4));
   }
   auto issue_h = [&](int slab, int stage) {
     const unsigned char* p = Ht + (size_t)slab_at(slab) * M_SLAB;
 #pragma unroll
     for (int i = 0; i < HL; ++i)
-      load16_to_lds(p, hsrc[i], lds_base + (uint32_t)(stage * STAGE + (i * WAVES + wave) * 1024));
+      load16_to_lds(p, hsrc[i], lds_base + (uint32_t)(stage * STAGE + group_of(i) * 1024));
   };
   // operand reads: block j, row lane & 31, logical chunk 2 q + half
   const int sw = (lane >> 1) & 7;
@@ -434,12 +438,16 @@ int z2z_logits_mid_columns(const z2z_ctx* c, int w_rows) {
 template <int WAVES>
 static void launch_mid(const LogitsArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.n_vtiles + a.hyper.n_work)), block(64 * WAVES);
-  const int blocks = a.rows <= 64 ? 2 : (a.rows <= 128 ? 4 : 6);
+  const int blocks = a.rows <= 64 ? 2 : (a.rows + 31) / 32;
   if (a.row_grad) {
     if (blocks == 2)
       hipLaunchKernelGGL((logits_mid_kernel<2, 7, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
+    else if (blocks == 3)
+      hipLaunchKernelGGL((logits_mid_kernel<3, 7, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
     else if (blocks == 4)
       hipLaunchKernelGGL((logits_mid_kernel<4, 7, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
+    else if (blocks == 5)
+      hipLaunchKernelGGL((logits_mid_kernel<5, 7, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
     else
       hipLaunchKernelGGL((logits_mid_kernel<6, 7, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
     return;
@@ -447,15 +455,23 @@ static void launch_mid(const LogitsArgs& a, hipStream_t s) {
   if (a.sample == 1) {
     if (blocks == 2)
       hipLaunchKernelGGL((logits_mid_kernel<2, 5, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
+    else if (blocks == 3)
+      hipLaunchKernelGGL((logits_mid_kernel<3, 1, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
     else if (blocks == 4)
       hipLaunchKernelGGL((logits_mid_kernel<4, 1, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
+    else if (blocks == 5)
+      hipLaunchKernelGGL((logits_mid_kernel<5, 1, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
     else
       hipLaunchKernelGGL((logits_mid_kernel<6, 1, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
   } else if (a.sample == 2) {
     if (blocks == 2)
       hipLaunchKernelGGL((logits_mid_kernel<2, 6, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
+    else if (blocks == 3)
+      hipLaunchKernelGGL((logits_mid_kernel<3, 2, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
     else if (blocks == 4)
       hipLaunchKernelGGL((logits_mid_kernel<4, 2, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
+    else if (blocks == 5)
+      hipLaunchKernelGGL((logits_mid_kernel<5, 2, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
     else
       hipLaunchKernelGGL((logits_mid_kernel<6, 2, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
   } else {
@@ -463,8 +479,12 @@ static void launch_mid(const LogitsArgs& a, hipStream_t s) {
       hipLaunchKernelGGL((logits_mid_kernel<2, 4, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
     else if (blocks == 2)
       hipLaunchKernelGGL((logits_mid_kernel<2, 0, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
+    else if (blocks == 3)
+      hipLaunchKernelGGL((logits_mid_kernel<3, 0, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
     else if (blocks == 4)
       hipLaunchKernelGGL((logits_mid_kernel<4, 0, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
+    else if (blocks == 5)
+      hipLaunchKernelGGL((logits_mid_kernel<5, 0, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
     else
       hipLaunchKernelGGL((logits_mid_kernel<6, 0, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
   }
@@ -485,9 +505,12 @@ int z2z_launch_logits_mid(z2z_ctx* c, LogitsArgs a, const void* W, int w_rows, i
   if (a.hyper.n_work > 0 && (a.sample != 0 || (a.rows_per_seq <= 64 && !a.row_grad && a.inv_t == 1.f))) return Z2Z_EUNSUPPORTED;
   // (two workgroups of the 64-row build per weight tile for 65..128 rows, sharing the tile's weights through an
   // XCD's L2, measured slower than one of the 128-row build: 383 against 293 us at config 2's shape)
-  // builds: 2, 4 or 6 blocks of 32 hidden rows; the sampling calls come with one row per sequence.  (8 blocks, up to 256
-  // rows, measured level with the tile kernel when weights still went through registers: 650 against 645 us for a decode step of
-  // 256 sequences.)
+  // builds: 2 to 6 blocks of 32 hidden rows; the sampling calls come with one row per sequence.  (3 blocks for 65..96 rows and 5 for
+  // 129..160, the latter with three stages of hidden rows where 6 have room for two.  Whole calls, us, in the builds of 4 and 6 / 3 and 5, 80, 135 and
+  // 160 rows: greedy V = 128256, d = 4096 196 / 177, 213 / 202, 227 / 203; V = 32000 55 / 51, 70 / 63, 71 / 63; V = 50257, d = 1024 30.6 /
+  // 29.9, 36.8 / 33.8, 36.6 / 33.9; beams V = 80000, d = 4096 167 / 158, 203 / 192, 207 / 198; draws 183 / 173, 228 / 218, 231 / 219.
+  // 8 blocks, up to 256 rows, measured level with the tile kernel when weights still went through registers: 650 against 645 us for a decode
+  // step of 256 sequences.)
   if (columns == M_WT)
     launch_mid<M_WAVES>(a, s);
   else
@@ -557,18 +580,28 @@ int z2z_logits_mid_prepare(z2z_ctx* c) {
   const void* kernels[] = {reinterpret_cast<const void*>(logits_mid_kernel<2, 3>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 3>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 7, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 7, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 7, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 7, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 7, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 7, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 7, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 7, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 7, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 7, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 0, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 4, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 5, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 6, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 0, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 0, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 0, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 1, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 1, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 1, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 2, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 2, M_WAVES>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 2, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 0, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 1, M_WAVES>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 2, M_WAVES>),
@@ -576,9 +609,15 @@ int z2z_logits_mid_prepare(z2z_ctx* c) {
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 4, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 5, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<2, 6, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 0, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 0, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 0, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 1, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 1, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 1, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<3, 2, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<4, 2, M_WAVES / 2>),
+                           reinterpret_cast<const void*>(logits_mid_kernel<5, 2, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 0, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 1, M_WAVES / 2>),
                            reinterpret_cast<const void*>(logits_mid_kernel<6, 2, M_WAVES / 2>)};

@@ -62,6 +62,10 @@ def _setup(dtype, B, V, d, M, cap, N, seed):
     ("bf16", 66, 6, 3001, 256, 3, 64, 150, 12),            # more rows than the decode kernel takes in a pass
     ("bf16", 200, 4, 1500, 128, 3, 40, 100, 5),            # more than the streaming kernel takes
     ("bf16", 12, 4, 30000, 512, 3, 700, 1000, 8),          # base vocabulary on the streaming kernel
+    ("bf16", 80, 5, 33000, 128, 3, 40, 60, 9),             # 80 and 150 rows of it, tiles of 256 and of 128 columns
+    ("bf16", 150, 5, 33000, 128, 3, 40, 60, 6),
+    ("bf16", 90, 3, 2500, 192, 3, 40, 60, 5),
+    ("bf16", 135, 5, 1300, 256, 3, 40, 60, 7),
     ("bf16", 8, 4, 5, 128, 3, 20, 30, 12),                 # a vocabulary of five
     ("bf16", 8, 4, 1, 128, 3, 20, 30, 64),                 # and of one: fewer continuations than picks
     ("bf16", 6, 2, 900, 72, 3, 50, 100, 4),                # a width of the general kernel

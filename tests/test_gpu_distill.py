@@ -82,6 +82,8 @@ SHAPES = [
     ("bf16", 4, 5, 2000, 256, 4, 300, 33, 1.0),       # a few rows
     ("bf16", 4, 5, 2000, 256, 4, 300, 33, 0.0625),
     ("bf16", 2, 61, 5003, 192, 3, 200, 64, 2.0),      # the streaming kernel
+    ("bf16", 2, 45, 33000, 64, 3, 60, 9, 2.0),        # 90 and 140 rows of it, tiles of 256 and of 128 columns
+    ("bf16", 2, 70, 700, 128, 3, 300, 11, 2.0),
     ("bf16", 2, 150, 2100, 64, 3, 300, 65, 1.5),      # the tile kernel
     ("bf16", 3, 301, 700, 320, 3, 120, 256, 1024.0),
     ("bf16", 2, 40, 300, 64, 3, 0, 1, 1.0),           # no codebook, one column
