@@ -594,9 +594,10 @@ static int ensure_sample_logits(z2z_ctx* c, int32_t rows, hipStream_t s) {
 }
 
 // One hidden row per sequence, every logit / T stored in the context's sample_logits (rows x (V + cap) floats) and folded into parts of
-// *base_columns and *hyper_columns columns (0: the decode kernel's units).  mid_base: the base vocabulary goes to the weight-streaming kernel.
+// *base_columns and *hyper_columns columns (0: the decode kernel's units).  mid_base: the base vocabulary goes to the weight-streaming kernel;
+// along: and takes the hyper part's tiles with it.
 static int launch_stored_logits(z2z_ctx* c, const void* H, int32_t rows, const void* W_base, const void* W_hyper,
-                                const z2z_sample_params& sp, bool mid_base, int* parts_out, int* base_out, int* hyper_out,
+                                const z2z_sample_params& sp, bool mid_base, bool along, int* parts_out, int* base_out, int* hyper_out,
                                 hipStream_t s) {
   const bool timed = c->opt_timing && c->n_timed < Z2Z_MAX_TIMED && c->ev_created;
   const bool timed_pair = timed && mid_base && rows <= 64;       // a split step's two launches are timed together
@@ -623,6 +624,7 @@ static int launch_stored_logits(z2z_ctx* c, const void* H, int32_t rows, const v
     const long long wide = (long long)rows * ((c->cfg.cap + 511) / 512);
     hyper_columns = z2z_logits_decode_hyper_unit(c, wide < 200 && (c->cfg.cap > 2048 || wide > 128) ? 512 : 200);
     while (hyper_columns < 512 && base_strips + (c->cfg.cap + hyper_columns - 1) / hyper_columns > z2z_sample_list_parts()) hyper_columns *= 2;
+    if (along) hyper_columns = mid_columns;
     n_parts = base_strips + (c->cfg.cap + hyper_columns - 1) / hyper_columns;
     base_columns = mid_base ? mid_columns : strip_b * 256;
     LogitsArgs a;
@@ -642,12 +644,16 @@ static int launch_stored_logits(z2z_ctx* c, const void* H, int32_t rows, const v
     a.ld = c->cfg.V + c->cfg.cap;
     if (timed_pair) Z2Z_HIP_TRY(hipEventRecord(c->ev_start[c->n_timed], s));
     a.once = mid_base && split_few_once(c, rows);
+    if (along) {
+      z2z_add_hyper_part(c, a, W_hyper, base_strips, 1, 1, 0, c->cfg.B);
+      a.hyper.n_work = c->cfg.B * ((c->cfg.cap + mid_columns - 1) / mid_columns);
+    }
     if (mid_base)
       rc = z2z_launch_logits_mid(c, a, W_base, c->cfg.V, 0, s);
     else
       rc = z2z_launch_logits_part(c, false, a, W_base, c->cfg.V, 0, 0, strip_b, rows, 1, timed, s);
     if (rc != Z2Z_OK) return rc;
-    if (c->cfg.cap > 0) {
+    if (c->cfg.cap > 0 && !along) {
       int np = 0;
       rc = z2z_launch_logits_decode(c, H, W_base, W_hyper, &np, false, &sp, c->sample_logits, s, base_strips, nullptr, 1, hyper_columns);
       if (rc != Z2Z_OK) return rc;
@@ -748,7 +754,7 @@ int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t 
   // gives the row maxima and log-sum-exps, and one workgroup per row selects the kept prefix and draws
   if (!c->trunc_ready) return Z2Z_EUNSUPPORTED;
   int base_columns = 0, hyper_columns = 0;
-  rc = launch_stored_logits(c, H, rows, W_base, W_hyper, sp, mid_base, &n_parts, &base_columns, &hyper_columns, s);
+  rc = launch_stored_logits(c, H, rows, W_base, W_hyper, sp, mid_base, false, &n_parts, &base_columns, &hyper_columns, s);
   if (rc != Z2Z_OK) return rc;
   if (!z2z_sample_truncated_merges_parts(c, n_parts, top_k, base_columns, hyper_columns)) {
     rc = launch_combine(ctx_parts(c), n_parts, rows, nullptr, c->row_max, c->row_max + rows, s);
@@ -756,6 +762,21 @@ int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t 
   }
   return z2z_launch_sample_truncated(c, c->sample_logits, c->row_max, rows, n_parts, c->row_max + 2 * (size_t)rows, &sp,
                                      top_k, top_p, token, logprob, s, base_columns, hyper_columns);
+}
+
+// A beam step's hyper part in the streaming kernel's launch, tile by tile, instead of the decode kernel's units in one of their own: where all tiles
+// together take fewer rounds of a workgroup per CU than the parts apart, the hyper part at most five (more of them are the units', which
+// hold a sequence's one row in registers), and with up to 32 rows of up to 2 KB, whose workgroups are short and two to a CU.  Apart / together, us, whole calls,
+// codebooks full: 4 rows, V = 8000, d = 512, 512 entries (63 and 16 tiles) 26.6 / 20.5; 32000 x 1024 x 512 (250 and 16, two to a CU) 36.5 / 33.7; 50257 x
+// 768 x 512 (197 and 8) 39.6 / 31.9; 80000 x 2048 x 1024 (313 and 16) 91 / 81; 136 rows of the last (313 and 544) 239 / 198.  Where no round
+// is saved: 4 rows, 128256 x 4096 x 1024 (501 and 16) 190 / 213, 80 rows, 32000 x 1024 x 3000 (250 and 1920) 121 / 155.
+static bool hyper_along(const z2z_ctx* c, int rows) {
+  if (c->cfg.cap <= 0) return false;
+  const int columns = z2z_logits_mid_columns(c, c->cfg.V), cu = c->num_cu;
+  const long long base = (c->cfg.V + columns - 1) / columns, hyper = (long long)rows * ((c->cfg.cap + columns - 1) / columns);
+  auto rounds = [&](long long tiles) { return (tiles + cu - 1) / cu; };
+  if (columns < 256 && rows <= 32 && c->cfg.d <= 1024) return true;
+  return rounds(hyper) <= 5 && rounds(base + hyper + 8) < rounds(base) + rounds(hyper);      // (a round of less than 8 is hardly saved)
 }
 
 int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
@@ -772,16 +793,14 @@ int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const voi
     z2z_sample_params sp;
     sp.temperature = 1.0f;
     sp.seed = sp.step = 0;
-    // The base vocabulary on the weight-streaming kernel, the hyper units in a launch of their own, from 4 rows on, and from 2 on up to 256 tiles
-    // of it; else the decode kernel's units, both in one launch.  One launch / two, us, whole calls: 1 x 4 rows V = 8000, d = 512 48 / 26, 32000 x 1024
-    // 52 / 35, 32000 x 4096 88 / 73, 50257 x 768 54 / 35, 128256 x 2048 108 / 108, 128256 x 4096 196 / 188, 151936 x 3584 216 / 214; 2 rows 32 / 25, 37 / 35,
-    // 83 / 71, 43 / 35, 90 / 106, 184 / 185, 189 / 212; 1 row 24 / 26, 32 / 35, 60 / 72, 41 / 34, 90 / 108, 184 / 184, 187 / 212; 8 x 4 rows, entries up to
-    // 512 / 4096, V = 32000, d = 1024 45 / 38, 74 / 77, d = 4096 97 / 81, 182 / 188, V = 80000, d = 4096 218 / 167, 274 / 273; 16 x 4 rows 51 / 48, 101 / 106,
-    // 108 / 104, 320 / 316, 235 / 188, 402 / 404.
-    const bool mid_base = (rows >= 4 || (rows >= 2 && z2z_logits_mid_tiles(c->cfg.V) <= 256)) && c->opt_logits_kernel == 0 &&
-                          c->opt_decode_kernel == 0 && z2z_logits_mid_ok(c, rows);
+    // The base vocabulary on the weight-streaming kernel, the hyper part along or in a launch of its own, from 3 rows on, and from 1 on up to 512 tiles
+    // of it; else the decode kernel's units, both in one launch.  One launch of units / this, us, whole calls, 512 entries: 1 row V = 8000, d = 512 37 / 22,
+    // 32000 x 1024 45 / 29, 32000 x 4096 95 / 67, 80000 x 2048 88 / 81, 128256 x 1024 68 / 65, 128256 x 4096 190 / 172, 151936 x 1024 75 / 81, 151936 x
+    // 4096 210 / 218; 2 rows 80000 x 4096 134 / 139, 128256 x 2048 111 / 108, 151936 x 4096 211 / 220; 3 rows 144 / 138, 106 / 109, 222 / 220.
+    const bool mid_base = (rows >= 3 || z2z_logits_mid_tiles(c->cfg.V) <= 512) && c->opt_logits_kernel == 0 && c->opt_decode_kernel == 0 &&
+                          z2z_logits_mid_ok(c, rows);
     int base = 0, hyper = 0;
-    rc = launch_stored_logits(c, H, rows, W_base, W_hyper, sp, mid_base, &n_parts, &base, &hyper, s);
+    rc = launch_stored_logits(c, H, rows, W_base, W_hyper, sp, mid_base, mid_base && hyper_along(c, rows), &n_parts, &base, &hyper, s);
     if (rc != Z2Z_OK) return rc;
     z2z_logits_decode_units(&base_columns, &hyper_columns);
     if (base > 0) base_columns = base;

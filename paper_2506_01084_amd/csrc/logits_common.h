@@ -311,14 +311,14 @@ constexpr size_t kKeepBytes = (size_t)128 << 20;
 // fp32, at logits[row, col0 + column] (the selection kernels read the rows back); 16-byte stores where the four
 // columns of a group all exist.
 template <int NI, int NJ>
-__device__ __forceinline__ void fold_tile_store(const f32x16 (&acc)[NI][NJ], Triple (&run)[NJ], const LogitsArgs& a,
+__device__ __forceinline__ void fold_tile_store(const f32x16 (&acc)[NI][NJ], Triple (&run)[NJ], const LogitsArgs& a, int col0,
                                                 int row_base, int r_end, int col_base, int n_valid) {
   const int lane31 = threadIdx.x & 31;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     if (row_base + j * 32 >= r_end) break;           // (uniform)
     const int row = row_base + j * 32 + lane31;
-    float* out = a.logits + (size_t)min(row, r_end - 1) * a.ld + a.col0;
+    float* out = a.logits + (size_t)min(row, r_end - 1) * a.ld + col0;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       float x[16];
@@ -336,7 +336,7 @@ __device__ __forceinline__ void fold_tile_store(const f32x16 (&acc)[NI][NJ], Tri
         for (int v = 14; v >= 0; --v) targ = (x[v] == gmax) ? v : targ;
         run[j].s = (run[j].m == kNegInf) ? 0.f : run[j].s * __expf(run[j].m - gmax);
         run[j].m = gmax;
-        run[j].i = a.col0 + col_base + i * 32 + (targ >> 2) * 8 + (targ & 3);
+        run[j].i = col0 + col_base + i * 32 + (targ >> 2) * 8 + (targ & 3);
       }
       if (run[j].m != kNegInf) {
         const float m = run[j].m;
@@ -350,7 +350,7 @@ __device__ __forceinline__ void fold_tile_store(const f32x16 (&acc)[NI][NJ], Tri
         for (int q = 0; q < 4; ++q) {
           const int col = col_base + i * 32 + q * 8;
           // (a row of the logits starts 4-byte aligned only: ld = V + cap is any number)
-          if (col + 3 < n_valid && ((((size_t)row * a.ld + a.col0 + col) & 3) == 0)) {
+          if (col + 3 < n_valid && ((((size_t)row * a.ld + col0 + col) & 3) == 0)) {
             *reinterpret_cast<float4*>(out + col) = float4{x[q * 4], x[q * 4 + 1], x[q * 4 + 2], x[q * 4 + 3]};
           } else {
 #pragma unroll

@@ -8,7 +8,7 @@
 // both operands between its waves, which meet at every slab (3.4-3.5 TB/s of weights at these row counts).  Here:
 //
 //   workgroup = 8 waves = one tile of 256 weight rows x all hidden rows; wave w owns weight rows 32 w .. 32 w + 31:
-//   2 to 6 blocks of v_mfma_f32_32x32x16_bf16 (the kernel is built for up to 64, 96, 128, 160 and 192 rows).
+//   1 to 6 blocks of v_mfma_f32_32x32x16_bf16 (a build for every 32 rows).
 //   K advances in slabs of 64.  A wave moves its own weights straight from global memory into a ring of its
 //   own in LDS, four requests of 8 whole lines per slab, two or three slabs ahead, and reads its operands from there; nobody else
 //   touches the ring, so it needs no barrier.  (Loaded in operand layout, 32 rows and half a line each way, a
@@ -31,26 +31,28 @@
 
 #include <string.h>
 
+#include <algorithm>
+
 namespace {
 
 using namespace z2z_logits;
 
 constexpr int M_WAVES = 8;                // of a workgroup; four where tiles of 256 weight rows are too few for the CUs
 constexpr int M_WT = 32 * M_WAVES;        // weight rows of a workgroup's tile
-constexpr int M_HT = 192;                 // hidden rows of a call at most (the builds below: 2 to 6 blocks of 32)
+constexpr int M_HT = 192;                 // hidden rows of a call at most (the builds below: 1 to 6 blocks of 32)
 constexpr int M_MAX_ROWS = M_HT;
 static_assert(M_HT <= 64 * M_WAVES / 2, "a thread per row");
 constexpr int M_SLAB = 128;               // bytes per row per K slab (64 bf16)
 // LDS per build (blocks of 32 hidden rows, waves): stages of a slab's hidden rows, and slots of the waves' rings.  Four waves
-// have the CU to themselves and ask for both up to five slabs ahead.
-constexpr int mid_stages(int njv, int waves) { return waves == 4 ? (njv == 2 ? 6 : njv <= 4 ? 5 : 4) : njv == 6 ? 2 : 3; }
-constexpr int mid_ring(int njv, int waves) { return waves == 4 ? mid_stages(njv, 4) : njv == 2 ? 4 : 3; }
+// have the CU to themselves and ask for both up to five slabs ahead; with up to 32 rows they take half of it and ask three ahead.
+constexpr int mid_stages(int njv, int waves) { return njv == 1 ? 4 : waves == 4 ? (njv == 2 ? 6 : njv <= 4 ? 5 : 4) : njv == 6 ? 2 : 3; }
+constexpr int mid_ring(int njv, int waves) { return waves == 4 ? mid_stages(njv, 4) : njv <= 2 ? 4 : 3; }
 constexpr int mid_lds(int njv, int waves) {
   return mid_stages(njv, waves) * 32 * njv * M_SLAB + waves * 32 * M_SLAB * mid_ring(njv, waves);
 }
 constexpr int M_LDS_MAX = 160 * 1024;
 constexpr bool mid_fits(int waves) {
-  for (int njv = 2; njv <= 6; ++njv)        // (the waves' triples are merged in the idle stages and rings)
+  for (int njv = 1; njv <= 6; ++njv)        // (the waves' triples are merged in the idle stages and rings)
     if (mid_lds(njv, waves) > M_LDS_MAX || mid_lds(njv, waves) < waves * M_HT * (int)(sizeof(Triple) + sizeof(Draw))) return false;
   return true;
 }
@@ -92,10 +94,10 @@ __device__ __forceinline__ uint32_t lds_offset_of(const void* p) {
 // 4, 5, 6 = 0, 1, 2 with the sums in levels, for a step of up to 64 sequences; 7 = the gradient of the loss with respect to the logits (the
 // tile kernel's mode 3).
 // What a workgroup's tile is cut from: weight tile vt of W (n_valid rows), all `rows` hidden rows at H, which are rows row0 ... of the call; its
-// columns start at col0, its part is `part`.
+// columns start at col0, its part is `part`, its walk over K starts at slab walk mod their number.
 struct MidTile {
   const void *W, *H;
-  int vt, n_valid, rows, row0, col0, part;
+  int vt, n_valid, rows, row0, col0, part, walk;
   void* out;                               // SMODE 7
   int ldo;
 };
@@ -152,7 +154,7 @@ __device__ __forceinline__ void mid_tile(const LogitsArgs& a, const MidTile& t, 
   // The tiles walk K in the same order but start at different slabs (tile t at slab t mod n_slabs, wrapping round):
   // at any moment the workgroups in flight ask for different 128-byte columns of their weight rows, not all for
   // the same one, which would keep landing on the same few memory channels (rows are a power of two apart).
-  const int rot = vt % n_slabs;
+  const int rot = t.walk % n_slabs;
   auto slab_at = [&](int s) {                              // step -> slab
     const int x = s + rot;
     return slab0 + (x >= n_slabs ? x - n_slabs : x);
@@ -180,9 +182,12 @@ __device__ __forceinline__ void mid_tile(const LogitsArgs& a, const MidTile& t, 
   // hidden rows: the 4 NJV groups of 8 rows of a slab are dealt to the waves, group g = i * WAVES + wave for the
   // wave's i-th request; lane l moves, for row g * 8 + (l >> 3), the chunk that lands at position l & 7 of the row's
   // 128 LDS bytes: chunk (l & 7) ^ ((row >> 1) & 7).  Rows past the last valid one read the last valid one.
-  // (with an odd number of blocks half of eight waves ask for their last group twice: every wave has as many requests to wait for)
+  // (with an odd number of blocks half of eight waves ask for a group that another has, too: every wave has as many requests to wait for)
   constexpr int HL = (4 * NJV + WAVES - 1) / WAVES;        // requests per wave and slab
-  auto group_of = [&](int i) { return i * WAVES + wave < 4 * NJV ? i * WAVES + wave : (i - 1) * WAVES + wave; };
+  auto group_of = [&](int i) {
+    const int g = i * WAVES + wave;
+    return g < 4 * NJV ? g : g - 4 * NJV;
+  };
   const unsigned char* Ht = reinterpret_cast<const unsigned char*>(t.H);
   const uint32_t lds_base = lds_offset_of(lds);
   uint32_t hsrc[HL];
@@ -331,7 +336,7 @@ __device__ __forceinline__ void mid_tile(const LogitsArgs& a, const MidTile& t, 
   if (SMODE == 1 || SMODE == 5)
     fold_tile_sample<1, NJV>(acc, run, draw, a, 0, col_base, n_valid);
   else if (SMODE == 2 || SMODE == 6)
-    fold_tile_store<1, NJV>(acc, run, a, 0, r_end, col_base, n_valid);
+    fold_tile_store<1, NJV>(acc, run, a, t.col0, t.row0, t.row0 + r_end, col_base, n_valid);
   else
     fold_tile<1, NJV>(acc, run, col_base, t.col0, n_valid, v0 + TILE > n_valid, a.inv_t, a.log2e_t);
   const float inv_t = SMODE == 0 || SMODE == 4 ? a.inv_t : 1.f;         // (the draws' values are logit / T)
@@ -383,8 +388,8 @@ __device__ __forceinline__ void mid_tile(const LogitsArgs& a, const MidTile& t, 
 template <int NJV, int SMODE, int WAVES = M_WAVES>
 __global__ void __launch_bounds__(64 * WAVES) logits_mid_kernel(LogitsArgs a) {
   extern __shared__ __align__(1024) unsigned char lds[];
-  MidTile t = {a.W, a.H, (int)blockIdx.x, a.w_rows, a.rows, 0, a.col0, a.part0 + (int)blockIdx.x, a.out, a.ldo};
-  if constexpr (SMODE == 0 || SMODE == 7) {
+  MidTile t = {a.W, a.H, (int)blockIdx.x, a.w_rows, a.rows, 0, a.col0, a.part0 + (int)blockIdx.x, (int)blockIdx.x, a.out, a.ldo};
+  if constexpr (SMODE == 0 || SMODE == 7 || SMODE == 2 || SMODE == 6) {
     // Workgroups behind the base part's tiles take the hyper part's (a.hyper): tile u of sequence b against that sequence's rows alone, the first
     // tile of every sequence first.  In a launch of its own on the tile kernel this part was one round of a few workgroups, 58-80
     // us: V = 32064, 1 x 72 rows 99 -> 43 us; V = 128256, 1 x 80 242 -> 179, 2 x 79 275 -> 230; V = 151936, 1 x 103 277 -> 220.
@@ -393,6 +398,8 @@ __global__ void __launch_bounds__(64 * WAVES) logits_mid_kernel(LogitsArgs a) {
       t.W = reinterpret_cast<const unsigned char*>(a.hyper.W) + (size_t)b * a.hyper.cap * a.d * 2;
       t.H = reinterpret_cast<const unsigned char*>(a.H) + (size_t)b * a.rows_per_seq * a.d * 2;
       t.vt = u;
+      // (a beam step has as many first tiles as sequences: 136 rows, V = 80000, d = 2048, 1024 entries 222 -> 198 us)
+      t.walk = SMODE == 0 || SMODE == 7 ? u : (int)blockIdx.x;
       t.n_valid = min(max(a.hyper.size[b], 0), a.hyper.cap);
       t.rows = a.rows_per_seq;
       t.row0 = b * a.rows_per_seq;
@@ -401,12 +408,16 @@ __global__ void __launch_bounds__(64 * WAVES) logits_mid_kernel(LogitsArgs a) {
       t.out = a.hyper.out;
       t.ldo = a.hyper.ldo;
       if (u * 32 * WAVES >= t.n_valid) {                   // entries that do not exist: empty triples
-        if (SMODE == 0 && (int)threadIdx.x < t.rows) {     // (a thread per row)
+        if (SMODE != 7 && (int)threadIdx.x < t.rows) {     // (a thread per row)
           const size_t p = (size_t)(t.row0 + (int)threadIdx.x) * a.n_parts + t.part;
           a.part_m[p] = kNegInf;
           a.part_s[p] = 0.f;
           a.part_i[p] = kNoColumn;
         }
+        return;
+      }
+      if constexpr (SMODE == 2 || SMODE == 6) {            // one row a sequence, whatever the base part's build
+        mid_tile<1, 6, WAVES>(a, t, lds);
         return;
       }
     }
@@ -435,58 +446,39 @@ int z2z_logits_mid_columns(const z2z_ctx* c, int w_rows) {
   return (w_rows + M_WT - 1) / M_WT * 2 <= c->num_cu ? M_WT / 2 : M_WT;
 }
 
+template <int NJV, int SMODE, int WAVES>
+static void launch_as(const LogitsArgs& a, hipStream_t s) {
+  // (a beam step's hyper tiles run as the 32-row build does)
+  const bool along = a.hyper.n_work > 0 && (SMODE == 2 || SMODE == 6);
+  const int lds = along ? std::max(mid_lds(NJV, WAVES), mid_lds(1, WAVES)) : mid_lds(NJV, WAVES);
+  hipLaunchKernelGGL((logits_mid_kernel<NJV, SMODE, WAVES>), dim3((unsigned)(a.n_vtiles + a.hyper.n_work)), dim3(64 * WAVES), lds, s, a);
+}
+
+// The build for up to 32 NJV hidden rows.
+template <int NJV, int WAVES>
+static void launch_blocks(const LogitsArgs& a, hipStream_t s) {
+  constexpr bool FEW = NJV <= 2;                           // (sums in levels)
+  if (a.row_grad)
+    launch_as<NJV, 7, WAVES>(a, s);
+  else if (a.sample == 1)
+    launch_as<NJV, FEW ? 5 : 1, WAVES>(a, s);
+  else if (a.sample == 2)
+    launch_as<NJV, FEW ? 6 : 2, WAVES>(a, s);
+  else if (FEW && a.rows_per_seq == 1 && a.hyper.n_work == 0)      // (the hyper part rides along in SMODE 0)
+    launch_as<NJV, FEW ? 4 : 0, WAVES>(a, s);
+  else
+    launch_as<NJV, 0, WAVES>(a, s);
+}
+
 template <int WAVES>
 static void launch_mid(const LogitsArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.n_vtiles + a.hyper.n_work)), block(64 * WAVES);
-  const int blocks = a.rows <= 64 ? 2 : (a.rows + 31) / 32;
-  if (a.row_grad) {
-    if (blocks == 2)
-      hipLaunchKernelGGL((logits_mid_kernel<2, 7, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
-    else if (blocks == 3)
-      hipLaunchKernelGGL((logits_mid_kernel<3, 7, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
-    else if (blocks == 4)
-      hipLaunchKernelGGL((logits_mid_kernel<4, 7, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
-    else if (blocks == 5)
-      hipLaunchKernelGGL((logits_mid_kernel<5, 7, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
-    else
-      hipLaunchKernelGGL((logits_mid_kernel<6, 7, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
-    return;
-  }
-  if (a.sample == 1) {
-    if (blocks == 2)
-      hipLaunchKernelGGL((logits_mid_kernel<2, 5, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
-    else if (blocks == 3)
-      hipLaunchKernelGGL((logits_mid_kernel<3, 1, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
-    else if (blocks == 4)
-      hipLaunchKernelGGL((logits_mid_kernel<4, 1, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
-    else if (blocks == 5)
-      hipLaunchKernelGGL((logits_mid_kernel<5, 1, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
-    else
-      hipLaunchKernelGGL((logits_mid_kernel<6, 1, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
-  } else if (a.sample == 2) {
-    if (blocks == 2)
-      hipLaunchKernelGGL((logits_mid_kernel<2, 6, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
-    else if (blocks == 3)
-      hipLaunchKernelGGL((logits_mid_kernel<3, 2, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
-    else if (blocks == 4)
-      hipLaunchKernelGGL((logits_mid_kernel<4, 2, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
-    else if (blocks == 5)
-      hipLaunchKernelGGL((logits_mid_kernel<5, 2, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
-    else
-      hipLaunchKernelGGL((logits_mid_kernel<6, 2, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
-  } else {
-    if (blocks == 2 && a.rows_per_seq == 1 && a.hyper.n_work == 0)   // (the hyper part rides along in SMODE 0)
-      hipLaunchKernelGGL((logits_mid_kernel<2, 4, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
-    else if (blocks == 2)
-      hipLaunchKernelGGL((logits_mid_kernel<2, 0, WAVES>), grid, block, mid_lds(2, WAVES), s, a);
-    else if (blocks == 3)
-      hipLaunchKernelGGL((logits_mid_kernel<3, 0, WAVES>), grid, block, mid_lds(3, WAVES), s, a);
-    else if (blocks == 4)
-      hipLaunchKernelGGL((logits_mid_kernel<4, 0, WAVES>), grid, block, mid_lds(4, WAVES), s, a);
-    else if (blocks == 5)
-      hipLaunchKernelGGL((logits_mid_kernel<5, 0, WAVES>), grid, block, mid_lds(5, WAVES), s, a);
-    else
-      hipLaunchKernelGGL((logits_mid_kernel<6, 0, WAVES>), grid, block, mid_lds(6, WAVES), s, a);
+  switch ((a.rows + 31) / 32) {
+    case 1: return launch_blocks<1, WAVES>(a, s);
+    case 2: return launch_blocks<2, WAVES>(a, s);
+    case 3: return launch_blocks<3, WAVES>(a, s);
+    case 4: return launch_blocks<4, WAVES>(a, s);
+    case 5: return launch_blocks<5, WAVES>(a, s);
+    default: return launch_blocks<6, WAVES>(a, s);
   }
 }
 
@@ -502,14 +494,15 @@ int z2z_launch_logits_mid(z2z_ctx* c, LogitsArgs a, const void* W, int w_rows, i
   a.n_vtiles = (w_rows + columns - 1) / columns;
   a.once = a.once || (size_t)w_rows * a.d * sizeof(uint16_t) > kKeepBytes;
   c->n_launch[Z2Z_KERNEL_MID]++;
-  if (a.hyper.n_work > 0 && (a.sample != 0 || (a.rows_per_seq <= 64 && !a.row_grad && a.inv_t == 1.f))) return Z2Z_EUNSUPPORTED;
+  if (a.hyper.n_work > 0 && (a.sample == 1 || (a.sample == 0 && a.rows_per_seq <= 64 && !a.row_grad && a.inv_t == 1.f))) return Z2Z_EUNSUPPORTED;
   // (two workgroups of the 64-row build per weight tile for 65..128 rows, sharing the tile's weights through an
   // XCD's L2, measured slower than one of the 128-row build: 383 against 293 us at config 2's shape)
-  // builds: 2 to 6 blocks of 32 hidden rows; the sampling calls come with one row per sequence.  (3 blocks for 65..96 rows and 5 for
+  // builds: 1 to 6 blocks of 32 hidden rows; the sampling calls come with one row per sequence.  (3 blocks for 65..96 rows and 5 for
   // 129..160, the latter with three stages of hidden rows where 6 have room for two.  Whole calls, us, in the builds of 4 and 6 / 3 and 5, 80, 135 and
   // 160 rows: greedy V = 128256, d = 4096 196 / 177, 213 / 202, 227 / 203; V = 32000 55 / 51, 70 / 63, 71 / 63; V = 50257, d = 1024 30.6 /
   // 29.9, 36.8 / 33.8, 36.6 / 33.9; beams V = 80000, d = 4096 167 / 158, 203 / 192, 207 / 198; draws 183 / 173, 228 / 218, 231 / 219.
-  // 8 blocks, up to 256 rows, measured level with the tile kernel when weights still went through registers: 650 against 645 us for a decode
+  // 1 block for up to 32 rows, of 2: beams of 4 rows V = 32000, d = 1024 38.6 / 36.6, d = 4096 74 / 69, V = 151936, d = 2048 140 / 134, V =
+  // 128256, d = 4096 192 / 190.  8 blocks, up to 256 rows, measured level with the tile kernel when weights still went through registers: 650 against 645 us for a decode
   // step of 256 sequences.)
   if (columns == M_WT)
     launch_mid<M_WAVES>(a, s);
@@ -575,53 +568,24 @@ int z2z_launch_linear_mid(z2z_ctx* c, const void* A, const void* W, int R, const
 
 int z2z_logits_mid_tiles(int w_rows) { return (w_rows + M_WT - 1) / M_WT; }
 
+template <int NJV, int SMODE, int WAVES>
+static bool raise_lds() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(logits_mid_kernel<NJV, SMODE, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             M_LDS_MAX) == hipSuccess;
+}
+
+template <int NJV>
+static bool raise_blocks() {
+  constexpr bool FEW = NJV <= 2;
+  return raise_lds<NJV, 0, 8>() && raise_lds<NJV, FEW ? 4 : 0, 8>() && raise_lds<NJV, FEW ? 5 : 1, 8>() && raise_lds<NJV, FEW ? 6 : 2, 8>() &&
+         raise_lds<NJV, 7, 8>() && raise_lds<NJV, 0, 4>() && raise_lds<NJV, FEW ? 4 : 0, 4>() && raise_lds<NJV, FEW ? 5 : 1, 4>() &&
+         raise_lds<NJV, FEW ? 6 : 2, 4>() && raise_lds<NJV, 7, 4>();
+}
+
 int z2z_logits_mid_prepare(z2z_ctx* c) {
   if (c->lds_limit < M_LDS_MAX) return Z2Z_EUNSUPPORTED;
-  const void* kernels[] = {reinterpret_cast<const void*>(logits_mid_kernel<2, 3>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 3>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 7, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 7, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 7, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 7, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 7, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 7, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 7, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 7, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 7, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 7, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 0, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 4, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 5, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 6, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 0, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 0, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 0, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 1, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 1, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 1, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 2, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 2, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 2, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 0, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 1, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 2, M_WAVES>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 0, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 4, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 5, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<2, 6, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 0, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 0, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 0, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 1, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 1, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 1, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<3, 2, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<4, 2, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<5, 2, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 0, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 1, M_WAVES / 2>),
-                           reinterpret_cast<const void*>(logits_mid_kernel<6, 2, M_WAVES / 2>)};
-  for (const void* k : kernels)
-    Z2Z_HIP_TRY(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, M_LDS_MAX));
+  bool ok = raise_lds<2, 3, M_WAVES>() && raise_lds<4, 3, M_WAVES>();
+  ok = ok && raise_blocks<1>() && raise_blocks<2>() && raise_blocks<3>() && raise_blocks<4>() && raise_blocks<5>() && raise_blocks<6>();
+  if (!ok) return Z2Z_EHIP;
   return Z2Z_OK;
 }

@@ -65,6 +65,11 @@ def _setup(dtype, B, V, d, M, cap, N, seed):
     ("bf16", 80, 5, 33000, 128, 3, 40, 60, 9),             # 80 and 150 rows of it, tiles of 256 and of 128 columns
     ("bf16", 150, 5, 33000, 128, 3, 40, 60, 6),
     ("bf16", 90, 3, 2500, 192, 3, 40, 60, 5),
+    ("bf16", 40, 4, 33000, 128, 3, 30, 60, 5),             # hyper tiles along in every build
+    ("bf16", 100, 4, 33000, 64, 3, 20, 60, 5),
+    ("bf16", 135, 5, 33000, 64, 3, 300, 500, 5),
+    ("bf16", 165, 5, 33000, 64, 3, 300, 500, 5),
+    ("bf16", 24, 3, 30000, 1024, 3, 400, 600, 7),          # two workgroups a CU
     ("bf16", 135, 5, 1300, 256, 3, 40, 60, 7),
     ("bf16", 8, 4, 5, 128, 3, 20, 30, 12),                 # a vocabulary of five
     ("bf16", 8, 4, 1, 128, 3, 20, 30, 64),                 # and of one: fewer continuations than picks
