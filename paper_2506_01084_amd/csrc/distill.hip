@@ -105,20 +105,27 @@ __device__ __forceinline__ float dot16(const uint4& x, const uint4& y, float acc
   return acc;
 }
 
-// One workgroup per hidden row: its waves, up to eight, take the listed columns in turn, eight at a time against one read of the hidden row; then
-// wave 0 has the loss.  Bound by the gather of K rows of W per hidden row (popular ones come out of the caches): 8192 rows
+// One workgroup per hidden row: its first `gather` waves, up to eight, take the listed columns in turn, eight at a time against one read of the hidden
+// row; the others, where there are some, merge the row's parts (fold) into its log-sum-exp meanwhile, as logits_combine_kernel does; then wave 0 has the loss.  Bound by the gather of K rows of W per hidden row (popular ones come out of the caches): 8192 rows
 // of 64 columns, d = 4096, 4.3 GB: 307 us with four at a time, 286 with eight.
 template <bool BF16, int PL>
-__global__ void __launch_bounds__(512) teacher_loss_kernel(TeacherArgs a, const uint4* H, const uint4* W_base, const uint4* W_hyper, int d,
-                                                           const float* lse, float* kl, float* student) {
+__global__ void __launch_bounds__(768) teacher_loss_kernel(TeacherArgs a, const uint4* H, const uint4* W_base, const uint4* W_hyper, int d, int gather,
+                                                           z2z_fold fold, float* lse, float* kl, float* student) {
   __shared__ float z_row[Z2Z_MAX_TEACHER];
+  __shared__ Triple merged[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x, b = r / a.rows_per_seq;
   const int columns = a.V + min(max(a.size[b], 0), a.cap);
   const int n_chunks = d / (BF16 ? 8 : 4);
   const uint4* h = H + (size_t)r * n_chunks;
   constexpr int G = T_GROUP;
-  for (int k0 = wave * G; k0 < a.K; k0 += (int)(blockDim.x >> 6) * G) {
+  const int mergers = (int)(blockDim.x >> 6) - gather;
+  if (wave >= gather) {
+    const size_t at = (size_t)r * fold.n_parts;
+    const Triple tr = merge_parts(fold.m + at, fold.s + at, fold.i + at, (wave - gather) * 64 + lane, 64 * mergers, fold.n_parts, fold.inv_t);
+    if (lane == 0) merged[wave - gather] = tr;
+  }
+  for (int k0 = wave < gather ? wave * G : a.K; k0 < a.K; k0 += gather * G) {
     const uint4* w[G];
     bool there[G];
     float acc[G];
@@ -147,7 +154,15 @@ __global__ void __launch_bounds__(512) teacher_loss_kernel(TeacherArgs a, const 
   for (int k = threadIdx.x; k < a.K; k += (int)blockDim.x) student[(size_t)r * a.K + k] = z_row[k];
   if (wave != 0) return;
   const Teacher<PL> t = load_teacher<PL>(a, r, columns);
-  const float l = lse[r];
+  float l;
+  if (mergers > 0) {
+    Triple tr = merged[0];
+    for (int w = 1; w < mergers; ++w) merge_triple(tr, merged[w], fold.inv_t);
+    l = fmaf(tr.m, fold.inv_t, logf(tr.s));
+    if (lane == 0) lse[r] = l;
+  } else {
+    l = lse[r];
+  }
   float sum = 0.f;
 #pragma unroll
   for (int u = 0; u < PL; ++u)
@@ -236,19 +251,27 @@ TeacherArgs teacher_args(const z2z_ctx* c, const z2z_teacher& t, int r0, int row
 
 int z2z_launch_extended_distill(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base, const void* W_hyper,
                                 const z2z_teacher& t, float* kl, float* lse, float* student, hipStream_t s) {
-  const int rc = z2z_launch_extended_logits(c, H, rows, rows_per_seq, W_base, W_hyper, nullptr, nullptr, lse, nullptr, s, false, t.temperature);
+  // The parts' merge in the loss's launch, a launch less, in waves of its own: with up to 40 columns, whose workgroups are small enough to have a CU's
+  // wave slots left, and with more for up to 512 rows.  Apart / together, us, T = 2: fp32 V = 5000, d = 128, 122 rows, 33 columns 21.1 / 17.8, V = 32000, d = 256
+  // 36.4 / 32.8, 351 rows 73.6 / 69.8; bf16 V = 50257, d = 1024, 122 rows 35.8 / 32.2, 4096 454 / 451, of 64 columns 351 rows 76.4 / 76.0, 1000 144 /
+  // 147, 4096 486 / 508.
+  const int gather = std::min((t.K + T_GROUP - 1) / T_GROUP, 8);
+  const bool together = gather <= 5 || rows <= 512;
+  z2z_fold fold = {};
+  const int rc = z2z_launch_extended_logits(c, H, rows, rows_per_seq, W_base, W_hyper, nullptr, nullptr, lse, nullptr, s, false, t.temperature,
+                                            together ? &fold : nullptr);
   if (rc != Z2Z_OK) return rc;
   const TeacherArgs a = teacher_args(c, t, 0, rows, rows_per_seq);
   const uint4 *h = reinterpret_cast<const uint4*>(H), *wb = reinterpret_cast<const uint4*>(W_base), *wh = reinterpret_cast<const uint4*>(W_hyper);
-  const dim3 grid((unsigned)rows), block(64u * (unsigned)std::min((t.K + T_GROUP - 1) / T_GROUP, 8));
+  const dim3 grid((unsigned)rows), block(64u * (unsigned)(gather + (fold.n_parts > 256 ? 4 : fold.n_parts > 0 ? 1 : 0)));
   if (c->cfg.dtype == Z2Z_BF16 && t.K <= 64)
-    hipLaunchKernelGGL((teacher_loss_kernel<true, 1>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, lse, kl, student);
+    hipLaunchKernelGGL((teacher_loss_kernel<true, 1>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, gather, fold, lse, kl, student);
   else if (c->cfg.dtype == Z2Z_BF16)
-    hipLaunchKernelGGL((teacher_loss_kernel<true, 4>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, lse, kl, student);
+    hipLaunchKernelGGL((teacher_loss_kernel<true, 4>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, gather, fold, lse, kl, student);
   else if (t.K <= 64)
-    hipLaunchKernelGGL((teacher_loss_kernel<false, 1>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, lse, kl, student);
+    hipLaunchKernelGGL((teacher_loss_kernel<false, 1>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, gather, fold, lse, kl, student);
   else
-    hipLaunchKernelGGL((teacher_loss_kernel<false, 4>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, lse, kl, student);
+    hipLaunchKernelGGL((teacher_loss_kernel<false, 4>), grid, block, 0, s, a, h, wb, wh, c->cfg.d, gather, fold, lse, kl, student);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }

@@ -28,25 +28,8 @@ __global__ void __launch_bounds__(256) logits_combine_kernel(const float* part_m
   const int lane = threadIdx.x & 63;
   const int t = threadIdx.x % ROW_THREADS;
   const int r = blockIdx.x * ROWS_PER_BLOCK + threadIdx.x / ROW_THREADS;
-  Triple tr = empty_triple();
-  if (r < rows) {
-    const size_t base = (size_t)r * n_parts;
-    for (int p = t; p < n_parts; p += ROW_THREADS) {
-      Triple o;
-      o.m = part_m[base + p];
-      o.s = part_s[base + p];
-      o.i = part_i[base + p];
-      merge_triple(tr, o, inv_t);
-    }
-  }
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    Triple o;
-    o.m = __shfl_xor(tr.m, off);
-    o.s = __shfl_xor(tr.s, off);
-    o.i = __shfl_xor(tr.i, off);
-    merge_triple(tr, o, inv_t);
-  }
+  const size_t base = (size_t)r * n_parts;
+  Triple tr = merge_parts(part_m + base, part_s + base, part_i + base, t, ROW_THREADS, r < rows ? n_parts : 0, inv_t);
   if (ROW_THREADS > 64) {
     __shared__ Triple xch[4];
     if (lane == 0) xch[threadIdx.x >> 6] = tr;
@@ -405,7 +388,7 @@ static size_t step_parts(const z2z_ctx* c) {
 
 int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                const void* W_hyper, int32_t* argmax, float* mx, float* lse, float* logits,
-                               hipStream_t s, bool use_static, float temperature) {
+                               hipStream_t s, bool use_static, float temperature, z2z_fold* fold) {
   const int V = c->cfg.V, cap = c->cfg.cap;
   const bool timed = c->opt_timing && c->n_timed < Z2Z_MAX_TIMED && c->ev_created;
   z2z_parts parts;
@@ -421,6 +404,12 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
 
   // the fast kernels never store logits: the full-logits output (small shapes) takes the general kernel
   const bool fast_ok = c->cfg.dtype == Z2Z_BF16 && c->cfg.d % 64 == 0 && c->fast_ready && logits == nullptr;
+  // the end of every way: the parts are merged, or left as they are
+  auto merge = [&](int n, float inv_t) -> int {
+    if (!fold) return launch_combine(parts, n, rows, argmax, mx, lse, s, inv_t);
+    *fold = {parts.m, parts.s, parts.i, n, inv_t};
+    return Z2Z_OK;
+  };
   // decode step: one hidden row per sequence -> the bandwidth-bound kernel (it can store the logits too).
   // Its base units serve 64 rows per pass over W_base, each pass at about the cost of the first; from the second
   // pass on the tile kernel takes the base vocabulary (all rows at once) and only the hyper units run here
@@ -444,7 +433,7 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
                          c->st.size);
       Z2Z_HIP_TRY(hipGetLastError());
     }
-    return launch_combine(parts, n_parts, rows, argmax, mx, lse, s);
+    return merge(n_parts, 1.f);
   }
 
   // (the general kernel is many times slower per bf16 tile: even a tile with a few valid rows goes to the tile kernel)
@@ -531,7 +520,7 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
                          c->st.size);
       Z2Z_HIP_TRY(hipGetLastError());
     }
-    return launch_combine(parts, n_parts, rows, argmax, mx, lse, s, a.inv_t);
+    return merge(n_parts, a.inv_t);
   }
 
   // Both parts in one launch of the tile kernel (the measurement probes run the base part alone), up to 32768 tiles, where the hyper part is a hundredth
@@ -571,7 +560,7 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
     Z2Z_HIP_TRY(hipEventRecord(c->ev_stop[c->n_timed], s));
     c->n_timed++;
   }
-  return launch_combine(parts, n_parts, rows, argmax, mx, lse, s, a.inv_t);
+  return merge(n_parts, a.inv_t);
 }
 
 // Room for one row of logits per sequence, the row maxima and log-sum-exps.

@@ -45,6 +45,27 @@ __device__ __forceinline__ void merge_triple(Triple& a, const Triple& b, float i
   a.i = b_wins ? b.i : a.i;
 }
 
+// A wave's share of a row's n parts, every `step`-th from p on for each lane, merged across the lanes.
+__device__ __forceinline__ Triple merge_parts(const float* part_m, const float* part_s, const int32_t* part_i, int p, int step, int n, float inv_t) {
+  Triple tr = empty_triple();
+  for (; p < n; p += step) {
+    Triple o;
+    o.m = part_m[p];
+    o.s = part_s[p];
+    o.i = part_i[p];
+    merge_triple(tr, o, inv_t);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    Triple o;
+    o.m = __shfl_xor(tr.m, off);
+    o.s = __shfl_xor(tr.s, off);
+    o.i = __shfl_xor(tr.i, off);
+    merge_triple(tr, o, inv_t);
+  }
+  return tr;
+}
+
 // The running best of a Gumbel-max draw.
 struct Draw {
   float v;   // largest perturbed value so far

@@ -40,6 +40,14 @@ struct z2z_parts {
   size_t capacity;
 };
 
+// The parts that a logits call has left, [rows, n_parts], and the 1 / T of their sums.
+struct z2z_fold {
+  const float *m, *s;
+  const int32_t* i;
+  int32_t n_parts;
+  float inv_t;
+};
+
 // A work buffer of the context that grows with the calls.
 struct z2z_work {
   void* p;
@@ -137,7 +145,7 @@ int z2z_launch_hyper_embed(z2z_ctx* c, const void* E, void* W_hyper, const int32
 // do not fit) instead of the context's growable buffers
 int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                const void* W_hyper, int32_t* argmax, float* mx, float* lse, float* logits,
-                               hipStream_t s, bool use_static = false, float temperature = 1.0f);
+                               hipStream_t s, bool use_static = false, float temperature = 1.0f, z2z_fold* fold = nullptr);   // fold: the parts are left to the caller
 int z2z_static_scratch_prepare(z2z_ctx* c);   // z2z_create: look up the static array's address on c->device
 int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                const void* W_hyper, float temperature, int32_t top_k, float top_p, uint64_t seed,

@@ -131,15 +131,20 @@ clean()
 
 
 def test_a_temperature_leaves_the_decode_kernels(without_a_device):
-    """At T = 1 the log-sum-exp comes from the kernels that extended_nll takes, at another T from those whose folds take one."""
+    """At T = 1 the logits' parts come from the kernels that extended_nll takes (merged in the loss's own launch), at another T from those whose folds
+    take one."""
     without_a_device("""
 for rps in (1, 5, 100):
     h = context(B=8, V=40000, M=3, cap=1024, d=256)
     fwd = lambda T: lib.z2z_extended_distill(h, P, 8 * rps, rps, P, P, 4, P, P, T, P, P, P + 64, None)
     assert lib.z2z_extended_nll(h, P, 8 * rps, rps, P, P, P, P, P, None) == 0
-    nll = [n for n, _ in launches() if "logits_" in n]
+    parts = lambda log: [n for n, _ in log if "logits_" in n and "combine" not in n]
+    nll = parts(launches())
     assert fwd(1.0) == 0
-    assert [n for n, _ in launches() if "logits_" in n] == nll
+    log = launches()
+    assert parts(log) == nll and len(named(log, "combine")) == 0
+    assert lib.z2z_extended_distill(h, P, 8 * rps, rps, P, P, 64, P, P, 1.0, P, P, P + 64, None) == 0
+    assert len(named(launches(), "combine")) == (rps == 100)              # (800 rows of 64 columns)
     assert fwd(2.0) == 0
     assert not named(launches(), "logits_decode")
 """)
