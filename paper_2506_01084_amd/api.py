@@ -185,6 +185,7 @@ class Context:
             cfg.w[j] = float(w[j]) if w is not None and j < len(w) else 0.0
         self.B, self.V, self.M, self.cap, self.d, self.dtype = B, V, M, cap, d, dtype
         self.torch_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
+        self._E_shape, self._W_shape = (V, d), (B, cap, d)
         self._device = torch.cuda.current_device()
         self._h = c_void_p()
         _check(self._lib.z2z_create(byref(self._h), byref(cfg)), "z2z_create")
@@ -308,12 +309,12 @@ class Context:
     def embed_codes(self, codes: torch.Tensor, n_codes: Optional[torch.Tensor], E: torch.Tensor, W_hyper: torch.Tensor,
                     X: torch.Tensor, status: torch.Tensor, scale: float = 1.0) -> None:
         """X[b, i] = scale * (row of E or W_hyper[b] that codes[b, i] names); rows behind n_codes[b] are left as they were."""
-        assert codes.dim() == 2 and codes.shape[0] == self.B and X.shape == (*codes.shape, self.d)
-        assert E.shape == (self.V, self.d) and W_hyper.shape == (self.B, self.cap, self.d)
-        assert (n_codes is None or n_codes.numel() == self.B) and status.numel() == self.B
-        _check(self._lib.z2z_embed_codes(self._h, self._own(codes, torch.int32), self._own(n_codes, torch.int32), codes.shape[1],
-                                         self._own(E, self.torch_dtype), self._own(W_hyper, self.torch_dtype), float(scale),
-                                         self._own(X, self.torch_dtype), self._own(status, torch.int32), _stream()), "z2z_embed_codes")
+        B, stride = codes.shape
+        assert B == self.B and X.shape == (B, stride, self.d) and E.shape == self._E_shape and W_hyper.shape == self._W_shape
+        assert (n_codes is None or n_codes.numel() == B) and status.numel() == B
+        own, i32, kind = self._own, torch.int32, self.torch_dtype
+        _check(self._lib.z2z_embed_codes(self._h, own(codes, i32), own(n_codes, i32), stride, own(E, kind), own(W_hyper, kind), float(scale),
+                                         own(X, kind), own(status, i32), _stream()), "z2z_embed_codes")
 
     def embed_codes_backward(self, codes: torch.Tensor, n_codes: Optional[torch.Tensor], dX: torch.Tensor, dE: torch.Tensor,
                              dW_hyper: torch.Tensor, scale: float = 1.0, add: bool = False) -> None:
@@ -328,7 +329,7 @@ class Context:
 
     def codebook_reorder(self, beams: int, source: torch.Tensor, W_hyper: Optional[torch.Tensor] = None) -> None:
         """Sequence p * beams + k takes over the state of sequence p * beams + source[p * beams + k] (in place, cache rows too)."""
-        assert source.numel() == self.B and (W_hyper is None or W_hyper.shape == (self.B, self.cap, self.d))
+        assert source.numel() == self.B and (W_hyper is None or W_hyper.shape == self._W_shape)
         _check(self._lib.z2z_codebook_reorder(self._h, int(beams), self._own(source, torch.int32), self._own(W_hyper, self.torch_dtype),
                                               _stream()), "z2z_codebook_reorder")
 
