@@ -454,9 +454,10 @@ int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t ro
  * contribute nothing.
  *   d_lse, d_student   what z2z_extended_distill returned for the same inputs
  *   d_grad_kl          [rows] float or NULL (= 1 for every row)
- * dZ is rounded to bf16 where nothing is listed; the listed columns' values, nearly all of the gradient, stay fp32 and are added to the
- * products by rows of W and H.  Types, restrictions, errors and work space as for z2z_extended_nll_backward; besides, rows * K below
- * 2^31 (else Z2Z_EUNSUPPORTED) and 20 + d / 8 bytes of work space per listed column.  Every hidden row has to be finite, as there: a NaN times
+ * dZ is rounded to bf16 where nothing is listed; the listed columns' values, nearly all of the gradient, stay fp32.  The gradients are sums of
+ * products with both, in fp32, rounded once (dW_base once per pass where dZ takes more than 200 GB and the sequences go in several).  Types,
+ * restrictions, errors and work space as for z2z_extended_nll_backward; besides, rows * K below 2^31 (else Z2Z_EUNSUPPORTED), and work space: 4 d
+ * bytes per hidden row, 4 d per listed column (V + B * cap of them at most) and 21 + d / 8 per listed column.  Every hidden row has to be finite, as there: a NaN times
  * a gradient of zero is a NaN in the products. */
 int z2z_extended_distill_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,
                                   const void* d_W_hyper, int32_t n_teacher, const int32_t* d_ids, const float* d_teacher,

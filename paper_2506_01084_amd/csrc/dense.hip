@@ -208,18 +208,21 @@ int launch_kmajor(z2z_ctx* c, LogitsArgs& a, bool rows_too, const void* A, int l
 }  // namespace
 
 int z2z_launch_linear_input(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const void* residual, void* out, int ldo,
-                            int R, const int32_t* rows_dev, int N, int K, hipStream_t s, z2z_linear_batch batch) {
+                            int R, const int32_t* rows_dev, int N, int K, hipStream_t s, z2z_linear_batch batch, int stream_f32) {
   LogitsArgs a;
   memset(&a, 0, sizeof(a));
   a.d = K;
+  a.stream_f32 = stream_f32;
   a.rows_dev = rows_dev;
   return launch_kmajor(c, a, false, A, lda, W, ldw, k_rows, residual, out, ldo, R, N, batch, s);
 }
 
 int z2z_launch_linear_weight(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const int32_t* k_dev,
-                             const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch) {
+                             const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch, z2z_row_sums row_sums) {
   LogitsArgs a;
   memset(&a, 0, sizeof(a));
+  a.sums = row_sums.sums;
+  a.row_slot = row_sums.row_slot;
   a.d = (k_rows + 63) / 64 * 64;
   a.k_dev = k_dev;
   return launch_kmajor(c, a, true, A, lda, W, ldw, k_rows, residual, out, N, R, N, batch, s);

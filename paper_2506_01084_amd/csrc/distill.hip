@@ -171,31 +171,35 @@ __global__ void __launch_bounds__(768) teacher_loss_kernel(TeacherArgs a, const 
   if (lane == 0) kl[r] = !t.some ? 0.f : (t.outside ? INFINITY : sum);
 }
 
-// g[r] = the row's upstream gradient (1 without one) / T, 0 for rows without a distribution or with some of it on a column that
-// does not exist; targets[r] = -1: the probability epilogue takes no column out.
-template <int PL>
-__global__ void __launch_bounds__(256) teacher_grad_kernel(TeacherArgs a, const float* grad, float* g, int32_t* targets) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= a.rows) return;
-  const int columns = a.V + min(max(a.size[r / a.rows_per_seq], 0), a.cap);
-  const Teacher<PL> t = load_teacher<PL>(a, r, columns);
-  if ((threadIdx.x & 63) == 0) {
-    g[r] = t.some && !t.outside ? (grad ? grad[r] : 1.0f) * a.inv_t : 0.f;
-    targets[r] = -1;
-  }
-}
+struct WeightArgs {
+  const float *lse, *student, *grad;
+  float *weight, *row_grad;
+  int32_t* no_target;
+  uint4* slot;              // 16-byte pieces of it
+  size_t slot_pieces;
+  int32_t row_blocks;
+};
 
-// The listed columns of dZ = g (p - q), behind the kernel that has stored g p everywhere: zero there, the value itself to `weight`, from the row's
-// own logits; a column listed several times has the sum of its q, and its value at the first place.  A wave per row.
+// The first row_blocks: dZ = g (p - q) of a row's listed columns, from the row's own logits, a wave per row; a column listed several times has the
+// sum of its q, and its value at the first place.  g = the row's upstream gradient (1 without one) / T, 0 for rows without a distribution or with
+// some of it on a column that does not exist; the probability epilogue stores g p everywhere and takes no target out.  The other blocks clear the slots.
 template <int PL>
-__global__ void __launch_bounds__(256) teacher_dz_kernel(TeacherArgs a, const float* lse, const float* student, const float* g, float* weight,
-                                                         uint16_t* base, size_t ld_base, uint16_t* hyper, size_t ld_hyper) {
+__global__ void __launch_bounds__(256) teacher_weight_kernel(TeacherArgs a, WeightArgs w) {
+  if ((int)blockIdx.x >= w.row_blocks) {
+    const size_t step = (size_t)(gridDim.x - (unsigned)w.row_blocks) * 256;
+    for (size_t i = (size_t)(blockIdx.x - (unsigned)w.row_blocks) * 256 + threadIdx.x; i < w.slot_pieces; i += step) w.slot[i] = uint4{~0u, ~0u, ~0u, ~0u};
+    return;
+  }
   const int lane = threadIdx.x & 63;
   const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= a.rows) return;
-  const float gr = g[r];
   const int columns = a.V + min(max(a.size[r / a.rows_per_seq], 0), a.cap);
   const Teacher<PL> t = load_teacher<PL>(a, r, columns);
+  const float gr = t.some && !t.outside ? (w.grad ? w.grad[r] : 1.0f) * a.inv_t : 0.f;
+  if (lane == 0) {
+    w.row_grad[r] = gr;
+    w.no_target[r] = -1;
+  }
   float total[PL];
   bool again[PL];
 #pragma unroll
@@ -217,20 +221,28 @@ __global__ void __launch_bounds__(256) teacher_dz_kernel(TeacherArgs a, const fl
       }
     }
   }
-  const float l = lse[r];
+  const float l = w.lse[r];
 #pragma unroll
   for (int u = 0; u < PL; ++u) {
     const int k = lane + 64 * u, id = t.id[u];
     if (k >= a.K) continue;
     const size_t at = (size_t)r * a.K + k;
     const bool there = id >= 0 && id < columns && gr != 0.f;
-    weight[at] = there && !again[u] ? gr * (expf(fmaf(student[at], a.inv_t, -l)) - total[u]) : 0.f;
-    if (!there) continue;
-    if (id < a.V)
-      base[(size_t)r * ld_base + id] = 0;
-    else
-      hyper[(size_t)r * ld_hyper + (id - a.V)] = 0;
+    w.weight[at] = there && !again[u] ? gr * (expf(fmaf(w.student[at], a.inv_t, -l)) - total[u]) : 0.f;
   }
+}
+
+// Zeros in the listed columns of dZ, behind the kernel that has stored g p everywhere: what stands there is the weights' part of the products.
+__global__ void __launch_bounds__(256) teacher_dz_kernel(TeacherArgs a, uint16_t* base, size_t ld_base, uint16_t* hyper, size_t ld_hyper) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int r = (int)(i / a.K);
+  if (r >= a.rows) return;
+  const int id = a.ids[i];
+  if (id < 0) return;
+  if (id < a.V)
+    base[(size_t)r * ld_base + id] = 0;
+  else if (id - a.V < min(max(a.size[r / a.rows_per_seq], 0), a.cap))
+    hyper[(size_t)r * ld_hyper + (id - a.V)] = 0;
 }
 
 TeacherArgs teacher_args(const z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq) {
@@ -276,27 +288,34 @@ int z2z_launch_extended_distill(z2z_ctx* c, const void* H, int32_t rows, int32_t
   return Z2Z_OK;
 }
 
-int z2z_launch_teacher_grad(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* grad, float* g, int32_t* targets,
-                            hipStream_t s) {
-  const TeacherArgs a = teacher_args(c, t, r0, rows, rows_per_seq);
+int z2z_launch_teacher_weight(z2z_ctx* c, const z2z_teacher& t, int rows, int rows_per_seq, const float* lse, const float* grad,
+                              const z2z_listed_part& l, hipStream_t s) {
+  const TeacherArgs a = teacher_args(c, t, 0, rows, rows_per_seq);
+  const size_t keys = (size_t)c->cfg.V + (size_t)c->cfg.B * c->cfg.cap;
+  WeightArgs w;
+  w.lse = lse;
+  w.student = t.student;
+  w.grad = grad;
+  w.weight = l.weight;
+  w.row_grad = l.row_grad;
+  w.no_target = l.no_target;
+  w.slot = reinterpret_cast<uint4*>(l.slot);
+  w.slot_pieces = (keys + 3) / 4;                    // (its room is a multiple of 256 bytes)
+  w.row_blocks = (rows + 3) / 4;
+  const dim3 grid((unsigned)w.row_blocks + (unsigned)std::min<size_t>((w.slot_pieces + 255) / 256, 1024)), block(256);
   if (t.K <= 64)
-    hipLaunchKernelGGL(teacher_grad_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, grad ? grad + r0 : nullptr, g, targets);
+    hipLaunchKernelGGL(teacher_weight_kernel<1>, grid, block, 0, s, a, w);
   else
-    hipLaunchKernelGGL(teacher_grad_kernel<4>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, grad ? grad + r0 : nullptr, g, targets);
+    hipLaunchKernelGGL(teacher_weight_kernel<4>, grid, block, 0, s, a, w);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
 
-int z2z_launch_teacher_dz(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* lse, const float* g, float* weight,
-                          void* base, size_t ld_base, void* hyper, size_t ld_hyper, hipStream_t s) {
+int z2z_launch_teacher_dz(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, void* base, size_t ld_base, void* hyper,
+                          size_t ld_hyper, hipStream_t s) {
   const TeacherArgs a = teacher_args(c, t, r0, rows, rows_per_seq);
-  const size_t at = (size_t)r0 * t.K;
-  if (t.K <= 64)
-    hipLaunchKernelGGL(teacher_dz_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, lse + r0, t.student + at, g, weight + at,
-                       reinterpret_cast<uint16_t*>(base), ld_base, reinterpret_cast<uint16_t*>(hyper), ld_hyper);
-  else
-    hipLaunchKernelGGL(teacher_dz_kernel<4>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, lse + r0, t.student + at, g, weight + at,
-                       reinterpret_cast<uint16_t*>(base), ld_base, reinterpret_cast<uint16_t*>(hyper), ld_hyper);
+  hipLaunchKernelGGL(teacher_dz_kernel, dim3((unsigned)(((long long)rows * t.K + 255) / 256)), dim3(256), 0, s, a, reinterpret_cast<uint16_t*>(base),
+                     ld_base, reinterpret_cast<uint16_t*>(hyper), ld_hyper);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }

@@ -328,7 +328,8 @@ __global__ void __launch_bounds__(1024) sort_place_kernel(LookupArgs a, uint32_t
 // ---- gradient: sums over runs of equal keys -----------------------------------------------------------------------------------
 // What is summed up, and where to (KIND):
 //   LOOKUP_BF16, LOOKUP_F32   the rows of dX, a position's own each; base rows are fp32
-//   WEIGHTED                  weight[position] times row position / per_row of a bf16 matrix; base rows are bf16, everything is added
+//   WEIGHTED                  weight[position] times row position / per_row of a bf16 matrix; to sums, fp32 rows of their own: a table row's is
+//                             slot[row] (the row itself, or where there are fewer positions than rows the number of its first sorted position)
 enum { LOOKUP_BF16 = 0, LOOKUP_F32 = 1, WEIGHTED = 2 };
 
 // Sorted positions of a wave: 8 where there are few, so that more waves share them, 32 or 64 else (sums that cross the ends of a piece go
@@ -354,11 +355,20 @@ struct GradArgs {
   int32_t chunks, slices, d, add, fill_blocks, per_row;
   bool past;                              // zeros past the caches
   float scale;
+  float* sums;                            // WEIGHTED
+  int32_t* slot;
+  int32_t by_row;
 };
 
-// N consecutive features of a table row := (+=) scale * sum.
+// N consecutive features of a table row := (+=) scale * sum.  first: the sorted position that its run begins at (WEIGHTED).
 template <int KIND, int N>
-__device__ __forceinline__ void store_row(const GradArgs& a, uint32_t key, size_t at, const float (&sum)[N]) {
+__device__ __forceinline__ void store_row(const GradArgs& a, uint32_t key, uint32_t first, size_t at, const float (&sum)[N]) {
+  if (KIND == WEIGHTED) {
+    float4* to = reinterpret_cast<float4*>(a.sums + (size_t)(a.by_row ? key : first) * a.d + at);
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) to[q] = float4{sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
+    return;
+  }
   float x[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = sum[e] * a.scale;
@@ -453,6 +463,7 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   }
   uint32_t key = __builtin_amdgcn_readfirstlane(my_key);
   if (key >= a.sentinel) return;
+  uint32_t first = p0;
   const uint32_t prev = p0 > 0u ? a.skey[p0 - 1] : kNoKey, next = p0 + cnt < a.n ? a.skey[p0 + cnt] : kNoKey;
   bool began_before = prev == key;
   float acc[EPC];
@@ -487,19 +498,21 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
       if (last || after != key) {
         const bool goes_on = last && after == key;
         if (goes_on && !began_before && chunk == 0) a.joins[1u + atomicAdd(a.joins, 1u)] = piece;
+        if (KIND == WEIGHTED && !began_before && chunk == 0) a.slot[key] = (int32_t)(a.by_row ? key : first);
         if (on) {
           if (began_before || goes_on) {
             float4* to = reinterpret_cast<float4*>((began_before ? a.head : a.tail) + (size_t)piece * a.d + (size_t)chunk * EPC);
 #pragma unroll
             for (int q = 0; q < EPC / 4; ++q) to[q] = float4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
           } else {
-            store_row<KIND, EPC>(a, key, (size_t)chunk * EPC, acc);
+            store_row<KIND, EPC>(a, key, first, (size_t)chunk * EPC, acc);
           }
         }
 #pragma unroll
         for (int e = 0; e < EPC; ++e) acc[e] = 0.f;
         began_before = false;
         key = after;
+        first = p0 + (uint32_t)i + 1u;
       }
     }
   }
@@ -553,7 +566,7 @@ __global__ void __launch_bounds__(256) join_kernel(GradArgs a) {
         sum.w += x.w;
       }
       const float s[4] = {sum.x, sum.y, sum.z, sum.w};
-      store_row<KIND, 4>(a, key, (size_t)f, s);
+      store_row<KIND, 4>(a, key, KIND == WEIGHTED ? (uint32_t)a.slot[key] : 0u, (size_t)f, s);
     }
     __syncthreads();
   }
@@ -644,7 +657,7 @@ bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
 }
 
 // Sort the positions, sum up the runs, join those that cross pieces.  g: what is summed and where to.
-// listed (WEIGHTED): a teacher's listed rows for dH, in the sort's launch or in one of their own.
+// listed (WEIGHTED): a teacher's listed rows for the hidden rows, in the sort's launch or in one of their own.
 template <int KIND>
 int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned char* ws, GradArgs g, hipStream_t s,
                const z2z_listed::ListedArgs& listed = z2z_listed::ListedArgs()) {
@@ -733,36 +746,68 @@ int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int3
   return c->cfg.dtype == Z2Z_BF16 ? launch_sum<LOOKUP_BF16>(c, a, p, ws, g, s) : launch_sum<LOOKUP_F32>(c, a, p, ws, g, s);
 }
 
-int z2z_weighted_rows_reserve(z2z_ctx* c, long long rows, int per_row, float** weight, hipStream_t s) {
-  SumPlan p;
-  if (!plan_sum(c, rows * per_row, WEIGHTED, &p)) return Z2Z_EUNSUPPORTED;
-  const int rc = z2z_work_reserve(c, &c->lookup_ws, p.bytes + (size_t)p.n * sizeof(float), s);
+namespace {
+
+// A teacher's listed part of the gradient: the sum's own work space, then what it leaves to the products.
+struct ListedPlan {
+  SumPlan sum;
+  size_t o_weight, o_grad, o_none, o_hidden, o_slot, o_sums, bytes;
+  bool by_row;
+};
+
+bool plan_listed(const z2z_ctx* c, long long rows, int per_row, ListedPlan* p) {
+  if (!plan_sum(c, rows * per_row, WEIGHTED, &p->sum)) return false;
+  const size_t n = p->sum.n, keys = (size_t)c->cfg.V + (size_t)c->cfg.B * c->cfg.cap, row = (size_t)c->cfg.d * sizeof(float);
+  p->by_row = keys <= n;
+  p->bytes = p->sum.bytes;
+  auto take = [&](size_t bytes) { const size_t at = p->bytes; p->bytes += (bytes + 255) / 256 * 256; return at; };
+  p->o_weight = take(n * sizeof(float));
+  p->o_grad = take((size_t)rows * sizeof(float));
+  p->o_none = take((size_t)rows * sizeof(int32_t));
+  p->o_hidden = take((size_t)rows * row);
+  p->o_slot = take(keys * sizeof(int32_t));
+  p->o_sums = take((p->by_row ? keys : n) * row);
+  return true;
+}
+
+}  // namespace
+
+int z2z_listed_reserve(z2z_ctx* c, long long rows, int per_row, z2z_listed_part* l, hipStream_t s) {
+  ListedPlan p;
+  if (!plan_listed(c, rows, per_row, &p)) return Z2Z_EUNSUPPORTED;
+  const int rc = z2z_work_reserve(c, &c->lookup_ws, p.bytes, s);
   if (rc != Z2Z_OK) return rc;
-  *weight = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(c->lookup_ws.p) + p.bytes);
+  unsigned char* ws = reinterpret_cast<unsigned char*>(c->lookup_ws.p);
+  l->weight = reinterpret_cast<float*>(ws + p.o_weight);
+  l->row_grad = reinterpret_cast<float*>(ws + p.o_grad);
+  l->no_target = reinterpret_cast<int32_t*>(ws + p.o_none);
+  l->hidden = reinterpret_cast<float*>(ws + p.o_hidden);
+  l->slot = reinterpret_cast<int32_t*>(ws + p.o_slot);
+  l->sums = reinterpret_cast<float*>(ws + p.o_sums);
   return Z2Z_OK;
 }
 
-int z2z_launch_weighted_rows(z2z_ctx* c, const int32_t* ids, long long rows, int per_row, const float* weight, const void* H,
-                             const void* W_base, const void* W_hyper, void* dH, void* dW_base, void* dW_hyper, hipStream_t s) {
-  SumPlan p;
-  if (!plan_sum(c, rows * per_row, WEIGHTED, &p)) return Z2Z_EUNSUPPORTED;
+int z2z_launch_listed(z2z_ctx* c, const int32_t* ids, long long rows, int per_row, const void* H, const void* W_base, const void* W_hyper,
+                      const z2z_listed_part& part, hipStream_t s) {
+  ListedPlan p;
+  if (!plan_listed(c, rows, per_row, &p)) return Z2Z_EUNSUPPORTED;
   GradArgs g;
   memset(&g, 0, sizeof(g));
   g.dX = reinterpret_cast<const u32x4*>(H);
-  g.weight = weight;
-  g.dE = dW_base;
-  g.dW = dW_hyper;
-  g.add = 1;
+  g.weight = part.weight;
+  g.add = 1;                                         // (rows that no position names are not looked after)
   g.per_row = per_row;
-  g.scale = 1.0f;
+  g.sums = part.sums;
+  g.slot = part.slot;
+  g.by_row = p.by_row ? 1 : 0;
   const LookupArgs a = lookup_args(c, ids, nullptr, (int32_t)(rows / c->cfg.B * per_row));     // (a sequence's lists behind each other)
   z2z_listed::ListedArgs l;
   l.ids = ids;
-  l.weight = weight;
+  l.weight = part.weight;
   l.size = c->st.size;
   l.W_base = reinterpret_cast<const uint4*>(W_base);
   l.W_hyper = reinterpret_cast<const uint4*>(W_hyper);
-  l.dH = reinterpret_cast<uint4*>(dH);
+  l.sum = reinterpret_cast<float4*>(part.hidden);
   l.rows = (int32_t)rows;
   l.rows_per_seq = (int32_t)(rows / c->cfg.B);
   l.V = c->cfg.V;
@@ -770,5 +815,5 @@ int z2z_launch_weighted_rows(z2z_ctx* c, const int32_t* ids, long long rows, int
   l.K = per_row;
   l.n_chunks = a.chunks;
   l.slices = (a.chunks + 63) / 64;
-  return launch_sum<WEIGHTED>(c, a, p, reinterpret_cast<unsigned char*>(c->lookup_ws.p), g, s, l);
+  return launch_sum<WEIGHTED>(c, a, p.sum, reinterpret_cast<unsigned char*>(c->lookup_ws.p), g, s, l);
 }

@@ -1,5 +1,5 @@
-// dH[r] += sum_k weight[r, k] W[ids[r, k]] over the columns that a row lists, W the joint unembedding [W_base ; W_hyper[b]]: the listed part of
-// the distillation loss's gradient with respect to the hidden rows.
+// sum[r] = sum_k weight[r, k] W[ids[r, k]] over the columns that a row lists, W the joint unembedding [W_base ; W_hyper[b]]: the listed part of
+// the distillation loss's gradient with respect to the hidden rows, which the products of the other columns are added to.
 #pragma once
 
 #include "logits_common.h"
@@ -11,12 +11,12 @@ struct ListedArgs {
   const float* weight;      // [rows, K]
   const int32_t* size;      // [sequences]
   const uint4 *W_base, *W_hyper;
-  uint4* dH;
+  float4* sum;              // [rows, d]
   int32_t rows, rows_per_seq, V, cap, K;
   int32_t n_chunks, slices; // 16-byte pieces of a row, and those by 64
 };
 
-// One wave, 64 pieces of 16 bytes of row r = wid / slices: eight rows of W requested at a time; fp32, one rounding.
+// One wave, 64 pieces of 16 bytes of row r = wid / slices: eight rows of W requested at a time; fp32.
 __device__ __forceinline__ void add_listed_rows(const ListedArgs& a, long long wid) {
   const int lane = threadIdx.x & 63;
   const int r = (int)(wid / a.slices);
@@ -27,13 +27,11 @@ __device__ __forceinline__ void add_listed_rows(const ListedArgs& a, long long w
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  bool any = false;
   for (int k0 = 0; k0 < a.K; k0 += 64) {
     const int k = k0 + lane;
     const int my_id = k < a.K ? a.ids[(size_t)r * a.K + k] : -1;
     const float my_w = k < a.K && my_id >= 0 && my_id < columns ? a.weight[(size_t)r * a.K + k] : 0.f;
     uint64_t left = __ballot(my_w != 0.f);
-    any |= left != 0ull;
     while (left != 0ull) {
       uint4 x[8];
       float w[8];
@@ -59,15 +57,10 @@ __device__ __forceinline__ void add_listed_rows(const ListedArgs& a, long long w
       }
     }
   }
-  if (!any || chunk >= a.n_chunks) return;
-  uint4* to = a.dH + (size_t)r * a.n_chunks + chunk;
-  const uint4 was = *to;
-  const uint32_t ws[4] = {was.x, was.y, was.z, was.w};
-  uint32_t out[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    out[e] = z2z_logits::pack_bf16(__uint_as_float(ws[e] << 16) + acc[2 * e], __uint_as_float(ws[e] & 0xFFFF0000u) + acc[2 * e + 1]);
-  *to = uint4{out[0], out[1], out[2], out[3]};
+  if (chunk >= a.n_chunks) return;
+  float4* to = a.sum + ((size_t)r * a.n_chunks + chunk) * 2;
+  to[0] = float4{acc[0], acc[1], acc[2], acc[3]};
+  to[1] = float4{acc[4], acc[5], acc[6], acc[7]};
 }
 
 }  // namespace z2z_listed

@@ -189,7 +189,7 @@ __device__ __forceinline__ float gelu_erf(float x) {
 }
 
 // A dense layer's epilogue on 4 columns of a row, whose first is element `at` of the output and the residual: out = act(x + bias) + residual.
-__device__ __forceinline__ void finish_linear(float4 x, const float4& bias, int act, const void* residual, void* out, bool stream_f32, size_t at) {
+__device__ __forceinline__ void finish_linear(float4 x, const float4& bias, int act, const void* residual, void* out, int stream_f32, size_t at) {
   x.x += bias.x;
   x.y += bias.y;
   x.z += bias.z;
@@ -200,7 +200,7 @@ __device__ __forceinline__ void finish_linear(float4 x, const float4& bias, int 
     x.z = gelu_erf(x.z);
     x.w = gelu_erf(x.w);
   }
-  if (stream_f32) {                                  // fp32 residual and output: no rounding
+  if (stream_f32) {                                  // fp32 residual, and (1) output: no rounding
     if (residual) {
       const float4 rv = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(residual) + at);
       x.x += rv.x;
@@ -208,10 +208,11 @@ __device__ __forceinline__ void finish_linear(float4 x, const float4& bias, int 
       x.z += rv.z;
       x.w += rv.w;
     }
-    *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at) = x;
-    return;
-  }
-  if (residual) {
+    if (stream_f32 == 1) {
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at) = x;
+      return;
+    }
+  } else if (residual) {
     const uint2 rv = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(residual) + at);
     x.x += __uint_as_float(rv.x << 16);
     x.y += __uint_as_float(rv.x & 0xFFFF0000u);
@@ -277,7 +278,10 @@ struct LogitsArgs {
   const void* residual;   // [rows, ldo] bf16 or nullptr
   int32_t act;            // 0 none, 1 GELU (erf)
   int32_t ldo;
-  int32_t stream_f32;     // 1: residual and out are fp32 (a residual stream kept unrounded between layers)
+  int32_t stream_f32;     // 1: residual and out are fp32 (a residual stream kept unrounded between layers), 2: the residual alone
+  // K-major products: sums[row_slot[r]] is added to output row r where row_slot[r] is not negative (fp32 rows of ldo columns); nullptr: none
+  const float* sums;
+  const int32_t* row_slot;
   // softmax at a temperature (folds that draw nothing, probability mode): 1 / T, and log2(e) / T; 1 and log2(e) without one.  The triples'
   // maxima are of the logits, their sums of exp((logit - max) / T)
   float inv_t, log2e_t;
@@ -499,14 +503,20 @@ int z2z_launch_linear(z2z_ctx* c, const void* A, const void* W, const float* bia
 //   z2z_launch_linear_input    out[R, N] = A[R, K] . W[k_rows, N] + residual;  A's columns from k_rows to K (K: a multiple of 64) are finite
 //   z2z_launch_linear_weight   out[R, N] = A[k_rows, R]^T . W[k_rows, N] + residual;  with k_dev only the first *k_dev rows exist
 // A batch of them: outputs of R rows below each other, W (and the second's A) batch_w (batch_a) elements apart.
+// stream_f32 as in LogitsArgs: a sum of several products is rounded once.  The second adds row_sums where they are given.
 struct z2z_linear_batch {
   int n;
   size_t a, w;
 };
+struct z2z_row_sums {
+  const float* sums;       // fp32 rows, as wide as the output
+  const int32_t* row_slot; // [output rows] which of them is added to the row, or negative
+};
 int z2z_launch_linear_input(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const void* residual, void* out, int ldo,
-                            int R, const int32_t* rows_dev, int N, int K, hipStream_t s, z2z_linear_batch batch = {1, 0, 0});
+                            int R, const int32_t* rows_dev, int N, int K, hipStream_t s, z2z_linear_batch batch = {1, 0, 0}, int stream_f32 = 0);
 int z2z_launch_linear_weight(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const int32_t* k_dev,
-                             const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch = {1, 0, 0});
+                             const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch = {1, 0, 0},
+                             z2z_row_sums row_sums = {nullptr, nullptr});
 // Row pitch for n columns of an activation that is an operand of dense layers: n, or 64 more where n columns are a
 // multiple of 4 KiB -- the tile kernel's workgroups read the same slab of 256 rows at a time, and rows that far apart
 // on a power of two put it on a few memory channels (35400 rows x 4096 columns, K = 16384: 1.07 -> 1.18

@@ -614,6 +614,62 @@ __device__ __forceinline__ void store_tile16_f32(const Acc& acc, const LogitsArg
   }
 }
 
+// Store one finished tile of a product that is one term of a sum: the others come in fp32 (LogitsArgs::stream_f32: a residual of the output's
+// shape; ROWS: row_slot and sums, rows of their own), and the sum is rounded once, by the last term's product.
+template <bool ROWS>
+__device__ __forceinline__ void store_sum16(const Acc& acc, const LogitsArgs& a, int row_base, int r_end, int col_base, int n_valid) {
+  const int lane15 = threadIdx.x & 15;
+  int slot[F_N];
+#pragma unroll
+  for (int j = 0; j < F_N; ++j) slot[j] = ROWS ? a.row_slot[min(row_base + j * 16 + lane15, r_end - 1)] : 0;
+#pragma unroll
+  for (int j = 0; j < F_N; ++j) {
+    const int row = row_base + j * 16 + lane15;
+    const bool row_ok = row < r_end;
+    const float* from = ROWS ? a.sums + (size_t)max(slot[j], 0) * a.ldo : reinterpret_cast<const float*>(a.residual) + (size_t)row * a.ldo;
+    float4 rv[F_N];
+#pragma unroll
+    for (int i = 0; i < F_N; ++i) {
+      const int col = col_base + i * 16;
+      rv[i] = row_ok && slot[j] >= 0 && col < n_valid ? *reinterpret_cast<const float4*>(from + col) : float4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (ROWS && a.residual) {                // (what earlier passes over the rows have left, bf16)
+      const uint16_t* was = reinterpret_cast<const uint16_t*>(a.residual) + (size_t)row * a.ldo;
+#pragma unroll
+      for (int i = 0; i < F_N; ++i) {
+        const int col = col_base + i * 16;
+        const uint2 w = row_ok && col < n_valid ? *reinterpret_cast<const uint2*>(was + col) : uint2{0u, 0u};
+        rv[i].x += __uint_as_float(w.x << 16);
+        rv[i].y += __uint_as_float(w.x & 0xFFFF0000u);
+        rv[i].z += __uint_as_float(w.y << 16);
+        rv[i].w += __uint_as_float(w.y & 0xFFFF0000u);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < F_N; ++i) {
+      rv[i].x += read_acc(acc[i][j][0]);
+      rv[i].y += read_acc(acc[i][j][1]);
+      rv[i].z += read_acc(acc[i][j][2]);
+      rv[i].w += read_acc(acc[i][j][3]);
+    }
+    if (!ROWS && a.stream_f32 == 1) {
+      float* out = reinterpret_cast<float*>(a.out) + (size_t)row * a.ldo;
+#pragma unroll
+      for (int i = 0; i < F_N; ++i)
+        if (row_ok && col_base + i * 16 < n_valid) *reinterpret_cast<float4*>(out + col_base + i * 16) = rv[i];
+      continue;
+    }
+    uint16_t* out_row = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo;
+#pragma unroll
+    for (int i = 0; i < F_N; i += 2) {
+      uint2 o[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) o[h] = uint2{pack_bf16(rv[i + h].x, rv[i + h].y), pack_bf16(rv[i + h].z, rv[i + h].w)};
+      store_two_blocks(out_row, row_ok, col_base, i, o[0], o[1], n_valid);
+    }
+  }
+}
+
 // Store one finished tile as it is (fp32), for a dense layer whose K range is split over several workgroups.
 __device__ __forceinline__ void store_partial16(const Acc& acc, float* part, int ld, int row_base, int r_end, int col_base,
                                                 int n_valid) {
@@ -732,11 +788,13 @@ __device__ __forceinline__ void merge_rows(R (&a)[F_N], S swap, float inv_t = 1.
 // V = 128256, d = 4096, 3 x 176 654 -> 597, 2 x 577 1090 -> 1043; level about 10000 rows (3 x 3577 7818 and 7826).
 // TEMP (modes 0, 1 and 3): the softmax has a temperature.  (Instances of their own: with 1 / T and log2(e) / T read from the arguments in every call,
 // which costs two more scalar registers, 32768 rows x 128256 at T = 1 took 23.82 ms instead of 23.66.)
-template <int MODE, bool ROT = false, bool TW = false, bool TH = false, bool HYP = false, bool TEMP = false>
+// SUM (K-major products): one term of a sum (store_sum16); by rows where H is K-major too.
+template <int MODE, bool ROT = false, bool TW = false, bool TH = false, bool HYP = false, bool TEMP = false, bool SUM = false>
 __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   static_assert((MODE == 2 || !TW) && (TW || !TH), "dense layers only, and H K-major only where W is");
   static_assert(!HYP || MODE == 0 || (MODE == 3 && !ROT), "");
   static_assert(!TEMP || MODE == 0 || MODE == 1 || MODE == 3, "");
+  static_assert(!SUM || TW, "");
   const float inv_t = TEMP ? a.inv_t : 1.f, log2e_t = TEMP ? a.log2e_t : 1.4426950408889634f;
   constexpr bool PROBE_NOREQ = MODE == 8 || MODE == 9;
   constexpr bool PROBE_MFMA = MODE == 9;
@@ -1170,6 +1228,8 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
       if (MODE == 2) {
         if (it.part >= 0)
           store_partial16(acc, a.split + (ptrdiff_t)it.part * (FT * FT) - ((ptrdiff_t)r0 * FT + vt * FT), FT, row_base, r_end, col_base, n_valid);
+        else if (SUM)
+          store_sum16<TH>(acc, a, row_base, r_end, col_base, n_valid);
         else if (TW && !a.residual)
           store_plain16(acc, a, row_base, r_end, col_base, n_valid);
         else if (!TW && a.stream_f32)
@@ -1276,9 +1336,15 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
       }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (r0 + trow + i * 4 < r_end)
-        finish_linear(x[i], bias, a.act, a.residual, a.out, a.stream_f32, (size_t)(r0 + trow + i * 4) * a.ldo + col);
+    for (int i = 0; i < 2; ++i) {
+      const int row = r0 + trow + i * 4;
+      if (row >= r_end) break;
+      if (a.row_slot && a.row_slot[row] >= 0) {
+        const float4 y = *reinterpret_cast<const float4*>(a.sums + (size_t)a.row_slot[row] * a.ldo + col);
+        x[i] = float4{x[i].x + y.x, x[i].y + y.y, x[i].z + y.z, x[i].w + y.w};
+      }
+      finish_linear(x[i], bias, a.act, a.residual, a.out, a.stream_f32, (size_t)row * a.ldo + col);
+    }
   }
 }
 
@@ -1317,7 +1383,11 @@ bool z2z_logits_fast_cuts(const LogitsArgs& a) {
 }
 
 int z2z_launch_linear_kmajor(const LogitsArgs& a, bool rows_too, unsigned grid, hipStream_t s) {
-  if (rows_too)
+  if (rows_too && a.row_slot)
+    hipLaunchKernelGGL((logits_fast_kernel<2, false, true, true, false, false, true>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+  else if (!rows_too && a.stream_f32)
+    hipLaunchKernelGGL((logits_fast_kernel<2, false, true, false, false, false, true>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+  else if (rows_too)
     hipLaunchKernelGGL((logits_fast_kernel<2, false, true, true>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
   else
     hipLaunchKernelGGL((logits_fast_kernel<2, false, true, false>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
@@ -1419,6 +1489,10 @@ int z2z_logits_fast_prepare(z2z_ctx* c) {
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, true, false>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, true, true>),
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
+  Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, true, false, false, false, true>),
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
+  Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, true, true, false, false, true>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<0, true>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));

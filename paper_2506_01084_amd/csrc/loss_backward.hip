@@ -82,8 +82,13 @@ int z2z_launch_hyper_embed_backward(z2z_ctx* c, const void* dW_hyper, float* dE,
 // every operand as it is.
 // With a teacher dZ = g (p - q) is large in its listed columns, where q is, and small everywhere else; rounded to bf16, those few values would
 // carry nearly all of the products' error.  They stay fp32 (weight) and out of the matrix: the epilogue stores g p, a small kernel behind it
-// zeros in the listed columns, and the listed rows of W and H, weight times each, are added to the products in fp32 (8 x 1024 rows
-// of 64 columns, V = 128256, d = 4096: gradients 2.6e-3 from exact instead of 1.7e-3, which is their own rounding, without this).
+// zeros in the listed columns, and the products' epilogues add the listed rows of W and H, weight times each, summed up in fp32 ahead of them.
+// A row of dZ sums to zero, so what the rows of W have in common nearly cancels between the listed columns and the others (and between base and
+// hyper columns); what the rows of H have in common does so in a row of dW, where student and teachers agree about a column.  So no part of a
+// gradient is rounded before its last term is in: dH is fp32 until the hyper product.  (Relative errors with every product's result rounded / this,
+// the outputs' own rounding being 1.65e-3: dH, a common row of W four times the individual ones, V = 3000, 33 columns 3.0e-2 / 1.7e-3, as large as
+// they are 8.0e-3 / 1.6e-3; dW_base, the same of H, V = 1200, 200 columns 5.1e-3 / 1.7e-3.  8 x 1024 rows of 64 columns, V = 128256, d = 4096 26.1 /
+// 26.3-26.6 ms, loss and gradient; 2 x 61 of 33, V = 50257, d = 1024 242 / 240 us.)
 int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base,
                                      const void* W_hyper, const int32_t* targets, const float* lse,
                                      const float* grad_nll, void* dH, void* dW_base, void* dW_hyper, hipStream_t s,
@@ -95,19 +100,18 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   // the benchmark configurations): dH and dW_hyper of a chunk are its own, dW_base of a later chunk adds to the
   // bf16 result of the earlier ones (one more rounding per chunk).
   // work space (bf16 unless noted), 256-byte aligned pieces
-  float* weight = nullptr;
+  z2z_listed_part listed = {};
   if (teacher) {
-    const int rc = z2z_weighted_rows_reserve(c, rows, teacher->K, &weight, s);
+    const int rc = z2z_listed_reserve(c, rows, teacher->K, &listed, s);
     if (rc != Z2Z_OK) return rc;
   }
   size_t off = 0;
-  size_t o_g, o_t, o_Pb, o_Ph;
+  size_t o_g, o_Pb, o_Ph;
   auto take = [&](size_t bytes) { const size_t at = off; off += round_up(bytes, 256); return at; };
   auto layout = [&](int n_seq) {
     const size_t rc = (size_t)n_seq * rows_per_seq;
     off = 0;
-    o_g = take(rc * 4);                              // float g[rows of the chunk]
-    o_t = teacher ? take(rc * 4) : 0;                // their targets: none
+    o_g = teacher ? 0 : take(rc * 4);                // float g[rows of the chunk]
     o_Pb = take(rc * Vp * 2);                        // dZ, base columns      [rows, Vp]
     o_Ph = take(rc * capp * 2);                      // dZ, hyper columns     [rows, capp]
     return off;
@@ -127,7 +131,6 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   }
   unsigned char* ws = reinterpret_cast<unsigned char*>(c->bwd_ws);
   float* g = reinterpret_cast<float*>(ws + o_g);
-  int32_t* no_targets = reinterpret_cast<int32_t*>(ws + o_t);
   void *Pb = ws + o_Pb, *Ph = ws + o_Ph;
   // (nothing is folded over a strip here, and a workgroup's operand stream runs on from tile to tile anyway.  Tiles one by one, against
   // strips of four: base part of 1448 rows, V = 151936 1332 -> 1238 us, 109, V = 32064 237 -> 66, 32768, V = 128256 24.55 -> 24.39 ms;
@@ -137,18 +140,19 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   const uint16_t* Wh16 = reinterpret_cast<const uint16_t*>(W_hyper);
 
   int rc;
+  if (teacher) {
+    rc = z2z_launch_teacher_weight(c, *teacher, rows, rows_per_seq, lse, grad_nll, listed, s);
+    if (rc == Z2Z_OK) rc = z2z_launch_listed(c, teacher->ids, rows, teacher->K, H, W_base, W_hyper, listed, s);
+    if (rc != Z2Z_OK) return rc;
+  }
   for (int b0 = 0; b0 < B; b0 += n_seq) {
     const int nb = b0 + n_seq <= B ? n_seq : B - b0;
     const int r0 = b0 * rows_per_seq, rows_c = nb * rows_per_seq;
     const uint16_t* Hc = H16 + (size_t)r0 * d;
     const uint16_t* Whc = Wh16 + (size_t)b0 * cap * d;
-    if (teacher) {
-      rc = z2z_launch_teacher_grad(c, *teacher, r0, rows_c, rows_per_seq, grad_nll, g, no_targets, s);
-      if (rc != Z2Z_OK) return rc;
-    } else {
+    if (!teacher)
       hipLaunchKernelGGL(row_grad_kernel, dim3((rows_c + 255) / 256), dim3(256), 0, s, targets + r0,
                          grad_nll ? grad_nll + r0 : nullptr, c->st.size + b0, rows_c, rows_per_seq, V, cap, g);
-    }
     // ---- dZ: the forward kernel with the probability epilogue -------------------------------------------
     // (up to 192 rows are bound by the weights' bytes, as in the forward pass: the streaming kernel)
     const bool few = c->opt_logits_kernel == 0 && z2z_logits_mid_ok(c, rows_c);
@@ -171,8 +175,8 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
       a.d = d;
       set_softmax_temperature(a, teacher ? teacher->temperature : 1.0f);
       a.lse = lse + r0 + row;
-      a.row_grad = g + row;
-      a.targets = teacher ? no_targets + row : targets + r0 + row;
+      a.row_grad = teacher ? listed.row_grad + r0 + row : g + row;
+      a.targets = teacher ? listed.no_target + r0 + row : targets + r0 + row;
       a.out = reinterpret_cast<uint16_t*>(Pb) + row * Vp;
       a.ldo = (int)Vp;
       if (cap > 0) {
@@ -190,25 +194,30 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
       if (rc != Z2Z_OK) return rc;
     }
     if (teacher) {
-      rc = z2z_launch_teacher_dz(c, *teacher, r0, rows_c, rows_per_seq, lse, g, weight, Pb, Vp, Ph, capp, s);
+      rc = z2z_launch_teacher_dz(c, *teacher, r0, rows_c, rows_per_seq, Pb, Vp, Ph, capp, s);
       if (rc != Z2Z_OK) return rc;
     }
     // ---- the products ------------------------------------------------------------------------------------------
     uint16_t* dHc = reinterpret_cast<uint16_t*>(dH) + (size_t)r0 * d;
-    rc = z2z_launch_linear_input(c, Pb, (int)Vp, W_base, d, V, nullptr, dHc, d, rows_c, nullptr, d, (int)Vp, s);
+    float* dHs = teacher ? listed.hidden + (size_t)r0 * d : nullptr;      // the sum of dH's terms; bf16 without a teacher
+    rc = z2z_launch_linear_input(c, Pb, (int)Vp, W_base, d, V, dHs, teacher && cap > 0 ? (void*)dHs : dHc, d, rows_c, nullptr, d, (int)Vp, s, {1, 0, 0},
+                                 !teacher ? 0 : cap > 0 ? 1 : 2);
     if (rc != Z2Z_OK) return rc;
-    rc = z2z_launch_linear_weight(c, Pb, (int)Vp, Hc, d, rows_c, nullptr, b0 > 0 ? dW_base : nullptr, dW_base, V, d, s);
+    // (the listed rows go in once, with the last pass over the sequences)
+    const z2z_row_sums none = {nullptr, nullptr};
+    rc = z2z_launch_linear_weight(c, Pb, (int)Vp, Hc, d, rows_c, nullptr, b0 > 0 ? dW_base : nullptr, dW_base, V, d, s, {1, 0, 0},
+                                  teacher && b0 + nb == B ? z2z_row_sums{listed.sums, listed.slot} : none);
     if (rc != Z2Z_OK) return rc;
     if (cap > 0) {                                   // one product per sequence
       uint16_t* dWh = reinterpret_cast<uint16_t*>(dW_hyper) + (size_t)b0 * cap * d;
-      rc = z2z_launch_linear_input(c, Ph, (int)capp, Whc, d, cap, dHc, dHc, d, rows_per_seq, nullptr, d, (int)capp, s,
-                                   {nb, 0, (size_t)cap * d});
+      rc = z2z_launch_linear_input(c, Ph, (int)capp, Whc, d, cap, teacher ? (const void*)dHs : dHc, dHc, d, rows_per_seq, nullptr, d, (int)capp, s,
+                                   {nb, 0, (size_t)cap * d}, teacher ? 2 : 0);
       if (rc != Z2Z_OK) return rc;
       rc = z2z_launch_linear_weight(c, Ph, (int)capp, Hc, d, rows_per_seq, nullptr, nullptr, dWh, cap, d, s,
-                                    {nb, (size_t)rows_per_seq * capp, (size_t)rows_per_seq * d});
+                                    {nb, (size_t)rows_per_seq * capp, (size_t)rows_per_seq * d},
+                                    teacher ? z2z_row_sums{listed.sums, listed.slot + V + (size_t)b0 * cap} : none);
       if (rc != Z2Z_OK) return rc;
     }
   }
-  if (teacher) return z2z_launch_weighted_rows(c, teacher->ids, rows, teacher->K, weight, H, W_base, W_hyper, dH, dW_base, dW_hyper, s);
   return Z2Z_OK;
 }

@@ -97,7 +97,7 @@ struct z2z_ctx {
   // dense layers on few rows with K split over workgroups: the partial tiles
   void* skinny_partial;
   size_t skinny_partial_bytes;
-  z2z_work lookup_ws;      // gradient of the code lookup: sorted positions, sums that cross pieces
+  z2z_work lookup_ws;      // gradient of the code lookup: sorted positions, sums that cross pieces; a teacher's listed part
   bool captured;           // a call that uses work buffers has been captured into a graph: none is freed from then on
   z2z_kept* kept;
   // options
@@ -170,17 +170,24 @@ int z2z_launch_embed_codes_backward(z2z_ctx* c, const int32_t* codes, const int3
                                     int32_t flags, float* dE, void* dW_hyper, hipStream_t s);
 int z2z_launch_extended_distill(z2z_ctx* c, const void* H, int32_t rows, int32_t rows_per_seq, const void* W_base, const void* W_hyper,
                                 const z2z_teacher& t, float* kl, float* lse, float* student, hipStream_t s);
-// For the backward pass, rows [r0, r0 + rows): the row gradients and targets of the probability epilogue; behind it zeros for the listed columns of
-// dZ, whose values go to weight [rows of the call, K].
-int z2z_launch_teacher_grad(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* grad, float* g, int32_t* targets,
-                            hipStream_t s);
-int z2z_launch_teacher_dz(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, const float* lse, const float* g, float* weight,
-                          void* base, size_t ld_base, void* hyper, size_t ld_hyper, hipStream_t s);
-// dH[r] += sum_k weight[r, k] W[ids[r, k]] and dW[ids[r, k]] += weight[r, k] H[r] over all listed columns, bf16, the latter sorted by row of
-// [dW_base ; dW_hyper[b]] (embed_codes.hip).  The first call makes room for it in the work space, and for the weights.
-int z2z_weighted_rows_reserve(z2z_ctx* c, long long rows, int per_row, float** weight, hipStream_t s);
-int z2z_launch_weighted_rows(z2z_ctx* c, const int32_t* ids, long long rows, int per_row, const float* weight, const void* H,
-                             const void* W_base, const void* W_hyper, void* dH, void* dW_base, void* dW_hyper, hipStream_t s);
+// The backward pass's listed columns, for all rows of the call: dZ there (weight), and what it adds to the gradients, in fp32.
+struct z2z_listed_part {
+  float* weight;           // [rows, K]
+  float* row_grad;         // [rows] of the probability epilogue
+  int32_t* no_target;      // [rows] its targets: none
+  float* hidden;           // [rows, d]: sum_k weight[r, k] W[ids[r, k]]
+  int32_t* slot;           // [V + B * cap] where in sums a row of [W_base ; W_hyper[b]] has its sum of weight[r, k] H[r], -1: none lists it
+  float* sums;             // rows of d
+};
+int z2z_listed_reserve(z2z_ctx* c, long long rows, int per_row, z2z_listed_part* l, hipStream_t s);
+// weight, row_grad, no_target, and no slots yet; then hidden, slot and sums, the latter sorted by row (embed_codes.hip)
+int z2z_launch_teacher_weight(z2z_ctx* c, const z2z_teacher& t, int rows, int rows_per_seq, const float* lse, const float* grad,
+                              const z2z_listed_part& l, hipStream_t s);
+int z2z_launch_listed(z2z_ctx* c, const int32_t* ids, long long rows, int per_row, const void* H, const void* W_base, const void* W_hyper,
+                      const z2z_listed_part& part, hipStream_t s);
+// Zeros in the listed columns of dZ, rows [r0, r0 + rows).
+int z2z_launch_teacher_dz(z2z_ctx* c, const z2z_teacher& t, int r0, int rows, int rows_per_seq, void* base, size_t ld_base, void* hyper,
+                          size_t ld_hyper, hipStream_t s);
 int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
                              int32_t picks, int32_t* parent, int32_t* code, float* picked, hipStream_t s);
 // The pick from stored logits [B, V + cap] and the largest of each part of base_columns / hyper_columns columns (powers of two); the
