@@ -223,8 +223,9 @@ int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_cod
  *   flags  0: both gradients are overwritten, rows that no position names (and rows at and beyond C_b) with zeros;
  *          Z2Z_GRAD_ADD: added to what is there (rows that no position names are not touched), one rounding per element
  * With z2z_hyper_embed_backward behind it the gradient reaches E through the entries, too: that call adds to the same d_dE.
- * B * stride and V + B * cap below 2^31, else Z2Z_EUNSUPPORTED.  Work space: 16 bytes per position and a quarter of dX's
- * size (an eighth in fp32), library scratch. */
+ * B * stride and V + B * cap below 2^31, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 18 bytes per position and d / 4 more, an eighth
+ * of dX's size (a sixteenth in fp32), or d more for the first 131072 / ceil(d / 512) positions (fp32: d / 256) if that is more.  A call makes room for
+ * every call of fewer positions. */
 #define Z2Z_GRAD_ADD 1
 int z2z_embed_codes_backward(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, float scale,
                              const void* d_dX, int32_t flags, float* d_dE, void* d_dW_hyper, void* stream);
@@ -457,7 +458,8 @@ int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t ro
  * dZ is rounded to bf16 where nothing is listed; the listed columns' values, nearly all of the gradient, stay fp32.  The gradients are sums of
  * products with both, in fp32, rounded once (dW_base once per pass where dZ takes more than 200 GB and the sequences go in several).  Types,
  * restrictions, errors and work space as for z2z_extended_nll_backward; besides, rows * K below 2^31 (else Z2Z_EUNSUPPORTED), and work space: 4 d
- * bytes per hidden row, 4 d per listed column (V + B * cap of them at most) and 21 + d / 8 per listed column.  Every hidden row has to be finite, as there: a NaN times
+ * bytes per hidden row, 4 d per listed column (V + B * cap of them at most), 4 per row of the joint tables, and 22 + d / 8 per listed column or d more
+ * for the first 262144 / ceil(d / 512) of them if that is more.  Every hidden row has to be finite, as there: a NaN times
  * a gradient of zero is a NaN in the products. */
 int z2z_extended_distill_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,
                                   const void* d_W_hyper, int32_t n_teacher, const int32_t* d_ids, const float* d_teacher,

@@ -335,10 +335,9 @@ enum { LOOKUP_BF16 = 0, LOOKUP_F32 = 1, WEIGHTED = 2 };
 // Sorted positions of a wave: 8 where there are few, so that more waves share them, 32 or 64 else (sums that cross the ends of a piece go
 // through memory, [pieces, d] twice, and a teacher's lists have K positions a row).
 constexpr int kShortPiece = 8;
-int piece_of(int kind, long long positions, int slices) {
-  const int piece = kind == WEIGHTED ? 64 : 32;
-  return positions * slices < 4096LL * piece ? kShortPiece : piece;
-}
+int long_piece(int kind) { return kind == WEIGHTED ? 64 : 32; }
+// Positions from which on the pieces are long.
+long long long_from(int kind, int slices) { return (4096LL * long_piece(kind) + slices - 1) / slices; }
 
 struct GradArgs {
   const u32x4* dX;
@@ -621,7 +620,8 @@ __global__ void __launch_bounds__(256) listed_rows_kernel(z2z_listed::ListedArgs
   z2z_listed::add_listed_rows(a, (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
-// How the work space of a sum by rows is laid out, and what its sort takes.
+// How the work space of a sum by rows is laid out, and what its sort takes.  bytes: enough for every call of fewer positions, too, whose pieces may be
+// short ones (d = 4096: 16383 positions of a lookup leave 64 MiB of sums, 32768 half of that), so that one call at the largest shape makes room for all.
 struct SumPlan {
   uint32_t n, tiles, pieces;
   int bits, passes, piece;
@@ -630,6 +630,7 @@ struct SumPlan {
 };
 
 bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
+  const int slices = (c->cfg.d / (kind == LOOKUP_F32 ? 4 : 8) + 63) / 64;
   const long long keys = (long long)c->cfg.V + (long long)c->cfg.B * c->cfg.cap;
   // (positions and rows of the joint table are 32-bit numbers here)
   if (positions > 0x7FFFFFFFLL || keys > 0x7FFFFFFFLL) return false;
@@ -639,7 +640,7 @@ bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
   p->passes = (key_bits + 9) / 10;
   p->bits = (key_bits + p->passes - 1) / p->passes;
   p->tiles = (p->n + S_TILE - 1) / S_TILE;
-  p->piece = piece_of(kind, positions, (c->cfg.d / (kind == LOOKUP_F32 ? 4 : 8) + 63) / 64);
+  p->piece = positions < long_from(kind, slices) ? kShortPiece : long_piece(kind);
   p->pieces = (p->n + p->piece - 1) / p->piece;
   p->small = p->n <= (uint32_t)S_TILE;
   // sorted keys and positions (twice where the passes go through memory), the tiles' counts, sums that cross pieces
@@ -653,6 +654,8 @@ bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
   p->o_joins = take(((size_t)p->pieces + 1) * 4);
   p->o_head = p->pieces > 1 ? take((size_t)p->pieces * c->cfg.d * 4) : 0;
   p->o_tail = p->pieces > 1 ? take((size_t)p->pieces * c->cfg.d * 4) : 0;
+  SumPlan most;                                      // (of the calls with short pieces)
+  if (p->piece != kShortPiece && plan_sum(c, long_from(kind, slices) - 1, kind, &most)) p->bytes = std::max(p->bytes, most.bytes);
   return true;
 }
 
