@@ -35,8 +35,8 @@
  *     `stream` is being captured into a graph a buffer cannot grow: the call returns Z2Z_ECAPTURE and
  *     enqueues nothing -- make one eager call at the same shape before capturing, or use
  *     z2z_extended_logits_static, which never allocates.
- *     Once a call that uses work space has been captured, no work buffer of the context is freed before z2z_destroy: one that
- *     grows leaves the old one to the graph.
+ *     A work buffer that a captured call uses is not freed before z2z_destroy: where a later call needs a larger one, the old one
+ *     is left to the graph.  A call that returns Z2Z_ENOMEM leaves the buffers at the size they had.
  *   - Calls on one context must be issued from one host thread at a time, and work of one context
  *     must be ordered (same stream, or synchronised by the caller).
  *   - z2z_embed_codes, z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward, z2z_extended_beam and

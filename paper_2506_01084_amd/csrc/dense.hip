@@ -37,15 +37,7 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(const float* partial, i
 
 // The partial tiles' buffer, at least `need` bytes of it.
 int ensure_partial(z2z_ctx* c, size_t need, hipStream_t s) {
-  if (need <= c->skinny_partial_bytes) return Z2Z_OK;
-  Z2Z_TRY_GROW(s);
-  z2z_release(c, c->skinny_partial);
-  c->skinny_partial = nullptr;
-  c->skinny_partial_bytes = 0;
-  const size_t want = need > ((size_t)64 << 20) ? need : ((size_t)64 << 20);
-  if (!z2z_device_malloc(&c->skinny_partial, want)) return Z2Z_ENOMEM;
-  c->skinny_partial_bytes = want;
-  return Z2Z_OK;
+  return z2z_work_reserve(c, &c->partial_ws, need, s, (size_t)64 << 20);
 }
 
 }  // namespace
@@ -62,9 +54,9 @@ int z2z_launch_linear_parts(z2z_ctx* c, const void* A, const void* W, int R, con
     const int ksplit = z2z_linear_mid_ksplit(N, K);
     int rc = ensure_partial(c, (size_t)ksplit * R * N * sizeof(float), s);
     if (rc != Z2Z_OK) return rc;
-    *partial = reinterpret_cast<const float*>(c->skinny_partial);
-    return z2z_launch_linear_mid(c, A, W, R, rows_dev, N, K, once, reinterpret_cast<float*>(c->skinny_partial),
-                                 c->skinny_partial_bytes / sizeof(float), ksplit_out, s);
+    *partial = reinterpret_cast<const float*>(c->partial_ws.p);
+    return z2z_launch_linear_mid(c, A, W, R, rows_dev, N, K, once, reinterpret_cast<float*>(c->partial_ws.p),
+                                 c->partial_ws.bytes / sizeof(float), ksplit_out, s);
   }
   // more rows than the 64 the decode-step kernel serves per pass over the weights, but fewer 256 x 256 output
   // tiles than would give every CU one (a few hundred rows, or up to a few thousand with a narrow layer): the
@@ -96,7 +88,7 @@ int z2z_launch_linear_parts(z2z_ctx* c, const void* A, const void* W, int R, con
       a.rows_dev = rows_dev;
       a.ksplit = ksplit;
       a.slabs_per_part = per;
-      a.partial = reinterpret_cast<float*>(c->skinny_partial);
+      a.partial = reinterpret_cast<float*>(c->partial_ws.p);
       *partial = a.partial;
       *ksplit_out = ksplit;
       return z2z_launch_logits_fast(5, a, (unsigned)(tiles * ksplit), s);
@@ -118,7 +110,7 @@ constexpr int kSplitSlabs = 32;
 unsigned order_dense(z2z_ctx* c, LogitsArgs& a, bool parts, hipStream_t s) {
   const unsigned grid = z2z_logits_fast_order(a, 0);
   if (!parts || !z2z_logits_fast_cuts(a) || ensure_partial(c, kSplitBytes, s) != Z2Z_OK) return grid;
-  a.split = reinterpret_cast<float*>(c->skinny_partial);
+  a.split = reinterpret_cast<float*>(c->partial_ws.p);
   return 256;
 }
 }  // namespace

@@ -889,28 +889,19 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
     // per row: the stream X and Y in fp32 (2 x 4 bytes x d), A, O (d), QKV (3d) and F (d_ff) in bf16
     return R_max * ((size_t)8 * d + ((size_t)2 * d + (size_t)3 * d + (size_t)dffp) * 2) + index_bytes;
   };
-  auto room = [&](size_t need) -> int {
-    if (need <= c->enc_ws_bytes) return Z2Z_OK;
-    Z2Z_TRY_GROW(s);
-    z2z_release(c, c->enc_ws);
-    c->enc_ws = nullptr;
-    c->enc_ws_bytes = 0;
-    if (!z2z_device_malloc(&c->enc_ws, need)) return Z2Z_ENOMEM;
-    c->enc_ws_bytes = need;
-    return Z2Z_OK;
-  };
+  auto room = [&](size_t need) -> int { return z2z_work_reserve(c, &c->enc_ws, need, s); };
   // (where the buffer cannot grow that far, or not at all under capture, passes of half as many rows.  What the device has refused is not asked
   // for again: every call would free the buffer that does)
   size_t need = layout(131072);
-  int rc = c->enc_ws_refused && need >= c->enc_ws_refused && need > c->enc_ws_bytes ? Z2Z_ENOMEM : room(need);
+  int rc = c->enc_ws_refused && need >= c->enc_ws_refused && need > c->enc_ws.bytes ? Z2Z_ENOMEM : room(need);
   if (rc != Z2Z_OK) {
     if (rc == Z2Z_ENOMEM) c->enc_ws_refused = need;
     need = layout(65536);
     rc = room(need);
   }
   if (rc != Z2Z_OK) return rc;
-  int32_t* index = reinterpret_cast<int32_t*>(c->enc_ws);
-  float* X = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(c->enc_ws) + index_bytes);
+  int32_t* index = reinterpret_cast<int32_t*>(c->enc_ws.p);
+  float* X = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(c->enc_ws.p) + index_bytes);
   float* Y = X + R_max * d;
   uint16_t* A = reinterpret_cast<uint16_t*>(Y + R_max * d);
   uint16_t* O = A + R_max * d;
@@ -1079,15 +1070,9 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
   // the rows a mode-1 call left are those of this encoder's shape only if the layout is the same
   if (mode == 2 && (!c->enc_kept || c->enc_kept_need != need || c->enc_kept_E != E)) return Z2Z_EINVAL;
   c->enc_kept = false;
-  if (need > c->enc_bwd_ws_bytes) {
-    Z2Z_TRY_GROW(s);
-    z2z_release(c, c->enc_bwd_ws);
-    c->enc_bwd_ws = nullptr;
-    c->enc_bwd_ws_bytes = 0;
-    if (!z2z_device_malloc(&c->enc_bwd_ws, need)) return Z2Z_ENOMEM;
-    c->enc_bwd_ws_bytes = need;
-  }
-  unsigned char* base = reinterpret_cast<unsigned char*>(c->enc_bwd_ws);
+  int rc = z2z_work_reserve(c, &c->enc_bwd_ws, need, s);
+  if (rc != Z2Z_OK) return rc;
+  unsigned char* base = reinterpret_cast<unsigned char*>(c->enc_bwd_ws.p);
   int32_t* index = reinterpret_cast<int32_t*>(base);
   float* dP = reinterpret_cast<float*>(base + index_bytes);
   float2* ln_stats = reinterpret_cast<float2*>(base + index_bytes + pos_bytes);
@@ -1158,7 +1143,6 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
     hipLaunchKernelGGL(enc_fill_kernel, dim3(64, (unsigned)zero.n), dim3(256), 0, s, zero);
   }
 
-  int rc;
 #define Z2Z_TRY_RC(expr)      \
   do {                        \
     rc = (expr);              \

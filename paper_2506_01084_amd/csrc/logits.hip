@@ -179,34 +179,25 @@ __global__ void __launch_bounds__(256) target_nll_kernel(const uint4* H, const u
   if (lane == 0) nll[r] = lse[r] - acc;
 }
 
+// Arrays of four-byte elements that share a work buffer evenly.
+size_t array_bytes(size_t elements) { return (elements * 4 + 255) / 256 * 256; }
+float* array_of(const z2z_work& w, int i, int n) { return reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(w.p) + w.bytes / n / 256 * 256 * i); }
+
 int ensure_sample_scratch(z2z_ctx* c, size_t need, hipStream_t s) {
-  if (need <= c->part_vl_capacity) return Z2Z_OK;
-  Z2Z_TRY_GROW(s);
-  z2z_release(c, c->part_v);
-  z2z_release(c, c->part_l);
-  c->part_v = nullptr;
-  c->part_l = nullptr;
-  c->part_vl_capacity = 0;
-  if (!z2z_device_malloc(&c->part_v, need * sizeof(float))) return Z2Z_ENOMEM;
-  if (!z2z_device_malloc(&c->part_l, need * sizeof(float))) return Z2Z_ENOMEM;
-  c->part_vl_capacity = need;
+  const int rc = z2z_work_reserve(c, &c->draws_ws, 2 * array_bytes(need), s);
+  if (rc != Z2Z_OK) return rc;
+  c->part_v = array_of(c->draws_ws, 0, 2);
+  c->part_l = array_of(c->draws_ws, 1, 2);
   return Z2Z_OK;
 }
 
 int ensure_scratch(z2z_ctx* c, size_t need, hipStream_t s) {
-  if (need <= c->part_capacity) return Z2Z_OK;
-  Z2Z_TRY_GROW(s);
-  z2z_release(c, c->part_m);
-  z2z_release(c, c->part_s);
-  z2z_release(c, c->part_i);
-  c->part_m = nullptr;
-  c->part_s = nullptr;
-  c->part_i = nullptr;
-  c->part_capacity = 0;
-  if (!z2z_device_malloc(&c->part_m, need * sizeof(float))) return Z2Z_ENOMEM;
-  if (!z2z_device_malloc(&c->part_s, need * sizeof(float))) return Z2Z_ENOMEM;
-  if (!z2z_device_malloc(&c->part_i, need * sizeof(int32_t))) return Z2Z_ENOMEM;
-  c->part_capacity = need;
+  const int rc = z2z_work_reserve(c, &c->parts_ws, 3 * array_bytes(need), s);
+  if (rc != Z2Z_OK) return rc;
+  c->part_m = array_of(c->parts_ws, 0, 3);
+  c->part_s = array_of(c->parts_ws, 1, 3);
+  c->part_i = reinterpret_cast<int32_t*>(array_of(c->parts_ws, 2, 3));
+  c->part_capacity = c->parts_ws.bytes / 3 / 256 * 64;
   return Z2Z_OK;
 }
 
@@ -566,19 +557,12 @@ int z2z_launch_extended_logits(z2z_ctx* c, const void* H, int32_t rows, int32_t 
 // Room for one row of logits per sequence, the row maxima and log-sum-exps.
 static int ensure_sample_logits(z2z_ctx* c, int32_t rows, hipStream_t s) {
   const size_t need = (size_t)rows * (size_t)(c->cfg.V + c->cfg.cap);
-  if (need > c->sample_logits_capacity) {
-    Z2Z_TRY_GROW(s);
-    z2z_release(c, c->sample_logits);
-    z2z_release(c, c->row_max);
-    c->sample_logits = nullptr;
-    c->row_max = nullptr;
-    c->sample_logits_capacity = 0;
-    if (!z2z_device_malloc(&c->sample_logits, need * sizeof(float))) return Z2Z_ENOMEM;
-    // the row maxima and log-sum-exps, followed by the selection kernels' scratch
-    if (!z2z_device_malloc(&c->row_max, (2 * (size_t)rows + z2z_sample_truncated_work_floats(rows)) * sizeof(float)))
-      return Z2Z_ENOMEM;
-    c->sample_logits_capacity = need;
-  }
+  // the row maxima and log-sum-exps, followed by the selection kernels' scratch
+  const size_t behind = 2 * (size_t)rows + z2z_sample_truncated_work_floats(rows);
+  const int rc = z2z_work_reserve(c, &c->sample_ws, array_bytes(need) + array_bytes(behind), s);
+  if (rc != Z2Z_OK) return rc;
+  c->sample_logits = reinterpret_cast<float*>(c->sample_ws.p);
+  c->row_max = c->sample_logits + array_bytes(need) / sizeof(float);
   return Z2Z_OK;
 }
 

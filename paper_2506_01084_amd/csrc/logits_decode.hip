@@ -918,16 +918,9 @@ int z2z_launch_linear_skinny(z2z_ctx* c, const void* A, const void* W, const flo
   if (ksplit > 1) {
     const size_t slots = (size_t)a.n_base_units * a.n_groups;
     const size_t need = slots * ksplit * D_LINEAR_UNIT * 64 * sizeof(float);
-    if (need > c->skinny_partial_bytes) {
-      Z2Z_TRY_GROW(s);
-      z2z_release(c, c->skinny_partial);
-      c->skinny_partial = nullptr;
-      c->skinny_partial_bytes = 0;
-      const size_t want_bytes = need > ((size_t)16 << 20) ? need : ((size_t)16 << 20);
-      if (!z2z_device_malloc(&c->skinny_partial, want_bytes)) return Z2Z_ENOMEM;
-      c->skinny_partial_bytes = want_bytes;
-    }
-    a.partial = reinterpret_cast<float*>(c->skinny_partial);
+    const int rc = z2z_work_reserve(c, &c->partial_ws, need, s, (size_t)16 << 20);
+    if (rc != Z2Z_OK) return rc;
+    a.partial = reinterpret_cast<float*>(c->partial_ws.p);
   }
   const unsigned grid = 8u * (unsigned)((a.n_base_units + 7) / 8) * (unsigned)(a.n_groups * ksplit);
   hipLaunchKernelGGL(logits_decode_kernel<3>, dim3(grid), dim3(D_THREADS), D_LDS, s, a);

@@ -121,15 +121,9 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   if (c->opt_backward_chunk > 0 && c->opt_backward_chunk < n_seq) n_seq = c->opt_backward_chunk;
   while (n_seq > 1 && layout(n_seq) > limit) n_seq = (n_seq + 1) / 2;
   if (layout(n_seq) > limit) return Z2Z_ENOMEM;      // one sequence alone does not fit
-  if (off > c->bwd_ws_bytes) {
-    Z2Z_TRY_GROW(s);
-    z2z_release(c, c->bwd_ws);
-    c->bwd_ws = nullptr;
-    c->bwd_ws_bytes = 0;
-    if (!z2z_device_malloc(&c->bwd_ws, off)) return Z2Z_ENOMEM;
-    c->bwd_ws_bytes = off;
-  }
-  unsigned char* ws = reinterpret_cast<unsigned char*>(c->bwd_ws);
+  int rc = z2z_work_reserve(c, &c->bwd_ws, off, s);
+  if (rc != Z2Z_OK) return rc;
+  unsigned char* ws = reinterpret_cast<unsigned char*>(c->bwd_ws.p);
   float* g = reinterpret_cast<float*>(ws + o_g);
   void *Pb = ws + o_Pb, *Ph = ws + o_Ph;
   // (nothing is folded over a strip here, and a workgroup's operand stream runs on from tile to tile anyway.  Tiles one by one, against
@@ -139,7 +133,6 @@ int z2z_launch_extended_nll_backward(z2z_ctx* c, const void* H, int32_t rows, in
   const uint16_t* H16 = reinterpret_cast<const uint16_t*>(H);
   const uint16_t* Wh16 = reinterpret_cast<const uint16_t*>(W_hyper);
 
-  int rc;
   if (teacher) {
     rc = z2z_launch_teacher_weight(c, *teacher, rows, rows_per_seq, lse, grad_nll, listed, s);
     if (rc == Z2Z_OK) rc = z2z_launch_listed(c, teacher->ids, rows, teacher->K, H, W_base, W_hyper, listed, s);

@@ -3,8 +3,10 @@
 #include "z2z_internal.h"
 
 #include <math.h>
-#include <new>
 #include <string.h>
+
+#include <algorithm>
+#include <new>
 
 #include "logits_common.h"
 #include "logits_mid.h"
@@ -23,20 +25,10 @@ void free_ctx(z2z_ctx* c) {
   (void)hipFree(c->st.ent_tokens);
   (void)hipFree(c->st.ent_len);
   (void)hipFree(c->st.slots);
-  (void)hipFree(c->part_m);
-  (void)hipFree(c->part_s);
-  (void)hipFree(c->part_i);
-  (void)hipFree(c->part_v);
-  (void)hipFree(c->part_l);
-  (void)hipFree(c->sample_logits);
-  (void)hipFree(c->row_max);
-  (void)hipFree(c->enc_ws);
-  (void)hipFree(c->enc_bwd_ws);
-  (void)hipFree(c->bwd_ws);
+  for (z2z_work* w : {&c->parts_ws, &c->draws_ws, &c->sample_ws, &c->enc_ws, &c->enc_bwd_ws, &c->bwd_ws, &c->partial_ws, &c->lookup_ws})
+    (void)hipFree(w->p);
   (void)hipFree(c->coef_dev);
   (void)hipFree(c->prune_prefix);
-  (void)hipFree(c->skinny_partial);
-  (void)hipFree(c->lookup_ws.p);
   while (c->kept) {
     z2z_kept* k = c->kept;
     c->kept = k->next;
@@ -55,15 +47,14 @@ void free_ctx(z2z_ctx* c) {
 // (beyond this range the fp32 exponents of the softmax lose what they are to tell apart)
 bool temperature_ok(float t) { return t >= 0.0625f && t <= 1024.0f; }
 
-// A call that uses work buffers is noted where it is captured into a graph (or may be: the runtime does not say).
+// At the start of every call that uses work buffers: whether it is captured into a graph (or may be: the runtime does not say).
 void note_capture(z2z_ctx* c, hipStream_t s) {
-  if (c->captured) return;
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
   if (hipStreamIsCapturing(s, &st) == hipSuccess) {
-    c->captured = st != hipStreamCaptureStatusNone;
+    c->capturing = st != hipStreamCaptureStatusNone;
   } else {
     (void)hipGetLastError();
-    c->captured = true;
+    c->capturing = true;
   }
 }
 
@@ -78,28 +69,44 @@ int enter(z2z_ctx* c, hipStream_t s) {
 
 }  // namespace
 
-void z2z_release(z2z_ctx* c, void* p) {
-  if (!p) return;
-  if (!c->captured) {
-    (void)hipFree(p);
-    return;
+int z2z_work_reserve(z2z_ctx* c, z2z_work* w, size_t bytes, hipStream_t s, size_t at_least) {
+  if (bytes <= w->bytes) {
+    w->named = w->named || c->capturing;
+    return Z2Z_OK;
   }
-  z2z_kept* k = new (std::nothrow) z2z_kept;
-  if (!k) return;                                    // (lost rather than pulled away under a graph)
-  k->p = p;
-  k->next = c->kept;
-  c->kept = k;
-}
-
-int z2z_work_reserve(z2z_ctx* c, z2z_work* w, size_t bytes, hipStream_t s) {
-  if (bytes <= w->bytes) return Z2Z_OK;
   Z2Z_TRY_GROW(s);
-  z2z_release(c, w->p);
+  size_t want = std::max(bytes, at_least);
+  if (w->named) {
+    // What a graph names stays until z2z_destroy, the new memory is nobody's yet.  By half at least: with every length captured before the next one
+    // asks for more, all that is kept is no more than twice the last buffer.
+    want = std::max(want, w->bytes + w->bytes / 2);
+    z2z_kept* k = new (std::nothrow) z2z_kept;
+    void* p = nullptr;
+    if (!k) return Z2Z_ENOMEM;
+    if (!z2z_device_malloc(&p, want) && !z2z_device_malloc(&p, want = bytes)) {
+      delete k;
+      return Z2Z_ENOMEM;
+    }
+    k->p = w->p;
+    k->next = c->kept;
+    c->kept = k;
+    w->p = p;
+    w->bytes = want;
+    w->named = c->capturing;
+    return Z2Z_OK;
+  }
+  const size_t was = w->bytes;
+  if (w->p) (void)hipFree(w->p);
   w->p = nullptr;
   w->bytes = 0;
-  if (!z2z_device_malloc(&w->p, bytes)) return Z2Z_ENOMEM;
-  w->bytes = bytes;
-  return Z2Z_OK;
+  if (z2z_device_malloc(&w->p, want)) {
+    w->bytes = want;
+    w->named = c->capturing;
+    return Z2Z_OK;
+  }
+  // (no room: smaller calls go on with what they had)
+  if (was > 0 && z2z_device_malloc(&w->p, was)) w->bytes = was;
+  return Z2Z_ENOMEM;
 }
 
 extern "C" {

@@ -52,9 +52,10 @@ struct z2z_fold {
 struct z2z_work {
   void* p;
   size_t bytes;
+  bool named;              // a call that uses it has been captured into a graph
 };
 
-// Work buffers that had to grow after a call was captured into a graph: the graph still names the old one.
+// Memory of work buffers that had to grow although a graph names it.
 struct z2z_kept {
   void* p;
   z2z_kept* next;
@@ -67,38 +68,35 @@ struct z2z_ctx {
   int num_cu;
   LzwState st;
   float coef[Z2Z_MAX_M + 1][Z2Z_MAX_M];   // coef[L][j]: pooling coefficient of token j of a length-L entry
-  // extended_logits scratch: partial (max, sum-exp, argmax) per (part, row)
+  // extended_logits scratch: partial (max, sum-exp, argmax) per (part, row), in parts_ws
+  z2z_work parts_ws;
   float* part_m;
   float* part_s;
   int32_t* part_i;
   size_t part_capacity;    // elements in each of the three arrays
-  // extended_sample scratch: best perturbed value and the scaled logit at that column (its column is part_i)
+  // extended_sample scratch: best perturbed value and the scaled logit at that column (its column is part_i), in draws_ws
+  z2z_work draws_ws;
   float* part_v;
   float* part_l;
-  size_t part_vl_capacity;
-  // truncated sampling: the rows' logits as the decode kernel stores them, and the row maxima
+  // truncated sampling: the rows' logits as the decode kernel stores them, and the row maxima, in sample_ws
+  z2z_work sample_ws;
   float* sample_logits;
   float* row_max;
-  size_t sample_logits_capacity;   // floats
   int trunc_ready;
   // hyper_encode work space: the activations of one pass (bf16)
-  void* enc_ws;
-  size_t enc_ws_bytes;
+  z2z_work enc_ws;
   size_t enc_ws_refused;   // 0, or a size the device had no room for
-  void* enc_bwd_ws;        // saved activations and gradients of the learned encoder's backward pass
-  size_t enc_bwd_ws_bytes;
+  z2z_work enc_bwd_ws;     // saved activations and gradients of the learned encoder's backward pass
   bool enc_kept;           // the work space holds the rows of a z2z_hyper_encode_keep call ...
   size_t enc_kept_need;    // ... laid out for this size ...
   const void* enc_kept_E;  // ... computed from this embedding matrix
-  void* bwd_ws;            // backward pass of the loss: dZ of both parts (bf16), the row gradients
-  size_t bwd_ws_bytes;
+  z2z_work bwd_ws;         // backward pass of the loss: dZ of both parts (bf16), the row gradients
   void* prune_prefix;      // codebook pruning: every entry's prefix entry (scratch, [B, cap] int32)
   void* coef_dev;          // the pooling coefficients on the device (pooling backward)
   // dense layers on few rows with K split over workgroups: the partial tiles
-  void* skinny_partial;
-  size_t skinny_partial_bytes;
+  z2z_work partial_ws;
   z2z_work lookup_ws;      // gradient of the code lookup: sorted positions, sums that cross pieces; a teacher's listed part
-  bool captured;           // a call that uses work buffers has been captured into a graph: none is freed from then on
+  bool capturing;          // the present call is being captured into a graph, or may be
   z2z_kept* kept;
   // options
   int opt_backward_chunk;
@@ -198,10 +196,9 @@ int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, c
 int z2z_launch_part_max(z2z_ctx* c, const float* logits, float* part_m, int* n_parts, hipStream_t s);   // parts of 256 columns
 int z2z_launch_codebook_reorder(z2z_ctx* c, int32_t beams, const int32_t* source, void* W_hyper, hipStream_t s);
 
-// A work buffer's memory is given back, or kept until z2z_destroy where a captured graph may still use it.
-void z2z_release(z2z_ctx* c, void* p);
-// At least `bytes` in the work buffer (Z2Z_ECAPTURE where it would have to grow under capture).
-int z2z_work_reserve(z2z_ctx* c, z2z_work* w, size_t bytes, hipStream_t s);
+// At least `bytes` in the work buffer, every time a call is about to use it (Z2Z_ECAPTURE where it would have to grow under capture, Z2Z_ENOMEM where
+// the device has no room: what was there is there still, or as much).  `at_least`: no less where it grows.
+int z2z_work_reserve(z2z_ctx* c, z2z_work* w, size_t bytes, hipStream_t s, size_t at_least = 0);
 
 // A work buffer that has to grow is freed and allocated again (hipFree / hipMalloc: the device synchronises that
 // once).  A stream capture does not survive that, so under capture the call is refused instead, before anything

@@ -53,3 +53,81 @@ for B, V, cap, d, dtype in ((1, 1000, 10, 4096, api.BF16), (4, 50000, 100, 64, a
         assert lib.z2z_destroy(h) == 0
 clean()
 """)
+
+
+CALLS = """
+V, cap, d = 4096, 100, 128
+enc = encoder(d)
+calls = dict(
+    logits=lambda h, n: lib.z2z_extended_logits(h, P, 4 * n, n, P, P, P, P, P, None, None),
+    nll_backward=lambda h, n: nll_backward(h, 4, n),
+    encode=lambda h, n: lib.z2z_hyper_encode(h, P, ctypes.byref(enc), P, None, n, None),
+    distill_backward=lambda h, n: lib.z2z_extended_distill_backward(h, P, 4 * n, n, P, P, 8, P, P, 2.0, P, P, P, P, P, P, None),
+    lookup_backward=lambda h, n: lib.z2z_embed_codes_backward(h, P, P, n, 1.0, P, 0, P, P, None))
+def make():
+    return context(B=4, V=V, M=3, cap=cap, d=d)
+def captured(call, h, n):
+    stub.stub_capturing(1)
+    rc = call(h, n)
+    stub.stub_capturing(0)
+    return rc
+"""
+
+
+def test_what_no_graph_names_is_given_back(without_a_device):
+    """A context with one captured step and eager calls of slowly growing length holds the step's buffers and the last lengths', not every length's."""
+    without_a_device(CALLS + """
+step = lambda h: lib.z2z_extended_logits(h, P, 4, 1, P, P, P, P, P, None, None)
+for name, call in calls.items():
+    h = make()
+    assert step(h) == 0 and captured(lambda h, n: step(h), h, 0) == 0
+    fixed = stub.stub_used()
+    for n in range(30, 100):
+        assert call(h, n) == 0, name
+    held = stub.stub_used() - fixed
+    fresh = make()
+    before = stub.stub_used()
+    assert call(fresh, 99) == 0
+    alone = stub.stub_used() - before
+    assert held <= 1.5 * alone, (name, held, alone)       # (a half more where the step's own buffer had to grow)
+clean()
+""")
+
+
+def test_a_refused_growth_leaves_what_there_was(without_a_device):
+    """... to the shape that fitted, eager and captured, however often the growth is refused; named by a graph or not."""
+    without_a_device(CALLS + """
+for name, call in calls.items():
+    for graph in (False, True):
+        h = make()
+        assert call(h, 40) == 0
+        if graph:
+            assert captured(call, h, 40) == 0
+        used = stub.stub_used()
+        stub.stub_capacity(used)
+        for _ in range(5):
+            rc = call(h, 90)
+            assert rc in (0, api.E_NOMEM), (name, rc)     # (0: the encoder's shorter passes, or nothing had to grow)
+            assert stub.stub_used() == used, (name, graph)
+            assert captured(call, h, 40) == 0, (name, graph)
+        stub.stub_capacity(1 << 40)
+        assert call(h, 90) == 0
+        clean()
+""")
+
+
+def test_graphs_of_every_length_keep_a_bounded_sum(without_a_device):
+    without_a_device(CALLS + """
+for name, call in calls.items():
+    h = make()
+    fixed = stub.stub_used()
+    for n in range(30, 100):                              # every length captured before the next one needs more
+        assert call(h, n) == 0 and captured(call, h, n) == 0, name
+    held = stub.stub_used() - fixed
+    fresh = make()
+    before = stub.stub_used()
+    assert call(fresh, 99) == 0
+    assert held <= 4.5 * (stub.stub_used() - before), name        # 1.5 of it, and twice that kept
+    assert lib.z2z_destroy(h) == 0
+clean()
+""")
