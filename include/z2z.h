@@ -37,6 +37,8 @@
  *     z2z_extended_logits_static, which never allocates.
  *     A work buffer that a captured call uses is not freed before z2z_destroy: where a later call needs a larger one, the old one
  *     is left to the graph.  A call that returns Z2Z_ENOMEM leaves the buffers at the size they had.
+ *   - An output overlaps no input and no other output of the call unless its entry point allows it (the calls do not look for that but where
+ *     they say so): workgroups read their inputs while others write.
  *   - Calls on one context must be issued from one host thread at a time, and work of one context
  *     must be ordered (same stream, or synchronised by the caller).
  *   - z2z_embed_codes, z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward, z2z_extended_beam and
@@ -209,8 +211,8 @@ int z2z_hyper_embed(z2z_ctx* ctx, const void* d_E, void* d_W_hyper, const int32_
  * the product in fp32, rounded once to the storage type (scale = 1: the row as it is).  A code that names no row gives a row of zeros
  * and sets BAD_CODE for its sequence; the others are unaffected.  Rows at and behind n_codes[b] are left as they were.
  *   d_codes [B, stride] int32, d_n_codes [B] or NULL (every row has `stride`);  scale finite (else Z2Z_EINVAL)
- *   d_E [V, d], d_W_hyper [B, cap, d], d_X [B, stride, d] out: dtype of the context;  d_status [B] int32 out (not the buffer of
- *   d_n_codes: Z2Z_EINVAL)
+ *   d_E [V, d], d_W_hyper [B, cap, d], d_X [B, stride, d] out: dtype of the context;  d_status [B] int32 out (not in the buffer
+ *   of d_n_codes: Z2Z_EINVAL)
  * One code per sequence (stride 1) is the input of a generation step. */
 int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, const void* d_E,
                     const void* d_W_hyper, float scale, void* d_X, int32_t* d_status, void* stream);
@@ -375,8 +377,8 @@ int z2z_extended_sample(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t row
  *   d_parent [B / beams, n_pick] int32 out: the beam, 0 .. beams - 1, that is continued
  *   d_code   [B / beams, n_pick] int32 out: by this base token or hypertoken (of the parent's codebook)
  *   d_picked [B / beams, n_pick] float out: the value above, the new beam's score
- *            (-1, -1 and -inf where fewer continuations are there); with n_pick = beams it may be the buffer of d_score
- *            (else Z2Z_EINVAL)
+ *            (-1, -1 and -inf where fewer continuations are there); with n_pick = beams it may be d_score, else it
+ *            may not overlap it (Z2Z_EINVAL)
  * n_pick may be larger than beams: the caller takes out finished sequences first.  A step goes on with z2z_codebook_reorder,
  * then z2z_step_update with the picked codes.
  * beams <= Z2Z_MAX_BEAMS and n_pick <= Z2Z_MAX_PICK, else Z2Z_EUNSUPPORTED; any storage type and width.  The logits go
@@ -441,7 +443,7 @@ int z2z_extended_nll_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32
  * T = 1 is z2z_extended_nll.
  *   d_ids [rows, K] int32; d_teacher [rows, K] float
  *   d_kl, d_lse [rows] float out; d_student [rows, K] float out: logit[r, ids_k] (not divided by T; 0 where no existing column is listed);
- *            not the teacher's buffer (Z2Z_EINVAL)
+ *            not d_teacher or d_ids (Z2Z_EINVAL)
  *   temperature between 1/16 and 1024 (else Z2Z_EINVAL); K <= Z2Z_MAX_TEACHER, else Z2Z_EUNSUPPORTED
  * Any shape and storage type z2z_extended_logits takes, and its work buffers. */
 #define Z2Z_MAX_TEACHER 256

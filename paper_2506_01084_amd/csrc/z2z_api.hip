@@ -15,6 +15,12 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Of n and m four-byte elements.
+bool overlap(const void* p, long long n, const void* q, long long m) {
+  const char *a = static_cast<const char*>(p), *b = static_cast<const char*>(q);
+  return a && b && a < b + 4 * m && b < a + 4 * n;
+}
+
 void free_ctx(z2z_ctx* c) {
   if (!c) return;
   (void)hipFree(c->st.size);
@@ -389,7 +395,7 @@ Z2Z_API int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t*
   if (!ctx || !d_E || !d_status || stride < 0) return Z2Z_EINVAL;
   if (stride > 0 && (!d_codes || !d_X)) return Z2Z_EINVAL;
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
-  if (d_status == d_n_codes) return Z2Z_EINVAL;      // (other workgroups read the lengths while the statuses are written)
+  if (overlap(d_status, ctx->cfg.B, d_n_codes, ctx->cfg.B)) return Z2Z_EINVAL;   // (other workgroups read the lengths while the statuses are written)
   if (!isfinite(scale)) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper) || !aligned16(d_X)) return Z2Z_EINVAL;
   const int rc = enter(ctx, static_cast<hipStream_t>(stream));
@@ -417,8 +423,9 @@ Z2Z_API int z2z_extended_beam(z2z_ctx* ctx, const void* d_H, int32_t rows, int32
   if (!ctx || !d_H || !d_W_base || !d_score || !d_parent || !d_code || !d_picked) return Z2Z_EINVAL;
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (rows != ctx->cfg.B || beams < 1 || rows % beams != 0 || n_pick < 1) return Z2Z_EINVAL;
-  if (d_picked == d_score && n_pick != beams) return Z2Z_EINVAL;     // (other prompts' scores would be written over)
   if (beams > Z2Z_MAX_BEAMS || n_pick > Z2Z_MAX_PICK) return Z2Z_EUNSUPPORTED;
+  if (overlap(d_score, rows, d_picked, (long long)(rows / beams) * n_pick) && (d_picked != d_score || n_pick != beams))
+    return Z2Z_EINVAL;                               // (other prompts' scores would be written over)
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   const int rc = enter(ctx, static_cast<hipStream_t>(stream));
   if (rc != Z2Z_OK) return rc;
@@ -471,7 +478,7 @@ Z2Z_API int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, in
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (rows_per_seq < 1 || rows < 1 || n_teacher < 1) return Z2Z_EINVAL;
   if ((long long)rows_per_seq * ctx->cfg.B != (long long)rows) return Z2Z_EINVAL;
-  if (d_student == d_teacher) return Z2Z_EINVAL;     // (written before the teacher is read)
+  if (d_student == d_teacher || (const void*)d_student == d_ids) return Z2Z_EINVAL;      // (written before the teacher is read)
   if (!temperature_ok(temperature)) return Z2Z_EINVAL;
   if (!aligned16(d_H) || !aligned16(d_W_base) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (n_teacher > Z2Z_MAX_TEACHER) return Z2Z_EUNSUPPORTED;
