@@ -418,7 +418,7 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* skey, uint32_t l
 // write zeros to the table rows that no position names: a wave per 16 rows.
 // Bound by HBM: dX read once, the gradients written once.  8 x 4096 positions of 24.6 k in use, V = 128256, d = 2048 (1.25 GB): zeros past the caches
 // where the gradients are larger than half of the memory-side one 280 -> 240 us (128 MB of them, V = 32000, d = 1000 fp32: 31 -> 38), these blocks
-// last 240 -> 237.
+// last 240 -> 237; row V - 1 in half of all positions 341 with its positions walked through by the wave that looks after it, 250 searched past.
 template <int KIND, int PIECE>
 __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   const int lane = threadIdx.x & 63;
@@ -428,14 +428,16 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   if (blockIdx.x >= sum_blocks) {
     const uint32_t first = a.fill_from + ((blockIdx.x - sum_blocks) * 4u + (threadIdx.x >> 6)) * 16u;
     uint32_t named = 0u;                             // a bit per row
-    for (uint32_t at = lower_bound(a.skey, 0u, a.n, first); at < a.n; at += 64u) {
+    for (uint32_t at = lower_bound(a.skey, 0u, a.n, first); at < a.n;) {
       const uint32_t k = at + lane < a.n ? a.skey[at + lane] : kNoKey;
       const uint32_t row = k - first;
       uint32_t bits = k >= first && row < 16u ? 1u << row : 0u;
 #pragma unroll
       for (int off = 32; off >= 1; off >>= 1) bits |= __shfl_xor(bits, off);
       named |= bits;
-      if ((uint32_t)__builtin_amdgcn_readlane((int)k, 63) - first >= 16u) break;
+      const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)k, 63);
+      if (last - first >= 16u) break;
+      at = lower_bound(a.skey, at + 64u, a.n, last + 1u);      // (a row that is named very often is left behind in a few steps)
     }
     for (int r = 0; r < 16; ++r) {
       if (((named >> r) & 1u) || first + (uint32_t)r >= a.sentinel) continue;
