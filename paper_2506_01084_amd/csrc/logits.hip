@@ -739,17 +739,22 @@ int z2z_launch_extended_sample(z2z_ctx* c, const void* H, int32_t rows, int32_t 
 
 // A beam step's hyper part in the streaming kernel's launch, tile by tile, instead of the decode kernel's units in one of their own: where all tiles
 // together take fewer rounds of a workgroup per CU than the parts apart, the hyper part at most five (more of them are the units', which
-// hold a sequence's one row in registers), and with up to 32 rows of up to 2 KB, whose workgroups are short and two to a CU.  Apart / together, us, whole calls,
+// hold a sequence's one row in registers), and with up to 32 rows of up to 2 KB, whose workgroups are short and two to a CU, however many there are.
+// Where the hyper part is several rounds of its own, eight places have to be left in the last one: a round that is as good as full is not saved.  Apart /
+// together, us, whole calls,
 // codebooks full: 4 rows, V = 8000, d = 512, 512 entries (63 and 16 tiles) 26.6 / 20.5; 32000 x 1024 x 512 (250 and 16, two to a CU) 36.5 / 33.7; 50257 x
 // 768 x 512 (197 and 8) 39.6 / 31.9; 80000 x 2048 x 1024 (313 and 16) 91 / 81; 136 rows of the last (313 and 544) 239 / 198.  Where no round
-// is saved: 4 rows, 128256 x 4096 x 1024 (501 and 16) 190 / 213, 80 rows, 32000 x 1024 x 3000 (250 and 1920) 121 / 155.
+// is saved: 4 rows, 128256 x 4096 x 1024 (501 and 16) 190 / 213, 80 rows, 32000 x 1024 x 3000 (250 and 1920) 121 / 155.  As good as full: 64 rows,
+// 16000 x 4096 x 256 (125 and 128) 83 / 63, x 2048 55 / 43, 16 rows, 16000 x 4096 x 1024 (125 and 128) 71 / 55; 80 rows of the last (125 and 640) 157 / 172.
+// Room for many entries, full / an eighth / a few of them: 32 rows, 32000 x 256 x 4096 (1024 tiles) 52, 48, 26 / 34, 22, 22, x 16384 (4096) 105, 57, 28 / 68,
+// 30, 24, x 65535 345, 74, 37 / 229, 63, 40; d = 1024 75, 69, 34 / 70, 35, 32, 191, 71, 36 / 209, 55, 33, 685, 123, 45 / 694, 128, 46.
 static bool hyper_along(const z2z_ctx* c, int rows) {
   if (c->cfg.cap <= 0) return false;
   const int columns = z2z_logits_mid_columns(c, c->cfg.V), cu = c->num_cu;
   const long long base = (c->cfg.V + columns - 1) / columns, hyper = (long long)rows * ((c->cfg.cap + columns - 1) / columns);
   auto rounds = [&](long long tiles) { return (tiles + cu - 1) / cu; };
   if (columns < 256 && rows <= 32 && c->cfg.d <= 1024) return true;
-  return rounds(hyper) <= 5 && rounds(base + hyper + 8) < rounds(base) + rounds(hyper);      // (a round of less than 8 is hardly saved)
+  return rounds(hyper) <= 5 && rounds(base + hyper + (hyper > cu ? 8 : 0)) < rounds(base) + rounds(hyper);
 }
 
 int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
