@@ -502,7 +502,9 @@ int z2z_launch_logits_mid(z2z_ctx* c, LogitsArgs a, const void* W, int w_rows, i
   // 160 rows: greedy V = 128256, d = 4096 196 / 177, 213 / 202, 227 / 203; V = 32000 55 / 51, 70 / 63, 71 / 63; V = 50257, d = 1024 30.6 /
   // 29.9, 36.8 / 33.8, 36.6 / 33.9; beams V = 80000, d = 4096 167 / 158, 203 / 192, 207 / 198; draws 183 / 173, 228 / 218, 231 / 219.
   // 1 block for up to 32 rows, of 2: beams of 4 rows V = 32000, d = 1024 38.6 / 36.6, d = 4096 74 / 69, V = 151936, d = 2048 140 / 134, V =
-  // 128256, d = 4096 192 / 190.  8 blocks, up to 256 rows, measured level with the tile kernel when weights still went through registers: 650 against 645 us for a decode
+  // 128256, d = 4096 192 / 190.  A few rows a sequence and dZ, the loss and its gradient: V = 128256, d = 4096, 4 x 5 rows 197 / 196, 735 / 727; 16 x 5
+  // 208 / 204, 876 / 871; 27 x 5 264 / 240, 1071 / 1049; 1 x 160 220 / 200, 927 / 914; V = 32000, d = 1024 35 / 34, 120 / 116; 37 / 36, 135 / 132; 42 / 40, 149 /
+  // 147; 31 / 29, 135 / 134; V = 50257, d = 768, 1 x 90 30 / 29, 133 / 135.  8 blocks, up to 256 rows, measured level with the tile kernel when weights still went through registers: 650 against 645 us for a decode
   // step of 256 sequences.)
   if (columns == M_WT)
     launch_mid<M_WAVES>(a, s);
