@@ -225,7 +225,7 @@ int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_cod
  *   flags  0: both gradients are overwritten, rows that no position names (and rows at and beyond C_b) with zeros;
  *          Z2Z_GRAD_ADD: added to what is there (rows that no position names are not touched), one rounding per element
  * With z2z_hyper_embed_backward behind it the gradient reaches E through the entries, too: that call adds to the same d_dE.
- * B * stride and V + B * cap below 2^31, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 18 bytes per position and d / 4 more, an eighth
+ * B * stride and V + B * cap below 2^31, 4 (V + B * cap) + 2 B * stride * ceil(d / 512) (fp32: d / 256) below 2^32 - 2^27, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 18 bytes per position and d / 4 more, an eighth
  * of dX's size (a sixteenth in fp32), or d more for the first 131072 / ceil(d / 512) positions (fp32: d / 256) if that is more.  A call makes room for
  * every call of fewer positions. */
 #define Z2Z_GRAD_ADD 1
@@ -381,7 +381,8 @@ int z2z_extended_sample(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t row
  *            may not overlap it (Z2Z_EINVAL)
  * n_pick may be larger than beams: the caller takes out finished sequences first.  A step goes on with z2z_codebook_reorder,
  * then z2z_step_update with the picked codes.
- * beams <= Z2Z_MAX_BEAMS and n_pick <= Z2Z_MAX_PICK, else Z2Z_EUNSUPPORTED; any storage type and width.  The logits go
+ * beams <= Z2Z_MAX_BEAMS, n_pick <= Z2Z_MAX_PICK, prompts below 2^22 and (fp32, widths of the general kernel) rows * (V + cap) below 2^34, else
+ * Z2Z_EUNSUPPORTED; any storage type and width.  The logits go
  * through rows * (V + cap) floats of library scratch. */
 #define Z2Z_MAX_BEAMS 32
 #define Z2Z_MAX_PICK 64
@@ -445,7 +446,7 @@ int z2z_extended_nll_backward(z2z_ctx* ctx, const void* d_H, int32_t rows, int32
  *   d_kl, d_lse [rows] float out; d_student [rows, K] float out: logit[r, ids_k] (not divided by T; 0 where no existing column is listed);
  *            not d_teacher or d_ids (Z2Z_EINVAL)
  *   temperature between 1/16 and 1024 (else Z2Z_EINVAL); K <= Z2Z_MAX_TEACHER, else Z2Z_EUNSUPPORTED
- * Any shape and storage type z2z_extended_logits takes, and its work buffers. */
+ * Any shape and storage type z2z_extended_logits takes, and its work buffers; rows below 2^26 / (min(ceil(K / 8), 8) + 4), else Z2Z_EUNSUPPORTED. */
 #define Z2Z_MAX_TEACHER 256
 int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq, const void* d_W_base,
                          const void* d_W_hyper, int32_t n_teacher, const int32_t* d_ids, const float* d_teacher,
@@ -459,7 +460,8 @@ int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t ro
  *   d_grad_kl          [rows] float or NULL (= 1 for every row)
  * dZ is rounded to bf16 where nothing is listed; the listed columns' values, nearly all of the gradient, stay fp32.  The gradients are sums of
  * products with both, in fp32, rounded once (dW_base once per pass where dZ takes more than 200 GB and the sequences go in several).  Types,
- * restrictions, errors and work space as for z2z_extended_nll_backward; besides, rows * K below 2^31 (else Z2Z_EUNSUPPORTED), and work space: 4 d
+ * restrictions, errors and work space as for z2z_extended_nll_backward; besides, rows * K and the joint tables as for
+ * positions of z2z_embed_codes_backward, rows * ceil(d / 512) below 2^26 - 2^12 (else Z2Z_EUNSUPPORTED), and work space: 4 d
  * bytes per hidden row, 4 d per listed column (V + B * cap of them at most), 4 per row of the joint tables, and 22 + d / 8 per listed column or d more
  * for the first 262144 / ceil(d / 512) of them if that is more.  Every hidden row has to be finite, as there: a NaN times
  * a gradient of zero is a NaN in the products. */

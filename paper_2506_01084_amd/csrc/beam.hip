@@ -286,7 +286,8 @@ struct ReorderArgs {
   const int32_t* source;    // [B], within the prompt
   u32x4* W;                 // [B, cap, d] or nullptr
   int32_t B, beams, chunks;
-  int32_t entry_blocks;     // blocks that move entries; then those of the hash tables, then one of the counts
+  long long first_entry;    // wave 0's, of prompts x cap
+  int32_t entry_blocks;     // blocks that move entries; then, in the last launch, those of the hash tables, then one of the counts
   int32_t table_blocks;
 };
 
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(256) reorder_kernel(ReorderArgs a) {
   const int prompts = a.B / a.beams;
   if ((int)blockIdx.x < a.entry_blocks) {
     const int lane = threadIdx.x & 63;
-    const long long wid = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long wid = a.first_entry + (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int prompt = (int)(wid / a.st.cap), e = (int)(wid % a.st.cap);
     if (prompt >= prompts) return;
     const int b0 = prompt * a.beams, M = a.st.M;
@@ -433,20 +434,26 @@ int z2z_launch_codebook_reorder(z2z_ctx* c, int32_t beams, const int32_t* source
   a.B = c->cfg.B;
   a.beams = beams;
   a.chunks = c->cfg.d / (c->cfg.dtype == Z2Z_BF16 ? 8 : 4);
-  const long long prompts = a.B / beams;
-  const long long entry_blocks = (prompts * c->cfg.cap + 3) / 4, table_blocks = (prompts * (c->st.nslots >> 1) + 255) / 256;
-  if (entry_blocks + table_blocks + 1 > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
-  a.entry_blocks = (int)entry_blocks;
-  a.table_blocks = (int)table_blocks;
-  const dim3 grid((unsigned)(entry_blocks + table_blocks + 1)), block(256);
-  if (beams <= 4)
-    hipLaunchKernelGGL(reorder_kernel<4>, grid, block, 0, s, a);
-  else if (beams <= 8)
-    hipLaunchKernelGGL(reorder_kernel<8>, grid, block, 0, s, a);
-  else if (beams <= 16)
-    hipLaunchKernelGGL(reorder_kernel<16>, grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL(reorder_kernel<32>, grid, block, 0, s, a);
+  const long long prompts = a.B / beams, entries = prompts * c->cfg.cap, table_blocks = (prompts * (c->st.nslots >> 1) + 255) / 256;
+  const long long most = kLaunchThreads / 256 - 1;                // blocks of a launch
+  if (table_blocks >= most) return Z2Z_EUNSUPPORTED;
+  // (one launch for up to 2^26 entries and tables; else entries ahead of it)
+  auto launch = [&](long long entry_blocks, bool last) {
+    a.entry_blocks = (int)entry_blocks;
+    a.table_blocks = last ? (int)table_blocks : 0;
+    const dim3 grid((unsigned)(entry_blocks + (last ? table_blocks + 1 : 0))), block(256);
+    if (beams <= 4)
+      hipLaunchKernelGGL(reorder_kernel<4>, grid, block, 0, s, a);
+    else if (beams <= 8)
+      hipLaunchKernelGGL(reorder_kernel<8>, grid, block, 0, s, a);
+    else if (beams <= 16)
+      hipLaunchKernelGGL(reorder_kernel<16>, grid, block, 0, s, a);
+    else
+      hipLaunchKernelGGL(reorder_kernel<32>, grid, block, 0, s, a);
+    a.first_entry += entry_blocks * 4;
+  };
+  while ((entries - a.first_entry + 3) / 4 + table_blocks > most) launch(std::min((entries - a.first_entry + 3) / 4, most), false);
+  launch((entries - a.first_entry + 3) / 4, true);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }

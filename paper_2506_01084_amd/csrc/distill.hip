@@ -269,6 +269,7 @@ int z2z_launch_extended_distill(z2z_ctx* c, const void* H, int32_t rows, int32_t
   // 147, 4096 486 / 508.
   const int gather = std::min((t.K + T_GROUP - 1) / T_GROUP, 8);
   const bool together = gather <= 5 || rows <= 512;
+  if ((long long)rows * 64 * (gather + 4) > kLaunchThreads) return Z2Z_EUNSUPPORTED;
   z2z_fold fold = {};
   const int rc = z2z_launch_extended_logits(c, H, rows, rows_per_seq, W_base, W_hyper, nullptr, nullptr, lse, nullptr, s, false, t.temperature,
                                             together ? &fold : nullptr);

@@ -47,15 +47,15 @@ __device__ __forceinline__ u32x4 scaled(u32x4 x, float scale) {
   return x;
 }
 
-// Blocks [0, B): the status of sequence b, all of its codes looked over.  The others: a wave per position and `split`-th of its
-// row.  Bound by HBM: the rows written and each named row read once (popular ones come out of the caches).  PAST: the rows go out past the
+// Blocks [0, status_blocks): the status of sequence b, all of its codes looked over.  The others: a wave per position and `split`-th of its
+// row, from number `first` on.  Bound by HBM: the rows written and each named row read once (popular ones come out of the caches).  PAST: the rows go out past the
 // caches, where they are more than half of the memory-side one (8 x 4096 positions, three quarters in use, d = 4096, 0.2 GB written and 0.18 read at
 // most: 65 -> 58 us with other rows before, 54 -> 48 over and over; the model finds fewer rows than that in the cache).
 template <bool BF16, bool PAST>
 __global__ void __launch_bounds__(256) embed_codes_kernel(LookupArgs a, const u32x4* E, const u32x4* W, u32x4* X, int32_t* status,
-                                                          float scale, int split) {
+                                                          float scale, int split, int status_blocks, long long first) {
   const int lane = threadIdx.x & 63;
-  if ((int)blockIdx.x < a.B) {
+  if ((int)blockIdx.x < status_blocks) {
     const int b = blockIdx.x, n = codes_of(a, b), columns = a.V + min(max(a.size[b], 0), a.cap);
     const int32_t* c = a.codes + (size_t)b * a.stride;
     bool bad = false;
@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(256) embed_codes_kernel(LookupArgs a, const u3
     if (threadIdx.x == 0) status[b] = any ? Z2Z_ST_BAD_CODE : Z2Z_ST_OK;
     return;
   }
-  const long long wid = (long long)(blockIdx.x - a.B) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long wid = first + (long long)(blockIdx.x - (unsigned)status_blocks) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long pos = wid / split;
   const int part = (int)(wid % split);
   if (pos >= (long long)a.B * a.stride) return;
@@ -595,20 +595,28 @@ int z2z_launch_embed_codes(z2z_ctx* c, const int32_t* codes, const int32_t* n_co
   const long long positions = (long long)a.B * stride;
   int split = 1;
   while (split < 16 && positions * split < 2048 && a.chunks > 64 * split) split *= 2;
-  const long long blocks = a.B + (positions * split + 3) / 4;
-  if (blocks > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
-  const dim3 grid((unsigned)blocks), block(256);
+  const dim3 block(256);
   const u32x4 *e = reinterpret_cast<const u32x4*>(E), *w = reinterpret_cast<const u32x4*>(W_hyper);
   u32x4* x = reinterpret_cast<u32x4*>(X);
   const bool past = (size_t)positions * a.chunks * 16 > kPastBytes;
-  if (c->cfg.dtype == Z2Z_BF16 && past)
-    hipLaunchKernelGGL((embed_codes_kernel<true, true>), grid, block, 0, s, a, e, w, x, status, scale, split);
-  else if (c->cfg.dtype == Z2Z_BF16)
-    hipLaunchKernelGGL((embed_codes_kernel<true, false>), grid, block, 0, s, a, e, w, x, status, scale, split);
-  else if (past)
-    hipLaunchKernelGGL((embed_codes_kernel<false, true>), grid, block, 0, s, a, e, w, x, status, scale, split);
-  else
-    hipLaunchKernelGGL((embed_codes_kernel<false, false>), grid, block, 0, s, a, e, w, x, status, scale, split);
+  // (one launch for up to 2^26 positions, with the statuses; then more: kLaunchThreads)
+  const long long waves = positions * split;
+  long long first = 0;
+  int status_blocks = a.B;
+  do {
+    const long long most = (kLaunchThreads / 256 - status_blocks) * 4, n = std::min(waves - first, most);
+    const dim3 grid((unsigned)(status_blocks + (n + 3) / 4));
+    if (c->cfg.dtype == Z2Z_BF16 && past)
+      hipLaunchKernelGGL((embed_codes_kernel<true, true>), grid, block, 0, s, a, e, w, x, status, scale, split, status_blocks, first);
+    else if (c->cfg.dtype == Z2Z_BF16)
+      hipLaunchKernelGGL((embed_codes_kernel<true, false>), grid, block, 0, s, a, e, w, x, status, scale, split, status_blocks, first);
+    else if (past)
+      hipLaunchKernelGGL((embed_codes_kernel<false, true>), grid, block, 0, s, a, e, w, x, status, scale, split, status_blocks, first);
+    else
+      hipLaunchKernelGGL((embed_codes_kernel<false, false>), grid, block, 0, s, a, e, w, x, status, scale, split, status_blocks, first);
+    first += n;
+    status_blocks = 0;
+  } while (first < waves);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
@@ -634,8 +642,8 @@ struct SumPlan {
 bool plan_sum(const z2z_ctx* c, long long positions, int kind, SumPlan* p) {
   const int slices = (c->cfg.d / (kind == LOOKUP_F32 ? 4 : 8) + 63) / 64;
   const long long keys = (long long)c->cfg.V + (long long)c->cfg.B * c->cfg.cap;
-  // (positions and rows of the joint table are 32-bit numbers here)
-  if (positions > 0x7FFFFFFFLL || keys > 0x7FFFFFFFLL) return false;
+  // (positions and rows of the joint table are 32-bit numbers here; reduce_kernel's blocks: 4 threads a row, 2 a position and slice)
+  if (positions > 0x7FFFFFFFLL || keys > 0x7FFFFFFFLL || 4 * keys + 2 * positions * slices + (1LL << 27) > kLaunchThreads) return false;
   p->n = (uint32_t)positions;
   int key_bits = 1;
   while ((keys >> key_bits) != 0) ++key_bits;        // (the sentinel is a key, too)
@@ -717,8 +725,7 @@ int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned
   g.joins = joins;
   g.fill_from = (uint32_t)(z.end / row16);
   g.fill_blocks = g.add ? 0 : (int)(((long long)a.sentinel - g.fill_from + 63) / 64);
-  const long long blocks = g.fill_blocks + ((long long)p.pieces * g.slices + 3) / 4;
-  if (blocks > 0x7FFFFFFFLL) return Z2Z_EUNSUPPORTED;
+  const long long blocks = g.fill_blocks + ((long long)p.pieces * g.slices + 3) / 4;      // (plan_sum)
   if (p.piece == kShortPiece)
     hipLaunchKernelGGL((reduce_kernel<KIND, kShortPiece>), dim3((unsigned)blocks), dim3(256), 0, s, g);
   else
@@ -761,7 +768,7 @@ struct ListedPlan {
 };
 
 bool plan_listed(const z2z_ctx* c, long long rows, int per_row, ListedPlan* p) {
-  if (!plan_sum(c, rows * per_row, WEIGHTED, &p->sum)) return false;
+  if (!plan_sum(c, rows * per_row, WEIGHTED, &p->sum) || rows * ((c->cfg.d + 511) / 512) * 64 + 1024 * 256 > kLaunchThreads) return false;
   const size_t n = p->sum.n, keys = (size_t)c->cfg.V + (size_t)c->cfg.B * c->cfg.cap, row = (size_t)c->cfg.d * sizeof(float);
   p->by_row = keys <= n;
   p->bytes = p->sum.bytes;

@@ -760,6 +760,8 @@ static bool hyper_along(const z2z_ctx* c, int rows) {
 int z2z_launch_extended_beam(z2z_ctx* c, const void* H, int32_t beams, const void* W_base, const void* W_hyper, const float* score,
                              int32_t picks, int32_t* parent, int32_t* code, float* picked, hipStream_t s) {
   const int rows = c->cfg.B;
+  const long long parts_of_256 = (c->cfg.V + 255) / 256 + (c->cfg.cap + 255) / 256;
+  if ((long long)(rows / beams) * 1024 > kLaunchThreads || (!c->decode_ready && rows * parts_of_256 * 64 + 192 > kLaunchThreads)) return Z2Z_EUNSUPPORTED;
   int n_parts = 0, base_columns = 256, hyper_columns = 256;
   int rc = ensure_scratch(c, step_parts(c) * rows, s);
   if (rc != Z2Z_OK) return rc;

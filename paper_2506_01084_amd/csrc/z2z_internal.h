@@ -214,6 +214,9 @@ inline int z2z_can_allocate(hipStream_t s) {
     if (_g != Z2Z_OK) return _g;               \
   } while (0)
 
+// A launch's threads are counted in 32 bits: beyond that the count wraps round, and fewer workgroups run, without an error.
+constexpr long long kLaunchThreads = 0xFFFFFFFFLL;
+
 // Device memory, or false.  A refusal is the call's to answer (another way, or Z2Z_ENOMEM): it does not stay behind as the runtime's last error,
 // which the next launch, the program's too, would report as its own.
 template <typename T>
