@@ -461,7 +461,7 @@ int z2z_extended_distill(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t ro
  * dZ is rounded to bf16 where nothing is listed; the listed columns' values, nearly all of the gradient, stay fp32.  The gradients are sums of
  * products with both, in fp32, rounded once (dW_base once per pass where dZ takes more than 200 GB and the sequences go in several).  Types,
  * restrictions, errors and work space as for z2z_extended_nll_backward; besides, rows * K and the joint tables as for
- * positions of z2z_embed_codes_backward, rows * ceil(d / 512) below 2^26 - 2^12 (else Z2Z_EUNSUPPORTED), and work space: 4 d
+ * positions of z2z_embed_codes_backward, rows * ceil(d / 512) below 2^26 - 2^12 (else Z2Z_EUNSUPPORTED), and work space: 4 d + 8
  * bytes per hidden row, 4 d per listed column (V + B * cap of them at most), 4 per row of the joint tables, and 22 + d / 8 per listed column or d more
  * for the first 262144 / ceil(d / 512) of them if that is more.  Every hidden row has to be finite, as there: a NaN times
  * a gradient of zero is a NaN in the products. */

@@ -519,7 +519,6 @@ __global__ void __launch_bounds__(256) reduce_kernel(GradArgs a) {
   }
 }
 
-// (8192 blocks at most; 2048 leave a teacher's lists, 524288 positions, at 92 us instead of 69.)
 // Runs over several pieces, each 256 features at a time: the four waves of a block add a quarter of the run's pieces each, in order, and the quarters
 // in order.
 template <int KIND>
@@ -730,6 +729,7 @@ int launch_sum(const z2z_ctx* c, const LookupArgs& a, const SumPlan& p, unsigned
     hipLaunchKernelGGL((reduce_kernel<KIND, kShortPiece>), dim3((unsigned)blocks), dim3(256), 0, s, g);
   else
     hipLaunchKernelGGL((reduce_kernel<KIND, KIND == WEIGHTED ? 64 : 32>), dim3((unsigned)blocks), dim3(256), 0, s, g);
+  // (8192 blocks at most: 2048 leave a teacher's lists, 524288 positions, at 92 us instead of 69)
   if (p.pieces > 1)
     hipLaunchKernelGGL(join_kernel<KIND>, dim3((unsigned)std::min<long long>((long long)p.pieces * ((c->cfg.d + 255) / 256), 8192)), dim3(256), 0, s, g);
   Z2Z_HIP_TRY(hipGetLastError());

@@ -51,6 +51,18 @@ for B, V, cap, d, dtype in ((1, 1000, 10, 4096, api.BF16), (4, 50000, 100, 64, a
         sums = max(positions * d / 4, min(positions, 131072 / slices) * d)
         assert got <= 18 * positions + sums + 8 * d + 4096, (B, d, n, got)
         assert lib.z2z_destroy(h) == 0
+for B, V, cap, d, K in ((1, 1000, 10, 4096, 64), (4, 50000, 100, 64, 3), (2, 5000, 300, 1024, 200)):
+    for rows in (1, 61, 1000, 20000):
+        nll, h = context(B=B, V=V, M=3, cap=cap, d=d), context(B=B, V=V, M=3, cap=cap, d=d)
+        before = stub.stub_used()
+        assert nll_backward(nll, B, rows) == 0
+        middle = stub.stub_used()
+        assert lib.z2z_extended_distill_backward(h, P, B * rows, rows, P, P, K, P, P, 2.0, P, P, P, P, P, P, None) == 0
+        got = (stub.stub_used() - middle) - (middle - before)
+        n, tables = B * rows * K, V + B * cap
+        sums = max(n * d / 8, min(n, 262144 / -(-d // 512)) * d)
+        assert got <= B * rows * (4 * d + 8) + min(n, tables) * 4 * d + 4 * tables + 22 * n + sums + 8 * d + 8192, (B, d, rows, got)
+        assert lib.z2z_destroy(nll) == 0 and lib.z2z_destroy(h) == 0
 clean()
 """)
 
