@@ -213,7 +213,7 @@ int z2z_hyper_embed(z2z_ctx* ctx, const void* d_E, void* d_W_hyper, const int32_
  *   d_codes [B, stride] int32, d_n_codes [B] or NULL (every row has `stride`);  scale finite (else Z2Z_EINVAL)
  *   d_E [V, d], d_W_hyper [B, cap, d], d_X [B, stride, d] out: dtype of the context;  d_status [B] int32 out (not in the buffer
  *   of d_n_codes: Z2Z_EINVAL)
- * One code per sequence (stride 1) is the input of a generation step. */
+ * One code per sequence (stride 1) is the input of a generation step.  B below 2^24 - 1, else Z2Z_EUNSUPPORTED. */
 int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, const void* d_E,
                     const void* d_W_hyper, float scale, void* d_X, int32_t* d_status, void* stream);
 

@@ -599,6 +599,7 @@ int z2z_launch_embed_codes(z2z_ctx* c, const int32_t* codes, const int32_t* n_co
   u32x4* x = reinterpret_cast<u32x4*>(X);
   const bool past = (size_t)positions * a.chunks * 16 > kPastBytes;
   // (one launch for up to 2^26 positions, with the statuses; then more: kLaunchThreads)
+  if (a.B >= kLaunchThreads / 256) return Z2Z_EUNSUPPORTED;
   const long long waves = positions * split;
   long long first = 0;
   int status_blocks = a.B;

@@ -14,6 +14,9 @@ for positions in (3, 3 << 20, (1 << 26) - 13, (1 << 26) - 12, 1 << 26, 3 << 25, 
     grids = named(launches(), "embed_codes")
     assert sum(grids) - 3 >= (3 * stride + 3) // 4 and all(g * 256 <= LIMIT for g in grids), (positions, grids)
     assert len(grids) == -(-(3 + (3 * stride + 3) // 4) // (LIMIT // 256)), (positions, grids)
+many = context(B=(1 << 24) - 1, V=100, M=2, cap=0, d=8)   # a workgroup each for the statuses
+assert lib.z2z_embed_codes(many, P, None, 1, P, None, 1.0, P, P, None) == api.E_UNSUPPORTED and launches() == []
+assert lib.z2z_destroy(many) == 0
 back = lambda c, stride: lib.z2z_embed_codes_backward(c, P, None, stride, 1.0, P, 0, P, P, None)
 wide = context(B=1, V=100, M=2, cap=10, d=4096)
 for c, B, slices, stride in ((h, 3, 1, 1000), (h, 3, 1, 600 << 20), (h, 3, 1, 670 << 20), (wide, 1, 8, 100 << 20), (wide, 1, 8, 500 << 20)):
