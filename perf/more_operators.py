@@ -78,17 +78,21 @@ def _normal(gen, shape, std, dtype=torch.bfloat16):
 
 
 def _to_four_bits(W, group):
-    """W [rows, cols] -> words [rows, cols / 8] int32 and scales [cols / group, rows] bf16."""
+    """W [rows, cols] -> words [rows / 16, blocks of 128 columns, 64, 4] int32 and scales [cols / group, rows] bf16.  Word m of lane 16 j + r
+    holds columns 32 m + 8 j .. of row r of its block; of eight, column 2 i is at bit 4 i, column 2 i + 1 at bit 16 + 4 i; 8 is zero."""
     rows, cols = W.shape
     w = W.float().reshape(rows, cols // group, group)
     scale = (w.abs().amax(dim=2) / 7).to(torch.bfloat16)
     q = torch.clamp(torch.round(w / scale.float()[:, :, None]), -8, 7).to(torch.int64) + 8
-    q = q.reshape(rows, cols // 8, 8)
-    word = torch.zeros((rows, cols // 8), dtype=torch.int64, device="cuda")
-    for i in range(4):                                 # column 2 i of eight at bit 4 i, column 2 i + 1 at bit 16 + 4 i
-        word |= q[:, :, 2 * i] << (4 * i) | q[:, :, 2 * i + 1] << (16 + 4 * i)
+    blocks = (cols + 127) // 128
+    padded = torch.full((rows, blocks * 128), 8, dtype=torch.int64, device="cuda")
+    padded[:, :cols] = q.reshape(rows, cols)
+    q = padded.reshape(rows // 16, 16, blocks, 4, 4, 8).permute(0, 2, 4, 1, 3, 5)      # tile, block, j, r, m, column of eight
+    word = torch.zeros(q.shape[:-1], dtype=torch.int64, device="cuda")
+    for i in range(4):
+        word |= q[..., 2 * i] << (4 * i) | q[..., 2 * i + 1] << (16 + 4 * i)
     word = torch.where(word >= 1 << 31, word - (1 << 32), word).int()
-    return word.contiguous(), scale.T.contiguous()
+    return word.reshape(rows // 16, blocks, 64, 4).contiguous(), scale.T.contiguous()
 
 
 def _shapes(case):
@@ -156,23 +160,25 @@ def _slope(x, kind):
     return 0.5 * (1 + torch.erf(x * math.sqrt(0.5))) + x * torch.exp(-0.5 * x * x) / math.sqrt(2 * math.pi)
 
 
-def _weights(W, scale):
+def _weights(W, scale, cols):
     """The matrix in 32 bits, out of 4 where there are scales."""
     if scale is None:
         return W.float()
-    rows, words = W.shape
+    tiles, blocks = W.shape[:2]
+    groups, rows = scale.shape
     bits = torch.tensor([0, 16, 4, 20, 8, 24, 12, 28], dtype=torch.int32, device="cuda")
-    q = (W[:, :, None] >> bits & 15).reshape(rows, scale.shape[0], -1)
-    return ((q - 8).float() * scale.T.float()[:, :, None]).reshape(rows, 8 * words)
+    q = W[:, :, :, :, None] >> bits & 15
+    q = q.reshape(tiles, blocks, 4, 16, 4, 8).permute(0, 3, 1, 4, 2, 5).reshape(rows, blocks * 128)
+    return ((q[:, :cols] - 8).float().reshape(rows, groups, -1) * scale.T.float()[:, :, None]).reshape(rows, cols)
 
 
 def _run_ffn(st):
     if own:
         st["ctx"].gated_ffn(st["X"], st["block"], st["Y"], residual=st["residual"])
         return st["Y"]
-    f, act = st["case"]["f"], st["case"]["act"]
-    GU = st["X"].float() @ _weights(st["W1"], st["scale1"]).T
-    Y = (_act(GU[:, :f], act) * GU[:, f:]) @ _weights(st["W2"], st["scale2"]).T
+    d, f, act = st["case"]["d"], st["case"]["f"], st["case"]["act"]
+    GU = st["X"].float() @ _weights(st["W1"], st["scale1"], d).T
+    Y = (_act(GU[:, :f], act) * GU[:, f:]) @ _weights(st["W2"], st["scale2"], f).T
     return (Y if st["residual"] is None else Y + st["residual"].float()).to(st["Y"].dtype)
 
 
@@ -219,15 +225,18 @@ def work(case):
 
 
 # ---- the definition in 64 bits --------------------------------------------------------------------------------------------------
-def _decoded(words, scale):
-    """4-bit weights in 64 bits, column by column of eight."""
-    s = scale.to(torch.float64).repeat_interleave(8 * words.shape[1] // scale.shape[0], dim=0).T
-    w = words.to(torch.int64)
-    W = torch.empty(s.shape, dtype=torch.float64, device="cuda")
-    for column in range(8):
-        nibble = (w >> (4 * (column // 2) + 16 * (column % 2))) & 15
-        W[:, column::8] = (nibble.to(torch.float64) - 8) * s[:, column::8]
-    return W
+def _decoded(words, scale, group):
+    """4-bit weights in 64 bits, one place in a word at a time."""
+    groups, rows = scale.shape
+    W = torch.zeros((rows, words.shape[1] * 128), dtype=torch.float64, device="cuda")
+    w = words.to(torch.int64).reshape(-1, words.shape[1], 4, 16, 4)
+    for j in range(4):
+        for m in range(4):
+            for column in range(8):
+                nibble = (w[:, :, j, :, m] >> (4 * (column // 2) + 16 * (column % 2))) & 15
+                W[:, 32 * m + 8 * j + column::128] = nibble.permute(0, 2, 1).reshape(rows, -1).to(torch.float64) - 8
+    W = W[:, :groups * group]
+    return W * scale.to(torch.float64).repeat_interleave(group, dim=0).T
 
 
 def exact(case, seed):
@@ -241,7 +250,7 @@ def exact(case, seed):
     d, f = case["d"], case["f"]
     X = st["X"].to(f64)
     if case["kind"] == "q4":
-        W1, W2 = _decoded(st["W1"], st["scale1"]), _decoded(st["W2"], st["scale2"])
+        W1, W2 = (_decoded(st[w], st[s], case["group"]) for w, s in (("W1", "scale1"), ("W2", "scale2")))
     else:
         W1, W2 = st["W1"].to(f64), st["W2"].to(f64)
     gate, up = X @ W1[:f].T, X @ W1[f:].T
