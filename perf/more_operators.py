@@ -77,20 +77,26 @@ def _normal(gen, shape, std, dtype=torch.bfloat16):
     return (torch.randn(shape, generator=gen, device="cuda") * std).to(dtype)
 
 
+FOUR_BITS = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0]
+
+
 def _to_four_bits(W, group):
     """W [rows, cols] -> words [rows / 16, blocks of 128 columns, 64, 4] int32 and scales [cols / group, rows] bf16.  Word m of lane 16 j + r
-    holds columns 32 m + 8 j .. of row r of its block; of eight, column 2 i is at bit 4 i, column 2 i + 1 at bit 16 + 4 i; 8 is zero."""
+    holds columns 32 m + 8 j .. of row r of its block, the first in its lowest four bits; weights are the scale times one of FOUR_BITS."""
     rows, cols = W.shape
     w = W.float().reshape(rows, cols // group, group)
-    scale = (w.abs().amax(dim=2) / 7).to(torch.bfloat16)
-    q = torch.clamp(torch.round(w / scale.float()[:, :, None]), -8, 7).to(torch.int64) + 8
+    scale = (w.abs().amax(dim=2) / 6).to(torch.bfloat16)
+    x = w / scale.float()[:, :, None]
+    y = x.abs()
+    code = (y > 0.25).int() + (y >= 0.75) + (y > 1.25) + (y >= 1.75) + (y > 2.5) + (y >= 3.5) + (y > 5)
+    code = torch.where((code > 0) & (x < 0), code + 8, code)
     blocks = (cols + 127) // 128
-    padded = torch.full((rows, blocks * 128), 8, dtype=torch.int64, device="cuda")
-    padded[:, :cols] = q.reshape(rows, cols)
+    padded = torch.zeros((rows, blocks * 128), dtype=torch.int64, device="cuda")
+    padded[:, :cols] = code.reshape(rows, cols)
     q = padded.reshape(rows // 16, 16, blocks, 4, 4, 8).permute(0, 2, 4, 1, 3, 5)      # tile, block, j, r, m, column of eight
     word = torch.zeros(q.shape[:-1], dtype=torch.int64, device="cuda")
-    for i in range(4):
-        word |= q[..., 2 * i] << (4 * i) | q[..., 2 * i + 1] << (16 + 4 * i)
+    for i in range(8):
+        word |= q[..., i] << (4 * i)
     word = torch.where(word >= 1 << 31, word - (1 << 32), word).int()
     return word.reshape(rows // 16, blocks, 64, 4).contiguous(), scale.T.contiguous()
 
@@ -166,10 +172,10 @@ def _weights(W, scale, cols):
         return W.float()
     tiles, blocks = W.shape[:2]
     groups, rows = scale.shape
-    bits = torch.tensor([0, 16, 4, 20, 8, 24, 12, 28], dtype=torch.int32, device="cuda")
-    q = W[:, :, :, :, None] >> bits & 15
+    q = W[:, :, :, :, None] >> torch.arange(0, 32, 4, dtype=torch.int32, device="cuda") & 15
     q = q.reshape(tiles, blocks, 4, 16, 4, 8).permute(0, 3, 1, 4, 2, 5).reshape(rows, blocks * 128)
-    return ((q[:, :cols] - 8).float().reshape(rows, groups, -1) * scale.T.float()[:, :, None]).reshape(rows, cols)
+    value = torch.tensor(FOUR_BITS, device="cuda")[q[:, :cols]]
+    return (value.reshape(rows, groups, -1) * scale.T.float()[:, :, None]).reshape(rows, cols)
 
 
 def _run_ffn(st):
@@ -233,8 +239,10 @@ def _decoded(words, scale, group):
     for j in range(4):
         for m in range(4):
             for column in range(8):
-                nibble = (w[:, :, j, :, m] >> (4 * (column // 2) + 16 * (column % 2))) & 15
-                W[:, 32 * m + 8 * j + column::128] = nibble.permute(0, 2, 1).reshape(rows, -1).to(torch.float64) - 8
+                code = ((w[:, :, j, :, m] >> (4 * column)) & 15).permute(0, 2, 1).reshape(rows, -1)
+                fraction, power = (code & 1).to(torch.float64), (code >> 1 & 3).to(torch.float64)
+                size = torch.where(power == 0, fraction / 2, (1 + fraction / 2) * torch.exp2(power - 1))
+                W[:, 32 * m + 8 * j + column::128] = torch.where(code >= 8, -size, size)
     W = W[:, :groups * group]
     return W * scale.to(torch.float64).repeat_interleave(group, dim=0).T
 
