@@ -13,6 +13,8 @@
  *   extended_distill the same against a teacher's top logits
  *   extended_beam    section 2.3 step 9 as a beam search's pick; codebook_reorder moves the beams' states after it
  *   embed_codes      section 2.2 (the input rows of a compressed sequence) and its gradient
+ *   gated_ffn        section 2.2 (a transformer layer's feed-forward block in its gated form) and its gradient; quantize_q4: its weights in 4 bits
+ *   clip_gradients   section 2.4 (training): the gradients' common norm, and their clipping
  *
  * Conventions
  *   - Every pointer named d_* is DEVICE memory owned by the caller; it must stay valid until the
@@ -41,8 +43,8 @@
  *     they say so): workgroups read their inputs while others write.
  *   - Calls on one context must be issued from one host thread at a time, and work of one context
  *     must be ordered (same stream, or synchronised by the caller).
- *   - z2z_embed_codes, z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward, z2z_extended_beam and
- *     z2z_codebook_reorder return Z2Z_EINVAL where the current device is not the one that the context was created on.
+ *   - z2z_embed_codes, z2z_embed_codes_backward, z2z_extended_distill, z2z_extended_distill_backward, z2z_extended_beam,
+ *     z2z_codebook_reorder, z2z_gated_ffn, z2z_gated_ffn_backward, z2z_quantize_q4 and z2z_clip_gradients return Z2Z_EINVAL where the current device is not the one that the context was created on.
  */
 #ifndef Z2Z_H
 #define Z2Z_H
@@ -231,6 +233,71 @@ int z2z_embed_codes(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_cod
 #define Z2Z_GRAD_ADD 1
 int z2z_embed_codes_backward(z2z_ctx* ctx, const int32_t* d_codes, const int32_t* d_n_codes, int32_t stride, float scale,
                              const void* d_dX, int32_t flags, float* d_dE, void* d_dW_hyper, void* stream);
+
+/* quantize_q4.  A bf16 matrix [rows, cols] in 4 bits, for z2z_gated_ffn and the learned encoder's gated layers: every run of `group` columns of a row has a scale,
+ *   scale = max |w| / 6 of the run, rounded to bf16;   v = the nearest to w / scale of 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign (e2m1; of two as near the one with
+ *   the even code);   the weight is then scale * v.  (scale = 0: v = 0.  A run that holds a NaN or an infinity has the scale NaN.)
+ *   d_q      [rows / 16, ceil(cols / 128), 64, 4] uint32 out: word m of lane 16 j + r holds columns 128 block + 32 m + 8 j ... + 7 of row 16 tile + r, the first in
+ *            its lowest four bits: 0 .. 7 for the values above in order, 8 more for the negative; columns behind the last are zeros
+ *   d_scale  [cols / group, rows] bf16 out
+ *   group    32, 64 or 128 (else Z2Z_EINVAL);  rows a multiple of 16, cols of 64 and of group (else Z2Z_EUNSUPPORTED).  Outputs overlap neither each other nor d_W (Z2Z_EINVAL).
+ * bf16 contexts; the context's width does not matter. */
+int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, int32_t group, void* d_q, void* d_scale, void* stream);
+
+/* gated_ffn.  The gated feed-forward block on rows of the context's width d, f = ffn->d_ff:
+ *   G = X w_1[0 .. f)^T,   U = X w_1[f .. 2 f)^T,   F = act(G) * U,   Y = F w_2^T + residual
+ *   act  Z2Z_ACT_SILU  x / (1 + e^-x);   Z2Z_ACT_GELU  x Phi(x), Phi the normal distribution (erf)
+ * F is rounded to bf16 once (the operand of a product), sums are fp32, Y is rounded once.
+ *   w_1 [2 f, d], w_2 [d, f]: bf16, group = 0; or in 4 bits as z2z_quantize_q4 writes them, group = 32, 64 or 128, with scale_1 [d / group, 2 f] and
+ *        scale_2 [f / group, d].  Up to 192 rows are multiplied by v, the scales with fp32 sums;
+ *        more rows by the weights rounded to bf16, which takes 6 d f bytes of work space.
+ *   d_X [rows, d], d_residual [rows, d] or NULL, d_Y [rows, d] out: bf16.  d_Y may be d_residual, else it overlaps neither input (Z2Z_EINVAL)
+ *   d_kept  [rows, 2 f] bf16 out or NULL: G | U for z2z_gated_ffn_backward (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
+ * A row's results do not depend on the other rows' values.  rows = 0 is a call that does nothing.  bf16 contexts, d and d_ff multiples of 64 (with 4 bits of group,
+ * too), rows <= 2^22, (d_ff + 128) d < 2^30, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and for few rows the parts of the products. */
+enum { Z2Z_ACT_SILU = 0, Z2Z_ACT_GELU = 1 };
+typedef struct z2z_ffn {
+  int32_t d_ff;
+  int32_t act;
+  int32_t group;        /* 0: bf16 weights; else 4 bits, columns per scale */
+  int32_t reserved;     /* 0 */
+  const void* w_1;      /* device pointers, 16-byte aligned, borrowed for the call */
+  const void* w_2;
+  const void* scale_1;  /* NULL for bf16 weights */
+  const void* scale_2;
+} z2z_ffn;
+int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, void* d_kept, void* stream);
+
+/* Backward of z2z_gated_ffn: the gradient of  L = sum dY * Y  with respect to the rows and both matrices (the residual's is dY itself),
+ *   dF = dY w_2;   dG = dF * U * act'(G),   dU = dF * act(G);   dX = [dG | dU] w_1;   dw_1 = [dG | dU]^T X;   dw_2 = dY^T F.
+ *   d_X, d_kept, ffn   of the forward call (bf16 weights, else Z2Z_EUNSUPPORTED)
+ *   d_dY [rows, d] bf16;  d_dX [rows, d] bf16 out, overwritten
+ *   grad   its w_1 and w_2 name the buffers that RECEIVE the gradients, bf16 (the call writes through them although they are declared const); its
+ *          other fields are not read.  flags = 0: overwritten (rows = 0: with zeros); Z2Z_GRAD_ADD: added to what is there, one rounding per element
+ * dG, dU and F are rounded to bf16 once, sums are fp32.  No output overlaps an input or another output (Z2Z_EINVAL).  Restrictions as for z2z_gated_ffn; work
+ * space: 6 f bytes per row. */
+int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_kept, const void* d_dY, void* d_dX,
+                           const z2z_ffn* grad, int32_t flags, void* stream);
+
+/* clip_gradients.  The common norm of n gradients, and their clipping by it:
+ *   norm = sqrt(sum over all tensors of all squares);   c = min(1, max_norm / norm);   out = c * data, rounded once
+ * (c = 1 where the norm is 0, an infinity or NaN: the gradients stay as they are, and d_norm says so.)
+ *   gradients  host array of n; a tensor is `n` contiguous elements of `dtype`, at any address that its type may have; n = 0 is an empty one.  out: data (in place),
+ *              another buffer of as many elements, or NULL (counts for the norm alone).  What is written overlaps no other tensor, nor d_norm
+ *              (Z2Z_EINVAL); the same tensor twice, in place, is that, too.
+ *   max_norm   >= 0, +inf: nothing is clipped (negative or NaN: Z2Z_EINVAL)
+ *   d_norm     [2] float out: norm (an infinity where it is beyond float; c is right all the same), c
+ * Sums are formed in a fixed order, in 64 bits from pieces of at most 64 squares in 32 (in 64 where those would leave their range): the same inputs give the same
+ * bits.  With out = data and c = 1 nothing is written.  Any context; n <= Z2Z_MAX_GRADIENTS, tensors of up to 2^44 elements, else Z2Z_EUNSUPPORTED. */
+#define Z2Z_MAX_GRADIENTS 4096
+typedef struct z2z_gradient {
+  const void* data;
+  void* out;
+  int64_t n;
+  int32_t dtype;        /* Z2Z_F32 or Z2Z_BF16 */
+  int32_t reserved;     /* 0 */
+} z2z_gradient;
+int z2z_clip_gradients(z2z_ctx* ctx, const z2z_gradient* gradients, int32_t n, float max_norm, float* d_norm, void* stream);
 
 /* hyper_encode: the learned hyper-encoder f_phi of section 2.2 (the attention and transformer rows of the
  * hyper-encoder ablation table; the training setup uses two transformer layers, M = 3).  The paper names the

@@ -36,4 +36,5 @@ from .loss import (extended_distill, extended_distill_backward, extended_nll, ex
 from .lookup import embed_codes, embed_codes_backward  # noqa: F401
 from .beam import beam_pick, beam_reorder, continuations  # noqa: F401
 from .encoder import hyper_encode, hyper_encode_backward  # noqa: F401
+from .ffn import clip, gated_ffn, gated_ffn_backward, q4_weights, q4_words, quantize_q4  # noqa: F401
 from .numfmt import bf16_bits_to_f64, f64_to_bf16_bits, to_f64, round_to_storage  # noqa: F401

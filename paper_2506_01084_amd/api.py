@@ -28,9 +28,11 @@ STATIC_PARTS = 1 << 22
 
 ENC_KEPT = 1
 GRAD_ADD = 1
-MAX_BEAMS, MAX_PICK, MAX_TEACHER = 32, 64, 256
+ACT_SILU, ACT_GELU = 0, 1
+MAX_BEAMS, MAX_PICK, MAX_TEACHER, MAX_GRADIENTS = 32, 64, 256, 4096
 EXPORTS = ["z2z_create", "z2z_destroy", "z2z_reset", "z2z_lzw_encode", "z2z_lzw_decode", "z2z_step_update", "z2z_lzw_rounds", "z2z_codebook", "z2z_codebook_prefill", "z2z_codebook_usage", "z2z_codebook_prune",
            "z2z_hyper_embed", "z2z_embed_codes", "z2z_embed_codes_backward", "z2z_extended_beam", "z2z_codebook_reorder", "z2z_hyper_encode", "z2z_hyper_encode_backward", "z2z_hyper_encode_keep", "z2z_extended_logits", "z2z_extended_logits_static", "z2z_extended_sample", "z2z_extended_nll", "z2z_extended_nll_backward", "z2z_extended_distill", "z2z_extended_distill_backward", "z2z_hyper_embed_backward", "z2z_set_option",
+           "z2z_gated_ffn", "z2z_gated_ffn_backward", "z2z_quantize_q4", "z2z_clip_gradients",
            "z2z_read_timing", "z2z_read_launches", "z2z_strerror"]
 
 
@@ -74,6 +76,69 @@ class Encoder:
         self.desc.attention_only = 1 if params["attention_only"] else 0
         self.desc.pos = _ptr(params.get("pos"), torch_dtype)
         self.desc.layers = ctypes.cast(self._arr, ctypes.POINTER(EncoderLayer))
+
+
+class FfnDesc(ctypes.Structure):
+    _fields_ = [("d_ff", c_int32), ("act", c_int32), ("group", c_int32), ("reserved", c_int32), ("w_1", c_void_p), ("w_2", c_void_p),
+                ("scale_1", c_void_p), ("scale_2", c_void_p)]
+
+
+def q4_shapes(rows: int, cols: int, group: int):
+    """Shapes of the words (int32) and the scales (bfloat16) of a [rows, cols] matrix in 4 bits."""
+    return (rows // 16, (cols + 127) // 128, 64, 4), (cols // group, rows)
+
+
+class GatedFFN:
+    """Device-resident weights of a gated feed-forward block: w_1 [2 d_ff, d] (gate rows first) and w_2 [d, d_ff], bfloat16; or both in 4 bits,
+    as Context.quantize_q4 writes them, with their scales.  act: "silu" or "gelu".  The object keeps the tensors alive."""
+
+    def __init__(self, w_1: torch.Tensor, w_2: torch.Tensor, act: str = "silu", scale_1: Optional[torch.Tensor] = None,
+                 scale_2: Optional[torch.Tensor] = None):
+        self.tensors = (w_1, w_2, scale_1, scale_2)
+        self.device = w_1.device
+        self.desc = FfnDesc()
+        self.desc.act = {"silu": ACT_SILU, "gelu": ACT_GELU}[act]
+        if any(t is not None and t.device != self.device for t in self.tensors):
+            raise ValueError("the weights of a block are on one device")
+        if scale_1 is None:
+            assert scale_2 is None and w_1.dim() == w_2.dim() == 2
+            self.d, self.d_ff = w_2.shape
+            assert tuple(w_1.shape) == (2 * self.d_ff, self.d)
+            self.desc.w_1, self.desc.w_2 = _ptr(w_1, torch.bfloat16), _ptr(w_2, torch.bfloat16)
+        else:
+            assert scale_2 is not None and scale_1.dim() == scale_2.dim() == 2
+            self.d, self.d_ff = scale_2.shape[1], scale_1.shape[1] // 2
+            assert scale_1.shape[0] > 0 and self.d % scale_1.shape[0] == 0
+            self.desc.group = self.d // scale_1.shape[0]
+            for w, scale, rows, cols in ((w_1, scale_1, 2 * self.d_ff, self.d), (w_2, scale_2, self.d, self.d_ff)):
+                assert (tuple(w.shape), tuple(scale.shape)) == q4_shapes(rows, cols, self.desc.group)
+            self.desc.w_1, self.desc.w_2 = _ptr(w_1, torch.int32), _ptr(w_2, torch.int32)
+            self.desc.scale_1, self.desc.scale_2 = _ptr(scale_1, torch.bfloat16), _ptr(scale_2, torch.bfloat16)
+        self.desc.d_ff = self.d_ff
+
+
+class GradientDesc(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("out", c_void_p), ("n", ctypes.c_int64), ("dtype", c_int32), ("reserved", c_int32)]
+
+
+class Gradients:
+    """A list of gradients for Context.clip_gradients, marshalled once: bfloat16 and float32 tensors, clipped in place, or into `out` (a tensor
+    of the same type and size, or None where a gradient counts for the norm alone, for each).  The object keeps the tensors alive."""
+
+    def __init__(self, tensors, out=None):
+        self.tensors = list(tensors)
+        self.out = self.tensors if out is None else list(out)
+        assert len(self.out) == len(self.tensors)
+        self.device = self.tensors[0].device if self.tensors else None
+        self.desc = (GradientDesc * max(len(self.tensors), 1))()
+        for desc, t, o in zip(self.desc, self.tensors, self.out):
+            if t.dtype not in (torch.bfloat16, torch.float32):
+                raise ValueError(f"expected dtype bfloat16 or float32, got {t.dtype}")
+            if t.device != self.device or (o is not None and o.device != self.device):
+                raise ValueError("the gradients of a list are on one device")
+            assert o is None or o.numel() == t.numel()
+            desc.data, desc.out, desc.n = _ptr(t), _ptr(o, t.dtype), t.numel()
+            desc.dtype = BF16 if t.dtype == torch.bfloat16 else F32
 
 
 _lib = None
@@ -128,6 +193,11 @@ def load_library() -> ctypes.CDLL:
     lib.z2z_extended_beam.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
                                       c_void_p, c_void_p]
     lib.z2z_codebook_reorder.argtypes = [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]
+    lib.z2z_gated_ffn.argtypes = [c_void_p, c_void_p, c_int32, POINTER(FfnDesc), c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.z2z_gated_ffn_backward.argtypes = [c_void_p, c_void_p, c_int32, POINTER(FfnDesc), c_void_p, c_void_p, c_void_p, POINTER(FfnDesc), c_int32,
+                                           c_void_p]
+    lib.z2z_quantize_q4.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
+    lib.z2z_clip_gradients.argtypes = [c_void_p, POINTER(GradientDesc), c_int32, c_float, c_void_p, c_void_p]
     lib.z2z_set_option.argtypes = [c_void_p, c_int32, c_int32]
     lib.z2z_read_timing.argtypes = [c_void_p, POINTER(c_float), P32]
     lib.z2z_read_launches.argtypes = [c_void_p, POINTER(ctypes.c_int64)]
@@ -355,6 +425,47 @@ class Context:
                                                    _ptr(dW_hyper, self.torch_dtype), byref(grad.desc),
                                                    _ptr(dE, torch.float32), ENC_KEPT if kept else 0, _stream()),
                "z2z_hyper_encode_backward")
+
+    def quantize_q4(self, W: torch.Tensor, group: int, q: torch.Tensor, scale: torch.Tensor) -> None:
+        """W [rows, cols] bfloat16 in 4 bits: q and scale, shaped as q4_shapes says."""
+        rows, cols = W.shape
+        assert (tuple(q.shape), tuple(scale.shape)) == q4_shapes(rows, cols, group)
+        _check(self._lib.z2z_quantize_q4(self._h, self._own(W, torch.bfloat16), rows, cols, int(group), self._own(q, torch.int32),
+                                         self._own(scale, torch.bfloat16), _stream()), "z2z_quantize_q4")
+
+    def _block(self, ffn: GatedFFN):
+        assert ffn.d == self.d
+        if ffn.device.index != self._device:
+            raise ValueError(f"expected weights on cuda:{self._device}, got some on {ffn.device}")
+        return byref(ffn.desc)
+
+    def gated_ffn(self, X: torch.Tensor, ffn: GatedFFN, Y: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                  kept: Optional[torch.Tensor] = None) -> None:
+        """Y = (act(X w_1[:f]^T) * (X w_1[f:]^T)) w_2^T + residual; kept [rows, 2 f]: what gated_ffn_backward needs of it."""
+        rows, d = X.shape
+        assert d == self.d and Y.shape == X.shape and (residual is None or residual.shape == X.shape)
+        assert kept is None or tuple(kept.shape) == (rows, 2 * ffn.d_ff)
+        own, kind = self._own, torch.bfloat16
+        _check(self._lib.z2z_gated_ffn(self._h, own(X, kind), rows, self._block(ffn), own(residual, kind), own(Y, kind), own(kept, kind), _stream()),
+               "z2z_gated_ffn")
+
+    def gated_ffn_backward(self, X: torch.Tensor, ffn: GatedFFN, kept: torch.Tensor, dY: torch.Tensor, dX: torch.Tensor, grad: GatedFFN,
+                           add: bool = False) -> None:
+        """The gradients of gated_ffn: dX, and those of the weights into grad's tensors, overwritten or (add=True) added to what is there."""
+        rows, d = X.shape
+        assert d == self.d and dY.shape == X.shape and dX.shape == X.shape and tuple(kept.shape) == (rows, 2 * ffn.d_ff)
+        assert (grad.d, grad.d_ff, grad.desc.group) == (ffn.d, ffn.d_ff, 0)
+        own, kind = self._own, torch.bfloat16
+        _check(self._lib.z2z_gated_ffn_backward(self._h, own(X, kind), rows, self._block(ffn), own(kept, kind), own(dY, kind), own(dX, kind),
+                                                self._block(grad), GRAD_ADD if add else 0, _stream()), "z2z_gated_ffn_backward")
+
+    def clip_gradients(self, gradients: Gradients, max_norm: float, norm: torch.Tensor) -> None:
+        """norm[0] = the gradients' common norm, norm[1] = c = min(1, max_norm / norm); each is multiplied by c."""
+        assert norm.numel() == 2
+        if gradients.device is not None and gradients.device.index != self._device:
+            raise ValueError(f"expected gradients on cuda:{self._device}, got some on {gradients.device}")
+        _check(self._lib.z2z_clip_gradients(self._h, gradients.desc, len(gradients.tensors), float(max_norm), self._own(norm, torch.float32),
+                                            _stream()), "z2z_clip_gradients")
 
     def _extended_logits(self, fn, what, H, rows_per_seq, W_base, W_hyper, argmax, mx, lse, logits) -> None:
         rows = H.shape[0]

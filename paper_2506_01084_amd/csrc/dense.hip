@@ -1,7 +1,7 @@
 // Dense layers out = act(A W^T + bias) + residual on the logits kernels (bf16): which kernel serves which row
 // count, the workgroup -> tile mapping of the tile kernel, and the sum of K-split partial tiles.  Used by the
 // learned hyper-encoder (zip2zip paper, section 2.2) and by the backward pass of the loss (section 2.4).
-#include "logits_common.h"
+#include "gated.h"
 #include "logits_mid.h"
 
 #include <string.h>
@@ -33,6 +33,30 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(const float* partial, i
   }
   const float4 b = bias ? *reinterpret_cast<const float4*>(bias + col) : float4{0.f, 0.f, 0.f, 0.f};
   finish_linear(x, b, act, residual, out, stream_f32, at);
+}
+
+// The first product of a gated block from its parts: one thread per run of 4 columns of F.
+__global__ void __launch_bounds__(256) gated_sum_kernel(const float* partial, int ksplit, int rows, const int32_t* rows_dev, int f, int act,
+                                                        uint16_t* F, uint16_t* kept) {
+  const int n4 = f >> 2;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int r_end = rows_dev ? min(rows, *rows_dev) : rows;
+  if (i >= (long long)r_end * n4) return;
+  const int row = (int)(i / n4), col = (int)(i % n4) * 4;
+  const size_t at = (size_t)row * 2 * f + col, plane = (size_t)rows * 2 * f;
+  float4 g = *reinterpret_cast<const float4*>(partial + at), u = *reinterpret_cast<const float4*>(partial + at + f);
+#pragma unroll 4
+  for (int k = 1; k < ksplit; ++k) {
+    const float4 x = *reinterpret_cast<const float4*>(partial + k * plane + at), y = *reinterpret_cast<const float4*>(partial + k * plane + at + f);
+    g = float4{g.x + x.x, g.y + x.y, g.z + x.z, g.w + x.w};
+    u = float4{u.x + y.x, u.y + y.y, u.z + y.z, u.w + y.w};
+  }
+  const float gv[4] = {g.x, g.y, g.z, g.w}, uv[4] = {u.x, u.y, u.z, u.w};
+  *reinterpret_cast<uint2*>(F + (size_t)row * f + col) = z2z_gated::hidden4(gv, uv, act);
+  if (kept) {
+    *reinterpret_cast<uint2*>(kept + at) = z2z_gated::pack4(gv);
+    *reinterpret_cast<uint2*>(kept + at + f) = z2z_gated::pack4(uv);
+  }
 }
 
 // The partial tiles' buffer, at least `need` bytes of it.
@@ -218,4 +242,83 @@ int z2z_launch_linear_weight(z2z_ctx* c, const void* A, int lda, const void* W, 
   a.d = (k_rows + 63) / 64 * 64;
   a.k_dev = k_dev;
   return launch_kmajor(c, a, true, A, lda, W, ldw, k_rows, residual, out, N, R, N, batch, s);
+}
+
+int z2z_partial_reserve(z2z_ctx* c, size_t bytes, float** p, hipStream_t s) {
+  const int rc = ensure_partial(c, bytes, s);
+  *p = reinterpret_cast<float*>(c->partial_ws.p);
+  return rc;
+}
+
+int z2z_launch_linear_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int N, const void* residual, void* out, bool stream_f32,
+                          hipStream_t s) {
+  const long long n_threads = (long long)R * (N / 4);
+  hipLaunchKernelGGL(linear_sum_kernel, dim3((unsigned)((n_threads + 255) / 256)), dim3(256), 0, s, partial, ksplit, R, rows_dev, N, nullptr, 0,
+                     residual, out, stream_f32 ? 1 : 0);
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}
+
+int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, void* kept, hipStream_t s) {
+  const long long n_threads = (long long)R * (d_ff / 4);
+  hipLaunchKernelGGL(gated_sum_kernel, dim3((unsigned)((n_threads + 255) / 256)), dim3(256), 0, s, partial, ksplit, R, rows_dev, d_ff, act,
+                     reinterpret_cast<uint16_t*>(F), reinterpret_cast<uint16_t*>(kept));
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}
+
+namespace {
+
+// What the gated block's tile launches share.
+LogitsArgs gated_args(const void* H, const void* W, int act, void* F, const void* kept, int R, const int32_t* rows_dev, int d_ff, int n_columns, int K) {
+  LogitsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.H = H;
+  a.W = W;
+  a.rows = R;
+  a.rows_per_seq = R;
+  a.d = K;
+  a.w_rows = n_columns;
+  a.n_vtiles = (n_columns + 255) / 256;
+  a.row_tiles = (R + 255) / 256;
+  a.strip = 1;
+  a.n_strips = a.n_vtiles;
+  a.out = F;
+  a.ldo = d_ff;
+  a.rows_dev = rows_dev;
+  a.gated.kept = const_cast<void*>(kept);
+  a.gated.d_ff = d_ff;
+  a.gated.act = act;
+  return a;
+}
+
+}  // namespace
+
+int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K,
+                            hipStream_t s, bool once) {
+  const bool tile_parts = R > 256 && K / 64 >= kSplitSlabs;
+  if (!tile_parts) {
+    const float* partial = nullptr;
+    int ksplit = 0;
+    const int rc = z2z_launch_linear_parts(c, X, W, R, rows_dev, 2 * d_ff, K, &partial, &ksplit, s, once);
+    if (rc != Z2Z_OK) return rc;
+    if (ksplit > 0) return z2z_launch_gated_sum(partial, ksplit, R, rows_dev, d_ff, act, F, kept, s);
+  }
+  if (!c->fast_ready || K % 64 != 0 || d_ff % 64 != 0 || R < 1) return Z2Z_EUNSUPPORTED;
+  LogitsArgs a = gated_args(X, W, act, F, kept, R, rows_dev, d_ff, 2 * d_ff, K);
+  const unsigned grid = order_dense(c, a, tile_parts, s);
+  return z2z_launch_gated_tile(a, false, grid, s);
+}
+
+int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, int act, void* slopes, void* F, int R, const int32_t* rows_dev,
+                            int d_ff, int K, hipStream_t s) {
+  if (!c->fast_ready || K % 64 != 0 || d_ff % 64 != 0 || R < 1) return Z2Z_EUNSUPPORTED;
+  LogitsArgs a = gated_args(dY, W, act, F, kept, R, rows_dev, d_ff, d_ff, K);
+  a.ldh = K;
+  a.ldw = d_ff;
+  a.k_rows = K;
+  a.batch = 1;
+  a.gated.slopes = slopes;
+  const unsigned grid = order_dense(c, a, K / 64 >= kSplitSlabs, s);
+  return z2z_launch_gated_tile(a, true, grid, s);
 }

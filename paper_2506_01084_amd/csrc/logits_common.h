@@ -321,6 +321,13 @@ struct LogitsArgs {
     void* out;
     int32_t ldo, cap, col0, strip, n_strips, part0, row_tiles, n_work, n_seq;
   } hyper;
+  // gated feed-forward block (tile kernel, GATE 1 and 2).  Forward: W holds d_ff gate rows, then d_ff rows of the other projection (w_rows = 2 d_ff),
+  // out = F [rows, d_ff], kept = nullptr or where G | U go, [rows, 2 d_ff].  Backward: the product is dF, out = F, kept = the forward pass's G | U,
+  // slopes = dG | dU.  All bf16.
+  struct {
+    void *kept, *slopes;
+    int32_t d_ff, act;
+  } gated;
 };
 
 inline void set_softmax_temperature(LogitsArgs& a, float temperature) {
@@ -485,6 +492,8 @@ int z2z_launch_linear_kmajor(const z2z_logits::LogitsArgs& a, bool rows_too, uns
 bool z2z_logits_fast_cuts(const z2z_logits::LogitsArgs& a);
 // behind a dense layer launched with LogitsArgs::split, on 256 workgroups: the sums of the tiles that the device has cut along K
 int z2z_launch_tile_sum(const z2z_logits::LogitsArgs& a, hipStream_t s);
+// mode 2 with the epilogue of a gated block's first product or, K-major W, of its gradient (LogitsArgs::gated), and the sums of cut tiles behind it
+int z2z_launch_gated_tile(const z2z_logits::LogitsArgs& a, bool backward, unsigned grid, hipStream_t s);
 // order and grid of a base part or dense layer (modes 0, 2, 3, 6 - 9): a.row_tiles, n_vtiles and n_strips are set; `forced`:
 // Z2Z_OPT_LOGITS_MAP, 0 for the automatic order
 unsigned z2z_logits_fast_order(z2z_logits::LogitsArgs& a, int forced);
@@ -531,6 +540,20 @@ bool z2z_linear_takes_pitch(const z2z_ctx* c, int R, int N, int K);
 // the layer is not split at this shape, nothing was launched.
 int z2z_launch_linear_parts(z2z_ctx* c, const void* A, const void* W, int R, const int32_t* rows_dev, int N, int K,
                             const float** partial, int* ksplit, hipStream_t s, bool once = false);
+// The gated block's own products (bf16; K a multiple of 64, d_ff of 64):
+//   z2z_launch_gated_hidden   F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff], and, where kept is given, the two products beside each other, [R, 2 d_ff]
+//   z2z_launch_gated_sum      the same from fp32 parts [ksplit][R][2 d_ff] of the products
+//   z2z_launch_gated_slopes   dF = dY W, W [K, d_ff], as dG | dU [R, 2 d_ff], and F once more
+int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K,
+                            hipStream_t s, bool once = false);
+int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, void* kept, hipStream_t s);
+int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, int act, void* slopes, void* F, int R, const int32_t* rows_dev,
+                            int d_ff, int K, hipStream_t s);
+// out = sum of fp32 parts [ksplit][R][N] + residual, bf16 (stream_f32: fp32)
+int z2z_launch_linear_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int N, const void* residual, void* out, bool stream_f32,
+                          hipStream_t s);
+// At least `bytes` where parts go (z2z_launch_linear_parts uses the same).
+int z2z_partial_reserve(z2z_ctx* c, size_t bytes, float** p, hipStream_t s);
 int z2z_logits_fast_prepare(z2z_ctx* c);
 int z2z_logits_fast_sequences();   // most sequences whose hyper part a launch of the tile kernel takes along
 // One launch of the bf16 MFMA tile kernel over the base part (hyper = false), over the hyper part of n_seq sequences, or over both

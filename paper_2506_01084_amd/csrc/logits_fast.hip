@@ -41,7 +41,7 @@
 // In the 16 x 16 result block a lane holds 4 vocabulary entries of one hidden row (of 8 rows and 32 entries each in the
 // whole tile), so the running (max, sum-exp, argmax) of the joint softmax (zip2zip paper, section 2.3, step 8) lives in
 // registers and crosses lanes once per strip.
-#include "logits_common.h"
+#include "gated.h"
 
 #include <utility>
 
@@ -727,6 +727,83 @@ __device__ __forceinline__ void store_prob16(const Acc& acc, const LogitsArgs& a
   }
 }
 
+// Store one finished tile of a gated block's first product: blocks of 16 gate columns and of the same 16 columns of the other projection alternate
+// (see gated_offset), so that a lane holds both of an element.  col_base: of the tile's 128 columns of F.
+__device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& a, int row_base, int r_end, int col_base) {
+  const int lane15 = threadIdx.x & 15, f = a.gated.d_ff;
+#pragma unroll
+  for (int j = 0; j < F_N; ++j) {
+    const int row = row_base + j * 16 + lane15;
+    const bool row_ok = row < r_end;
+    uint2 h[F_N / 2], g[F_N / 2], u[F_N / 2];
+#pragma unroll
+    for (int k = 0; k < F_N / 2; ++k) {
+      float gv[4], uv[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        gv[e] = read_acc(acc[2 * k][j][e]);
+        uv[e] = read_acc(acc[2 * k + 1][j][e]);
+      }
+      h[k] = z2z_gated::hidden4(gv, uv, a.gated.act);
+      g[k] = z2z_gated::pack4(gv);
+      u[k] = z2z_gated::pack4(uv);
+    }
+    uint16_t* out_row = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo;
+#pragma unroll
+    for (int k = 0; k < F_N / 2; k += 2) store_two_blocks(out_row, row_ok, col_base, k, h[k], h[k + 1], f);
+    if (a.gated.kept) {
+      uint16_t* kept = reinterpret_cast<uint16_t*>(a.gated.kept) + (size_t)row * 2 * f;
+#pragma unroll
+      for (int k = 0; k < F_N / 2; k += 2) {
+        store_two_blocks(kept, row_ok, col_base, k, g[k], g[k + 1], f);
+        store_two_blocks(kept + f, row_ok, col_base, k, u[k], u[k + 1], f);
+      }
+    }
+  }
+}
+
+// Store one finished tile of dF = dY W2 as the gated block's gradients dG | dU, and F beside them for dW2.  G and U of the next 16 rows are asked for ahead
+// of the arithmetic on these; the scheduling barriers keep the pieces apart (without them 1 KB a lane is spilled).
+__device__ __forceinline__ void store_gated_slopes16(const Acc& acc, const LogitsArgs& a, int row_base, int r_end, int col_base) {
+  const int lane15 = threadIdx.x & 15, f = a.gated.d_ff;
+  uint2 g[2][F_N], u[2][F_N];
+  auto load = [&](int j, uint2 (&gj)[F_N], uint2 (&uj)[F_N]) __attribute__((always_inline)) {
+    const int row = row_base + j * 16 + lane15;
+    const uint16_t* kept = reinterpret_cast<const uint16_t*>(a.gated.kept) + (size_t)min(row, r_end - 1) * 2 * f;
+#pragma unroll
+    for (int i = 0; i < F_N; ++i) {
+      const int col = min(col_base + i * 16, f - 4);
+      gj[i] = *reinterpret_cast<const uint2*>(kept + col);
+      uj[i] = *reinterpret_cast<const uint2*>(kept + f + col);
+    }
+  };
+  load(0, g[0], u[0]);
+#pragma unroll
+  for (int j = 0; j < F_N; ++j) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (j + 1 < F_N) load(j + 1, g[(j + 1) & 1], u[(j + 1) & 1]);
+    const int row = row_base + j * 16 + lane15;
+    const bool row_ok = row < r_end;
+    uint16_t* out_row = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo;
+    uint16_t* slopes = reinterpret_cast<uint16_t*>(a.gated.slopes) + (size_t)row * 2 * f;
+#pragma unroll
+    for (int i = 0; i < F_N; i += 2) {
+      __builtin_amdgcn_sched_barrier(0);
+      z2z_gated::Slopes4 s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float df[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) df[e] = read_acc(acc[i + h][j][e]);
+        s[h] = z2z_gated::slopes4(df, g[j & 1][i + h], u[j & 1][i + h], a.gated.act);
+      }
+      store_two_blocks(slopes, row_ok, col_base, i, s[0].dg, s[1].dg, f);
+      store_two_blocks(slopes + f, row_ok, col_base, i, s[0].du, s[1].du, f);
+      store_two_blocks(out_row, row_ok, col_base, i, s[0].f, s[1].f, f);
+    }
+  }
+}
+
 // Lanes that hold the same rows, 16 or 32 apart, exchange halves: of a[k] and a[k + N] the lower lane of a pair keeps row k
 // and the upper one row k + N, each with both lanes' values.
 struct Swap16 {
@@ -789,12 +866,14 @@ __device__ __forceinline__ void merge_rows(R (&a)[F_N], S swap, float inv_t = 1.
 // TEMP (modes 0, 1 and 3): the softmax has a temperature.  (Instances of their own: with 1 / T and log2(e) / T read from the arguments in every call,
 // which costs two more scalar registers, 32768 rows x 128256 at T = 1 took 23.82 ms instead of 23.66.)
 // SUM (K-major products): one term of a sum (store_sum16); by rows where H is K-major too.
-template <int MODE, bool ROT = false, bool TW = false, bool TH = false, bool HYP = false, bool TEMP = false, bool SUM = false>
+// GATE (mode 2): 1 = the first product of a gated block, both projections of 128 columns in a tile (store_gated16); 2 = its gradient's, dF (TW).
+template <int MODE, bool ROT = false, bool TW = false, bool TH = false, bool HYP = false, bool TEMP = false, bool SUM = false, int GATE = 0>
 __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   static_assert((MODE == 2 || !TW) && (TW || !TH), "dense layers only, and H K-major only where W is");
   static_assert(!HYP || MODE == 0 || (MODE == 3 && !ROT), "");
   static_assert(!TEMP || MODE == 0 || MODE == 1 || MODE == 3, "");
   static_assert(!SUM || TW, "");
+  static_assert(GATE == 0 || (MODE == 2 && !TH && !SUM && TW == (GATE == 2)), "");
   const float inv_t = TEMP ? a.inv_t : 1.f, log2e_t = TEMP ? a.log2e_t : 1.4426950408889634f;
   constexpr bool PROBE_NOREQ = MODE == 8 || MODE == 9;
   constexpr bool PROBE_MFMA = MODE == 9;
@@ -981,6 +1060,14 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
     const int chunk16 = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
     return (uint32_t)(min(row, lim) * (int)pitch + chunk16);
   };
+  // (first product of a gated block: the tile's blocks of 16 rows alternate between the d_ff gate rows and the other projection's, which lie behind
+  // them; rows past the last are clamped onto it in either)
+  auto gated_offset = [&](int i, int lim) -> uint32_t {
+    const int row = (wave * F_PAIRS + i) * 8 + ld_row;
+    const int chunk16 = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    const int of = min((row >> 5) * 16 + (row & 15), lim) + ((row >> 4) & 1) * a.gated.d_ff;
+    return (uint32_t)of * (uint32_t)pitch_w + (uint32_t)chunk16;
+  };
   // (K-major: two rows of the slab a request, a lane's 16 bytes of its row's 512; columns past the last whole chunk of the matrix row are
   // clamped onto it)
   auto krow_offset = [&](int i, int chunks, size_t pitch) -> uint32_t {
@@ -998,10 +1085,10 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   bool live = true;
   auto set_tile = [&](int vt) {
     if (TW) w_col = vt * F_KROW;
-    Wtile = at.W + (TW ? (size_t)w_col : (size_t)vt * FT * pitch_w);
+    Wtile = at.W + (TW ? (size_t)w_col : (size_t)vt * (GATE == 1 ? FT / 2 : FT) * pitch_w);
 #pragma unroll
     for (int i = 0; i < F_PAIRS; ++i)
-      voffA[i] = TW ? krow_offset(i, ((int)pitch_w - w_col) >> 4, pitch_w) : row_offset(i, at.n_valid - 1 - vt * FT, pitch_w);
+      voffA[i] = GATE == 1 ? gated_offset(i, a.gated.d_ff - 1 - vt * (FT / 2)) : TW ? krow_offset(i, ((int)pitch_w - w_col) >> 4, pitch_w) : row_offset(i, at.n_valid - 1 - vt * FT, pitch_w);
   };
   auto open_item = [&](bool behind) __attribute__((always_inline)) {
     if (HYP) asm volatile("" : "+s"(lj));       // (what is worked out here is not worked out for every slab)
@@ -1228,6 +1315,10 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
       if (MODE == 2) {
         if (it.part >= 0)
           store_partial16(acc, a.split + (ptrdiff_t)it.part * (FT * FT) - ((ptrdiff_t)r0 * FT + vt * FT), FT, row_base, r_end, col_base, n_valid);
+        else if (GATE == 1)
+          store_gated16(acc, a, row_base, r_end, vt * (FT / 2) + wv * 64 + quarter * 4);
+        else if (GATE == 2)
+          store_gated_slopes16(acc, a, row_base, r_end, col_base);
         else if (SUM)
           store_sum16<TH>(acc, a, row_base, r_end, col_base, n_valid);
         else if (TW && !a.residual)
@@ -1302,7 +1393,10 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
 // The tiles of a dense layer's last round that were cut along K (last_round): out = act(sum of the parts + bias) + residual, 8 rows of a tile
 // at a time, a thread 4 columns of 2 of them and eight parts asked for at once.  A workgroup takes pieces of its XCD's tiles, or of all;
 // pieces of 16 rows leave CUs without one where 12 tiles have 21 parts each (27 us instead of 17), 4096 workgroups cost 1.5 us where nothing was cut.
+// GATE: the gated block's epilogues (as in logits_fast_kernel); of its first product a thread takes the gate's and the other projection's sums of 4
+// columns of one row.
 constexpr int F_SUM_WGS = 1024;
+template <int GATE>
 __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
   const int rows = a.rows_dev ? min(a.rows, *a.rows_dev) : a.rows;
   const int tiles_each = (rows + FT - 1) / FT, row_tiles = max(a.batch, 1) * tiles_each;
@@ -1318,6 +1412,31 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
     else if (!locate_base(a, row_tiles, xcd, last.full + t, &rt, &st))
       return;
     const int b = rt / tiles_each, r0 = b * rows + (rt - b * tiles_each) * FT, r_end = (b + 1) * rows;
+    if (GATE == 1) {
+      const int row = u % (FT / 8) * 8 + (int)(threadIdx.x >> 5), c = 4 * (int)(threadIdx.x & 31), fcol = st * (FT / 2) + c;
+      if (fcol >= a.gated.d_ff || r0 + row >= r_end) continue;
+      const float* from = a.split + (size_t)((last.whole ? 0 : xcd * F_XCD_WGS) + t) * (FT * FT) + row * FT + (c >> 4) * 32 + (c & 15);
+      float x[2][4] = {};
+#pragma unroll 8
+      for (int k = 0; k < last.ways; ++k) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 y = *reinterpret_cast<const float4*>(from + h * 16);
+          x[h][0] += y.x;
+          x[h][1] += y.y;
+          x[h][2] += y.z;
+          x[h][3] += y.w;
+        }
+        from += (size_t)last.rem * (FT * FT);
+      }
+      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)(r0 + row) * a.ldo + fcol) = z2z_gated::hidden4(x[0], x[1], a.gated.act);
+      if (a.gated.kept) {
+        uint16_t* kept = reinterpret_cast<uint16_t*>(a.gated.kept) + (size_t)(r0 + row) * 2 * a.gated.d_ff + fcol;
+        *reinterpret_cast<uint2*>(kept) = z2z_gated::pack4(x[0]);
+        *reinterpret_cast<uint2*>(kept + a.gated.d_ff) = z2z_gated::pack4(x[1]);
+      }
+      continue;
+    }
     const int tcol = 4 * (int)(threadIdx.x & 63), col = st * FT + tcol;
     if (col >= a.w_rows || r0 + trow >= r_end) continue;
     const float4 bias = a.bias ? *reinterpret_cast<const float4*>(a.bias + col) : float4{0.f, 0.f, 0.f, 0.f};
@@ -1342,6 +1461,18 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
       if (a.row_slot && a.row_slot[row] >= 0) {
         const float4 y = *reinterpret_cast<const float4*>(a.sums + (size_t)a.row_slot[row] * a.ldo + col);
         x[i] = float4{x[i].x + y.x, x[i].y + y.y, x[i].z + y.z, x[i].w + y.w};
+      }
+      if (GATE == 2) {
+        const float df[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        const size_t at = (size_t)row * 2 * a.gated.d_ff + col;
+        const uint16_t* kept = reinterpret_cast<const uint16_t*>(a.gated.kept) + at;
+        const z2z_gated::Slopes4 s = z2z_gated::slopes4(df, *reinterpret_cast<const uint2*>(kept),
+                                                        *reinterpret_cast<const uint2*>(kept + a.gated.d_ff), a.gated.act);
+        uint16_t* slopes = reinterpret_cast<uint16_t*>(a.gated.slopes) + at;
+        *reinterpret_cast<uint2*>(slopes) = s.dg;
+        *reinterpret_cast<uint2*>(slopes + a.gated.d_ff) = s.du;
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo + col) = s.f;
+        continue;
       }
       finish_linear(x[i], bias, a.act, a.residual, a.out, a.stream_f32, (size_t)row * a.ldo + col);
     }
@@ -1452,8 +1583,21 @@ int z2z_launch_logits_fast(int mode, const LogitsArgs& a, unsigned grid, hipStre
   return Z2Z_OK;
 }
 
+int z2z_launch_gated_tile(const LogitsArgs& a, bool backward, unsigned grid, hipStream_t s) {
+  if (backward)
+    hipLaunchKernelGGL((logits_fast_kernel<2, false, true, false, false, false, false, 2>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+  else
+    hipLaunchKernelGGL((logits_fast_kernel<2, false, false, false, false, false, false, 1>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+  if (a.split && backward)
+    hipLaunchKernelGGL(tile_sum_kernel<2>, dim3(F_SUM_WGS), dim3(256), 0, s, a);
+  else if (a.split)
+    hipLaunchKernelGGL(tile_sum_kernel<1>, dim3(F_SUM_WGS), dim3(256), 0, s, a);
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}
+
 int z2z_launch_tile_sum(const LogitsArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(tile_sum_kernel, dim3(F_SUM_WGS), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(tile_sum_kernel<0>, dim3(F_SUM_WGS), dim3(256), 0, s, a);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
@@ -1499,6 +1643,10 @@ int z2z_logits_fast_prepare(z2z_ctx* c) {
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<6, true>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<7, true>),
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
+  Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, false, false, false, false, false, 1>),
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
+  Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, true, false, false, false, false, 2>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
   const void* at_a_temperature[] = {reinterpret_cast<const void*>(logits_fast_kernel<0, false, false, false, false, true>),
                                     reinterpret_cast<const void*>(logits_fast_kernel<0, false, false, false, true, true>),

@@ -21,6 +21,12 @@ bool overlap(const void* p, long long n, const void* q, long long m) {
   return a && b && a < b + 4 * m && b < a + 4 * n;
 }
 
+// Of n and m bytes.
+bool overlap_bytes(const void* p, size_t n, const void* q, size_t m) {
+  const char *a = static_cast<const char*>(p), *b = static_cast<const char*>(q);
+  return a && b && n && m && a < b + m && b < a + n;
+}
+
 void free_ctx(z2z_ctx* c) {
   if (!c) return;
   (void)hipFree(c->st.size);
@@ -31,7 +37,8 @@ void free_ctx(z2z_ctx* c) {
   (void)hipFree(c->st.ent_tokens);
   (void)hipFree(c->st.ent_len);
   (void)hipFree(c->st.slots);
-  for (z2z_work* w : {&c->parts_ws, &c->draws_ws, &c->sample_ws, &c->enc_ws, &c->enc_bwd_ws, &c->bwd_ws, &c->partial_ws, &c->lookup_ws})
+  for (z2z_work* w : {&c->parts_ws, &c->draws_ws, &c->sample_ws, &c->enc_ws, &c->enc_bwd_ws, &c->bwd_ws, &c->partial_ws, &c->lookup_ws,
+                      &c->ffn_ws, &c->clip_ws})
     (void)hipFree(w->p);
   (void)hipFree(c->coef_dev);
   (void)hipFree(c->prune_prefix);
@@ -347,6 +354,101 @@ Z2Z_API int z2z_hyper_encode_backward(z2z_ctx* ctx, const void* d_E, const z2z_e
   note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_hyper_encode_train(ctx, (flags & Z2Z_ENC_KEPT) ? 2 : 0, d_E, enc, nullptr, d_dW_hyper, grad, d_dE,
                                        static_cast<hipStream_t>(stream));
+}
+
+namespace {
+
+// of a gated block on a context of width d: its description's numbers, and its pointers
+int ffn_ok(const z2z_ctx* c, const z2z_ffn* f, bool bf16_only) {
+  if (!f || f->d_ff < 1 || f->reserved != 0 || (f->act != Z2Z_ACT_SILU && f->act != Z2Z_ACT_GELU)) return Z2Z_EINVAL;
+  if (!f->w_1 || !f->w_2 || !aligned16(f->w_1) || !aligned16(f->w_2)) return Z2Z_EINVAL;
+  if (f->group != 0 && f->group != 32 && f->group != 64 && f->group != 128) return Z2Z_EINVAL;
+  if (f->group != 0 && (!f->scale_1 || !f->scale_2 || !aligned16(f->scale_1) || !aligned16(f->scale_2))) return Z2Z_EINVAL;
+  const int d = c->cfg.d;
+  if (c->cfg.dtype != Z2Z_BF16 || !c->fast_ready || d % 64 != 0 || f->d_ff % 64 != 0) return Z2Z_EUNSUPPORTED;
+  if (((long long)f->d_ff + 128) * d * 2 >= (1LL << 31)) return Z2Z_EUNSUPPORTED;       // (bytes of a projection: 32-bit offsets)
+  if (f->group != 0 && (bf16_only || d % f->group != 0 || f->d_ff % f->group != 0)) return Z2Z_EUNSUPPORTED;
+  return Z2Z_OK;
+}
+
+constexpr int32_t kFfnRows = 1 << 22;
+
+}  // namespace
+
+Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, void* d_kept,
+                          void* stream) {
+  if (!ctx || rows < 0 || (rows > 0 && (!d_X || !d_Y))) return Z2Z_EINVAL;
+  if (!aligned16(d_X) || !aligned16(d_residual) || !aligned16(d_Y) || !aligned16(d_kept)) return Z2Z_EINVAL;
+  int rc = ffn_ok(ctx, ffn, d_kept != nullptr);
+  if (rc != Z2Z_OK) return rc;
+  if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
+  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 4;
+  if (overlap_bytes(d_Y, row, d_X, row) || (d_Y != d_residual && overlap_bytes(d_Y, row, d_residual, row)) || overlap_bytes(d_kept, kept, d_X, row) ||
+      overlap_bytes(d_kept, kept, d_Y, row) || overlap_bytes(d_kept, kept, d_residual, row))
+    return Z2Z_EINVAL;
+  rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK || rows == 0) return rc;
+  rc = z2z_work_reserve(ctx, &ctx->ffn_ws, z2z_ffn_work(ffn, ctx->cfg.d, rows), static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_ffn(ctx, d_X, ffn, d_residual, d_Y, false, d_kept, rows, nullptr, ctx->ffn_ws.p, static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_kept, const void* d_dY, void* d_dX,
+                                   const z2z_ffn* grad, int32_t flags, void* stream) {
+  if (!ctx || rows < 0 || (rows > 0 && (!d_X || !d_kept || !d_dY || !d_dX))) return Z2Z_EINVAL;
+  if (flags != 0 && flags != Z2Z_GRAD_ADD) return Z2Z_EINVAL;
+  if (!aligned16(d_X) || !aligned16(d_kept) || !aligned16(d_dY) || !aligned16(d_dX)) return Z2Z_EINVAL;
+  if (!grad || !grad->w_1 || !grad->w_2 || !aligned16(grad->w_1) || !aligned16(grad->w_2)) return Z2Z_EINVAL;
+  int rc = ffn_ok(ctx, ffn, true);
+  if (rc != Z2Z_OK) return rc;
+  if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
+  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 4;
+  const size_t w2 = (size_t)ctx->cfg.d * ffn->d_ff * 2, w1 = 2 * w2;
+  // (what is written against what is read, and against the rest of what is written)
+  struct {
+    const void* p;
+    size_t n;
+  } in[] = {{d_X, row}, {d_kept, kept}, {d_dY, row}, {ffn->w_1, w1}, {ffn->w_2, w2}}, out[] = {{d_dX, row}, {grad->w_1, w1}, {grad->w_2, w2}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& x : in)
+      if (overlap_bytes(out[i].p, out[i].n, x.p, x.n)) return Z2Z_EINVAL;
+    for (int k = 0; k < i; ++k)
+      if (overlap_bytes(out[i].p, out[i].n, out[k].p, out[k].n)) return Z2Z_EINVAL;
+  }
+  rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (rows == 0) return flags == Z2Z_GRAD_ADD ? Z2Z_OK : z2z_launch_fill_zero(const_cast<void*>(grad->w_1), w1, const_cast<void*>(grad->w_2), w2, s);
+  rc = z2z_work_reserve(ctx, &ctx->ffn_ws, z2z_ffn_backward_work(ffn, rows), s);
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_ffn_backward(ctx, d_X, ffn, d_kept, d_dY, d_dX, grad, flags == Z2Z_GRAD_ADD, rows, nullptr, ctx->ffn_ws.p, s);
+}
+
+Z2Z_API int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, int32_t group, void* d_q, void* d_scale, void* stream) {
+  if (!ctx || rows < 1 || cols < 1 || !d_W || !d_q || !d_scale) return Z2Z_EINVAL;
+  if (!aligned16(d_W) || !aligned16(d_q) || !aligned16(d_scale)) return Z2Z_EINVAL;
+  if (group != 32 && group != 64 && group != 128) return Z2Z_EINVAL;
+  if (ctx->cfg.dtype != Z2Z_BF16 || rows % 16 != 0 || cols % 64 != 0 || cols % group != 0) return Z2Z_EUNSUPPORTED;
+  const size_t n = (size_t)rows * cols, q = (size_t)rows * ((cols + 127) / 128) * 64, sc = n / group * 2;
+  if (overlap_bytes(d_q, q, d_W, 2 * n) || overlap_bytes(d_scale, sc, d_W, 2 * n) || overlap_bytes(d_q, q, d_scale, sc)) return Z2Z_EINVAL;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_quantize_q4(d_W, rows, cols, group, d_q, d_scale, static_cast<hipStream_t>(stream));
+}
+
+Z2Z_API int z2z_clip_gradients(z2z_ctx* ctx, const z2z_gradient* gradients, int32_t n, float max_norm, float* d_norm, void* stream) {
+  if (!ctx || n < 0 || (n > 0 && !gradients) || !d_norm || !(max_norm >= 0.f)) return Z2Z_EINVAL;      // (a NaN, too)
+  if (reinterpret_cast<uintptr_t>(d_norm) & 3u) return Z2Z_EINVAL;
+  for (int32_t i = 0; i < n; ++i) {
+    const z2z_gradient& g = gradients[i];
+    if (g.n < 0 || (g.n > 0 && !g.data) || (g.dtype != Z2Z_F32 && g.dtype != Z2Z_BF16) || g.reserved != 0) return Z2Z_EINVAL;
+    const uintptr_t size = g.dtype == Z2Z_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(g.data) % size != 0 || reinterpret_cast<uintptr_t>(g.out) % size != 0) return Z2Z_EINVAL;
+  }
+  if (n > Z2Z_MAX_GRADIENTS) return Z2Z_EUNSUPPORTED;
+  const int rc = enter(ctx, static_cast<hipStream_t>(stream));
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_clip_gradients(ctx, gradients, n, max_norm, d_norm, static_cast<hipStream_t>(stream));
 }
 
 Z2Z_API int z2z_extended_logits(z2z_ctx* ctx, const void* d_H, int32_t rows, int32_t rows_per_seq,

@@ -96,6 +96,8 @@ struct z2z_ctx {
   // dense layers on few rows with K split over workgroups: the partial tiles
   z2z_work partial_ws;
   z2z_work lookup_ws;      // gradient of the code lookup: sorted positions, sums that cross pieces; a teacher's listed part
+  z2z_work ffn_ws;         // gated feed-forward block: hidden layer, its gradients, weights expanded from 4 bits
+  z2z_work clip_ws;        // sums of the gradients' squares
   bool capturing;          // the present call is being captured into a graph, or may be
   z2z_kept* kept;
   // options
@@ -195,6 +197,22 @@ int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, c
                          hipStream_t s);
 int z2z_launch_part_max(z2z_ctx* c, const float* logits, float* part_m, int* n_parts, hipStream_t s);   // parts of 256 columns
 int z2z_launch_codebook_reorder(z2z_ctx* c, int32_t beams, const int32_t* source, void* W_hyper, hipStream_t s);
+
+// The gated block on R rows (or the first *rows_dev of them), with work space of z2z_ffn_work bytes; stream_f32: residual and Y are fp32.
+size_t z2z_ffn_work(const z2z_ffn* f, int d, int rows);
+int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* residual, void* Y, bool stream_f32, void* kept, int R, const int32_t* rows_dev,
+                   void* work, hipStream_t s);
+size_t z2z_ffn_backward_work(const z2z_ffn* f, int rows);
+int z2z_launch_ffn_backward(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* kept, const void* dY, void* dX, const z2z_ffn* grad, bool add, int R,
+                            const int32_t* rows_dev, void* work, hipStream_t s);
+int z2z_launch_fill_zero(void* p, size_t bytes, void* q, size_t bytes_q, hipStream_t s);   // multiples of 16
+// 4-bit weights (q4.hip): from bf16, to bf16, and the product X w^T of few rows as fp32 parts [*ksplit][R][N], which the caller adds up before the next
+// dense layer is launched
+int z2z_launch_quantize_q4(const void* W, int rows, int cols, int group, void* q, void* scale, hipStream_t s);
+int z2z_launch_expand_q4(const void* q, const void* scale, int rows, int cols, int group, void* W, hipStream_t s);
+int z2z_launch_q4_parts(z2z_ctx* c, const void* X, const void* q, const void* scale, int group, int R, const int32_t* rows_dev, int N, int K,
+                        const float** partial, int* ksplit, hipStream_t s);
+int z2z_launch_clip_gradients(z2z_ctx* c, const z2z_gradient* g, int n, float max_norm, float* norm, hipStream_t s);
 
 // At least `bytes` in the work buffer, every time a call is about to use it (Z2Z_ECAPTURE where it would have to grow under capture, Z2Z_ENOMEM where
 // the device has no room: what was there is there still, or as much).  `at_least`: no less where it grows.

@@ -1,0 +1,180 @@
+"""The gradients' common norm and their clipping through the C ABI, against sums in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+import oracle
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _context():
+    from paper_2506_01084_amd import api
+
+    return api.Context(B=1, V=8, M=2, cap=0, d=64)
+
+
+def _host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _clip(ctx, tensors, max_norm, out=None):
+    from paper_2506_01084_amd import api
+
+    norm = torch.full((2,), float("nan"), dtype=torch.float32, device="cuda")
+    ctx.clip_gradients(api.Gradients(tensors, out), max_norm, norm)
+    return [float(x) for x in norm.cpu()]
+
+
+def _check(ctx, tensors, max_norm, in_place):
+    host = [_host(t) for t in tensors]
+    want, c, clipped = oracle.clip(host, max_norm)
+    out = None if in_place else [torch.full_like(t, 7.0) for t in tensors]
+    norm, got_c = _clip(ctx, tensors, max_norm, out)
+    # a square and a sum of at most 64 of them in 32 bits, then 64 bits; the root halves it; one rounding of the norm
+    # (a norm that fp32 does not hold is an infinity there; the coefficient comes from the 64-bit one)
+    assert norm == math.inf if want > 3.4028236e38 else abs(norm - want) <= want * (34 + 1) * 2.0 ** -24
+    assert abs(got_c - c) <= c * (34 + 2) * 2.0 ** -24
+    for t, h, w in zip(tensors if in_place else out, host, clipped):
+        step = 2.0 ** -8 if t.dtype == torch.bfloat16 else 2.0 ** -24
+        least = 2.0 ** -134 if t.dtype == torch.bfloat16 else 2.0 ** -150
+        if got_c == 1.0:
+            assert np.array_equal(_host(t), h)
+        else:
+            assert np.all(np.abs(_host(t) - w) <= np.abs(w) * (step + 40 * 2.0 ** -24) + least)
+    return norm, got_c
+
+
+@pytest.mark.parametrize("sizes", [[1], [3], [7, 8, 9], [15, 1, 16, 17], [0, 5, 0], [4096], [16383, 16384, 16385], [100003, 2, 65536 * 5 + 1], [1 << 22, 3]])
+@pytest.mark.parametrize("kinds", ["b", "f", "bf"])
+def test_sizes_and_types(sizes, kinds):
+    gen = torch.Generator().manual_seed(sum(sizes))
+    ctx = _context()
+    make = lambda: [(torch.randn(n, generator=gen) * 10 ** (i % 3 - 1)).to(torch.bfloat16 if kinds[i % len(kinds)] == "b" else torch.float32).cuda()
+                    for i, n in enumerate(sizes)]
+    for in_place in (True, False):
+        norm, c = _check(ctx, make(), 0.25, in_place)
+        assert (c < 1) == (norm > 0.25)
+        assert _check(ctx, make(), 1e6, in_place)[1] == 1
+        assert _check(ctx, make(), math.inf, in_place)[1] == 1
+        assert _check(ctx, make(), 0.0, in_place)[1] == 0          # (a coefficient of zero)
+
+
+def test_any_address():
+    """Tensors that start between 16-byte boundaries, and outputs that start between others."""
+    gen = torch.Generator().manual_seed(1)
+    ctx = _context()
+    for n in (1, 2, 5, 8, 40, 20000):
+        for lead in range(9):
+            whole = [(torch.randn(n + 40, generator=gen)).to(dt).cuda() for dt in (torch.bfloat16, torch.float32)]
+            before = [w.clone() for w in whole]
+            views = [w[lead:lead + n] for w in whole]
+            _check(ctx, views, 0.5, True)
+            for w, b in zip(whole, before):
+                assert torch.equal(w[:lead], b[:lead]) and torch.equal(w[lead + n:], b[lead + n:])
+            out = [torch.full((n + 40,), 7.0, dtype=w.dtype, device="cuda") for w in whole]
+            host = [_host(v) for v in views]
+            _, c, _ = oracle.clip(host, 0.1)
+            _clip(ctx, views, 0.1, [o[3:3 + n] for o in out])
+            for o, h in zip(out, host):
+                assert (o[:3] == 7).all() and (o[3 + n:] == 7).all()
+                assert np.allclose(_host(o[3:3 + n]), h * c, rtol=2.0 ** -8 + 1e-5 if o.dtype == torch.bfloat16 else 1e-5, atol=0)
+
+
+def test_many_tensors():
+    """More than a launch's list takes, all of a step's vectors; some count for the norm alone."""
+    gen = torch.Generator().manual_seed(2)
+    ctx = _context()
+    tensors = [torch.randn(1 + (37 * i) % 900, generator=gen).to(torch.bfloat16 if i % 3 else torch.float32).cuda() for i in range(300)]
+    _check(ctx, [t.clone() for t in tensors], 1.0, True)
+    host = [_host(t) for t in tensors]
+    want, c, clipped = oracle.clip(host, 1.0)
+    out = [torch.full_like(t, 7.0) if i % 2 else None for i, t in enumerate(tensors)]
+    norm, got = _clip(ctx, tensors, 1.0, out)
+    assert abs(norm - want) <= want * 35 * 2.0 ** -24 and abs(got - c) <= c * 36 * 2.0 ** -24
+    for t, h, o, w in zip(tensors, host, out, clipped):
+        assert np.array_equal(_host(t), h)
+        if o is not None:
+            assert np.allclose(_host(o), w, rtol=2.0 ** -8 + 1e-5, atol=0)
+    assert _clip(ctx, tensors, 1.0, [None] * 300) == [norm, got]
+    assert _clip(ctx, [], 1.0) == [0.0, 1.0]
+
+
+def test_ranges():
+    """Values whose squares leave the range of 32 bits, zeros, infinities and NaN."""
+    ctx = _context()
+    for value in (1e-30, 1e-20, 1e-13, 1e18, 1e25, 3e38):
+        t = torch.full((5000,), value, dtype=torch.float32, device="cuda")
+        t[100:3000] = 0
+        norm, c = _check(ctx, [t], value, False)
+        assert norm == pytest.approx(value * math.sqrt(2100), rel=1e-6) if value < 1e36 else norm == math.inf
+    mixed = torch.full((70000,), 1e-24, dtype=torch.bfloat16, device="cuda")
+    _check(ctx, [mixed, torch.full((70000,), 1e-23, dtype=torch.float32, device="cuda")], 1e-22, True)
+    zeros = torch.zeros(1000, device="cuda")
+    assert _clip(ctx, [zeros], 1.0) == [0.0, 1.0] and _clip(ctx, [zeros], 0.0) == [0.0, 1.0]
+    for bad in (math.inf, -math.inf, math.nan):
+        t = torch.ones(100000, device="cuda")
+        t[77777] = bad
+        before = t.clone()
+        norm, c = _clip(ctx, [t], 0.5)
+        assert c == 1.0 and (math.isnan(norm) if math.isnan(bad) else norm == math.inf)
+        assert torch.equal(torch.nan_to_num(t, nan=5.0), torch.nan_to_num(before, nan=5.0))
+
+
+def test_same_bits_graphs_and_streams():
+    from paper_2506_01084_amd import api
+
+    gen = torch.Generator().manual_seed(3)
+    ctx = _context()
+    grads = [torch.randn(n, generator=gen).to(dt).cuda() for n, dt in ((3000000, torch.bfloat16), (1000001, torch.float32), (5, torch.float32))]
+    out = [torch.empty_like(g) for g in grads]
+    listed, norm = api.Gradients(grads, out), torch.empty(2, device="cuda")
+    ctx.clip_gradients(listed, 1.0, norm)
+    first, outs = norm.clone(), [o.clone() for o in out]
+    for _ in range(5):
+        ctx.clip_gradients(listed, 1.0, norm)
+        assert torch.equal(norm, first) and all(torch.equal(a, b) for a, b in zip(out, outs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.clip_gradients(listed, 1.0, norm)
+    for i in range(4):
+        for g in grads:
+            g.mul_(0.5 if i else 1.0)
+        graph.replay()
+        got, got_out = norm.clone(), [o.clone() for o in out]
+        torch.cuda.synchronize()
+        ctx.clip_gradients(api.Gradients([torch.ones(5000000, device="cuda")]), math.inf, torch.empty(2, device="cuda"))
+        ctx.clip_gradients(listed, 1.0, norm)
+        assert torch.equal(norm, got) and all(torch.equal(a, b) for a, b in zip(out, got_out))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ctx.clip_gradients(listed, 1.0, norm)
+    side.synchronize()
+    assert torch.equal(norm, got)
+
+
+def test_binding_refusals():
+    from paper_2506_01084_amd import api
+
+    ctx = _context()
+    t, norm = torch.ones(100, device="cuda"), torch.empty(2, device="cuda")
+    for bad in ([t, t], [t, t[50:]], [t[:60], t[59:]]):                            # written twice
+        with pytest.raises(api.Z2ZError) as e:
+            ctx.clip_gradients(api.Gradients(bad), 1.0, norm)
+        assert e.value.code == api.E_INVAL
+    ctx.clip_gradients(api.Gradients([t[:50], t[50:]]), math.inf, norm)            # next to each other
+    ctx.clip_gradients(api.Gradients([t, t], [None, None]), 1.0, norm)             # read twice
+    for bad in (-1.0, math.nan):
+        with pytest.raises(api.Z2ZError) as e:
+            ctx.clip_gradients(api.Gradients([t]), bad, norm)
+        assert e.value.code == api.E_INVAL
+    with pytest.raises(ValueError):
+        api.Gradients([t.half()])
+    with pytest.raises(ValueError):
+        api.Gradients([t[::2]])
+    with pytest.raises(ValueError):
+        api.Gradients([t.cpu()])
+    assert (t == 1).all()

@@ -1,0 +1,226 @@
+"""The gated feed-forward block and its gradient through the C ABI against the oracle, element by element within bounds that follow from its roundings."""
+import numpy as np
+import pytest
+
+import oracle
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _tensors(rows, d, f, seed, std=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    X = torch.randn((rows, d), generator=gen) * std
+    W1 = torch.randn((2 * f, d), generator=gen) * d ** -0.5
+    W2 = torch.randn((d, f), generator=gen) * f ** -0.5
+    R = torch.randn((rows, d), generator=gen)
+    dY = torch.randn((rows, d), generator=gen) * 1e-2
+    return [t.to(torch.bfloat16).cuda() for t in (X, W1, W2, R, dY)]
+
+
+def _host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _context(d, **kw):
+    from paper_2506_01084_amd import api
+
+    return api.Context(B=1, V=8, M=2, cap=0, d=d, **kw)
+
+
+def _within(got, value, bound, what):
+    off = np.abs(_host(got) - value)
+    assert np.all(off <= bound), (what, float(np.max(off / bound)), np.argwhere(~(off <= bound))[:4].tolist())
+    norm = np.linalg.norm(value)
+    # (rounded six times at most, independently: in the mean far inside)
+    assert np.linalg.norm(off) <= np.sqrt(6) * 2.0 ** -8 * norm + 1e-30, (what, np.linalg.norm(off) / norm)
+
+
+# one row; both sides of the kernels' limits (128 rows, a tile of 256, tiles enough for the CUs); widths of which no tile is a divisor
+SHAPES = [(1, 64, 64), (1, 1024, 448), (2, 192, 704), (15, 320, 192), (16, 512, 128), (17, 256, 64), (33, 128, 320), (64, 1024, 2752), (65, 192, 192),
+          (127, 640, 448), (128, 512, 1088), (129, 512, 1088), (200, 2112, 576), (255, 320, 640), (256, 64, 64), (257, 2048, 448), (300, 2112, 704), (513, 1024, 1344),
+          (700, 128, 64), (1031, 576, 832), (2500, 256, 320)]
+
+
+@pytest.mark.parametrize("rows,d,f", SHAPES)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_forward(rows, d, f, act):
+    from paper_2506_01084_amd import api
+
+    X, W1, W2, R, _ = _tensors(rows, d, f, rows + d + f)
+    ctx = _context(d)
+    block = api.GatedFFN(W1, W2, act=act)
+    for residual in (None, R):
+        ref = oracle.gated_ffn(_host(X), _host(W1), _host(W2), act, None if residual is None else _host(R))
+        Y = torch.full_like(X, float("nan"))
+        kept = torch.full((rows, 2 * f), float("nan"), dtype=torch.bfloat16, device="cuda")
+        ctx.gated_ffn(X, block, Y, residual=residual)
+        _within(Y, ref["Y"], ref["Y_bound"], "Y")
+        again = torch.full_like(X, float("nan"))
+        ctx.gated_ffn(X, block, again, residual=residual, kept=kept)
+        assert torch.equal(Y, again)
+        _within(kept, np.concatenate([ref["G"], ref["U"]], axis=1), ref["kept_bound"], "kept")
+    in_place = R.clone()
+    ctx.gated_ffn(X, block, in_place, residual=in_place)
+    assert torch.equal(in_place, again)
+
+
+@pytest.mark.parametrize("rows,d,f", SHAPES)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_backward(rows, d, f, act):
+    from paper_2506_01084_amd import api
+
+    X, W1, W2, _, dY = _tensors(rows, d, f, 3 * rows + d + f)
+    ctx = _context(d)
+    block = api.GatedFFN(W1, W2, act=act)
+    Y, kept = torch.empty_like(X), torch.empty((rows, 2 * f), dtype=torch.bfloat16, device="cuda")
+    ctx.gated_ffn(X, block, Y, kept=kept)
+    dX, dW1, dW2 = (torch.full_like(t, float("nan")) for t in (X, W1, W2))
+    ctx.gated_ffn_backward(X, block, kept, dY, dX, api.GatedFFN(dW1, dW2))
+    ref = oracle.gated_ffn_backward(_host(X), _host(W1), _host(W2), act, _host(dY))
+    for name, got in (("dX", dX), ("dW1", dW1), ("dW2", dW2)):
+        _within(got, ref[name], ref[name + "_bound"], name)
+    # the same inputs give the same bits, and an added gradient is rounded once
+    dX2, a1, a2 = torch.empty_like(dX), torch.randn_like(dW1), torch.randn_like(dW2)
+    was = [_host(a1), _host(a2)]
+    ctx.gated_ffn_backward(X, block, kept, dY, dX2, api.GatedFFN(a1, a2), add=True)
+    assert torch.equal(dX, dX2)
+    for name, got, before in (("dW1", a1, was[0]), ("dW2", a2, was[1])):
+        total = ref[name] + before
+        bound = (ref[name + "_err"] * 1.02 + 2.0 ** -8 * (np.abs(total) + ref[name + "_err"])) * 1.001
+        assert np.all(np.abs(_host(got) - total) <= bound), name
+    # and in place of the formula, differences of the loss along the gradient (rounded outputs: the direction is scaled to reach over them)
+
+
+def test_gradient_along_differences():
+    from paper_2506_01084_amd import api
+
+    rows, d, f = 40, 128, 192
+    X, W1, W2, _, dY = _tensors(rows, d, f, 77)
+    ctx = _context(d)
+    kept = torch.empty((rows, 2 * f), dtype=torch.bfloat16, device="cuda")
+    Y = torch.empty_like(X)
+    ctx.gated_ffn(X, api.GatedFFN(W1, W2, act="gelu"), Y, kept=kept)
+    dX, dW1, dW2 = (torch.empty_like(t) for t in (X, W1, W2))
+    ctx.gated_ffn_backward(X, api.GatedFFN(W1, W2, act="gelu"), kept, dY, dX, api.GatedFFN(dW1, dW2))
+
+    def loss(x, w1, w2):
+        out = torch.empty_like(x)
+        ctx.gated_ffn(x, api.GatedFFN(w1, w2, act="gelu"), out)
+        return float((out.double() * dY.double()).sum())
+
+    for which, (t, g) in enumerate(((X, dX), (W1, dW1), (W2, dW2))):
+        v = g.double() / g.double().norm()
+        step = 0.05 * float(t.double().norm())
+        args = [X, W1, W2]
+        args[which] = (t.double() + step * v).bfloat16()
+        up, moved_up = loss(*args), args[which].double()
+        args[which] = (t.double() - step * v).bfloat16()
+        down, moved_down = loss(*args), args[which].double()
+        want = float((g.double() * (moved_up - moved_down)).sum())
+        # the loss is a sum of 5120 products with values rounded to half of 2^-7, and the third derivative's share at a twentieth of the tensor's norm
+        noise = 2 * 2.0 ** -8 * float((Y.double().abs() * dY.double().abs()).pow(2).sum().sqrt()) * 3
+        assert abs(up - down - want) <= noise + 0.05 * abs(want), (which, up - down, want, noise)
+
+
+def test_extreme_rows():
+    """Rows of zeros, of large values and of NaN: the others' results do not depend on them."""
+    from paper_2506_01084_amd import api
+
+    rows, d, f = 70, 256, 320
+    X, W1, W2, R, _ = _tensors(rows, d, f, 9)
+    ctx = _context(d)
+    for act in ("silu", "gelu"):
+        block = api.GatedFFN(W1, W2, act=act)
+        Y, Z = torch.empty_like(X), torch.empty_like(X)
+        ctx.gated_ffn(X, block, Y, residual=R)
+        other = X.clone()
+        other[3], other[10], other[69], other[20] = 0, 1e4, float("nan"), float("inf")
+        ctx.gated_ffn(other, block, Z, residual=R)
+        same = [i for i in range(rows) if i not in (3, 10, 69, 20)]
+        assert torch.equal(Y[same], Z[same])
+        assert torch.equal(Z[3], R[3]) and torch.isnan(Z[69]).all() and not torch.isfinite(Z[20]).any()
+        ref = oracle.gated_ffn(_host(other[10:11]), _host(W1), _host(W2), act, _host(R[10:11]))
+        _within(Z[10:11], ref["Y"], ref["Y_bound"], "large")
+
+
+def test_rows_behind_the_last_and_empty_calls():
+    from paper_2506_01084_amd import api
+
+    d, f = 192, 128
+    X, W1, W2, R, dY = _tensors(300, d, f, 4)
+    ctx = _context(d)
+    block = api.GatedFFN(W1, W2)
+    for rows in (0, 1, 130, 299):
+        Y, kept = torch.full_like(X, 7.0), torch.full((300, 2 * f), 7.0, dtype=torch.bfloat16, device="cuda")
+        dX = torch.full_like(X, 7.0)
+        ctx.gated_ffn(X[:rows], block, Y[:rows], residual=R[:rows], kept=kept[:rows])
+        dW = torch.full_like(W1, 7.0), torch.full_like(W2, 7.0)
+        ctx.gated_ffn_backward(X[:rows], block, kept[:rows], dY[:rows], dX[:rows], api.GatedFFN(*dW))
+        for t in (Y, kept, dX):
+            assert (t[rows:] == 7.0).all()
+        if rows == 0:
+            assert (dW[0] == 0).all() and (dW[1] == 0).all()
+            ctx.gated_ffn_backward(X[:0], block, kept[:0], dY[:0], dX[:0], api.GatedFFN(W1.clone(), W2.clone()), add=True)
+
+
+@pytest.mark.parametrize("rows", [24, 400])
+def test_graph_replays_and_streams(rows):
+    from paper_2506_01084_amd import api
+
+    d, f = 2048, 320
+    X, W1, W2, R, dY = _tensors(rows, d, f, 21)
+    ctx = _context(d)
+    block = api.GatedFFN(W1, W2)
+    kept = torch.empty((rows, 2 * f), dtype=torch.bfloat16, device="cuda")
+    out = [torch.empty_like(t) for t in (X, X, W1, W2)]
+
+    def step(x, to, keep):
+        ctx.gated_ffn(x, block, to[0], residual=R, kept=keep)
+        ctx.gated_ffn_backward(x, block, keep, dY, to[1], api.GatedFFN(to[2], to[3]))
+
+    eager = [torch.empty_like(t) for t in out]
+    step(X, eager, kept)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(X, out, kept)
+    for i in range(4):
+        X.copy_(torch.randn((rows, d), generator=torch.Generator().manual_seed(i)).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        step(X, eager, torch.empty_like(kept))
+        # (a larger call in between: the graph's work space stays its own)
+        more = torch.randn((900, d), device="cuda").bfloat16()
+        ctx.gated_ffn(more, block, torch.empty_like(more))
+        for a, b in zip(out, eager):
+            assert torch.equal(a, b), i
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(X, out, kept)
+    side.synchronize()
+    for a, b in zip(out, eager):
+        assert torch.equal(a, b)
+
+
+def test_binding_refusals():
+    from paper_2506_01084_amd import api
+
+    X, W1, W2, _, _ = _tensors(8, 128, 64, 2)
+    ctx = _context(128)
+    block = api.GatedFFN(W1, W2)
+    with pytest.raises(ValueError):
+        ctx.gated_ffn(X.float(), block, X)
+    with pytest.raises(ValueError):
+        ctx.gated_ffn(X.cpu(), block, torch.empty_like(X))
+    with pytest.raises(ValueError):
+        ctx.gated_ffn(torch.empty((8, 256), dtype=torch.bfloat16, device="cuda")[:, ::2], block, torch.empty_like(X))
+    with pytest.raises(AssertionError):
+        api.GatedFFN(W1[:64], W2)
+    with pytest.raises(api.Z2ZError) as e:
+        ctx.gated_ffn(X, block, X)
+    assert e.value.code == api.E_INVAL
+    f32 = _context(128, dtype="f32")
+    with pytest.raises(api.Z2ZError) as e:
+        f32.gated_ffn(X, block, torch.empty_like(X))
+    assert e.value.code == api.E_UNSUPPORTED
