@@ -252,7 +252,7 @@ int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, i
  *        scale_2 [f / group, d].  Up to 192 rows are multiplied by v, the scales with fp32 sums;
  *        more rows by the weights rounded to bf16, which takes 6 d f bytes of work space.
  *   d_X [rows, d], d_residual [rows, d] or NULL, d_Y [rows, d] out: bf16.  d_Y may be d_residual, else it overlaps neither input (Z2Z_EINVAL)
- *   d_kept  [rows, 2 f] bf16 out or NULL: G | U for z2z_gated_ffn_backward (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
+ *   d_kept  [rows, 2 f] float out or NULL: G | U for z2z_gated_ffn_backward (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
  * A row's results do not depend on the other rows' values.  rows = 0 is a call that does nothing.  bf16 contexts, d and d_ff multiples of 64 (with 4 bits of group,
  * too), rows <= 2^22, (d_ff + 128) d < 2^30, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and for few rows the parts of the products. */
 enum { Z2Z_ACT_SILU = 0, Z2Z_ACT_GELU = 1 };
@@ -266,7 +266,7 @@ typedef struct z2z_ffn {
   const void* scale_1;  /* NULL for bf16 weights */
   const void* scale_2;
 } z2z_ffn;
-int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, void* d_kept, void* stream);
+int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, float* d_kept, void* stream);
 
 /* Backward of z2z_gated_ffn: the gradient of  L = sum dY * Y  with respect to the rows and both matrices (the residual's is dY itself),
  *   dF = dY w_2;   dG = dF * U * act'(G),   dU = dF * act(G);   dX = [dG | dU] w_1;   dw_1 = [dG | dU]^T X;   dw_2 = dY^T F.
@@ -276,7 +276,7 @@ int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ff
  *          other fields are not read.  flags = 0: overwritten (rows = 0: with zeros); Z2Z_GRAD_ADD: added to what is there, one rounding per element
  * dG, dU and F are rounded to bf16 once, sums are fp32.  No output overlaps an input or another output (Z2Z_EINVAL).  Restrictions as for z2z_gated_ffn; work
  * space: 6 f bytes per row. */
-int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_kept, const void* d_dY, void* d_dX,
+int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const float* d_kept, const void* d_dY, void* d_dX,
                            const z2z_ffn* grad, int32_t flags, void* stream);
 
 /* clip_gradients.  The common norm of n gradients, and their clipping by it:

@@ -4,7 +4,7 @@ Section 2.2 of the zip2zip paper trains a transformer as hyper-encoder; the gate
     G = X W1[:f]^T,  U = X W1[f:]^T,  F = act(G) * U,  Y = F W2^T + residual,
 act = SiLU or GELU (erf).  A 4-bit weight is scale[column // group, row] times one of
 0, 1/2, 1, 3/2, 2, 3, 4, 6, with a sign.  Everything is float64; with each result comes an
-elementwise bound on how far a computation may be off that rounds F (and, backward, dG, dU and the kept G and U) to bf16 once
+elementwise bound on how far a computation may be off that rounds F (and, backward, dG and dU) to bf16 once
 and forms its sums in float32.
 """
 from __future__ import annotations
@@ -50,7 +50,7 @@ def gated_ffn(X, W1, W2, kind: str, residual=None, round_weights: bool = False):
     w2 = np.abs(W2).T
     Y_err = F_err @ w2 + _sum_bound(F, W2.T) + (HALF_BF16 * (np.abs(F) @ w2) if round_weights else 0.0)
     Y_bound = (Y_err * 1.02 + HALF_BF16 * (np.abs(Y) + Y_err)) * 1.001 + 1e-30
-    return dict(Y=Y, Y_bound=Y_bound, Y_err=Y_err, G=G, U=U, F=F, kept_bound=np.concatenate([g_err, u_err], axis=1) + HALF_BF16 * np.abs(GU) + 1e-30)
+    return dict(Y=Y, Y_bound=Y_bound, Y_err=Y_err, G=G, U=U, F=F, kept_bound=np.concatenate([g_err, u_err], axis=1) + 1e-30)
 
 
 def gated_ffn_backward(X, W1, W2, kind: str, dY):

@@ -441,12 +441,13 @@ class Context:
 
     def gated_ffn(self, X: torch.Tensor, ffn: GatedFFN, Y: torch.Tensor, residual: Optional[torch.Tensor] = None,
                   kept: Optional[torch.Tensor] = None) -> None:
-        """Y = (act(X w_1[:f]^T) * (X w_1[f:]^T)) w_2^T + residual; kept [rows, 2 f]: what gated_ffn_backward needs of it."""
+        """Y = (act(X w_1[:f]^T) * (X w_1[f:]^T)) w_2^T + residual; kept [rows, 2 f] float32: what gated_ffn_backward needs of it."""
         rows, d = X.shape
         assert d == self.d and Y.shape == X.shape and (residual is None or residual.shape == X.shape)
         assert kept is None or tuple(kept.shape) == (rows, 2 * ffn.d_ff)
         own, kind = self._own, torch.bfloat16
-        _check(self._lib.z2z_gated_ffn(self._h, own(X, kind), rows, self._block(ffn), own(residual, kind), own(Y, kind), own(kept, kind), _stream()),
+        _check(self._lib.z2z_gated_ffn(self._h, own(X, kind), rows, self._block(ffn), own(residual, kind), own(Y, kind),
+                                       own(kept, torch.float32), _stream()),
                "z2z_gated_ffn")
 
     def gated_ffn_backward(self, X: torch.Tensor, ffn: GatedFFN, kept: torch.Tensor, dY: torch.Tensor, dX: torch.Tensor, grad: GatedFFN,
@@ -456,7 +457,7 @@ class Context:
         assert d == self.d and dY.shape == X.shape and dX.shape == X.shape and tuple(kept.shape) == (rows, 2 * ffn.d_ff)
         assert (grad.d, grad.d_ff, grad.desc.group) == (ffn.d, ffn.d_ff, 0)
         own, kind = self._own, torch.bfloat16
-        _check(self._lib.z2z_gated_ffn_backward(self._h, own(X, kind), rows, self._block(ffn), own(kept, kind), own(dY, kind), own(dX, kind),
+        _check(self._lib.z2z_gated_ffn_backward(self._h, own(X, kind), rows, self._block(ffn), own(kept, torch.float32), own(dY, kind), own(dX, kind),
                                                 self._block(grad), GRAD_ADD if add else 0, _stream()), "z2z_gated_ffn_backward")
 
     def clip_gradients(self, gradients: Gradients, max_norm: float, norm: torch.Tensor) -> None:

@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(const float* partial, i
 
 // The first product of a gated block from its parts: one thread per run of 4 columns of F.
 __global__ void __launch_bounds__(256) gated_sum_kernel(const float* partial, int ksplit, int rows, const int32_t* rows_dev, int f, int act,
-                                                        uint16_t* F, uint16_t* kept) {
+                                                        uint16_t* F, float* kept) {
   const int n4 = f >> 2;
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   const int r_end = rows_dev ? min(rows, *rows_dev) : rows;
@@ -54,8 +54,8 @@ __global__ void __launch_bounds__(256) gated_sum_kernel(const float* partial, in
   const float gv[4] = {g.x, g.y, g.z, g.w}, uv[4] = {u.x, u.y, u.z, u.w};
   *reinterpret_cast<uint2*>(F + (size_t)row * f + col) = z2z_gated::hidden4(gv, uv, act);
   if (kept) {
-    *reinterpret_cast<uint2*>(kept + at) = z2z_gated::pack4(gv);
-    *reinterpret_cast<uint2*>(kept + at + f) = z2z_gated::pack4(uv);
+    *reinterpret_cast<float4*>(kept + at) = g;
+    *reinterpret_cast<float4*>(kept + at + f) = u;
   }
 }
 
@@ -262,7 +262,7 @@ int z2z_launch_linear_sum(const float* partial, int ksplit, int R, const int32_t
 int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, void* kept, hipStream_t s) {
   const long long n_threads = (long long)R * (d_ff / 4);
   hipLaunchKernelGGL(gated_sum_kernel, dim3((unsigned)((n_threads + 255) / 256)), dim3(256), 0, s, partial, ksplit, R, rows_dev, d_ff, act,
-                     reinterpret_cast<uint16_t*>(F), reinterpret_cast<uint16_t*>(kept));
+                     reinterpret_cast<uint16_t*>(F), reinterpret_cast<float*>(kept));
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }

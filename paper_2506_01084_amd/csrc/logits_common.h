@@ -323,7 +323,7 @@ struct LogitsArgs {
   } hyper;
   // gated feed-forward block (tile kernel, GATE 1 and 2).  Forward: W holds d_ff gate rows, then d_ff rows of the other projection (w_rows = 2 d_ff),
   // out = F [rows, d_ff], kept = nullptr or where G | U go, [rows, 2 d_ff].  Backward: the product is dF, out = F, kept = the forward pass's G | U,
-  // slopes = dG | dU.  All bf16.
+  // slopes = dG | dU.  bf16, what is kept fp32.
   struct {
     void *kept, *slopes;
     int32_t d_ff, act;
@@ -541,7 +541,7 @@ bool z2z_linear_takes_pitch(const z2z_ctx* c, int R, int N, int K);
 int z2z_launch_linear_parts(z2z_ctx* c, const void* A, const void* W, int R, const int32_t* rows_dev, int N, int K,
                             const float** partial, int* ksplit, hipStream_t s, bool once = false);
 // The gated block's own products (bf16; K a multiple of 64, d_ff of 64):
-//   z2z_launch_gated_hidden   F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff], and, where kept is given, the two products beside each other, [R, 2 d_ff]
+//   z2z_launch_gated_hidden   F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff], and, where kept is given, the two products beside each other, fp32 [R, 2 d_ff]
 //   z2z_launch_gated_sum      the same from fp32 parts [ksplit][R][2 d_ff] of the products
 //   z2z_launch_gated_slopes   dF = dY W, W [K, d_ff], as dG | dU [R, 2 d_ff], and F once more
 int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K,

@@ -735,30 +735,26 @@ __device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& 
   for (int j = 0; j < F_N; ++j) {
     const int row = row_base + j * 16 + lane15;
     const bool row_ok = row < r_end;
-    uint2 h[F_N / 2], g[F_N / 2], u[F_N / 2];
+    uint2 h[F_N / 2];
+    float* kept = a.gated.kept ? reinterpret_cast<float*>(a.gated.kept) + (size_t)row * 2 * f : nullptr;
 #pragma unroll
     for (int k = 0; k < F_N / 2; ++k) {
-      float gv[4], uv[4];
+      float g[4], u[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        gv[e] = read_acc(acc[2 * k][j][e]);
-        uv[e] = read_acc(acc[2 * k + 1][j][e]);
+        g[e] = read_acc(acc[2 * k][j][e]);
+        u[e] = read_acc(acc[2 * k + 1][j][e]);
       }
-      h[k] = z2z_gated::hidden4(gv, uv, a.gated.act);
-      g[k] = z2z_gated::pack4(gv);
-      u[k] = z2z_gated::pack4(uv);
+      h[k] = z2z_gated::hidden4(g, u, a.gated.act);
+      const int col = col_base + k * 16;
+      if (kept && row_ok && col < f) {
+        *reinterpret_cast<float4*>(kept + col) = float4{g[0], g[1], g[2], g[3]};
+        *reinterpret_cast<float4*>(kept + f + col) = float4{u[0], u[1], u[2], u[3]};
+      }
     }
     uint16_t* out_row = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo;
 #pragma unroll
     for (int k = 0; k < F_N / 2; k += 2) store_two_blocks(out_row, row_ok, col_base, k, h[k], h[k + 1], f);
-    if (a.gated.kept) {
-      uint16_t* kept = reinterpret_cast<uint16_t*>(a.gated.kept) + (size_t)row * 2 * f;
-#pragma unroll
-      for (int k = 0; k < F_N / 2; k += 2) {
-        store_two_blocks(kept, row_ok, col_base, k, g[k], g[k + 1], f);
-        store_two_blocks(kept + f, row_ok, col_base, k, u[k], u[k + 1], f);
-      }
-    }
   }
 }
 
@@ -766,40 +762,43 @@ __device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& 
 // of the arithmetic on these; the scheduling barriers keep the pieces apart (without them 1 KB a lane is spilled).
 __device__ __forceinline__ void store_gated_slopes16(const Acc& acc, const LogitsArgs& a, int row_base, int r_end, int col_base) {
   const int lane15 = threadIdx.x & 15, f = a.gated.d_ff;
-  uint2 g[2][F_N], u[2][F_N];
-  auto load = [&](int j, uint2 (&gj)[F_N], uint2 (&uj)[F_N]) __attribute__((always_inline)) {
-    const int row = row_base + j * 16 + lane15;
-    const uint16_t* kept = reinterpret_cast<const uint16_t*>(a.gated.kept) + (size_t)min(row, r_end - 1) * 2 * f;
+  // (four blocks of 16 rows x 16 columns at a time)
+  constexpr int N = F_N / 2;
+  float4 g[2][N], u[2][N];
+  auto load = [&](int p, float4 (&gp)[N], float4 (&up)[N]) __attribute__((always_inline)) {
+    const int row = row_base + (p >> 1) * 16 + lane15;
+    const float* kept = reinterpret_cast<const float*>(a.gated.kept) + (size_t)min(row, r_end - 1) * 2 * f;
 #pragma unroll
-    for (int i = 0; i < F_N; ++i) {
-      const int col = min(col_base + i * 16, f - 4);
-      gj[i] = *reinterpret_cast<const uint2*>(kept + col);
-      uj[i] = *reinterpret_cast<const uint2*>(kept + f + col);
+    for (int i = 0; i < N; ++i) {
+      const int col = min(col_base + ((p & 1) * N + i) * 16, f - 4);
+      gp[i] = *reinterpret_cast<const float4*>(kept + col);
+      up[i] = *reinterpret_cast<const float4*>(kept + f + col);
     }
   };
   load(0, g[0], u[0]);
 #pragma unroll
-  for (int j = 0; j < F_N; ++j) {
+  for (int p = 0; p < 2 * F_N; ++p) {
     __builtin_amdgcn_sched_barrier(0);
-    if (j + 1 < F_N) load(j + 1, g[(j + 1) & 1], u[(j + 1) & 1]);
+    if (p + 1 < 2 * F_N) load(p + 1, g[(p + 1) & 1], u[(p + 1) & 1]);
+    const int j = p >> 1, i0 = (p & 1) * N;
     const int row = row_base + j * 16 + lane15;
     const bool row_ok = row < r_end;
     uint16_t* out_row = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo;
     uint16_t* slopes = reinterpret_cast<uint16_t*>(a.gated.slopes) + (size_t)row * 2 * f;
 #pragma unroll
-    for (int i = 0; i < F_N; i += 2) {
+    for (int i = 0; i < N; i += 2) {
       __builtin_amdgcn_sched_barrier(0);
       z2z_gated::Slopes4 s[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float df[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) df[e] = read_acc(acc[i + h][j][e]);
-        s[h] = z2z_gated::slopes4(df, g[j & 1][i + h], u[j & 1][i + h], a.gated.act);
+        for (int e = 0; e < 4; ++e) df[e] = read_acc(acc[i0 + i + h][j][e]);
+        s[h] = z2z_gated::slopes4(df, g[p & 1][i + h], u[p & 1][i + h], a.gated.act);
       }
-      store_two_blocks(slopes, row_ok, col_base, i, s[0].dg, s[1].dg, f);
-      store_two_blocks(slopes + f, row_ok, col_base, i, s[0].du, s[1].du, f);
-      store_two_blocks(out_row, row_ok, col_base, i, s[0].f, s[1].f, f);
+      store_two_blocks(slopes, row_ok, col_base, i0 + i, s[0].dg, s[1].dg, f);
+      store_two_blocks(slopes + f, row_ok, col_base, i0 + i, s[0].du, s[1].du, f);
+      store_two_blocks(out_row, row_ok, col_base, i0 + i, s[0].f, s[1].f, f);
     }
   }
 }
@@ -1431,9 +1430,9 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
       }
       *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)(r0 + row) * a.ldo + fcol) = z2z_gated::hidden4(x[0], x[1], a.gated.act);
       if (a.gated.kept) {
-        uint16_t* kept = reinterpret_cast<uint16_t*>(a.gated.kept) + (size_t)(r0 + row) * 2 * a.gated.d_ff + fcol;
-        *reinterpret_cast<uint2*>(kept) = z2z_gated::pack4(x[0]);
-        *reinterpret_cast<uint2*>(kept + a.gated.d_ff) = z2z_gated::pack4(x[1]);
+        float* kept = reinterpret_cast<float*>(a.gated.kept) + (size_t)(r0 + row) * 2 * a.gated.d_ff + fcol;
+        *reinterpret_cast<float4*>(kept) = float4{x[0][0], x[0][1], x[0][2], x[0][3]};
+        *reinterpret_cast<float4*>(kept + a.gated.d_ff) = float4{x[1][0], x[1][1], x[1][2], x[1][3]};
       }
       continue;
     }
@@ -1465,9 +1464,9 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
       if (GATE == 2) {
         const float df[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
         const size_t at = (size_t)row * 2 * a.gated.d_ff + col;
-        const uint16_t* kept = reinterpret_cast<const uint16_t*>(a.gated.kept) + at;
-        const z2z_gated::Slopes4 s = z2z_gated::slopes4(df, *reinterpret_cast<const uint2*>(kept),
-                                                        *reinterpret_cast<const uint2*>(kept + a.gated.d_ff), a.gated.act);
+        const float* kept = reinterpret_cast<const float*>(a.gated.kept) + at;
+        const z2z_gated::Slopes4 s = z2z_gated::slopes4(df, *reinterpret_cast<const float4*>(kept),
+                                                        *reinterpret_cast<const float4*>(kept + a.gated.d_ff), a.gated.act);
         uint16_t* slopes = reinterpret_cast<uint16_t*>(a.gated.slopes) + at;
         *reinterpret_cast<uint2*>(slopes) = s.dg;
         *reinterpret_cast<uint2*>(slopes + a.gated.d_ff) = s.du;

@@ -375,14 +375,14 @@ constexpr int32_t kFfnRows = 1 << 22;
 
 }  // namespace
 
-Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, void* d_kept,
+Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, float* d_kept,
                           void* stream) {
   if (!ctx || rows < 0 || (rows > 0 && (!d_X || !d_Y))) return Z2Z_EINVAL;
   if (!aligned16(d_X) || !aligned16(d_residual) || !aligned16(d_Y) || !aligned16(d_kept)) return Z2Z_EINVAL;
   int rc = ffn_ok(ctx, ffn, d_kept != nullptr);
   if (rc != Z2Z_OK) return rc;
   if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
-  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 4;
+  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 8;
   if (overlap_bytes(d_Y, row, d_X, row) || (d_Y != d_residual && overlap_bytes(d_Y, row, d_residual, row)) || overlap_bytes(d_kept, kept, d_X, row) ||
       overlap_bytes(d_kept, kept, d_Y, row) || overlap_bytes(d_kept, kept, d_residual, row))
     return Z2Z_EINVAL;
@@ -393,7 +393,7 @@ Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z
   return z2z_launch_ffn(ctx, d_X, ffn, d_residual, d_Y, false, d_kept, rows, nullptr, ctx->ffn_ws.p, static_cast<hipStream_t>(stream));
 }
 
-Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_kept, const void* d_dY, void* d_dX,
+Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const float* d_kept, const void* d_dY, void* d_dX,
                                    const z2z_ffn* grad, int32_t flags, void* stream) {
   if (!ctx || rows < 0 || (rows > 0 && (!d_X || !d_kept || !d_dY || !d_dX))) return Z2Z_EINVAL;
   if (flags != 0 && flags != Z2Z_GRAD_ADD) return Z2Z_EINVAL;
@@ -402,7 +402,7 @@ Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, 
   int rc = ffn_ok(ctx, ffn, true);
   if (rc != Z2Z_OK) return rc;
   if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
-  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 4;
+  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 8;
   const size_t w2 = (size_t)ctx->cfg.d * ffn->d_ff * 2, w1 = 2 * w2;
   // (what is written against what is read, and against the rest of what is written)
   struct {

@@ -140,5 +140,5 @@ def test_kept_needs_bf16_weights():
     (q1, s1), (q2, s2) = _quantized(ctx, W1, 32), _quantized(ctx, W2, 32)
     block = api.GatedFFN(q1, q2, scale_1=s1, scale_2=s2)
     with pytest.raises(api.Z2ZError) as e:
-        ctx.gated_ffn(X, block, torch.empty_like(X), kept=torch.empty((4, 128), dtype=torch.bfloat16, device="cuda"))
+        ctx.gated_ffn(X, block, torch.empty_like(X), kept=torch.empty((4, 128), device="cuda"))
     assert e.value.code == api.E_UNSUPPORTED
