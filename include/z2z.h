@@ -335,10 +335,20 @@ typedef struct z2z_encoder {
   int32_t n_layers;
   int32_t n_heads;
   int32_t d_ff;             /* width of the feed-forward block (ignored when attention_only) */
-  int32_t attention_only;   /* 1: every layer is the attention layer alone */
+  int32_t attention_only;   /* 1: every layer is the attention layer alone, Z2Z_ENC_GATED: see z2z_gated_encoder */
   const void* pos;          /* [M, d] bf16 learned slot positions, or NULL */
   const z2z_encoder_layer* layers;   /* host array of n_layers */
 } z2z_encoder;
+/* Transformer layers with gated feed-forward blocks (z2z_gated_ffn):  Z = Y + block_l(LayerNorm(Y; ln2)).  Every call that takes a z2z_encoder takes the
+ * `encoder` of this struct with attention_only = Z2Z_ENC_GATED (a value that it has nowhere else); ffn then has the layers' blocks, and of `encoder` d_ff and of its layers w_1,
+ * b_1, w_2 and b_2 are not read.  Blocks over 4-bit weights serve z2z_hyper_encode; z2z_hyper_encode_keep and z2z_hyper_encode_backward need bf16 (else
+ * Z2Z_EUNSUPPORTED), and the latter's `grad` is the `encoder` of such a struct, too: w_1 and w_2 of its blocks receive the matrices' gradients.  All blocks have one d_ff
+ * (else Z2Z_EINVAL). */
+#define Z2Z_ENC_GATED 2
+typedef struct z2z_gated_encoder {
+  z2z_encoder encoder;
+  const z2z_ffn* ffn;       /* host array of n_layers */
+} z2z_gated_encoder;
 int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* encoder, void* d_W_hyper,
                      const int32_t* d_first, int32_t max_new, void* stream);
 
@@ -361,7 +371,7 @@ int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* encoder, 
  * Without the flag the call runs the forward pass again, keeping every layer's rows, then reverse mode over the
  * same steps; activations and gradients between kernels are bf16, sums fp32; passes of up to 65536 slot rows
  * (matrix gradients of later passes add to the bf16 result of the earlier ones).  Work space (about
- * 2 * (n_layers * (10 d + 2 d_ff) + 9 d + d_ff) bytes per slot row) is library scratch, Z2Z_ENOMEM beyond 200 GB.
+ * 2 * (n_layers * (10 d + 2 d_ff) + 9 d + d_ff) bytes per slot row; 2 * (n_layers * (10 d + 4 d_ff) + 9 d + 3 d_ff) with gated blocks) is library scratch, Z2Z_ENOMEM beyond 200 GB.
  * Restrictions and errors as for z2z_hyper_encode. */
 #define Z2Z_ENC_KEPT 1
 int z2z_hyper_encode_backward(z2z_ctx* ctx, const void* d_E, const z2z_encoder* encoder, const void* d_dW_hyper,

@@ -17,6 +17,7 @@ taken here, layer by layer, is the standard pre-norm transformer encoder:
         O_h = softmax_rows(S) V_h
     Y     = X + O Wo^T + bo                                   -- "attention layer"
     Z     = Y + GELU(LayerNorm_2(Y) W1^T + b1) W2^T + b2      -- "transformer layer" (GELU with erf)
+            (gated: Z = Y + (act(N W1[:f]^T) * (N W1[f:]^T)) W2^T, N = LayerNorm_2(Y))
     h     = mean over the L real slots of the last layer's output
 
 LayerNorm is over the d features with the biased variance and eps inside the
@@ -35,6 +36,7 @@ from typing import Sequence, Tuple
 import numpy as np
 from scipy.special import erf
 
+from .ffn import act as gate_act
 from .numfmt import round_to_storage, to_f64
 
 EPS = 1e-5
@@ -70,11 +72,14 @@ def attention(A: np.ndarray, w_qkv: np.ndarray, b_qkv: np.ndarray, w_o: np.ndarr
 
 def widen_encoder(enc: dict, dtype: str) -> dict:
     """The encoder's parameters as float64 arrays (exact widening of what is stored)."""
-    out = dict(n_heads=int(enc["n_heads"]), attention_only=bool(enc["attention_only"]),
+    out = dict(n_heads=int(enc["n_heads"]), attention_only=bool(enc["attention_only"]), gated=enc.get("gated"),
                pos=None if enc.get("pos") is None else to_f64(enc["pos"], dtype), layers=[])
     for lay in enc["layers"]:
         w = {}
         for k, v in lay.items():
+            if v.dtype == np.float64:                    # (values that are stored in fewer bits)
+                w[k] = v
+                continue
             w[k] = to_f64(v, dtype) if k.startswith("w_") else np.asarray(v, dtype=np.float32).astype(np.float64)
         out["layers"].append(w)
     return out
@@ -85,7 +90,11 @@ def encode_entry(X: np.ndarray, enc64: dict) -> np.ndarray:
     for lay in enc64["layers"]:
         A = layer_norm(X, lay["ln1_g"], lay["ln1_b"])
         X = X + attention(A, lay["w_qkv"], lay["b_qkv"], lay["w_o"], lay["b_o"], enc64["n_heads"])
-        if not enc64["attention_only"]:
+        if enc64["gated"]:
+            GU = layer_norm(X, lay["ln2_g"], lay["ln2_b"]) @ lay["w_1"].T
+            f = GU.shape[1] // 2
+            X = X + (gate_act(GU[:, :f], enc64["gated"])[0] * GU[:, f:]) @ lay["w_2"].T
+        elif not enc64["attention_only"]:
             F = gelu(layer_norm(X, lay["ln2_g"], lay["ln2_b"]) @ lay["w_1"].T + lay["b_1"])
             X = X + F @ lay["w_2"].T + lay["b_2"]
     return X.mean(axis=0)
@@ -176,7 +185,11 @@ def encode_entry_backward(X0: np.ndarray, enc64: dict, dh_out: np.ndarray, grads
         Y = X + attention(A, lay["w_qkv"], lay["b_qkv"], lay["w_o"], lay["b_o"], enc64["n_heads"])
         xs.append((X, A, Y))
         X = Y
-        if not enc64["attention_only"]:
+        if enc64["gated"]:
+            GU = layer_norm(Y, lay["ln2_g"], lay["ln2_b"]) @ lay["w_1"].T
+            f = GU.shape[1] // 2
+            X = Y + (gate_act(GU[:, :f], enc64["gated"])[0] * GU[:, f:]) @ lay["w_2"].T
+        elif not enc64["attention_only"]:
             N2 = layer_norm(Y, lay["ln2_g"], lay["ln2_b"])
             U = N2 @ lay["w_1"].T + lay["b_1"]
             X = Y + gelu(U) @ lay["w_2"].T + lay["b_2"]
@@ -184,7 +197,20 @@ def encode_entry_backward(X0: np.ndarray, enc64: dict, dh_out: np.ndarray, grads
     dX = np.tile(dh_out / L, (L, 1))             # h = mean over the L real slots
     for lay, g, (Xin, A, Y) in zip(reversed(enc64["layers"]), reversed(grads["layers"]), reversed(xs)):
         dY = dX
-        if not enc64["attention_only"]:
+        if enc64["gated"]:
+            N2 = layer_norm(Y, lay["ln2_g"], lay["ln2_b"])
+            GU = N2 @ lay["w_1"].T
+            f = GU.shape[1] // 2
+            value, slope = gate_act(GU[:, :f], enc64["gated"])
+            g["w_2"] += dX.T @ (value * GU[:, f:])
+            dF = dX @ lay["w_2"]
+            dGU = np.concatenate([dF * GU[:, f:] * slope, dF * value], axis=1)
+            g["w_1"] += dGU.T @ N2
+            dYn, dg, db = layer_norm_backward(dGU @ lay["w_1"], Y, lay["ln2_g"])
+            g["ln2_g"] += dg
+            g["ln2_b"] += db
+            dY = dX + dYn
+        elif not enc64["attention_only"]:
             N2 = layer_norm(Y, lay["ln2_g"], lay["ln2_b"])
             U = N2 @ lay["w_1"].T + lay["b_1"]
             F = gelu(U)

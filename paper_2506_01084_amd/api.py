@@ -27,6 +27,7 @@ E_INVAL, E_NOMEM, E_HIP, E_UNSUPPORTED, E_LIMIT, E_CAPTURE = -1, -2, -3, -4, -5,
 STATIC_PARTS = 1 << 22
 
 ENC_KEPT = 1
+ENC_GATED = 2
 GRAD_ADD = 1
 ACT_SILU, ACT_GELU = 0, 1
 MAX_BEAMS, MAX_PICK, MAX_TEACHER, MAX_GRADIENTS = 32, 64, 256, 4096
@@ -51,36 +52,13 @@ class EncoderDesc(ctypes.Structure):
                 ("pos", c_void_p), ("layers", ctypes.POINTER(EncoderLayer))]
 
 
-class Encoder:
-    """Device-resident parameters of a learned hyper-encoder, marshalled into the C structs.
-
-    `params`: n_heads, attention_only, d_ff, pos ([M, d] tensor or None) and layers, a list of dicts of
-    device tensors named as the fields of z2z_encoder_layer (matrices in the context's dtype, vectors float32).
-    The object keeps the tensors alive."""
-
-    def __init__(self, params: dict, torch_dtype):
-        self.params = params
-        layers = params["layers"]
-        self._arr = (EncoderLayer * len(layers))()
-        for l, lay in enumerate(layers):
-            for name, _ in EncoderLayer._fields_:
-                t = lay.get(name)
-                if t is None:
-                    setattr(self._arr[l], name, None)
-                else:
-                    setattr(self._arr[l], name, _ptr(t, torch_dtype if name.startswith("w_") else torch.float32))
-        self.desc = EncoderDesc()
-        self.desc.n_layers = len(layers)
-        self.desc.n_heads = int(params["n_heads"])
-        self.desc.d_ff = int(params.get("d_ff", 0))
-        self.desc.attention_only = 1 if params["attention_only"] else 0
-        self.desc.pos = _ptr(params.get("pos"), torch_dtype)
-        self.desc.layers = ctypes.cast(self._arr, ctypes.POINTER(EncoderLayer))
-
-
 class FfnDesc(ctypes.Structure):
     _fields_ = [("d_ff", c_int32), ("act", c_int32), ("group", c_int32), ("reserved", c_int32), ("w_1", c_void_p), ("w_2", c_void_p),
                 ("scale_1", c_void_p), ("scale_2", c_void_p)]
+
+
+class GatedEncoderDesc(ctypes.Structure):
+    _fields_ = [("encoder", EncoderDesc), ("ffn", ctypes.POINTER(FfnDesc))]
 
 
 def q4_shapes(rows: int, cols: int, group: int):
@@ -115,6 +93,39 @@ class GatedFFN:
             self.desc.w_1, self.desc.w_2 = _ptr(w_1, torch.int32), _ptr(w_2, torch.int32)
             self.desc.scale_1, self.desc.scale_2 = _ptr(scale_1, torch.bfloat16), _ptr(scale_2, torch.bfloat16)
         self.desc.d_ff = self.d_ff
+
+
+class Encoder:
+    """Device-resident parameters of a learned hyper-encoder, marshalled into the C structs.
+
+    `params`: n_heads, attention_only, d_ff, pos ([M, d] tensor or None) and layers, a list of dicts of
+    device tensors named as the fields of z2z_encoder_layer (matrices in the context's dtype, vectors float32).
+    With ffn, a list of GatedFFN, the layers have these blocks in place of w_1, b_1, w_2 and b_2.  The object keeps the tensors alive."""
+
+    def __init__(self, params: dict, torch_dtype):
+        self.params = params
+        layers = params["layers"]
+        self._arr = (EncoderLayer * len(layers))()
+        for l, lay in enumerate(layers):
+            for name, _ in EncoderLayer._fields_:
+                t = lay.get(name)
+                if t is None:
+                    setattr(self._arr[l], name, None)
+                else:
+                    setattr(self._arr[l], name, _ptr(t, torch_dtype if name.startswith("w_") else torch.float32))
+        ffn = params.get("ffn")
+        self._gated = GatedEncoderDesc()
+        self.desc = self._gated.encoder
+        self.desc.n_layers = len(layers)
+        self.desc.n_heads = int(params["n_heads"])
+        self.desc.d_ff = int(params.get("d_ff", 0))
+        self.desc.attention_only = ENC_GATED if ffn is not None else 1 if params["attention_only"] else 0
+        if ffn is not None:
+            assert len(ffn) == len(layers)
+            self._ffn = (FfnDesc * len(ffn))(*[f.desc for f in ffn])
+            self._gated.ffn = ctypes.cast(self._ffn, ctypes.POINTER(FfnDesc))
+        self.desc.pos = _ptr(params.get("pos"), torch_dtype)
+        self.desc.layers = ctypes.cast(self._arr, ctypes.POINTER(EncoderLayer))
 
 
 class GradientDesc(ctypes.Structure):

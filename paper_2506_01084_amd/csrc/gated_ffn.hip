@@ -27,36 +27,47 @@ size_t z2z_ffn_work(const z2z_ffn* f, int d, int rows) {
   return padded((size_t)rows * f->d_ff * 2) + (f->group && rows > kExpandRows ? (size_t)3 * d * f->d_ff * 2 : 0);
 }
 
-int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* residual, void* Y, bool stream_f32, void* kept, int R, const int32_t* rows_dev,
-                   void* work, hipStream_t s) {
+int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
+                          hipStream_t s) {
   const int d = c->cfg.d, dff = f->d_ff;
   unsigned char* F = reinterpret_cast<unsigned char*>(work);
-  const void *w1 = f->w_1, *w2 = f->w_2;
+  const void* w1 = f->w_1;
+  *out = z2z_ffn_out{F, f->w_2, nullptr, 0, dff, false};
   if (f->group && R <= kExpandRows) {
+    out->scale = f->scale_2;
+    out->group = f->group;
     const float* partial = nullptr;
     int ksplit = 0;
-    int rc = z2z_launch_q4_parts(c, X, w1, f->scale_1, f->group, R, rows_dev, 2 * dff, d, &partial, &ksplit, s);
+    const int rc = z2z_launch_q4_parts(c, X, w1, f->scale_1, f->group, R, rows_dev, 2 * dff, d, &partial, &ksplit, s);
     if (rc != Z2Z_OK) return rc;
-    rc = z2z_launch_gated_sum(partial, ksplit, R, rows_dev, dff, f->act, F, nullptr, s);
-    if (rc != Z2Z_OK) return rc;
-    rc = z2z_launch_q4_parts(c, F, w2, f->scale_2, f->group, R, rows_dev, d, dff, &partial, &ksplit, s);
-    if (rc != Z2Z_OK) return rc;
-    return z2z_launch_linear_sum(partial, ksplit, R, rows_dev, d, residual, Y, stream_f32, s);
+    return z2z_launch_gated_sum(partial, ksplit, R, rows_dev, dff, f->act, F, nullptr, s);
   }
   if (f->group) {
-    unsigned char* e = F + padded((size_t)R * dff * 2);
-    int rc = z2z_launch_expand_q4(w1, f->scale_1, 2 * dff, d, f->group, e, s);
+    unsigned char *e1 = F + padded((size_t)R * dff * 2), *e2 = e1 + (size_t)2 * dff * d * 2;
+    int rc = z2z_launch_expand_q4(w1, f->scale_1, 2 * dff, d, f->group, e1, s);
     if (rc != Z2Z_OK) return rc;
-    rc = z2z_launch_expand_q4(w2, f->scale_2, d, dff, f->group, e + (size_t)2 * dff * d * 2, s);
+    rc = z2z_launch_expand_q4(f->w_2, f->scale_2, d, dff, f->group, e2, s);
     if (rc != Z2Z_OK) return rc;
-    w1 = e;
-    w2 = e + (size_t)2 * dff * d * 2;
+    w1 = e1;
+    out->w = e2;
   }
   // (few rows: does anything of the weights stay in the memory-side cache until the next call?)
-  const bool once = (size_t)3 * d * dff * sizeof(uint16_t) > z2z_logits::kKeepBytes;
-  const int rc = z2z_launch_gated_hidden(c, X, w1, f->act, F, kept, R, rows_dev, dff, d, s, once);
+  out->once = (size_t)3 * d * dff * sizeof(uint16_t) > z2z_logits::kKeepBytes;
+  return z2z_launch_gated_hidden(c, X, w1, f->act, F, kept, R, rows_dev, dff, d, s, out->once);
+}
+
+int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* residual, void* Y, bool stream_f32, void* kept, int R, const int32_t* rows_dev,
+                   void* work, hipStream_t s) {
+  const int d = c->cfg.d;
+  z2z_ffn_out o;
+  int rc = z2z_launch_ffn_hidden(c, X, f, kept, R, rows_dev, work, &o, s);
   if (rc != Z2Z_OK) return rc;
-  return z2z_launch_linear(c, F, w2, nullptr, residual, 0, Y, R, rows_dev, d, dff, s, stream_f32, nullptr, once);
+  if (!o.group) return z2z_launch_linear(c, o.F, o.w, nullptr, residual, 0, Y, R, rows_dev, d, o.d_ff, s, stream_f32, nullptr, o.once);
+  const float* partial = nullptr;
+  int ksplit = 0;
+  rc = z2z_launch_q4_parts(c, o.F, o.w, o.scale, o.group, R, rows_dev, d, o.d_ff, &partial, &ksplit, s);
+  if (rc != Z2Z_OK) return rc;
+  return z2z_launch_linear_sum(partial, ksplit, R, rows_dev, d, residual, Y, stream_f32, s);
 }
 
 size_t z2z_ffn_backward_work(const z2z_ffn* f, int rows) { return padded((size_t)rows * f->d_ff * 2) + (size_t)rows * 2 * f->d_ff * 2; }

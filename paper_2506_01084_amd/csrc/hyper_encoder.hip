@@ -5,7 +5,9 @@
 // slots, padding masked out as keys, mean of the real slots at the end:
 //
 //   X_i = E[y_i] + P_i;  A = LN1(X);  QKV = A Wqkv^T + b;  O = softmax(Q K^T / sqrt(d_head)) V per head;
-//   Y = X + O Wo^T + bo;  Z = Y + GELU(LN2(Y) W1^T + b1) W2^T + b2  (transformer layers);  h = mean_i Z_i.
+//   Y = X + O Wo^T + bo;  Z = Y + GELU(LN2(Y) W1^T + b1) W2^T + b2  (transformer layers);  h = mean_i Z_i
+//
+// (or with the gated block of gated_ffn.hip in place of the last).
 //
 // All entries of a pass are batched, and only their real slots are rows: a one-workgroup scan over the entry
 // lengths gives every entry its first row (padding slots and missing entries take no rows at all; a quarter
@@ -18,6 +20,8 @@
 // the matrix products (LayerNorm outputs, q | k | v, attention outputs, the hidden layer) are bf16;
 // accumulation and statistics are fp32.
 #include "logits_common.h"
+
+#include <algorithm>
 
 namespace {
 
@@ -861,7 +865,7 @@ bool z2z_hyper_encode_ok(const z2z_ctx* c, const z2z_encoder* enc) {
   if (enc->n_heads < 1 || d % enc->n_heads != 0) return false;
   const int dh = d / enc->n_heads;
   if (dh < 8 || dh > 512 || (dh & (dh - 1)) != 0) return false;
-  if (!enc->attention_only && (enc->d_ff < 64 || enc->d_ff % 64 != 0)) return false;
+  if (!enc->attention_only && (enc->d_ff < 64 || enc->d_ff % 64 != 0)) return false;      // (gated blocks: checked by themselves)
   return true;
 }
 
@@ -871,9 +875,12 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
   if (cap == 0) return Z2Z_OK;
   const bool incremental = first || max_new > 0;
   const int units = incremental ? (max_new < 1 ? cap : (max_new < cap ? max_new : cap)) : cap;
+  const z2z_ffn* gated = z2z_gated_layers(enc);
   const int dff = enc->attention_only ? 0 : enc->d_ff;
   // (few rows: does anything of the weights stay in the memory-side cache until the next call?)
-  const bool once = (size_t)enc->n_layers * ((size_t)4 * d + (size_t)2 * dff) * d * sizeof(uint16_t) > z2z_logits::kKeepBytes;
+  size_t weights = (size_t)enc->n_layers * ((size_t)4 * d + (size_t)2 * dff) * d * sizeof(uint16_t);
+  for (int l = 0; gated && l < enc->n_layers; ++l) weights += (size_t)3 * d * gated[l].d_ff * (gated[l].group ? 1 : 4) / 2;
+  const bool once = weights > z2z_logits::kKeepBytes;
   // rows per pass: all sequences, u_step entries each, M slots per entry
   long long u_step = 0;
   size_t R_max = 0, n_units_max = 0, index_bytes = 0;
@@ -887,7 +894,9 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
     n_units_max = (size_t)B * (size_t)u_step;
     index_bytes = ((n_units_max + 1 + R_max) * sizeof(int32_t) + 255) & ~(size_t)255;
     // per row: the stream X and Y in fp32 (2 x 4 bytes x d), A, O (d), QKV (3d) and F (d_ff) in bf16
-    return R_max * ((size_t)8 * d + ((size_t)2 * d + (size_t)3 * d + (size_t)dffp) * 2) + index_bytes;
+    size_t ffn_bytes = R_max * dffp * 2;
+    for (int l = 0; gated && l < enc->n_layers; ++l) ffn_bytes = std::max(ffn_bytes, z2z_ffn_work(gated + l, d, (int)R_max));
+    return R_max * ((size_t)8 * d + ((size_t)2 * d + (size_t)3 * d) * 2) + ffn_bytes + index_bytes;
   };
   auto room = [&](size_t need) -> int { return z2z_work_reserve(c, &c->enc_ws, need, s); };
   // (where the buffer cannot grow that far, or not at all under capture, passes of half as many rows.  What the device has refused is not asked
@@ -940,15 +949,17 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
     // (gamma, beta -> A) or, behind the last layer, the mean over an entry's rows.  Where K is split those
     // add up the partial tiles themselves; else *fused stays false and only `out` is written.
     auto layer_out = [&](const uint16_t* in, const void* w, const float* bias, const float* residual, float* out, int K,
-                         const float* gamma, const float* beta, bool* fused) -> int {
+                         const float* gamma, const float* beta, bool* fused, const z2z_ffn_out* four_bits = nullptr) -> int {
       Parts parts = {};
       *fused = false;
       const z2z_linear_pitch pitch = {dffp, dff, d};
-      const bool padded = in == F && dffp != dff;
+      const bool padded = in == F && !gated && dffp != dff;
       int ret = Z2Z_OK;
       // (with more rows -- K is split there too in a narrow encoder -- a wave per row is the better LayerNorm: 6144 rows,
       // d = 256: the pass 275 us fused, 267 in launches of their own)
-      if (!padded && R <= E_FEW_ROWS)
+      if (four_bits)
+        ret = z2z_launch_q4_parts(c, in, w, four_bits->scale, four_bits->group, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s);
+      else if (!padded && R <= E_FEW_ROWS)
         ret = z2z_launch_linear_parts(c, in, w, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s, once);
       if (ret != Z2Z_OK) return ret;
       if (parts.ksplit == 0)
@@ -987,7 +998,7 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
                          reinterpret_cast<const uint4*>(QKV), reinterpret_cast<uint4*>(O), dh / 8, scale, groups,
                          n_units);
       bool fused = false;
-      if (enc->attention_only) {
+      if (enc->attention_only && !gated) {
         rc = layer_out(O, lay.w_o, lay.b_o, x, y, d, next ? next->ln1_g : nullptr, next ? next->ln1_b : nullptr, &fused);
         if (rc != Z2Z_OK) return rc;
         float* t = x;
@@ -999,11 +1010,18 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
         if (!fused)
           hipLaunchKernelGGL(enc_norm_kernel<false>, dim3(row_blocks), dim3(256), 0, s, m, nullptr, nullptr, y,
                              reinterpret_cast<uint4*>(A), lay.ln2_g, lay.ln2_b, n_units);
-        const z2z_linear_pitch to_wide = {d, d, dffp};
-        rc = z2z_launch_linear(c, A, lay.w_1, lay.b_1, nullptr, 1, F, R, rows_dev, dff, d, s, false,
-                               dffp != dff ? &to_wide : nullptr, once);
-        if (rc != Z2Z_OK) return rc;
-        rc = layer_out(F, lay.w_2, lay.b_2, y, x, dff, next ? next->ln1_g : nullptr, next ? next->ln1_b : nullptr, &fused);
+        if (gated) {
+          z2z_ffn_out o;
+          rc = z2z_launch_ffn_hidden(c, A, gated + l, nullptr, R, rows_dev, F, &o, s);
+          if (rc != Z2Z_OK) return rc;
+          rc = layer_out(F, o.w, nullptr, y, x, o.d_ff, next ? next->ln1_g : nullptr, next ? next->ln1_b : nullptr, &fused, o.group ? &o : nullptr);
+        } else {
+          const z2z_linear_pitch to_wide = {d, d, dffp};
+          rc = z2z_launch_linear(c, A, lay.w_1, lay.b_1, nullptr, 1, F, R, rows_dev, dff, d, s, false,
+                                 dffp != dff ? &to_wide : nullptr, once);
+          if (rc != Z2Z_OK) return rc;
+          rc = layer_out(F, lay.w_2, lay.b_2, y, x, dff, next ? next->ln1_g : nullptr, next ? next->ln1_b : nullptr, &fused);
+        }
         if (rc != Z2Z_OK) return rc;
       }
       normed = fused && next;
@@ -1050,25 +1068,29 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
   if (cap == 0) return Z2Z_OK;
   if (mode != 0 && (long long)B * cap * M > 65536) return Z2Z_EUNSUPPORTED;
   const int nl = enc->n_layers;
-  const bool ffn = !enc->attention_only;
-  const int dff = ffn ? enc->d_ff : 0;
+  const z2z_ffn *gated = z2z_gated_layers(enc), *gated_grad = grad ? z2z_gated_layers(grad) : nullptr;
+  const bool ffn = gated || !enc->attention_only;
+  const int dff = gated ? gated[0].d_ff : ffn ? enc->d_ff : 0;
   long long u_step = 65536 / ((long long)B * M);
   if (u_step < 1) u_step = 1;
   if (u_step > cap) u_step = cap;
   const size_t R_max = (size_t)B * (size_t)u_step * M;
-  const int dffp = ffn_pitch(c, B, M, cap, (int)u_step, d, dff);
+  const int dffp = gated ? dff : ffn_pitch(c, B, M, cap, (int)u_step, d, dff);
   const size_t n_units_max = (size_t)B * (size_t)u_step;
   const size_t index_bytes = ((n_units_max + 1 + R_max) * sizeof(int32_t) + 255) & ~(size_t)255;
   const size_t pos_bytes = ((size_t)Z2Z_MAX_M * d * sizeof(float) + 255) & ~(size_t)255;
   // in units of bf16 elements (an fp32 element counts as two): per layer what LayerSave names (Xin and Y fp32);
   // the last layer's output (fp32); the running gradients dX dY dN dO (d each), dQKV (3d), dF (d_ff)
-  const size_t per_layer = R_max * ((size_t)10 * d + (size_t)2 * dffp);
-  const size_t elems = (size_t)nl * per_layer + R_max * ((size_t)7 * d + dffp) + R_max * 2 * d;
+  // (gated blocks: what they keep, 2 d_ff fp32 a row, in place of the layer before and behind the activation, and their work space in place of dF)
+  const size_t per_layer = R_max * ((size_t)10 * d + (size_t)(gated ? 4 : 2) * dffp);
+  const size_t ffn_work = gated ? (z2z_ffn_backward_work(gated, (int)R_max) + 255) / 256 * 128 : R_max * (size_t)dffp;
+  const size_t elems = (size_t)nl * per_layer + R_max * (size_t)7 * d + ffn_work + R_max * 2 * d;
   const size_t nb_bytes = (R_max * sizeof(float2) + 255) & ~(size_t)255;   // mean and rstd of every row of a LayerNorm
   const size_t need = index_bytes + pos_bytes + nb_bytes + elems * 2;
   if (need > ((size_t)200 << 30)) return Z2Z_ENOMEM;
   // the rows a mode-1 call left are those of this encoder's shape only if the layout is the same
-  if (mode == 2 && (!c->enc_kept || c->enc_kept_need != need || c->enc_kept_E != E)) return Z2Z_EINVAL;
+  const size_t kept_as = need | (gated ? 1 : 0);     // (sizes are even)
+  if (mode == 2 && (!c->enc_kept || c->enc_kept_need != kept_as || c->enc_kept_E != E)) return Z2Z_EINVAL;
   c->enc_kept = false;
   int rc = z2z_work_reserve(c, &c->enc_bwd_ws, need, s);
   if (rc != Z2Z_OK) return rc;
@@ -1091,8 +1113,8 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
     sv[l].QKV = take(R_max * 3 * d);
     sv[l].O = take(R_max * d);
     sv[l].N2 = take(R_max * d);
-    sv[l].U = take(R_max * (size_t)dffp);
-    sv[l].F = take(R_max * (size_t)dffp);
+    sv[l].U = take(R_max * (size_t)dffp * (gated ? 4 : 1));
+    sv[l].F = gated ? nullptr : take(R_max * (size_t)dffp);
   }
   float* Xout = take_f32(R_max * d);
   uint16_t* dX = take(R_max * d);
@@ -1100,7 +1122,7 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
   uint16_t* dN = take(R_max * d);
   uint16_t* dO = take(R_max * d);
   uint16_t* dQKV = take(R_max * 3 * d);
-  uint16_t* dF = take(R_max * (size_t)dffp);
+  uint16_t* dF = take(ffn_work);
 
   RowMap m;
   m.size = c->st.size;
@@ -1134,6 +1156,8 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
     if (ffn) {
       clear(g.ln2_g, d);
       clear(g.ln2_b, d);
+    }
+    if (ffn && !gated) {
       clear(g.b_1, dff);
       clear(g.b_2, d);
     }
@@ -1184,6 +1208,10 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
       if (ffn) {
         hipLaunchKernelGGL(enc_norm_kernel<false>, dim3(row_blocks), dim3(256), 0, s, m, nullptr, nullptr, v.Y,
                            reinterpret_cast<uint4*>(v.N2), lay.ln2_g, lay.ln2_b, n_units);
+      }
+      if (gated) {
+        Z2Z_TRY_RC(z2z_launch_ffn(c, v.N2, gated + l, v.Y, next, true, v.U, R, rows_dev, dF, s));
+      } else if (ffn) {
         Z2Z_TRY_RC(z2z_launch_linear(c, v.N2, lay.w_1, lay.b_1, nullptr, 0, v.U, R, rows_dev, dff, d, s, false, to_wide));
         hipLaunchKernelGGL(enc_gelu_kernel, dim3(flat_grid((size_t)R * dffp / 8)), dim3(256), 0, s,
                            reinterpret_cast<const uint4*>(v.U), reinterpret_cast<uint4*>(v.F), dffp / 8, rows_dev);
@@ -1215,7 +1243,11 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
       const LayerSave& v = sv[l];
       const void* acc = nullptr;                     // weight gradients of later passes add to the earlier ones
       uint16_t* dy = dX;                             // gradient at Y (attention layers: the layer's output)
-      if (ffn) {
+      if (gated) {
+        Z2Z_TRY_RC(z2z_launch_ffn_backward(c, v.N2, gated + l, v.U, dX, dN, gated_grad + l, pass > 0, R, rows_dev, dF, s));
+        norm_backward(dN, v.Y, lay.ln2_g, dX, dY, g.ln2_g, g.ln2_b);
+        dy = dY;
+      } else if (ffn) {
         colsum_to(dX, d, d, rows_dev, const_cast<float*>(g.b_2), s);
         Z2Z_TRY_RC(z2z_launch_linear_input(c, dX, d, lay.w_2, dff, d, nullptr, dF, dffp, R, rows_dev, dff, d, s));
         acc = pass > 0 ? g.w_2 : nullptr;
@@ -1255,7 +1287,7 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
   if (mode == 1) {
     Z2Z_HIP_TRY(hipGetLastError());
     c->enc_kept = true;
-    c->enc_kept_need = need;
+    c->enc_kept_need = kept_as;
     c->enc_kept_E = E;
     return Z2Z_OK;
   }

@@ -302,6 +302,19 @@ Z2Z_API int z2z_hyper_embed(z2z_ctx* ctx, const void* d_E, void* d_W_hyper, cons
 
 namespace {
 
+// of a gated block on a context of width d: its description's numbers, and its pointers
+int ffn_ok(const z2z_ctx* c, const z2z_ffn* f, bool bf16_only) {
+  if (!f || f->d_ff < 1 || f->reserved != 0 || (f->act != Z2Z_ACT_SILU && f->act != Z2Z_ACT_GELU)) return Z2Z_EINVAL;
+  if (!f->w_1 || !f->w_2 || !aligned16(f->w_1) || !aligned16(f->w_2)) return Z2Z_EINVAL;
+  if (f->group != 0 && f->group != 32 && f->group != 64 && f->group != 128) return Z2Z_EINVAL;
+  if (f->group != 0 && (!f->scale_1 || !f->scale_2 || !aligned16(f->scale_1) || !aligned16(f->scale_2))) return Z2Z_EINVAL;
+  const int d = c->cfg.d;
+  if (c->cfg.dtype != Z2Z_BF16 || !c->fast_ready || d % 64 != 0 || f->d_ff % 64 != 0) return Z2Z_EUNSUPPORTED;
+  if (((long long)f->d_ff + 128) * d * 2 >= (1LL << 31)) return Z2Z_EUNSUPPORTED;       // (bytes of a projection: 32-bit offsets)
+  if (f->group != 0 && (bf16_only || d % f->group != 0 || f->d_ff % f->group != 0)) return Z2Z_EUNSUPPORTED;
+  return Z2Z_OK;
+}
+
 // every pointer a layer of the description must carry, present and 16-byte aligned
 bool encoder_pointers_ok(const z2z_encoder* enc) {
   if (!enc || !enc->layers) return false;
@@ -312,13 +325,29 @@ bool encoder_pointers_ok(const z2z_encoder* enc) {
     const void* always[] = {y.ln1_g, y.ln1_b, y.w_qkv, y.b_qkv, y.w_o, y.b_o};
     for (const void* p : always)
       if (!p || !aligned16(p)) return false;
-    if (!enc->attention_only) {
+    if (enc->attention_only == Z2Z_ENC_GATED) {
+      const z2z_ffn* f = z2z_gated_layers(enc);
+      const void* ffn[] = {y.ln2_g, y.ln2_b, f ? f[l].w_1 : nullptr, f ? f[l].w_2 : nullptr};
+      for (const void* p : ffn)
+        if (!p || !aligned16(p)) return false;
+    } else if (!enc->attention_only) {
       const void* ffn[] = {y.ln2_g, y.ln2_b, y.w_1, y.b_1, y.w_2, y.b_2};
       for (const void* p : ffn)
         if (!p || !aligned16(p)) return false;
     }
   }
   return true;
+}
+
+// the rest of a description with gated blocks; training: over bf16 weights
+int gated_layers_ok(const z2z_ctx* c, const z2z_encoder* enc, bool training) {
+  const z2z_ffn* f = z2z_gated_layers(enc);
+  for (int l = 0; f && l < enc->n_layers; ++l) {
+    const int rc = ffn_ok(c, f + l, training);
+    if (rc != Z2Z_OK) return rc;
+    if (f[l].d_ff != f[0].d_ff) return Z2Z_EINVAL;
+  }
+  return Z2Z_OK;
 }
 
 }  // namespace
@@ -329,6 +358,8 @@ Z2Z_API int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* e
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
+  const int ok = gated_layers_ok(ctx, enc, false);
+  if (ok != Z2Z_OK) return ok;
   note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_hyper_encode(ctx, d_E, enc, d_W_hyper, d_first, max_new, static_cast<hipStream_t>(stream));
 }
@@ -338,6 +369,8 @@ Z2Z_API int z2z_hyper_encode_keep(z2z_ctx* ctx, const void* d_E, const z2z_encod
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
+  const int ok = gated_layers_ok(ctx, enc, true);
+  if (ok != Z2Z_OK) return ok;
   note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_hyper_encode_train(ctx, 1, d_E, enc, d_W_hyper, nullptr, nullptr, nullptr,
                                        static_cast<hipStream_t>(stream));
@@ -351,25 +384,15 @@ Z2Z_API int z2z_hyper_encode_backward(z2z_ctx* ctx, const void* d_E, const z2z_e
   if (flags & ~Z2Z_ENC_KEPT) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_dW_hyper) || !aligned16(d_dE)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
+  if ((enc->attention_only == Z2Z_ENC_GATED) != (grad->attention_only == Z2Z_ENC_GATED)) return Z2Z_EINVAL;
+  const int ok = gated_layers_ok(ctx, enc, true);
+  if (ok != Z2Z_OK) return ok;
   note_capture(ctx, static_cast<hipStream_t>(stream));
   return z2z_launch_hyper_encode_train(ctx, (flags & Z2Z_ENC_KEPT) ? 2 : 0, d_E, enc, nullptr, d_dW_hyper, grad, d_dE,
                                        static_cast<hipStream_t>(stream));
 }
 
 namespace {
-
-// of a gated block on a context of width d: its description's numbers, and its pointers
-int ffn_ok(const z2z_ctx* c, const z2z_ffn* f, bool bf16_only) {
-  if (!f || f->d_ff < 1 || f->reserved != 0 || (f->act != Z2Z_ACT_SILU && f->act != Z2Z_ACT_GELU)) return Z2Z_EINVAL;
-  if (!f->w_1 || !f->w_2 || !aligned16(f->w_1) || !aligned16(f->w_2)) return Z2Z_EINVAL;
-  if (f->group != 0 && f->group != 32 && f->group != 64 && f->group != 128) return Z2Z_EINVAL;
-  if (f->group != 0 && (!f->scale_1 || !f->scale_2 || !aligned16(f->scale_1) || !aligned16(f->scale_2))) return Z2Z_EINVAL;
-  const int d = c->cfg.d;
-  if (c->cfg.dtype != Z2Z_BF16 || !c->fast_ready || d % 64 != 0 || f->d_ff % 64 != 0) return Z2Z_EUNSUPPORTED;
-  if (((long long)f->d_ff + 128) * d * 2 >= (1LL << 31)) return Z2Z_EUNSUPPORTED;       // (bytes of a projection: 32-bit offsets)
-  if (f->group != 0 && (bf16_only || d % f->group != 0 || f->d_ff % f->group != 0)) return Z2Z_EUNSUPPORTED;
-  return Z2Z_OK;
-}
 
 constexpr int32_t kFfnRows = 1 << 22;
 

@@ -198,6 +198,19 @@ int z2z_launch_beam_pick(z2z_ctx* c, const float* logits, const float* part_m, c
 int z2z_launch_part_max(z2z_ctx* c, const float* logits, float* part_m, int* n_parts, hipStream_t s);   // parts of 256 columns
 int z2z_launch_codebook_reorder(z2z_ctx* c, int32_t beams, const int32_t* source, void* W_hyper, hipStream_t s);
 
+// The layers' gated blocks where the encoder has them, else nullptr (an encoder with the flag is the first member of a z2z_gated_encoder).
+inline const z2z_ffn* z2z_gated_layers(const z2z_encoder* enc) {
+  return enc->attention_only == Z2Z_ENC_GATED ? reinterpret_cast<const z2z_gated_encoder*>(enc)->ffn : nullptr;
+}
+// The gated block's first product alone, and what its second is of: F [R, d_ff] and w [d, d_ff], bf16 or (group) in 4 bits.
+struct z2z_ffn_out {
+  void* F;
+  const void *w, *scale;
+  int group, d_ff;
+  bool once;
+};
+int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
+                          hipStream_t s);
 // The gated block on R rows (or the first *rows_dev of them), with work space of z2z_ffn_work bytes; stream_f32: residual and Y are fp32.
 size_t z2z_ffn_work(const z2z_ffn* f, int d, int rows);
 int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* residual, void* Y, bool stream_f32, void* kept, int R, const int32_t* rows_dev,

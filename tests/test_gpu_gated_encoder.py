@@ -1,0 +1,252 @@
+"""The learned hyper-encoder with gated feed-forward blocks through the C ABI, forward, gradient and over 4-bit weights, against the float64 oracle; and a training
+step with clipping and the quantized weights that serve what it trained.
+
+Bars as for the ungated layers (forward 2e-2 of a row's largest, gradient 6e-2 of a tensor's largest, means a quarter and a tenth): a gated block rounds what the other rounds,
+the normalised rows and the layer before its second product; backward dG and dU, where the other has dU and the kept pre-activation."""
+import numpy as np
+import pytest
+
+import oracle
+from paper_2506_01084_amd import workloads as wl
+
+from helpers import gpu_encode, oracle_encode_batch, storage_to_host, torch_storage
+
+pytestmark = pytest.mark.gpu
+
+TOL, TOL_GRAD = 2e-2, 6e-2
+
+
+def _bf16(x):
+    return oracle.bf16_bits_to_f64(oracle.f64_to_bf16_bits(np.nan_to_num(x, nan=0.0, posinf=0.0)))
+
+
+def _device(enc, grad=False):
+    """The binding's encoder; grad: one of the same shape, full of junk, that receives gradients."""
+    import torch
+    from paper_2506_01084_amd import api
+
+    layers, blocks = [], []
+    for lay in enc["layers"]:
+        t = {k: (torch_storage(v, "bf16") if k.startswith("w_") else torch.from_numpy(v).cuda()) for k, v in lay.items()}
+        if grad:
+            t = {k: torch.full_like(v, 9.0) for k, v in t.items()}
+        blocks.append(api.GatedFFN(t.pop("w_1"), t.pop("w_2"), act=enc["gated"]))
+        layers.append(t)
+    pos = None if enc["pos"] is None else torch_storage(enc["pos"], "bf16")
+    if grad and pos is not None:
+        pos = torch.full_like(pos, 9.0)
+    return api.Encoder(dict(n_heads=enc["n_heads"], attention_only=False, pos=pos, layers=layers, ffn=blocks), torch.bfloat16)
+
+
+def _four_bits(ctx, enc, group):
+    """The device encoder over 4-bit blocks, and the oracle's with the values that they stand for."""
+    import torch
+    from paper_2506_01084_amd import api
+
+    device, host = _device(enc), dict(enc, layers=[])
+    blocks = []
+    for lay, block in zip(enc["layers"], device.params["ffn"]):
+        new, made = dict(lay), []
+        for k, w in (("w_1", block.tensors[0]), ("w_2", block.tensors[1])):
+            words, scales = api.q4_shapes(*w.shape, group)
+            q, s = torch.empty(words, dtype=torch.int32, device="cuda"), torch.empty(scales, dtype=torch.bfloat16, device="cuda")
+            ctx.quantize_q4(w, group, q, s)
+            made.append((q, s))
+            codes, scale = oracle.quantize_q4(oracle.bf16_bits_to_f64(lay[k]), group, _bf16)
+            new[k] = oracle.q4_weights(codes, scale, group)
+        host["layers"].append(new)
+        blocks.append(api.GatedFFN(made[0][0], made[1][0], act=enc["gated"], scale_1=made[0][1], scale_2=made[1][1]))
+    return api.Encoder(dict(device.params, ffn=blocks), torch.bfloat16), host
+
+
+def _setup(B, N, V, d, M, cap, seed):
+    from paper_2506_01084_amd import api
+
+    cfg = wl.scaled(wl.CONFIGS["c2"], B=B, N=N, V=V, d=d, M=M, cap=cap, zipf_s=1.3, seed=seed)
+    lens = wl.make_lens(cfg, ragged=True)
+    if B > 1:
+        lens[1] = 0
+    tokens, E = wl.make_tokens(cfg), wl.make_embeddings(cfg)
+    ctx = api.Context(B=B, V=V, M=M, cap=cap, d=d, dtype="bf16")
+    gpu_encode(ctx, tokens, lens)
+    return cfg, ctx, [r[1] for r in oracle_encode_batch(tokens, lens, V, M, cap)], E, torch_storage(E, "bf16")
+
+
+def _compare(got, ref, what):
+    got = oracle.bf16_bits_to_f64(storage_to_host(got, "bf16"))
+    err = np.abs(got - ref) / np.maximum(1.0, np.abs(ref).max(axis=-1, keepdims=True))
+    assert err.max() <= TOL and err.mean(axis=-1).max() <= TOL / 4, (what, err.max(), err.mean(axis=-1).max())
+
+
+CASES = [(3, 300, 1000, 256, 3, 200, 2, 4, 512, "silu", True), (2, 260, 700, 512, 3, 130, 1, 1, 192, "gelu", False),
+         (5, 150, 400, 64, 4, 64, 3, 8, 64, "silu", True), (1, 900, 3000, 1024, 3, 600, 1, 8, 1088, "gelu", True),
+         (1, 100, 300, 384, 4, 20, 1, 6, 1152, "silu", True), (2, 300, 600, 2048, 5, 90, 1, 8, 448, "silu", True)]
+
+
+@pytest.mark.parametrize("B,N,V,d,M,cap,n_layers,n_heads,d_ff,act,with_pos", CASES)
+def test_forward(B, N, V, d, M, cap, n_layers, n_heads, d_ff, act, with_pos):
+    import torch
+
+    cfg, ctx, books, E, d_E = _setup(B, N, V, d, M, cap, 11 * B + d)
+    enc = wl.make_encoder(cfg, n_layers=n_layers, n_heads=n_heads, d_ff=d_ff, gated=act, with_pos=with_pos)
+    device = _device(enc)
+    W = torch.full((B, cap, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    ctx.hyper_encode(d_E, device, W)
+    kept = torch.full_like(W, 5.0)
+    ctx.hyper_encode_keep(d_E, device, kept)
+    newest = W.clone()
+    for b in range(B):
+        if books[b]:
+            newest[b, max(len(books[b]) - 2, 0):len(books[b])] = 3.0
+    ctx.hyper_encode(d_E, device, newest, max_new=2)
+    q4, host = _four_bits(ctx, enc, 64)
+    W4, n4 = torch.full_like(W, 7.0), torch.full_like(W, 7.0)
+    ctx.hyper_encode(d_E, q4, W4)
+    ctx.hyper_encode(d_E, q4, n4, max_new=1)
+    for b in range(B):
+        n = len(books[b])
+        ref = oracle.hyper_encode(E, "bf16", books[b], cap, enc, rounded=False)
+        ref4 = oracle.hyper_encode(E, "bf16", books[b], cap, host, rounded=False)
+        _compare(W[b], ref, "all")
+        _compare(kept[b], ref, "kept")
+        _compare(newest[b], ref, "newest")
+        _compare(W4[b], ref4, "four bits")
+        if n:
+            _compare(n4[b, n - 1:n], ref4[n - 1:n], "newest, four bits")
+        assert (n4[b, :max(n - 1, 0)] == 7).all() and (n4[b, n:] == 7).all()
+
+
+@pytest.mark.parametrize("B,N,V,d,M,cap,n_layers,n_heads,d_ff,act,with_pos", CASES)
+def test_backward(B, N, V, d, M, cap, n_layers, n_heads, d_ff, act, with_pos):
+    import torch
+
+    cfg, ctx, books, E, d_E = _setup(B, N, V, d, M, cap, 7 * B + d)
+    enc = wl.make_encoder(cfg, n_layers=n_layers, n_heads=n_heads, d_ff=d_ff, gated=act, with_pos=with_pos)
+    device, grad = _device(enc), _device(enc, grad=True)
+    dW = wl.normal_matrix(B + d, B * cap, d, 1.0, "bf16").reshape(B, cap, d)
+    dE = torch.zeros((V, d), device="cuda")
+    ctx.hyper_encode_backward(d_E, device, torch_storage(dW, "bf16"), grad, dE)
+    W, again, dE2 = torch.empty((B, cap, d), dtype=torch.bfloat16, device="cuda"), _device(enc, grad=True), torch.zeros_like(dE)
+    ctx.hyper_encode_keep(d_E, device, W)
+    ctx.hyper_encode_backward(d_E, device, torch_storage(dW, "bf16"), again, dE2, kept=True)
+    want = None
+    for b in range(B):
+        r = oracle.hyper_encode_backward(E, "bf16", books[b], enc, oracle.bf16_bits_to_f64(dW[b]))
+        if want is None:
+            want = r
+            continue
+        want["dE"] += r["dE"]
+        if with_pos:
+            want["pos"] += r["pos"]
+        for a, x in zip(want["layers"], r["layers"]):
+            for k in a:
+                a[k] += x[k]
+
+    def check(got, ref, what):
+        got = got.double().cpu().numpy()
+        err = np.abs(got - ref) / max(np.abs(ref).max(), 1e-30)
+        assert np.isfinite(got).all() and err.max() <= TOL_GRAD and err.mean() <= TOL_GRAD / 10, (what, err.max(), err.mean())
+
+    for g, e in ((grad, dE), (again, dE2)):
+        check(e, want["dE"], "dE")
+        if with_pos:
+            check(g.params["pos"], want["pos"], "pos")
+        for l, layer in enumerate(want["layers"]):
+            for k, ref in layer.items():
+                t = g.params["ffn"][l].tensors[0 if k == "w_1" else 1] if k in ("w_1", "w_2") else g.params["layers"][l][k]
+                check(t, ref, (l, k))
+    for a, b in zip(grad.params["ffn"], again.params["ffn"]):             # (no atomics on the way to these)
+        assert torch.equal(a.tensors[0], b.tensors[0]) and torch.equal(a.tensors[1], b.tensors[1])
+
+
+def test_training_step_then_serving():
+    """Encode, loss, gradients, clipping of all of them, an update, and generation steps over the updated blocks in 4 bits, captured."""
+    import torch
+    from paper_2506_01084_amd import api
+
+    B, N, V, d, M, cap, f = 3, 200, 700, 256, 3, 150, 320
+    cfg, ctx, books, E, d_E = _setup(B, N, V, d, M, cap, 3)
+    enc = wl.make_encoder(cfg, n_layers=2, n_heads=4, d_ff=f, gated="silu")
+    device, grad = _device(enc), _device(enc, grad=True)
+    W, dW = (torch.zeros((B, cap, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    H = torch.randn((B * 40, d), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    targets = torch.randint(0, V, (B * 40,), generator=torch.Generator().manual_seed(2), dtype=torch.int32).cuda()
+    Wb = (torch.randn((V, d), generator=torch.Generator().manual_seed(3)) * 0.05).bfloat16().cuda()
+    nll, lse = torch.empty(B * 40, device="cuda"), torch.empty(B * 40, device="cuda")
+    dH, dWb, dE = torch.empty_like(H), torch.empty_like(Wb), torch.zeros((V, d), device="cuda")
+    vectors = [t for lay in grad.params["layers"] for t in lay.values()]
+    matrices = [t for b in grad.params["ffn"] for t in b.tensors[:2]]
+    everything = [dWb, dE, grad.params["pos"], *vectors, *matrices]
+    clip, norm = api.Gradients(everything), torch.empty(2, device="cuda")
+    ctx.hyper_encode_keep(d_E, device, W)
+    ctx.extended_nll(H, 40, Wb, W, targets, nll, lse)
+    ctx.extended_nll_backward(H, 40, Wb, W, targets, lse, None, dH, dWb, dW)
+    ctx.hyper_encode_backward(d_E, device, dW, grad, dE, kept=True)
+    before = [t.double() for t in everything]
+    ctx.clip_gradients(clip, 0.75, norm)
+    total = float(torch.sqrt(sum((t * t).sum() for t in before)))
+    assert total > 0.75 and float(norm[0]) == pytest.approx(total, rel=3e-6) and float(norm[1]) == pytest.approx(0.75 / total, rel=3e-6)
+    for t, b in zip(everything, before):
+        step = 2.0 ** -8 if t.dtype == torch.bfloat16 else 2.0 ** -24
+        assert torch.all((t.double() - b * 0.75 / total).abs() <= (b.abs() * 0.75 / total) * (step + 1e-5) + 1e-38)
+    for block, g in zip(device.params["ffn"], grad.params["ffn"]):
+        for w, dw in zip(block.tensors[:2], g.tensors[:2]):
+            w.sub_(0.1 * dw)
+    # serving
+    trained = dict(enc, layers=[dict(lay, w_1=storage_to_host(b.tensors[0], "bf16"), w_2=storage_to_host(b.tensors[1], "bf16"))
+                                for lay, b in zip(enc["layers"], device.params["ffn"])])
+    q4, host = _four_bits(ctx, trained, 64)
+    ctx.hyper_encode(d_E, q4, W)
+    n_tok, status = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    code = torch.empty((B, 1), dtype=torch.int32, device="cuda")
+    ones = torch.ones(B, dtype=torch.int32, device="cuda")
+
+    def step():
+        ctx.lzw_decode(code, ones, None, n_tok, status, api.APPEND)
+        ctx.hyper_encode(d_E, q4, W, max_new=1)
+
+    code.fill_(3)
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    rng = np.random.default_rng(4)
+    for _ in range(4):
+        code.copy_(torch.from_numpy(rng.integers(0, V, size=(B, 1)).astype(np.int32)))
+        graph.replay()
+        torch.cuda.synchronize()
+    entries, lens, sizes = ctx.codebook()
+    for b in range(B):
+        n = int(sizes[b])
+        now = [tuple(entries[b, e, :int(lens[b, e])].tolist()) for e in range(n)]
+        ref = oracle.hyper_encode(E, "bf16", now, cap, host, rounded=False)
+        _compare(W[b, :n], ref[:n], "served")
+
+
+def test_refusals():
+    import torch
+    from paper_2506_01084_amd import api
+
+    cfg, ctx, books, E, d_E = _setup(2, 60, 200, 128, 3, 20, 5)
+    enc = wl.make_encoder(cfg, n_layers=1, n_heads=4, d_ff=64, gated="silu")
+    device, grad = _device(enc), _device(enc, grad=True)
+    q4, _ = _four_bits(ctx, enc, 64)
+    W, dE = torch.empty((2, 20, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((200, 128), device="cuda")
+    plain = wl.make_encoder(cfg, n_layers=1, n_heads=4, d_ff=64)
+    from helpers import encoder_to_device
+
+    def refused(code, call):
+        with pytest.raises(api.Z2ZError) as e:
+            call()
+        assert e.value.code == code
+
+    refused(api.E_UNSUPPORTED, lambda: ctx.hyper_encode_keep(d_E, q4, W))
+    refused(api.E_UNSUPPORTED, lambda: ctx.hyper_encode_backward(d_E, q4, W, grad, dE))
+    refused(api.E_INVAL, lambda: ctx.hyper_encode_backward(d_E, device, W, encoder_to_device(plain, "bf16"), dE))
+    # rows kept for another encoder's shape
+    ctx.hyper_encode_keep(d_E, encoder_to_device(plain, "bf16"), W)
+    refused(api.E_INVAL, lambda: ctx.hyper_encode_backward(d_E, device, W, grad, dE, kept=True))
+    device.desc.attention_only = 1
+    ctx.hyper_encode(d_E, device, W)
+    device.desc.attention_only = api.ENC_GATED
+    ctx.hyper_encode(d_E, device, W)

@@ -79,3 +79,47 @@ def test_clip():
     assert norm == 5 and c == 0.2 and np.allclose(out[0], [0.6, 0]) and np.allclose(out[1], 0.8)
     assert oracle.clip([a, b], 6.0)[1] == 1.0 and oracle.clip([a * 0], 0.0)[:2] == (0.0, 1.0)
     assert oracle.clip([np.array([math.inf])], 1.0)[1] == 1.0 and math.isnan(oracle.clip([np.array([math.nan])], 1.0)[0])
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_gated_encoder(kind):
+    """A gated layer is the attention layer and the block behind it; its gradient, against differences."""
+    from paper_2506_01084_amd import workloads as wl
+
+    cfg = dict(d=16, M=3, dtype="f32", seed=4)
+    enc = wl.make_encoder(cfg, n_layers=2, n_heads=2, d_ff=24, gated=kind)
+    assert enc["layers"][0]["w_1"].shape == (48, 16) and "b_1" not in enc["layers"][0]
+    E = wl.normal_matrix(8, 9, 16, 0.6, "f32")
+    entries = [(0, 3), (4, 4, 1), (2, 8)]
+    one = dict(enc, layers=enc["layers"][:1])
+    attention = dict(one, gated=None, attention_only=True)
+    lay = one["layers"][0]
+    for e in entries:                                       # one slot at a time of a layer's output: the mean of one
+        X = E[list(e)].astype(np.float64) + enc["pos"][:len(e)]
+        A64, full = oracle.encoder.widen_encoder(attention, "f32"), oracle.encoder.widen_encoder(one, "f32")
+        Y = X + oracle.encoder.attention(oracle.encoder.layer_norm(X, lay["ln1_g"], lay["ln1_b"]), lay["w_qkv"].astype(np.float64),
+                                         lay["b_qkv"], lay["w_o"].astype(np.float64), lay["b_o"], 2)
+        assert np.allclose(Y.mean(axis=0), oracle.encoder.encode_entry(X, A64))
+        block = oracle.gated_ffn(oracle.encoder.layer_norm(Y, lay["ln2_g"], lay["ln2_b"]), lay["w_1"].astype(np.float64),
+                                 lay["w_2"].astype(np.float64), kind, Y)["Y"]
+        assert np.allclose(block.mean(axis=0), oracle.encoder.encode_entry(X, full), atol=1e-12)
+    rng = np.random.default_rng(2)
+    dW = rng.normal(size=(3, 16))
+    grad = oracle.hyper_encode_backward(E, "f32", entries, enc, dW)
+
+    def loss(enc64, table):
+        total = 0.0
+        for i, e in enumerate(entries):
+            total += float(dW[i] @ oracle.encoder.encode_entry(table[list(e)] + enc64["pos"][:len(e)], enc64))
+        return total
+
+    e64, table, eps = oracle.encoder.widen_encoder(enc, "f32"), E.astype(np.float64), 1e-6
+    for where, x, at, want in [(l, e64["layers"][l][k], at, grad["layers"][l][k][at]) for l in (0, 1)
+                               for k, at in (("w_1", (30, 5)), ("w_1", (3, 7)), ("w_2", (9, 20)), ("ln2_g", (4,)), ("w_qkv", (40, 2)))] + [("E", table, (4, 6), grad["dE"][4, 6])]:
+        was = x[at]
+        x[at] = was + eps
+        up = loss(e64, table)
+        x[at] = was - eps
+        down = loss(e64, table)
+        x[at] = was
+        assert abs((up - down) / (2 * eps) - want) < 1e-7 * max(1, abs(want)), where
