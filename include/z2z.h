@@ -249,10 +249,10 @@ int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, i
  *   act  Z2Z_ACT_SILU  x / (1 + e^-x);   Z2Z_ACT_GELU  x Phi(x), Phi the normal distribution (erf)
  * F is rounded to bf16 once (the operand of a product), sums are fp32, Y is rounded once.
  *   w_1 [2 f, d], w_2 [d, f]: bf16, group = 0; or in 4 bits as z2z_quantize_q4 writes them, group = 32, 64 or 128, with scale_1 [d / group, 2 f] and
- *        scale_2 [f / group, d].  Up to 192 rows are multiplied by v, the scales with fp32 sums;
+ *        scale_2 [f / group, d].  Up to 320 rows are multiplied by v, the scales with fp32 sums;
  *        more rows by the weights rounded to bf16, which takes 6 d f bytes of work space.
  *   d_X [rows, d], d_residual [rows, d] or NULL, d_Y [rows, d] out: bf16.  d_Y may be d_residual, else it overlaps neither input (Z2Z_EINVAL)
- *   d_kept  [rows, 2 f] float out or NULL: G | U for z2z_gated_ffn_backward (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
+ *   d_kept  [rows, 2 f] float out or NULL: what z2z_gated_ffn_backward needs of G and U, for that call alone to read (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
  * A row's results do not depend on the other rows' values.  rows = 0 is a call that does nothing.  bf16 contexts, d and d_ff multiples of 64 (with 4 bits of group,
  * too), rows <= 2^22, (d_ff + 128) d < 2^30, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and for few rows the parts of the products. */
 enum { Z2Z_ACT_SILU = 0, Z2Z_ACT_GELU = 1 };
@@ -275,7 +275,7 @@ int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ff
  *   grad   its w_1 and w_2 name the buffers that RECEIVE the gradients, bf16 (the call writes through them although they are declared const); its
  *          other fields are not read.  flags = 0: overwritten (rows = 0: with zeros); Z2Z_GRAD_ADD: added to what is there, one rounding per element
  * dG, dU and F are rounded to bf16 once, sums are fp32.  No output overlaps an input or another output (Z2Z_EINVAL).  Restrictions as for z2z_gated_ffn; work
- * space: 6 f bytes per row. */
+ * space: 4 f bytes per row. */
 int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const float* d_kept, const void* d_dY, void* d_dX,
                            const z2z_ffn* grad, int32_t flags, void* stream);
 
@@ -371,7 +371,7 @@ int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* encoder, 
  * Without the flag the call runs the forward pass again, keeping every layer's rows, then reverse mode over the
  * same steps; activations and gradients between kernels are bf16, sums fp32; passes of up to 65536 slot rows
  * (matrix gradients of later passes add to the bf16 result of the earlier ones).  Work space (about
- * 2 * (n_layers * (10 d + 2 d_ff) + 9 d + d_ff) bytes per slot row; 2 * (n_layers * (10 d + 4 d_ff) + 9 d + 3 d_ff) with gated blocks) is library scratch, Z2Z_ENOMEM beyond 200 GB.
+ * 2 * (n_layers * (10 d + 2 d_ff) + 9 d + d_ff) bytes per slot row; 2 * (n_layers * (10 d + 4 d_ff) + 9 d + 2 d_ff) with gated blocks) is library scratch, Z2Z_ENOMEM beyond 200 GB.
  * Restrictions and errors as for z2z_hyper_encode. */
 #define Z2Z_ENC_KEPT 1
 int z2z_hyper_encode_backward(z2z_ctx* ctx, const void* d_E, const z2z_encoder* encoder, const void* d_dW_hyper,

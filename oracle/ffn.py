@@ -15,6 +15,7 @@ import numpy as np
 
 HALF_BF16 = 2.0 ** -8                    # half a step of bf16, relative to the value
 HALF_F32 = 2.0 ** -24
+KEPT = 2.0 ** -17
 ACT_ERROR = 1e-6                         # of the activations' and slopes' own arithmetic in float32 (their erf: 1.5e-7; exponentials, reciprocals: a few steps)
 
 _erf = np.vectorize(math.erf, otypes=[np.float64])
@@ -50,24 +51,25 @@ def gated_ffn(X, W1, W2, kind: str, residual=None, round_weights: bool = False):
     w2 = np.abs(W2).T
     Y_err = F_err @ w2 + _sum_bound(F, W2.T) + (HALF_BF16 * (np.abs(F) @ w2) if round_weights else 0.0)
     Y_bound = (Y_err * 1.02 + HALF_BF16 * (np.abs(Y) + Y_err)) * 1.001 + 1e-30
-    return dict(Y=Y, Y_bound=Y_bound, Y_err=Y_err, G=G, U=U, F=F, kept_bound=np.concatenate([g_err, u_err], axis=1) + 1e-30)
+    # what the gradient needs: act(G) and U act'(G), which may be stored with 16 bits of fraction
+    slope = act(G, kind)[1]
+    slope_err = 0.8 * g_err + 4 * ACT_ERROR                      # (neither slope changes faster than 0.8)
+    a_bound = a_err + KEPT * (np.abs(a) + a_err) + 1e-30
+    s_bound = (u_err * (np.abs(slope) + slope_err) + np.abs(U) * slope_err) * 1.01
+    s_bound = s_bound + KEPT * (np.abs(U * slope) + s_bound) + 1e-30
+    return dict(Y=Y, Y_bound=Y_bound, Y_err=Y_err, G=G, U=U, F=F, F_err=F_err, a=a, a_bound=a_bound, s=U * slope, s_bound=s_bound)
 
 
 def gated_ffn_backward(X, W1, W2, kind: str, dY):
     """dict of dX, dW1, dW2 and their bounds (name + "_bound")."""
     f = W2.shape[1]
     forward = gated_ffn(X, W1, W2, kind)
-    G, U, F = forward["G"], forward["U"], forward["F"]
-    g_err, u_err = forward["kept_bound"][:, :f], forward["kept_bound"][:, f:]
-    a, slope = act(G, kind)
-    a_err = 1.13 * g_err + ACT_ERROR * (np.abs(G) + 1e-30)
-    slope_err = 0.8 * g_err + 4 * ACT_ERROR                      # (neither slope changes faster than 0.8)
-    F_err = (a_err * (np.abs(U) + u_err) + np.abs(a) * u_err) * 1.01 + HALF_BF16 * np.abs(F) * 1.01
+    F, F_err, a, a_err, s, s_err = (forward[k] for k in ("F", "F_err", "a", "a_bound", "s", "s_bound"))
     dF = dY @ W2
     dF_err = _sum_bound(dY, W2)
-    dG, dU = dF * U * slope, dF * a
+    dG, dU = dF * s, dF * a
     big = np.abs(dF) + dF_err
-    dG_err = (big * (u_err * (np.abs(slope) + slope_err) + np.abs(U) * slope_err) + dF_err * np.abs(U * slope)) * 1.01 + HALF_BF16 * np.abs(dG) * 1.01
+    dG_err = (big * s_err + dF_err * np.abs(s)) * 1.01 + HALF_BF16 * np.abs(dG) * 1.01
     dU_err = (big * a_err + dF_err * np.abs(a)) * 1.01 + HALF_BF16 * np.abs(dU) * 1.01
     D, D_err = np.concatenate([dG, dU], axis=1), np.concatenate([dG_err, dU_err], axis=1)
     out = {}

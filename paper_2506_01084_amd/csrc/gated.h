@@ -34,23 +34,57 @@ __device__ __forceinline__ uint2 hidden4(const float (&g)[4], const float (&u)[4
   return pack4(f);
 }
 
-// Four columns of the gradients dG = dF U act'(G) and dU = dF act(G), and of F once more, from dF and from G and U as the forward pass kept them, all fp32.
-// (Kept in bf16 the two roundings would be half of the gradients' error: 3.5e-3 of their norm instead of 2.4e-3, of which the rounding of
-// what is returned is 1.7e-3.  16411 rows, d_ff = 5504: 0.36 GB more to write and to read, KEPT_COST.)
-struct Slopes4 {
-  uint2 dg, du, f;
+// What the backward pass is given of an element: a = act(G) and s = U act'(G), by which dF is multiplied, with 16 bits of fraction (2^-17 off at most), and F.  Three matrices
+// one behind the other in one buffer of 8 bytes an element: F in bf16, an operand of products in both directions; the upper halves of a and s, 4 bytes; the next
+// bytes of either, 2.  (G and U in bf16 would be half of the gradients' error, 3.5e-3 of their norm instead of 2.3e-3, of which the rounding of what is returned is
+// 1.7e-3.  In fp32 the backward pass's epilogue read and wrote 14 bytes an element, with the matrix cores waiting, instead of 10, and formed exponentials
+// again: 16411 rows, d = 2048, d_ff = 5504 556 us for dF, 463 now, and 700 for the first product, 664.)
+struct Kept {
+  uint16_t* f;
+  uint32_t* hi;
+  uint16_t* lo;
 };
-__device__ __forceinline__ Slopes4 slopes4(const float (&df)[4], const float4& g4, const float4& u4, int act) {
-  const float g[4] = {g4.x, g4.y, g4.z, g4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
-  float dg[4], du[4], f[4];
+__host__ __device__ __forceinline__ Kept kept_in(void* p, size_t rows, int d_ff) {
+  const size_t n = rows * d_ff;
+  unsigned char* b = reinterpret_cast<unsigned char*>(p);
+  return Kept{reinterpret_cast<uint16_t*>(b), reinterpret_cast<uint32_t*>(b + 2 * n), reinterpret_cast<uint16_t*>(b + 6 * n)};
+}
+
+__device__ __forceinline__ uint32_t rounded24(float x) {
+  const uint32_t u = __float_as_uint(x);
+  // (the sum carries a fraction of ones into the exponent, as it should; not a NaN's into the sign, nor the largest number's into an infinity)
+  return (u & 0x7FFFFFFFu) < 0x7F7FFF80u ? u + 0x80u : u;
+}
+// Four columns of F out of fp32 sums, and what else is kept of them (element `at` of the matrices is the first).
+__device__ __forceinline__ uint2 hidden_and_kept4(const float (&g)[4], const float (&u)[4], int act, uint4* hi, uint2* lo) {
+  float f[4];
+  uint32_t h[4], l[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const Act a = act_and_slope(g[e], act);
-    dg[e] = df[e] * u[e] * a.slope;
-    du[e] = df[e] * a.value;
-    f[e] = a.value * u[e];
+    const Act x = act_and_slope(g[e], act);
+    f[e] = x.value * u[e];
+    const uint32_t a = rounded24(x.value), s = rounded24(x.slope * u[e]);
+    h[e] = __builtin_amdgcn_perm(s, a, 0x07060302u);
+    l[e] = __builtin_amdgcn_perm(s, a, 0x0C0C0501u);
   }
-  return Slopes4{pack4(dg), pack4(du), pack4(f)};
+  *hi = uint4{h[0], h[1], h[2], h[3]};
+  *lo = uint2{l[0] | l[1] << 16, l[2] | l[3] << 16};
+  return pack4(f);
+}
+
+// Four columns of the gradients dG = dF U act'(G) and dU = dF act(G), from dF and what the forward pass kept.
+struct Slopes4 {
+  uint2 dg, du;
+};
+__device__ __forceinline__ Slopes4 slopes4(const float (&df)[4], const uint4& hi, const uint2& lo) {
+  const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[2] = {lo.x, lo.y};
+  float dg[4], du[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    du[e] = df[e] * __uint_as_float(__builtin_amdgcn_perm(h[e], l[e >> 1], e & 1 ? 0x0504020Cu : 0x0504000Cu));
+    dg[e] = df[e] * __uint_as_float(__builtin_amdgcn_perm(h[e], l[e >> 1], e & 1 ? 0x0706030Cu : 0x0706010Cu));
+  }
+  return Slopes4{pack4(dg), pack4(du)};
 }
 
 }  // namespace z2z_gated

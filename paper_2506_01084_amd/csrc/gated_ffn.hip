@@ -3,20 +3,32 @@
 //
 // Forward, many rows: one launch of the tile kernel for both projections, activation and product (a tile of 256 weight rows is 128 gate columns and the same 128
 // of the other projection), one for the product with W2.  Few rows are bound by the weights' bytes: the weight-streaming kernel, in bf16 or from 4 bits (q4.hip), leaves
-// parts of the products, whose sum applies the activation.  Backward: dF = dY W2 becomes dG | dU and F in the epilogue; then dW2 = dY^T F,
+// parts of the products, whose sum applies the activation.  Backward: dF = dY W2 becomes dG | dU in the epilogue; then dW2 = dY^T F,
 // dW1 = [dG | dU]^T X, dX = [dG | dU] W1, all on operands as they are.
+#include "few_rows.h"
 #include "logits_common.h"
 
 namespace {
 
-// Rows from which on 4-bit weights are expanded to bf16 first: the products are the matrix cores' work then.
-constexpr int kExpandRows = 192;
+// More rows than this, and 4-bit weights are expanded to bf16 first: the products are the matrix cores' work then.  (us, product from 4 bits / expanded: d = 4096, d_ff = 10944
+// 256 rows 142 / 224, 300 173 / 232; 3584, 9600 300 128 / 196; 2048, 5504 300 70 / 100; 1024, 2752 300 34 / 66.)
+constexpr int kExpandRows = 320;
 
 __global__ void __launch_bounds__(256) fill_zero_kernel(uint4* p, size_t n, uint4* q, size_t n_q) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n + n_q; i += (size_t)gridDim.x * 256) {
     uint4* at = i < n ? p + i : q + (i - n);
     *at = uint4{0u, 0u, 0u, 0u};
   }
+}
+
+// Rows up to which the products run on the kernel that shares nothing between workgroups but has no parts to add up (few_rows.hip): every workgroup reads all rows, which
+// costs more than the sums from a number on that depends on the weights.  us, that kernel / the others:
+//   bf16   d = 4096, d_ff = 10944  1 row 47 / 54, 16 rows 57 / 61, 24 70 / 65;   2048, 5504  1 19.8 / 24.4, 16 25.5 / 26.9, 24 31.1 / 27.4;   1024, 2752  1 9.5 / 16.8, 64 22.8 / 24.3,
+//          256 34.4 / 52.3, 300 48.1 / 52.5
+//   4 bits d = 4096, d_ff = 10944, group 64  1 19.8 / 26.6, 4 21.7 / 27.8, 16 32.2 / 29.6;   3584, 9600, 128  4 17.8 / 21.6, 16 27.2 / 24.6;   2048, 5504, 32  4 13.7 / 15.1, 16 18.0 / 18.3,
+//          32 26.8 / 24.5;   1024, 2752, 64  1 8.3 / 13.1, 32 12.8 / 15.5, 64 20.1 / 20.6, 128 24.5 / 26.5
+bool few_rows(const z2z_ffn* f, int d, int R) {
+  return R <= (f->group ? 8 : 16) || ((long long)d * f->d_ff <= (1 << 22) && R <= (f->group ? 64 : 256));
 }
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -30,9 +42,15 @@ size_t z2z_ffn_work(const z2z_ffn* f, int d, int rows) {
 int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
                           hipStream_t s) {
   const int d = c->cfg.d, dff = f->d_ff;
-  unsigned char* F = reinterpret_cast<unsigned char*>(work);
+  unsigned char* F = reinterpret_cast<unsigned char*>(kept ? kept : work);     // (the first of what is kept)
   const void* w1 = f->w_1;
-  *out = z2z_ffn_out{F, f->w_2, nullptr, 0, dff, false};
+  *out = z2z_ffn_out{F, f->w_2, nullptr, 0, dff, false, false};
+  if (few_rows(f, d, R)) {
+    out->scale = f->scale_2;
+    out->group = f->group;
+    out->few = true;
+    return z2z_launch_few_gated(X, w1, f->scale_1, f->group, f->act, F, kept, R, rows_dev, dff, d, s);
+  }
   if (f->group && R <= kExpandRows) {
     out->scale = f->scale_2;
     out->group = f->group;
@@ -62,6 +80,7 @@ int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* resi
   z2z_ffn_out o;
   int rc = z2z_launch_ffn_hidden(c, X, f, kept, R, rows_dev, work, &o, s);
   if (rc != Z2Z_OK) return rc;
+  if (o.few) return z2z_launch_few_linear(o.F, o.w, o.scale, o.group, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
   if (!o.group) return z2z_launch_linear(c, o.F, o.w, nullptr, residual, 0, Y, R, rows_dev, d, o.d_ff, s, stream_f32, nullptr, o.once);
   const float* partial = nullptr;
   int ksplit = 0;
@@ -70,20 +89,20 @@ int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* resi
   return z2z_launch_linear_sum(partial, ksplit, R, rows_dev, d, residual, Y, stream_f32, s);
 }
 
-size_t z2z_ffn_backward_work(const z2z_ffn* f, int rows) { return padded((size_t)rows * f->d_ff * 2) + (size_t)rows * 2 * f->d_ff * 2; }
+size_t z2z_ffn_backward_work(const z2z_ffn* f, int rows) { return (size_t)rows * 2 * f->d_ff * 2; }
 
 int z2z_launch_ffn_backward(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* kept, const void* dY, void* dX, const z2z_ffn* grad, bool add, int R,
                             const int32_t* rows_dev, void* work, hipStream_t s) {
   const int d = c->cfg.d, dff = f->d_ff;
-  unsigned char *F = reinterpret_cast<unsigned char*>(work), *slopes = F + padded((size_t)R * dff * 2);
+  const void* F = kept;                              // (the first of what is kept)
   void *dw1 = const_cast<void*>(grad->w_1), *dw2 = const_cast<void*>(grad->w_2);
-  int rc = z2z_launch_gated_slopes(c, dY, f->w_2, kept, f->act, slopes, F, R, rows_dev, dff, d, s);
+  int rc = z2z_launch_gated_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, s);
   if (rc != Z2Z_OK) return rc;
   rc = z2z_launch_linear_weight(c, dY, d, F, dff, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
   if (rc != Z2Z_OK) return rc;
-  rc = z2z_launch_linear_weight(c, slopes, 2 * dff, X, d, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
+  rc = z2z_launch_linear_weight(c, work, 2 * dff, X, d, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
   if (rc != Z2Z_OK) return rc;
-  return z2z_launch_linear_input(c, slopes, 2 * dff, f->w_1, d, 2 * dff, nullptr, dX, d, R, rows_dev, d, 2 * dff, s);
+  return z2z_launch_linear_input(c, work, 2 * dff, f->w_1, d, 2 * dff, nullptr, dX, d, R, rows_dev, d, 2 * dff, s, {1, 0, 0}, 0, kGatedMinSaved);
 }
 
 int z2z_launch_fill_zero(void* p, size_t bytes, void* q, size_t bytes_q, hipStream_t s) {

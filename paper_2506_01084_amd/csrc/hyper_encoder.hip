@@ -19,6 +19,7 @@
 // and the final mean.  The residual stream (X, Y, Z) is fp32 from the gather to the final mean; the operands of
 // the matrix products (LayerNorm outputs, q | k | v, attention outputs, the hidden layer) are bf16;
 // accumulation and statistics are fp32.
+#include "few_rows.h"
 #include "logits_common.h"
 
 #include <algorithm>
@@ -949,7 +950,7 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
     // (gamma, beta -> A) or, behind the last layer, the mean over an entry's rows.  Where K is split those
     // add up the partial tiles themselves; else *fused stays false and only `out` is written.
     auto layer_out = [&](const uint16_t* in, const void* w, const float* bias, const float* residual, float* out, int K,
-                         const float* gamma, const float* beta, bool* fused, const z2z_ffn_out* four_bits = nullptr) -> int {
+                         const float* gamma, const float* beta, bool* fused, const z2z_ffn_out* block = nullptr) -> int {
       Parts parts = {};
       *fused = false;
       const z2z_linear_pitch pitch = {dffp, dff, d};
@@ -957,8 +958,10 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
       int ret = Z2Z_OK;
       // (with more rows -- K is split there too in a narrow encoder -- a wave per row is the better LayerNorm: 6144 rows,
       // d = 256: the pass 275 us fused, 267 in launches of their own)
-      if (four_bits)
-        ret = z2z_launch_q4_parts(c, in, w, four_bits->scale, four_bits->group, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s);
+      if (block && block->few)
+        return z2z_launch_few_linear(in, w, block->scale, block->group, residual, out, true, R, rows_dev, d, K, s);
+      if (block && block->group)
+        ret = z2z_launch_q4_parts(c, in, w, block->scale, block->group, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s);
       else if (!padded && R <= E_FEW_ROWS)
         ret = z2z_launch_linear_parts(c, in, w, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s, once);
       if (ret != Z2Z_OK) return ret;
@@ -1014,7 +1017,7 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
           z2z_ffn_out o;
           rc = z2z_launch_ffn_hidden(c, A, gated + l, nullptr, R, rows_dev, F, &o, s);
           if (rc != Z2Z_OK) return rc;
-          rc = layer_out(F, o.w, nullptr, y, x, o.d_ff, next ? next->ln1_g : nullptr, next ? next->ln1_b : nullptr, &fused, o.group ? &o : nullptr);
+          rc = layer_out(F, o.w, nullptr, y, x, o.d_ff, next ? next->ln1_g : nullptr, next ? next->ln1_b : nullptr, &fused, &o);
         } else {
           const z2z_linear_pitch to_wide = {d, d, dffp};
           rc = z2z_launch_linear(c, A, lay.w_1, lay.b_1, nullptr, 1, F, R, rows_dev, dff, d, s, false,
@@ -1081,9 +1084,9 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
   const size_t pos_bytes = ((size_t)Z2Z_MAX_M * d * sizeof(float) + 255) & ~(size_t)255;
   // in units of bf16 elements (an fp32 element counts as two): per layer what LayerSave names (Xin and Y fp32);
   // the last layer's output (fp32); the running gradients dX dY dN dO (d each), dQKV (3d), dF (d_ff)
-  // (gated blocks: what they keep, 2 d_ff fp32 a row, in place of the layer before and behind the activation, and their work space in place of dF)
+  // (gated blocks: what they keep, 8 d_ff bytes a row, in place of the layer before and behind the activation, and their work space in place of dF)
   const size_t per_layer = R_max * ((size_t)10 * d + (size_t)(gated ? 4 : 2) * dffp);
-  const size_t ffn_work = gated ? (z2z_ffn_backward_work(gated, (int)R_max) + 255) / 256 * 128 : R_max * (size_t)dffp;
+  const size_t ffn_work = gated ? z2z_ffn_backward_work(gated, (int)R_max) / 2 : R_max * (size_t)dffp;
   const size_t elems = (size_t)nl * per_layer + R_max * (size_t)7 * d + ffn_work + R_max * 2 * d;
   const size_t nb_bytes = (R_max * sizeof(float2) + 255) & ~(size_t)255;   // mean and rstd of every row of a LayerNorm
   const size_t need = index_bytes + pos_bytes + nb_bytes + elems * 2;

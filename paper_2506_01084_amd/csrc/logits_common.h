@@ -297,6 +297,7 @@ struct LogitsArgs {
   float* partial;           // [ksplit][rows][ldo]
   // dense layer whose last round of tiles may be cut along K, as the device sees fit: 256 tile buffers of 256 x 256; nullptr: never
   float* split;
+  int32_t min_saved;        // slabs such a cut has to save, 0: 16
   // sampling fold (base part of a sampled decode step with many rows): the triples are taken over
   // logit * inv_temperature, and next to them the largest perturbed value (part_v), the scaled logit there
   // (part_l) and its column (part_i, instead of the maximum's); generator key and counter words as in the
@@ -322,10 +323,10 @@ struct LogitsArgs {
     int32_t ldo, cap, col0, strip, n_strips, part0, row_tiles, n_work, n_seq;
   } hyper;
   // gated feed-forward block (tile kernel, GATE 1 and 2).  Forward: W holds d_ff gate rows, then d_ff rows of the other projection (w_rows = 2 d_ff),
-  // out = F [rows, d_ff], kept = nullptr or where G | U go, [rows, 2 d_ff].  Backward: the product is dF, out = F, kept = the forward pass's G | U,
-  // slopes = dG | dU.  bf16, what is kept fp32.
+  // out = F [rows, d_ff] bf16, kept_hi and kept_lo (or nullptr): what else the backward pass needs (gated.h).  Backward: the product is dF, out = dG | dU [rows, 2 d_ff] bf16.
   struct {
-    void *kept, *slopes;
+    uint32_t* kept_hi;
+    uint16_t* kept_lo;
     int32_t d_ff, act;
   } gated;
 };
@@ -512,7 +513,8 @@ int z2z_launch_linear(z2z_ctx* c, const void* A, const void* W, const float* bia
 //   z2z_launch_linear_input    out[R, N] = A[R, K] . W[k_rows, N] + residual;  A's columns from k_rows to K (K: a multiple of 64) are finite
 //   z2z_launch_linear_weight   out[R, N] = A[k_rows, R]^T . W[k_rows, N] + residual;  with k_dev only the first *k_dev rows exist
 // A batch of them: outputs of R rows below each other, W (and the second's A) batch_w (batch_a) elements apart.
-// stream_f32 as in LogitsArgs: a sum of several products is rounded once.  The second adds row_sums where they are given.
+// stream_f32 as in LogitsArgs: a sum of several products is rounded once.  The second adds row_sums where they are given.  min_saved: a cut along K (LogitsArgs::split)
+// is made from so many slabs saved on, 0: 16, and of contractions of 32 and more.
 struct z2z_linear_batch {
   int n;
   size_t a, w;
@@ -522,10 +524,11 @@ struct z2z_row_sums {
   const int32_t* row_slot; // [output rows] which of them is added to the row, or negative
 };
 int z2z_launch_linear_input(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const void* residual, void* out, int ldo,
-                            int R, const int32_t* rows_dev, int N, int K, hipStream_t s, z2z_linear_batch batch = {1, 0, 0}, int stream_f32 = 0);
+                            int R, const int32_t* rows_dev, int N, int K, hipStream_t s, z2z_linear_batch batch = {1, 0, 0}, int stream_f32 = 0,
+                            int min_saved = 0);
 int z2z_launch_linear_weight(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const int32_t* k_dev,
                              const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch = {1, 0, 0},
-                             z2z_row_sums row_sums = {nullptr, nullptr});
+                             z2z_row_sums row_sums = {nullptr, nullptr}, int min_saved = 0);
 // Row pitch for n columns of an activation that is an operand of dense layers: n, or 64 more where n columns are a
 // multiple of 4 KiB -- the tile kernel's workgroups read the same slab of 256 rows at a time, and rows that far apart
 // on a power of two put it on a few memory channels (35400 rows x 4096 columns, K = 16384: 1.07 -> 1.18
@@ -540,15 +543,19 @@ bool z2z_linear_takes_pitch(const z2z_ctx* c, int R, int N, int K);
 // the layer is not split at this shape, nothing was launched.
 int z2z_launch_linear_parts(z2z_ctx* c, const void* A, const void* W, int R, const int32_t* rows_dev, int N, int K,
                             const float** partial, int* ksplit, hipStream_t s, bool once = false);
+// Slabs that a cut saves in the gated block's dF and dX: few tiles wait for memory at every slab, two microseconds of it, and eight saved are worth the sum's launch.  (237 rows,
+// d = 1024, d_ff = 2752: dF 41.5 -> 21.1 + 6.9 us; a training step of 16 / 100 rows, d = 256, d_ff = 704 73 / 82 -> 61 / 72.  The weights' gradients lose: 1000 rows, d = 2048
+// the step 323 -> 335.)
+constexpr int kGatedMinSaved = 8;
 // The gated block's own products (bf16; K a multiple of 64, d_ff of 64):
-//   z2z_launch_gated_hidden   F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff], and, where kept is given, the two products beside each other, fp32 [R, 2 d_ff]
+//   z2z_launch_gated_hidden   F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff]; kept (or nullptr): what the backward pass is given, F the first of it
 //   z2z_launch_gated_sum      the same from fp32 parts [ksplit][R][2 d_ff] of the products
-//   z2z_launch_gated_slopes   dF = dY W, W [K, d_ff], as dG | dU [R, 2 d_ff], and F once more
+//   z2z_launch_gated_slopes   dF = dY W, W [K, d_ff], as dG | dU [R, 2 d_ff]
 int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K,
                             hipStream_t s, bool once = false);
 int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, void* kept, hipStream_t s);
-int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, int act, void* slopes, void* F, int R, const int32_t* rows_dev,
-                            int d_ff, int K, hipStream_t s);
+int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+                            hipStream_t s);
 // out = sum of fp32 parts [ksplit][R][N] + residual, bf16 (stream_f32: fp32)
 int z2z_launch_linear_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int N, const void* residual, void* out, bool stream_f32,
                           hipStream_t s);

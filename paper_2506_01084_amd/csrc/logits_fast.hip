@@ -281,7 +281,7 @@ __host__ __device__ __forceinline__ LastRound last_round(const LogitsArgs& a, in
   r.per = n_slabs;
   // (what the XCD with the most tiles left gains decides: the launch ends with that one)
   const int wgs = r.whole ? F_WGS : F_XCD_WGS, most = r.whole ? tiles : longest - r.full;
-  if (r.rem > 0 && most <= wgs / 2 && n_slabs - part_slabs(wgs, most, n_slabs) >= F_MIN_SAVED) {
+  if (r.rem > 0 && most <= wgs / 2 && n_slabs - part_slabs(wgs, most, n_slabs) >= (a.min_saved ? a.min_saved : F_MIN_SAVED)) {
     r.per = part_slabs(wgs, r.rem, n_slabs);
     r.ways = (n_slabs + r.per - 1) / r.per;    // no empty parts
   }
@@ -728,15 +728,18 @@ __device__ __forceinline__ void store_prob16(const Acc& acc, const LogitsArgs& a
 }
 
 // Store one finished tile of a gated block's first product: blocks of 16 gate columns and of the same 16 columns of the other projection alternate
-// (see gated_offset), so that a lane holds both of an element.  col_base: of the tile's 128 columns of F.
-__device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& a, int row_base, int r_end, int col_base) {
-  const int lane15 = threadIdx.x & 15, f = a.gated.d_ff;
+// (see gated_offset), so that a lane holds both of an element.  row0, col0: of the wave's 128 rows and 64 columns of F (uniform, as every address but a lane's
+// offset is).  WHOLE: all of them exist.
+template <bool WHOLE>
+__device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& a, int row0, int r_end, int col0) {
+  const int lane15 = threadIdx.x & 15, quarter = (threadIdx.x >> 4) & 3, f = a.gated.d_ff;
+  const uint32_t own = (uint32_t)(lane15 * f + quarter * 4);                               // element of this lane's four in a block
+  const uint32_t eight = (uint32_t)(lane15 * a.ldo + (quarter & 1) * 16 + (quarter >> 1) * 8);     // ... of its eight in two blocks (eight_columns)
 #pragma unroll
   for (int j = 0; j < F_N; ++j) {
-    const int row = row_base + j * 16 + lane15;
-    const bool row_ok = row < r_end;
+    const bool row_ok = WHOLE || row0 + j * 16 + lane15 < r_end;
+    const size_t at = (size_t)(row0 + j * 16) * f + col0;
     uint2 h[F_N / 2];
-    float* kept = a.gated.kept ? reinterpret_cast<float*>(a.gated.kept) + (size_t)row * 2 * f : nullptr;
 #pragma unroll
     for (int k = 0; k < F_N / 2; ++k) {
       float g[4], u[4];
@@ -745,46 +748,65 @@ __device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& 
         g[e] = read_acc(acc[2 * k][j][e]);
         u[e] = read_acc(acc[2 * k + 1][j][e]);
       }
-      h[k] = z2z_gated::hidden4(g, u, a.gated.act);
-      const int col = col_base + k * 16;
-      if (kept && row_ok && col < f) {
-        *reinterpret_cast<float4*>(kept + col) = float4{g[0], g[1], g[2], g[3]};
-        *reinterpret_cast<float4*>(kept + f + col) = float4{u[0], u[1], u[2], u[3]};
+      if (a.gated.kept_hi) {
+        uint4 hi;
+        uint2 lo;
+        h[k] = z2z_gated::hidden_and_kept4(g, u, a.gated.act, &hi, &lo);
+        if (WHOLE || (row_ok && col0 + k * 16 + quarter * 4 < f)) {
+          *reinterpret_cast<uint4*>(a.gated.kept_hi + at + k * 16 + own) = hi;
+          *reinterpret_cast<uint2*>(a.gated.kept_lo + at + k * 16 + own) = lo;
+        }
+      } else {
+        h[k] = z2z_gated::hidden4(g, u, a.gated.act);
       }
     }
-    uint16_t* out_row = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo;
+    uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + (size_t)(row0 + j * 16) * a.ldo + col0;
 #pragma unroll
-    for (int k = 0; k < F_N / 2; k += 2) store_two_blocks(out_row, row_ok, col_base, k, h[k], h[k + 1], f);
+    for (int k = 0; k < F_N / 2; k += 2) {
+      const uint4 v = eight_columns(h[k], h[k + 1]);
+      if (WHOLE || (row_ok && col0 + k * 16 + (quarter & 1) * 16 + (quarter >> 1) * 8 < f)) *reinterpret_cast<uint4*>(out + k * 16 + eight) = v;
+    }
   }
 }
 
-// Store one finished tile of dF = dY W2 as the gated block's gradients dG | dU, and F beside them for dW2.  G and U of the next 16 rows are asked for ahead
-// of the arithmetic on these; the scheduling barriers keep the pieces apart (without them 1 KB a lane is spilled).
-__device__ __forceinline__ void store_gated_slopes16(const Acc& acc, const LogitsArgs& a, int row_base, int r_end, int col_base) {
-  const int lane15 = threadIdx.x & 15, f = a.gated.d_ff;
+// Store one finished tile of dF = dY W2 as the gated block's gradients dG | dU; row0, col0: of the wave's 128 rows and columns.  What was kept of the next rows is
+// asked for two pieces ahead; the scheduling barriers keep the pieces apart (without them 1 KB a lane is spilled).
+template <bool WHOLE>
+__device__ __forceinline__ void store_gated_slopes16(const Acc& acc, const LogitsArgs& a, int row0, int r_end, int col0) {
+  const int lane15 = threadIdx.x & 15, quarter = (threadIdx.x >> 4) & 3, f = a.gated.d_ff;
+  const uint32_t own = (uint32_t)(lane15 * f + quarter * 4), eight = (uint32_t)(lane15 * a.ldo + (quarter & 1) * 16 + (quarter >> 1) * 8);
   // (four blocks of 16 rows x 16 columns at a time)
-  constexpr int N = F_N / 2;
-  float4 g[2][N], u[2][N];
-  auto load = [&](int p, float4 (&gp)[N], float4 (&up)[N]) __attribute__((always_inline)) {
-    const int row = row_base + (p >> 1) * 16 + lane15;
-    const float* kept = reinterpret_cast<const float*>(a.gated.kept) + (size_t)min(row, r_end - 1) * 2 * f;
+  constexpr int N = F_N / 2, AHEAD = 2;
+  uint4 hi[AHEAD + 1][N];
+  uint2 lo[AHEAD + 1][N];
+  auto load = [&](int p, uint4 (&hp)[N], uint2 (&lp)[N]) __attribute__((always_inline)) {
+    const int row = row0 + (p >> 1) * 16, col = col0 + (p & 1) * N * 16;
+    if (WHOLE) {
+      const size_t at = (size_t)row * f + col;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int col = min(col_base + ((p & 1) * N + i) * 16, f - 4);
-      gp[i] = *reinterpret_cast<const float4*>(kept + col);
-      up[i] = *reinterpret_cast<const float4*>(kept + f + col);
+      for (int i = 0; i < N; ++i) {
+        hp[i] = *reinterpret_cast<const uint4*>(a.gated.kept_hi + at + i * 16 + own);
+        lp[i] = *reinterpret_cast<const uint2*>(a.gated.kept_lo + at + i * 16 + own);
+      }
+    } else {
+      const size_t at = (size_t)min(row + lane15, r_end - 1) * f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = min(col + i * 16 + quarter * 4, f - 4);
+        hp[i] = *reinterpret_cast<const uint4*>(a.gated.kept_hi + at + c);
+        lp[i] = *reinterpret_cast<const uint2*>(a.gated.kept_lo + at + c);
+      }
     }
   };
-  load(0, g[0], u[0]);
+#pragma unroll
+  for (int p = 0; p < AHEAD; ++p) load(p, hi[p], lo[p]);
 #pragma unroll
   for (int p = 0; p < 2 * F_N; ++p) {
     __builtin_amdgcn_sched_barrier(0);
-    if (p + 1 < 2 * F_N) load(p + 1, g[(p + 1) & 1], u[(p + 1) & 1]);
+    if (p + AHEAD < 2 * F_N) load(p + AHEAD, hi[(p + AHEAD) % (AHEAD + 1)], lo[(p + AHEAD) % (AHEAD + 1)]);
     const int j = p >> 1, i0 = (p & 1) * N;
-    const int row = row_base + j * 16 + lane15;
-    const bool row_ok = row < r_end;
-    uint16_t* out_row = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo;
-    uint16_t* slopes = reinterpret_cast<uint16_t*>(a.gated.slopes) + (size_t)row * 2 * f;
+    const bool row_ok = WHOLE || row0 + j * 16 + lane15 < r_end;
+    uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + (size_t)(row0 + j * 16) * a.ldo + col0 + i0 * 16;
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
       __builtin_amdgcn_sched_barrier(0);
@@ -794,11 +816,13 @@ __device__ __forceinline__ void store_gated_slopes16(const Acc& acc, const Logit
         float df[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) df[e] = read_acc(acc[i0 + i + h][j][e]);
-        s[h] = z2z_gated::slopes4(df, g[p & 1][i + h], u[p & 1][i + h], a.gated.act);
+        s[h] = z2z_gated::slopes4(df, hi[p % (AHEAD + 1)][i + h], lo[p % (AHEAD + 1)][i + h]);
       }
-      store_two_blocks(slopes, row_ok, col_base, i0 + i, s[0].dg, s[1].dg, f);
-      store_two_blocks(slopes + f, row_ok, col_base, i0 + i, s[0].du, s[1].du, f);
-      store_two_blocks(out_row, row_ok, col_base, i0 + i, s[0].f, s[1].f, f);
+      const uint4 dg = eight_columns(s[0].dg, s[1].dg), du = eight_columns(s[0].du, s[1].du);
+      if (WHOLE || (row_ok && col0 + (i0 + i) * 16 + (quarter & 1) * 16 + (quarter >> 1) * 8 < f)) {
+        *reinterpret_cast<uint4*>(out + i * 16 + eight) = dg;
+        *reinterpret_cast<uint4*>(out + f + i * 16 + eight) = du;
+      }
     }
   }
 }
@@ -1314,10 +1338,19 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
       if (MODE == 2) {
         if (it.part >= 0)
           store_partial16(acc, a.split + (ptrdiff_t)it.part * (FT * FT) - ((ptrdiff_t)r0 * FT + vt * FT), FT, row_base, r_end, col_base, n_valid);
-        else if (GATE == 1)
-          store_gated16(acc, a, row_base, r_end, vt * (FT / 2) + wv * 64 + quarter * 4);
-        else if (GATE == 2)
-          store_gated_slopes16(acc, a, row_base, r_end, col_base);
+        else if (GATE != 0) {
+          int row0 = r0 + wr * 128, col0 = GATE == 1 ? vt * (FT / 2) + wv * 64 : vt * FT + wv * 128;
+          asm volatile("" : "+s"(row0), "+s"(col0));
+          const bool whole = row0 + 128 <= r_end && col0 + (GATE == 1 ? 64 : 128) <= a.gated.d_ff;
+          if (GATE == 1 && whole)
+            store_gated16<true>(acc, a, row0, r_end, col0);
+          else if (GATE == 1)
+            store_gated16<false>(acc, a, row0, r_end, col0);
+          else if (whole)
+            store_gated_slopes16<true>(acc, a, row0, r_end, col0);
+          else
+            store_gated_slopes16<false>(acc, a, row0, r_end, col0);
+        }
         else if (SUM)
           store_sum16<TH>(acc, a, row_base, r_end, col_base, n_valid);
         else if (TW && !a.residual)
@@ -1428,11 +1461,13 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
         }
         from += (size_t)last.rem * (FT * FT);
       }
-      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)(r0 + row) * a.ldo + fcol) = z2z_gated::hidden4(x[0], x[1], a.gated.act);
-      if (a.gated.kept) {
-        float* kept = reinterpret_cast<float*>(a.gated.kept) + (size_t)(r0 + row) * 2 * a.gated.d_ff + fcol;
-        *reinterpret_cast<float4*>(kept) = float4{x[0][0], x[0][1], x[0][2], x[0][3]};
-        *reinterpret_cast<float4*>(kept + a.gated.d_ff) = float4{x[1][0], x[1][1], x[1][2], x[1][3]};
+      uint2* out = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)(r0 + row) * a.ldo + fcol);
+      if (a.gated.kept_hi) {
+        const size_t at = (size_t)(r0 + row) * a.gated.d_ff + fcol;
+        *out = z2z_gated::hidden_and_kept4(x[0], x[1], a.gated.act, reinterpret_cast<uint4*>(a.gated.kept_hi + at),
+                                           reinterpret_cast<uint2*>(a.gated.kept_lo + at));
+      } else {
+        *out = z2z_gated::hidden4(x[0], x[1], a.gated.act);
       }
       continue;
     }
@@ -1463,14 +1498,12 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
       }
       if (GATE == 2) {
         const float df[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        const size_t at = (size_t)row * 2 * a.gated.d_ff + col;
-        const float* kept = reinterpret_cast<const float*>(a.gated.kept) + at;
-        const z2z_gated::Slopes4 s = z2z_gated::slopes4(df, *reinterpret_cast<const float4*>(kept),
-                                                        *reinterpret_cast<const float4*>(kept + a.gated.d_ff), a.gated.act);
-        uint16_t* slopes = reinterpret_cast<uint16_t*>(a.gated.slopes) + at;
+        const size_t at = (size_t)row * a.gated.d_ff + col;
+        const z2z_gated::Slopes4 s = z2z_gated::slopes4(df, *reinterpret_cast<const uint4*>(a.gated.kept_hi + at),
+                                                        *reinterpret_cast<const uint2*>(a.gated.kept_lo + at));
+        uint16_t* slopes = reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo + col;
         *reinterpret_cast<uint2*>(slopes) = s.dg;
         *reinterpret_cast<uint2*>(slopes + a.gated.d_ff) = s.du;
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)row * a.ldo + col) = s.f;
         continue;
       }
       finish_linear(x[i], bias, a.act, a.residual, a.out, a.stream_f32, (size_t)row * a.ldo + col);

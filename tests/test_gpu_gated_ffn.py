@@ -59,7 +59,14 @@ def test_forward(rows, d, f, act):
         again = torch.full_like(X, float("nan"))
         ctx.gated_ffn(X, block, again, residual=residual, kept=kept)
         assert torch.equal(Y, again)
-        _within(kept, np.concatenate([ref["G"], ref["U"]], axis=1), ref["kept_bound"], "kept")
+        # (what the library keeps: F, then act(G) and U act'(G), the upper halves of both, then the next bytes)
+        n, raw = rows * f, kept.view(torch.uint8).flatten()
+        F = raw[:2 * n].view(torch.bfloat16).reshape(rows, f)
+        hi, lo = raw[2 * n:6 * n].reshape(n, 4).int(), raw[6 * n:].reshape(n, 2).int()
+        for i, name in enumerate(("a", "s")):
+            word = lo[:, i] << 8 | hi[:, 2 * i] << 16 | hi[:, 2 * i + 1] << 24
+            _within(word.view(torch.float32).reshape(rows, f), ref[name], ref[name + "_bound"], name)
+        _within(F, ref["F"], ref["F_err"] + 1e-30, "F")
     in_place = R.clone()
     ctx.gated_ffn(X, block, in_place, residual=in_place)
     assert torch.equal(in_place, again)

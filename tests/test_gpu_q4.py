@@ -46,7 +46,7 @@ def test_quantize(rows, cols, group):
 
 
 # rows on both sides of the product's blocks of 16 and of the change to expanded weights; widths that no block of 128 columns divides
-@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 32, 33, 48, 49, 100, 192, 193, 300])
+@pytest.mark.parametrize("rows", [1, 2, 8, 9, 15, 16, 17, 32, 33, 48, 49, 64, 65, 100, 192, 193, 320, 321, 400])
 @pytest.mark.parametrize("d,f,group,act", [(64, 64, 32, "silu"), (192, 448, 64, "gelu"), (320, 64, 32, "gelu"), (512, 1152, 128, "silu"), (1088, 320, 64, "silu"),
                                            (2048, 192, 32, "silu")])
 def test_forward(rows, d, f, group, act):
@@ -63,11 +63,11 @@ def test_forward(rows, d, f, group, act):
     assert (block.desc.group, block.d, block.d_ff) == (group, d, f)
     Y = torch.full_like(X, float("nan"))
     ctx.gated_ffn(X, block, Y, residual=R)
-    ref = oracle.gated_ffn(_host(X), *host, act, _host(R), round_weights=rows > 192)
+    ref = oracle.gated_ffn(_host(X), *host, act, _host(R), round_weights=rows > 320)
     _within(Y, ref["Y"], ref["Y_bound"], "Y")
     Z = torch.full_like(X, float("nan"))
     ctx.gated_ffn(X, block, Z, residual=None)
-    ref = oracle.gated_ffn(_host(X), *host, act, None, round_weights=rows > 192)
+    ref = oracle.gated_ffn(_host(X), *host, act, None, round_weights=rows > 320)
     _within(Z, ref["Y"], ref["Y_bound"], "Y without a residual")
 
 
