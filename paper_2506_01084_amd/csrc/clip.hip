@@ -211,7 +211,9 @@ __global__ void __launch_bounds__(C_THREADS) clip_scale_kernel(ClipList l, const
       const uint4 y = c == 1.0f ? v[i] : bf16 ? scaled<true>(v[i], c) : scaled<false>(v[i], c);
       unsigned char* to = out + first + (int64_t)at * 16;
       if (wide) {
-        *reinterpret_cast<uint4*>(to) = y;
+        // (past the caches, which hold what is still to be read: 0.8 GB in 36 tensors 457 -> 424 us, 4 GB 2218 -> 2180)
+        typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+        __builtin_nontemporal_store(u32x4{y.x, y.y, y.z, y.w}, reinterpret_cast<u32x4*>(to));
       } else {                       // (on other boundaries than what is read)
         const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll

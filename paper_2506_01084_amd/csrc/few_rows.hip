@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(64 * W_WAVES, 2) few_rows_kernel(FewArgs a) {
   constexpr bool Q4 = CHAIN != 0;
   constexpr int LOADS = Q4 ? 1 : 4;                // of a tile's unit, 16 bytes a lane
   constexpr int SCALES = Q4 ? 4 / (Q4 ? CHAIN : 1) : 1;
-  constexpr int DEPTH = Q4 && NB == 1 ? 2 : 1;     // units ahead
+  constexpr int DEPTH = Q4 && NB == 1 ? 2 : 1;     // units ahead (three of weights with one of X: 1 row, d = 4096, d_ff = 10944 19.8 us -> 23.2)
   __shared__ f32x4 sums[W_WAVES][TILES * NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r = lane & 15, j = lane >> 4;
   const int R = a.rows_dev ? min(a.R, *a.rows_dev) : a.R;
