@@ -251,7 +251,7 @@ int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, i
  *   w_1 [2 f, d], w_2 [d, f]: bf16, group = 0; or in 4 bits as z2z_quantize_q4 writes them, group = 32, 64 or 128, with scale_1 [d / group, 2 f] and
  *        scale_2 [f / group, d].  Up to 320 rows are multiplied by v, the scales with fp32 sums;
  *        more rows by the weights rounded to bf16, which takes 6 d f bytes of work space.
- *   d_X [rows, d], d_residual [rows, d] or NULL, d_Y [rows, d] out: bf16.  d_Y may be d_residual, else it overlaps neither input (Z2Z_EINVAL)
+ *   d_X [rows, d], d_residual [rows, d] or NULL, d_Y [rows, d] out: bf16.  d_Y may be d_residual, else it overlaps nothing that the call reads (Z2Z_EINVAL)
  *   d_kept  [rows, 2 f] float out or NULL: what z2z_gated_ffn_backward needs of G and U, for that call alone to read (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
  * A row's results do not depend on the other rows' values.  rows = 0 is a call that does nothing.  bf16 contexts, d and d_ff multiples of 64 (with 4 bits of group,
  * too), rows <= 2^22, (d_ff + 128) d < 2^30, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and for few rows the parts of the products. */

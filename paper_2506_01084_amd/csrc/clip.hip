@@ -234,6 +234,16 @@ __global__ void __launch_bounds__(C_THREADS) clip_scale_kernel(ClipList l, const
   }
 }
 
+// Many sums as one, ahead of many launches that would each add them up: one workgroup.
+constexpr int C_PARTS = 4096;
+__global__ void __launch_bounds__(C_THREADS) clip_total_kernel(const double* part, int parts, double* total) {
+  __shared__ double xch[4];
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < parts; i += C_THREADS) sum += part[i];
+  sum = workgroup_sum(sum, xch);
+  if (threadIdx.x == 0) *total = sum;
+}
+
 struct Interval {
   uintptr_t begin, end;
   bool written;
@@ -242,6 +252,13 @@ struct Interval {
 }  // namespace
 
 int z2z_launch_clip_gradients(z2z_ctx* c, const z2z_gradient* g, int n, float max_norm, float* norm, hipStream_t s) {
+  // (a list's chunks are counted in 32 bits: 64 TiB)
+  long long all = 0;
+  for (int i = 0; i < n; ++i) {
+    if (g[i].n > (1LL << 44)) return Z2Z_EUNSUPPORTED;
+    all += std::max(1LL, ((long long)g[i].n * 4 + C_CHUNK - 1) / C_CHUNK);
+  }
+  if (all > 0x7FFF0000LL) return Z2Z_EUNSUPPORTED;
   // what is written overlaps nothing else
   Interval* iv = new (std::nothrow) Interval[2 * (size_t)n + 1];
   if (!iv) return Z2Z_ENOMEM;
@@ -267,19 +284,17 @@ int z2z_launch_clip_gradients(z2z_ctx* c, const z2z_gradient* g, int n, float ma
   delete[] iv;
   if (clash) return Z2Z_EINVAL;
 
-  // (a list's chunks are counted in 32 bits: 64 TiB)
-  long long all = 0;
-  for (int i = 0; i < n; ++i) {
-    if (g[i].n > (1LL << 44)) return Z2Z_EUNSUPPORTED;
-    all += std::max(1LL, ((long long)g[i].n * 4 + C_CHUNK - 1) / C_CHUNK);
-  }
-  if (all > 0x7FFF0000LL) return Z2Z_EUNSUPPORTED;
   const int lists = std::max(1, (n + C_LIST - 1) / C_LIST), most = 4 * c->num_cu;
-  int rc = z2z_work_reserve(c, &c->clip_ws, (size_t)lists * most * sizeof(double), s);
+  int rc = z2z_work_reserve(c, &c->clip_ws, ((size_t)lists * most + 1) * sizeof(double), s);
   if (rc != Z2Z_OK) return rc;
   double* part = reinterpret_cast<double*>(c->clip_ws.p);
   int parts = 0;
   for (int pass = 0; pass < 2; ++pass) {
+    if (pass == 1 && parts > C_PARTS) {
+      hipLaunchKernelGGL(clip_total_kernel, dim3(1), dim3(C_THREADS), 0, s, part, parts, part + parts);
+      part += parts;
+      parts = 1;
+    }
     for (int first = 0; first < std::max(n, 1); first += C_LIST) {
       ClipList l = {};
       long long chunks = 0;

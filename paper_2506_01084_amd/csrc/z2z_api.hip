@@ -396,6 +396,33 @@ namespace {
 
 constexpr int32_t kFfnRows = 1 << 22;
 
+struct Bytes {
+  const void* p;
+  size_t n;
+};
+// Whether anything that is written overlaps anything that is read, or the rest of what is written.
+bool clashes(const Bytes* in, int n_in, const Bytes* out, int n_out) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int k = 0; k < n_in; ++k)
+      if (overlap_bytes(out[i].p, out[i].n, in[k].p, in[k].n)) return true;
+    for (int k = 0; k < i; ++k)
+      if (overlap_bytes(out[i].p, out[i].n, out[k].p, out[k].n)) return true;
+  }
+  return false;
+}
+
+// Bytes of a matrix of 4-bit weights as quantize_q4 writes them.
+size_t q4_bytes(size_t rows, size_t cols) { return rows * ((cols + 127) / 128) * 64; }
+
+struct FfnBytes {
+  size_t w_1, w_2, scale_1, scale_2;
+};
+FfnBytes ffn_bytes(const z2z_ctx* c, const z2z_ffn* f) {
+  const size_t d = c->cfg.d, n = f->d_ff;
+  if (!f->group) return FfnBytes{4 * n * d, 2 * n * d, 0, 0};
+  return FfnBytes{q4_bytes(2 * n, d), q4_bytes(d, n), 4 * n * d / f->group, 2 * n * d / f->group};
+}
+
 }  // namespace
 
 Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, float* d_kept,
@@ -406,9 +433,10 @@ Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z
   if (rc != Z2Z_OK) return rc;
   if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
   const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 8;
-  if (overlap_bytes(d_Y, row, d_X, row) || (d_Y != d_residual && overlap_bytes(d_Y, row, d_residual, row)) || overlap_bytes(d_kept, kept, d_X, row) ||
-      overlap_bytes(d_kept, kept, d_Y, row) || overlap_bytes(d_kept, kept, d_residual, row))
-    return Z2Z_EINVAL;
+  const FfnBytes w = ffn_bytes(ctx, ffn);
+  const Bytes in[] = {{d_X, row}, {d_residual == d_Y ? nullptr : d_residual, row}, {ffn->w_1, w.w_1}, {ffn->w_2, w.w_2}, {ffn->scale_1, w.scale_1}, {ffn->scale_2, w.scale_2}};
+  const Bytes out[] = {{d_Y, row}, {d_kept, kept}};
+  if (clashes(in, 6, out, 2) || overlap_bytes(d_kept, kept, d_residual, row)) return Z2Z_EINVAL;
   rc = enter(ctx, static_cast<hipStream_t>(stream));
   if (rc != Z2Z_OK || rows == 0) return rc;
   rc = z2z_work_reserve(ctx, &ctx->ffn_ws, z2z_ffn_work(ffn, ctx->cfg.d, rows), static_cast<hipStream_t>(stream));
@@ -426,18 +454,10 @@ Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, 
   if (rc != Z2Z_OK) return rc;
   if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
   const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 8;
-  const size_t w2 = (size_t)ctx->cfg.d * ffn->d_ff * 2, w1 = 2 * w2;
-  // (what is written against what is read, and against the rest of what is written)
-  struct {
-    const void* p;
-    size_t n;
-  } in[] = {{d_X, row}, {d_kept, kept}, {d_dY, row}, {ffn->w_1, w1}, {ffn->w_2, w2}}, out[] = {{d_dX, row}, {grad->w_1, w1}, {grad->w_2, w2}};
-  for (int i = 0; i < 3; ++i) {
-    for (const auto& x : in)
-      if (overlap_bytes(out[i].p, out[i].n, x.p, x.n)) return Z2Z_EINVAL;
-    for (int k = 0; k < i; ++k)
-      if (overlap_bytes(out[i].p, out[i].n, out[k].p, out[k].n)) return Z2Z_EINVAL;
-  }
+  const FfnBytes w = ffn_bytes(ctx, ffn);
+  const size_t w1 = w.w_1, w2 = w.w_2;
+  const Bytes in[] = {{d_X, row}, {d_kept, kept}, {d_dY, row}, {ffn->w_1, w1}, {ffn->w_2, w2}}, out[] = {{d_dX, row}, {grad->w_1, w1}, {grad->w_2, w2}};
+  if (clashes(in, 5, out, 3)) return Z2Z_EINVAL;
   rc = enter(ctx, static_cast<hipStream_t>(stream));
   if (rc != Z2Z_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -452,7 +472,7 @@ Z2Z_API int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t
   if (!aligned16(d_W) || !aligned16(d_q) || !aligned16(d_scale)) return Z2Z_EINVAL;
   if (group != 32 && group != 64 && group != 128) return Z2Z_EINVAL;
   if (ctx->cfg.dtype != Z2Z_BF16 || rows % 16 != 0 || cols % 64 != 0 || cols % group != 0) return Z2Z_EUNSUPPORTED;
-  const size_t n = (size_t)rows * cols, q = (size_t)rows * ((cols + 127) / 128) * 64, sc = n / group * 2;
+  const size_t n = (size_t)rows * cols, q = q4_bytes(rows, cols), sc = n / group * 2;
   if (overlap_bytes(d_q, q, d_W, 2 * n) || overlap_bytes(d_scale, sc, d_W, 2 * n) || overlap_bytes(d_q, q, d_scale, sc)) return Z2Z_EINVAL;
   const int rc = enter(ctx, static_cast<hipStream_t>(stream));
   if (rc != Z2Z_OK) return rc;

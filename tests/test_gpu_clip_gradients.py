@@ -178,3 +178,16 @@ def test_binding_refusals():
     with pytest.raises(ValueError):
         api.Gradients([t.cpu()])
     assert (t == 1).all()
+
+
+def test_more_sums_than_a_launch_adds_up():
+    """Some of 600 tensors of 40 chunks each: the launches' sums are added up by one of their own."""
+    ctx = _context()
+    whole = torch.randn(600 * 40 * 16384, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda").bfloat16()
+    tensors = list(whole.split(40 * 16384))
+    assert len(tensors) == 600
+    want = float(whole.double().norm())
+    before = whole.double()
+    norm, c = _clip(ctx, tensors, 2.0)
+    assert abs(norm - want) <= want * 35 * 2.0 ** -24 and abs(c - 2.0 / want) <= 2.0 / want * 36 * 2.0 ** -24
+    assert torch.all((whole.double() - before * (2.0 / want)).abs() <= before.abs() * (2.0 / want) * (2.0 ** -8 + 1e-5) + 1e-38)
