@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libz2z.so")
 
 SOURCES = ["z2z_api.hip", "lzw.hip", "hyper_embed.hip", "logits.hip", "logits_general.hip", "logits_fast.hip", "logits_mid.hip", "logits_decode.hip",
            "sample_trunc.hip", "hyper_encoder.hip", "dense.hip", "loss_backward.hip", "embed_codes.hip", "beam.hip", "distill.hip", "gated_ffn.hip", "q4.hip", "few_rows.hip",
-           "clip.hip"]
+           "small_tile.hip", "clip.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -2,11 +2,12 @@
 // more of its block): Y = (act(X W1[:f]^T) * (X W1[f:]^T)) W2^T + residual.
 //
 // Forward, many rows: one launch of the tile kernel for both projections, activation and product (a tile of 256 weight rows is 128 gate columns and the same 128
-// of the other projection), one for the product with W2.  Few rows are bound by the weights' bytes: the weight-streaming kernel, in bf16 or from 4 bits (q4.hip), leaves
+// of the other projection), one for the product with W2; fewer take smaller tiles (small_tile.hip).  Few rows are bound by the weights' bytes: the weight-streaming kernel, in bf16 or from 4 bits (q4.hip), leaves
 // parts of the products, whose sum applies the activation.  Backward: dF = dY W2 becomes dG | dU in the epilogue; then dW2 = dY^T F,
 // dW1 = [dG | dU]^T X, dX = [dG | dU] W1, all on operands as they are.
 #include "few_rows.h"
 #include "logits_common.h"
+#include "small_tile.h"
 
 namespace {
 
@@ -22,13 +23,28 @@ __global__ void __launch_bounds__(256) fill_zero_kernel(uint4* p, size_t n, uint
 }
 
 // Rows up to which the products run on the kernel that shares nothing between workgroups but has no parts to add up (few_rows.hip): every workgroup reads all rows, which
-// costs more than the sums from a number on that depends on the weights.  us, that kernel / the others:
-//   bf16   d = 4096, d_ff = 10944  1 row 47 / 54, 16 rows 57 / 61, 24 70 / 65;   2048, 5504  1 19.8 / 24.4, 16 25.5 / 26.9, 24 31.1 / 27.4;   1024, 2752  1 9.5 / 16.8, 64 22.8 / 24.3,
-//          256 34.4 / 52.3, 300 48.1 / 52.5
+// costs more than the others' sums, or tiles, from a number on that depends on the weights.  us, that kernel / the others:
+//   bf16   d = 4096, d_ff = 10944  1 row 47 / 54, 16 rows 57 / 61, 24 70 / 65;   2048, 5504  1 19.8 / 23.7, 16 25.7 / 24.7, 24 31.1 / 27.4;   1024, 2752  1 10.5 / 14.5, 16 12.2 / 15.2,
+//          33 17.4 / 15.8;   512, 1408  33 11.5 / 13.1, 65 14.4 / 13.4;   256, 704  237 10.3 / 12.9
 //   4 bits d = 4096, d_ff = 10944, group 64  1 19.8 / 26.6, 4 21.7 / 27.8, 16 32.2 / 29.6;   3584, 9600, 128  4 17.8 / 21.6, 16 27.2 / 24.6;   2048, 5504, 32  4 13.7 / 15.1, 16 18.0 / 18.3,
 //          32 26.8 / 24.5;   1024, 2752, 64  1 8.3 / 13.1, 32 12.8 / 15.5, 64 20.1 / 20.6, 128 24.5 / 26.5
 bool few_rows(const z2z_ffn* f, int d, int R) {
-  return R <= (f->group ? 8 : 16) || ((long long)d * f->d_ff <= (1 << 22) && R <= (f->group ? 64 : 256));
+  if (f->group) return R <= 8 || ((long long)d * f->d_ff <= (1 << 22) && R <= 64);
+  return R <= 16 || (R <= 256 && (long long)R * d * f->d_ff <= (3 << 24));
+}
+
+// Rows times d times d_ff up to which a product runs on tiles of 64 x 64 (small_tile.hip): more, and its 256 x 256 tiles keep enough CUs busy.  us of a product, or of
+// the two of a forward pass, with the others / on small tiles:
+//   forward    d = 1024, d_ff = 2752  65 rows 25.6 / 18.0, 300 53 / 24, 2000 93 / 62, 4000 114 / 151;   2048, 5504  100 39.7 / 30.2, 500 80 / 67, 700 94 / 93, 1000 99 / 113;   3584, 9600  65 62.4 / 59.5,
+//              160 92 / 76, 300 121 / 136;   4096, 10944  65 of weights that no cache holds: 78 / 86
+//   dF         1024, 2752  2000 -13 us, 4000 +10;   2048, 5504  1000 -5, 1500 +7;   3584, 9600  237 -3, 500 +9
+//   dX         1024, 2752  1000 -8, 1500 +1;   2048, 5504  237 -12, 500 +1;   2560, 6912  65 -9, 237 +1
+//   dW1, dW2   1024, 2752  1500 -9, 2000 +4;   512, 1408  2000 -26, 4000 0;   1536, 4096  237 +1;   2048, 5504  65 -4, 237 +11: whatever the rows, large outputs are not for it
+constexpr long long kSmallForward = 3ll << 31, kSmallSlopes = 5ll << 31, kSmallInput = 3ll << 30, kSmallWeight = 1ll << 32;
+
+bool small_tiles(const z2z_ffn* f, int d, int R, long long most) { return (long long)d * f->d_ff * R <= most; }
+bool small_forward(const z2z_ffn* f, int d, int R) {
+  return small_tiles(f, d, R, kSmallForward) && (size_t)3 * d * f->d_ff * sizeof(uint16_t) <= 2 * z2z_logits::kKeepBytes;
 }
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -44,7 +60,7 @@ int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kep
   const int d = c->cfg.d, dff = f->d_ff;
   unsigned char* F = reinterpret_cast<unsigned char*>(kept ? kept : work);     // (the first of what is kept)
   const void* w1 = f->w_1;
-  *out = z2z_ffn_out{F, f->w_2, nullptr, 0, dff, false, false};
+  *out = z2z_ffn_out{F, f->w_2, nullptr, 0, dff, false, false, false};
   if (few_rows(f, d, R)) {
     out->scale = f->scale_2;
     out->group = f->group;
@@ -69,6 +85,10 @@ int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kep
     w1 = e1;
     out->w = e2;
   }
+  if (small_forward(f, d, R)) {
+    out->small = true;
+    return z2z_launch_small_gated(X, w1, f->act, F, kept, R, rows_dev, dff, d, s);
+  }
   // (few rows: does anything of the weights stay in the memory-side cache until the next call?)
   out->once = (size_t)3 * d * dff * sizeof(uint16_t) > z2z_logits::kKeepBytes;
   return z2z_launch_gated_hidden(c, X, w1, f->act, F, kept, R, rows_dev, dff, d, s, out->once);
@@ -81,6 +101,7 @@ int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* resi
   int rc = z2z_launch_ffn_hidden(c, X, f, kept, R, rows_dev, work, &o, s);
   if (rc != Z2Z_OK) return rc;
   if (o.few) return z2z_launch_few_linear(o.F, o.w, o.scale, o.group, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
+  if (o.small) return z2z_launch_small_linear(c, o.F, o.w, false, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
   if (!o.group) return z2z_launch_linear(c, o.F, o.w, nullptr, residual, 0, Y, R, rows_dev, d, o.d_ff, s, stream_f32, nullptr, o.once);
   const float* partial = nullptr;
   int ksplit = 0;
@@ -96,12 +117,18 @@ int z2z_launch_ffn_backward(z2z_ctx* c, const void* X, const z2z_ffn* f, const v
   const int d = c->cfg.d, dff = f->d_ff;
   const void* F = kept;                              // (the first of what is kept)
   void *dw1 = const_cast<void*>(grad->w_1), *dw2 = const_cast<void*>(grad->w_2);
-  int rc = z2z_launch_gated_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, s);
+  int rc = small_tiles(f, d, R, kSmallSlopes) ? z2z_launch_small_slopes(dY, f->w_2, kept, work, R, rows_dev, dff, d, s)
+                                              : z2z_launch_gated_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, s);
   if (rc != Z2Z_OK) return rc;
-  rc = z2z_launch_linear_weight(c, dY, d, F, dff, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
+  if (small_tiles(f, d, R, kSmallWeight) && small_tiles(f, d, 1, 1 << 22)) {
+    rc = z2z_launch_small_weight(dY, F, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
+    if (rc == Z2Z_OK) rc = z2z_launch_small_weight(work, X, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
+  } else {
+    rc = z2z_launch_linear_weight(c, dY, d, F, dff, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
+    if (rc == Z2Z_OK) rc = z2z_launch_linear_weight(c, work, 2 * dff, X, d, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
+  }
   if (rc != Z2Z_OK) return rc;
-  rc = z2z_launch_linear_weight(c, work, 2 * dff, X, d, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
-  if (rc != Z2Z_OK) return rc;
+  if (small_tiles(f, d, R, kSmallInput)) return z2z_launch_small_linear(c, work, f->w_1, true, nullptr, dX, false, R, rows_dev, d, 2 * dff, s);
   return z2z_launch_linear_input(c, work, 2 * dff, f->w_1, d, 2 * dff, nullptr, dX, d, R, rows_dev, d, 2 * dff, s, {1, 0, 0}, 0, kGatedMinSaved);
 }
 

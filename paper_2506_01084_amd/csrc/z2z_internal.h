@@ -207,7 +207,7 @@ struct z2z_ffn_out {
   void* F;
   const void *w, *scale;
   int group, d_ff;
-  bool once, few;          // few: the second product runs on z2z_launch_few_linear
+  bool once, few, small;   // few, small: the second product runs on z2z_launch_few_linear, z2z_launch_small_linear
 };
 int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
                           hipStream_t s);

@@ -161,6 +161,18 @@ def test_backward(B, N, V, d, M, cap, n_layers, n_heads, d_ff, act, with_pos):
         assert torch.equal(a.tensors[0], b.tensors[0]) and torch.equal(a.tensors[1], b.tensors[1])
 
 
+# (books with room for far more rows than there are: the kernels are chosen by the room)
+ROOM = (1, 60, 900, 1024, 3, 2600, 1, 8, 1408, "silu", True)
+
+
+def test_forward_with_room():
+    test_forward(*ROOM)
+
+
+def test_backward_with_room():
+    test_backward(*ROOM)
+
+
 def test_training_step_then_serving():
     """Encode, loss, gradients, clipping of all of them, an update, and generation steps over the updated blocks in 4 bits, captured."""
     import torch

@@ -42,6 +42,18 @@ SHAPES = [(1, 64, 64), (1, 1024, 448), (2, 192, 704), (15, 320, 192), (16, 512, 
           (700, 128, 64), (1031, 576, 832), (2500, 256, 320)]
 
 
+# more work than tiles of 64 x 64 are for: two row tiles, widths of which the tile is no divisor, few slabs and many (in order of rows d d_ff; from the third on the gradient's
+# first product, too), and few rows over weights that no cache holds
+LARGE = [(1031, 3520, 1792), (300, 6400, 3456), (2500, 2048, 2112), (16411, 512, 1344), (40, 8192, 5504)]
+
+
+@pytest.mark.parametrize("rows,d,f", LARGE)
+def test_more_work_than_small_tiles_take(rows, d, f):
+    test_forward(rows, d, f, "silu")
+    if rows > 40:
+        test_backward(rows, d, f, "silu")
+
+
 @pytest.mark.parametrize("rows,d,f", SHAPES)
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 def test_forward(rows, d, f, act):
