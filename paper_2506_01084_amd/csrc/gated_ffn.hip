@@ -101,7 +101,7 @@ int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* resi
   int rc = z2z_launch_ffn_hidden(c, X, f, kept, R, rows_dev, work, &o, s);
   if (rc != Z2Z_OK) return rc;
   if (o.few) return z2z_launch_few_linear(o.F, o.w, o.scale, o.group, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
-  if (o.small) return z2z_launch_small_linear(c, o.F, o.w, false, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
+  if (o.small) return z2z_launch_small_linear(c, o.F, o.w, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
   if (!o.group) return z2z_launch_linear(c, o.F, o.w, nullptr, residual, 0, Y, R, rows_dev, d, o.d_ff, s, stream_f32, nullptr, o.once);
   const float* partial = nullptr;
   int ksplit = 0;
@@ -117,18 +117,18 @@ int z2z_launch_ffn_backward(z2z_ctx* c, const void* X, const z2z_ffn* f, const v
   const int d = c->cfg.d, dff = f->d_ff;
   const void* F = kept;                              // (the first of what is kept)
   void *dw1 = const_cast<void*>(grad->w_1), *dw2 = const_cast<void*>(grad->w_2);
-  int rc = small_tiles(f, d, R, kSmallSlopes) ? z2z_launch_small_slopes(dY, f->w_2, kept, work, R, rows_dev, dff, d, s)
+  // on small tiles the weight gradients go along with the products beside them
+  const bool weights = small_tiles(f, d, R, kSmallWeight) && small_tiles(f, d, 1, 1 << 22), input = small_tiles(f, d, R, kSmallInput);
+  const z2z_small_weight w1 = {work, X, add ? dw1 : nullptr, dw1, 2 * dff, d}, w2 = {dY, F, add ? dw2 : nullptr, dw2, d, dff};
+  int rc = small_tiles(f, d, R, kSmallSlopes) ? z2z_launch_small_slopes(dY, f->w_2, kept, work, R, rows_dev, dff, d, weights ? &w2 : nullptr, s)
                                               : z2z_launch_gated_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, s);
-  if (rc != Z2Z_OK) return rc;
-  if (small_tiles(f, d, R, kSmallWeight) && small_tiles(f, d, 1, 1 << 22)) {
-    rc = z2z_launch_small_weight(dY, F, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
-    if (rc == Z2Z_OK) rc = z2z_launch_small_weight(work, X, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
-  } else {
+  if (rc == Z2Z_OK && weights && !input) rc = z2z_launch_small_weight(w1, R, rows_dev, s);
+  if (rc == Z2Z_OK && !weights) {
     rc = z2z_launch_linear_weight(c, dY, d, F, dff, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
     if (rc == Z2Z_OK) rc = z2z_launch_linear_weight(c, work, 2 * dff, X, d, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
   }
   if (rc != Z2Z_OK) return rc;
-  if (small_tiles(f, d, R, kSmallInput)) return z2z_launch_small_linear(c, work, f->w_1, true, nullptr, dX, false, R, rows_dev, d, 2 * dff, s);
+  if (input) return z2z_launch_small_input(c, work, f->w_1, dX, R, rows_dev, d, 2 * dff, weights ? &w1 : nullptr, s);
   return z2z_launch_linear_input(c, work, 2 * dff, f->w_1, d, 2 * dff, nullptr, dX, d, R, rows_dev, d, 2 * dff, s, {1, 0, 0}, 0, kGatedMinSaved);
 }
 

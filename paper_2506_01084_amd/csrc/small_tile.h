@@ -1,15 +1,25 @@
 // The gated block's products on tiles of 64 x 64 (small_tile.hip), bf16; widths are multiples of 64:
 //   z2z_launch_small_gated    F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff]; kept: nullptr, or what the backward pass is given, F the first of it
 //   z2z_launch_small_slopes   dF = dY W, W [K, d_ff], as dG | dU [R, 2 d_ff]
-//   z2z_launch_small_linear   out [R, N] = A [R, K] W^T + residual, W [N, K] or (k_major) [K, N]; f32: residual and out are fp32
+//   z2z_launch_small_linear   out [R, N] = A [R, K] W^T + residual, W [N, K]; f32: residual and out are fp32
+//   z2z_launch_small_input    out [R, N] = A [R, K] W, W [K, N]
 //   z2z_launch_small_weight   out [M, N] = A [rows, M]^T W [rows, N] + residual
-// rows_dev: nullptr, or how many of the R rows, or rows, exist.
+// rows_dev: nullptr, or how many of the R rows, or rows, exist.  weight: nullptr, or a weight gradient over the same rows that goes along in the launch.
 #pragma once
 
 #include "z2z_internal.h"
 
+struct z2z_small_weight {
+  const void *A, *W, *residual;
+  void* out;
+  int M, N;
+};
+
 int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K, hipStream_t s);
-int z2z_launch_small_slopes(const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K, hipStream_t s);
-int z2z_launch_small_linear(z2z_ctx* c, const void* A, const void* W, bool k_major, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N,
-                            int K, hipStream_t s);
-int z2z_launch_small_weight(const void* A, const void* W, int rows, const int32_t* rows_dev, const void* residual, void* out, int M, int N, hipStream_t s);
+int z2z_launch_small_slopes(const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+                            const z2z_small_weight* weight, hipStream_t s);
+int z2z_launch_small_linear(z2z_ctx* c, const void* A, const void* W, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N, int K,
+                            hipStream_t s);
+int z2z_launch_small_input(z2z_ctx* c, const void* A, const void* W, void* out, int R, const int32_t* rows_dev, int N, int K, const z2z_small_weight* weight,
+                           hipStream_t s);
+int z2z_launch_small_weight(const z2z_small_weight& w, int rows, const int32_t* rows_dev, hipStream_t s);

@@ -6,8 +6,10 @@
 // chunk c at c ^ (row & 7)) or K-major ([K, rows]: 64 rows of 128 bytes, read transposed; the 32-byte piece b of row k at b ^ g(k), g = bits 1 and 3 of k, so that
 // the eight pieces that 32 lanes read at a time are on different banks).  A lane's two blocks of weight rows are groups of four that alternate, so that it stores eight columns
 // of a row at once (the gated product: the gate's block and the other projection's); the places in LDS follow.  Widths are multiples of 64: only the rows of the call have a ragged end.
-// Bound by LDS reads (32 KB a slab for 128 clocks of matrix instructions), half of the peak at best, and at these sizes by launches and round trips: 237 rows, d = 1024,
-// d_ff = 2752 (us, / on the kernels for more or fewer rows): first product 13.4 / 21.1, second 10.5 with its sum / 15.4, dF 10.6 / 28, dW2 and dW1 20.7 / 31, dX 15.2 with its sum / 31.
+// Bound by LDS reads (32 KB a slab for 128 clocks of matrix instructions), half of the peak at best, and at these sizes by launches and round trips: products that do not
+// need each other share a launch (forward and gradient, d = 1024, d_ff = 2752: 237 rows 67 -> 57 us, 1000 rows 141 -> 126; d = 256, d_ff = 704, 237 rows 34 -> 25).
+// 237 rows, d = 1024, d_ff = 2752, each in a launch of its own (us, / on the kernels for more or fewer rows): first product 13.1 / 21.1, second 10.0 with its sum / 15.4, dF 10.9 / 28,
+// dW2 and dW1 20.7 / 31, dX 13.9 with its sum / 31.
 #include "small_tile.h"
 
 #include "gated.h"
@@ -21,6 +23,7 @@ using z2z_logits::f32x4;
 
 constexpr int S_T = 64;                      // tile edge and slab
 constexpr int S_D = 2;                       // slabs on their way in registers (237 rows, d = 1024, d_ff = 2752: dW2 and dW1 20.7 us, 22.3 with four)
+constexpr int S_WAVES = 4;                   // a SIMD: no accumulators in AGPRs
 
 struct SmallArgs {
   const uint16_t *H, *W;
@@ -30,7 +33,7 @@ struct SmallArgs {
   z2z_gated::Kept kept;
   const int32_t *rows_dev, *k_dev;           // nullptr, or how many rows of the output, of the contraction, exist
   int32_t R, N, K, ldh, ldw, ldo;
-  int32_t n_slabs, per;                      // slabs of the contraction, of a part
+  int32_t per;                               // slabs of a part
   int32_t tiles_n, tiles_r, n_work;
   int32_t d_ff, act, f32;
 };
@@ -62,20 +65,19 @@ __device__ __forceinline__ uint4 in_order(const unsigned char* tile, int first, 
 // TW, TH: the operand is K-major.  EPI: 0 = out = sum + residual, 1 = the gated block's first product (a tile's 64 weight rows: 16 gate rows, 16 of the other
 // projection, and once more), 2 = its gradient's.  PARTS: K is shared out over workgroups, and the sums of a part go to `partial` as they are.
 template <bool TW, bool TH, int EPI, bool PARTS>
-__global__ void __launch_bounds__(256) small_tile_kernel(SmallArgs a) {
-  __shared__ __align__(256) unsigned char lds[2][2][S_T * 128];
+__device__ __forceinline__ void small_tile(const SmallArgs& a, unsigned block, unsigned char (&lds)[2][2][S_T * 128]) {
   constexpr bool WIDE = EPI != 1;             // a lane has 8 columns of a row in a row, not 4 of each of two blocks
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wv = wave & 1, wr = wave >> 1;
   const int lane15 = lane & 15, quarter = lane >> 4;
   // workgroup ids go round the 8 XCDs: an XCD takes a run of items, the tiles of a weight tile's rows next to each other
-  const int each = (a.n_work + 7) / 8, item = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
-  if (item >= a.n_work || (int)(blockIdx.x >> 3) >= each) return;
+  const int each = (a.n_work + 7) / 8, item = (int)(block & 7) * each + (int)(block >> 3);
+  if (item >= a.n_work || (int)(block >> 3) >= each) return;
   const int rt = item % a.tiles_r, rest = item / a.tiles_r, nt = rest % a.tiles_n, part = PARTS ? rest / a.tiles_n : 0;
   const int R = !TH && a.rows_dev ? min(a.R, max(__builtin_amdgcn_readfirstlane(*a.rows_dev), 0)) : a.R;
   const int r0 = rt * S_T;
   if (r0 >= R) return;
   const int k_rows = TH && a.k_dev ? min(a.K, max(__builtin_amdgcn_readfirstlane(*a.k_dev), 0)) : a.K;
-  int slabs = (k_rows + S_T - 1) / S_T;
+  const int slabs = (k_rows + S_T - 1) / S_T;
   const int s0 = PARTS ? part * a.per : 0, s1 = PARTS ? min(s0 + a.per, slabs) : slabs;
 
   // ---- what a thread moves of a slab: rows tid / 8 and 32 more of either operand's 64, 16 bytes at chunk tid % 8
@@ -205,27 +207,96 @@ __global__ void __launch_bounds__(256) small_tile_kernel(SmallArgs a) {
 }
 
 template <bool TW, bool TH, int EPI, bool PARTS>
-int launch(SmallArgs& a, int parts, hipStream_t s) {
+__global__ void __launch_bounds__(256, S_WAVES) small_tile_kernel(SmallArgs a) {
+  __shared__ __align__(256) unsigned char lds[2][2][S_T * 128];
+  small_tile<TW, TH, EPI, PARTS>(a, blockIdx.x, lds);
+}
+
+// Two products that do not need each other in one launch: dF, or dX, in the first `n_a` workgroups, a weight gradient in the others.
+template <int EPI, bool PARTS>
+__global__ void __launch_bounds__(256, S_WAVES) small_pair_kernel(SmallArgs a, SmallArgs b, unsigned n_a) {
+  __shared__ __align__(256) unsigned char lds[2][2][S_T * 128];
+  if (blockIdx.x < n_a)
+    small_tile<true, false, EPI, PARTS>(a, blockIdx.x, lds);
+  else
+    small_tile<true, true, 0, false>(b, blockIdx.x - n_a, lds);
+}
+
+unsigned count(SmallArgs& a, int parts) {
   a.tiles_r = (a.R + S_T - 1) / S_T;
   a.n_work = a.tiles_r * a.tiles_n * parts;
-  hipLaunchKernelGGL((small_tile_kernel<TW, TH, EPI, PARTS>), dim3((unsigned)((a.n_work + 7) / 8 * 8)), dim3(256), 0, s, a);
+  return (unsigned)((a.n_work + 7) / 8 * 8);
+}
+
+template <bool TW, bool TH, int EPI, bool PARTS>
+int launch(SmallArgs& a, int parts, hipStream_t s) {
+  const unsigned n = count(a, parts);
+  hipLaunchKernelGGL((small_tile_kernel<TW, TH, EPI, PARTS>), dim3(n), dim3(256), 0, s, a);
+  Z2Z_HIP_TRY(hipGetLastError());
+  return Z2Z_OK;
+}
+
+template <int EPI, bool PARTS>
+int launch_pair(SmallArgs& a, int parts, SmallArgs& b, hipStream_t s) {
+  const unsigned n_a = count(a, parts), n_b = count(b, 1);
+  hipLaunchKernelGGL((small_pair_kernel<EPI, PARTS>), dim3(n_a + n_b), dim3(256), 0, s, a, b, n_a);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
 
 // out = H W^T + residual with K minor or major on the weights' side; where the tiles are fewer than the workgroups that the chip holds, K is shared out.
+// weight: nullptr, or the weight gradient that goes along.
 template <bool TW>
-int linear(z2z_ctx* c, SmallArgs& a, hipStream_t s) {
+int linear(z2z_ctx* c, SmallArgs& a, SmallArgs* weight, hipStream_t s) {
   a.tiles_n = a.N / S_T;
   const int tiles = (a.R + S_T - 1) / S_T * a.tiles_n, slabs = a.K / S_T;
   const int ways = std::max(1, std::min(2 * c->num_cu / std::max(tiles, 1), slabs / 4));
   a.per = (slabs + ways - 1) / ways;
   const int parts = (slabs + a.per - 1) / a.per;
-  if (parts <= 1) return launch<TW, false, 0, false>(a, 1, s);
-  const int rc = z2z_partial_reserve(c, (size_t)parts * a.R * a.N * sizeof(float), &a.partial, s);
+  if (parts <= 1) {
+    if constexpr (TW)
+      if (weight) return launch_pair<0, false>(a, 1, *weight, s);
+    return launch<TW, false, 0, false>(a, 1, s);
+  }
+  int rc = z2z_partial_reserve(c, (size_t)parts * a.R * a.N * sizeof(float), &a.partial, s);
   if (rc != Z2Z_OK) return rc;
-  const int rl = launch<TW, false, 0, true>(a, parts, s);
-  return rl != Z2Z_OK ? rl : z2z_launch_linear_sum(a.partial, parts, a.R, a.rows_dev, a.N, a.residual, a.out, a.f32 != 0, s);
+  bool along = false;
+  if constexpr (TW)
+    if (weight) {
+      rc = launch_pair<0, true>(a, parts, *weight, s);
+      along = true;
+    }
+  if (!along) rc = launch<TW, false, 0, true>(a, parts, s);
+  return rc != Z2Z_OK ? rc : z2z_launch_linear_sum(a.partial, parts, a.R, a.rows_dev, a.N, a.residual, a.out, a.f32 != 0, s);
+}
+
+SmallArgs linear_args(const void* A, const void* W, bool k_major, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N, int K) {
+  SmallArgs a = {};
+  a.H = reinterpret_cast<const uint16_t*>(A);
+  a.W = reinterpret_cast<const uint16_t*>(W);
+  a.out = out;
+  a.residual = residual;
+  a.rows_dev = rows_dev;
+  a.R = R;
+  a.N = a.ldo = N;
+  a.K = a.ldh = K;
+  a.ldw = k_major ? N : K;
+  a.f32 = f32 ? 1 : 0;
+  return a;
+}
+
+SmallArgs weight_args(const z2z_small_weight& w, int rows, const int32_t* rows_dev) {
+  SmallArgs a = {};
+  a.H = reinterpret_cast<const uint16_t*>(w.A);
+  a.W = reinterpret_cast<const uint16_t*>(w.W);
+  a.out = w.out;
+  a.residual = w.residual;
+  a.k_dev = rows_dev;
+  a.R = a.ldh = w.M;
+  a.N = a.ldo = a.ldw = w.N;
+  a.K = rows;
+  a.tiles_n = w.N / S_T;
+  return a;
 }
 
 }  // namespace
@@ -245,7 +316,8 @@ int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, void*
   return launch<false, false, 1, false>(a, 1, s);
 }
 
-int z2z_launch_small_slopes(const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K, hipStream_t s) {
+int z2z_launch_small_slopes(const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+                            const z2z_small_weight* weight, hipStream_t s) {
   SmallArgs a = {};
   a.H = reinterpret_cast<const uint16_t*>(dY);
   a.W = reinterpret_cast<const uint16_t*>(W);
@@ -257,35 +329,26 @@ int z2z_launch_small_slopes(const void* dY, const void* W, const void* kept, voi
   a.ldw = a.d_ff = d_ff;
   a.ldo = 2 * d_ff;
   a.tiles_n = d_ff / S_T;
-  return launch<true, false, 2, false>(a, 1, s);
+  if (!weight) return launch<true, false, 2, false>(a, 1, s);
+  SmallArgs b = weight_args(*weight, R, rows_dev);
+  return launch_pair<2, false>(a, 1, b, s);
 }
 
-int z2z_launch_small_linear(z2z_ctx* c, const void* A, const void* W, bool k_major, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N,
-                            int K, hipStream_t s) {
-  SmallArgs a = {};
-  a.H = reinterpret_cast<const uint16_t*>(A);
-  a.W = reinterpret_cast<const uint16_t*>(W);
-  a.out = out;
-  a.residual = residual;
-  a.rows_dev = rows_dev;
-  a.R = R;
-  a.N = a.ldo = N;
-  a.K = a.ldh = K;
-  a.ldw = k_major ? N : K;
-  a.f32 = f32 ? 1 : 0;
-  return k_major ? linear<true>(c, a, s) : linear<false>(c, a, s);
+int z2z_launch_small_linear(z2z_ctx* c, const void* A, const void* W, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N, int K,
+                            hipStream_t s) {
+  SmallArgs a = linear_args(A, W, false, residual, out, f32, R, rows_dev, N, K);
+  return linear<false>(c, a, nullptr, s);
 }
 
-int z2z_launch_small_weight(const void* A, const void* W, int rows, const int32_t* rows_dev, const void* residual, void* out, int M, int N, hipStream_t s) {
-  SmallArgs a = {};
-  a.H = reinterpret_cast<const uint16_t*>(A);
-  a.W = reinterpret_cast<const uint16_t*>(W);
-  a.out = out;
-  a.residual = residual;
-  a.k_dev = rows_dev;
-  a.R = a.ldh = M;
-  a.N = a.ldo = a.ldw = N;
-  a.K = rows;
-  a.tiles_n = N / S_T;
+int z2z_launch_small_input(z2z_ctx* c, const void* A, const void* W, void* out, int R, const int32_t* rows_dev, int N, int K, const z2z_small_weight* weight,
+                           hipStream_t s) {
+  SmallArgs a = linear_args(A, W, true, nullptr, out, false, R, rows_dev, N, K);
+  if (!weight) return linear<true>(c, a, nullptr, s);
+  SmallArgs b = weight_args(*weight, R, rows_dev);
+  return linear<true>(c, a, &b, s);
+}
+
+int z2z_launch_small_weight(const z2z_small_weight& w, int rows, const int32_t* rows_dev, hipStream_t s) {
+  SmallArgs a = weight_args(w, rows, rows_dev);
   return launch<true, true, 0, false>(a, 1, s);
 }
