@@ -961,12 +961,14 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
       // d = 256: the pass 275 us fused, 267 in launches of their own)
       if (block && block->few)
         return z2z_launch_few_linear(in, w, block->scale, block->group, residual, out, true, R, rows_dev, d, K, s);
-      if (block && block->small) return z2z_launch_small_linear(c, in, w, residual, out, true, R, rows_dev, d, K, s);
-      if (block && block->group)
+      if (block && block->small && R <= E_FEW_ROWS)
+        ret = z2z_launch_small_parts(c, in, w, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s);
+      else if (block && block->group)
         ret = z2z_launch_q4_parts(c, in, w, block->scale, block->group, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s);
       else if (!padded && R <= E_FEW_ROWS)
         ret = z2z_launch_linear_parts(c, in, w, R, rows_dev, d, K, &parts.partial, &parts.ksplit, s, once);
       if (ret != Z2Z_OK) return ret;
+      if (parts.ksplit == 0 && block && block->small) return z2z_launch_small_linear(c, in, w, residual, out, true, R, rows_dev, d, K, s);
       if (parts.ksplit == 0)
         return z2z_launch_linear(c, in, w, bias, residual, 0, out, R, rows_dev, d, K, s, true, padded ? &pitch : nullptr, once);
       parts.R = R;

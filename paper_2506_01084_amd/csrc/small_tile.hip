@@ -206,20 +206,43 @@ __device__ __forceinline__ void small_tile(const SmallArgs& a, unsigned block, u
   }
 }
 
-template <bool TW, bool TH, int EPI, bool PARTS>
+template <bool TW, int EPI, bool PARTS>
 __global__ void __launch_bounds__(256, S_WAVES) small_tile_kernel(SmallArgs a) {
   __shared__ __align__(256) unsigned char lds[2][2][S_T * 128];
-  small_tile<TW, TH, EPI, PARTS>(a, blockIdx.x, lds);
+  small_tile<TW, false, EPI, PARTS>(a, blockIdx.x, lds);
 }
 
 // Two products that do not need each other in one launch: dF, or dX, in the first `n_a` workgroups, a weight gradient in the others.
-template <int EPI, bool PARTS>
+template <int EPI, bool PARTS, bool W_PARTS>
 __global__ void __launch_bounds__(256, S_WAVES) small_pair_kernel(SmallArgs a, SmallArgs b, unsigned n_a) {
   __shared__ __align__(256) unsigned char lds[2][2][S_T * 128];
   if (blockIdx.x < n_a)
     small_tile<true, false, EPI, PARTS>(a, blockIdx.x, lds);
   else
-    small_tile<true, true, 0, false>(b, blockIdx.x - n_a, lds);
+    small_tile<true, true, 0, W_PARTS>(b, blockIdx.x - n_a, lds);
+}
+
+// Parts of K for `tiles` tiles: as many as bring the workgroups up to `most`, of `least` slabs or more.
+int cut(SmallArgs& a, int tiles, int most, int least) {
+  const int slabs = (a.K + S_T - 1) / S_T, ways = std::max(1, std::min(most / std::max(tiles, 1), slabs / least));
+  a.per = (slabs + ways - 1) / ways;
+  return (slabs + a.per - 1) / a.per;
+}
+size_t part_bytes(const SmallArgs& a, int parts) { return parts > 1 ? (size_t)parts * a.R * a.N * sizeof(float) : 0; }
+
+// The parts' buffers, behind each other.  b: nullptr, or a weight gradient beside `a`.
+int reserve(z2z_ctx* c, SmallArgs& a, int parts, SmallArgs* b, int parts_b, hipStream_t s) {
+  const size_t n = part_bytes(a, parts), m = b ? part_bytes(*b, parts_b) : 0;
+  if (n + m == 0) return Z2Z_OK;
+  float* p = nullptr;
+  const int rc = z2z_partial_reserve(c, n + m, &p, s);
+  a.partial = p;
+  if (b) b->partial = p + n / sizeof(float);
+  return rc;
+}
+
+int add_up(const SmallArgs& a, int parts, hipStream_t s) {
+  return parts > 1 ? z2z_launch_linear_sum(a.partial, parts, a.R, a.rows_dev, a.N, a.residual, a.out, a.f32 != 0, s) : Z2Z_OK;
 }
 
 unsigned count(SmallArgs& a, int parts) {
@@ -228,47 +251,34 @@ unsigned count(SmallArgs& a, int parts) {
   return (unsigned)((a.n_work + 7) / 8 * 8);
 }
 
-template <bool TW, bool TH, int EPI, bool PARTS>
+template <bool TW, int EPI, bool PARTS>
 int launch(SmallArgs& a, int parts, hipStream_t s) {
   const unsigned n = count(a, parts);
-  hipLaunchKernelGGL((small_tile_kernel<TW, TH, EPI, PARTS>), dim3(n), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((small_tile_kernel<TW, EPI, PARTS>), dim3(n), dim3(256), 0, s, a);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
 
 template <int EPI, bool PARTS>
-int launch_pair(SmallArgs& a, int parts, SmallArgs& b, hipStream_t s) {
-  const unsigned n_a = count(a, parts), n_b = count(b, 1);
-  hipLaunchKernelGGL((small_pair_kernel<EPI, PARTS>), dim3(n_a + n_b), dim3(256), 0, s, a, b, n_a);
+int launch_pair(SmallArgs& a, int parts, SmallArgs& b, int parts_b, hipStream_t s) {
+  const unsigned n_a = count(a, parts), n_b = count(b, parts_b);
+  if (parts_b > 1)
+    hipLaunchKernelGGL((small_pair_kernel<EPI, PARTS, true>), dim3(n_a + n_b), dim3(256), 0, s, a, b, n_a);
+  else
+    hipLaunchKernelGGL((small_pair_kernel<EPI, PARTS, false>), dim3(n_a + n_b), dim3(256), 0, s, a, b, n_a);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
 
-// out = H W^T + residual with K minor or major on the weights' side; where the tiles are fewer than the workgroups that the chip holds, K is shared out.
-// weight: nullptr, or the weight gradient that goes along.
-template <bool TW>
-int linear(z2z_ctx* c, SmallArgs& a, SmallArgs* weight, hipStream_t s) {
+int rows_of_tiles(int R) { return (R + S_T - 1) / S_T; }
+
+// A product [R, N] whose tiles are fewer than the workgroups that the chip holds has K shared out.
+int cut_linear(const z2z_ctx* c, SmallArgs& a) {
   a.tiles_n = a.N / S_T;
-  const int tiles = (a.R + S_T - 1) / S_T * a.tiles_n, slabs = a.K / S_T;
-  const int ways = std::max(1, std::min(2 * c->num_cu / std::max(tiles, 1), slabs / 4));
-  a.per = (slabs + ways - 1) / ways;
-  const int parts = (slabs + a.per - 1) / a.per;
-  if (parts <= 1) {
-    if constexpr (TW)
-      if (weight) return launch_pair<0, false>(a, 1, *weight, s);
-    return launch<TW, false, 0, false>(a, 1, s);
-  }
-  int rc = z2z_partial_reserve(c, (size_t)parts * a.R * a.N * sizeof(float), &a.partial, s);
-  if (rc != Z2Z_OK) return rc;
-  bool along = false;
-  if constexpr (TW)
-    if (weight) {
-      rc = launch_pair<0, true>(a, parts, *weight, s);
-      along = true;
-    }
-  if (!along) rc = launch<TW, false, 0, true>(a, parts, s);
-  return rc != Z2Z_OK ? rc : z2z_launch_linear_sum(a.partial, parts, a.R, a.rows_dev, a.N, a.residual, a.out, a.f32 != 0, s);
+  return cut(a, rows_of_tiles(a.R) * a.tiles_n, 2 * c->num_cu, 4);
 }
+// A weight gradient, whose K is the rows, where those are many (forward and gradient, us: d = 256, d_ff = 704, 16000 rows 347 -> 169; d = d_ff = 64, 64000 rows 870 -> 61).
+int cut_weight(const z2z_ctx* c, SmallArgs& a) { return cut(a, rows_of_tiles(a.R) * a.tiles_n, 4 * c->num_cu, 16); }
 
 SmallArgs linear_args(const void* A, const void* W, bool k_major, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N, int K) {
   SmallArgs a = {};
@@ -313,10 +323,10 @@ int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, void*
   a.tiles_n = 2 * d_ff / S_T;
   a.d_ff = d_ff;
   a.act = act;
-  return launch<false, false, 1, false>(a, 1, s);
+  return launch<false, 1, false>(a, 1, s);
 }
 
-int z2z_launch_small_slopes(const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+int z2z_launch_small_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
                             const z2z_small_weight* weight, hipStream_t s) {
   SmallArgs a = {};
   a.H = reinterpret_cast<const uint16_t*>(dY);
@@ -329,26 +339,51 @@ int z2z_launch_small_slopes(const void* dY, const void* W, const void* kept, voi
   a.ldw = a.d_ff = d_ff;
   a.ldo = 2 * d_ff;
   a.tiles_n = d_ff / S_T;
-  if (!weight) return launch<true, false, 2, false>(a, 1, s);
+  if (!weight) return launch<true, 2, false>(a, 1, s);
   SmallArgs b = weight_args(*weight, R, rows_dev);
-  return launch_pair<2, false>(a, 1, b, s);
+  const int parts = cut_weight(c, b);
+  int rc = reserve(c, a, 1, &b, parts, s);
+  if (rc == Z2Z_OK) rc = launch_pair<2, false>(a, 1, b, parts, s);
+  return rc == Z2Z_OK ? add_up(b, parts, s) : rc;
 }
 
 int z2z_launch_small_linear(z2z_ctx* c, const void* A, const void* W, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N, int K,
                             hipStream_t s) {
   SmallArgs a = linear_args(A, W, false, residual, out, f32, R, rows_dev, N, K);
-  return linear<false>(c, a, nullptr, s);
+  const int parts = cut_linear(c, a);
+  int rc = reserve(c, a, parts, nullptr, 1, s);
+  if (rc == Z2Z_OK) rc = parts > 1 ? launch<false, 0, true>(a, parts, s) : launch<false, 0, false>(a, 1, s);
+  return rc == Z2Z_OK ? add_up(a, parts, s) : rc;
+}
+
+int z2z_launch_small_parts(z2z_ctx* c, const void* A, const void* W, int R, const int32_t* rows_dev, int N, int K, const float** partial, int* ksplit,
+                           hipStream_t s) {
+  SmallArgs a = linear_args(A, W, false, nullptr, nullptr, false, R, rows_dev, N, K);
+  const int parts = cut_linear(c, a);
+  *ksplit = 0;
+  if (parts <= 1) return Z2Z_OK;
+  const int rc = reserve(c, a, parts, nullptr, 1, s);
+  if (rc != Z2Z_OK) return rc;
+  *partial = a.partial;
+  *ksplit = parts;
+  return launch<false, 0, true>(a, parts, s);
 }
 
 int z2z_launch_small_input(z2z_ctx* c, const void* A, const void* W, void* out, int R, const int32_t* rows_dev, int N, int K, const z2z_small_weight* weight,
                            hipStream_t s) {
-  SmallArgs a = linear_args(A, W, true, nullptr, out, false, R, rows_dev, N, K);
-  if (!weight) return linear<true>(c, a, nullptr, s);
-  SmallArgs b = weight_args(*weight, R, rows_dev);
-  return linear<true>(c, a, &b, s);
-}
-
-int z2z_launch_small_weight(const z2z_small_weight& w, int rows, const int32_t* rows_dev, hipStream_t s) {
-  SmallArgs a = weight_args(w, rows, rows_dev);
-  return launch<true, true, 0, false>(a, 1, s);
+  SmallArgs a = linear_args(A, W, true, nullptr, out, false, R, rows_dev, N, K), b = {};
+  const int parts = cut_linear(c, a);
+  int parts_b = 1;
+  if (weight) {
+    b = weight_args(*weight, R, rows_dev);
+    parts_b = cut_weight(c, b);
+  }
+  int rc = reserve(c, a, parts, weight ? &b : nullptr, parts_b, s);
+  if (rc != Z2Z_OK) return rc;
+  if (weight)
+    rc = parts > 1 ? launch_pair<0, true>(a, parts, b, parts_b, s) : launch_pair<0, false>(a, 1, b, parts_b, s);
+  else
+    rc = parts > 1 ? launch<true, 0, true>(a, parts, s) : launch<true, 0, false>(a, 1, s);
+  if (rc == Z2Z_OK) rc = add_up(a, parts, s);
+  return rc == Z2Z_OK ? add_up(b, parts_b, s) : rc;
 }
