@@ -127,9 +127,10 @@ constexpr int Q_STEPS = Q_CHUNK / Q_BLOCK;
 // Workgroup = 128 weight rows x a part of K x up to 16 NB rows of X.  X goes through LDS 256 columns at a time, in the order of the matrix instruction's operand
 // (position r of a fragment's 16 exchanged by the column chunk, so that writes of consecutive chunks are on different banks), its scales beside it; the
 // weights go from memory to registers, two chunks (8 loads of 1024 bytes a wave) ahead.  CHAIN: matrix instructions per group.  (512 columns a chunk, one
-// ahead: 24 rows, d = 3584, d_ff = 9600 13.2 us instead of 11.9 for the first product, 9.2 instead of 8.9 for the second.)
+// ahead: 24 rows, d = 3584, d_ff = 9600 13.2 us instead of 11.9 for the first product, 9.2 instead of 8.9 for the second.)  Bounds on the waves of a SIMD keep the sums out of
+// AGPRs, which the scaling would have to copy them from (300 rows, d = 2048, d_ff = 5504, groups of 32: the block 73 -> 65 us; d = 4096 178 -> 163).
 template <int CHAIN, int NB>
-__global__ void __launch_bounds__(64 * Q_WAVES) q4_kernel(Q4Args a) {
+__global__ void __launch_bounds__(64 * Q_WAVES, NB == 1 ? 4 : NB == 2 ? 3 : 2) q4_kernel(Q4Args a) {
   __shared__ uint4 xs[Q_CHUNK / 32 * NB * 64];
   __shared__ uint4 ss[Q_CHUNK / 32 / CHAIN * Q_ROWS / 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, j = lane >> 4;
