@@ -38,16 +38,16 @@ bool few_rows(const z2z_ffn* f, int d, int R) {
 //   forward    d = 1024, d_ff = 2752  65 rows 25.6 / 18.0, 300 53 / 24, 2000 93 / 62, 4000 114 / 151;   2048, 5504  100 39.7 / 30.2, 500 80 / 67, 700 94 / 93, 1000 99 / 113;   3584, 9600  65 62.4 / 59.5,
 //              160 92 / 76, 300 121 / 136;   4096, 10944  65 of weights that no cache holds: 78 / 86
 //   dF         1024, 2752  2000 -13 us, 4000 +10;   2048, 5504  1000 -5, 1500 +7;   3584, 9600  237 -3, 500 +9
-//   dX         1024, 2752  1000 -8, 1500 +1;   2048, 5504  237 -12, 500 +1;   2560, 6912  65 -9, 237 +1: alone
-//   dW1, dW2   1536, 4096  237 +1;   2048, 5504  65 -4, 237 +11: whatever the rows, large outputs are not for it
-//   all three  (forward and gradient) 1024, 2752  1500 248 / 172, 1700 266 / 198, 2000 276 / 234;   512, 1408  4000 214 / 155, 8000 257 / 286;   256, 704  20000 271 / 207,
-//              30000 347 / 315;   64, 64  64000 170 / 61
-constexpr long long kSmallForward = 3ll << 31, kSmallSlopes = 5ll << 31, kSmallInput = 3ll << 30, kSmallWeight = 5ll << 30;
+//   dX         1024, 2752  1000 -8, 1500 +1;   2048, 5504  237 -12, 500 +1;   4096, 10944  16 -11, 65 -3, 100 0: alone
+//   all three, two in a launch (forward and gradient)   1024, 2752  237 122 / 57, 1500 248 / 172, 2000 276 / 234;   2048, 5504  16 83 / 69, 237 129 / 124, 500 200 / 201;   3584, 9600
+//              65 230 / 211, 128 249 / 254;   4096, 10944  16 225 / 202, 33 231 / 232, 100 286 / 308;   512, 1408  4000 214 / 155, 8000 257 / 286;   256, 704  20000 271 / 207, 30000 347 / 315
+constexpr long long kSmallForward = 3ll << 31, kSmallSlopes = 5ll << 31, kSmallInput = 3ll << 30, kSmallGradient = 5ll << 30;
 
 bool small_tiles(const z2z_ffn* f, int d, int R, long long most) { return (long long)d * f->d_ff * R <= most; }
-bool small_forward(const z2z_ffn* f, int d, int R) {
-  return small_tiles(f, d, R, kSmallForward) && (size_t)3 * d * f->d_ff * sizeof(uint16_t) <= 2 * z2z_logits::kKeepBytes;
-}
+// (Weights that the memory-side cache does not hold are read for every 64 rows.)
+bool held(const z2z_ffn* f, int d) { return (size_t)3 * d * f->d_ff * sizeof(uint16_t) <= 2 * z2z_logits::kKeepBytes; }
+bool small_forward(const z2z_ffn* f, int d, int R) { return small_tiles(f, d, R, kSmallForward) && held(f, d); }
+bool small_gradient(const z2z_ffn* f, int d, int R) { return small_tiles(f, d, R, kSmallGradient) && (R <= 16 || held(f, d)); }
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
@@ -120,7 +120,7 @@ int z2z_launch_ffn_backward(z2z_ctx* c, const void* X, const z2z_ffn* f, const v
   const void* F = kept;                              // (the first of what is kept)
   void *dw1 = const_cast<void*>(grad->w_1), *dw2 = const_cast<void*>(grad->w_2);
   // on small tiles the weight gradients go along with the products beside them
-  const bool weights = small_tiles(f, d, R, kSmallWeight) && small_tiles(f, d, 1, 1 << 22), input = weights || small_tiles(f, d, R, kSmallInput);
+  const bool weights = small_gradient(f, d, R), input = weights || small_tiles(f, d, R, kSmallInput);
   const z2z_small_weight w1 = {work, X, add ? dw1 : nullptr, dw1, 2 * dff, d}, w2 = {dY, F, add ? dw2 : nullptr, dw2, d, dff};
   int rc = small_tiles(f, d, R, kSmallSlopes) ? z2z_launch_small_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, weights ? &w2 : nullptr, s)
                                               : z2z_launch_gated_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, s);

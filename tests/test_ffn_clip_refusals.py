@@ -83,12 +83,14 @@ for rows in (9, 320):
     assert fwd(big, four(**wide), rows=rows) == 0 and names() == ["q4_kernel", "few_sum_kernel"] * 2
 assert fwd(big, four(**wide), rows=321) == 0 and names()[:4] == ["q4_expand", "q4_expand"] + ["small_tile_kernel"] * 2
 assert fwd(big, four(**wide), rows=769) == 0 and names()[:3] == ["q4_expand", "q4_expand", "logits_fast_kernel"]
-for rows, small in ((1, 2), (384, 2), (385, 1), (1280, 1), (1281, 0)):                     # (dX up to 3 * 2^30 of rows * d * d_ff, dF up to 5 * 2^31, outputs too large for dW)
-    assert bwd(big, block(**wide), rows=rows) == 0 and names().count("small_tile_kernel") == small
-assert bwd(big, block(d_ff=2048), rows=1280) == 0 and names() == ["small_pair_kernel"] * 2       # (dF with dW2, dX with dW1: up to 5 * 2^30 of them)
-assert bwd(big, block(d_ff=2048), rows=1281) == 0
-more = names()
-assert more[0] == "small_tile_kernel" and set(more[1:]) <= {"logits_fast_kernel", "tile_sum_kernel"}
+pairs = ["small_pair_kernel"] * 2                                                         # (dF with dW2, dX with dW1)
+for rows in (1, 64, 639, 640):
+    assert bwd(big, block(**wide), rows=rows) == 0
+    assert [n for n in names() if n != "few_sum_kernel"] == pairs, rows
+for rows, d_ff, small in ((641, 4096, 1), (1280, 4096, 1), (1281, 4096, 0), (16, 22016, None), (17, 22016, 2), (71, 22016, 2), (72, 22016, 1)):
+    assert bwd(big, block(d_ff=d_ff), rows=rows) == 0
+    now = names()
+    assert [n for n in now if n != "few_sum_kernel"] == pairs if small is None else now.count("small_tile_kernel") == small, (rows, now)
 assert bwd(big, block(d_ff=2048), rows=60) == 0 and names() == ["small_pair_kernel"] * 2 + ["few_sum_kernel"]
 assert fwd(h, block(), rows=256) == 0 and names() == ["few_rows_kernel"] * 2             # (small weights)
 # nothing grows under capture; what a graph names stays

@@ -47,8 +47,8 @@ SHAPES = [(1, 64, 64), (1, 1024, 448), (2, 192, 704), (15, 320, 192), (16, 512, 
 LARGE = [(1031, 3520, 1792), (300, 6400, 3456), (2500, 2048, 2112), (16411, 512, 1344), (40, 8192, 5504)]
 
 
-# gradients of the weights with the rows shared out (a part's end inside a slab, dX in parts or not), and on either side of where they leave the small tiles
-NARROW = [(2049, 64, 64), (4000, 256, 704), (3000, 128, 1344), (40000, 64, 128), (1943, 1024, 2688), (1955, 1024, 2688)]
+# the whole gradient on small tiles: with the rows shared out (a part's end inside a slab, dX in parts or not), on either side of where it leaves them, wide outputs of few rows
+NARROW = [(2049, 64, 64), (4000, 256, 704), (3000, 128, 1344), (40000, 64, 128), (1943, 1024, 2688), (1955, 1024, 2688), (100, 2048, 2752), (16, 8192, 5504)]
 
 
 @pytest.mark.parametrize("rows,d,f", NARROW)
