@@ -254,7 +254,7 @@ int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, i
  *   d_X [rows, d], d_residual [rows, d] or NULL, d_Y [rows, d] out: bf16.  d_Y may be d_residual, else it overlaps nothing that the call reads (Z2Z_EINVAL)
  *   d_kept  [rows, 2 f] float out or NULL: what z2z_gated_ffn_backward needs of G and U, for that call alone to read (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
  * A row's results do not depend on the other rows' values.  rows = 0 is a call that does nothing.  bf16 contexts, d and d_ff multiples of 64 (with 4 bits of group,
- * too), rows <= 2^22, (d_ff + 128) d < 2^30, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and for few rows the parts of the products. */
+ * too), rows <= 2^22, (d_ff + 128) d < 2^30, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and the parts of products that are shared out. */
 enum { Z2Z_ACT_SILU = 0, Z2Z_ACT_GELU = 1 };
 typedef struct z2z_ffn {
   int32_t d_ff;
@@ -275,7 +275,7 @@ int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ff
  *   grad   its w_1 and w_2 name the buffers that RECEIVE the gradients, bf16 (the call writes through them although they are declared const); its
  *          other fields are not read.  flags = 0: overwritten (rows = 0: with zeros); Z2Z_GRAD_ADD: added to what is there, one rounding per element
  * dG, dU and F are rounded to bf16 once, sums are fp32.  No output overlaps an input or another output (Z2Z_EINVAL).  Restrictions as for z2z_gated_ffn; work
- * space: 4 f bytes per row. */
+ * space: 4 f bytes per row, and the parts of products that are shared out. */
 int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const float* d_kept, const void* d_dY, void* d_dX,
                            const z2z_ffn* grad, int32_t flags, void* stream);
 

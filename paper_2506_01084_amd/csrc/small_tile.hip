@@ -22,7 +22,7 @@ using z2z_logits::bf16x8;
 using z2z_logits::f32x4;
 
 constexpr int S_T = 64;                      // tile edge and slab
-constexpr int S_D = 2;                       // slabs on their way in registers (237 rows, d = 1024, d_ff = 2752: dW2 and dW1 20.7 us, 22.3 with four)
+constexpr int S_D = 2;                       // slabs on their way in registers (forward and gradient, 237 rows, d = 1024, d_ff = 2752 57 us with one, 55 with two; four do not fit)
 constexpr int S_WAVES = 4;                   // a SIMD: no accumulators in AGPRs
 
 struct SmallArgs {
@@ -124,31 +124,45 @@ __device__ __forceinline__ void small_tile(const SmallArgs& a, unsigned block, u
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // one barrier: what a slab later goes to this buffer again is written behind the next one, which a wave reaches when it has read this
+  auto multiply = [&](int buf) __attribute__((always_inline)) {
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      uint4 av[2], bv[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        av[i] = weights_of(buf, i, q);
+        bv[i] = in_order<TH>(lds[buf][1], wr * 32 + i * 16, q, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av[i]), __builtin_bit_cast(bf16x8, bv[j]), acc[i][j], 0, 0, 0);
+    }
+  };
   if (s0 < s1) {
 #pragma unroll
-    for (int u = 0; u < S_D; ++u) fetch(ahead[u], min(s0 + u, s1 - 1));
-    for (int s = s0; s < s1; s += S_D) {
+    for (int u = 0; u < S_D; ++u) {
+      fetch(ahead[u], min(s0 + u, s1 - 1));
+      __builtin_amdgcn_sched_barrier(0);       // (in this order: the loop waits for the first slab's loads alone, not for what came behind them)
+    }
+    // (no way out of the middle of the loop: where loads may have been left out the compiler waits for all)
+    int s = s0;
+    for (; s + S_D <= s1; s += S_D) {
 #pragma unroll
       for (int u = 0; u < S_D; ++u) {
-        if (s + u >= s1) break;
         put(u & 1, ahead[u], s + u);
         fetch(ahead[u], min(s + u + S_D, s1 - 1));
-        // one barrier: what a slab later goes to this buffer again is written behind the next one, which a wave reaches when it has read this
-        __syncthreads();
+        multiply(u & 1);
+      }
+    }
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint4 av[2], bv[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            av[i] = weights_of(u & 1, i, q);
-            bv[i] = in_order<TH>(lds[u & 1][1], wr * 32 + i * 16, q, lane);
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av[i]), __builtin_bit_cast(bf16x8, bv[j]), acc[i][j], 0, 0, 0);
-        }
+    for (int u = 0; u < S_D - 1; ++u) {
+      if (s + u < s1) {
+        put(u & 1, ahead[u], s + u);
+        multiply(u & 1);
       }
     }
   }
