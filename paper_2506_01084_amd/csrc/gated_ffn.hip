@@ -12,7 +12,7 @@
 namespace {
 
 // More rows than this, and 4-bit weights are expanded to bf16 first: the products are the matrix cores' work then.  (us, 300 rows from 4 bits / 330 expanded: d = 4096, d_ff = 10944
-// 163 / 248; 3584, 9600 124 / 204; 2048, 5504 65 / 82; 1024, 2752 32 / 38; 400 rows expanded 248, 202, 84, 39.)
+// 155 / 245; 3584, 9600 115 / 204; 2048, 5504 62 / 79; 1024, 2752 31 / 38; 400 rows expanded 244, 202, 81, 38.)
 constexpr int kExpandRows = 320;
 
 __global__ void __launch_bounds__(256) fill_zero_kernel(uint4* p, size_t n, uint4* q, size_t n_q) {

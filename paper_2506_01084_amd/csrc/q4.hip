@@ -226,23 +226,29 @@ __global__ void __launch_bounds__(64 * Q_WAVES, NB == 1 ? 4 : NB == 2 ? 3 : 2) q
     }
   };
 
+  // (The weights ahead are asked for behind the part's end, too, where they are its last block's, and there is no way out of the middle of the loop: where
+  // loads may have been left out the compiler waits for all of them before it publishes the rows.)
   fetch_w(w[0], b0);
+  __builtin_amdgcn_sched_barrier(0);
   fetch(b0);
-  if (b0 + Q_STEPS < b1) fetch_w(w[1], b0 + Q_STEPS);
-  for (int blk = b0; blk < b1; blk += 2 * Q_STEPS) {
+  __builtin_amdgcn_sched_barrier(0);
+  fetch_w(w[1], b0 + Q_STEPS);
+  int blk = b0, chunks = (b1 - b0 + Q_STEPS - 1) / Q_STEPS;
+  for (; chunks >= 2; chunks -= 2, blk += 2 * Q_STEPS) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      publish();
+      __syncthreads();
+      fetch(blk + (u + 1) * Q_STEPS);
+      compute(w[u]);
+      fetch_w(w[u], blk + (u + 2) * Q_STEPS);
+      __syncthreads();
+    }
+  }
+  if (chunks > 0) {
     publish();
     __syncthreads();
-    if (blk + Q_STEPS < b1) fetch(blk + Q_STEPS);
     compute(w[0]);
-    if (blk + 2 * Q_STEPS < b1) fetch_w(w[0], blk + 2 * Q_STEPS);
-    __syncthreads();
-    if (blk + Q_STEPS >= b1) break;
-    publish();
-    __syncthreads();
-    if (blk + 2 * Q_STEPS < b1) fetch(blk + 2 * Q_STEPS);
-    compute(w[1]);
-    if (blk + 3 * Q_STEPS < b1) fetch_w(w[1], blk + 3 * Q_STEPS);
-    __syncthreads();
   }
   float* out = a.partial + (size_t)blockIdx.y * a.R * a.N;
 #pragma unroll
