@@ -193,11 +193,11 @@ def test_rows_behind_the_last_and_empty_calls():
             ctx.gated_ffn_backward(X[:0], block, kept[:0], dY[:0], dX[:0], api.GatedFFN(W1.clone(), W2.clone()), add=True)
 
 
-@pytest.mark.parametrize("rows", [24, 400])
-def test_graph_replays_and_streams(rows):
+# (3000 rows of a narrow block: the weights' gradients are added up from parts)
+@pytest.mark.parametrize("rows,d,f", [(24, 2048, 320), (400, 2048, 320), (3000, 128, 704)])
+def test_graph_replays_and_streams(rows, d, f):
     from paper_2506_01084_amd import api
 
-    d, f = 2048, 320
     X, W1, W2, R, dY = _tensors(rows, d, f, 21)
     ctx = _context(d)
     block = api.GatedFFN(W1, W2)
