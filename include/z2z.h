@@ -252,21 +252,24 @@ int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, i
  *        scale_2 [f / group, d].  Up to 320 rows are multiplied by v, the scales with fp32 sums;
  *        more rows by the weights rounded to bf16, which takes 6 d f bytes of work space.
  *   d_X [rows, d], d_residual [rows, d] or NULL, d_Y [rows, d] out: bf16.  d_Y may be d_residual, else it overlaps nothing that the call reads (Z2Z_EINVAL)
- *   d_kept  [rows, 2 f] float out or NULL: what z2z_gated_ffn_backward needs of G and U, for that call alone to read (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL)
+ *   d_kept  [rows, 2 f] out or NULL: what z2z_gated_ffn_backward needs of G and U, for that call alone to read (bf16 weights only).  Overlaps no other tensor of the call (Z2Z_EINVAL).
+ *           ffn->kept says in how many bits, and the backward call's says the same: Z2Z_KEPT_32, 4 bytes an element of [rows, 2 f]; Z2Z_KEPT_16, 2 bytes: G and U with 9
+ *           bits of fraction (magnitudes from 2^-16 to 2^16; all others with 6), for gradients that are slightly less exact
  * A row's results do not depend on the other rows' values.  rows = 0 is a call that does nothing.  bf16 contexts, d and d_ff multiples of 64 (with 4 bits of group,
  * too), rows <= 2^22, (d_ff + 128) d < 2^30, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and the parts of products that are shared out. */
 enum { Z2Z_ACT_SILU = 0, Z2Z_ACT_GELU = 1 };
+enum { Z2Z_KEPT_32 = 0, Z2Z_KEPT_16 = 16 };
 typedef struct z2z_ffn {
   int32_t d_ff;
   int32_t act;
   int32_t group;        /* 0: bf16 weights; else 4 bits, columns per scale */
-  int32_t reserved;     /* 0 */
+  int32_t kept;         /* Z2Z_KEPT_32, Z2Z_KEPT_16 */
   const void* w_1;      /* device pointers, 16-byte aligned, borrowed for the call */
   const void* w_2;
   const void* scale_1;  /* NULL for bf16 weights */
   const void* scale_2;
 } z2z_ffn;
-int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, float* d_kept, void* stream);
+int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, void* d_kept, void* stream);
 
 /* Backward of z2z_gated_ffn: the gradient of  L = sum dY * Y  with respect to the rows and both matrices (the residual's is dY itself),
  *   dF = dY w_2;   dG = dF * U * act'(G),   dU = dF * act(G);   dX = [dG | dU] w_1;   dw_1 = [dG | dU]^T X;   dw_2 = dY^T F.
@@ -275,8 +278,8 @@ int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ff
  *   grad   its w_1 and w_2 name the buffers that RECEIVE the gradients, bf16 (the call writes through them although they are declared const); its
  *          other fields are not read.  flags = 0: overwritten (rows = 0: with zeros); Z2Z_GRAD_ADD: added to what is there, one rounding per element
  * dG, dU and F are rounded to bf16 once, sums are fp32.  No output overlaps an input or another output (Z2Z_EINVAL).  Restrictions as for z2z_gated_ffn; work
- * space: 4 f bytes per row, and the parts of products that are shared out. */
-int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const float* d_kept, const void* d_dY, void* d_dX,
+ * space: 4 f bytes per row (Z2Z_KEPT_16: 12 f), and the parts of products that are shared out. */
+int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_kept, const void* d_dY, void* d_dX,
                            const z2z_ffn* grad, int32_t flags, void* stream);
 
 /* clip_gradients.  The common norm of n gradients, and their clipping by it:
@@ -343,7 +346,7 @@ typedef struct z2z_encoder {
  * `encoder` of this struct with attention_only = Z2Z_ENC_GATED (a value that it has nowhere else); ffn then has the layers' blocks, and of `encoder` d_ff and of its layers w_1,
  * b_1, w_2 and b_2 are not read.  Blocks over 4-bit weights serve z2z_hyper_encode; z2z_hyper_encode_keep and z2z_hyper_encode_backward need bf16 (else
  * Z2Z_EUNSUPPORTED), and the latter's `grad` is the `encoder` of such a struct, too: w_1 and w_2 of its blocks receive the matrices' gradients.  All blocks have one d_ff
- * (else Z2Z_EINVAL). */
+ * and kept = Z2Z_KEPT_32 (else Z2Z_EINVAL). */
 #define Z2Z_ENC_GATED 2
 typedef struct z2z_gated_encoder {
   z2z_encoder encoder;

@@ -36,11 +36,20 @@ def _sum_bound(A: np.ndarray, B: np.ndarray) -> np.ndarray:
     return (A.shape[1] + 8) * HALF_F32 * (np.abs(A) @ np.abs(B))
 
 
-def gated_ffn(X, W1, W2, kind: str, residual=None, round_weights: bool = False):
-    """dict(Y, Y_bound, G, U, F and their bounds).  round_weights: the weights may each be rounded to bf16."""
+def _sixteen_bits(x, err):
+    """How far numbers that are `err` off x may be moved by 16 bits: half a step of 9 bits of fraction from 2^-16 to 2^16, of 6 elsewhere."""
+    size = np.abs(x)
+    near = (size - err >= 2.0 ** -16) & (size + err < 2.0 ** 16 * (1 - 2.0 ** -10))
+    return np.where(near, 2.0 ** -10, 2.0 ** -7) * (size + err)
+
+
+def gated_ffn(X, W1, W2, kind: str, residual=None, round_weights: bool = False, kept16: bool = False):
+    """dict(Y, Y_bound, G, U, F and their bounds).  round_weights: the weights may each be rounded to bf16; kept16: G and U to 16 bits (as a gradient may have them)."""
     f = W2.shape[1]
     GU = X @ W1.T
     gu_err = _sum_bound(X, W1.T) + (HALF_BF16 * (np.abs(X) @ np.abs(W1).T) if round_weights else 0.0)
+    if kept16:
+        gu_err = gu_err + _sixteen_bits(GU, gu_err)
     G, U = GU[:, :f], GU[:, f:]
     g_err, u_err = gu_err[:, :f], gu_err[:, f:]
     a, _ = act(G, kind)
@@ -60,10 +69,10 @@ def gated_ffn(X, W1, W2, kind: str, residual=None, round_weights: bool = False):
     return dict(Y=Y, Y_bound=Y_bound, Y_err=Y_err, G=G, U=U, F=F, F_err=F_err, a=a, a_bound=a_bound, s=U * slope, s_bound=s_bound)
 
 
-def gated_ffn_backward(X, W1, W2, kind: str, dY):
-    """dict of dX, dW1, dW2 and their bounds (name + "_bound")."""
+def gated_ffn_backward(X, W1, W2, kind: str, dY, kept16: bool = False):
+    """dict of dX, dW1, dW2 and their bounds (name + "_bound").  kept16: from G and U in 16 bits."""
     f = W2.shape[1]
-    forward = gated_ffn(X, W1, W2, kind)
+    forward = gated_ffn(X, W1, W2, kind, kept16=kept16)
     F, F_err, a, a_err, s, s_err = (forward[k] for k in ("F", "F_err", "a", "a_bound", "s", "s_bound"))
     dF = dY @ W2
     dF_err = _sum_bound(dY, W2)

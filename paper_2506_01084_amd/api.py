@@ -30,6 +30,7 @@ ENC_KEPT = 1
 ENC_GATED = 2
 GRAD_ADD = 1
 ACT_SILU, ACT_GELU = 0, 1
+KEPT_32, KEPT_16 = 0, 16
 MAX_BEAMS, MAX_PICK, MAX_TEACHER, MAX_GRADIENTS = 32, 64, 256, 4096
 EXPORTS = ["z2z_create", "z2z_destroy", "z2z_reset", "z2z_lzw_encode", "z2z_lzw_decode", "z2z_step_update", "z2z_lzw_rounds", "z2z_codebook", "z2z_codebook_prefill", "z2z_codebook_usage", "z2z_codebook_prune",
            "z2z_hyper_embed", "z2z_embed_codes", "z2z_embed_codes_backward", "z2z_extended_beam", "z2z_codebook_reorder", "z2z_hyper_encode", "z2z_hyper_encode_backward", "z2z_hyper_encode_keep", "z2z_extended_logits", "z2z_extended_logits_static", "z2z_extended_sample", "z2z_extended_nll", "z2z_extended_nll_backward", "z2z_extended_distill", "z2z_extended_distill_backward", "z2z_hyper_embed_backward", "z2z_set_option",
@@ -53,8 +54,16 @@ class EncoderDesc(ctypes.Structure):
 
 
 class FfnDesc(ctypes.Structure):
-    _fields_ = [("d_ff", c_int32), ("act", c_int32), ("group", c_int32), ("reserved", c_int32), ("w_1", c_void_p), ("w_2", c_void_p),
+    _fields_ = [("d_ff", c_int32), ("act", c_int32), ("group", c_int32), ("kept", c_int32), ("w_1", c_void_p), ("w_2", c_void_p),
                 ("scale_1", c_void_p), ("scale_2", c_void_p)]
+
+    @property
+    def reserved(self) -> int:         # (the name that `kept` had)
+        return self.kept
+
+    @reserved.setter
+    def reserved(self, value: int) -> None:
+        self.kept = value
 
 
 class GatedEncoderDesc(ctypes.Structure):
@@ -93,6 +102,8 @@ class GatedFFN:
             self.desc.w_1, self.desc.w_2 = _ptr(w_1, torch.int32), _ptr(w_2, torch.int32)
             self.desc.scale_1, self.desc.scale_2 = _ptr(scale_1, torch.bfloat16), _ptr(scale_2, torch.bfloat16)
         self.desc.d_ff = self.d_ff
+        self.desc_16 = FfnDesc.from_buffer_copy(self.desc)     # (for calls that keep 16 bits)
+        self.desc_16.kept = KEPT_16
 
 
 class Encoder:
@@ -240,6 +251,10 @@ def _ptr(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"expected dtype {dtype}, got {t.dtype}")
     return t.data_ptr()
+
+
+def _kept_type(kept: Optional[torch.Tensor]):
+    return torch.bfloat16 if kept is not None and kept.dtype == torch.bfloat16 else torch.float32
 
 
 # (the handle alone: building a torch.cuda.Stream object for it takes 2.8 us a call, this 0.3)
@@ -444,21 +459,22 @@ class Context:
         _check(self._lib.z2z_quantize_q4(self._h, self._own(W, torch.bfloat16), rows, cols, int(group), self._own(q, torch.int32),
                                          self._own(scale, torch.bfloat16), _stream()), "z2z_quantize_q4")
 
-    def _block(self, ffn: GatedFFN):
+    def _block(self, ffn: GatedFFN, kept: Optional[torch.Tensor] = None):
         assert ffn.d == self.d
         if ffn.device.index != self._device:
             raise ValueError(f"expected weights on cuda:{self._device}, got some on {ffn.device}")
-        return byref(ffn.desc)
+        return byref(ffn.desc if kept is None or kept.dtype != torch.bfloat16 else ffn.desc_16)
 
     def gated_ffn(self, X: torch.Tensor, ffn: GatedFFN, Y: torch.Tensor, residual: Optional[torch.Tensor] = None,
                   kept: Optional[torch.Tensor] = None) -> None:
-        """Y = (act(X w_1[:f]^T) * (X w_1[f:]^T)) w_2^T + residual; kept [rows, 2 f] float32: what gated_ffn_backward needs of it."""
+        """Y = (act(X w_1[:f]^T) * (X w_1[f:]^T)) w_2^T + residual; kept [rows, 2 f], float32 or, for half of the memory and gradients that are slightly
+        less exact, bfloat16: what gated_ffn_backward needs of it, for that call alone to read."""
         rows, d = X.shape
         assert d == self.d and Y.shape == X.shape and (residual is None or residual.shape == X.shape)
         assert kept is None or tuple(kept.shape) == (rows, 2 * ffn.d_ff)
         own, kind = self._own, torch.bfloat16
-        _check(self._lib.z2z_gated_ffn(self._h, own(X, kind), rows, self._block(ffn), own(residual, kind), own(Y, kind),
-                                       own(kept, torch.float32), _stream()),
+        _check(self._lib.z2z_gated_ffn(self._h, own(X, kind), rows, self._block(ffn, kept), own(residual, kind), own(Y, kind),
+                                       own(kept, _kept_type(kept)), _stream()),
                "z2z_gated_ffn")
 
     def gated_ffn_backward(self, X: torch.Tensor, ffn: GatedFFN, kept: torch.Tensor, dY: torch.Tensor, dX: torch.Tensor, grad: GatedFFN,
@@ -468,7 +484,7 @@ class Context:
         assert d == self.d and dY.shape == X.shape and dX.shape == X.shape and tuple(kept.shape) == (rows, 2 * ffn.d_ff)
         assert (grad.d, grad.d_ff, grad.desc.group) == (ffn.d, ffn.d_ff, 0)
         own, kind = self._own, torch.bfloat16
-        _check(self._lib.z2z_gated_ffn_backward(self._h, own(X, kind), rows, self._block(ffn), own(kept, torch.float32), own(dY, kind), own(dX, kind),
+        _check(self._lib.z2z_gated_ffn_backward(self._h, own(X, kind), rows, self._block(ffn, kept), own(kept, _kept_type(kept)), own(dY, kind), own(dX, kind),
                                                 self._block(grad), GRAD_ADD if add else 0, _stream()), "z2z_gated_ffn_backward")
 
     def clip_gradients(self, gradients: Gradients, max_norm: float, norm: torch.Tensor) -> None:

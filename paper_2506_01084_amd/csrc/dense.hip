@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(const float* partial, i
 // 3584 columns in 19 parts 6.6 us, here 3.5.)
 template <bool GATED>
 __global__ void __launch_bounds__(256) few_sum_kernel(const float* partial, int ksplit, int rows, const int32_t* rows_dev, int N, int act,
-                                                      const void* residual, void* out, int stream_f32, z2z_gated::Kept kept) {
+                                                      const void* residual, void* out, int stream_f32, z2z_ffn_kept kept) {
   constexpr int H = GATED ? 2 : 1;
   __shared__ float4 xch[3][H][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n4 = N >> 2;
@@ -80,10 +80,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const float* partial, int 
     const float g[4] = {g4.x, g4.y, g4.z, g4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
     const size_t e = (size_t)row * N + col;
     uint2* f4 = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(out) + e);
-    if (kept.hi)
-      *f4 = z2z_gated::hidden_and_kept4(g, u, act, reinterpret_cast<uint4*>(kept.hi + e), reinterpret_cast<uint2*>(kept.lo + e));
-    else
-      *f4 = z2z_gated::hidden4(g, u, act);
+    *f4 = z2z_gated::hidden_and_keep4(g, u, act, kept, e);
   } else {
     finish_linear(x[0], float4{0.f, 0.f, 0.f, 0.f}, 0, residual, out, stream_f32, at);
   }
@@ -286,14 +283,14 @@ int z2z_partial_reserve(z2z_ctx* c, size_t bytes, float** p, hipStream_t s) {
 int z2z_launch_linear_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int N, const void* residual, void* out, bool stream_f32,
                           hipStream_t s) {
   hipLaunchKernelGGL(few_sum_kernel<false>, dim3((unsigned)(((long long)R * (N / 4) + 63) / 64)), dim3(256), 0, s, partial, ksplit, R, rows_dev, N, 0, residual,
-                     out, stream_f32 ? 1 : 0, z2z_gated::Kept{});
+                     out, stream_f32 ? 1 : 0, z2z_ffn_kept{});
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
 
-int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, void* kept, hipStream_t s) {
+int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, const z2z_ffn_kept& kept, hipStream_t s) {
   hipLaunchKernelGGL(few_sum_kernel<true>, dim3((unsigned)(((long long)R * (d_ff / 4) + 63) / 64)), dim3(256), 0, s, partial, ksplit, R, rows_dev, d_ff, act,
-                     nullptr, F, 0, kept ? z2z_gated::kept_in(kept, (size_t)R, d_ff) : z2z_gated::Kept{});
+                     nullptr, F, 0, kept);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
 }
@@ -301,7 +298,7 @@ int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t*
 namespace {
 
 // What the gated block's tile launches share.
-LogitsArgs gated_args(const void* H, const void* W, void* out, int ldo, const void* kept, int R, const int32_t* rows_dev, int d_ff, int n_columns, int K) {
+LogitsArgs gated_args(const void* H, const void* W, void* out, int ldo, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, int d_ff, int n_columns, int K) {
   LogitsArgs a;
   memset(&a, 0, sizeof(a));
   a.H = H;
@@ -318,17 +315,14 @@ LogitsArgs gated_args(const void* H, const void* W, void* out, int ldo, const vo
   a.ldo = ldo;
   a.rows_dev = rows_dev;
   a.gated.d_ff = d_ff;
-  if (kept) {
-    const z2z_gated::Kept k = z2z_gated::kept_in(const_cast<void*>(kept), (size_t)R, d_ff);
-    a.gated.kept_hi = k.hi;
-    a.gated.kept_lo = k.lo;
-  }
+  a.gated.kept_hi = kept.hi;
+  a.gated.kept_lo = kept.lo;
   return a;
 }
 
 }  // namespace
 
-int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K,
+int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, int d_ff, int K,
                             hipStream_t s, bool once) {
   const bool tile_parts = R > 256 && K / 64 >= kSplitSlabs;
   if (!tile_parts) {
@@ -345,7 +339,7 @@ int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, v
   return z2z_launch_gated_tile(a, false, grid, s);
 }
 
-int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const z2z_ffn_kept& kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
                             hipStream_t s) {
   if (!c->fast_ready || K % 64 != 0 || d_ff % 64 != 0 || R < 1) return Z2Z_EUNSUPPORTED;
   LogitsArgs a = gated_args(dY, W, slopes, 2 * d_ff, kept, R, rows_dev, d_ff, d_ff, K);

@@ -24,7 +24,7 @@ struct FewArgs {
   const uint16_t* X;       // [R, K]
   void* out;               // gated: F [R, N] bf16; else [R, N] bf16 or fp32
   const void* residual;    // else: [R, N] as `out`, or nullptr
-  z2z_gated::Kept kept;    // gated: what the backward pass is given, or nothing
+  z2z_ffn_kept kept;       // gated: what the backward pass is given, or nothing
   const int32_t* rows_dev;
   int32_t R, N, K, n_w;    // n_w: rows of W
   int32_t act, f32;
@@ -185,10 +185,7 @@ __global__ void __launch_bounds__(64 * W_WAVES, 2) few_rows_kernel(FewArgs a) {
       }
       const size_t e = (size_t)row * a.N + n;
       uint2* f4 = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + e);
-      if (a.kept.hi)
-        *f4 = z2z_gated::hidden_and_kept4(g, u, a.act, reinterpret_cast<uint4*>(a.kept.hi + e), reinterpret_cast<uint2*>(a.kept.lo + e));
-      else
-        *f4 = z2z_gated::hidden4(g, u, a.act);
+      *f4 = z2z_gated::hidden_and_keep4(g, u, a.act, a.kept, e);
     } else {
       float4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -235,10 +232,10 @@ void launch_group(const FewArgs& a, int group, int tiles, int blocks, hipStream_
 
 }  // namespace
 
-int z2z_launch_few_gated(const void* X, const void* W, const void* scale, int group, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff,
+int z2z_launch_few_gated(const void* X, const void* W, const void* scale, int group, int act, void* F, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, int d_ff,
                          int K, hipStream_t s) {
   const FewArgs a = {reinterpret_cast<const unsigned char*>(W), reinterpret_cast<const uint16_t*>(scale), reinterpret_cast<const uint16_t*>(X), F, nullptr,
-                     kept ? z2z_gated::kept_in(kept, (size_t)R, d_ff) : z2z_gated::Kept{}, rows_dev, R, d_ff, K, 2 * d_ff, act, 0};
+                     kept, rows_dev, R, d_ff, K, 2 * d_ff, act, 0};
   launch_group<2, true>(a, group, d_ff / 16, few_blocks(R), s);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;
@@ -247,7 +244,7 @@ int z2z_launch_few_gated(const void* X, const void* W, const void* scale, int gr
 int z2z_launch_few_linear(const void* X, const void* W, const void* scale, int group, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev,
                           int N, int K, hipStream_t s) {
   const FewArgs a = {reinterpret_cast<const unsigned char*>(W), reinterpret_cast<const uint16_t*>(scale), reinterpret_cast<const uint16_t*>(X), out, residual,
-                     z2z_gated::Kept{}, rows_dev, R, N, K, N, 0, f32 ? 1 : 0};
+                     z2z_ffn_kept{}, rows_dev, R, N, K, N, 0, f32 ? 1 : 0};
   launch_group<1, false>(a, group, N / 16, few_blocks(R), s);
   Z2Z_HIP_TRY(hipGetLastError());
   return Z2Z_OK;

@@ -39,17 +39,10 @@ __device__ __forceinline__ uint2 hidden4(const float (&g)[4], const float (&u)[4
 // bytes of either, 2.  (G and U in bf16 would be half of the gradients' error, 3.5e-3 of their norm instead of 2.3e-3, of which the rounding of what is returned is
 // 1.7e-3.  In fp32 the backward pass's epilogue read and wrote 14 bytes an element, with the matrix cores waiting, instead of 10, and formed exponentials
 // again: 16411 rows, d = 2048, d_ff = 5504 556 us for dF, 463 now, and 700 for the first product, 664.)
-struct Kept {
-  uint16_t* f;
-  uint32_t* hi;
-  uint16_t* lo;
-};
-__host__ __device__ __forceinline__ Kept kept_in(void* p, size_t rows, int d_ff) {
-  const size_t n = rows * d_ff;
-  unsigned char* b = reinterpret_cast<unsigned char*>(p);
-  return Kept{reinterpret_cast<uint16_t*>(b), reinterpret_cast<uint32_t*>(b + 2 * n), reinterpret_cast<uint16_t*>(b + 6 * n)};
-}
-
+//
+// Or, in a buffer of 4 bytes an element, G and U with 16 bits each, of which the backward pass forms those three matrices first.  Sign, then 0, 5 bits of exponent and 9
+// of fraction for magnitudes from 2^-16 to 2^16 (2^-10 off at most), or 1, 8 bits of exponent and 6 of fraction for all others (2^-7; zeros, infinities and NaN stay
+// what they are).  (bf16, with 2^-8 for all, doubles what these add to the gradients' error: 2.3e-3 of their norm to 3.5e-3.)
 __device__ __forceinline__ uint32_t rounded24(float x) {
   const uint32_t u = __float_as_uint(x);
   // (the sum carries a fraction of ones into the exponent, as it should; not a NaN's into the sign, nor the largest number's into an infinity)
@@ -70,6 +63,29 @@ __device__ __forceinline__ uint2 hidden_and_kept4(const float (&g)[4], const flo
   *hi = uint4{h[0], h[1], h[2], h[3]};
   *lo = uint2{l[0] | l[1] << 16, l[2] | l[3] << 16};
   return pack4(f);
+}
+
+// A number in 16 bits, as above.
+constexpr uint32_t kNear = 111u << 9;        // 2^-16: exponent and 9 bits of fraction of the least number with the finer step
+__device__ __forceinline__ uint32_t code16(float x) {
+  const uint32_t u = __float_as_uint(x), size = u & 0x7FFFFFFFu, near = (size + 0x2000u) >> 14;
+  // (the largest numbers stay below the infinity, a NaN stays one without its payload)
+  const uint32_t far = size < 0x7F800000u ? min((size + 0x10000u) >> 17, 0x3FBFu) : size == 0x7F800000u ? 0x3FC0u : 0x3FE0u;
+  return (near - kNear < 0x4000u ? near - kNear : 0x4000u | far) | (u >> 16 & 0x8000u);
+}
+__device__ __forceinline__ float of_code16(uint32_t c) {
+  const uint32_t m = c & 0x3FFFu;
+  return __uint_as_float((c & 0x4000u ? m << 17 : (m + kNear) << 14) | (c & 0x8000u) << 16);
+}
+__device__ __forceinline__ uint4 pairs4(const float (&g)[4], const float (&u)[4]) {
+  return uint4{code16(g[0]) | code16(u[0]) << 16, code16(g[1]) | code16(u[1]) << 16, code16(g[2]) | code16(u[2]) << 16, code16(g[3]) | code16(u[3]) << 16};
+}
+
+// Four columns of F, of which element `at` is the first, and what is kept beside them.
+__device__ __forceinline__ uint2 hidden_and_keep4(const float (&g)[4], const float (&u)[4], int act, const z2z_ffn_kept& kept, size_t at) {
+  if (kept.lo) return hidden_and_kept4(g, u, act, reinterpret_cast<uint4*>(kept.hi + at), reinterpret_cast<uint2*>(kept.lo + at));
+  if (kept.hi) *reinterpret_cast<uint4*>(kept.hi + at) = pairs4(g, u);
+  return hidden4(g, u, act);
 }
 
 // Four columns of the gradients dG = dF U act'(G) and dU = dF act(G), from dF and what the forward pass kept.

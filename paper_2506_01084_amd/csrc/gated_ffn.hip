@@ -6,8 +6,10 @@
 // parts of the products, whose sum applies the activation.  Backward: dF = dY W2 becomes dG | dU in the epilogue; then dW2 = dY^T F,
 // dW1 = [dG | dU]^T X, dX = [dG | dU] W1, all on operands as they are.
 #include "few_rows.h"
-#include "logits_common.h"
+#include "gated.h"
 #include "small_tile.h"
+
+#include <algorithm>
 
 namespace {
 
@@ -19,6 +21,16 @@ __global__ void __launch_bounds__(256) fill_zero_kernel(uint4* p, size_t n, uint
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n + n_q; i += (size_t)gridDim.x * 256) {
     uint4* at = i < n ? p + i : q + (i - n);
     *at = uint4{0u, 0u, 0u, 0u};
+  }
+}
+
+// F and its factors out of pairs of 16 bits: the matrices that the gradient's products and their epilogues read.  Bound by memory, 12 bytes an element.
+__global__ void __launch_bounds__(256) kept_pairs_kernel(const uint4* pairs, size_t quads, int act, z2z_ffn_kept to) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (size_t)gridDim.x * 256) {
+    const uint4 v = pairs[i];
+    const float g[4] = {z2z_gated::of_code16(v.x), z2z_gated::of_code16(v.y), z2z_gated::of_code16(v.z), z2z_gated::of_code16(v.w)};
+    const float u[4] = {z2z_gated::of_code16(v.x >> 16), z2z_gated::of_code16(v.y >> 16), z2z_gated::of_code16(v.z >> 16), z2z_gated::of_code16(v.w >> 16)};
+    reinterpret_cast<uint2*>(to.f)[i] = z2z_gated::hidden_and_keep4(g, u, act, to, 4 * i);
   }
 }
 
@@ -57,10 +69,10 @@ size_t z2z_ffn_work(const z2z_ffn* f, int d, int rows) {
   return padded((size_t)rows * f->d_ff * 2) + (f->group && rows > kExpandRows ? (size_t)3 * d * f->d_ff * 2 : 0);
 }
 
-int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
+int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
                           hipStream_t s) {
   const int d = c->cfg.d, dff = f->d_ff;
-  unsigned char* F = reinterpret_cast<unsigned char*>(kept ? kept : work);     // (the first of what is kept)
+  unsigned char* F = kept.f ? reinterpret_cast<unsigned char*>(kept.f) : reinterpret_cast<unsigned char*>(work);
   const void* w1 = f->w_1;
   *out = z2z_ffn_out{F, f->w_2, nullptr, 0, dff, false, false, false};
   if (few_rows(f, d, R)) {
@@ -76,7 +88,7 @@ int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kep
     int ksplit = 0;
     const int rc = z2z_launch_q4_parts(c, X, w1, f->scale_1, f->group, R, rows_dev, 2 * dff, d, &partial, &ksplit, s);
     if (rc != Z2Z_OK) return rc;
-    return z2z_launch_gated_sum(partial, ksplit, R, rows_dev, dff, f->act, F, nullptr, s);
+    return z2z_launch_gated_sum(partial, ksplit, R, rows_dev, dff, f->act, F, z2z_ffn_kept{}, s);
   }
   if (f->group) {
     unsigned char *e1 = F + padded((size_t)R * dff * 2), *e2 = e1 + (size_t)2 * dff * d * 2;
@@ -100,7 +112,7 @@ int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* resi
                    void* work, hipStream_t s) {
   const int d = c->cfg.d;
   z2z_ffn_out o;
-  int rc = z2z_launch_ffn_hidden(c, X, f, kept, R, rows_dev, work, &o, s);
+  int rc = z2z_launch_ffn_hidden(c, X, f, z2z_kept_in(kept, (size_t)R, f->d_ff, f->kept), R, rows_dev, work, &o, s);
   if (rc != Z2Z_OK) return rc;
   if (o.few) return z2z_launch_few_linear(o.F, o.w, o.scale, o.group, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
   if (o.small) return z2z_launch_small_linear(c, o.F, o.w, residual, Y, stream_f32, R, rows_dev, d, o.d_ff, s);
@@ -112,20 +124,26 @@ int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* resi
   return z2z_launch_linear_sum(partial, ksplit, R, rows_dev, d, residual, Y, stream_f32, s);
 }
 
-size_t z2z_ffn_backward_work(const z2z_ffn* f, int rows) { return (size_t)rows * 2 * f->d_ff * 2; }
+size_t z2z_ffn_backward_work(const z2z_ffn* f, int rows) { return (size_t)rows * f->d_ff * (f->kept == Z2Z_KEPT_16 ? 4 + 8 : 4); }
 
 int z2z_launch_ffn_backward(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* kept, const void* dY, void* dX, const z2z_ffn* grad, bool add, int R,
                             const int32_t* rows_dev, void* work, hipStream_t s) {
   const int d = c->cfg.d, dff = f->d_ff;
-  const void* F = kept;                              // (the first of what is kept)
+  z2z_ffn_kept k = z2z_kept_in(const_cast<void*>(kept), (size_t)R, dff, f->kept);
+  if (f->kept == Z2Z_KEPT_16) {
+    const size_t quads = (size_t)R * dff / 4;
+    k = z2z_kept_in(reinterpret_cast<unsigned char*>(work) + (size_t)R * dff * 4, (size_t)R, dff);
+    hipLaunchKernelGGL(kept_pairs_kernel, dim3((unsigned)std::min<size_t>((quads + 255) / 256, 16384)), dim3(256), 0, s, reinterpret_cast<const uint4*>(kept), quads,
+                       f->act, k);
+  }
   void *dw1 = const_cast<void*>(grad->w_1), *dw2 = const_cast<void*>(grad->w_2);
   // on small tiles the weight gradients go along with the products beside them
   const bool weights = small_gradient(f, d, R), input = weights || small_tiles(f, d, R, kSmallInput);
-  const z2z_small_weight w1 = {work, X, add ? dw1 : nullptr, dw1, 2 * dff, d}, w2 = {dY, F, add ? dw2 : nullptr, dw2, d, dff};
-  int rc = small_tiles(f, d, R, kSmallSlopes) ? z2z_launch_small_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, weights ? &w2 : nullptr, s)
-                                              : z2z_launch_gated_slopes(c, dY, f->w_2, kept, work, R, rows_dev, dff, d, s);
+  const z2z_small_weight w1 = {work, X, add ? dw1 : nullptr, dw1, 2 * dff, d}, w2 = {dY, k.f, add ? dw2 : nullptr, dw2, d, dff};
+  int rc = small_tiles(f, d, R, kSmallSlopes) ? z2z_launch_small_slopes(c, dY, f->w_2, k, work, R, rows_dev, dff, d, weights ? &w2 : nullptr, s)
+                                              : z2z_launch_gated_slopes(c, dY, f->w_2, k, work, R, rows_dev, dff, d, s);
   if (rc == Z2Z_OK && !weights) {
-    rc = z2z_launch_linear_weight(c, dY, d, F, dff, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
+    rc = z2z_launch_linear_weight(c, dY, d, k.f, dff, R, rows_dev, add ? dw2 : nullptr, dw2, d, dff, s);
     if (rc == Z2Z_OK) rc = z2z_launch_linear_weight(c, work, 2 * dff, X, d, R, rows_dev, add ? dw1 : nullptr, dw1, 2 * dff, d, s);
   }
   if (rc != Z2Z_OK) return rc;

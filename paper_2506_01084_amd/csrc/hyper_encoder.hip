@@ -1019,7 +1019,7 @@ int z2z_launch_hyper_encode(z2z_ctx* c, const void* E, const z2z_encoder* enc, v
                              reinterpret_cast<uint4*>(A), lay.ln2_g, lay.ln2_b, n_units);
         if (gated) {
           z2z_ffn_out o;
-          rc = z2z_launch_ffn_hidden(c, A, gated + l, nullptr, R, rows_dev, F, &o, s);
+          rc = z2z_launch_ffn_hidden(c, A, gated + l, z2z_ffn_kept{}, R, rows_dev, F, &o, s);
           if (rc != Z2Z_OK) return rc;
           rc = layer_out(F, o.w, nullptr, y, x, o.d_ff, next ? next->ln1_g : nullptr, next ? next->ln1_b : nullptr, &fused, &o);
         } else {

@@ -323,7 +323,7 @@ struct LogitsArgs {
     int32_t ldo, cap, col0, strip, n_strips, part0, row_tiles, n_work, n_seq;
   } hyper;
   // gated feed-forward block (tile kernel, GATE 1 and 2).  Forward: W holds d_ff gate rows, then d_ff rows of the other projection (w_rows = 2 d_ff),
-  // out = F [rows, d_ff] bf16, kept_hi and kept_lo (or nullptr): what else the backward pass needs (gated.h).  Backward: the product is dF, out = dG | dU [rows, 2 d_ff] bf16.
+  // out = F [rows, d_ff] bf16, kept_hi and kept_lo: what else the backward pass needs (hi and lo of z2z_ffn_kept).  Backward: the product is dF, out = dG | dU [rows, 2 d_ff] bf16.
   struct {
     uint32_t* kept_hi;
     uint16_t* kept_lo;
@@ -548,13 +548,13 @@ int z2z_launch_linear_parts(z2z_ctx* c, const void* A, const void* W, int R, con
 // the step 323 -> 335.)
 constexpr int kGatedMinSaved = 8;
 // The gated block's own products (bf16; K a multiple of 64, d_ff of 64):
-//   z2z_launch_gated_hidden   F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff]; kept (or nullptr): what the backward pass is given, F the first of it
+//   z2z_launch_gated_hidden   F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff]; kept: what the backward pass is given, or nothing
 //   z2z_launch_gated_sum      the same from fp32 parts [ksplit][R][2 d_ff] of the products
 //   z2z_launch_gated_slopes   dF = dY W, W [K, d_ff], as dG | dU [R, 2 d_ff]
-int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K,
+int z2z_launch_gated_hidden(z2z_ctx* c, const void* X, const void* W, int act, void* F, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, int d_ff, int K,
                             hipStream_t s, bool once = false);
-int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, void* kept, hipStream_t s);
-int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+int z2z_launch_gated_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int d_ff, int act, void* F, const z2z_ffn_kept& kept, hipStream_t s);
+int z2z_launch_gated_slopes(z2z_ctx* c, const void* dY, const void* W, const z2z_ffn_kept& kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
                             hipStream_t s);
 // out = sum of fp32 parts [ksplit][R][N] + residual, bf16 (stream_f32: fp32)
 int z2z_launch_linear_sum(const float* partial, int ksplit, int R, const int32_t* rows_dev, int N, const void* residual, void* out, bool stream_f32,

@@ -729,8 +729,8 @@ __device__ __forceinline__ void store_prob16(const Acc& acc, const LogitsArgs& a
 
 // Store one finished tile of a gated block's first product: blocks of 16 gate columns and of the same 16 columns of the other projection alternate
 // (see gated_offset), so that a lane holds both of an element.  row0, col0: of the wave's 128 rows and 64 columns of F (uniform, as every address but a lane's
-// offset is).  WHOLE: all of them exist.
-template <bool WHOLE>
+// offset is).  WHOLE: all of them exist.  PAIRS: G and U are kept in 16 bits each (with that as a branch here, accumulators are spilled).
+template <bool WHOLE, bool PAIRS>
 __device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& a, int row0, int r_end, int col0) {
   const int lane15 = threadIdx.x & 15, quarter = (threadIdx.x >> 4) & 3, f = a.gated.d_ff;
   const uint32_t own = (uint32_t)(lane15 * f + quarter * 4);                               // element of this lane's four in a block
@@ -748,7 +748,12 @@ __device__ __forceinline__ void store_gated16(const Acc& acc, const LogitsArgs& 
         g[e] = read_acc(acc[2 * k][j][e]);
         u[e] = read_acc(acc[2 * k + 1][j][e]);
       }
-      if (a.gated.kept_hi) {
+      if (PAIRS) {
+        const uint4 pairs = z2z_gated::pairs4(g, u);
+        if (WHOLE || (row_ok && col0 + k * 16 + quarter * 4 < f)) *reinterpret_cast<uint4*>(a.gated.kept_hi + at + k * 16 + own) = pairs;
+        h[k] = z2z_gated::hidden4(g, u, a.gated.act);
+        __builtin_amdgcn_sched_barrier(0);
+      } else if (a.gated.kept_hi) {
         uint4 hi;
         uint2 lo;
         h[k] = z2z_gated::hidden_and_kept4(g, u, a.gated.act, &hi, &lo);
@@ -889,7 +894,7 @@ __device__ __forceinline__ void merge_rows(R (&a)[F_N], S swap, float inv_t = 1.
 // TEMP (modes 0, 1 and 3): the softmax has a temperature.  (Instances of their own: with 1 / T and log2(e) / T read from the arguments in every call,
 // which costs two more scalar registers, 32768 rows x 128256 at T = 1 took 23.82 ms instead of 23.66.)
 // SUM (K-major products): one term of a sum (store_sum16); by rows where H is K-major too.
-// GATE (mode 2): 1 = the first product of a gated block, both projections of 128 columns in a tile (store_gated16); 2 = its gradient's, dF (TW).
+// GATE (mode 2): 1 = the first product of a gated block, both projections of 128 columns in a tile (store_gated16), 3 = with G and U kept in 16 bits; 2 = its gradient's, dF (TW).
 template <int MODE, bool ROT = false, bool TW = false, bool TH = false, bool HYP = false, bool TEMP = false, bool SUM = false, int GATE = 0>
 __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   static_assert((MODE == 2 || !TW) && (TW || !TH), "dense layers only, and H K-major only where W is");
@@ -897,6 +902,7 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   static_assert(!TEMP || MODE == 0 || MODE == 1 || MODE == 3, "");
   static_assert(!SUM || TW, "");
   static_assert(GATE == 0 || (MODE == 2 && !TH && !SUM && TW == (GATE == 2)), "");
+  constexpr bool FIRST_OF_BLOCK = GATE == 1 || GATE == 3;
   const float inv_t = TEMP ? a.inv_t : 1.f, log2e_t = TEMP ? a.log2e_t : 1.4426950408889634f;
   constexpr bool PROBE_NOREQ = MODE == 8 || MODE == 9;
   constexpr bool PROBE_MFMA = MODE == 9;
@@ -1108,10 +1114,10 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   bool live = true;
   auto set_tile = [&](int vt) {
     if (TW) w_col = vt * F_KROW;
-    Wtile = at.W + (TW ? (size_t)w_col : (size_t)vt * (GATE == 1 ? FT / 2 : FT) * pitch_w);
+    Wtile = at.W + (TW ? (size_t)w_col : (size_t)vt * (FIRST_OF_BLOCK ? FT / 2 : FT) * pitch_w);
 #pragma unroll
     for (int i = 0; i < F_PAIRS; ++i)
-      voffA[i] = GATE == 1 ? gated_offset(i, a.gated.d_ff - 1 - vt * (FT / 2)) : TW ? krow_offset(i, ((int)pitch_w - w_col) >> 4, pitch_w) : row_offset(i, at.n_valid - 1 - vt * FT, pitch_w);
+      voffA[i] = FIRST_OF_BLOCK ? gated_offset(i, a.gated.d_ff - 1 - vt * (FT / 2)) : TW ? krow_offset(i, ((int)pitch_w - w_col) >> 4, pitch_w) : row_offset(i, at.n_valid - 1 - vt * FT, pitch_w);
   };
   auto open_item = [&](bool behind) __attribute__((always_inline)) {
     if (HYP) asm volatile("" : "+s"(lj));       // (what is worked out here is not worked out for every slab)
@@ -1339,13 +1345,13 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
         if (it.part >= 0)
           store_partial16(acc, a.split + (ptrdiff_t)it.part * (FT * FT) - ((ptrdiff_t)r0 * FT + vt * FT), FT, row_base, r_end, col_base, n_valid);
         else if (GATE != 0) {
-          int row0 = r0 + wr * 128, col0 = GATE == 1 ? vt * (FT / 2) + wv * 64 : vt * FT + wv * 128;
+          int row0 = r0 + wr * 128, col0 = FIRST_OF_BLOCK ? vt * (FT / 2) + wv * 64 : vt * FT + wv * 128;
           asm volatile("" : "+s"(row0), "+s"(col0));
-          const bool whole = row0 + 128 <= r_end && col0 + (GATE == 1 ? 64 : 128) <= a.gated.d_ff;
-          if (GATE == 1 && whole)
-            store_gated16<true>(acc, a, row0, r_end, col0);
-          else if (GATE == 1)
-            store_gated16<false>(acc, a, row0, r_end, col0);
+          const bool whole = row0 + 128 <= r_end && col0 + (FIRST_OF_BLOCK ? 64 : 128) <= a.gated.d_ff;
+          if (FIRST_OF_BLOCK && whole)
+            store_gated16<true, GATE == 3>(acc, a, row0, r_end, col0);
+          else if (FIRST_OF_BLOCK)
+            store_gated16<false, GATE == 3>(acc, a, row0, r_end, col0);
           else if (whole)
             store_gated_slopes16<true>(acc, a, row0, r_end, col0);
           else
@@ -1462,13 +1468,8 @@ __global__ void __launch_bounds__(256) tile_sum_kernel(LogitsArgs a) {
         from += (size_t)last.rem * (FT * FT);
       }
       uint2* out = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + (size_t)(r0 + row) * a.ldo + fcol);
-      if (a.gated.kept_hi) {
-        const size_t at = (size_t)(r0 + row) * a.gated.d_ff + fcol;
-        *out = z2z_gated::hidden_and_kept4(x[0], x[1], a.gated.act, reinterpret_cast<uint4*>(a.gated.kept_hi + at),
-                                           reinterpret_cast<uint2*>(a.gated.kept_lo + at));
-      } else {
-        *out = z2z_gated::hidden4(x[0], x[1], a.gated.act);
-      }
+      *out = z2z_gated::hidden_and_keep4(x[0], x[1], a.gated.act, z2z_ffn_kept{nullptr, a.gated.kept_hi, a.gated.kept_lo},
+                                         (size_t)(r0 + row) * a.gated.d_ff + fcol);
       continue;
     }
     const int tcol = 4 * (int)(threadIdx.x & 63), col = st * FT + tcol;
@@ -1618,6 +1619,8 @@ int z2z_launch_logits_fast(int mode, const LogitsArgs& a, unsigned grid, hipStre
 int z2z_launch_gated_tile(const LogitsArgs& a, bool backward, unsigned grid, hipStream_t s) {
   if (backward)
     hipLaunchKernelGGL((logits_fast_kernel<2, false, true, false, false, false, false, 2>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
+  else if (a.gated.kept_hi && !a.gated.kept_lo)
+    hipLaunchKernelGGL((logits_fast_kernel<2, false, false, false, false, false, false, 3>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
   else
     hipLaunchKernelGGL((logits_fast_kernel<2, false, false, false, false, false, false, 1>), dim3(grid), dim3(F_THREADS), F_LDS, s, a);
   if (a.split && backward)
@@ -1677,6 +1680,8 @@ int z2z_logits_fast_prepare(z2z_ctx* c) {
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<7, true>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, false, false, false, false, false, 1>),
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
+  Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, false, false, false, false, false, 3>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));
   Z2Z_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(logits_fast_kernel<2, false, true, false, false, false, false, 2>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, F_LDS));

@@ -1,5 +1,5 @@
 // The gated block's products on tiles of 64 x 64 (small_tile.hip), bf16; widths are multiples of 64:
-//   z2z_launch_small_gated    F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff]; kept: nullptr, or what the backward pass is given, F the first of it
+//   z2z_launch_small_gated    F = act(X W[:d_ff]^T) * (X W[d_ff:]^T), [R, d_ff]; kept: what the backward pass is given, or nothing
 //   z2z_launch_small_slopes   dF = dY W, W [K, d_ff], as dG | dU [R, 2 d_ff]
 //   z2z_launch_small_linear   out [R, N] = A [R, K] W^T + residual, W [N, K]; f32: residual and out are fp32
 //   z2z_launch_small_parts    A W^T as fp32 parts [*ksplit][R][N], which the caller adds up before the next dense layer is launched; or nothing (0) where K is not shared out
@@ -16,8 +16,8 @@ struct z2z_small_weight {
   int M, N;
 };
 
-int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K, hipStream_t s);
-int z2z_launch_small_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, int d_ff, int K, hipStream_t s);
+int z2z_launch_small_slopes(z2z_ctx* c, const void* dY, const void* W, const z2z_ffn_kept& kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
                             const z2z_small_weight* weight, hipStream_t s);
 int z2z_launch_small_linear(z2z_ctx* c, const void* A, const void* W, const void* residual, void* out, bool f32, int R, const int32_t* rows_dev, int N, int K,
                             hipStream_t s);

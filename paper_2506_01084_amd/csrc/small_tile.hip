@@ -30,7 +30,7 @@ struct SmallArgs {
   void* out;
   const void* residual;
   float* partial;                            // [parts][R][N]
-  z2z_gated::Kept kept;
+  z2z_ffn_kept kept;
   const int32_t *rows_dev, *k_dev;           // nullptr, or how many rows of the output, of the contraction, exist
   int32_t R, N, K, ldh, ldw, ldo;
   int32_t per;                               // slabs of a part
@@ -177,10 +177,7 @@ __device__ __forceinline__ void small_tile(const SmallArgs& a, unsigned block, u
       const int col = nt * 32 + wv * 16 + quarter * 4;
       const size_t at = (size_t)row * a.d_ff + col;
       uint2* f4 = reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + at);
-      if (a.kept.hi)
-        *f4 = z2z_gated::hidden_and_kept4(g, u, a.act, reinterpret_cast<uint4*>(a.kept.hi + at), reinterpret_cast<uint2*>(a.kept.lo + at));
-      else
-        *f4 = z2z_gated::hidden4(g, u, a.act);
+      *f4 = z2z_gated::hidden_and_keep4(g, u, a.act, a.kept, at);
       continue;
     }
     const int col = nt * S_T + wv * 32 + quarter * 8;
@@ -325,12 +322,12 @@ SmallArgs weight_args(const z2z_small_weight& w, int rows, const int32_t* rows_d
 
 }  // namespace
 
-int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, void* kept, int R, const int32_t* rows_dev, int d_ff, int K, hipStream_t s) {
+int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, int d_ff, int K, hipStream_t s) {
   SmallArgs a = {};
   a.H = reinterpret_cast<const uint16_t*>(X);
   a.W = reinterpret_cast<const uint16_t*>(W);
   a.out = F;
-  if (kept) a.kept = z2z_gated::kept_in(kept, (size_t)R, d_ff);
+  a.kept = kept;
   a.rows_dev = rows_dev;
   a.R = R;
   a.K = a.ldh = a.ldw = K;
@@ -340,13 +337,13 @@ int z2z_launch_small_gated(const void* X, const void* W, int act, void* F, void*
   return launch<false, 1, false>(a, 1, s);
 }
 
-int z2z_launch_small_slopes(z2z_ctx* c, const void* dY, const void* W, const void* kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
+int z2z_launch_small_slopes(z2z_ctx* c, const void* dY, const void* W, const z2z_ffn_kept& kept, void* slopes, int R, const int32_t* rows_dev, int d_ff, int K,
                             const z2z_small_weight* weight, hipStream_t s) {
   SmallArgs a = {};
   a.H = reinterpret_cast<const uint16_t*>(dY);
   a.W = reinterpret_cast<const uint16_t*>(W);
   a.out = slopes;
-  a.kept = z2z_gated::kept_in(const_cast<void*>(kept), (size_t)R, d_ff);
+  a.kept = kept;
   a.rows_dev = rows_dev;
   a.R = R;
   a.K = a.ldh = K;

@@ -304,7 +304,7 @@ namespace {
 
 // of a gated block on a context of width d: its description's numbers, and its pointers
 int ffn_ok(const z2z_ctx* c, const z2z_ffn* f, bool bf16_only) {
-  if (!f || f->d_ff < 1 || f->reserved != 0 || (f->act != Z2Z_ACT_SILU && f->act != Z2Z_ACT_GELU)) return Z2Z_EINVAL;
+  if (!f || f->d_ff < 1 || (f->kept != Z2Z_KEPT_32 && f->kept != Z2Z_KEPT_16) || (f->act != Z2Z_ACT_SILU && f->act != Z2Z_ACT_GELU)) return Z2Z_EINVAL;
   if (!f->w_1 || !f->w_2 || !aligned16(f->w_1) || !aligned16(f->w_2)) return Z2Z_EINVAL;
   if (f->group != 0 && f->group != 32 && f->group != 64 && f->group != 128) return Z2Z_EINVAL;
   if (f->group != 0 && (!f->scale_1 || !f->scale_2 || !aligned16(f->scale_1) || !aligned16(f->scale_2))) return Z2Z_EINVAL;
@@ -345,7 +345,7 @@ int gated_layers_ok(const z2z_ctx* c, const z2z_encoder* enc, bool training) {
   for (int l = 0; f && l < enc->n_layers; ++l) {
     const int rc = ffn_ok(c, f + l, training);
     if (rc != Z2Z_OK) return rc;
-    if (f[l].d_ff != f[0].d_ff) return Z2Z_EINVAL;
+    if (f[l].d_ff != f[0].d_ff || f[l].kept != Z2Z_KEPT_32) return Z2Z_EINVAL;
   }
   return Z2Z_OK;
 }
@@ -417,6 +417,8 @@ size_t q4_bytes(size_t rows, size_t cols) { return rows * ((cols + 127) / 128) *
 struct FfnBytes {
   size_t w_1, w_2, scale_1, scale_2;
 };
+// ... of what is kept of a call
+size_t kept_bytes(const z2z_ffn* f, int32_t rows) { return (size_t)rows * f->d_ff * (f->kept == Z2Z_KEPT_16 ? 4 : 8); }
 FfnBytes ffn_bytes(const z2z_ctx* c, const z2z_ffn* f) {
   const size_t d = c->cfg.d, n = f->d_ff;
   if (!f->group) return FfnBytes{4 * n * d, 2 * n * d, 0, 0};
@@ -425,14 +427,14 @@ FfnBytes ffn_bytes(const z2z_ctx* c, const z2z_ffn* f) {
 
 }  // namespace
 
-Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, float* d_kept,
+Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_residual, void* d_Y, void* d_kept,
                           void* stream) {
   if (!ctx || rows < 0 || (rows > 0 && (!d_X || !d_Y))) return Z2Z_EINVAL;
   if (!aligned16(d_X) || !aligned16(d_residual) || !aligned16(d_Y) || !aligned16(d_kept)) return Z2Z_EINVAL;
   int rc = ffn_ok(ctx, ffn, d_kept != nullptr);
   if (rc != Z2Z_OK) return rc;
   if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
-  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 8;
+  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = kept_bytes(ffn, rows);
   const FfnBytes w = ffn_bytes(ctx, ffn);
   const Bytes in[] = {{d_X, row}, {d_residual == d_Y ? nullptr : d_residual, row}, {ffn->w_1, w.w_1}, {ffn->w_2, w.w_2}, {ffn->scale_1, w.scale_1}, {ffn->scale_2, w.scale_2}};
   const Bytes out[] = {{d_Y, row}, {d_kept, kept}};
@@ -444,7 +446,7 @@ Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z
   return z2z_launch_ffn(ctx, d_X, ffn, d_residual, d_Y, false, d_kept, rows, nullptr, ctx->ffn_ws.p, static_cast<hipStream_t>(stream));
 }
 
-Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const float* d_kept, const void* d_dY, void* d_dX,
+Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z_ffn* ffn, const void* d_kept, const void* d_dY, void* d_dX,
                                    const z2z_ffn* grad, int32_t flags, void* stream) {
   if (!ctx || rows < 0 || (rows > 0 && (!d_X || !d_kept || !d_dY || !d_dX))) return Z2Z_EINVAL;
   if (flags != 0 && flags != Z2Z_GRAD_ADD) return Z2Z_EINVAL;
@@ -453,7 +455,7 @@ Z2Z_API int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, 
   int rc = ffn_ok(ctx, ffn, true);
   if (rc != Z2Z_OK) return rc;
   if (rows > kFfnRows) return Z2Z_EUNSUPPORTED;
-  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = (size_t)rows * ffn->d_ff * 8;
+  const size_t row = (size_t)rows * ctx->cfg.d * 2, kept = kept_bytes(ffn, rows);
   const FfnBytes w = ffn_bytes(ctx, ffn);
   const size_t w1 = w.w_1, w2 = w.w_2;
   const Bytes in[] = {{d_X, row}, {d_kept, kept}, {d_dY, row}, {ffn->w_1, w1}, {ffn->w_2, w2}}, out[] = {{d_dX, row}, {grad->w_1, w1}, {grad->w_2, w2}};

@@ -209,9 +209,24 @@ struct z2z_ffn_out {
   int group, d_ff;
   bool once, few, small;   // few, small: the second product runs on z2z_launch_few_linear, z2z_launch_small_linear
 };
-int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, void* kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
+// What of a forward call on R rows is kept for its gradient (gated.h): nothing (all null), three matrices one behind the other in a buffer of 8 bytes an element
+// of F, or (lo and f null) one of 4.
+struct z2z_ffn_kept {
+  uint16_t* f;
+  uint32_t* hi;
+  uint16_t* lo;
+};
+inline z2z_ffn_kept z2z_kept_in(void* p, size_t rows, int d_ff, int form = Z2Z_KEPT_32) {
+  const size_t n = rows * d_ff;
+  unsigned char* b = reinterpret_cast<unsigned char*>(p);
+  if (!b) return z2z_ffn_kept{nullptr, nullptr, nullptr};
+  if (form == Z2Z_KEPT_16) return z2z_ffn_kept{nullptr, reinterpret_cast<uint32_t*>(b), nullptr};
+  return z2z_ffn_kept{reinterpret_cast<uint16_t*>(b), reinterpret_cast<uint32_t*>(b + 2 * n), reinterpret_cast<uint16_t*>(b + 6 * n)};
+}
+int z2z_launch_ffn_hidden(z2z_ctx* c, const void* X, const z2z_ffn* f, const z2z_ffn_kept& kept, int R, const int32_t* rows_dev, void* work, z2z_ffn_out* out,
                           hipStream_t s);
-// The gated block on R rows (or the first *rows_dev of them), with work space of z2z_ffn_work bytes; stream_f32: residual and Y are fp32.
+// The gated block on R rows (or the first *rows_dev of them), with work space of z2z_ffn_work bytes; stream_f32: residual and Y are fp32; kept: in the form that
+// f->kept says, or nullptr.
 size_t z2z_ffn_work(const z2z_ffn* f, int d, int rows);
 int z2z_launch_ffn(z2z_ctx* c, const void* X, const z2z_ffn* f, const void* residual, void* Y, bool stream_f32, void* kept, int R, const int32_t* rows_dev,
                    void* work, hipStream_t s);

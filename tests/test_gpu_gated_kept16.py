@@ -1,0 +1,185 @@
+"""The gated block's gradient from what a forward call kept in 16 bits (a bfloat16 tensor), against the oracle: the numbers kept, and the gradients element by element."""
+import numpy as np
+import pytest
+
+import oracle
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_gated_ffn import _context, _host, _tensors, _within  # noqa: E402
+
+NEAR = 111 << 9
+
+
+def _decoded(kept, rows, f):
+    """What a kept tensor holds: G and U, [rows, f] float64."""
+    words = kept.contiguous().view(torch.int32).cpu().numpy().view(np.uint32).reshape(rows, f)
+    out = []
+    for c in (words & 0xFFFF, words >> 16):
+        m = c & 0x3FFF
+        bits = np.where(c & 0x4000, m << 17, (m + NEAR) << 14) | (c & 0x8000) << 16
+        out.append(bits.astype(np.uint32).view(np.float32).astype(np.float64))
+    return out
+
+
+def _steps(x):
+    """float32 numbers [n] in 16 bits, one at a time."""
+    out = []
+    for v in x:
+        m, e = np.frexp(abs(np.float64(v)))                 # m in [1/2, 1)
+        if not np.isfinite(v) or v == 0:
+            out.append(float(v))
+            continue
+        near = np.floor(m * 2 ** 10 + 0.5) / 2 ** 10 * 2.0 ** e
+        least = max(e, -125)                                # (subnormal numbers have the step of the least normal ones)
+        far = np.floor(np.ldexp(abs(np.float64(v)), 7 - least) + 0.5) * 2.0 ** (least - 7)
+        far = min(far, 2.0 ** 128 - 2.0 ** 121)
+        out.append(float(np.sign(v)) * (near if 2.0 ** -16 <= near < 2.0 ** 16 else far))
+    return np.array(out)
+
+
+# (every kernel that keeps: few rows in one launch, small tiles, parts that are added up, whole and cut tiles of the tile kernel)
+SHAPES = [(1, 64, 64), (16, 512, 128), (33, 128, 320), (65, 192, 192), (237, 1024, 448), (40, 8192, 5504), (1031, 3520, 1792), (16411, 512, 1344), (3000, 128, 704), (300, 6400, 3456)]
+
+
+@pytest.mark.parametrize("rows,d,f", SHAPES)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gradient(rows, d, f, act):
+    from paper_2506_01084_amd import api
+
+    if rows * d * f > 1 << 32 and act == "silu":
+        pytest.skip("one activation is enough of the largest")
+    X, W1, W2, R, dY = _tensors(rows, d, f, rows + d + f)
+    ctx, block = _context(d), api.GatedFFN(W1, W2, act=act)
+    Y, without = torch.full_like(X, float("nan")), torch.full_like(X, float("nan"))
+    kept = torch.full((rows, 2 * f), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ctx.gated_ffn(X, block, without, residual=R)
+    ctx.gated_ffn(X, block, Y, residual=R, kept=kept)
+    assert torch.equal(Y, without)
+    x, w1, w2 = _host(X), _host(W1), _host(W2)
+    ref = oracle.gated_ffn(x, w1, w2, act)
+    for name, got in zip("GU", _decoded(kept, rows, f)):
+        err = (d + 8) * 2.0 ** -24 * (np.abs(x) @ np.abs(w1[:f] if name == "G" else w1[f:]).T)
+        size = np.abs(ref[name])
+        step = np.where((size - err >= 2.0 ** -16) & (size + err < 2.0 ** 15), 2.0 ** -10, 2.0 ** -7)
+        assert np.all(np.abs(got - ref[name]) <= err + step * (size + err)), name
+    dX, dW1, dW2 = (torch.full_like(t, float("nan")) for t in (X, W1, W2))
+    ctx.gated_ffn_backward(X, block, kept, dY, dX, api.GatedFFN(dW1, dW2))
+    want = oracle.gated_ffn_backward(x, w1, w2, act, _host(dY), kept16=True)
+    for name, got in (("dX", dX), ("dW1", dW1), ("dW2", dW2)):
+        _within(got, want[name], want[name + "_bound"], name)
+        # a rounding to bf16 is 2^-8 sqrt(0.54 / 3) of numbers' norm (0.54: the mean of 1 / m^2 over mantissas m, evenly spread in their logarithm); two of them here, and three of
+        # a quarter: 2.45e-3.  With G and U in bf16 they would be five: 3.7e-3
+        if rows * d * f > 1 << 20:
+            off = np.linalg.norm(_host(got) - want[name]) / np.linalg.norm(want[name])
+            assert off <= 2.6e-3, (name, off)
+    # the same bits again, and added to what is there
+    a1, a2 = torch.randn_like(dW1), torch.randn_like(dW2)
+    was = [_host(a1), _host(a2)]
+    again = torch.full_like(dX, float("nan"))
+    ctx.gated_ffn_backward(X, block, kept, dY, again, api.GatedFFN(a1, a2), add=True)
+    assert torch.equal(dX, again)
+    for name, got, before in (("dW1", a1, was[0]), ("dW2", a2, was[1])):
+        total = want[name] + before
+        assert np.all(np.abs(_host(got) - total) <= (want[name + "_err"] * 1.02 + 2.0 ** -8 * (np.abs(total) + want[name + "_err"])) * 1.001), name
+
+
+@pytest.mark.parametrize("rows", [1, 70, 600])
+def test_numbers_kept(rows):
+    """Given numbers as G and U, exactly: ties, borders of the finer steps, the largest, the least, zeros, infinities."""
+    from paper_2506_01084_amd import api
+
+    d, f = 128, 64
+    top = 2.0 ** 16
+    values = [0.0, 1.0, 1 + 2.0 ** -9, 1 + 2.0 ** -10, 1 + 3 * 2.0 ** -10, 1 + 2.0 ** -10 - 2.0 ** -15, 2 - 2.0 ** -10, 2 - 2.0 ** -11, 2.0 ** -16, 2.0 ** -16 * (1 - 2.0 ** -8),
+              2.0 ** -16 * (1 - 2.0 ** -11), 2.0 ** -17, 2.0 ** -17 * (1 + 2.0 ** -6), 2.0 ** -17 * (1 + 2.0 ** -7), 2.0 ** -17 * (1 + 2.0 ** -7 - 2.0 ** -12), top * (1 - 2.0 ** -9), top * (1 - 2.0 ** -10),
+              top * (1 - 2.0 ** -11), top, top * (1 + 2.0 ** -7), 3e38, 2.0 ** 128 - 2.0 ** 120, 1e-30, 1.2e-38, 123.4375, -0.37109375]
+    values = torch.tensor((values + [-v for v in values])[:51] + [float("inf"), float("-inf")] + [0.5] * 11, dtype=torch.float64)
+    W1 = torch.zeros((2 * f, d), dtype=torch.float64)
+    hi = values.bfloat16().double()                          # (each the sum of at most two bf16)
+    hi[torch.isinf(hi) & torch.isfinite(values)] = float(torch.finfo(torch.bfloat16).max)
+    lo = torch.where(torch.isfinite(values), values - hi, torch.zeros(()).double())
+    W1[:f, 0], W1[:f, 1] = hi, lo
+    W1[f:, 0], W1[f:, 1] = hi.flip(0), lo.flip(0)
+    W2 = torch.zeros((d, f))
+    X = torch.zeros((rows, d))
+    X[:, :2] = 1
+    got_hi, got_lo = W1[:f, 0].bfloat16().double(), W1[:f, 1].bfloat16().double()
+    X, W1, W2 = (t.bfloat16().cuda() for t in (X, W1, W2))
+    kept = torch.empty((rows, 2 * f), dtype=torch.bfloat16, device="cuda")
+    _context(d).gated_ffn(X, api.GatedFFN(W1, W2), torch.empty_like(X), kept=kept)
+    G, U = _decoded(kept, rows, f)
+    want = _steps((got_hi + got_lo).float().numpy())
+    least = 2.0 ** -131                                       # (a matrix instruction may take a subnormal number, at most 2^-133 here, for zero: a step of the least numbers)
+    for got in (G, U[:, ::-1]):
+        with np.errstate(invalid="ignore"):
+            same = (got == want) | (np.abs(got - want) <= least)
+        assert np.all(same), [(float(v), float(a), float(b)) for v, a, b, ok in zip(values, got[0], want, same[0]) if not ok]
+
+
+def test_nan_rows_and_rows_behind_the_last():
+    from paper_2506_01084_amd import api
+
+    d, f = 192, 128
+    X, W1, W2, R, dY = _tensors(300, d, f, 4)
+    ctx, block = _context(d), api.GatedFFN(W1, W2)
+    X[5] = float("nan")
+    for rows in (0, 1, 130, 299):
+        Y, kept, dX = torch.full_like(X, 7.0), torch.full((300, 2 * f), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full_like(X, 7.0)
+        dW = torch.full_like(W1, 7.0), torch.full_like(W2, 7.0)
+        ctx.gated_ffn(X[:rows], block, Y[:rows], residual=R[:rows], kept=kept[:rows])
+        ctx.gated_ffn_backward(X[:rows], block, kept[:rows], dY[:rows], dX[:rows], api.GatedFFN(*dW))
+        for t in (Y, kept, dX):
+            assert (t[rows:] == 7.0).all()
+        if rows == 0:
+            assert (dW[0] == 0).all() and (dW[1] == 0).all()
+        if rows > 5:
+            assert torch.isnan(dX[5]).all() and torch.isfinite(dX[6:rows]).all()
+
+
+@pytest.mark.parametrize("rows,d,f", [(24, 2048, 320), (900, 2048, 1344)])
+def test_graph_replays_and_streams(rows, d, f):
+    from paper_2506_01084_amd import api
+
+    X, W1, W2, R, dY = _tensors(rows, d, f, 21)
+    ctx, block = _context(d), api.GatedFFN(W1, W2, act="gelu")
+    kept = torch.empty((rows, 2 * f), dtype=torch.bfloat16, device="cuda")
+    out, eager = ([torch.empty_like(t) for t in (X, X, W1, W2)] for _ in range(2))
+
+    def step(to, keep):
+        ctx.gated_ffn(X, block, to[0], residual=R, kept=keep)
+        ctx.gated_ffn_backward(X, block, keep, dY, to[1], api.GatedFFN(to[2], to[3]))
+
+    step(eager, torch.empty_like(kept))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, kept)
+    for i in range(4):
+        X.copy_(torch.randn((rows, d), generator=torch.Generator().manual_seed(i)).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager, torch.empty_like(kept))
+        for a, b in zip(out, eager):
+            assert torch.equal(a, b), i
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(out, kept)
+    side.synchronize()
+    for a, b in zip(out, eager):
+        assert torch.equal(a, b)
+
+
+def test_binding_refusals():
+    from paper_2506_01084_amd import api
+
+    X, W1, W2, _, dY = _tensors(8, 128, 64, 2)
+    ctx, block = _context(128), api.GatedFFN(W1, W2)
+    for kept in (torch.empty((8, 128), dtype=torch.float16, device="cuda"), torch.empty((8, 256), dtype=torch.bfloat16, device="cuda")[:, ::2]):
+        with pytest.raises(ValueError):
+            ctx.gated_ffn(X, block, torch.empty_like(X), kept=kept)
+        with pytest.raises(ValueError):
+            ctx.gated_ffn_backward(X, block, kept, dY, torch.empty_like(X), api.GatedFFN(W1.clone(), W2.clone()))
+    with pytest.raises(AssertionError):
+        ctx.gated_ffn(X, block, torch.empty_like(X), kept=torch.empty((8, 64), dtype=torch.bfloat16, device="cuda"))
