@@ -138,7 +138,7 @@ def prepare(case, seed):
         st["W2"], st["scale2"] = _to_four_bits(st["W2"], case["group"])
     if case["kind"] == "train":
         st["dY"] = _normal(gen, (rows, d), 1e-2)
-        st["kept"] = torch.empty((rows, 2 * f), dtype=torch.float32, device="cuda")
+        st["kept"] = torch.empty((rows, 2 * f), dtype=torch.bfloat16, device="cuda")
         st["dX"], st["dW1"], st["dW2"] = torch.empty_like(st["X"]), torch.empty_like(st["W1"]), torch.empty_like(st["W2"])
     if own:
         from paper_2506_01084_amd import api
