@@ -1087,7 +1087,7 @@ __global__ void __launch_bounds__(F_THREADS) logits_fast_kernel(LogitsArgs a) {
   auto row_offset = [&](int i, int lim, size_t pitch) -> uint32_t {
     const int row = (wave * F_PAIRS + i) * 8 + ld_row;
     const int chunk16 = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
-    return (uint32_t)(min(row, lim) * (int)pitch + chunk16);
+    return (uint32_t)min(row, lim) * (uint32_t)pitch + (uint32_t)chunk16;
   };
   // (first product of a gated block: the tile's blocks of 16 rows alternate between the d_ff gate rows and the other projection's, which lie behind
   // them; rows past the last are clamped onto it in either)

@@ -310,7 +310,8 @@ int ffn_ok(const z2z_ctx* c, const z2z_ffn* f, bool bf16_only) {
   if (f->group != 0 && (!f->scale_1 || !f->scale_2 || !aligned16(f->scale_1) || !aligned16(f->scale_2))) return Z2Z_EINVAL;
   const int d = c->cfg.d;
   if (c->cfg.dtype != Z2Z_BF16 || !c->fast_ready || d % 64 != 0 || f->d_ff % 64 != 0) return Z2Z_EUNSUPPORTED;
-  if (((long long)f->d_ff + 128) * d * 2 >= (1LL << 31)) return Z2Z_EUNSUPPORTED;       // (bytes of a projection: 32-bit offsets)
+  // (offsets of 32 bits: in a projection, and in 256 rows of dG | dU, whose products read them from the first of these on; no launch has 2^32 threads then)
+  if (((long long)f->d_ff + 128) * d * 2 >= (1LL << 31) || 256LL * 4 * f->d_ff >= (1LL << 32)) return Z2Z_EUNSUPPORTED;
   if (f->group != 0 && (bf16_only || d % f->group != 0 || f->d_ff % f->group != 0)) return Z2Z_EUNSUPPORTED;
   return Z2Z_OK;
 }
