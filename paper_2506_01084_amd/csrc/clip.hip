@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(C_THREADS) clip_scale_kernel(ClipList l, const
     const int chunk = chunks - 1 - k, t = tensor_of(l, chunk);
     const bool bf16 = l.bf16[t] != 0;
     unsigned char* out = l.out[t];
-    if (!out || (c == 1.0f && out == l.data[t])) continue;
+    if (c == 1.0f && out == l.data[t]) continue;
     int64_t first;
     const Span s = span_of(l, t, chunk, &first);
     const bool wide = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(l.data[t])) & 15) == 0;
@@ -263,14 +263,12 @@ int z2z_launch_clip_gradients(z2z_ctx* c, const z2z_gradient* g, int n, float ma
   Interval* iv = new (std::nothrow) Interval[2 * (size_t)n + 1];
   if (!iv) return Z2Z_ENOMEM;
   int m = 0;
-  bool writes = false;
   for (int i = 0; i < n; ++i) {
     if (g[i].n == 0) continue;
     const uintptr_t bytes = (uintptr_t)g[i].n * (g[i].dtype == Z2Z_BF16 ? 2 : 4);
     const uintptr_t in = reinterpret_cast<uintptr_t>(g[i].data), out = reinterpret_cast<uintptr_t>(g[i].out);
     iv[m++] = Interval{in, in + bytes, in == out};
     if (out && out != in) iv[m++] = Interval{out, out + bytes, true};
-    writes = writes || out;
   }
   iv[m++] = Interval{reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm) + 2 * sizeof(float), true};
   std::sort(iv, iv + m, [](const Interval& a, const Interval& b) { return a.begin < b.begin; });
@@ -299,7 +297,8 @@ int z2z_launch_clip_gradients(z2z_ctx* c, const z2z_gradient* g, int n, float ma
       ClipList l = {};
       long long chunks = 0;
       for (int i = first; i < std::min(n, first + C_LIST); ++i) {
-        if (g[i].n == 0) continue;
+        // (the second launch has nothing to do with a tensor that counts for the norm alone: 4 GiB of them: one workgroup went over their chunks, 37 ms instead of 0.7)
+        if (g[i].n == 0 || (pass == 1 && !g[i].out)) continue;
         const int t = l.tensors++;
         l.data[t] = reinterpret_cast<const unsigned char*>(g[i].data);
         l.out[t] = reinterpret_cast<unsigned char*>(g[i].out);
@@ -313,8 +312,8 @@ int z2z_launch_clip_gradients(z2z_ctx* c, const z2z_gradient* g, int n, float ma
       if (pass == 0) {
         hipLaunchKernelGGL(clip_squares_kernel, dim3(grid), dim3(C_THREADS), 0, s, l, part + parts);
         parts += (int)grid;
-      } else {
-        hipLaunchKernelGGL(clip_scale_kernel, dim3(writes ? grid : 1u), dim3(C_THREADS), 0, s, l, part, parts, max_norm, first == 0 ? norm : nullptr);
+      } else if (l.tensors > 0 || first == 0) {
+        hipLaunchKernelGGL(clip_scale_kernel, dim3(grid), dim3(C_THREADS), 0, s, l, part, parts, max_norm, first == 0 ? norm : nullptr);
       }
     }
   }
