@@ -125,6 +125,7 @@ class Encoder:
                 else:
                     setattr(self._arr[l], name, _ptr(t, torch_dtype if name.startswith("w_") else torch.float32))
         ffn = params.get("ffn")
+        self.ffn = list(ffn) if ffn is not None else []
         self._gated = GatedEncoderDesc()
         self.desc = self._gated.encoder
         self.desc.n_layers = len(layers)
@@ -429,15 +430,21 @@ class Context:
         _check(self._lib.z2z_codebook_reorder(self._h, int(beams), self._own(source, torch.int32), self._own(W_hyper, self.torch_dtype),
                                               _stream()), "z2z_codebook_reorder")
 
+    def _blocks(self, encoder: "Encoder") -> None:
+        for ffn in encoder.ffn:
+            self._block(ffn)
+
     def hyper_encode(self, E: torch.Tensor, encoder: "Encoder", W_hyper: torch.Tensor,
                      first: Optional[torch.Tensor] = None, max_new: int = 0) -> None:
         assert tuple(E.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
+        self._blocks(encoder)
         _check(self._lib.z2z_hyper_encode(self._h, _ptr(E, self.torch_dtype), byref(encoder.desc),
                                           _ptr(W_hyper, self.torch_dtype), _ptr(first, torch.int32), max_new,
                                           _stream()), "z2z_hyper_encode")
 
     def hyper_encode_keep(self, E: torch.Tensor, encoder: "Encoder", W_hyper: torch.Tensor) -> None:
         assert tuple(E.shape) == (self.V, self.d) and tuple(W_hyper.shape) == (self.B, self.cap, self.d)
+        self._blocks(encoder)
         _check(self._lib.z2z_hyper_encode_keep(self._h, _ptr(E, self.torch_dtype), byref(encoder.desc),
                                                _ptr(W_hyper, self.torch_dtype), _stream()), "z2z_hyper_encode_keep")
 
@@ -447,6 +454,10 @@ class Context:
         kept=True: use the rows of the preceding hyper_encode_keep call."""
         assert tuple(E.shape) == (self.V, self.d) and tuple(dW_hyper.shape) == (self.B, self.cap, self.d)
         assert tuple(dE.shape) == (self.V, self.d)
+        self._blocks(encoder)
+        self._blocks(grad)
+        if encoder.ffn and grad.ffn:
+            assert [(g.d_ff, g.desc.group) for g in grad.ffn] == [(f.d_ff, 0) for f in encoder.ffn]
         _check(self._lib.z2z_hyper_encode_backward(self._h, _ptr(E, self.torch_dtype), byref(encoder.desc),
                                                    _ptr(dW_hyper, self.torch_dtype), byref(grad.desc),
                                                    _ptr(dE, torch.float32), ENC_KEPT if kept else 0, _stream()),
