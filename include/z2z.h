@@ -338,16 +338,16 @@ typedef struct z2z_encoder {
   int32_t n_layers;
   int32_t n_heads;
   int32_t d_ff;             /* width of the feed-forward block (ignored when attention_only) */
-  int32_t attention_only;   /* 1: every layer is the attention layer alone, Z2Z_ENC_GATED: see z2z_gated_encoder */
+  int32_t attention_only;   /* not 0: every layer is the attention layer alone, Z2Z_ENC_GATED: see z2z_gated_encoder */
   const void* pos;          /* [M, d] bf16 learned slot positions, or NULL */
   const z2z_encoder_layer* layers;   /* host array of n_layers */
 } z2z_encoder;
 /* Transformer layers with gated feed-forward blocks (z2z_gated_ffn):  Z = Y + block_l(LayerNorm(Y; ln2)).  Every call that takes a z2z_encoder takes the
- * `encoder` of this struct with attention_only = Z2Z_ENC_GATED (a value that it has nowhere else); ffn then has the layers' blocks, and of `encoder` d_ff and of its layers w_1,
+ * `encoder` of this struct with attention_only = Z2Z_ENC_GATED (a value that it has nowhere else: of a plain z2z_encoder nothing behind it is read); ffn then has the layers' blocks, and of `encoder` d_ff and of its layers w_1,
  * b_1, w_2 and b_2 are not read.  Blocks over 4-bit weights serve z2z_hyper_encode; z2z_hyper_encode_keep and z2z_hyper_encode_backward need bf16 (else
  * Z2Z_EUNSUPPORTED), and the latter's `grad` is the `encoder` of such a struct, too: w_1 and w_2 of its blocks receive the matrices' gradients.  All blocks have one d_ff
  * and kept = Z2Z_KEPT_32 (else Z2Z_EINVAL). */
-#define Z2Z_ENC_GATED 2
+#define Z2Z_ENC_GATED 0x5A474646
 typedef struct z2z_gated_encoder {
   z2z_encoder encoder;
   const z2z_ffn* ffn;       /* host array of n_layers */
@@ -363,7 +363,7 @@ int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* encoder, 
  *   grad       a second description with the shape of `encoder` whose pointers name the device buffers that
  *              RECEIVE the gradients (the call writes through them although the struct declares them const):
  *              matrices and pos bf16, vectors float, all overwritten; n_heads, d_ff, attention_only of `grad`
- *              are not read; grad->pos is required when encoder->pos is given
+ *              are not read (of a gated encoder's attention_only is Z2Z_ENC_GATED); grad->pos is required when encoder->pos is given
  *   d_dE       [V, d] float, ACCUMULATED into (tokens recur across entries; the caller clears it)
  *   flags      0, or Z2Z_ENC_KEPT: use the rows the latest z2z_hyper_encode_keep call on this context left
  *              instead of running the forward pass again.  The caller guarantees that d_E's contents and the

@@ -27,7 +27,7 @@ E_INVAL, E_NOMEM, E_HIP, E_UNSUPPORTED, E_LIMIT, E_CAPTURE = -1, -2, -3, -4, -5,
 STATIC_PARTS = 1 << 22
 
 ENC_KEPT = 1
-ENC_GATED = 2
+ENC_GATED = 0x5A474646
 GRAD_ADD = 1
 ACT_SILU, ACT_GELU = 0, 1
 KEPT_32, KEPT_16 = 0, 16

@@ -1075,7 +1075,7 @@ int z2z_launch_hyper_encode_train(z2z_ctx* c, int mode, const void* E, const z2z
   if (cap == 0) return Z2Z_OK;
   if (mode != 0 && (long long)B * cap * M > 65536) return Z2Z_EUNSUPPORTED;
   const int nl = enc->n_layers;
-  const z2z_ffn *gated = z2z_gated_layers(enc), *gated_grad = grad ? z2z_gated_layers(grad) : nullptr;
+  const z2z_ffn *gated = z2z_gated_layers(enc), *gated_grad = gated && grad ? z2z_gated_layers(grad) : nullptr;
   const bool ffn = gated || !enc->attention_only;
   const int dff = gated ? gated[0].d_ff : ffn ? enc->d_ff : 0;
   long long u_step = 65536 / ((long long)B * M);

@@ -316,8 +316,8 @@ int ffn_ok(const z2z_ctx* c, const z2z_ffn* f, bool bf16_only) {
   return Z2Z_OK;
 }
 
-// every pointer a layer of the description must carry, present and 16-byte aligned
-bool encoder_pointers_ok(const z2z_encoder* enc) {
+// every pointer a layer of the description must carry, present and 16-byte aligned; kind: attention_only of the encoder, or of the one whose gradients it names
+bool encoder_pointers_ok(const z2z_encoder* enc, int32_t kind) {
   if (!enc || !enc->layers) return false;
   if (enc->n_layers < 1 || enc->n_layers > Z2Z_MAX_ENCODER_LAYERS) return false;
   if (!aligned16(enc->pos)) return false;
@@ -326,12 +326,12 @@ bool encoder_pointers_ok(const z2z_encoder* enc) {
     const void* always[] = {y.ln1_g, y.ln1_b, y.w_qkv, y.b_qkv, y.w_o, y.b_o};
     for (const void* p : always)
       if (!p || !aligned16(p)) return false;
-    if (enc->attention_only == Z2Z_ENC_GATED) {
+    if (kind == Z2Z_ENC_GATED) {
       const z2z_ffn* f = z2z_gated_layers(enc);
       const void* ffn[] = {y.ln2_g, y.ln2_b, f ? f[l].w_1 : nullptr, f ? f[l].w_2 : nullptr};
       for (const void* p : ffn)
         if (!p || !aligned16(p)) return false;
-    } else if (!enc->attention_only) {
+    } else if (!kind) {
       const void* ffn[] = {y.ln2_g, y.ln2_b, y.w_1, y.b_1, y.w_2, y.b_2};
       for (const void* p : ffn)
         if (!p || !aligned16(p)) return false;
@@ -339,6 +339,8 @@ bool encoder_pointers_ok(const z2z_encoder* enc) {
   }
   return true;
 }
+
+bool encoder_ok(const z2z_encoder* enc) { return enc && encoder_pointers_ok(enc, enc->attention_only); }
 
 // the rest of a description with gated blocks; training: over bf16 weights
 int gated_layers_ok(const z2z_ctx* c, const z2z_encoder* enc, bool training) {
@@ -355,7 +357,7 @@ int gated_layers_ok(const z2z_ctx* c, const z2z_encoder* enc, bool training) {
 
 Z2Z_API int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* enc, void* d_W_hyper,
                              const int32_t* d_first, int32_t max_new, void* stream) {
-  if (!ctx || !d_E || !encoder_pointers_ok(enc)) return Z2Z_EINVAL;
+  if (!ctx || !d_E || !encoder_ok(enc)) return Z2Z_EINVAL;
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
@@ -366,7 +368,7 @@ Z2Z_API int z2z_hyper_encode(z2z_ctx* ctx, const void* d_E, const z2z_encoder* e
 }
 
 Z2Z_API int z2z_hyper_encode_keep(z2z_ctx* ctx, const void* d_E, const z2z_encoder* enc, void* d_W_hyper, void* stream) {
-  if (!ctx || !d_E || !encoder_pointers_ok(enc)) return Z2Z_EINVAL;
+  if (!ctx || !d_E || !encoder_ok(enc)) return Z2Z_EINVAL;
   if (ctx->cfg.cap > 0 && !d_W_hyper) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_W_hyper)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
@@ -379,13 +381,14 @@ Z2Z_API int z2z_hyper_encode_keep(z2z_ctx* ctx, const void* d_E, const z2z_encod
 
 Z2Z_API int z2z_hyper_encode_backward(z2z_ctx* ctx, const void* d_E, const z2z_encoder* enc, const void* d_dW_hyper,
                                       const z2z_encoder* grad, float* d_dE, int32_t flags, void* stream) {
-  if (!ctx || !d_E || !d_dE || !encoder_pointers_ok(enc) || !encoder_pointers_ok(grad)) return Z2Z_EINVAL;
+  if (!ctx || !d_E || !d_dE || !encoder_ok(enc) || !grad) return Z2Z_EINVAL;
+  if (enc->attention_only == Z2Z_ENC_GATED && grad->attention_only != Z2Z_ENC_GATED) return Z2Z_EINVAL;
+  if (!encoder_pointers_ok(grad, enc->attention_only)) return Z2Z_EINVAL;
   if (ctx->cfg.cap > 0 && !d_dW_hyper) return Z2Z_EINVAL;
   if (grad->n_layers != enc->n_layers || (enc->pos && !grad->pos)) return Z2Z_EINVAL;
   if (flags & ~Z2Z_ENC_KEPT) return Z2Z_EINVAL;
   if (!aligned16(d_E) || !aligned16(d_dW_hyper) || !aligned16(d_dE)) return Z2Z_EINVAL;
   if (!z2z_hyper_encode_ok(ctx, enc)) return Z2Z_EUNSUPPORTED;
-  if ((enc->attention_only == Z2Z_ENC_GATED) != (grad->attention_only == Z2Z_ENC_GATED)) return Z2Z_EINVAL;
   const int ok = gated_layers_ok(ctx, enc, true);
   if (ok != Z2Z_OK) return ok;
   note_capture(ctx, static_cast<hipStream_t>(stream));
