@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(64 * W_WAVES, 2) few_rows_kernel(FewArgs a) {
     uint2 s[TILES][SCALES];
     uint4 x[NB][4];
   };
-  // (columns behind the last are zeros of X; what the weights there are read as does not count: a unit's second half may not be there)
+  // (columns behind the last, where a unit's second half is not there: zeros of X, and of bf16 weights before they are multiplied, which may be infinite where they are read)
   auto fetch = [&](Unit& f, int u) __attribute__((always_inline)) {
     const bool whole = (u + 1) * W_UNIT <= a.K;
 #pragma unroll
@@ -118,13 +118,15 @@ __global__ void __launch_bounds__(64 * W_WAVES, 2) few_rows_kernel(FewArgs a) {
   for (int t = 0; t < TILES; ++t)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto compute = [&](const Unit& f) __attribute__((always_inline)) {
+  auto compute = [&](const Unit& f, int u) __attribute__((always_inline)) {
+    const uint32_t second = Q4 || (u + 1) * W_UNIT <= a.K ? 0xFFFFFFFFu : 0u;
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
       f32x4 part[NB];
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        const uint4 v = Q4 ? values_of(word_of(f.w[t][0], m)) : f.w[t][Q4 ? 0 : m];
+        uint4 v = Q4 ? values_of(word_of(f.w[t][0], m)) : f.w[t][Q4 ? 0 : m];
+        if (!Q4 && m >= 2) v = uint4{v.x & second, v.y & second, v.z & second, v.w & second};
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           if (Q4)
@@ -157,7 +159,7 @@ __global__ void __launch_bounds__(64 * W_WAVES, 2) few_rows_kernel(FewArgs a) {
 #pragma unroll
     for (int k = 0; k <= DEPTH; ++k) {
       if (u + k + DEPTH < u1) fetch(f[(k + DEPTH) % (DEPTH + 1)], u + k + DEPTH);
-      if (u + k < u1) compute(f[k]);
+      if (u + k < u1) compute(f[k], u + k);
     }
   }
 
