@@ -256,7 +256,8 @@ int z2z_quantize_q4(z2z_ctx* ctx, const void* d_W, int32_t rows, int32_t cols, i
  *           ffn->kept says in how many bits, and the backward call's says the same: Z2Z_KEPT_32, 4 bytes an element of [rows, 2 f]; Z2Z_KEPT_16, 2 bytes: G and U with 9
  *           bits of fraction (magnitudes from 2^-16 to 2^16; all others with 6), for gradients that are slightly less exact
  * A row's results do not depend on the other rows' values.  rows = 0 is a call that does nothing.  bf16 contexts, d and d_ff multiples of 64 (with 4 bits of group,
- * too), rows <= 2^22, (d_ff + 128) d < 2^30, d_ff < 2^22, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row, and the parts of products that are shared out. */
+ * too), rows <= 2^22, (d_ff + 128) d < 2^30, d_ff < 2^22, else Z2Z_EUNSUPPORTED.  Work space (library scratch): 2 f bytes per row (none with d_kept of
+ * Z2Z_KEPT_32), and the parts of products that are shared out. */
 enum { Z2Z_ACT_SILU = 0, Z2Z_ACT_GELU = 1 };
 enum { Z2Z_KEPT_32 = 0, Z2Z_KEPT_16 = 16 };
 typedef struct z2z_ffn {

@@ -445,8 +445,10 @@ Z2Z_API int z2z_gated_ffn(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2z
   if (clashes(in, 6, out, 2) || overlap_bytes(d_kept, kept, d_residual, row)) return Z2Z_EINVAL;
   rc = enter(ctx, static_cast<hipStream_t>(stream));
   if (rc != Z2Z_OK || rows == 0) return rc;
-  rc = z2z_work_reserve(ctx, &ctx->ffn_ws, z2z_ffn_work(ffn, ctx->cfg.d, rows), static_cast<hipStream_t>(stream));
-  if (rc != Z2Z_OK) return rc;
+  if (!d_kept || ffn->kept != Z2Z_KEPT_32) {       // (else F is a part of what is kept, and weights that would be expanded keep nothing)
+    rc = z2z_work_reserve(ctx, &ctx->ffn_ws, z2z_ffn_work(ffn, ctx->cfg.d, rows), static_cast<hipStream_t>(stream));
+    if (rc != Z2Z_OK) return rc;
+  }
   return z2z_launch_ffn(ctx, d_X, ffn, d_residual, d_Y, false, d_kept, rows, nullptr, ctx->ffn_ws.p, static_cast<hipStream_t>(stream));
 }
 

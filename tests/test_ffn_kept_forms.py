@@ -80,3 +80,22 @@ def test_the_tile_kernel_spills_nothing(tmp_path):
             seen += 1
             assert int(scratch) == 0, name
     assert seen >= 20
+
+
+def test_a_call_that_keeps_its_hidden_layer_takes_no_work_space(without_a_device):
+    without_a_device(BLOCK + """
+used = stub.stub_used()
+stub.stub_capturing(1)
+for rows in (1, 16, 64, 200):                             # (no parts either)
+    assert fwd(h, block(), rows=rows, kept=K) == 0 and len(launches()) == 2, rows
+assert fwd(h, block(), rows=16) == api.E_CAPTURE and launches() == []
+f = block()
+f.kept = api.KEPT_16
+assert fwd(h, f, rows=16, kept=K) == api.E_CAPTURE and launches() == []
+stub.stub_capturing(0)
+assert stub.stub_used() == used
+assert fwd(h, f, rows=16, kept=K) == 0 and stub.stub_used() == used + 16 * 256 * 2
+launches()
+assert fwd(h, block(), rows=200) == 0 and stub.stub_used() == used + 200 * 256 * 2
+clean()
+""")
