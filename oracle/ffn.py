@@ -15,7 +15,7 @@ import numpy as np
 
 HALF_BF16 = 2.0 ** -8                    # half a step of bf16, relative to the value
 HALF_F32 = 2.0 ** -24
-KEPT = 2.0 ** -17
+KEPT = 2.0 ** -16                        # half a step of 15 bits of fraction: a number's upper 24 bits are its sign, 8 of exponent and these
 ACT_ERROR = 1e-6                         # of the activations' and slopes' own arithmetic in float32 (their erf: 1.5e-7; exponentials, reciprocals: a few steps)
 
 _erf = np.vectorize(math.erf, otypes=[np.float64])
@@ -60,7 +60,7 @@ def gated_ffn(X, W1, W2, kind: str, residual=None, round_weights: bool = False, 
     w2 = np.abs(W2).T
     Y_err = F_err @ w2 + _sum_bound(F, W2.T) + (HALF_BF16 * (np.abs(F) @ w2) if round_weights else 0.0)
     Y_bound = (Y_err * 1.02 + HALF_BF16 * (np.abs(Y) + Y_err)) * 1.001 + 1e-30
-    # what the gradient needs: act(G) and U act'(G), which may be stored with 16 bits of fraction
+    # what the gradient needs: act(G) and U act'(G), which may be stored with 15 bits of fraction
     slope = act(G, kind)[1]
     slope_err = 0.8 * g_err + 4 * ACT_ERROR                      # (neither slope changes faster than 0.8)
     a_bound = a_err + KEPT * (np.abs(a) + a_err) + 1e-30

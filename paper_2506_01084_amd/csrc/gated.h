@@ -36,7 +36,7 @@ __device__ __forceinline__ uint2 hidden4(const float (&g)[4], const float (&u)[4
   return pack4(f);
 }
 
-// What the backward pass is given of an element: a = act(G) and s = U act'(G), by which dF is multiplied, with 16 bits of fraction (2^-17 off at most), and F.  Three matrices
+// What the backward pass is given of an element: a = act(G) and s = U act'(G), by which dF is multiplied, with 15 bits of fraction (2^-16 off at most), and F.  Three matrices
 // one behind the other in one buffer of 8 bytes an element: F in bf16, an operand of products in both directions; the upper halves of a and s, 4 bytes; the next
 // bytes of either, 2.  (G and U in bf16 would be half of the gradients' error, 3.5e-3 of their norm instead of 2.3e-3, of which the rounding of what is returned is
 // 1.7e-3.  In fp32 the backward pass's epilogue read and wrote 14 bytes an element, with the matrix cores waiting, instead of 10, and formed exponentials
