@@ -290,7 +290,8 @@ int z2z_gated_ffn_backward(z2z_ctx* ctx, const void* d_X, int32_t rows, const z2
  *              another buffer of as many elements, or NULL (counts for the norm alone).  What is written overlaps no other tensor, nor d_norm
  *              (Z2Z_EINVAL); the same tensor twice, in place, is that, too.
  *   max_norm   >= 0, +inf: nothing is clipped (negative or NaN: Z2Z_EINVAL)
- *   d_norm     [2] float out: norm (an infinity where it is beyond float; c is right all the same), c
+ *   d_norm     [2] float out: norm (an infinity where it is beyond float; c is right all the same), c (below 2^-100 the gradients are multiplied by more of its bits
+ *              than a float that small has)
  * Sums are formed in a fixed order, in 64 bits from pieces of at most 64 squares in 32 (in 64 where those would leave their range): the same inputs give the same
  * bits.  With out = data and c = 1 nothing is written.  Any context; n <= Z2Z_MAX_GRADIENTS, tensors of up to 2^44 elements, else Z2Z_EUNSUPPORTED. */
 #define Z2Z_MAX_GRADIENTS 4096
