@@ -243,7 +243,7 @@ int launch_kmajor(z2z_ctx* c, LogitsArgs& a, bool rows_too, const void* A, int l
   a.row_tiles = batch.n * ((R + 255) / 256);
   a.strip = 1;
   a.n_strips = a.n_vtiles;
-  const unsigned grid = order_dense(c, a, a.d / 64 >= (a.min_saved ? a.min_saved + 4 : kSplitSlabs), s);
+  const unsigned grid = order_dense(c, a, a.d / 64 >= (a.min_saved ? a.min_saved + 4 : kSplitSlabs), s);      // (a part has four slabs at least)
   const int rc = z2z_launch_linear_kmajor(a, rows_too, grid, s);
   return rc == Z2Z_OK && a.split ? z2z_launch_tile_sum(a, s) : rc;
 }
@@ -262,11 +262,9 @@ int z2z_launch_linear_input(z2z_ctx* c, const void* A, int lda, const void* W, i
 }
 
 int z2z_launch_linear_weight(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const int32_t* k_dev,
-                             const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch, z2z_row_sums row_sums,
-                             int min_saved) {
+                             const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch, z2z_row_sums row_sums) {
   LogitsArgs a;
   memset(&a, 0, sizeof(a));
-  a.min_saved = min_saved;
   a.sums = row_sums.sums;
   a.row_slot = row_sums.row_slot;
   a.d = (k_rows + 63) / 64 * 64;

@@ -514,7 +514,7 @@ int z2z_launch_linear(z2z_ctx* c, const void* A, const void* W, const float* bia
 //   z2z_launch_linear_weight   out[R, N] = A[k_rows, R]^T . W[k_rows, N] + residual;  with k_dev only the first *k_dev rows exist
 // A batch of them: outputs of R rows below each other, W (and the second's A) batch_w (batch_a) elements apart.
 // stream_f32 as in LogitsArgs: a sum of several products is rounded once.  The second adds row_sums where they are given.  min_saved: a cut along K (LogitsArgs::split)
-// is made from so many slabs saved on, 0: 16, and of contractions of 32 and more.
+// is made from so many slabs saved on, and of contractions of four slabs more (0: 16 saved, contractions of 32 and more).
 struct z2z_linear_batch {
   int n;
   size_t a, w;
@@ -528,7 +528,7 @@ int z2z_launch_linear_input(z2z_ctx* c, const void* A, int lda, const void* W, i
                             int min_saved = 0);
 int z2z_launch_linear_weight(z2z_ctx* c, const void* A, int lda, const void* W, int ldw, int k_rows, const int32_t* k_dev,
                              const void* residual, void* out, int R, int N, hipStream_t s, z2z_linear_batch batch = {1, 0, 0},
-                             z2z_row_sums row_sums = {nullptr, nullptr}, int min_saved = 0);
+                             z2z_row_sums row_sums = {nullptr, nullptr});
 // Row pitch for n columns of an activation that is an operand of dense layers: n, or 64 more where n columns are a
 // multiple of 4 KiB -- the tile kernel's workgroups read the same slab of 256 rows at a time, and rows that far apart
 // on a power of two put it on a few memory channels (35400 rows x 4096 columns, K = 16384: 1.07 -> 1.18
