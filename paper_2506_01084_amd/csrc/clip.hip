@@ -11,6 +11,7 @@
 
 namespace {
 
+using z2z_logits::load_if;
 using z2z_logits::pack_bf16;
 
 constexpr int C_THREADS = 256;
@@ -30,13 +31,6 @@ static_assert(sizeof(ClipList) <= 3800, "kernel arguments are 4 KiB at most");
 
 // Bytes ahead of the first 16-byte boundary; chunks are cut from there on, and the first takes these along.
 __host__ __device__ __forceinline__ int head_bytes(const void* p) { return (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15); }
-
-// *p, or zeros.  (A choice between two vectors would be made between their addresses.)
-__device__ __forceinline__ uint4 load_if(bool ok, const uint4* p) {
-  uint4 v = {0u, 0u, 0u, 0u};
-  if (ok) v = *p;
-  return v;
-}
 
 __device__ __forceinline__ int tensor_of(const ClipList& l, int chunk) {
   int lo = 0, hi = l.tensors - 1;

@@ -8,13 +8,16 @@
 #include "few_rows.h"
 
 #include "gated.h"
+#include "q4.h"
 
 #include <algorithm>
 
 namespace {
 
-using z2z_logits::bf16x8;
 using z2z_logits::f32x4;
+using z2z_logits::load_if;
+using z2z_q4::mfma;
+using z2z_q4::values_of;
 
 constexpr int W_UNIT = 128;              // columns
 
@@ -30,23 +33,6 @@ struct FewArgs {
   int32_t act, f32;
 };
 
-__device__ __forceinline__ uint4 load_if(bool ok, const uint4* p) {
-  uint4 v = {0u, 0u, 0u, 0u};
-  if (ok) v = *p;
-  return v;
-}
-
-__device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// The eight values of a word of 4-bit weights.
-__device__ __forceinline__ uint4 values_of(uint32_t w) {
-  return uint4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3))};
-}
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int m) { return m == 0 ? v.x : m == 1 ? v.y : m == 2 ? v.z : v.w; }
 
 // WAVES: of a workgroup, that share K out.  CHAIN: 0 = bf16 weights, else 4 bits with a scale per CHAIN matrix instructions (of 32 columns); TILES: tiles of 16 weight rows; NB: blocks of 16 rows of X.

@@ -28,6 +28,7 @@
 namespace {
 
 using z2z_logits::bf16_bits_rne;
+using z2z_logits::load_if;
 
 constexpr int E_KCH = 8;             // 16-byte chunks per lane of one row: d <= 64 * 8 * E_KCH = 4096
 constexpr float E_EPS = 1e-5f;
@@ -51,14 +52,6 @@ __device__ __forceinline__ int entry_of(const RowMap& m, int b, int u, int* C_ou
   *C_out = C;
   const int base = m.first ? max(m.first[b], 0) : (m.last_n > 0 ? max(C - m.last_n, 0) : 0);
   return base + m.u0 + u;
-}
-
-// *p, or zeros.  (A choice between two vectors, `ok ? *p : zero`, is made between their addresses: a flat load, and scratch memory
-// for the zeros.)
-__device__ __forceinline__ uint4 load_if(bool ok, const uint4* p) {
-  uint4 v = {0u, 0u, 0u, 0u};
-  if (ok) v = *p;
-  return v;
 }
 
 __device__ __forceinline__ void unpack8(const uint4& x, float (&f)[8]) {

@@ -85,6 +85,14 @@ __device__ __forceinline__ void merge_draw(Draw& a, const Draw& b) {
   if (b.v > a.v || (b.v == a.v && b.i < a.i)) a = b;
 }
 
+// *p, or zeros.  (A choice between two vectors, `ok ? *p : zero`, is made between their addresses: a flat load, and scratch memory
+// for the zeros.)
+__device__ __forceinline__ uint4 load_if(bool ok, const uint4* p) {
+  uint4 v = {0u, 0u, 0u, 0u};
+  if (ok) v = *p;
+  return v;
+}
+
 // One accumulator element, AGPR -> VGPR.  Spelled as an instruction so that the accumulators stay in
 // the accumulation registers and are fetched block by block: left to itself the compiler copies the whole
 // accumulator tile into VGPRs at the end of the K loop, and what that displaces is spilled inside the loop.

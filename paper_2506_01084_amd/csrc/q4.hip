@@ -7,29 +7,18 @@
 // two bf16, exactly; the products of a group are summed in fp32, and the scale multiplies the sum: nothing is rounded but sums.  (Whole numbers q - 8 made as 128 + q in
 // bf16, with 136 times the sum of the rows' values taken off again, cost as much and leave the rounding of sums 136 times as large.)
 // Rows beyond the last whole block of columns are filled up with zeros.
-#include "logits_common.h"
+#include "q4.h"
 
 #include <algorithm>
 
 namespace {
 
-using z2z_logits::bf16x8;
 using z2z_logits::bf16_bits_rne;
 using z2z_logits::f32x4;
+using z2z_q4::mfma;
+using z2z_q4::values_of;
 
 constexpr int Q_BLOCK = 128;             // columns of a block
-
-// The eight values of a word.
-__device__ __forceinline__ uint4 values_of(uint32_t w) {
-  return uint4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3))};
-}
-
-__device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
 
 // ---- bf16 -> 4 bits: a wave per block --------------------------------------------------------------------------------------------
 // scale = largest magnitude of the group / 6, rounded to bf16; v = the nearest to w / scale, of two as near the one whose code is even.  (Where that changes is
