@@ -43,13 +43,11 @@ def _steps(x):
 SHAPES = [(1, 64, 64), (16, 512, 128), (33, 128, 320), (65, 192, 192), (237, 1024, 448), (40, 8192, 5504), (1031, 3520, 1792), (16411, 512, 1344), (3000, 128, 704), (300, 6400, 3456)]
 
 
-@pytest.mark.parametrize("rows,d,f", SHAPES)
-@pytest.mark.parametrize("act", ["silu", "gelu"])
+# (one activation is enough of the largest)
+@pytest.mark.parametrize("rows,d,f,act", [(*shape, act) for act in ("silu", "gelu") for shape in SHAPES if act == "gelu" or np.prod(shape, dtype=float) <= 2.0 ** 32])
 def test_gradient(rows, d, f, act):
     from paper_2506_01084_amd import api
 
-    if rows * d * f > 1 << 32 and act == "silu":
-        pytest.skip("one activation is enough of the largest")
     X, W1, W2, R, dY = _tensors(rows, d, f, rows + d + f)
     ctx, block = _context(d), api.GatedFFN(W1, W2, act=act)
     Y, without = torch.full_like(X, float("nan")), torch.full_like(X, float("nan"))
